@@ -462,6 +462,120 @@ int            cerar_set_kernel_mode(cerar_plan_t* plan, int mode);
  * Returns 0, or -1 for an unknown name. */
 int            cerar_set_tuning(const char* name, int value);
 
+/* ---- Operators of the training step around the aggregation ----
+ *
+ * A data-parallel step makes the weight gradients (products of a layer's activations and of the
+ * gradients of its outputs), aggregates them (the calls above), and applies them (norm, clip, optimizer).
+ * The calls below are the two outer parts.  (The paper has no counterpart; it reduces gradients that a
+ * bfloat16 / binary32 training loop hands it, Sec. IV and its appendix on the training runs.)
+ *
+ * Every call takes a cerar_ops_t of the current device: it owns the status word that kernels with bounded
+ * waits report through, and counts launches.  The rules are those of the data path: the caller owns every
+ * buffer, calls are asynchronous on `stream`, allocate nothing, and report argument and launch errors;
+ * nothing throws.  Calls on one handle from several host threads are serialised by the caller; the
+ * operators of one handle may run on several streams at a time, except the calls on ONE cerar_tensors_t. */
+typedef struct cerar_ops cerar_ops_t;            /* opaque, library-owned */
+typedef struct cerar_tensors cerar_tensors_t;    /* opaque, library-owned */
+
+typedef enum { CERAR_TYPE_F32 = 0, CERAR_TYPE_BF16 = 1 } cerar_type_t;
+
+cerar_status_t cerar_ops_create(cerar_ops_t** out);     /* CERAR_ERR_CUDA without a device */
+void           cerar_ops_destroy(cerar_ops_t* ops);
+/* Synchronises `stream`; CERAR_ERR_TIMEOUT if a kernel gave up on a bounded wait since the last check. */
+cerar_status_t cerar_ops_status(cerar_ops_t* ops, cerar_stream_t stream);
+uint64_t       cerar_ops_launch_count(const cerar_ops_t* ops);
+
+/* A matrix in 8 bits: row-major e4m3 codes (4 exponent bits with bias 7, 3 mantissa bits, no infinities,
+ * largest value 448; the format of the 8-bit messages above) and binary32 scales, one for every 128 values.
+ * The value at (r, c) is code(r, c) times
+ *     CERAR_BY_ROW     scales[(c / 128) * lds + r]            lds >= rows    128 columns of one row
+ *     CERAR_BY_COLUMN  scales[(r / 128) * lds + c]            lds >= cols    128 rows of one column
+ *     CERAR_BY_BLOCK   scales[(r / 128) * lds + c / 128]      lds >= ceil(cols / 128)
+ * codes start on a 16-byte boundary and ld (bytes between rows, >= cols) is a multiple of 16: what
+ * tensor-map copies need.  Nothing between cols and ld is read for its value or written. */
+typedef enum { CERAR_BY_ROW = 0, CERAR_BY_COLUMN = 1, CERAR_BY_BLOCK = 2 } cerar_scaling_t;
+typedef struct {
+    uint8_t* codes;
+    float*   scales;
+    int64_t  rows, cols, ld, lds;
+    int32_t  scaling;            /* cerar_scaling_t */
+} cerar_fp8_matrix_t;
+
+/* Converts x (rows x cols of `type`, ldx elements between rows) into `count` (1..3) 8-bit matrices of the
+ * same size and different scalings, reading x once.  Scale: 2^e with the smallest integer e that brings the
+ * largest finite magnitude of the block to 448 or below, kept within [-100, 100]; 1 for a block of zeros.
+ * Code: x 2^-e rounded to nearest, ties to even; NaN and infinities become NaN. */
+cerar_status_t cerar_fp8_quantize(cerar_ops_t* ops, const void* x, cerar_type_t type, int64_t ldx,
+                                  const cerar_fp8_matrix_t* out, int count, cerar_stream_t stream);
+
+/* C (M x N of `type`, ldc elements between rows) = op(A) op(B), or C + op(A) op(B) with accumulate != 0;
+ * op is the matrix itself or, with trans_* != 0, its transpose.  The scales run along the summed
+ * dimension or in blocks: op(A) = A wants A by row or by block, op(A) = A^T by column or by block;
+ * op(B) = B wants B by column or by block, op(B) = B^T by row or by block.  Any finite scales.
+ *     C[m,n] (+)= sum_b sA(m,b) sB(b,n) sum_{k in block b} A[m,k] B[k,n]
+ * The inner sums run on the tensor cores, the outer one in binary32; one rounding to `type` at the end.
+ * A linear layer with weights W (outputs x inputs): Y = X W^T, dX = dY W, dW += dY^T X.
+ * Deterministic: the same operands give the same bits. */
+cerar_status_t cerar_fp8_matmul(cerar_ops_t* ops, const cerar_fp8_matrix_t* A, int trans_a,
+                                const cerar_fp8_matrix_t* B, int trans_b, void* C, cerar_type_t type,
+                                int64_t ldc, int accumulate, cerar_stream_t stream);
+
+/* A set of parameter tensors with their gradients and optimizer states, described once (the table is
+ * copied to the device) and then used by one launch, or a few, per call however many tensors there are.
+ * All pointers are device memory aligned to their elements; 16-byte alignment (and 4 bytes for the 8-bit
+ * states) is faster.  Sizes of zero are allowed. */
+#define CERAR_STATE_BLOCK 256
+typedef struct {
+    int64_t  numel;
+    void*    param;              /* of param_type; NULL in a set that is only used for its norm               */
+    float*   master;             /* binary32 copy that the step updates; param receives it rounded to nearest.
+                                    NULL: the step updates param itself (bfloat16: rounded stochastically)    */
+    void*    grad;               /* of grad_type, read only                                                   */
+    void*    m;                  /* first moment: numel floats, or numel e4m3 codes (8-bit states)            */
+    void*    v;                  /* second moment: numel floats, or numel e4m3 codes of its square root       */
+    float*   m_scale;            /* 8-bit states: one scale per CERAR_STATE_BLOCK elements, ceil(numel / 256) */
+    float*   v_scale;
+    float    lr_scale;           /* factor on the step's learning rate                                        */
+    float    weight_decay;
+    int32_t  param_type, grad_type;   /* cerar_type_t */
+} cerar_tensor_t;
+
+/* state_bits: 32, 8, or 0 (no states: the set serves cerar_grad_norm only, param / m / v are ignored). */
+cerar_status_t cerar_tensors_create(cerar_ops_t* ops, int64_t count, const cerar_tensor_t* tensors, int state_bits,
+                                    cerar_tensors_t** out);
+void           cerar_tensors_destroy(cerar_tensors_t* set);
+/* Points the set at other gradients (count pointers, same sizes and types); takes effect in stream order. */
+cerar_status_t cerar_tensors_set_grads(cerar_tensors_t* set, void* const* grads, cerar_stream_t stream);
+
+/* clip[0] = 2-norm of all gradients of the set, clip[1] = min(1, max_norm / (norm + 1e-6)) (1 for
+ * max_norm <= 0: no clipping), clip[2] = 1 if the norm is finite, else 0 (and clip[1] = 0).  clip: three floats
+ * of device memory.  Partial sums in binary64, added in a fixed order; no intermediate overflow or
+ * underflow: the result is finite exactly if all gradients are and the norm is below 3.4e38. */
+cerar_status_t cerar_grad_norm(cerar_tensors_t* set, float max_norm, float* clip, cerar_stream_t stream);
+
+/* One AdamW step (decoupled weight decay) over the set:
+ *     g1 = clip[1] g;  m1 = beta1 m + (1 - beta1) g1;  v1 = beta2 v + (1 - beta2) g1^2
+ *     p1 = p (1 - lr weight_decay) - lr / (1 - beta1^step) m1 / (sqrt(v1 / (1 - beta2^step)) + eps)
+ * with lr times the tensor's lr_scale; 1 - beta and the step's corrections are derived in binary64 and rounded
+ * once, all arithmetic on elements is binary32.  clip: what cerar_grad_norm wrote (device),
+ * or NULL for no clipping; where clip[2] is 0 the call changes nothing.  step counts from 1.
+ * 8-bit states: m and sqrt(v) are kept as e4m3 codes with one power-of-two scale (as in cerar_fp8_quantize)
+ * per 256 consecutive elements of a tensor, rounded up or down at random with the probabilities that make
+ * the kept value right on average: rounding to nearest would not move at all where a step changes a
+ * moment by less than half the distance of two codes (6 %), which (1 - beta) does.  A root above zero is
+ * never rounded to zero.  The kept root carries noise of about 4 % per step, which averages out over 1 / (1 - beta2)
+ * steps of memory to 4 % / sqrt(1 - beta2^2): 12 % at beta2 = 0.95, but over 80 % at 0.999, where states in
+ * 32 bits are the better choice.  The random bits are a function of `seed`, the element's place in the set and
+ * nothing else: give every step another seed, or the same one to repeat a step bit for bit.
+ * NaN: an element whose gradient is not finite (without a clip that skips the step) ends as NaN. */
+typedef struct {
+    double   lr, beta1, beta2, eps;
+    int64_t  step;
+    uint64_t seed;
+} cerar_adamw_options_t;
+cerar_status_t cerar_adamw_step(cerar_tensors_t* set, const cerar_adamw_options_t* opt, const float* clip,
+                                cerar_stream_t stream);
+
 const char*    cerar_status_string(cerar_status_t s);
 const char*    cerar_last_error(void);   /* thread-local detail of the last failure */
 

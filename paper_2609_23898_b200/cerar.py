@@ -47,6 +47,22 @@ class Counters(C.Structure):
                 ("bytes_stored_per_worker", C.c_uint64), ("bytes_gradient", C.c_uint64)]
 
 
+class Fp8Matrix(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ld", C.c_int64), ("lds", C.c_int64), ("scaling", C.c_int32)]
+
+
+class TensorDesc(C.Structure):
+    _fields_ = [("numel", C.c_int64), ("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p),
+                ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("lr_scale", C.c_float), ("weight_decay", C.c_float), ("param_type", C.c_int32), ("grad_type", C.c_int32)]
+
+
+class AdamwOptions(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("step", C.c_int64), ("seed", C.c_uint64)]
+
+
 def _load() -> C.CDLL:
     # CERAR_LIBRARY=checked selects the build whose kernels check every address they form (tests)
     checked = os.environ.get("CERAR_LIBRARY", "") == "checked"
@@ -111,6 +127,21 @@ lib.cerar_set_kernel_mode.argtypes = [_vp, C.c_int]
 lib.cerar_device_status.argtypes = [_vp, _vp]
 lib.cerar_selftest_wait_timeout.argtypes = [_vp, C.c_int, _vp]
 lib.cerar_set_tuning.argtypes = [C.c_char_p, C.c_int]
+lib.cerar_ops_create.argtypes = [C.POINTER(_vp)]
+lib.cerar_ops_destroy.argtypes = [_vp]
+lib.cerar_ops_destroy.restype = None
+lib.cerar_ops_status.argtypes = [_vp, _vp]
+lib.cerar_ops_launch_count.argtypes = [_vp]
+lib.cerar_ops_launch_count.restype = C.c_uint64
+lib.cerar_fp8_quantize.argtypes = [_vp, _vp, C.c_int, _i64, C.POINTER(Fp8Matrix), C.c_int, _vp]
+lib.cerar_fp8_matmul.argtypes = [_vp, C.POINTER(Fp8Matrix), C.c_int, C.POINTER(Fp8Matrix), C.c_int, _vp, C.c_int, _i64,
+                                 C.c_int, _vp]
+lib.cerar_tensors_create.argtypes = [_vp, _i64, C.POINTER(TensorDesc), C.c_int, C.POINTER(_vp)]
+lib.cerar_tensors_destroy.argtypes = [_vp]
+lib.cerar_tensors_destroy.restype = None
+lib.cerar_tensors_set_grads.argtypes = [_vp, C.POINTER(_vp), _vp]
+lib.cerar_grad_norm.argtypes = [_vp, C.c_float, _vp, _vp]
+lib.cerar_adamw_step.argtypes = [_vp, C.POINTER(AdamwOptions), _vp, _vp]
 lib.cerar_status_string.argtypes = [C.c_int]
 lib.cerar_status_string.restype = C.c_char_p
 lib.cerar_last_error.restype = C.c_char_p

@@ -1,0 +1,355 @@
+// Gradient norm and AdamW over a set of tensors (cerar_grad_norm, cerar_adamw_step).
+//
+// Both are one pass over memory: the norm reads every gradient once (4 or 2 bytes per element), the step reads and writes each
+// parameter and state once.  A set is cut into chunks of 2048 elements of one tensor each, in one list for all tensors, so one
+// launch serves hundreds of tensors and every SM has work whatever their sizes; blocks take chunks in turn.
+//
+// In a chunk warp w owns the 256 elements 256 w .. 256 w + 255: lane l has elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3 of
+// them, so every access of a warp is contiguous, and the 256 elements that share a scale of the 8-bit states belong to one warp.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <type_traits>
+
+#include "kernels.cuh"
+#include "ops.cuh"
+#include "ptx.cuh"
+
+namespace cerar {
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int PER_WARP = CERAR_STATE_BLOCK;
+static_assert(CHUNK == (THREADS / 32) * PER_WARP, "one state block per warp and chunk");
+
+// n (1..4) consecutive elements as binary32, the rest zero; vec: all four exist and are aligned
+__device__ __forceinline__ void load4(float* x, const float* p, int n, bool vec) {
+    if (vec) {
+        const float4 v = __ldcs(reinterpret_cast<const float4*>(p));
+        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = j < n ? __ldcs(p + j) : 0.f;
+    }
+}
+__device__ __forceinline__ void load4(float* x, const __nv_bfloat16* p, int n, bool vec) {
+    if (vec) {
+        const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p));
+        x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+        x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = j < n ? __bfloat162float(p[j]) : 0.f;
+    }
+}
+__device__ __forceinline__ void store4(float* p, const float* x, int n, bool vec) {
+    if (vec) {
+        __stcs(reinterpret_cast<float4*>(p), make_float4(x[0], x[1], x[2], x[3]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (j < n) p[j] = x[j];
+    }
+}
+__device__ __forceinline__ void store4_bf16(__nv_bfloat16* p, const uint32_t* b, int n, bool vec) {   // b: 16-bit patterns
+    if (vec) {
+        __stcs(reinterpret_cast<uint2*>(p), make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16)));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (j < n) reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)b[j];
+    }
+}
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int n, bool vec) {
+    if (vec) return __ldcs(reinterpret_cast<const uint32_t*>(p));
+    uint32_t v = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) if (j < n) v |= (uint32_t)p[j] << (8 * j);
+    return v;
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, uint32_t v, int n, bool vec) {
+    if (vec) { __stcs(reinterpret_cast<uint32_t*>(p), v); return; }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) if (j < n) p[j] = (uint8_t)(v >> (8 * j));
+}
+__device__ __forceinline__ bool aligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+// ---------------------------------------------------------------- gradient norm
+
+__device__ __forceinline__ double block_sum(double s, double* sh) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) s += sh[w];
+    __syncthreads();
+    return s;
+}
+
+// Squares are summed eight at a time in binary32 and from there in binary64.  A group whose sum leaves the range where
+// binary32 squares are good (overflow, underflow, NaN) is done again in binary64 from the registers.
+__device__ __forceinline__ double sum8(const float* x) {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fmaf(x[j], x[j], s);
+    if (s > 1e-25f && s < 1e37f) return (double)s;
+    double d = 0.0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) d = fma((double)x[j], (double)x[j], d);
+    return d;
+}
+
+__global__ void __launch_bounds__(THREADS) grad_norm_kernel(const __grid_constant__ NormArgs a) {
+    __shared__ double sh[THREADS / 32];
+    __shared__ bool last;
+    ptx::grid_dependency_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    double sum = 0.0;
+    for (int64_t c = blockIdx.x; c < a.nchunks; c += gridDim.x) {
+        const ChunkRef ref = a.chunks[c];
+        const TensorRec& t = a.tensors[ref.tensor];
+        const int64_t e0 = (int64_t)ref.index * CHUNK + warp * PER_WARP + 4 * lane;
+        const int64_t left = t.numel - e0;
+        const int n0 = left >= 4 ? 4 : (int)max((int64_t)0, left), n1 = left >= 132 ? 4 : (int)max((int64_t)0, left - 128);
+        float x[8];
+        if (t.grad_type == CERAR_TYPE_F32) {
+            const float* g = static_cast<const float*>(t.grad) + e0;
+            const bool al = aligned(t.grad, 16);
+            load4(x, g, n0, al && n0 == 4);
+            load4(x + 4, g + 128, n1, al && n1 == 4);
+        } else {
+            const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(t.grad) + e0;
+            const bool al = aligned(t.grad, 8);
+            load4(x, g, n0, al && n0 == 4);
+            load4(x + 4, g + 128, n1, al && n1 == 4);
+        }
+        sum += sum8(x);
+    }
+    sum = block_sum(sum, sh);
+    // the block that arrives last adds the partial sums of all blocks, in their order
+    if (threadIdx.x == 0) {
+        a.partial[blockIdx.x] = sum;
+        __threadfence();
+        last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double s = 0.0;
+    for (unsigned b = threadIdx.x; b < gridDim.x; b += THREADS) s += __ldcg(a.partial + b);
+    s = block_sum(s, sh);
+    if (threadIdx.x == 0) {
+        const float norm = (float)sqrt(s);
+        const bool finite = norm <= 3.4028234e38f;                     // false for NaN too
+        a.clip[0] = norm;
+        a.clip[1] = !finite ? 0.f : a.max_norm > 0.f ? fminf(1.f, a.max_norm / (norm + 1e-6f)) : 1.f;
+        a.clip[2] = finite ? 1.f : 0.f;
+        *a.ticket = 0u;
+    }
+}
+
+// ---------------------------------------------------------------- AdamW
+
+__device__ __forceinline__ uint32_t scramble(uint32_t h) {             // multiply and xor-shift rounds: every input bit reaches every output bit
+    h = (h ^ (h >> 16)) * 0x7FEB352Du;
+    h = (h ^ (h >> 15)) * 0x846CA68Bu;
+    return h ^ (h >> 16);
+}
+// random bits of a state block; element i of it then uses scramble(key + i * 0x9E3779B9)
+__device__ __forceinline__ uint32_t block_key(int64_t block, uint64_t seed, uint32_t stream) {
+    return scramble((uint32_t)block * 0x9E3779B1u + ((uint32_t)(block >> 32) + 1u) * 0x7FEB352Du + (uint32_t)seed * 0x85157AF5u +
+                    (uint32_t)(seed >> 32) * 0xC2B2AE35u + stream * 0x632BE5ABu);
+}
+__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Value of an e4m3 code: shifted to the binary32 exponent and mantissa it is the value times 2^-120, subnormals included.
+__device__ __forceinline__ float code_value(uint32_t code) {
+    const float mag = __uint_as_float((code & 0x7Fu) << 20) * 0x1p120f;
+    const float v = (code & 0x7Fu) == 0x7Fu ? __uint_as_float(0x7FC00000u) : mag;
+    return __uint_as_float(__float_as_uint(v) | ((code & 0x80u) << 24));
+}
+// Code of y, |y| <= 448, rounded away from zero with the probability of the part that is cut off: times 2^-120 the code is the
+// top of the binary32 number, and 16 random bits (plus half of their last place) are added to the 20 bits below it.
+__device__ __forceinline__ uint32_t random_code(float y, uint32_t bits16) {
+    const uint32_t b = __float_as_uint(y), sign = (b >> 24) & 0x80u;
+    if ((b & 0x7FFFFFFFu) >= 0x7F800000u) return sign | 0x7Fu;
+    const uint32_t c = (__float_as_uint(fabsf(y) * 0x1p-120f) + ((bits16 << 4) + 8u)) >> 20;
+    return sign | min(c, 0x7Eu);
+}
+__device__ __forceinline__ uint32_t finite_magnitude(float x) {
+    const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
+    return b < 0x7F800000u ? b : 0u;
+}
+
+template <int PK, typename G, int BITS>
+__device__ __forceinline__ void adamw_warp(const AdamwArgs& a, const TensorRec& t, int64_t e0 /* first element of the warp's block */, float coef,
+                                           bool vec, bool gvec) {
+    const int lane = threadIdx.x & 31;
+    const int64_t left = t.numel - e0 - 4 * lane;
+    const int n0 = left >= 4 ? 4 : (int)max((int64_t)0, left), n1 = left >= 132 ? 4 : (int)max((int64_t)0, left - 128);
+    const int64_t i0 = e0 + 4 * lane, i1 = i0 + 128;
+    const bool v0 = vec && n0 == 4, v1 = vec && n1 == 4, g0 = gvec && n0 == 4, g1 = gvec && n1 == 4;
+    float g[8], p[8], m[8], v[8];
+    uint32_t mc[2], vc[2];
+    float msc = 0.f, vsc = 0.f;
+    const G* gp = static_cast<const G*>(t.grad);
+    load4(g, gp + i0, n0, g0);
+    load4(g + 4, gp + i1, n1, g1);
+    if constexpr (PK == PARAM_BF16) {
+        const __nv_bfloat16* pp = static_cast<const __nv_bfloat16*>(t.param);
+        load4(p, pp + i0, n0, v0);
+        load4(p + 4, pp + i1, n1, v1);
+    } else {
+        const float* pp = PK == PARAM_MASTER ? t.master : static_cast<const float*>(t.param);
+        load4(p, pp + i0, n0, v0);
+        load4(p + 4, pp + i1, n1, v1);
+    }
+    if constexpr (BITS == 32) {
+        load4(m, static_cast<const float*>(t.m) + i0, n0, v0);
+        load4(m + 4, static_cast<const float*>(t.m) + i1, n1, v1);
+        load4(v, static_cast<const float*>(t.v) + i0, n0, v0);
+        load4(v + 4, static_cast<const float*>(t.v) + i1, n1, v1);
+    } else {
+        mc[0] = load_codes(static_cast<const uint8_t*>(t.m) + i0, n0, v0);
+        mc[1] = load_codes(static_cast<const uint8_t*>(t.m) + i1, n1, v1);
+        vc[0] = load_codes(static_cast<const uint8_t*>(t.v) + i0, n0, v0);
+        vc[1] = load_codes(static_cast<const uint8_t*>(t.v) + i1, n1, v1);
+        msc = t.m_scale[e0 / PER_WARP];
+        vsc = t.v_scale[e0 / PER_WARP];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            m[j] = code_value((mc[j >> 2] >> (8 * (j & 3))) & 0xFFu) * msc;
+            const float r = code_value((vc[j >> 2] >> (8 * (j & 3))) & 0xFFu) * vsc;
+            v[j] = __fmul_rn(r, r);
+        }
+    }
+    const float step = a.step_size * t.lr_scale, keep = 1.f - a.lr * t.lr_scale * t.weight_decay;
+    float r[8];
+    uint32_t mmax = 0u, rmax = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        // each product and sum rounded by itself (no contraction), as the formula is written
+        const float gc = __fmul_rn(g[j], coef);
+        m[j] = __fadd_rn(__fmul_rn(m[j], a.beta1), __fmul_rn(gc, a.one_minus_beta1));
+        v[j] = __fadd_rn(__fmul_rn(v[j], a.beta2), __fmul_rn(__fmul_rn(gc, gc), a.one_minus_beta2));
+        r[j] = __fsqrt_rn(v[j]);
+        p[j] = fmaf(-step, __fdividef(m[j], fmaf(r[j], a.root_scale, a.eps)), p[j] * keep);
+        if constexpr (BITS == 8) { mmax = max(mmax, finite_magnitude(m[j])); rmax = max(rmax, finite_magnitude(r[j])); }
+    }
+    if constexpr (BITS == 32) {
+        store4(static_cast<float*>(t.m) + i0, m, n0, v0);
+        store4(static_cast<float*>(t.m) + i1, m + 4, n1, v1);
+        store4(static_cast<float*>(t.v) + i0, v, n0, v0);
+        store4(static_cast<float*>(t.v) + i1, v + 4, n1, v1);
+    } else {
+        const int em = fp8_scale_exponent(__reduce_max_sync(0xffffffffu, mmax));
+        const int er = fp8_scale_exponent(__reduce_max_sync(0xffffffffu, rmax));
+        const float im = pow2f(-em), ir = pow2f(-er);
+        const uint32_t key = block_key(t.block0 + e0 / PER_WARP, a.seed, 0u);
+        mc[0] = mc[1] = vc[0] = vc[1] = 0u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t h = scramble(key + (uint32_t)((j >> 2) * 128 + 4 * lane + (j & 3)) * 0x9E3779B9u);
+            mc[j >> 2] |= random_code(m[j] * im, h >> 16) << (8 * (j & 3));
+            uint32_t c = random_code(r[j] * ir, h & 0xFFFFu);
+            if (r[j] > 0.f) c = max(c, 1u);
+            vc[j >> 2] |= c << (8 * (j & 3));
+        }
+        store_codes(static_cast<uint8_t*>(t.m) + i0, mc[0], n0, v0);
+        store_codes(static_cast<uint8_t*>(t.m) + i1, mc[1], n1, v1);
+        store_codes(static_cast<uint8_t*>(t.v) + i0, vc[0], n0, v0);
+        store_codes(static_cast<uint8_t*>(t.v) + i1, vc[1], n1, v1);
+        if (lane == 0) { t.m_scale[e0 / PER_WARP] = pow2f(em); t.v_scale[e0 / PER_WARP] = pow2f(er); }
+    }
+    if constexpr (PK == PARAM_F32 || PK == PARAM_MASTER) {
+        float* pp = PK == PARAM_MASTER ? t.master : static_cast<float*>(t.param);
+        store4(pp + i0, p, n0, v0);
+        store4(pp + i1, p + 4, n1, v1);
+    }
+    if constexpr (PK == PARAM_MASTER || PK == PARAM_BF16) {
+        // the copy is rounded to nearest; a parameter without one is rounded up or down at random, since a step is far
+        // smaller than the distance of two bfloat16 numbers (0.4 %) and rounding to nearest would lose it every time
+        const uint32_t key = PK == PARAM_BF16 ? block_key(t.block0 + e0 / PER_WARP, a.seed, 1u) : 0u;
+        uint32_t b[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (PK == PARAM_MASTER) {
+                b[j] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(p[j]));
+            } else {
+                const uint32_t h = scramble(key + (uint32_t)((j >> 2) * 128 + 4 * lane + (j & 3)) * 0x9E3779B9u);
+                const uint32_t u = __float_as_uint(p[j]);
+                b[j] = (u & 0x7FFFFFFFu) >= 0x7F800000u ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(p[j])) : (u + (h >> 16)) >> 16;
+            }
+        }
+        __nv_bfloat16* pp = static_cast<__nv_bfloat16*>(t.param);
+        store4_bf16(pp + i0, b, n0, v0);
+        store4_bf16(pp + i1, b + 4, n1, v1);
+    }
+}
+
+template <int PK, typename G, int BITS>
+__global__ void __launch_bounds__(THREADS, 4) adamw_kernel(const __grid_constant__ AdamwArgs a) {
+    ptx::grid_dependency_wait();
+    float coef = 1.f;
+    if (a.clip) {
+        if (a.clip[2] == 0.f) return;
+        coef = a.clip[1];
+    }
+    const int warp = threadIdx.x >> 5;
+    for (int64_t c = blockIdx.x; c < a.nchunks; c += gridDim.x) {
+        const ChunkRef ref = a.chunks[c];
+        const TensorRec t = a.tensors[ref.tensor];
+        const int64_t e0 = (int64_t)ref.index * CHUNK + warp * PER_WARP;
+        if (e0 >= t.numel) continue;
+        bool vec = BITS == 32 ? aligned(t.m, 16) && aligned(t.v, 16) : aligned(t.m, 4) && aligned(t.v, 4);
+        if (PK == PARAM_F32) vec = vec && aligned(t.param, 16);
+        else vec = vec && aligned(t.param, 8) && (PK != PARAM_MASTER || aligned(t.master, 16));
+        adamw_warp<PK, G, BITS>(a, t, e0, coef, vec, aligned(t.grad, 4 * sizeof(G)));
+    }
+}
+
+struct GradPointers { void* p[SET_GRADS_MAX]; };
+__global__ void set_grads_kernel(TensorRec* tensors, int64_t first, int count, const __grid_constant__ GradPointers g) {
+    ptx::grid_dependency_wait();
+    if ((int)threadIdx.x < count) tensors[first + threadIdx.x].grad = g.p[threadIdx.x];
+}
+
+template <int PK, typename G, int BITS>
+cudaError_t launch_kind(const AdamwArgs& a, int num_sms, cudaStream_t s) {
+    int64_t blocks = a.nchunks < (int64_t)num_sms * 4 ? a.nchunks : (int64_t)num_sms * 4;
+    return launch_pdl(adamw_kernel<PK, G, BITS>, dim3((unsigned)blocks), dim3(THREADS), 0, s, a);
+}
+template <int PK>
+cudaError_t launch_types(const AdamwArgs& a, int grad_type, int bits, int num_sms, cudaStream_t s) {
+    if (grad_type == CERAR_TYPE_F32)
+        return bits == 32 ? launch_kind<PK, float, 32>(a, num_sms, s) : launch_kind<PK, float, 8>(a, num_sms, s);
+    return bits == 32 ? launch_kind<PK, __nv_bfloat16, 32>(a, num_sms, s) : launch_kind<PK, __nv_bfloat16, 8>(a, num_sms, s);
+}
+
+}  // namespace
+
+cudaError_t launch_grad_norm(const NormArgs& a, int blocks, cudaStream_t s, uint64_t* launches) {
+    const cudaError_t e = launch_pdl(grad_norm_kernel, dim3((unsigned)blocks), dim3(THREADS), 0, s, a);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
+cudaError_t launch_adamw(const AdamwArgs& a, int param_kind, int grad_type, int state_bits, int num_sms, cudaStream_t s,
+                         uint64_t* launches) {
+    if (a.nchunks == 0) return cudaSuccess;
+    const cudaError_t e = param_kind == PARAM_F32    ? launch_types<PARAM_F32>(a, grad_type, state_bits, num_sms, s)
+                          : param_kind == PARAM_BF16 ? launch_types<PARAM_BF16>(a, grad_type, state_bits, num_sms, s)
+                                                     : launch_types<PARAM_MASTER>(a, grad_type, state_bits, num_sms, s);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
+cudaError_t launch_set_grads(TensorRec* tensors, int64_t first, int count, void* const* grads, cudaStream_t s, uint64_t* launches) {
+    GradPointers g = {};
+    for (int i = 0; i < count; ++i) g.p[i] = grads[i];
+    const cudaError_t e = launch_pdl(set_grads_kernel, dim3(1), dim3(SET_GRADS_MAX), 0, s, tensors, first, count, g);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
+}  // namespace cerar

@@ -1,0 +1,314 @@
+"""Operators of the training step around the aggregation, on torch tensors.
+
+A data-parallel step makes the weight gradients, aggregates them (`cerar.Plan`) and applies them.  This module is
+the two outer parts:
+
+  Ops.quantize, Ops.matmul   products in 8-bit floating point with a scale per 128 values (cerar_fp8_quantize, cerar_fp8_matmul)
+  linear, linear_backward, Linear8   a linear layer made of them; the weight gradient is added to a binary32 buffer of the
+                             caller's (a slice of the vector that is aggregated)
+  TensorSet.grad_norm        norm and clip coefficient of many gradients (cerar_grad_norm)
+  TensorSet.adamw            AdamW over many tensors, states in 32 or 8 bits (cerar_adamw_step)
+
+Everything runs on the current stream of the current device, without synchronisation.  The formulas, formats and rules
+stand in include/cerar.h.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import cerar
+from .cerar import CerarError, Fp8Matrix, lib
+
+BY_ROW, BY_COLUMN, BY_BLOCK = 0, 1, 2
+BLOCK = 128            # values that share a scale of an 8-bit matrix
+STATE_BLOCK = 256      # elements that share a scale of an 8-bit optimizer state
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+_check = cerar._check
+
+
+def _stream() -> int:
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{what}: float32 or bfloat16 wanted, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _matrix(t: torch.Tensor, what: str) -> torch.Tensor:
+    """A two-dimensional device tensor whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what}: a two-dimensional CUDA tensor is wanted")
+    if t.stride(1) != 1 and t.size(1) > 1 or t.stride(0) < t.size(1) and t.size(0) > 1:
+        raise ValueError(f"{what}: elements of a row must be contiguous and rows must not overlap")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Elements between rows (a tensor of one row may carry any stride)."""
+    return t.stride(0) if t.size(0) > 1 else max(t.stride(0), t.size(1))
+
+
+class Quantized:
+    """An 8-bit matrix: `codes` (rows x cols, float8_e4m3fn or uint8, rows a multiple of 16 bytes apart), `scales` (float32,
+    [ceil(cols/128), rows] by row, [ceil(rows/128), cols] by column, [ceil(rows/128), ceil(cols/128)] by block)."""
+
+    __slots__ = ("codes", "scales", "scaling", "desc")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, scaling: int):
+        if codes.element_size() != 1:
+            raise TypeError("codes: float8_e4m3fn or uint8 wanted")
+        _matrix(codes, "codes"), _matrix(scales, "scales")
+        if scales.dtype != torch.float32 or scales.device != codes.device:
+            raise TypeError("scales: float32 on the device of the codes wanted")
+        rows, cols = codes.shape
+        nr, nc = -(-rows // BLOCK), -(-cols // BLOCK)
+        want = {BY_ROW: (nc, rows), BY_COLUMN: (nr, cols), BY_BLOCK: (nr, nc)}.get(scaling)
+        if want is None:
+            raise ValueError("scaling must be BY_ROW, BY_COLUMN or BY_BLOCK")
+        if tuple(scales.shape) != want:
+            raise ValueError(f"scales of shape {want} wanted, got {tuple(scales.shape)}")
+        ld = codes.stride(0) if rows > 1 else -(-max(codes.stride(0), cols) // 16) * 16
+        self._set(codes, scales, scaling, rows, cols, ld, _ld(scales))
+
+    def _set(self, codes, scales, scaling, rows, cols, ld, lds):
+        self.codes, self.scales, self.scaling = codes, scales, scaling
+        self.desc = Fp8Matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, lds, scaling)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, scaling: int, device) -> "Quantized":
+        ld = -(-cols // 16) * 16
+        nr, nc = -(-rows // BLOCK), -(-cols // BLOCK)
+        shape = (nc, rows) if scaling == BY_ROW else (nr, cols) if scaling == BY_COLUMN else (nr, nc)
+        codes = torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=device)
+        q = cls.__new__(cls)
+        q._set(codes if ld == cols else codes[:, :cols], torch.empty(shape, dtype=torch.float32, device=device), scaling, rows, cols, ld, shape[1])
+        return q
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    def dequantize(self) -> torch.Tensor:
+        """The values in float32 (for inspection; torch operations)."""
+        r, c = self.codes.shape
+        s = self.scales.t() if self.scaling == BY_ROW else self.scales
+        if self.scaling != BY_ROW:
+            s = s.repeat_interleave(BLOCK, 0)[:r]
+        if self.scaling != BY_COLUMN:
+            s = s.repeat_interleave(BLOCK, 1)[:, :c]
+        return self.codes.view(torch.float8_e4m3fn).float() * s
+
+
+class Ops:
+    """Owns a cerar_ops_t of the current device."""
+
+    def __init__(self):
+        out = C.c_void_p()
+        _check(lib.cerar_ops_create(C.byref(out)))
+        self._h = out
+
+    def destroy(self):
+        if self._h:
+            lib.cerar_ops_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def status(self):
+        """Waits for the current stream; raises if a kernel gave up on a bounded wait."""
+        _check(lib.cerar_ops_status(self._h, _stream()))
+
+    def launch_count(self) -> int:
+        return lib.cerar_ops_launch_count(self._h)
+
+    def quantize(self, x: torch.Tensor, *scalings: int):
+        """8-bit matrices of x, one for each of `scalings` (BY_ROW, BY_COLUMN, BY_BLOCK), from one reading of x."""
+        t = _type(x, "x")
+        _matrix(x, "x")
+        rows, cols = x.shape
+        out = [Quantized.empty(rows, cols, s, x.device) for s in scalings]
+        arr = (Fp8Matrix * len(out))(*[q.desc for q in out])
+        _check(lib.cerar_fp8_quantize(self._h, x.data_ptr(), t, _ld(x), arr, len(out), _stream()))
+        return out
+
+    def matmul(self, a: Quantized, b: Quantized, *, trans_a=False, trans_b=False, out: torch.Tensor | None = None,
+               dtype: torch.dtype = torch.bfloat16, accumulate=False) -> torch.Tensor:
+        """op(a) op(b), into `out` if given (added to it with accumulate)."""
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate wants an `out` to add to")
+            out = torch.empty((a.desc.cols if trans_a else a.desc.rows, b.desc.rows if trans_b else b.desc.cols), dtype=dtype,
+                              device=a.codes.device)
+        else:
+            _matrix(out, "out")
+            want = (a.desc.cols if trans_a else a.desc.rows, b.desc.rows if trans_b else b.desc.cols)
+            if tuple(out.shape) != want:
+                raise ValueError(f"out of shape {want} wanted, got {tuple(out.shape)}")
+        _check(lib.cerar_fp8_matmul(self._h, a.desc, trans_a, b.desc, trans_b, out.data_ptr(), _type(out, "out"), _ld(out), accumulate, _stream()))
+        return out
+
+
+# ------------------------------------------------------------------------------------------------ a linear layer
+
+
+def linear(ops: Ops, x: torch.Tensor, w: Quantized):
+    """y = x w^T for x (tokens x inputs) and weights quantized by block.  Returns (y, what linear_backward wants of x)."""
+    xr, xc = ops.quantize(x, BY_ROW, BY_COLUMN)
+    return ops.matmul(xr, w, trans_b=True, dtype=x.dtype), xc
+
+
+def linear_backward(ops: Ops, dy: torch.Tensor, xc: Quantized, w: Quantized, dw: torch.Tensor | None, *, accumulate=True, need_dx=True):
+    """dx = dy w, and dw (outputs x inputs, float32 or bfloat16, e.g. a slice of the gradient vector) += dy^T x."""
+    if dw is None:
+        dr, = ops.quantize(dy, BY_ROW)
+    elif need_dx:
+        dr, dc = ops.quantize(dy, BY_ROW, BY_COLUMN)
+    else:
+        dc, = ops.quantize(dy, BY_COLUMN)
+    if dw is not None:
+        ops.matmul(dc, xc, trans_a=True, out=dw, accumulate=accumulate)
+    return ops.matmul(dr, w, dtype=dy.dtype) if need_dx else None
+
+
+class Linear8(torch.autograd.Function):
+    """linear and linear_backward for torch.autograd: y = Linear8.apply(x, w, ops, dw).  w: quantized weights (no gradient of
+    their own: it is added to `dw`, which may be None)."""
+
+    @staticmethod
+    def forward(ctx, x, w, ops, dw):
+        x2 = x.reshape(-1, x.shape[-1])
+        y, xc = linear(ops, x2, w)
+        ctx.ops, ctx.w, ctx.dw, ctx.xc = ops, w, dw, xc
+        return y.view(*x.shape[:-1], y.shape[-1])
+
+    @staticmethod
+    def backward(ctx, dy):
+        d2 = dy.reshape(-1, dy.shape[-1])
+        dx = linear_backward(ctx.ops, d2, ctx.xc, ctx.w, ctx.dw, need_dx=ctx.needs_input_grad[0])
+        return None if dx is None else dx.view(*dy.shape[:-1], dx.shape[-1]), None, None, None
+
+
+# ------------------------------------------------------------------------------------------------ norm and optimizer
+
+
+def _flat(tensors, what, n=None, device=None):
+    tensors = list(tensors)
+    for t in tensors:
+        if not t.is_cuda or not t.is_contiguous() or (device is not None and t.device != device):
+            raise ValueError(f"{what}: contiguous tensors on one CUDA device are wanted")
+    if n is not None and [t.numel() for t in tensors] != n:
+        raise ValueError(f"{what}: the sizes differ from the gradients'")
+    return tensors
+
+
+class TensorSet:
+    """Parameters, gradients and optimizer states of a step (cerar_tensors_t).
+
+    grads              tensors of float32 or bfloat16, e.g. views into the aggregated vector
+    params, masters    the parameters (float32 or bfloat16), and for bfloat16 ones optional float32 copies
+    state_bits         32 or 8; with no params the set serves grad_norm only
+    m, v               states of all tensors in one flat tensor each (zeros are made where none are given), tensor i at
+                       state_offsets[i]: float32 of both moments, or e4m3 codes of the first moment and of the second one's
+                       root with m_scale, v_scale, one float32 per 256 elements.  Every tensor starts at a multiple of 256.
+    weight_decay, lr_scale   one number, or one for each tensor
+    """
+
+    def __init__(self, ops: Ops, grads, params=None, masters=None, *, state_bits=32, m=None, v=None, m_scale=None, v_scale=None,
+                 weight_decay=0.0, lr_scale=1.0):
+        grads = _flat(grads, "grads")
+        n = [t.numel() for t in grads]
+        dev = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
+        _flat(grads, "grads", device=dev)
+        self.ops, self.grads = ops, grads
+        self.params = None if params is None else _flat(params, "params", n, dev)
+        self.masters = None if masters is None else _flat(masters, "masters", n, dev)
+        if self.masters is not None and any(t.dtype != torch.float32 for t in self.masters):
+            raise TypeError("masters: float32 wanted")
+        self.state_bits = state_bits if params is not None else 0
+        self.state_offsets = [0]
+        for k in n:
+            self.state_offsets.append(self.state_offsets[-1] + -(-k // STATE_BLOCK) * STATE_BLOCK)
+        total = self.state_offsets[-1]
+        if self.state_bits:
+            if state_bits not in (8, 32):
+                raise ValueError("state_bits must be 8 or 32")
+            dt = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+
+            def state(t, size, dtype, fill=0):
+                if t is None:
+                    return torch.full((size,), fill, dtype=torch.uint8, device=dev).view(dtype) if dtype.itemsize == 1 else \
+                        torch.full((size,), fill, dtype=dtype, device=dev)
+                if t.device != dev or not t.is_contiguous() or t.numel() != size or t.element_size() != dtype.itemsize or \
+                        (dtype.itemsize == 4 and t.dtype != dtype):
+                    raise ValueError(f"state: {size} contiguous values of {dtype} on {dev} wanted")
+                return t
+
+            self.m, self.v = state(m, total, dt), state(v, total, dt)
+            if state_bits == 8:
+                self.m_scale = state(m_scale, total // STATE_BLOCK, torch.float32, 1)
+                self.v_scale = state(v_scale, total // STATE_BLOCK, torch.float32, 1)
+        wd = list(weight_decay) if hasattr(weight_decay, "__iter__") else [weight_decay] * len(n)
+        lr = list(lr_scale) if hasattr(lr_scale, "__iter__") else [lr_scale] * len(n)
+        if len(wd) != len(n) or len(lr) != len(n):
+            raise ValueError("weight_decay and lr_scale: one number, or one for each tensor")
+        desc = (cerar.TensorDesc * len(n))()
+        for i, k in enumerate(n):
+            d = desc[i]
+            d.numel, d.grad, d.grad_type = k, grads[i].data_ptr(), _type(grads[i], "grads")
+            if self.state_bits:
+                at, size = self.state_offsets[i], state_bits // 8
+                d.param, d.param_type = self.params[i].data_ptr(), _type(self.params[i], "params")
+                d.master = None if self.masters is None else self.masters[i].data_ptr()
+                d.m, d.v = self.m.data_ptr() + at * size, self.v.data_ptr() + at * size
+                if state_bits == 8:
+                    d.m_scale = self.m_scale.data_ptr() + at // STATE_BLOCK * 4
+                    d.v_scale = self.v_scale.data_ptr() + at // STATE_BLOCK * 4
+                d.lr_scale, d.weight_decay = lr[i], wd[i]
+        out = C.c_void_p()
+        _check(lib.cerar_tensors_create(ops._h, len(n), desc, self.state_bits, C.byref(out)))
+        self._h = out
+        self._opt = cerar.AdamwOptions()
+
+    def destroy(self):
+        if getattr(self, "_h", None):
+            lib.cerar_tensors_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def set_grads(self, grads):
+        """Points the set at other gradients of the same sizes and types, in stream order."""
+        grads = _flat(grads, "grads", [t.numel() for t in self.grads], self.grads[0].device if self.grads else None)
+        if any(a.dtype != b.dtype for a, b in zip(grads, self.grads)):
+            raise TypeError("grads: the types differ from those the set was made with")
+        _check(lib.cerar_tensors_set_grads(self._h, (C.c_void_p * len(grads))(*[t.data_ptr() for t in grads]), _stream()))
+        self.grads = grads
+
+    def grad_norm(self, max_norm: float = 0.0, out: torch.Tensor | None = None) -> torch.Tensor:
+        """[norm, clip coefficient, 1 if finite] on the device; the third argument of a step that skips itself otherwise."""
+        if out is None:
+            out = torch.empty(3, dtype=torch.float32, device="cuda")
+        _check(lib.cerar_grad_norm(self._h, max_norm, out.data_ptr(), _stream()))
+        return out
+
+    def adamw(self, *, lr: float, betas=(0.9, 0.95), eps: float = 1e-8, step: int, clip: torch.Tensor | None = None, seed: int = 0):
+        """One AdamW step, in place.  clip: what grad_norm returned; seed: of the random rounding (8-bit states, bfloat16
+        parameters without masters), another one for every step."""
+        o = self._opt
+        o.lr, o.beta1, o.beta2, o.eps, o.step, o.seed = lr, betas[0], betas[1], eps, step, seed
+        if clip is not None and (clip.dtype != torch.float32 or clip.numel() != 3 or not clip.is_cuda or not clip.is_contiguous()):
+            raise ValueError("clip: the three floats that grad_norm returned are wanted")
+        _check(lib.cerar_adamw_step(self._h, o, None if clip is None else clip.data_ptr(), _stream()))
