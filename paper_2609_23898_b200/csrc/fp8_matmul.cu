@@ -1,84 +1,492 @@
-// Product of two 8-bit matrices with a scale per 128 values along the summed dimension (cerar_fp8_matmul).
+// Product of two 8-bit matrices with a scale per 128 values along the summed dimension (cerar_fp8_matmul; sm_100a:
+// TMA + tcgen05 + TMEM).
+//
+//   C[m,n] (+)= sum_b sA(m,b) sB(b,n) P_b[m,n],     P_b[m,n] = sum_{k in block b} A[m,k] B[k,n]
+//
+// P_b is four tcgen05.mma kind::f8f6f4 (128 x BN x 32) into tensor memory.  The scales differ from block to block, so P_b is
+// taken out after every block, multiplied by its scales and added to the running sum in registers (binary32), while the
+// tensor core works on the next block in the other half of tensor memory.  At 128 x 256 x 128 the products take 512 clk; taking
+// them out is 256 columns per warp quadrant (256 clk) and 64 packed multiply-adds per warp (twice that with a scale per
+// column of B), done by two warps per quadrant.
+//
+// Operands come in as tiles of 128 bytes of one dimension by 128 (or BN) of the other, in the 128-byte swizzle that the
+// tensor core reads, whichever dimension is contiguous in memory: a transposed operand is read in place (the "MN-major" form).
+//
+//   warp 0     producer: TMA loads of the stages
+//   warp 1     issues the products; owns the tensor memory
+//   warps 4-11 take the partial products out, scale, add; write the tile of C.  Warp w reads lanes 32 (w % 4) .. of tensor memory; the
+//              two warps of a quadrant share the columns.  A warp writes C through 4 KB of shared memory of its own, so
+//              that rows leave in 128-byte pieces; the products of the next tile go on meanwhile.
+// (Warps 2, 3 only complete the warpgroup that hands most of its registers to the other two: 128 sums per thread need more than
+// the 168 of an even share.)
+//
+// Few tiles, long sums: a cluster of S blocks shares a tile, each sums 1/S of the blocks of k, and the partial tiles are added
+// through distributed shared memory, in a fixed order.
+// Every wait is bounded; one that runs out sets the status word and the block leaves through the common exit.
+#include <cuda.h>
 #include <cuda_bf16.h>
-#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
 #include "kernels.cuh"
 #include "ops.cuh"
-#include "ptx.cuh"
+#include "tc_common.cuh"
 
 namespace cerar {
 namespace {
 
-// operand as op(X)[row][k] with row = m or n: codes at row * rs + k * ks, scale of (row, block b) at (row / rd) * srs + b * sbs
-struct Operand {
-    const uint8_t* codes;
-    const float* scales;
-    int64_t rs, ks, srs, sbs;
-    int rd;
+using namespace tc;
+
+constexpr int BM = 128, BK = FP8_BLOCK;
+constexpr int EPI_WARPS = 8, WARP_EPI0 = 4;
+// registers per thread: 128 x 56 + 256 x 224 = 384 x 168, what the block is launched with
+constexpr int REGS_FEW = 56, REGS_MANY = 224;
+constexpr int THREADS = 32 * (WARP_EPI0 + EPI_WARPS);
+constexpr uint32_t A_BYTES = BM * BK;
+constexpr uint32_t STAGING = 32 * 128;                 // per epilogue warp: 32 rows of 128 bytes; the column scales of B before that
+
+// scale of (row or column i, block b) at scales[(i / div) * si + b * sb]
+struct Scales {
+    const float* p;
+    int64_t si, sb;
+    int shift;                                         // div = 1 << shift (1 or 128)
 };
-__device__ __forceinline__ float value(uint8_t c) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3))); }
+struct Params {
+    Scales sa, sb;
+    void* C;
+    int64_t ldc;
+    int M, N, kblocks;
+    int tiles_m, tiles_n, group_m;
+    int64_t tiles;
+    int a_mn, b_mn;                                    // 1: the operand's own dimension (m or n) is the contiguous one
+    int accumulate, c_vec;
+    int stages, split;
+    int* status;
+};
 
-constexpr int TM = 64, TN = 64, TK = 32;
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                 " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Shared-memory descriptor of a tile in the 128-byte swizzle.  Summed dimension contiguous: rows of 128 bytes, groups of 8 rows
+// 1024 bytes apart.  The other dimension contiguous: groups of 8 k 1024 bytes apart, blocks of 128 rows or columns 16 KB apart.
+__device__ __forceinline__ uint64_t swizzled_desc(uint32_t saddr) {
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)((BK * 128u) >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 |
+           (uint64_t)1 << 46 /* sm_100 descriptor */ | (uint64_t)2 << 61 /* 128-byte swizzle */;
+}
+// two sums at a time (one instruction): a += x * y
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void fma_pair(uint64_t& a, uint64_t x, uint64_t y) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(a) : "l"(x), "l"(y)); }
+__device__ __forceinline__ uint64_t mul_pair(uint64_t x, uint64_t y) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t saddr, uint32_t rank) {
+    uint32_t ra;
+    float4 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(saddr), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(ra) : "memory");
+    return v;
+}
 
+// tile number -> (row tile, column tile): column by column inside bands of group_m row tiles, so that the tiles that run at the
+// same time share operand tiles in L2
+__device__ __forceinline__ void tile_of(const Params& p, int64_t t, int& tm, int& tn) {
+    const int64_t per_band = (int64_t)p.group_m * p.tiles_n;
+    const int band = (int)(t / per_band);
+    const int first = band * p.group_m;
+    const int rows = p.tiles_m - first < p.group_m ? p.tiles_m - first : p.group_m;
+    const int r = (int)(t - band * per_band);
+    tm = first + r % rows;
+    tn = r / rows;
+}
+
+template <typename C> struct Out;
+template <> struct Out<float> {
+    static constexpr int PER16 = 4;                    // elements in 16 bytes
+    static __device__ __forceinline__ uint4 pack(const float* v) {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+};
+template <> struct Out<__nv_bfloat16> {
+    static constexpr int PER16 = 8;
+    static __device__ __forceinline__ uint32_t two(float a, float b) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ uint4 pack(const float* v) { return make_uint4(two(v[0], v[1]), two(v[2], v[3]), two(v[4], v[5]), two(v[6], v[7])); }
+};
+
+// Rows row0 .. row0 + 31 (those below M) of C, columns col0 .. col0 + n - 1 of a slab of 128 bytes per row: the warp holds row
+// (lane)'s values in v[0 .. SLAB).  With accumulate the slab of C is read and added in binary32 before the one rounding.
 template <typename C>
-__global__ void __launch_bounds__(256) fp8_matmul_kernel(const __grid_constant__ Operand A, const __grid_constant__ Operand B, C* c, int64_t ldc,
-                                                         int64_t M, int64_t N, int64_t K, int accumulate) {
-    __shared__ float as[TK][TM + 1], bs[TK][TN + 1];
-    ptx::grid_dependency_wait();
-    const int64_t m0 = (int64_t)blockIdx.y * TM, n0 = (int64_t)blockIdx.x * TN;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {}, part[4][4] = {};
-    for (int64_t k0 = 0; k0 < K; k0 += TK) {
-        for (int i = threadIdx.x; i < TM * TK; i += 256) {
-            const int r = i / TK, k = i % TK;
-            as[k][r] = m0 + r < M && k0 + k < K ? value(A.codes[(m0 + r) * A.rs + (k0 + k) * A.ks]) : 0.f;
-            bs[k][r] = n0 + r < N && k0 + k < K ? value(B.codes[(n0 + r) * B.rs + (k0 + k) * B.ks]) : 0.f;
+__device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, int row0, int col0, const float* v) {
+    constexpr int PER16 = Out<C>::PER16, SLAB = 8 * PER16;
+    const int lane = threadIdx.x & 31;
+    const int nrows = p.M - row0 < 32 ? p.M - row0 : 32, n = p.N - col0 < SLAB ? p.N - col0 : SLAB;
+    if (nrows <= 0 || n <= 0) return;
+    C* c = static_cast<C*>(p.C);
+    __syncwarp();
+    if (!p.accumulate) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint4 q = Out<C>::pack(v + j * PER16);
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
         }
-        __syncthreads();
-        for (int k = 0; k < TK; ++k)
-            for (int i = 0; i < 4; ++i)
-                for (int j = 0; j < 4; ++j) part[i][j] = fmaf(as[k][ty * 4 + i], bs[k][tx * 4 + j], part[i][j]);
-        __syncthreads();
-        if ((k0 + TK) % FP8_BLOCK == 0 || k0 + TK >= K) {
-            const int64_t b = k0 / FP8_BLOCK;
-            for (int i = 0; i < 4; ++i)
-                for (int j = 0; j < 4; ++j) {
-                    const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j;
-                    if (m < M && n < N)
-                        acc[i][j] = fmaf(A.scales[m / A.rd * A.srs + b * A.sbs] * part[i][j], B.scales[n / B.rd * B.srs + b * B.sbs], acc[i][j]);
-                    part[i][j] = 0.f;
+        __syncwarp();
+        if (p.c_vec && n == SLAB) {
+#pragma unroll
+            for (int it = 0; it < 8; ++it) {
+                const int r = it * 4 + (lane >> 3), j = lane & 7;
+                uint4 q;
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
+                if (r < nrows) *reinterpret_cast<uint4*>(c + (int64_t)(row0 + r) * p.ldc + col0 + j * PER16) = q;
+            }
+        } else {
+            for (int r = 0; r < nrows; ++r)
+                for (int e = lane; e < n; e += 32) {
+                    const uint32_t at = staging + r * 128 + (((e / PER16) ^ (r & 7)) << 4) + (e % PER16) * sizeof(C);
+                    C* dst = c + (int64_t)(row0 + r) * p.ldc + col0 + e;
+                    if constexpr (sizeof(C) == 4) {
+                        float q;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(q) : "r"(at) : "memory");
+                        *dst = q;
+                    } else {
+                        uint16_t q;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(q) : "r"(at) : "memory");
+                        *reinterpret_cast<uint16_t*>(dst) = q;
+                    }
                 }
         }
-    }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j;
-            if (m >= M || n >= N) continue;
-            C& dst = c[m * ldc + n];
-            dst = (C)(accumulate ? (float)dst + acc[i][j] : acc[i][j]);
+    } else {
+        // binary32 through the staging rows, 32 columns at a time
+#pragma unroll
+        for (int h = 0; h < SLAB / 32; ++h) {
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((j ^ (lane & 7)) << 4)), "f"(v[h * 32 + 4 * j]), "f"(v[h * 32 + 4 * j + 1]),
+                             "f"(v[h * 32 + 4 * j + 2]), "f"(v[h * 32 + 4 * j + 3]) : "memory");
+            __syncwarp();
+            if (p.c_vec && n == SLAB) {
+#pragma unroll
+                for (int it = 0; it < 8; ++it) {
+                    const int r = it * 4 + (lane >> 3), j = lane & 7;
+                    float4 q;
+                    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
+                    if (r < nrows) {
+                        C* dst = c + (int64_t)(row0 + r) * p.ldc + col0 + h * 32 + j * 4;
+                        if constexpr (sizeof(C) == 4) {
+                            const float4 o = *reinterpret_cast<const float4*>(dst);
+                            *reinterpret_cast<float4*>(dst) = make_float4(o.x + q.x, o.y + q.y, o.z + q.z, o.w + q.w);
+                        } else {
+                            const uint2 o = *reinterpret_cast<const uint2*>(dst);
+                            *reinterpret_cast<uint2*>(dst) = make_uint2(
+                                Out<C>::two(__uint_as_float(o.x << 16) + q.x, __uint_as_float(o.x & 0xFFFF0000u) + q.y),
+                                Out<C>::two(__uint_as_float(o.y << 16) + q.z, __uint_as_float(o.y & 0xFFFF0000u) + q.w));
+                        }
+                    }
+                }
+            } else {
+                const int e = h * 32 + lane;
+                for (int r = 0; r < nrows; ++r) {
+                    float q;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(q) : "r"(staging + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
+                    if (e < n) {
+                        C* dst = c + (int64_t)(row0 + r) * p.ldc + col0 + e;
+                        *dst = (C)((float)*dst + q);
+                    }
+                }
+            }
         }
+    }
+}
+
+// BVEC: a scale per column of B (otherwise one for the warp's columns, which lie in one block)
+template <int BN, bool BVEC, typename C>
+__global__ void __launch_bounds__(THREADS, 1)
+fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Params p) {
+    constexpr int CW = BN / 2;                          // columns of a tile per epilogue warp
+    constexpr uint32_t B_BYTES = BN * BK, STAGE = A_BYTES + B_BYTES;
+    constexpr int NBUF = 512 / BN;                      // partial products in tensor memory
+    extern __shared__ unsigned char smem_dyn[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    const uint32_t staging0 = smem + (uint32_t)p.stages * STAGE;
+    const uint32_t bars = staging0 + EPI_WARPS * STAGING;
+    const uint32_t full = bars, empty = full + 8u * p.stages, acc_full = empty + 8u * p.stages, acc_empty = acc_full + 8u * NBUF;
+    const uint32_t slot = acc_empty + 8u * NBUF;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8u * s, 1); mbar_init(empty + 8u * s, 1); }
+        for (int b = 0; b < NBUF; ++b) { mbar_init(acc_full + 8u * b, 1); mbar_init(acc_empty + 8u * b, EPI_WARPS); }
+        mbar_init_fence();
+    }
+    if (warp == 1) tc_alloc(slot, 512u);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    grid_dependency_wait();
+
+    const int rank = p.split > 1 ? (int)cluster_rank() : 0;
+    const int64_t t0 = blockIdx.x / p.split, tstep = gridDim.x / p.split;
+    const int kb0 = (int)((int64_t)p.kblocks * rank / p.split), kb1 = (int)((int64_t)p.kblocks * (rank + 1) / p.split);
+    bool failed = false;
+
+    if (warp < WARP_EPI0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
+        if (warp == 0) {
+            if (lane == 0) {
+                uint32_t it = 0;
+                for (int64_t t = t0; t < p.tiles && !failed; t += tstep) {
+                    int tm, tn;
+                    tile_of(p, t, tm, tn);
+                    const int m0 = tm * BM, n0 = tn * BN;
+                    for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                        const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u;
+                        if (!mbar_wait_bounded(empty + 8u * s, ph ^ 1u)) { failed = true; break; }
+                        const uint32_t a = smem + s * STAGE, b = a + A_BYTES, bar = full + 8u * s;
+                        mbar_arrive_expect_tx(bar, STAGE);
+                        if (p.a_mn) tma_load_2d(a, &map_a, m0, kb * BK, bar);
+                        else tma_load_2d(a, &map_a, kb * BK, m0, bar);
+                        if (p.b_mn) {
+    #pragma unroll
+                            for (int j = 0; j < BN / 128; ++j) tma_load_2d(b + j * (128 * BK), &map_b, n0 + j * 128, kb * BK, bar);
+                        } else {
+                            tma_load_2d(b, &map_b, kb * BK, n0, bar);
+                        }
+                    }
+                }
+            }
+        } else if (warp == 1) {
+            if (lane == 0) {
+                // D binary32, A and B e4m3, M = 128, N = BN
+                const uint32_t idesc = (1u << 4) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) | ((128u >> 4) << 24);
+                // 32 values of k further: 32 bytes in a row of k, or 32 rows of 128 bytes
+                const uint64_t a_step = p.a_mn ? (32u * 128u) >> 4 : 32u >> 4, b_step = p.b_mn ? (32u * 128u) >> 4 : 32u >> 4;
+                uint32_t it = 0;
+                for (int64_t t = t0; t < p.tiles && !failed; t += tstep)
+                    for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                        const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u, buf = it % NBUF, bph = (it / NBUF) & 1u;
+                        if (!mbar_wait_bounded(acc_empty + 8u * buf, bph ^ 1u) || !mbar_wait_bounded(full + 8u * s, ph)) { failed = true; break; }
+                        tc_fence_after();
+                        const uint64_t da = swizzled_desc(smem + s * STAGE), db = swizzled_desc(smem + s * STAGE + A_BYTES);
+    #pragma unroll
+                        for (int k = 0; k < BK / 32; ++k) mma_f8(tmem + buf * BN, da + k * a_step, db + k * b_step, idesc, k != 0);
+                        tc_commit(empty + 8u * s);
+                        tc_commit(acc_full + 8u * buf);
+                    }
+            }
+        }
+        __syncwarp();
+        if (p.split > 1) { cluster_sync(); cluster_sync(); }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY));
+        const int quad = warp & 3, half = (warp - WARP_EPI0) >> 2;
+        const uint32_t staging = staging0 + (uint32_t)(warp - WARP_EPI0) * STAGING;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        uint32_t it = 0;
+        for (int64_t t = t0; t < p.tiles && !failed; t += tstep) {
+            int tm, tn;
+            tile_of(p, t, tm, tn);
+            const int row = tm * BM + quad * 32 + lane, col0 = tn * BN + half * CW;
+            // scales of this row and of these columns; rows and columns beyond the matrix use the last one's (their sums are not stored)
+            const float* sa = p.sa.p + (int64_t)((row < p.M ? row : p.M - 1) >> p.sa.shift) * p.sa.si;
+            const float* sb = p.sb.p + (int64_t)((col0 < p.N ? col0 : p.N - 1) >> p.sb.shift) * p.sb.si;
+            uint64_t acc2[CW / 2];                        // the sums, in pairs
+#pragma unroll
+            for (int j = 0; j < CW / 2; ++j) acc2[j] = 0ull;
+            float a_next = __ldg(sa + kb0 * p.sa.sb), b_next = 1.f;
+            float bv[CW / 32];
+            if constexpr (!BVEC) b_next = __ldg(sb + kb0 * p.sb.sb);
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const uint32_t buf = it % NBUF, bph = (it / NBUF) & 1u;
+                if constexpr (BVEC) {
+#pragma unroll
+                    for (int j = 0; j < CW / 32; ++j) {
+                        const int n = col0 + j * 32 + lane;
+                        bv[j] = __ldg(p.sb.p + (int64_t)(n < p.N ? n : p.N - 1) + kb * p.sb.sb);
+                    }
+                }
+                const uint64_t s = pair(a_next * b_next, a_next * b_next);
+                if (kb + 1 < kb1) {
+                    a_next = __ldg(sa + (kb + 1) * p.sa.sb);
+                    if constexpr (!BVEC) b_next = __ldg(sb + (kb + 1) * p.sb.sb);
+                }
+                if constexpr (BVEC) {
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < CW / 32; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(staging + 4u * (j * 32 + lane)), "f"(bv[j]) : "memory");
+                    __syncwarp();
+                }
+                if (!warp_wait(acc_full + 8u * buf, bph)) { failed = true; break; }
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < CW / 32; ++c) {
+                    float v[32];
+                    tc_ld32(tmem + lanes + buf * BN + half * CW + c * 32, v);
+                    if (c == CW / 32 - 1) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(acc_empty + 8u * buf);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        if constexpr (BVEC) {
+                            uint64_t q0, q1;
+                            asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(q0), "=l"(q1) : "r"(staging + 4u * (c * 32 + j)) : "memory");
+                            fma_pair(acc2[c * 16 + j / 2], mul_pair(s, pair(v[j], v[j + 1])), q0);
+                            fma_pair(acc2[c * 16 + j / 2 + 1], mul_pair(s, pair(v[j + 2], v[j + 3])), q1);
+                        } else {
+                            fma_pair(acc2[c * 16 + j / 2], s, pair(v[j], v[j + 1]));
+                            fma_pair(acc2[c * 16 + j / 2 + 1], s, pair(v[j + 2], v[j + 3]));
+                        }
+                    }
+                }
+            }
+            if (failed) break;
+            float acc[CW];
+#pragma unroll
+            for (int j = 0; j < CW; j += 2) asm("mov.b64 {%0, %1}, %2;" : "=f"(acc[j]), "=f"(acc[j + 1]) : "l"(acc2[j / 2]));
+            if (p.split == 1) {
+                constexpr int SLAB = 8 * Out<C>::PER16;
+#pragma unroll
+                for (int c = 0; c < CW / SLAB; ++c) write_slab<C>(p, staging, tm * BM + quad * 32, col0 + c * SLAB, acc + c * SLAB);
+                __syncwarp();
+            } else {
+                // the stages are free: every product of this block has been taken out.  Partial tile: row r at r * BN floats,
+                // 16-byte pieces exchanged by the row so that lanes do not meet in a bank
+                const uint32_t base = smem + (uint32_t)(quad * 32 + lane) * (BN * 4u);
+#pragma unroll
+                for (int j = 0; j < CW / 4; ++j)
+                    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + ((uint32_t)((half * (CW / 4) + j) ^ (lane & 7)) << 4)), "f"(acc[4 * j]), "f"(acc[4 * j + 1]),
+                                 "f"(acc[4 * j + 2]), "f"(acc[4 * j + 3]) : "memory");
+            }
+        }
+        if (p.split > 1) {
+            // one tile per cluster: add the partial tiles in the order of their blocks of k; block `rank` takes every split-th row
+            __syncwarp();
+            cluster_sync();
+            int tm, tn;
+            tile_of(p, t0, tm, tn);
+            const int rows = p.M - tm * BM < BM ? p.M - tm * BM : BM;
+            C* c = static_cast<C*>(p.C);
+            for (int i = threadIdx.x - 32 * WARP_EPI0; i < (BM / p.split) * (BN / 4); i += 32 * EPI_WARPS) {
+                const int r = (i / (BN / 4)) * p.split + rank, j = i % (BN / 4);
+                if (r >= rows) break;
+                const uint32_t at = smem + (uint32_t)r * (BN * 4u) + ((uint32_t)(j ^ (r & 7)) << 4);
+                float4 v = ld_cluster4(at, 0);
+                for (int q = 1; q < p.split; ++q) {
+                    const float4 w = ld_cluster4(at, q);
+                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+                }
+                const int n0 = tn * BN + 4 * j;
+                C* dst = c + (int64_t)(tm * BM + r) * p.ldc + n0;
+                const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n0 + e < p.N) dst[e] = (C)(p.accumulate ? (float)dst[e] + x[e] : x[e]);
+            }
+            __syncwarp();
+            cluster_sync();                             // no block leaves while another reads its part
+        }
+    }
+
+    if (failed) {
+        if (lane == 0) atomicExch(p.status, 2);
+        const unsigned long long start = global_ns();
+        while (global_ns() - start < 2000000ull) { }    // let copies and products in flight finish
+    }
+    grid_dependents_may_launch();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tc_dealloc(tmem, 512u);
+    }
+}
+
+bool make_map_8bit(CUtensorMap* m, const cerar_fp8_matrix_t& x, int box_rows) {
+    const cuuint64_t dim[2] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows}, stride[1] = {(cuuint64_t)x.ld};
+    const cuuint32_t box[2] = {(cuuint32_t)BK, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    return get_encode_fn()(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, x.codes, dim, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // rows_are_k: the summed dimension runs down the rows of the stored matrix
-Operand operand(const cerar_fp8_matrix_t& m, bool rows_are_k) {
-    Operand o;
-    o.codes = m.codes; o.scales = m.scales;
-    o.rs = rows_are_k ? 1 : m.ld; o.ks = rows_are_k ? m.ld : 1;
-    o.rd = m.scaling == CERAR_BY_BLOCK ? FP8_BLOCK : 1;
-    if (m.scaling == CERAR_BY_BLOCK) { o.srs = rows_are_k ? 1 : m.lds; o.sbs = rows_are_k ? m.lds : 1; }
-    else { o.srs = 1; o.sbs = m.lds; }
-    return o;
+Scales scales_of(const cerar_fp8_matrix_t& m, bool rows_are_k) {
+    if (m.scaling != CERAR_BY_BLOCK) return {m.scales, 1, m.lds, 0};
+    return rows_are_k ? Scales{m.scales, 1, m.lds, 7} : Scales{m.scales, m.lds, 1, 7};
+}
+
+template <int BN, bool BVEC, typename C>
+cudaError_t launch_one(const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, int grid, cudaStream_t s) {
+    auto kern = fp8_matmul_kernel<BN, BVEC, C>;
+    const size_t smem = 1024 + (size_t)p.stages * (A_BYTES + BN * BK) + EPI_WARPS * STAGING + 512;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = g_tune_pdl_off ? 0 : 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {(unsigned)p.split, 1, 1};
+    cfg.attrs = attr; cfg.numAttrs = p.split > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, ma, mb, p);
+}
+template <int BN>
+cudaError_t launch_bn(const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, bool bvec, int type, int grid, cudaStream_t s) {
+    if (type == CERAR_TYPE_F32) return bvec ? launch_one<BN, true, float>(ma, mb, p, grid, s) : launch_one<BN, false, float>(ma, mb, p, grid, s);
+    return bvec ? launch_one<BN, true, __nv_bfloat16>(ma, mb, p, grid, s) : launch_one<BN, false, __nv_bfloat16>(ma, mb, p, grid, s);
 }
 
 }  // namespace
 
-cudaError_t launch_fp8_matmul(const MatmulArgs& a, int, cudaStream_t s, uint64_t* launches) {
-    const dim3 grid((unsigned)((a.N + TN - 1) / TN), (unsigned)((a.M + TM - 1) / TM));
-    const Operand A = operand(a.A, a.trans_a), B = operand(a.B, !a.trans_b);
-    const cudaError_t e = a.type == CERAR_TYPE_F32
-        ? launch_pdl(fp8_matmul_kernel<float>, grid, dim3(256), 0, s, A, B, (float*)a.C, a.ldc, a.M, a.N, a.K, a.accumulate)
-        : launch_pdl(fp8_matmul_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, A, B, (__nv_bfloat16*)a.C, a.ldc, a.M, a.N, a.K, a.accumulate);
+cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, uint64_t* launches) {
+    if (!get_encode_fn()) return cudaErrorNotSupported;
+    Params p = {};
+    p.M = (int)a.M; p.N = (int)a.N; p.kblocks = (int)((a.K + BK - 1) / BK);
+    p.tiles_m = (p.M + BM - 1) / BM;
+    // wide tiles where they fill the GPU, otherwise narrow ones, and a tile shared by several blocks while SMs are left over
+    const bool wide = (int64_t)p.tiles_m * ((p.N + 255) / 256) >= num_sms;
+    const int BN = wide ? 256 : 128;
+    p.tiles_n = (p.N + BN - 1) / BN;
+    p.tiles = (int64_t)p.tiles_m * p.tiles_n;
+    p.split = 1;
+    if (!wide)
+        while (p.split < 8 && p.tiles * p.split * 2 <= num_sms && p.split * 4 <= p.kblocks) p.split *= 2;
+    p.group_m = 16;
+    p.stages = wide ? 4 : 6;
+    p.a_mn = a.trans_a; p.b_mn = !a.trans_b;
+    p.sa = scales_of(a.A, a.trans_a);
+    p.sb = scales_of(a.B, !a.trans_b);
+    p.C = a.C; p.ldc = a.ldc; p.accumulate = a.accumulate; p.status = a.status;
+    const int64_t size = a.type == CERAR_TYPE_F32 ? 4 : 2;
+    p.c_vec = (reinterpret_cast<uintptr_t>(a.C) & 15u) == 0 && (a.ldc * size) % 16 == 0;
+    CUtensorMap ma, mb;
+    if (!make_map_8bit(&ma, a.A, BM) || !make_map_8bit(&mb, a.B, p.b_mn ? BK : BN)) return cudaErrorInvalidValue;
+    const int64_t grid = p.split > 1 ? p.tiles * p.split : p.tiles < num_sms ? p.tiles : num_sms;
+    const bool bvec = a.B.scaling != CERAR_BY_BLOCK;
+    const cudaError_t e = wide ? launch_bn<256>(ma, mb, p, bvec, a.type, (int)grid, s) : launch_bn<128>(ma, mb, p, bvec, a.type, (int)grid, s);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
