@@ -499,6 +499,7 @@ typedef struct {
     float*   scales;
     int64_t  rows, cols, ld, lds;
     int32_t  scaling;            /* cerar_scaling_t */
+    int32_t  pow2;               /* 1: all scales are powers of two from 2^-126 to 2^127 (cerar_fp8_quantize writes such) */
 } cerar_fp8_matrix_t;
 
 /* Converts x (rows x cols of `type`, ldx elements between rows) into `count` (1..3) 8-bit matrices of the
@@ -514,6 +515,8 @@ cerar_status_t cerar_fp8_quantize(cerar_ops_t* ops, const void* x, cerar_type_t 
  * op(B) = B wants B by column or by block, op(B) = B^T by row or by block.  Any finite scales.
  *     C[m,n] (+)= sum_b sA(m,b) sB(b,n) sum_{k in block b} A[m,k] B[k,n]
  * The inner sums run on the tensor cores, the outer one in binary32; one rounding to `type` at the end.
+ * Where both matrices say pow2 the tensor cores apply the scales too, which is faster; a scale that is
+ * no power of two all the same makes the results it would touch NaN.
  * A linear layer with weights W (outputs x inputs): Y = X W^T, dX = dY W, dW += dY^T X.
  * Deterministic: the same operands give the same bits. */
 cerar_status_t cerar_fp8_matmul(cerar_ops_t* ops, const cerar_fp8_matrix_t* A, int trans_a,

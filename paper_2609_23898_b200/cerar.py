@@ -49,7 +49,7 @@ class Counters(C.Structure):
 
 class Fp8Matrix(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
-                ("ld", C.c_int64), ("lds", C.c_int64), ("scaling", C.c_int32)]
+                ("ld", C.c_int64), ("lds", C.c_int64), ("scaling", C.c_int32), ("pow2", C.c_int32)]
 
 
 class TensorDesc(C.Structure):

@@ -56,7 +56,7 @@ struct Params {
     int64_t ldc;
     int M, N, kblocks;
     int tiles_m, tiles_n, group_m;
-    int64_t tiles;
+    uint32_t tiles;
     int a_mn, b_mn;                                    // 1: the operand's own dimension (m or n) is the contiguous one
     int accumulate, c_vec;
     int stages, split;
@@ -77,10 +77,30 @@ __device__ __forceinline__ uint64_t swizzled_desc(uint32_t saddr) {
     return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)((BK * 128u) >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 |
            (uint64_t)1 << 46 /* sm_100 descriptor */ | (uint64_t)2 << 61 /* 128-byte swizzle */;
 }
+// 32 columns of this warp's lanes of tensor memory; the values may be used after ld32_done, which names them so that no use of
+// them is moved in front of the wait
+__device__ __forceinline__ void ld32_start(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void ld32_done(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+          "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+          "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+          "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29])  : : "memory");
+    asm volatile("" : "+r"(r[30]), "+r"(r[31]) : : "memory");
+}
 // two sums at a time (one instruction): a += x * y
-__device__ __forceinline__ uint64_t pair(float x, float y) {
+__device__ __forceinline__ uint64_t pair(uint32_t x, uint32_t y) {
     uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(x), "r"(y));
     return r;
 }
 __device__ __forceinline__ void fma_pair(uint64_t& a, uint64_t x, uint64_t y) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(a) : "l"(x), "l"(y)); }
@@ -107,8 +127,8 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t saddr, uint32_t rank) {
 
 // tile number -> (row tile, column tile): column by column inside bands of group_m row tiles, so that the tiles that run at the
 // same time share operand tiles in L2
-__device__ __forceinline__ void tile_of(const Params& p, int64_t t, int& tm, int& tn) {
-    const int64_t per_band = (int64_t)p.group_m * p.tiles_n;
+__device__ __forceinline__ void tile_of(const Params& p, uint32_t t, int& tm, int& tn) {
+    const uint32_t per_band = (uint32_t)(p.group_m * p.tiles_n);
     const int band = (int)(t / per_band);
     const int first = band * p.group_m;
     const int rows = p.tiles_m - first < p.group_m ? p.tiles_m - first : p.group_m;
@@ -185,6 +205,18 @@ __device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, in
                              "f"(v[h * 32 + 4 * j + 2]), "f"(v[h * 32 + 4 * j + 3]) : "memory");
             __syncwarp();
             if (p.c_vec && n == SLAB) {
+                // (all reads of C before the first store to it: they are independent, which the compiler cannot know)
+                constexpr int W = sizeof(C);                                // 32-bit words of four elements
+                uint32_t old[8][W];
+#pragma unroll
+                for (int it = 0; it < 8; ++it) {
+                    const int r = it * 4 + (lane >> 3), j = lane & 7;
+                    const C* src = c + (int64_t)(row0 + r) * p.ldc + col0 + h * 32 + j * 4;
+                    if (r < nrows) {
+                        if constexpr (W == 4) *reinterpret_cast<uint4*>(old[it]) = *reinterpret_cast<const uint4*>(src);
+                        else *reinterpret_cast<uint2*>(old[it]) = *reinterpret_cast<const uint2*>(src);
+                    }
+                }
 #pragma unroll
                 for (int it = 0; it < 8; ++it) {
                     const int r = it * 4 + (lane >> 3), j = lane & 7;
@@ -193,13 +225,13 @@ __device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, in
                     if (r < nrows) {
                         C* dst = c + (int64_t)(row0 + r) * p.ldc + col0 + h * 32 + j * 4;
                         if constexpr (sizeof(C) == 4) {
-                            const float4 o = *reinterpret_cast<const float4*>(dst);
-                            *reinterpret_cast<float4*>(dst) = make_float4(o.x + q.x, o.y + q.y, o.z + q.z, o.w + q.w);
+                            *reinterpret_cast<float4*>(dst) = make_float4(__uint_as_float(old[it][0]) + q.x, __uint_as_float(old[it][1]) + q.y,
+                                                                          __uint_as_float(old[it][2]) + q.z, __uint_as_float(old[it][3]) + q.w);
                         } else {
-                            const uint2 o = *reinterpret_cast<const uint2*>(dst);
+                            const uint32_t o0 = old[it][0], o1 = old[it][1];
                             *reinterpret_cast<uint2*>(dst) = make_uint2(
-                                Out<C>::two(__uint_as_float(o.x << 16) + q.x, __uint_as_float(o.x & 0xFFFF0000u) + q.y),
-                                Out<C>::two(__uint_as_float(o.y << 16) + q.z, __uint_as_float(o.y & 0xFFFF0000u) + q.w));
+                                Out<C>::two(__uint_as_float(o0 << 16) + q.x, __uint_as_float(o0 & 0xFFFF0000u) + q.y),
+                                Out<C>::two(__uint_as_float(o1 << 16) + q.z, __uint_as_float(o1 & 0xFFFF0000u) + q.w));
                         }
                     }
                 }
@@ -215,6 +247,84 @@ __device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, in
                 }
             }
         }
+    }
+}
+
+// The producer's thread: the stages of every block of k of every tile of this CTA.
+template <int BN>
+__device__ __forceinline__ void produce(const Params& p, const CUtensorMap& map_a, const CUtensorMap& map_b, uint32_t smem, uint32_t full, uint32_t empty,
+                                        uint32_t t0, uint32_t tstep, int kb0, int kb1, bool& failed) {
+    constexpr uint32_t STAGE = A_BYTES + BN * BK;
+    uint32_t it = 0;
+    for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
+        int tm, tn;
+        tile_of(p, t, tm, tn);
+        const int m0 = tm * BM, n0 = tn * BN;
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+            const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u;
+            if (!mbar_wait_bounded(empty + 8u * s, ph ^ 1u)) { failed = true; break; }
+            const uint32_t a = smem + s * STAGE, b = a + A_BYTES, bar = full + 8u * s;
+            mbar_arrive_expect_tx(bar, STAGE);
+            if (p.a_mn) tma_load_2d(a, &map_a, m0, kb * BK, bar);
+            else tma_load_2d(a, &map_a, kb * BK, m0, bar);
+            if (p.b_mn) {
+#pragma unroll
+                for (int j = 0; j < BN / 128; ++j) tma_load_2d(b + j * (128 * BK), &map_b, n0 + j * 128, kb * BK, bar);
+            } else {
+                tma_load_2d(b, &map_b, kb * BK, n0, bar);
+            }
+        }
+    }
+}
+
+// A tile whose sum is split over a cluster: every block leaves its partial tile in its stages (free by then), row r at r * BN floats,
+// 16-byte pieces exchanged by the row so that lanes do not meet in a bank ...
+template <int BN>
+__device__ __forceinline__ void store_partial(uint32_t smem, int row, int col, int n, const uint32_t* v) {
+    const uint32_t base = smem + (uint32_t)row * (BN * 4u);
+#pragma unroll
+    for (int j = 0; j < n / 4; ++j)
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + ((uint32_t)((col / 4 + j) ^ (row & 7)) << 4)), "r"(v[4 * j]), "r"(v[4 * j + 1]),
+                     "r"(v[4 * j + 2]), "r"(v[4 * j + 3]) : "memory");
+}
+// ... and adds every split-th row of all partial tiles, in the order of their blocks of k.
+template <int BN, typename C>
+__device__ __forceinline__ void add_partials(const Params& p, uint32_t smem, uint32_t t, int rank, int thread) {
+    int tm, tn;
+    tile_of(p, t, tm, tn);
+    const int rows = p.M - tm * BM < BM ? p.M - tm * BM : BM;
+    C* c = static_cast<C*>(p.C);
+    for (int i = thread; i < (BM / p.split) * (BN / 4); i += 32 * EPI_WARPS) {
+        const int r = (i / (BN / 4)) * p.split + rank, j = i % (BN / 4);
+        if (r >= rows) break;
+        const uint32_t at = smem + (uint32_t)r * (BN * 4u) + ((uint32_t)(j ^ (r & 7)) << 4);
+        float4 v = ld_cluster4(at, 0);
+        for (int q = 1; q < p.split; ++q) {
+            const float4 w = ld_cluster4(at, q);
+            v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+        }
+        const int n0 = tn * BN + 4 * j;
+        C* dst = c + (int64_t)(tm * BM + r) * p.ldc + n0;
+        const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n0 + e < p.N) dst[e] = (C)(p.accumulate ? (float)dst[e] + x[e] : x[e]);
+    }
+}
+
+// The common exit: every warp comes here, whatever it waited for in vain.
+__device__ __forceinline__ void leave(const Params& p, bool failed, int warp, int lane, uint32_t tmem) {
+    if (failed) {
+        if (lane == 0) atomicExch(p.status, 2);
+        const unsigned long long start = global_ns();
+        while (global_ns() - start < 2000000ull) { }    // let copies and products in flight finish
+    }
+    grid_dependents_may_launch();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tc_dealloc(tmem, 512u);
     }
 }
 
@@ -247,35 +357,14 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     grid_dependency_wait();
 
     const int rank = p.split > 1 ? (int)cluster_rank() : 0;
-    const int64_t t0 = blockIdx.x / p.split, tstep = gridDim.x / p.split;
+    const uint32_t t0 = blockIdx.x / p.split, tstep = gridDim.x / p.split;
     const int kb0 = (int)((int64_t)p.kblocks * rank / p.split), kb1 = (int)((int64_t)p.kblocks * (rank + 1) / p.split);
     bool failed = false;
 
     if (warp < WARP_EPI0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
         if (warp == 0) {
-            if (lane == 0) {
-                uint32_t it = 0;
-                for (int64_t t = t0; t < p.tiles && !failed; t += tstep) {
-                    int tm, tn;
-                    tile_of(p, t, tm, tn);
-                    const int m0 = tm * BM, n0 = tn * BN;
-                    for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                        const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u;
-                        if (!mbar_wait_bounded(empty + 8u * s, ph ^ 1u)) { failed = true; break; }
-                        const uint32_t a = smem + s * STAGE, b = a + A_BYTES, bar = full + 8u * s;
-                        mbar_arrive_expect_tx(bar, STAGE);
-                        if (p.a_mn) tma_load_2d(a, &map_a, m0, kb * BK, bar);
-                        else tma_load_2d(a, &map_a, kb * BK, m0, bar);
-                        if (p.b_mn) {
-    #pragma unroll
-                            for (int j = 0; j < BN / 128; ++j) tma_load_2d(b + j * (128 * BK), &map_b, n0 + j * 128, kb * BK, bar);
-                        } else {
-                            tma_load_2d(b, &map_b, kb * BK, n0, bar);
-                        }
-                    }
-                }
-            }
+            if (lane == 0) produce<BN>(p, map_a, map_b, smem, full, empty, t0, tstep, kb0, kb1, failed);
         } else if (warp == 1) {
             if (lane == 0) {
                 // D binary32, A and B e4m3, M = 128, N = BN
@@ -283,7 +372,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 // 32 values of k further: 32 bytes in a row of k, or 32 rows of 128 bytes
                 const uint64_t a_step = p.a_mn ? (32u * 128u) >> 4 : 32u >> 4, b_step = p.b_mn ? (32u * 128u) >> 4 : 32u >> 4;
                 uint32_t it = 0;
-                for (int64_t t = t0; t < p.tiles && !failed; t += tstep)
+                for (uint32_t t = t0; t < p.tiles && !failed; t += tstep)
                     for (int kb = kb0; kb < kb1; ++kb, ++it) {
                         const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u, buf = it % NBUF, bph = (it / NBUF) & 1u;
                         if (!mbar_wait_bounded(acc_empty + 8u * buf, bph ^ 1u) || !mbar_wait_bounded(full + 8u * s, ph)) { failed = true; break; }
@@ -304,7 +393,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         const uint32_t staging = staging0 + (uint32_t)(warp - WARP_EPI0) * STAGING;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         uint32_t it = 0;
-        for (int64_t t = t0; t < p.tiles && !failed; t += tstep) {
+        for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
             int tm, tn;
             tile_of(p, t, tm, tn);
             const int row = tm * BM + quad * 32 + lane, col0 = tn * BN + half * CW;
@@ -326,7 +415,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         bv[j] = __ldg(p.sb.p + (int64_t)(n < p.N ? n : p.N - 1) + kb * p.sb.sb);
                     }
                 }
-                const uint64_t s = pair(a_next * b_next, a_next * b_next);
+                const uint64_t s = pair(__float_as_uint(a_next * b_next), __float_as_uint(a_next * b_next));
                 if (kb + 1 < kb1) {
                     a_next = __ldg(sa + (kb + 1) * p.sa.sb);
                     if constexpr (!BVEC) b_next = __ldg(sb + (kb + 1) * p.sb.sb);
@@ -339,11 +428,17 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 }
                 if (!warp_wait(acc_full + 8u * buf, bph)) { failed = true; break; }
                 tc_fence_after();
+                // the next 32 columns are on their way while these are added
+                uint32_t v[2][32];
+                const uint32_t from = tmem + lanes + buf * BN + half * CW;
+                ld32_start(from, v[0]);
 #pragma unroll
                 for (int c = 0; c < CW / 32; ++c) {
-                    float v[32];
-                    tc_ld32(tmem + lanes + buf * BN + half * CW + c * 32, v);
-                    if (c == CW / 32 - 1) {
+                    uint32_t* x = v[c & 1];
+                    ld32_done(x);
+                    if (c < CW / 32 - 1) {
+                        ld32_start(from + (c + 1) * 32, v[(c + 1) & 1]);
+                    } else {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(acc_empty + 8u * buf);
@@ -353,11 +448,11 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         if constexpr (BVEC) {
                             uint64_t q0, q1;
                             asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(q0), "=l"(q1) : "r"(staging + 4u * (c * 32 + j)) : "memory");
-                            fma_pair(acc2[c * 16 + j / 2], mul_pair(s, pair(v[j], v[j + 1])), q0);
-                            fma_pair(acc2[c * 16 + j / 2 + 1], mul_pair(s, pair(v[j + 2], v[j + 3])), q1);
+                            fma_pair(acc2[c * 16 + j / 2], mul_pair(s, pair(x[j], x[j + 1])), q0);
+                            fma_pair(acc2[c * 16 + j / 2 + 1], mul_pair(s, pair(x[j + 2], x[j + 3])), q1);
                         } else {
-                            fma_pair(acc2[c * 16 + j / 2], s, pair(v[j], v[j + 1]));
-                            fma_pair(acc2[c * 16 + j / 2 + 1], s, pair(v[j + 2], v[j + 3]));
+                            fma_pair(acc2[c * 16 + j / 2], s, pair(x[j], x[j + 1]));
+                            fma_pair(acc2[c * 16 + j / 2 + 1], s, pair(x[j + 2], x[j + 3]));
                         }
                     }
                 }
@@ -372,56 +467,205 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 for (int c = 0; c < CW / SLAB; ++c) write_slab<C>(p, staging, tm * BM + quad * 32, col0 + c * SLAB, acc + c * SLAB);
                 __syncwarp();
             } else {
-                // the stages are free: every product of this block has been taken out.  Partial tile: row r at r * BN floats,
-                // 16-byte pieces exchanged by the row so that lanes do not meet in a bank
-                const uint32_t base = smem + (uint32_t)(quad * 32 + lane) * (BN * 4u);
-#pragma unroll
-                for (int j = 0; j < CW / 4; ++j)
-                    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + ((uint32_t)((half * (CW / 4) + j) ^ (lane & 7)) << 4)), "f"(acc[4 * j]), "f"(acc[4 * j + 1]),
-                                 "f"(acc[4 * j + 2]), "f"(acc[4 * j + 3]) : "memory");
+                store_partial<BN>(smem, quad * 32 + lane, half * CW, CW, reinterpret_cast<const uint32_t*>(acc));
             }
         }
+        __syncwarp();
         if (p.split > 1) {
-            // one tile per cluster: add the partial tiles in the order of their blocks of k; block `rank` takes every split-th row
-            __syncwarp();
             cluster_sync();
-            int tm, tn;
-            tile_of(p, t0, tm, tn);
-            const int rows = p.M - tm * BM < BM ? p.M - tm * BM : BM;
-            C* c = static_cast<C*>(p.C);
-            for (int i = threadIdx.x - 32 * WARP_EPI0; i < (BM / p.split) * (BN / 4); i += 32 * EPI_WARPS) {
-                const int r = (i / (BN / 4)) * p.split + rank, j = i % (BN / 4);
-                if (r >= rows) break;
-                const uint32_t at = smem + (uint32_t)r * (BN * 4u) + ((uint32_t)(j ^ (r & 7)) << 4);
-                float4 v = ld_cluster4(at, 0);
-                for (int q = 1; q < p.split; ++q) {
-                    const float4 w = ld_cluster4(at, q);
-                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-                }
-                const int n0 = tn * BN + 4 * j;
-                C* dst = c + (int64_t)(tm * BM + r) * p.ldc + n0;
-                const float x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (n0 + e < p.N) dst[e] = (C)(p.accumulate ? (float)dst[e] + x[e] : x[e]);
-            }
+            add_partials<BN, C>(p, smem, t0, rank, threadIdx.x - 32 * WARP_EPI0);
             __syncwarp();
             cluster_sync();                             // no block leaves while another reads its part
         }
     }
+    leave(p, failed, warp, lane, tmem);
+}
 
-    if (failed) {
-        if (lane == 0) atomicExch(p.status, 2);
-        const unsigned long long start = global_ns();
-        while (global_ns() - start < 2000000ull) { }    // let copies and products in flight finish
+// ---------------------------------------------------------------- scales that are powers of two
+//
+// The tensor core multiplies by such scales itself (kind::mxf8f6f4.block_scale: one 8-bit exponent per row and 32 values of k, from
+// tensor memory), so the sum over all blocks stays in the accumulator, nothing is taken out in between, and a tile costs its
+// products alone.  The exponents of 128 rows are 4 columns of 32 lanes (row r in lane r % 32 of column r / 32), present in
+// all four lane quadrants; a 32-bit word holds those of four blocks of k, which the instruction picks from by number.
+//
+//   warp 0       producer, warp 1 issues the products, as above
+//   warps 4-7    read the scales four blocks ahead, put their exponents into tensor memory.  A scale that is no power of two
+//                (the caller said they all are) becomes the exponent that means NaN, and so do the results it touches
+//   warps 8-15   write the tile of C
+// Two accumulators of 256 columns and the exponents do not fit into 512 columns: the accumulators overlap by 32 columns,
+// which are written out first; the products of the next tile wait for those only.
+constexpr int POW2_THREADS = 512, WARP_SCALE0 = 4, WARP_OUT0 = 8;
+constexpr uint32_t SF_COL = 480, SF_BUF = 16;            // exponents: two buffers of 4 (A) and, 8 further, 8 (B) columns
+
+__device__ __forceinline__ void mma_mxf8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+                 " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ uint32_t exponent_of(float s) {
+    const uint32_t b = __float_as_uint(s), e = b >> 23;
+    return (b & 0x807FFFFFu) == 0u && e >= 1u && e <= 254u ? e : 0xFFu;
+}
+
+template <int BN, typename C>
+__global__ void __launch_bounds__(POW2_THREADS, 1)
+fp8_matmul_pow2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Params p) {
+    constexpr int CW = BN / 2;
+    constexpr uint32_t B_BYTES = BN * BK, STAGE = A_BYTES + B_BYTES;
+    constexpr uint32_t OVERLAP = BN == 256 ? 32 : 0, D1 = BN - OVERLAP;       // first column of the second accumulator
+    constexpr int SLAB = 8 * Out<C>::PER16;
+    extern __shared__ unsigned char smem_dyn[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    const uint32_t staging0 = smem + (uint32_t)p.stages * STAGE;
+    const uint32_t bars = staging0 + EPI_WARPS * STAGING;
+    const uint32_t full = bars, empty = full + 8u * p.stages, acc_full = empty + 8u * p.stages, acc_empty = acc_full + 16u, over_empty = acc_empty + 16u;
+    const uint32_t sf_full = over_empty + 8u, sf_empty = sf_full + 16u, slot = sf_empty + 16u;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8u * s, 1); mbar_init(empty + 8u * s, 1); }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full + 8u * b, 1); mbar_init(acc_empty + 8u * b, EPI_WARPS);
+            mbar_init(sf_full + 8u * b, 4); mbar_init(sf_empty + 8u * b, 1);
+        }
+        mbar_init(over_empty, EPI_WARPS / 2);
+        mbar_init_fence();
     }
-    grid_dependents_may_launch();
+    if (warp == 1) tc_alloc(slot, 512u);
     tc_fence_before();
     __syncthreads();
-    if (warp == 1) {
-        tc_fence_after();
-        tc_dealloc(tmem, 512u);
+    tc_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    grid_dependency_wait();
+
+    const int rank = p.split > 1 ? (int)cluster_rank() : 0;
+    const uint32_t t0 = blockIdx.x / p.split, tstep = gridDim.x / p.split;
+    const int kb0 = (int)((int64_t)p.kblocks * rank / p.split), kb1 = (int)((int64_t)p.kblocks * (rank + 1) / p.split);
+    bool failed = false;
+
+    if (warp == 0) {
+        if (lane == 0) produce<BN>(p, map_a, map_b, smem, full, empty, t0, tstep, kb0, kb1, failed);
+    } else if (warp == 1) {
+        if (lane == 0) {
+            // exponents of 8 bits, A and B e4m3, M = 128, N = BN
+            const uint32_t idesc0 = (1u << 23) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) | ((128u >> 4) << 24);
+            const uint64_t a_step = p.a_mn ? (32u * 128u) >> 4 : 32u >> 4, b_step = p.b_mn ? (32u * 128u) >> 4 : 32u >> 4;
+            uint32_t it = 0, tile = 0, group = 0;
+            for (uint32_t t = t0; t < p.tiles && !failed; t += tstep, ++tile) {
+                const uint32_t buf = tile & 1u;
+                if (!mbar_wait_bounded(acc_empty + 8u * buf, ((tile >> 1) & 1u) ^ 1u)) { failed = true; break; }
+                if (OVERLAP && !mbar_wait_bounded(over_empty, (tile & 1u) ^ 1u)) { failed = true; break; }
+                tc_fence_after();
+                const uint32_t d = tmem + buf * D1;
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u, id = (uint32_t)(kb - kb0) & 3u, sbuf = group & 1u;
+                    if (id == 0u && !mbar_wait_bounded(sf_full + 8u * sbuf, (group >> 1) & 1u)) { failed = true; break; }
+                    if (!mbar_wait_bounded(full + 8u * s, ph)) { failed = true; break; }
+                    tc_fence_after();
+                    const uint64_t da = swizzled_desc(smem + s * STAGE), db = swizzled_desc(smem + s * STAGE + A_BYTES);
+                    const uint32_t sf = tmem + SF_COL + sbuf * SF_BUF, idesc = idesc0 | (id << 4) | (id << 29);
+#pragma unroll
+                    for (int k = 0; k < BK / 32; ++k) mma_mxf8(d, da + k * a_step, db + k * b_step, idesc, sf, sf + 8, kb != kb0 || k != 0);
+                    tc_commit(empty + 8u * s);
+                    if (id == 3u || kb + 1 == kb1) { tc_commit(sf_empty + 8u * sbuf); ++group; }
+                }
+                if (!failed) tc_commit(acc_full + 8u * buf);
+            }
+        }
+    } else if (warp >= WARP_SCALE0 && warp < WARP_OUT0) {
+        uint32_t group = 0;
+        for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
+            int tm, tn;
+            tile_of(p, t, tm, tn);
+            const float *a[4], *b[BN / 32];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int m = tm * BM + j * 32 + lane;
+                a[j] = p.sa.p + (int64_t)((m < p.M ? m : p.M - 1) >> p.sa.shift) * p.sa.si;
+            }
+#pragma unroll
+            for (int j = 0; j < BN / 32; ++j) {
+                const int n = tn * BN + j * 32 + lane;
+                b[j] = p.sb.p + (int64_t)((n < p.N ? n : p.N - 1) >> p.sb.shift) * p.sb.si;
+            }
+            for (int kb = kb0; kb < kb1; kb += 4, ++group) {
+                uint32_t ea[4] = {}, eb[BN / 32] = {};
+                float x[4][4 + BN / 32];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int k = kb + i < kb1 ? kb + i : kb1 - 1;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[i][j] = __ldg(a[j] + k * p.sa.sb);
+#pragma unroll
+                    for (int j = 0; j < BN / 32; ++j) x[i][4 + j] = __ldg(b[j] + k * p.sb.sb);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) ea[j] |= exponent_of(x[i][j]) << (8 * i);
+#pragma unroll
+                    for (int j = 0; j < BN / 32; ++j) eb[j] |= exponent_of(x[i][4 + j]) << (8 * i);
+                }
+                const uint32_t sbuf = group & 1u;
+                if (!warp_wait(sf_empty + 8u * sbuf, ((group >> 1) & 1u) ^ 1u)) { failed = true; break; }
+                tc_fence_after();
+                const uint32_t to = tmem + ((uint32_t)((warp & 3) * 32) << 16) + SF_COL + sbuf * SF_BUF;
+                tc_st_cols<4>(to, ea);
+                tc_st_cols<BN / 32>(to + 8, eb);
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sf_full + 8u * sbuf);
+            }
+        }
+    } else if (warp >= WARP_OUT0) {
+        const int quad = warp & 3, half = (warp - WARP_OUT0) >> 2;
+        const uint32_t staging = staging0 + (uint32_t)(warp - WARP_OUT0) * STAGING;
+        uint32_t tile = 0;
+        for (uint32_t t = t0; t < p.tiles && !failed; t += tstep, ++tile) {
+            int tm, tn;
+            tile_of(p, t, tm, tn);
+            const uint32_t buf = tile & 1u;
+            if (!warp_wait(acc_full + 8u * buf, (tile >> 1) & 1u)) { failed = true; break; }
+            tc_fence_after();
+            const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + buf * D1 + half * CW;
+            // the shared columns first: the last 32 of the first accumulator, the first 32 of the second
+            const bool shares = OVERLAP && half == (buf == 0u ? 1 : 0);
+            for (int i = 0; i < CW / SLAB; ++i) {
+                const int c = shares && buf == 0u ? CW / SLAB - 1 - i : i;
+                uint32_t v[SLAB];
+#pragma unroll
+                for (int h = 0; h < SLAB / 32; ++h) ld32_start(from + c * SLAB + h * 32, v + h * 32);
+#pragma unroll
+                for (int h = 0; h < SLAB / 32; ++h) ld32_done(v + h * 32);
+                if (i == 0 && shares) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(over_empty);
+                }
+                if (i == CW / SLAB - 1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(acc_empty + 8u * buf);
+                }
+                if (p.split == 1) {
+                    write_slab<C>(p, staging, tm * BM + quad * 32, tn * BN + half * CW + c * SLAB, reinterpret_cast<const float*>(v));
+                } else {
+                    store_partial<BN>(smem, quad * 32 + lane, half * CW + c * SLAB, SLAB, v);
+                }
+            }
+            __syncwarp();
+        }
     }
+    __syncwarp();
+    if (p.split > 1) {
+        cluster_sync();
+        if (warp >= WARP_OUT0) add_partials<BN, C>(p, smem, t0, rank, threadIdx.x - 32 * WARP_OUT0);
+        __syncwarp();
+        cluster_sync();
+    }
+    leave(p, failed, warp, lane, tmem);
 }
 
 bool make_map_8bit(CUtensorMap* m, const cerar_fp8_matrix_t& x, int box_rows) {
@@ -437,14 +681,14 @@ Scales scales_of(const cerar_fp8_matrix_t& m, bool rows_are_k) {
     return rows_are_k ? Scales{m.scales, 1, m.lds, 7} : Scales{m.scales, m.lds, 1, 7};
 }
 
-template <int BN, bool BVEC, typename C>
-cudaError_t launch_one(const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, int grid, cudaStream_t s) {
-    auto kern = fp8_matmul_kernel<BN, BVEC, C>;
+typedef void (*Kernel)(CUtensorMap, CUtensorMap, Params);
+
+cudaError_t launch_one(Kernel kern, int BN, int threads, const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, int grid, cudaStream_t s) {
     const size_t smem = 1024 + (size_t)p.stages * (A_BYTES + BN * BK) + EPI_WARPS * STAGING + 512;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = g_tune_pdl_off ? 0 : 1;
@@ -453,10 +697,9 @@ cudaError_t launch_one(const CUtensorMap& ma, const CUtensorMap& mb, const Param
     cfg.attrs = attr; cfg.numAttrs = p.split > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, ma, mb, p);
 }
-template <int BN>
-cudaError_t launch_bn(const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, bool bvec, int type, int grid, cudaStream_t s) {
-    if (type == CERAR_TYPE_F32) return bvec ? launch_one<BN, true, float>(ma, mb, p, grid, s) : launch_one<BN, false, float>(ma, mb, p, grid, s);
-    return bvec ? launch_one<BN, true, __nv_bfloat16>(ma, mb, p, grid, s) : launch_one<BN, false, __nv_bfloat16>(ma, mb, p, grid, s);
+template <int BN, typename C>
+Kernel kernel_for(bool pow2, bool bvec) {
+    return pow2 ? fp8_matmul_pow2_kernel<BN, C> : bvec ? fp8_matmul_kernel<BN, true, C> : fp8_matmul_kernel<BN, false, C>;
 }
 
 }  // namespace
@@ -470,10 +713,11 @@ cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, 
     const bool wide = (int64_t)p.tiles_m * ((p.N + 255) / 256) >= num_sms;
     const int BN = wide ? 256 : 128;
     p.tiles_n = (p.N + BN - 1) / BN;
-    p.tiles = (int64_t)p.tiles_m * p.tiles_n;
+    if ((int64_t)p.tiles_m * p.tiles_n > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+    p.tiles = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n;
     p.split = 1;
     if (!wide)
-        while (p.split < 8 && p.tiles * p.split * 2 <= num_sms && p.split * 4 <= p.kblocks) p.split *= 2;
+        while (p.split < 8 && (int)p.tiles * p.split * 2 <= num_sms && p.split * 4 <= p.kblocks) p.split *= 2;
     p.group_m = 16;
     p.stages = wide ? 4 : 6;
     p.a_mn = a.trans_a; p.b_mn = !a.trans_b;
@@ -484,9 +728,11 @@ cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, 
     p.c_vec = (reinterpret_cast<uintptr_t>(a.C) & 15u) == 0 && (a.ldc * size) % 16 == 0;
     CUtensorMap ma, mb;
     if (!make_map_8bit(&ma, a.A, BM) || !make_map_8bit(&mb, a.B, p.b_mn ? BK : BN)) return cudaErrorInvalidValue;
-    const int64_t grid = p.split > 1 ? p.tiles * p.split : p.tiles < num_sms ? p.tiles : num_sms;
-    const bool bvec = a.B.scaling != CERAR_BY_BLOCK;
-    const cudaError_t e = wide ? launch_bn<256>(ma, mb, p, bvec, a.type, (int)grid, s) : launch_bn<128>(ma, mb, p, bvec, a.type, (int)grid, s);
+    const int grid = p.split > 1 ? (int)p.tiles * p.split : (int)p.tiles < num_sms ? (int)p.tiles : num_sms;
+    const bool bvec = a.B.scaling != CERAR_BY_BLOCK, pow2 = a.A.pow2 && a.B.pow2;
+    const Kernel kern = a.type == CERAR_TYPE_F32 ? (wide ? kernel_for<256, float>(pow2, bvec) : kernel_for<128, float>(pow2, bvec))
+                                                 : (wide ? kernel_for<256, __nv_bfloat16>(pow2, bvec) : kernel_for<128, __nv_bfloat16>(pow2, bvec));
+    const cudaError_t e = launch_one(kern, BN, pow2 ? POW2_THREADS : THREADS, ma, mb, p, grid, s);
     if (e == cudaSuccess) ++*launches;
     return e;
 }

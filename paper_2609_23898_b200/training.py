@@ -55,11 +55,15 @@ def _ld(t: torch.Tensor) -> int:
 
 class Quantized:
     """An 8-bit matrix: `codes` (rows x cols, float8_e4m3fn or uint8, rows a multiple of 16 bytes apart), `scales` (float32,
-    [ceil(cols/128), rows] by row, [ceil(rows/128), cols] by column, [ceil(rows/128), ceil(cols/128)] by block)."""
+    [ceil(cols/128), rows] by row, [ceil(rows/128), cols] by column, [ceil(rows/128), ceil(cols/128)] by block).
+
+    pow2: whether all scales are powers of two, as Ops.quantize makes them: products of two such matrices are faster.  None: the
+    scales are read once, here, to see (which waits for the device).  Scales that are changed later have to keep to it:
+    what they touch becomes NaN otherwise."""
 
     __slots__ = ("codes", "scales", "scaling", "desc")
 
-    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, scaling: int):
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, scaling: int, pow2: bool | None = None):
         if codes.element_size() != 1:
             raise TypeError("codes: float8_e4m3fn or uint8 wanted")
         _matrix(codes, "codes"), _matrix(scales, "scales")
@@ -73,11 +77,14 @@ class Quantized:
         if tuple(scales.shape) != want:
             raise ValueError(f"scales of shape {want} wanted, got {tuple(scales.shape)}")
         ld = codes.stride(0) if rows > 1 else -(-max(codes.stride(0), cols) // 16) * 16
-        self._set(codes, scales, scaling, rows, cols, ld, _ld(scales))
+        if pow2 is None:
+            bits = scales.contiguous().view(torch.int32)
+            pow2 = bool(((bits & 0x7FFFFF == 0) & (bits >= 1 << 23) & (bits < 255 << 23)).all())
+        self._set(codes, scales, scaling, rows, cols, ld, _ld(scales), pow2)
 
-    def _set(self, codes, scales, scaling, rows, cols, ld, lds):
+    def _set(self, codes, scales, scaling, rows, cols, ld, lds, pow2):
         self.codes, self.scales, self.scaling = codes, scales, scaling
-        self.desc = Fp8Matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, lds, scaling)
+        self.desc = Fp8Matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, lds, scaling, pow2)
 
     @classmethod
     def empty(cls, rows: int, cols: int, scaling: int, device) -> "Quantized":
@@ -86,7 +93,7 @@ class Quantized:
         shape = (nc, rows) if scaling == BY_ROW else (nr, cols) if scaling == BY_COLUMN else (nr, nc)
         codes = torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=device)
         q = cls.__new__(cls)
-        q._set(codes if ld == cols else codes[:, :cols], torch.empty(shape, dtype=torch.float32, device=device), scaling, rows, cols, ld, shape[1])
+        q._set(codes if ld == cols else codes[:, :cols], torch.empty(shape, dtype=torch.float32, device=device), scaling, rows, cols, ld, shape[1], True)
         return q
 
     @property

@@ -112,8 +112,8 @@ def test_quantize_writes_nothing_else(ops):
 
 # ---------------------------------------------------------------------------------------------------- products
 
-def random_matrix(rng, rows, cols, scaling, nan=()):
-    """A Quantized with codes over the whole format and arbitrary positive scales, and its 64-bit values."""
+def random_matrix(rng, rows, cols, scaling, nan=(), pow2=False):
+    """A Quantized with codes over the whole format and positive scales (any, or powers of two), and its 64-bit values."""
     from paper_2609_23898_b200 import training as R
     import torch
     codes = np.delete(np.arange(256), [0x7F, 0xFF])[rng.integers(0, 254, (rows, cols))].astype(np.uint8)
@@ -122,7 +122,8 @@ def random_matrix(rng, rows, cols, scaling, nan=()):
         codes[r, c] = 0x7F
     nr, nc = -(-rows // 128), -(-cols // 128)
     shape = {0: (nc, rows), 1: (nr, cols), 2: (nr, nc)}[scaling]
-    scales = (2.0 ** rng.uniform(-6, 3, shape)).astype(np.float32)
+    e = rng.uniform(-6, 3, shape)
+    scales = (2.0 ** (np.floor(e) if pow2 else e)).astype(np.float32)
     ld = -(-cols // 16) * 16 + 16 * int(rng.integers(0, 3))
     buf = torch.full((rows, ld), 0x7F, dtype=torch.uint8, device="cuda")      # NaN between the rows: must not be read as data
     buf[:, :cols] = dev(codes)
@@ -141,26 +142,29 @@ def product_bound(a, b, blocks, c64, bf16):
 @pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 1, 128), (1, 300, 2048), (5, 64, 100), (128, 256, 128), (127, 255, 129), (129, 257, 127), (64, 1031, 300),
                                    (333, 200, 1000), (256, 512, 384), (700, 900, 640), (2, 2500, 16), (1500, 3, 272), (130, 130, 4100), (16, 16, 20000)])
 @pytest.mark.parametrize("trans_a,trans_b", [(False, True), (False, False), (True, False), (True, True)])
-def test_product(ops, m, n, k, trans_a, trans_b):
+@pytest.mark.parametrize("pow2", [False, True])
+def test_product(ops, m, n, k, trans_a, trans_b, pow2):
     import torch
     rng = np.random.default_rng(m * 7 + n * 3 + k + 2 * trans_a + trans_b)
     for a_block, b_block, bf16 in ((False, False, False), (False, True, True), (True, False, True), (True, True, False)):
-        A, a = random_matrix(rng, *((k, m) if trans_a else (m, k)), 2 if a_block else int(trans_a))
-        B, b = random_matrix(rng, *((n, k) if trans_b else (k, n)), 2 if b_block else int(not trans_b))
+        A, a = random_matrix(rng, *((k, m) if trans_a else (m, k)), 2 if a_block else int(trans_a), pow2=pow2)
+        B, b = random_matrix(rng, *((n, k) if trans_b else (k, n)), 2 if b_block else int(not trans_b), pow2=pow2)
+        assert A.desc.pow2 == B.desc.pow2 == int(pow2)
         a, b = (a.T if trans_a else a), (b.T if trans_b else b)
         c64 = a @ b
         c = ops.matmul(A, B, trans_a=trans_a, trans_b=trans_b, dtype=torch.bfloat16 if bf16 else torch.float32)
         assert (np.abs(f64(c) - c64) <= product_bound(a, b, -(-k // 128), c64, bf16)).all(), (a_block, b_block)
 
 
+@pytest.mark.parametrize("pow2", [False, True])
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("m,n,k,ldc,offset", [(128, 256, 256, 256, 0), (200, 130, 300, 137, 3), (1, 77, 128, 77, 1), (300, 260, 2000, 264, 8), (257, 128, 136, 130, 2)])
-def test_product_accumulates_into_a_strided_buffer(ops, m, n, k, ldc, offset, bf16):
+def test_product_accumulates_into_a_strided_buffer(ops, m, n, k, ldc, offset, bf16, pow2):
     """C + A B; what lies between the rows of C and around it stays; twice the same bits."""
     import torch
     rng = np.random.default_rng(m + n)
-    A, a = random_matrix(rng, k, m, 1)
-    B, b = random_matrix(rng, k, n, 1)
+    A, a = random_matrix(rng, k, m, 1, pow2=pow2)
+    B, b = random_matrix(rng, k, n, 1, pow2=pow2)
     dt = torch.bfloat16 if bf16 else torch.float32
     start = torch.randn(m * ldc + offset + 64, device="cuda").to(dt) * 100
     runs = []
@@ -179,16 +183,44 @@ def test_product_accumulates_into_a_strided_buffer(ops, m, n, k, ldc, offset, bf
     assert torch.equal(runs[0][mask], start[mask])
 
 
-def test_product_nan_stays_in_its_row_and_column(ops):
+@pytest.mark.parametrize("pow2", [False, True])
+def test_product_nan_stays_in_its_row_and_column(ops, pow2):
     import torch
     rng = np.random.default_rng(5)
-    A, a = random_matrix(rng, 300, 500, 0, nan=[(7, 3), (299, 499)])
-    B, b = random_matrix(rng, 400, 500, 2, nan=[(11, 250)])
+    A, a = random_matrix(rng, 300, 500, 0, nan=[(7, 3), (299, 499)], pow2=pow2)
+    B, b = random_matrix(rng, 400, 500, 2, nan=[(11, 250)], pow2=pow2)
     c = f64(ops.matmul(A, B, trans_b=True, dtype=torch.float32))
     want = np.zeros((300, 400), bool)
     want[[7, 299], :] = True
     want[:, 11] = True
     assert np.array_equal(np.isnan(c), want)
+
+
+def test_product_scale_that_is_no_power_of_two_after_all(ops):
+    """Declared powers of two, one scale changed afterwards: its row, and nothing else, is NaN."""
+    import torch
+    rng = np.random.default_rng(6)
+    A, a = random_matrix(rng, 200, 700, 0, pow2=True)
+    B, b = random_matrix(rng, 300, 700, 2, pow2=True)
+    A.scales[3, 77] = 0.75
+    c = f64(ops.matmul(A, B, trans_b=True, dtype=torch.float32))
+    want = np.zeros((200, 300), bool)
+    want[77] = True
+    assert np.array_equal(np.isnan(c), want)
+
+
+def test_product_extreme_scales(ops):
+    """Scales at the ends of what the conversion writes (2^-100, 2^100), whose products leave the range of one side only."""
+    import torch
+    rng = np.random.default_rng(8)
+    A, a = random_matrix(rng, 130, 300, 0, pow2=True)
+    B, b = random_matrix(rng, 140, 300, 0, pow2=True)
+    A.scales[:, :65], A.scales[:, 65:] = 2.0 ** 100, 2.0 ** -100
+    B.scales.fill_(2.0 ** -20)
+    a, b = f64(A.dequantize()), f64(B.dequantize())
+    c64 = a @ b.T
+    c = f64(ops.matmul(A, B, trans_b=True, dtype=torch.float32))
+    assert (np.abs(c - c64) <= product_bound(a, b.T, 3, c64, False)).all()
 
 
 def test_product_of_nothing(ops):
