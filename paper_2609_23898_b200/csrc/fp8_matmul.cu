@@ -67,6 +67,30 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+// The bounded wait of this file: an attempt lets the warp sleep until the phase is there or about 20 us have passed, so that
+// waiting warps leave the issue slots and the shared-memory port to the others; the timer is looked at after the first attempt.
+__device__ __forceinline__ bool try_wait_asleep(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool wait_soon(uint32_t bar, uint32_t parity) {
+    unsigned long long start = 0;
+    for (;;) {
+        for (int i = 0; i < 16; ++i)
+            if (try_wait_asleep(bar, parity)) return true;
+        const unsigned long long now = global_ns();
+        if (start == 0) start = now;
+        else if (now - start > WAIT_LIMIT_NS) return false;
+    }
+}
+__device__ __forceinline__ bool warp_wait_soon(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_soon(bar, parity) ? 1 : 0) != 0; }
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r;
+}
 __device__ __forceinline__ void mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
                  " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
@@ -87,15 +111,14 @@ __device__ __forceinline__ void ld32_start(uint32_t taddr, uint32_t* r) {
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
           "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
           "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr) : "memory");
+        : "r"(taddr));
 }
 __device__ __forceinline__ void ld32_done(uint32_t* r) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
         : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
           "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
           "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
-          "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29])  : : "memory");
-    asm volatile("" : "+r"(r[30]), "+r"(r[31]) : : "memory");
+          "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
 // two sums at a time (one instruction): a += x * y
 __device__ __forceinline__ uint64_t pair(uint32_t x, uint32_t y) {
@@ -154,9 +177,9 @@ template <> struct Out<__nv_bfloat16> {
 };
 
 // Rows row0 .. row0 + 31 (those below M) of C, columns col0 .. col0 + n - 1 of a slab of 128 bytes per row: the warp holds row
-// (lane)'s values in v[0 .. SLAB).  With accumulate the slab of C is read and added in binary32 before the one rounding.
+// (lane)'s values in v[0 .. SLAB) (flip = 4: of a slab of 64 columns the second 32 come first in v).  With accumulate the slab of C is read and added in binary32 before the one rounding.
 template <typename C>
-__device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, int row0, int col0, const float* v) {
+__device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, int row0, int col0, const float* v, int flip = 0) {
     constexpr int PER16 = Out<C>::PER16, SLAB = 8 * PER16;
     const int lane = threadIdx.x & 31;
     const int nrows = p.M - row0 < 32 ? p.M - row0 : 32, n = p.N - col0 < SLAB ? p.N - col0 : SLAB;
@@ -167,7 +190,7 @@ __device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, in
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint4 q = Out<C>::pack(v + j * PER16);
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((j ^ flip ^ (lane & 7)) << 4)), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
         }
         __syncwarp();
         if (p.c_vec && n == SLAB) {
@@ -198,6 +221,7 @@ __device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, in
         // binary32 through the staging rows, 32 columns at a time
 #pragma unroll
         for (int h = 0; h < SLAB / 32; ++h) {
+            const int hc = (h ^ (flip >> 2)) * 32;                         // first column of these 32
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -211,7 +235,7 @@ __device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, in
 #pragma unroll
                 for (int it = 0; it < 8; ++it) {
                     const int r = it * 4 + (lane >> 3), j = lane & 7;
-                    const C* src = c + (int64_t)(row0 + r) * p.ldc + col0 + h * 32 + j * 4;
+                    const C* src = c + (int64_t)(row0 + r) * p.ldc + col0 + hc + j * 4;
                     if (r < nrows) {
                         if constexpr (W == 4) *reinterpret_cast<uint4*>(old[it]) = *reinterpret_cast<const uint4*>(src);
                         else *reinterpret_cast<uint2*>(old[it]) = *reinterpret_cast<const uint2*>(src);
@@ -223,7 +247,7 @@ __device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, in
                     float4 q;
                     asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
                     if (r < nrows) {
-                        C* dst = c + (int64_t)(row0 + r) * p.ldc + col0 + h * 32 + j * 4;
+                        C* dst = c + (int64_t)(row0 + r) * p.ldc + col0 + hc + j * 4;
                         if constexpr (sizeof(C) == 4) {
                             *reinterpret_cast<float4*>(dst) = make_float4(__uint_as_float(old[it][0]) + q.x, __uint_as_float(old[it][1]) + q.y,
                                                                           __uint_as_float(old[it][2]) + q.z, __uint_as_float(old[it][3]) + q.w);
@@ -236,7 +260,7 @@ __device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, in
                     }
                 }
             } else {
-                const int e = h * 32 + lane;
+                const int e = hc + lane;
                 for (int r = 0; r < nrows; ++r) {
                     float q;
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(q) : "r"(staging + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
@@ -262,7 +286,7 @@ __device__ __forceinline__ void produce(const Params& p, const CUtensorMap& map_
         const int m0 = tm * BM, n0 = tn * BN;
         for (int kb = kb0; kb < kb1; ++kb, ++it) {
             const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u;
-            if (!mbar_wait_bounded(empty + 8u * s, ph ^ 1u)) { failed = true; break; }
+            if (!wait_soon(empty + 8u * s, ph ^ 1u)) { failed = true; break; }
             const uint32_t a = smem + s * STAGE, b = a + A_BYTES, bar = full + 8u * s;
             mbar_arrive_expect_tx(bar, STAGE);
             if (p.a_mn) tma_load_2d(a, &map_a, m0, kb * BK, bar);
@@ -313,6 +337,7 @@ __device__ __forceinline__ void add_partials(const Params& p, uint32_t smem, uin
 }
 
 // The common exit: every warp comes here, whatever it waited for in vain.
+template <int CG = 1>
 __device__ __forceinline__ void leave(const Params& p, bool failed, int warp, int lane, uint32_t tmem) {
     if (failed) {
         if (lane == 0) atomicExch(p.status, 2);
@@ -324,7 +349,8 @@ __device__ __forceinline__ void leave(const Params& p, bool failed, int warp, in
     __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        tc_dealloc(tmem, 512u);
+        if constexpr (CG == 1) tc_dealloc(tmem, 512u);
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
 }
 
@@ -366,24 +392,31 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         if (warp == 0) {
             if (lane == 0) produce<BN>(p, map_a, map_b, smem, full, empty, t0, tstep, kb0, kb1, failed);
         } else if (warp == 1) {
-            if (lane == 0) {
-                // D binary32, A and B e4m3, M = 128, N = BN
-                const uint32_t idesc = (1u << 4) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) | ((128u >> 4) << 24);
-                // 32 values of k further: 32 bytes in a row of k, or 32 rows of 128 bytes
-                const uint64_t a_step = p.a_mn ? (32u * 128u) >> 4 : 32u >> 4, b_step = p.b_mn ? (32u * 128u) >> 4 : 32u >> 4;
-                uint32_t it = 0;
-                for (uint32_t t = t0; t < p.tiles && !failed; t += tstep)
-                    for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                        const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u, buf = it % NBUF, bph = (it / NBUF) & 1u;
-                        if (!mbar_wait_bounded(acc_empty + 8u * buf, bph ^ 1u) || !mbar_wait_bounded(full + 8u * s, ph)) { failed = true; break; }
-                        tc_fence_after();
-                        const uint64_t da = swizzled_desc(smem + s * STAGE), db = swizzled_desc(smem + s * STAGE + A_BYTES);
-    #pragma unroll
+            // The whole warp goes through the loop and one lane issues: everything the products are made from is then the same in all
+            // lanes, as far as the compiler can see too, and stays in uniform registers, which is where the instruction takes
+            // its operands from (a lone lane moves them there one by one, product by product).
+            const uint32_t one = elect_one();
+            // D binary32, A and B e4m3, M = 128, N = BN
+            const uint32_t idesc = (1u << 4) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) | ((128u >> 4) << 24);
+            // 32 values of k further: 32 bytes in a row of k, or 32 rows of 128 bytes
+            const uint64_t a_step = p.a_mn ? (32u * 128u) >> 4 : 32u >> 4, b_step = p.b_mn ? (32u * 128u) >> 4 : 32u >> 4;
+            const uint64_t desc0 = swizzled_desc(smem);
+            uint32_t s = 0, ph = 0, buf = 0, bph = 1;
+            for (uint32_t t = t0; t < p.tiles && !failed; t += tstep)
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!warp_wait_soon(acc_empty + 8u * buf, bph) || !warp_wait_soon(full + 8u * s, ph)) { failed = true; break; }
+                    tc_fence_after();
+                    const uint64_t da = desc0 + (uint64_t)(s * (STAGE >> 4)), db = da + (A_BYTES >> 4);
+                    if (one) {
+#pragma unroll
                         for (int k = 0; k < BK / 32; ++k) mma_f8(tmem + buf * BN, da + k * a_step, db + k * b_step, idesc, k != 0);
                         tc_commit(empty + 8u * s);
                         tc_commit(acc_full + 8u * buf);
                     }
-            }
+                    __syncwarp();
+                    if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+                    if (++buf == NBUF) { buf = 0; bph ^= 1u; }
+                }
         }
         __syncwarp();
         if (p.split > 1) { cluster_sync(); cluster_sync(); }
@@ -426,7 +459,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     for (int j = 0; j < CW / 32; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(staging + 4u * (j * 32 + lane)), "f"(bv[j]) : "memory");
                     __syncwarp();
                 }
-                if (!warp_wait(acc_full + 8u * buf, bph)) { failed = true; break; }
+                if (!warp_wait_soon(acc_full + 8u * buf, bph)) { failed = true; break; }
                 tc_fence_after();
                 // the next 32 columns are on their way while these are added
                 uint32_t v[2][32];
@@ -447,7 +480,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     for (int j = 0; j < 32; j += 4) {
                         if constexpr (BVEC) {
                             uint64_t q0, q1;
-                            asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(q0), "=l"(q1) : "r"(staging + 4u * (c * 32 + j)) : "memory");
+                            asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(q0), "=l"(q1) : "r"(staging + 4u * (c * 32 + j)));
                             fma_pair(acc2[c * 16 + j / 2], mul_pair(s, pair(x[j], x[j + 1])), q0);
                             fma_pair(acc2[c * 16 + j / 2 + 1], mul_pair(s, pair(x[j + 2], x[j + 3])), q1);
                         } else {
@@ -489,29 +522,65 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 // all four lane quadrants; a 32-bit word holds those of four blocks of k, which the instruction picks from by number.
 //
 //   warp 0       producer, warp 1 issues the products, as above
-//   warps 4-7    read the scales four blocks ahead, put their exponents into tensor memory.  A scale that is no power of two
+//   warps 4-7    read the scales of four blocks of k (a warp each, a group ahead), exchange their exponents through shared
+//                memory and put them into tensor memory, every warp into its quadrant.  A scale that is no power of two
 //                (the caller said they all are) becomes the exponent that means NaN, and so do the results it touches
 //   warps 8-15   write the tile of C
 // Two accumulators of 256 columns and the exponents do not fit into 512 columns: the accumulators overlap by 32 columns,
 // which are written out first; the products of the next tile wait for those only.
 constexpr int POW2_THREADS = 512, WARP_SCALE0 = 4, WARP_OUT0 = 8;
+// registers per thread: 128 x 56 + 128 x 72 + 256 x 192 = 512 x 128, what the block is launched with
+constexpr int POW2_REGS_ISSUE = 56, POW2_REGS_SCALE = 72, POW2_REGS_OUT = 192;
+// blocks of k that stay in the accumulator: it drops what does not fit its 24 bits instead of rounding, an error that
+// grows with every addition (K = 16384: 1.2e-6 of a sum's norm), so longer sums are put together in registers
+constexpr int SEGMENT = 16;
+constexpr uint32_t SF_WORDS = 12 * 128;                  // shared memory of the exponents of a group
 constexpr uint32_t SF_COL = 480, SF_BUF = 16;            // exponents: two buffers of 4 (A) and, 8 further, 8 (B) columns
 
+template <int CG>
 __device__ __forceinline__ void mma_mxf8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
-                 " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+    if constexpr (CG == 1)
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+                     " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+                     " tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+// a barrier of this block (CG = 1), or the one at the same place in both blocks of the pair
+template <int CG>
+__device__ __forceinline__ void commit(uint32_t bar) {
+    if constexpr (CG == 1) tc_commit(bar);
+    else asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ uint32_t in_block(uint32_t saddr, uint32_t rank) {     // the same place in the shared memory of another block of the cluster
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
+    return r;
+}
+template <int CG>
+__device__ __forceinline__ void arrive(uint32_t bar) {                            // CG = 2: an address from in_block
+    if constexpr (CG == 1) mbar_arrive(bar);
+    else asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void tma_load_operand(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    if constexpr (CG == 1) tma_load_2d(dst, map, x, y, bar);
+    else asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 __device__ __forceinline__ uint32_t exponent_of(float s) {
     const uint32_t b = __float_as_uint(s), e = b >> 23;
     return (b & 0x807FFFFFu) == 0u && e >= 1u && e <= 254u ? e : 0xFFu;
 }
 
-template <int BN, typename C>
+template <int CG, int BN, typename C>
 __global__ void __launch_bounds__(POW2_THREADS, 1)
 fp8_matmul_pow2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Params p) {
-    constexpr int CW = BN / 2;
-    constexpr uint32_t B_BYTES = BN * BK, STAGE = A_BYTES + B_BYTES;
+    constexpr int CW = BN / 2;                           // columns per output warp
+    constexpr int B_ROWS = BN / CG;                      // of the tile of B, in this block
+    constexpr uint32_t STAGE = A_BYTES + B_ROWS * BK;
     constexpr uint32_t OVERLAP = BN == 256 ? 32 : 0, D1 = BN - OVERLAP;       // first column of the second accumulator
     constexpr int SLAB = 8 * Out<C>::PER16;
     extern __shared__ unsigned char smem_dyn[];
@@ -525,63 +594,116 @@ fp8_matmul_pow2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8u * s, 1); mbar_init(empty + 8u * s, 1); }
         for (int b = 0; b < 2; ++b) {
-            mbar_init(acc_full + 8u * b, 1); mbar_init(acc_empty + 8u * b, EPI_WARPS);
-            mbar_init(sf_full + 8u * b, 4); mbar_init(sf_empty + 8u * b, 1);
+            mbar_init(acc_full + 8u * b, 1); mbar_init(acc_empty + 8u * b, CG * EPI_WARPS);
+            mbar_init(sf_full + 8u * b, CG * 4); mbar_init(sf_empty + 8u * b, 1);
         }
-        mbar_init(over_empty, EPI_WARPS / 2);
+        mbar_init(over_empty, CG * EPI_WARPS / 2);
         mbar_init_fence();
     }
-    if (warp == 1) tc_alloc(slot, 512u);
+    if (warp == 1) {
+        if constexpr (CG == 1) {
+            tc_alloc(slot, 512u);
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(512u) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+    }
     tc_fence_before();
     __syncthreads();
+    if constexpr (CG == 2) cluster_sync();               // the other block's barriers are there before anything is sent to them
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
     grid_dependency_wait();
 
-    const int rank = p.split > 1 ? (int)cluster_rank() : 0;
-    const uint32_t t0 = blockIdx.x / p.split, tstep = gridDim.x / p.split;
+    // a cluster is a pair of blocks that share a tile of 256 rows (CG = 2), or `split` blocks that share the sum of a tile
+    const int crank = CG == 2 || p.split > 1 ? (int)cluster_rank() : 0;
+    const int pair_rank = CG == 2 ? crank : 0, rank = CG == 2 ? 0 : crank;
+    const uint32_t csize = CG == 2 ? 2 : p.split;
+    const uint32_t t0 = blockIdx.x / csize, tstep = gridDim.x / csize;
     const int kb0 = (int)((int64_t)p.kblocks * rank / p.split), kb1 = (int)((int64_t)p.kblocks * (rank + 1) / p.split);
     bool failed = false;
 
-    if (warp == 0) {
-        if (lane == 0) produce<BN>(p, map_a, map_b, smem, full, empty, t0, tstep, kb0, kb1, failed);
-    } else if (warp == 1) {
-        if (lane == 0) {
-            // exponents of 8 bits, A and B e4m3, M = 128, N = BN
-            const uint32_t idesc0 = (1u << 23) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) | ((128u >> 4) << 24);
-            const uint64_t a_step = p.a_mn ? (32u * 128u) >> 4 : 32u >> 4, b_step = p.b_mn ? (32u * 128u) >> 4 : 32u >> 4;
-            uint32_t it = 0, tile = 0, group = 0;
-            for (uint32_t t = t0; t < p.tiles && !failed; t += tstep, ++tile) {
-                const uint32_t buf = tile & 1u;
-                if (!mbar_wait_bounded(acc_empty + 8u * buf, ((tile >> 1) & 1u) ^ 1u)) { failed = true; break; }
-                if (OVERLAP && !mbar_wait_bounded(over_empty, (tile & 1u) ^ 1u)) { failed = true; break; }
-                tc_fence_after();
-                const uint32_t d = tmem + buf * D1;
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u, id = (uint32_t)(kb - kb0) & 3u, sbuf = group & 1u;
-                    if (id == 0u && !mbar_wait_bounded(sf_full + 8u * sbuf, (group >> 1) & 1u)) { failed = true; break; }
-                    if (!mbar_wait_bounded(full + 8u * s, ph)) { failed = true; break; }
-                    tc_fence_after();
-                    const uint64_t da = swizzled_desc(smem + s * STAGE), db = swizzled_desc(smem + s * STAGE + A_BYTES);
-                    const uint32_t sf = tmem + SF_COL + sbuf * SF_BUF, idesc = idesc0 | (id << 4) | (id << 29);
+    if (warp < WARP_SCALE0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(POW2_REGS_ISSUE));
+        if (warp == 0) {
+            if (lane == 0) {
+                uint32_t it = 0;
+                for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
+                    int tm, tn;
+                    tile_of(p, t, tm, tn);
+                    const int m0 = (tm * CG + pair_rank) * BM, n0 = tn * BN + pair_rank * B_ROWS;
+                    for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                        const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u;
+                        if (!wait_soon(empty + 8u * s, ph ^ 1u)) { failed = true; break; }
+                        const uint32_t a = smem + s * STAGE, b = a + A_BYTES;
+                        if (pair_rank == 0) mbar_arrive_expect_tx(full + 8u * s, CG * STAGE);       // what both blocks load
+                        const uint32_t bar = CG == 1 ? full + 8u * s : in_block(full + 8u * s, 0);
+                        if (p.a_mn) tma_load_operand<CG>(a, &map_a, m0, kb * BK, bar);
+                        else tma_load_operand<CG>(a, &map_a, kb * BK, m0, bar);
+                        if (p.b_mn) {
 #pragma unroll
-                    for (int k = 0; k < BK / 32; ++k) mma_mxf8(d, da + k * a_step, db + k * b_step, idesc, sf, sf + 8, kb != kb0 || k != 0);
-                    tc_commit(empty + 8u * s);
-                    if (id == 3u || kb + 1 == kb1) { tc_commit(sf_empty + 8u * sbuf); ++group; }
+                            for (int j = 0; j < B_ROWS / 128; ++j) tma_load_operand<CG>(b + j * (128 * BK), &map_b, n0 + j * 128, kb * BK, bar);
+                        } else {
+                            tma_load_operand<CG>(b, &map_b, kb * BK, n0, bar);
+                        }
+                    }
                 }
-                if (!failed) tc_commit(acc_full + 8u * buf);
+            }
+        } else if (warp == 1) {
+            if (pair_rank == 0) {                        // (the whole warp, one lane issuing: see above)
+                const uint32_t one = elect_one();
+                // exponents of 8 bits, A and B e4m3, M = 128 CG, N = BN
+                const uint32_t idesc0 = (1u << 23) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(CG * BM >> 4) << 24);
+                const uint64_t a_step = p.a_mn ? (32u * 128u) >> 4 : 32u >> 4, b_step = p.b_mn ? (32u * 128u) >> 4 : 32u >> 4;
+                const uint64_t desc0 = swizzled_desc(smem);
+                uint32_t s = 0, ph = 0, seg = 0, group = 0;
+                for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
+                    uint32_t id = 0;                     // block of k within its group of four
+                    for (int k0 = kb0; k0 < kb1 && !failed; k0 += SEGMENT, ++seg) {
+                        const uint32_t buf = seg & 1u;
+                        if (!warp_wait_soon(acc_empty + 8u * buf, ((seg >> 1) & 1u) ^ 1u)) { failed = true; break; }
+                        if (OVERLAP && !warp_wait_soon(over_empty, (seg & 1u) ^ 1u)) { failed = true; break; }
+                        const uint32_t d = tmem + buf * D1;
+                        const int k1 = k0 + SEGMENT < kb1 ? k0 + SEGMENT : kb1;
+                        for (int kb = k0; kb < k1; ++kb) {
+                            const uint32_t sbuf = group & 1u;
+                            if (id == 0u && !warp_wait_soon(sf_full + 8u * sbuf, (group >> 1) & 1u)) { failed = true; break; }
+                            if (!warp_wait_soon(full + 8u * s, ph)) { failed = true; break; }
+                            tc_fence_after();
+                            const uint64_t da = desc0 + (uint64_t)(s * (STAGE >> 4)), db = da + (A_BYTES >> 4);
+                            const uint32_t sf = tmem + SF_COL + sbuf * SF_BUF, idesc = idesc0 | (id << 4) | (id << 29);
+                            const bool last = id == 3u || kb + 1 == kb1;
+                            if (one) {
+#pragma unroll
+                                for (int k = 0; k < BK / 32; ++k) mma_mxf8<CG>(d, da + k * a_step, db + k * b_step, idesc, sf, sf + 8, kb != k0 || k != 0);
+                                commit<CG>(empty + 8u * s);
+                                if (last) commit<CG>(sf_empty + 8u * sbuf);
+                                if (kb + 1 == k1) commit<CG>(acc_full + 8u * buf);
+                            }
+                            __syncwarp();
+                            if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+                            if (last) ++group;
+                            id = (id + 1) & 3u;
+                        }
+                    }
+                }
             }
         }
-    } else if (warp >= WARP_SCALE0 && warp < WARP_OUT0) {
+    } else if (warp < WARP_OUT0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(POW2_REGS_SCALE));
+        constexpr int NW = 4 + BN / 32;                  // words of exponents per lane
+        const uint32_t ready = CG == 1 ? sf_full : in_block(sf_full, 0), words = slot + 16u;
         uint32_t group = 0;
-        for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
+        for (uint32_t t = t0; t < p.tiles; t += tstep) {
             int tm, tn;
             tile_of(p, t, tm, tn);
+            // this lane's rows and columns; warp w reads block w of every group of four, one group ahead
             const float *a[4], *b[BN / 32];
+            const int w = warp - WARP_SCALE0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int m = tm * BM + j * 32 + lane;
+                const int m = (tm * CG + pair_rank) * BM + j * 32 + lane;
                 a[j] = p.sa.p + (int64_t)((m < p.M ? m : p.M - 1) >> p.sa.shift) * p.sa.si;
             }
 #pragma unroll
@@ -589,90 +711,107 @@ fp8_matmul_pow2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                 const int n = tn * BN + j * 32 + lane;
                 b[j] = p.sb.p + (int64_t)((n < p.N ? n : p.N - 1) >> p.sb.shift) * p.sb.si;
             }
+            float x[NW];
+            auto load = [&](int kb) {
+                const int k = kb + w < kb1 ? kb + w : kb1 - 1;
+#pragma unroll
+                for (int j = 0; j < NW; ++j) x[j] = j < 4 ? __ldg(a[j < 4 ? j : 0] + k * p.sa.sb) : __ldg(b[j < 4 ? 0 : j - 4] + k * p.sb.sb);
+            };
+            load(kb0);
             for (int kb = kb0; kb < kb1; kb += 4, ++group) {
-                uint32_t ea[4] = {}, eb[BN / 32] = {};
-                float x[4][4 + BN / 32];
+                bar_sync(1, 128);                        // the words of the group before have been read
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = kb + i < kb1 ? kb + i : kb1 - 1;
+                for (int j = 0; j < NW; ++j)
+                    asm volatile("st.shared.u8 [%0], %1;" ::"r"(words + (uint32_t)(j * 128 + lane * 4 + w)), "r"(exponent_of(x[j])) : "memory");
+                if (kb + 4 < kb1) load(kb + 4);
+                bar_sync(1, 128);
+                uint32_t e[NW];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[i][j] = __ldg(a[j] + k * p.sa.sb);
-#pragma unroll
-                    for (int j = 0; j < BN / 32; ++j) x[i][4 + j] = __ldg(b[j] + k * p.sb.sb);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) ea[j] |= exponent_of(x[i][j]) << (8 * i);
-#pragma unroll
-                    for (int j = 0; j < BN / 32; ++j) eb[j] |= exponent_of(x[i][4 + j]) << (8 * i);
-                }
+                for (int j = 0; j < NW; ++j) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(e[j]) : "r"(words + (uint32_t)(j * 128 + lane * 4)) : "memory");
                 const uint32_t sbuf = group & 1u;
-                if (!warp_wait(sf_empty + 8u * sbuf, ((group >> 1) & 1u) ^ 1u)) { failed = true; break; }
+                if (!failed && !warp_wait_soon(sf_empty + 8u * sbuf, ((group >> 1) & 1u) ^ 1u)) failed = true;     // (goes on for the barriers' sake)
                 tc_fence_after();
                 const uint32_t to = tmem + ((uint32_t)((warp & 3) * 32) << 16) + SF_COL + sbuf * SF_BUF;
-                tc_st_cols<4>(to, ea);
-                tc_st_cols<BN / 32>(to + 8, eb);
+                tc_st_cols<4>(to, e);
+                tc_st_cols<BN / 32>(to + 8, e + 4);
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(sf_full + 8u * sbuf);
+                if (lane == 0) arrive<CG>(ready + 8u * sbuf);
             }
         }
-    } else if (warp >= WARP_OUT0) {
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(POW2_REGS_OUT));
         const int quad = warp & 3, half = (warp - WARP_OUT0) >> 2;
         const uint32_t staging = staging0 + (uint32_t)(warp - WARP_OUT0) * STAGING;
-        uint32_t tile = 0;
-        for (uint32_t t = t0; t < p.tiles && !failed; t += tstep, ++tile) {
+        const uint32_t freed = CG == 1 ? acc_empty : in_block(acc_empty, 0), over_freed = CG == 1 ? over_empty : in_block(over_empty, 0);
+        // columns of this warp, 32 at a time, from the shared ones on: the last 32 of the first accumulator and the first 32 of the
+        // second are taken out first, so the warps of the second half go backwards
+        const int first = half ? BN - 32 : 0, step = half ? -32 : 32;
+        uint32_t seg = 0;
+        for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
             int tm, tn;
             tile_of(p, t, tm, tn);
-            const uint32_t buf = tile & 1u;
-            if (!warp_wait(acc_full + 8u * buf, (tile >> 1) & 1u)) { failed = true; break; }
-            tc_fence_after();
-            const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + buf * D1 + half * CW;
-            // the shared columns first: the last 32 of the first accumulator, the first 32 of the second
-            const bool shares = OVERLAP && half == (buf == 0u ? 1 : 0);
-            for (int i = 0; i < CW / SLAB; ++i) {
-                const int c = shares && buf == 0u ? CW / SLAB - 1 - i : i;
-                uint32_t v[SLAB];
+            float acc[CW];
 #pragma unroll
-                for (int h = 0; h < SLAB / 32; ++h) ld32_start(from + c * SLAB + h * 32, v + h * 32);
+            for (int j = 0; j < CW; ++j) acc[j] = 0.f;
+            for (int k0 = kb0; k0 < kb1; k0 += SEGMENT, ++seg) {
+                const uint32_t buf = seg & 1u;
+                if (!warp_wait_soon(acc_full + 8u * buf, (seg >> 1) & 1u)) { failed = true; break; }
+                tc_fence_after();
+                const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + buf * D1 + first;
 #pragma unroll
-                for (int h = 0; h < SLAB / 32; ++h) ld32_done(v + h * 32);
-                if (i == 0 && shares) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(over_empty);
+                for (int c = 0; c < CW / 32; ++c) {
+                    uint32_t v[32];
+                    ld32_start(from + c * step, v);
+                    ld32_done(v);
+                    if (c == 0 && OVERLAP && half != (int)buf) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive<CG>(over_freed);
+                    }
+                    if (c == CW / 32 - 1) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive<CG>(freed + 8u * buf);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) acc[c * 32 + j] += __uint_as_float(v[j]);
                 }
-                if (i == CW / SLAB - 1) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(acc_empty + 8u * buf);
-                }
-                if (p.split == 1) {
-                    write_slab<C>(p, staging, tm * BM + quad * 32, tn * BN + half * CW + c * SLAB, reinterpret_cast<const float*>(v));
-                } else {
-                    store_partial<BN>(smem, quad * 32 + lane, half * CW + c * SLAB, SLAB, v);
-                }
+            }
+            if (failed) break;
+            if (CG == 2 || p.split == 1) {
+                const int row0 = (tm * CG + pair_rank) * BM + quad * 32, col0 = tn * BN + (half ? BN - SLAB : 0);
+#pragma unroll
+                for (int c = 0; c < CW / SLAB; ++c)
+                    write_slab<C>(p, staging, row0, col0 + (half ? -c : c) * SLAB, acc + c * SLAB, SLAB == 64 && half ? 4 : 0);
+            } else {
+#pragma unroll
+                for (int c = 0; c < CW / 32; ++c) store_partial<BN>(smem, quad * 32 + lane, first + c * step, 32, reinterpret_cast<const uint32_t*>(acc + 32 * c));
             }
             __syncwarp();
         }
     }
     __syncwarp();
-    if (p.split > 1) {
+    if (CG == 1 && p.split > 1) {
         cluster_sync();
         if (warp >= WARP_OUT0) add_partials<BN, C>(p, smem, t0, rank, threadIdx.x - 32 * WARP_OUT0);
         __syncwarp();
         cluster_sync();
     }
-    leave(p, failed, warp, lane, tmem);
+    if constexpr (CG == 2) {
+        tc_fence_before();
+        cluster_sync();                                  // nothing is sent to a block that has left
+        tc_fence_after();
+    }
+    leave<CG>(p, failed, warp, lane, tmem);
 }
 
 bool make_map_8bit(CUtensorMap* m, const cerar_fp8_matrix_t& x, int box_rows) {
     const cuuint64_t dim[2] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows}, stride[1] = {(cuuint64_t)x.ld};
     const cuuint32_t box[2] = {(cuuint32_t)BK, (cuuint32_t)box_rows}, step[2] = {1, 1};
     return get_encode_fn()(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, x.codes, dim, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // rows_are_k: the summed dimension runs down the rows of the stored matrix
@@ -683,8 +822,8 @@ Scales scales_of(const cerar_fp8_matrix_t& m, bool rows_are_k) {
 
 typedef void (*Kernel)(CUtensorMap, CUtensorMap, Params);
 
-cudaError_t launch_one(Kernel kern, int BN, int threads, const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, int grid, cudaStream_t s) {
-    const size_t smem = 1024 + (size_t)p.stages * (A_BYTES + BN * BK) + EPI_WARPS * STAGING + 512;
+cudaError_t launch_one(Kernel kern, int b_rows, int threads, int cluster, const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, int grid, cudaStream_t s) {
+    const size_t smem = 1024 + (size_t)p.stages * (A_BYTES + b_rows * BK) + EPI_WARPS * STAGING + 512 + SF_WORDS;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -693,13 +832,15 @@ cudaError_t launch_one(Kernel kern, int BN, int threads, const CUtensorMap& ma, 
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = g_tune_pdl_off ? 0 : 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim = {(unsigned)p.split, 1, 1};
-    cfg.attrs = attr; cfg.numAttrs = p.split > 1 ? 2 : 1;
+    attr[1].val.clusterDim = {(unsigned)cluster, 1, 1};
+    cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, ma, mb, p);
 }
-template <int BN, typename C>
-Kernel kernel_for(bool pow2, bool bvec) {
-    return pow2 ? fp8_matmul_pow2_kernel<BN, C> : bvec ? fp8_matmul_kernel<BN, true, C> : fp8_matmul_kernel<BN, false, C>;
+template <typename C>
+Kernel kernel_for(bool wide, bool pow2, bool bvec) {
+    if (pow2) return wide ? fp8_matmul_pow2_kernel<2, 256, C> : fp8_matmul_pow2_kernel<1, 128, C>;
+    if (bvec) return wide ? fp8_matmul_kernel<256, true, C> : fp8_matmul_kernel<128, true, C>;
+    return wide ? fp8_matmul_kernel<256, false, C> : fp8_matmul_kernel<128, false, C>;
 }
 
 }  // namespace
@@ -707,19 +848,21 @@ Kernel kernel_for(bool pow2, bool bvec) {
 cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, uint64_t* launches) {
     if (!get_encode_fn()) return cudaErrorNotSupported;
     Params p = {};
+    const bool bvec = a.B.scaling != CERAR_BY_BLOCK, pow2 = a.A.pow2 && a.B.pow2;
     p.M = (int)a.M; p.N = (int)a.N; p.kblocks = (int)((a.K + BK - 1) / BK);
-    p.tiles_m = (p.M + BM - 1) / BM;
     // wide tiles where they fill the GPU, otherwise narrow ones, and a tile shared by several blocks while SMs are left over
-    const bool wide = (int64_t)p.tiles_m * ((p.N + 255) / 256) >= num_sms;
-    const int BN = wide ? 256 : 128;
+    const bool wide = (int64_t)((p.M + BM - 1) / BM) * ((p.N + 255) / 256) >= num_sms;
+    const bool paired = wide && pow2;                    // tiles of 256 rows, by two blocks
+    const int BN = wide ? 256 : 128, rows = paired ? 2 * BM : BM, b_rows = paired ? BN / 2 : BN;
+    p.tiles_m = (p.M + rows - 1) / rows;
     p.tiles_n = (p.N + BN - 1) / BN;
-    if ((int64_t)p.tiles_m * p.tiles_n > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+    if ((int64_t)p.tiles_m * p.tiles_n > 0x3FFFFFFF) return cudaErrorInvalidConfiguration;
     p.tiles = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n;
     p.split = 1;
     if (!wide)
         while (p.split < 8 && (int)p.tiles * p.split * 2 <= num_sms && p.split * 4 <= p.kblocks) p.split *= 2;
-    p.group_m = 16;
-    p.stages = wide ? 4 : 6;
+    p.group_m = paired ? 8 : 16;
+    p.stages = wide && !paired ? 4 : 6;
     p.a_mn = a.trans_a; p.b_mn = !a.trans_b;
     p.sa = scales_of(a.A, a.trans_a);
     p.sb = scales_of(a.B, !a.trans_b);
@@ -727,12 +870,11 @@ cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, 
     const int64_t size = a.type == CERAR_TYPE_F32 ? 4 : 2;
     p.c_vec = (reinterpret_cast<uintptr_t>(a.C) & 15u) == 0 && (a.ldc * size) % 16 == 0;
     CUtensorMap ma, mb;
-    if (!make_map_8bit(&ma, a.A, BM) || !make_map_8bit(&mb, a.B, p.b_mn ? BK : BN)) return cudaErrorInvalidValue;
-    const int grid = p.split > 1 ? (int)p.tiles * p.split : (int)p.tiles < num_sms ? (int)p.tiles : num_sms;
-    const bool bvec = a.B.scaling != CERAR_BY_BLOCK, pow2 = a.A.pow2 && a.B.pow2;
-    const Kernel kern = a.type == CERAR_TYPE_F32 ? (wide ? kernel_for<256, float>(pow2, bvec) : kernel_for<128, float>(pow2, bvec))
-                                                 : (wide ? kernel_for<256, __nv_bfloat16>(pow2, bvec) : kernel_for<128, __nv_bfloat16>(pow2, bvec));
-    const cudaError_t e = launch_one(kern, BN, pow2 ? POW2_THREADS : THREADS, ma, mb, p, grid, s);
+    if (!make_map_8bit(&ma, a.A, BM) || !make_map_8bit(&mb, a.B, p.b_mn ? BK : b_rows)) return cudaErrorInvalidValue;
+    const int cluster = paired ? 2 : p.split, most = num_sms / cluster;
+    const int grid = cluster * (p.split > 1 || (int)p.tiles < most ? (int)p.tiles : most);
+    const Kernel kern = a.type == CERAR_TYPE_F32 ? kernel_for<float>(wide, pow2, bvec) : kernel_for<__nv_bfloat16>(wide, pow2, bvec);
+    const cudaError_t e = launch_one(kern, b_rows, pow2 ? POW2_THREADS : THREADS, cluster, ma, mb, p, grid, s);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
