@@ -133,15 +133,14 @@ lib.cerar_ops_destroy.restype = None
 lib.cerar_ops_status.argtypes = [_vp, _vp]
 lib.cerar_ops_launch_count.argtypes = [_vp]
 lib.cerar_ops_launch_count.restype = C.c_uint64
-lib.cerar_fp8_quantize.argtypes = [_vp, _vp, C.c_int, _i64, C.POINTER(Fp8Matrix), C.c_int, _vp]
-lib.cerar_fp8_matmul.argtypes = [_vp, C.POINTER(Fp8Matrix), C.c_int, C.POINTER(Fp8Matrix), C.c_int, _vp, C.c_int, _i64,
-                                 C.c_int, _vp]
+lib.cerar_fp8_quantize.argtypes = [_vp, _vp, C.c_int, _i64, _vp, C.c_int, _vp]       # (structures: by address)
+lib.cerar_fp8_matmul.argtypes = [_vp, _vp, C.c_int, _vp, C.c_int, _vp, C.c_int, _i64, C.c_int, _vp]
 lib.cerar_tensors_create.argtypes = [_vp, _i64, C.POINTER(TensorDesc), C.c_int, C.POINTER(_vp)]
 lib.cerar_tensors_destroy.argtypes = [_vp]
 lib.cerar_tensors_destroy.restype = None
 lib.cerar_tensors_set_grads.argtypes = [_vp, C.POINTER(_vp), _vp]
 lib.cerar_grad_norm.argtypes = [_vp, C.c_float, _vp, _vp]
-lib.cerar_adamw_step.argtypes = [_vp, C.POINTER(AdamwOptions), _vp, _vp]
+lib.cerar_adamw_step.argtypes = [_vp, _vp, _vp, _vp]
 lib.cerar_status_string.argtypes = [C.c_int]
 lib.cerar_status_string.restype = C.c_char_p
 lib.cerar_last_error.restype = C.c_char_p

@@ -27,6 +27,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 #include "kernels.cuh"
 #include "ops.cuh"
 #include "tc_common.cuh"
@@ -38,6 +40,7 @@ using namespace tc;
 
 constexpr int BM = 128, BK = FP8_BLOCK;
 constexpr int EPI_WARPS = 8, WARP_EPI0 = 4;
+constexpr int MAX_SPLIT = 8;                            // blocks that share the sum of a tile (a portable cluster)
 // registers per thread: 128 x 56 + 256 x 224 = 384 x 168, what the block is launched with
 constexpr int REGS_FEW = 56, REGS_MANY = 224;
 constexpr int THREADS = 32 * (WARP_EPI0 + EPI_WARPS);
@@ -60,6 +63,7 @@ struct Params {
     int a_mn, b_mn;                                    // 1: the operand's own dimension (m or n) is the contiguous one
     int accumulate, c_vec;
     int stages, split;
+    int early;                                         // 1: the next kernel of the stream may set itself up meanwhile (on SMs that this one leaves free)
     int* status;
 };
 
@@ -86,6 +90,7 @@ __device__ __forceinline__ bool wait_soon(uint32_t bar, uint32_t parity) {
     }
 }
 __device__ __forceinline__ bool warp_wait_soon(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_soon(bar, parity) ? 1 : 0) != 0; }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); }
 __device__ __forceinline__ uint32_t elect_one() {
     uint32_t r;
     asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
@@ -301,32 +306,34 @@ __device__ __forceinline__ void produce(const Params& p, const CUtensorMap& map_
     }
 }
 
-// A tile whose sum is split over a cluster: every block leaves its partial tile in its stages (free by then), row r at r * BN floats,
-// 16-byte pieces exchanged by the row so that lanes do not meet in a bank ...
+// A tile whose sum is split over a cluster: every block leaves the rows of its partial tile that exist in its stages (free by then),
+// row r at r * BN floats, 16-byte pieces exchanged by the row so that lanes do not meet in a bank ...
 template <int BN>
-__device__ __forceinline__ void store_partial(uint32_t smem, int row, int col, int n, const uint32_t* v) {
+__device__ __forceinline__ void store_partial(uint32_t smem, int rows, int row, int col, int n, const uint32_t* v) {
+    if (row >= rows) return;
     const uint32_t base = smem + (uint32_t)row * (BN * 4u);
 #pragma unroll
     for (int j = 0; j < n / 4; ++j)
         asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + ((uint32_t)((col / 4 + j) ^ (row & 7)) << 4)), "r"(v[4 * j]), "r"(v[4 * j + 1]),
                      "r"(v[4 * j + 2]), "r"(v[4 * j + 3]) : "memory");
 }
-// ... and adds every split-th row of all partial tiles, in the order of their blocks of k.
+// ... and adds every split-th run of 32 pieces (a warp's) of all partial tiles, in the order of their blocks of k.
 template <int BN, typename C>
-__device__ __forceinline__ void add_partials(const Params& p, uint32_t smem, uint32_t t, int rank, int thread) {
-    int tm, tn;
-    tile_of(p, t, tm, tn);
-    const int rows = p.M - tm * BM < BM ? p.M - tm * BM : BM;
+__device__ __forceinline__ void add_partials(const Params& p, uint32_t smem, int tm, int tn, int rows, int rank, int thread) {
     C* c = static_cast<C*>(p.C);
-    for (int i = thread; i < (BM / p.split) * (BN / 4); i += 32 * EPI_WARPS) {
-        const int r = (i / (BN / 4)) * p.split + rank, j = i % (BN / 4);
-        if (r >= rows) break;
+    const int pieces = rows * (BN / 4);
+    for (int run = (thread >> 5) * p.split + rank; run * 32 < pieces; run += EPI_WARPS * p.split) {
+        const int i = run * 32 + (thread & 31);         // (pieces is a multiple of 32)
+        const int r = i / (BN / 4), j = i % (BN / 4);
         const uint32_t at = smem + (uint32_t)r * (BN * 4u) + ((uint32_t)(j ^ (r & 7)) << 4);
-        float4 v = ld_cluster4(at, 0);
-        for (int q = 1; q < p.split; ++q) {
-            const float4 w = ld_cluster4(at, q);
-            v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-        }
+        float4 w[MAX_SPLIT];
+#pragma unroll
+        for (int q = 0; q < MAX_SPLIT; ++q)
+            if (q < p.split) w[q] = ld_cluster4(at, q);
+        float4 v = w[0];
+#pragma unroll
+        for (int q = 1; q < MAX_SPLIT; ++q)
+            if (q < p.split) { v.x += w[q].x; v.y += w[q].y; v.z += w[q].z; v.w += w[q].w; }
         const int n0 = tn * BN + 4 * j;
         C* dst = c + (int64_t)(tm * BM + r) * p.ldc + n0;
         const float x[4] = {v.x, v.y, v.z, v.w};
@@ -344,7 +351,7 @@ __device__ __forceinline__ void leave(const Params& p, bool failed, int warp, in
         const unsigned long long start = global_ns();
         while (global_ns() - start < 2000000ull) { }    // let copies and products in flight finish
     }
-    grid_dependents_may_launch();
+    if (!p.early) grid_dependents_may_launch();
     tc_fence_before();
     __syncthreads();
     if (warp == 1) {
@@ -370,6 +377,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const uint32_t slot = acc_empty + 8u * NBUF;
 
     if (threadIdx.x == 0) {
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8u * s, 1); mbar_init(empty + 8u * s, 1); }
         for (int b = 0; b < NBUF; ++b) { mbar_init(acc_full + 8u * b, 1); mbar_init(acc_empty + 8u * b, EPI_WARPS); }
         mbar_init_fence();
@@ -380,6 +389,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    if (p.early) grid_dependents_may_launch();
     grid_dependency_wait();
 
     const int rank = p.split > 1 ? (int)cluster_rank() : 0;
@@ -500,13 +510,15 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 for (int c = 0; c < CW / SLAB; ++c) write_slab<C>(p, staging, tm * BM + quad * 32, col0 + c * SLAB, acc + c * SLAB);
                 __syncwarp();
             } else {
-                store_partial<BN>(smem, quad * 32 + lane, half * CW, CW, reinterpret_cast<const uint32_t*>(acc));
+                store_partial<BN>(smem, p.M - tm * BM, quad * 32 + lane, half * CW, CW, reinterpret_cast<const uint32_t*>(acc));
             }
         }
         __syncwarp();
         if (p.split > 1) {
             cluster_sync();
-            add_partials<BN, C>(p, smem, t0, rank, threadIdx.x - 32 * WARP_EPI0);
+            int tm, tn;                                 // (one tile per cluster)
+            tile_of(p, t0, tm, tn);
+            add_partials<BN, C>(p, smem, tm, tn, p.M - tm * BM < BM ? p.M - tm * BM : BM, rank, threadIdx.x - 32 * WARP_EPI0);
             __syncwarp();
             cluster_sync();                             // no block leaves while another reads its part
         }
@@ -592,6 +604,8 @@ fp8_matmul_pow2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
     const uint32_t sf_full = over_empty + 8u, sf_empty = sf_full + 16u, slot = sf_empty + 16u;
 
     if (threadIdx.x == 0) {
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8u * s, 1); mbar_init(empty + 8u * s, 1); }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full + 8u * b, 1); mbar_init(acc_empty + 8u * b, CG * EPI_WARPS);
@@ -614,6 +628,7 @@ fp8_matmul_pow2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    if (p.early) grid_dependents_may_launch();
     grid_dependency_wait();
 
     // a cluster is a pair of blocks that share a tile of 256 rows (CG = 2), or `split` blocks that share the sum of a tile
@@ -787,7 +802,7 @@ fp8_matmul_pow2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                     write_slab<C>(p, staging, row0, col0 + (half ? -c : c) * SLAB, acc + c * SLAB, SLAB == 64 && half ? 4 : 0);
             } else {
 #pragma unroll
-                for (int c = 0; c < CW / 32; ++c) store_partial<BN>(smem, quad * 32 + lane, first + c * step, 32, reinterpret_cast<const uint32_t*>(acc + 32 * c));
+                for (int c = 0; c < CW / 32; ++c) store_partial<BN>(smem, p.M - tm * BM, quad * 32 + lane, first + c * step, 32, reinterpret_cast<const uint32_t*>(acc + 32 * c));
             }
             __syncwarp();
         }
@@ -795,7 +810,11 @@ fp8_matmul_pow2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
     __syncwarp();
     if (CG == 1 && p.split > 1) {
         cluster_sync();
-        if (warp >= WARP_OUT0) add_partials<BN, C>(p, smem, t0, rank, threadIdx.x - 32 * WARP_OUT0);
+        if (warp >= WARP_OUT0) {
+            int tm, tn;                                  // (one tile per cluster)
+            tile_of(p, t0, tm, tn);
+            add_partials<BN, C>(p, smem, tm, tn, p.M - tm * BM < BM ? p.M - tm * BM : BM, rank, threadIdx.x - 32 * WARP_OUT0);
+        }
         __syncwarp();
         cluster_sync();
     }
@@ -822,10 +841,21 @@ Scales scales_of(const cerar_fp8_matrix_t& m, bool rows_are_k) {
 
 typedef void (*Kernel)(CUtensorMap, CUtensorMap, Params);
 
-cudaError_t launch_one(Kernel kern, int b_rows, int threads, int cluster, const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, int grid, cudaStream_t s) {
+constexpr int KERNELS = 12, MAX_SMEM = 232448;
+
+cudaError_t launch_one(Kernel kern, int which, int b_rows, int threads, int cluster, const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, int grid, cudaStream_t s) {
     const size_t smem = 1024 + (size_t)p.stages * (A_BYTES + b_rows * BK) + EPI_WARPS * STAGING + 512 + SF_WORDS;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // Once per kernel and device (a call costs the host more than the rest of this function): every launch is allowed the most.
+    static std::atomic<uint64_t> allowed[KERNELS];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (!(allowed[which].load(std::memory_order_relaxed) & bit)) {
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
+        if (e != cudaSuccess) return e;
+        allowed[which].fetch_or(bit, std::memory_order_relaxed);
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -858,9 +888,13 @@ cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, 
     p.tiles_n = (p.N + BN - 1) / BN;
     if ((int64_t)p.tiles_m * p.tiles_n > 0x3FFFFFFF) return cudaErrorInvalidConfiguration;
     p.tiles = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n;
+    // as many blocks per tile as keep the grid within 0.82 of the SMs, 0.65 in clusters of more than 4, which do not fill the
+    // GPU's groups of SMs (measured, us for split 1, 2, .. 6, 8: 16 tiles of 64 blocks of k 25.6, 18.5, 15.1, 12.7, 11.7, 11.0, 18.7;
+    // 27 tiles of 16 13.0, 10.3, 9.4, 8.2, 13.7; 40 tiles of 32 19.1, 13.5, 11.5; 64 tiles of 16 9.7, 10.5)
     p.split = 1;
     if (!wide)
-        while (p.split < 8 && (int)p.tiles * p.split * 2 <= num_sms && p.split * 4 <= p.kblocks) p.split *= 2;
+        for (int q = 2; q <= MAX_SPLIT && q <= p.kblocks; ++q)
+            if ((int64_t)p.tiles * q * 100 <= (int64_t)num_sms * (q > 4 ? 65 : 82)) p.split = q;
     p.group_m = paired ? 8 : 16;
     p.stages = wide && !paired ? 4 : 6;
     p.a_mn = a.trans_a; p.b_mn = !a.trans_b;
@@ -873,8 +907,9 @@ cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, 
     if (!make_map_8bit(&ma, a.A, BM) || !make_map_8bit(&mb, a.B, p.b_mn ? BK : b_rows)) return cudaErrorInvalidValue;
     const int cluster = paired ? 2 : p.split, most = num_sms / cluster;
     const int grid = cluster * (p.split > 1 || (int)p.tiles < most ? (int)p.tiles : most);
+    p.early = 2 * grid <= num_sms;
     const Kernel kern = a.type == CERAR_TYPE_F32 ? kernel_for<float>(wide, pow2, bvec) : kernel_for<__nv_bfloat16>(wide, pow2, bvec);
-    const cudaError_t e = launch_one(kern, b_rows, pow2 ? POW2_THREADS : THREADS, cluster, ma, mb, p, grid, s);
+    const cudaError_t e = launch_one(kern, (pow2 ? 0 : bvec ? 1 : 2) * 4 + wide * 2 + (a.type == CERAR_TYPE_F32), b_rows, pow2 ? POW2_THREADS : THREADS, cluster, ma, mb, p, grid, s);
     if (e == cudaSuccess) ++*launches;
     return e;
 }

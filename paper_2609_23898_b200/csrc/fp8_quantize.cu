@@ -22,90 +22,108 @@ namespace {
 
 constexpr int T = FP8_BLOCK;             // tile edge
 constexpr int WARPS = 8, ROWS = T / WARPS;
+constexpr uint32_t INF = 0x7F800000u;
 
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// four scaled values to four codes; a value that is not finite becomes NaN: x * 0 is NaN exactly there
-__device__ __forceinline__ uint32_t codes4(const float* x, const float* inv) {
+// Four values of one row as they are in memory, and as binary32.
+template <typename X> struct Four;
+template <> struct Four<float> {
+    float4 v;
+    __device__ __forceinline__ void clear() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void load(const float* p) { v = __ldcs(reinterpret_cast<const float4*>(p)); }
+    __device__ __forceinline__ void set(int j, float x) { (&v.x)[j] = x; }
+    __device__ __forceinline__ void get(float* x) const { x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+};
+template <> struct Four<__nv_bfloat16> {
+    uint2 v;
+    __device__ __forceinline__ void clear() { v = make_uint2(0u, 0u); }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint2*>(p)); }
+    __device__ __forceinline__ void set(int j, __nv_bfloat16 x) {
+        const uint32_t b = (uint32_t)__bfloat16_as_ushort(x) << (16 * (j & 1));
+        if (j < 2) v.x |= b; else v.y |= b;
+    }
+    __device__ __forceinline__ void get(float* x) const {
+        x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+        x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    }
+};
+
+// Four scaled values to four codes.  bad: there may be values that are not finite, which become NaN: x * 0 is NaN exactly there
+// (the conversion by itself would turn an infinity into 448).
+__device__ __forceinline__ uint32_t codes4(const float* x, const float* inv, bool bad) {
     uint16_t lo, hi;
     float y[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = fmaf(x[j], inv[j], x[j] * 0.f);
+    for (int j = 0; j < 4; ++j) y[j] = x[j] * inv[j];
+    if (bad) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] += x[j] * 0.f;
+    }
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(y[1]), "f"(y[0]));
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(y[3]), "f"(y[2]));
     return (uint32_t)lo | ((uint32_t)hi << 16);
 }
-__device__ __forceinline__ uint32_t finite_magnitude(float x) {
-    const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
-    return b < 0x7F800000u ? b : 0u;
-}
 __device__ __forceinline__ void store_codes(uint8_t* dst, uint32_t v, int n) {
     if (n >= 4) { *reinterpret_cast<uint32_t*>(dst) = v; return; }
-    for (int j = 0; j < n; ++j) dst[j] = (uint8_t)(v >> (8 * j));
+#pragma unroll
+    for (int j = 0; j < 3; ++j) if (j < n) dst[j] = (uint8_t)(v >> (8 * j));
 }
 
 // FORMS: bit per cerar_scaling_t
 template <typename X, int FORMS>
-__global__ void __launch_bounds__(32 * WARPS) fp8_quantize_kernel(const __grid_constant__ QuantizeArgs a, uint32_t tiles_c) {
+__global__ void __launch_bounds__(32 * WARPS, sizeof(X) == 2 ? 3 : 2) fp8_quantize_kernel(const __grid_constant__ QuantizeArgs a, uint32_t tiles_c) {
     constexpr bool BY_ROW = FORMS & (1 << CERAR_BY_ROW), BY_COL = FORMS & (1 << CERAR_BY_COLUMN), BY_BLK = FORMS & (1 << CERAR_BY_BLOCK);
     __shared__ uint32_t colmax[BY_COL || BY_BLK ? WARPS : 1][T];
     ptx::grid_dependency_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
-    const int64_t r0 = tr * T + warp * ROWS, c0 = tc * T + 4 * lane;
+    const uint32_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+    const int64_t r0 = (int64_t)tr * T + warp * ROWS, c0 = (int64_t)tc * T + 4 * lane;
     const int64_t left = a.cols - c0;
     const int nc = left >= 4 ? 4 : left > 0 ? (int)left : 0;          // columns of this thread that exist
     const int nr = (int)(a.rows - r0 < ROWS ? (a.rows > r0 ? a.rows - r0 : 0) : ROWS);   // rows of this warp that exist
 
-    float x[ROWS][4];
+    Four<X> v[ROWS];
     const X* src = static_cast<const X*>(a.x) + r0 * a.ldx + c0;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) v[i].clear();
     if (a.vec && nc == 4) {
-        if constexpr (sizeof(X) == 4) {
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (i < nr) v = __ldg(reinterpret_cast<const float4*>(src + i * a.ldx));
-                x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
-            }
-        } else {
-            uint2 v[ROWS];
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                v[i] = make_uint2(0u, 0u);
-                if (i < nr) v[i] = __ldg(reinterpret_cast<const uint2*>(src + i * a.ldx));
-            }
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                x[i][0] = __uint_as_float(v[i].x << 16); x[i][1] = __uint_as_float(v[i].x & 0xFFFF0000u);
-                x[i][2] = __uint_as_float(v[i].y << 16); x[i][3] = __uint_as_float(v[i].y & 0xFFFF0000u);
-            }
-        }
+        for (int i = 0; i < ROWS; ++i)
+            if (i < nr) v[i].load(src + i * a.ldx);
     } else {
 #pragma unroll
         for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[i][j] = 0.f;
-                if (i < nr && j < nc) {
-                    if constexpr (sizeof(X) == 4) x[i][j] = src[i * a.ldx + j];
-                    else x[i][j] = __bfloat162float(src[i * a.ldx + j]);
-                }
-            }
+            for (int j = 0; j < 4; ++j)
+                if (i < nr && j < nc) v[i].set(j, src[i * a.ldx + j]);
     }
 
     uint32_t cm[4] = {0u, 0u, 0u, 0u};
+    bool bad = false;
     float row_scale = 1.f;                                             // of row `lane` of this warp (lanes 0 .. ROWS - 1)
     uint8_t* dst = BY_ROW ? a.codes[CERAR_BY_ROW] + r0 * a.ld[CERAR_BY_ROW] + c0 : nullptr;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
+        float x[4];
+        v[i].get(x);
         uint32_t m[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { m[j] = finite_magnitude(x[i][j]); cm[j] = max(cm[j], m[j]); }
+        for (int j = 0; j < 4; ++j) m[j] = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+        if (max(max(m[0], m[1]), max(m[2], m[3])) >= INF) {           // rare: only finite magnitudes count
+            bad = true;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (m[j] >= INF) m[j] = 0u;
+        }
+        if constexpr (BY_COL || BY_BLK) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) cm[j] = max(cm[j], m[j]);
+        }
         if constexpr (BY_ROW) {
             const int e = fp8_scale_exponent(__reduce_max_sync(0xffffffffu, max(max(m[0], m[1]), max(m[2], m[3]))));
             if (lane == i) row_scale = pow2f(e);
             const float k = pow2f(-e), inv[4] = {k, k, k, k};
-            if (i < nr) store_codes(dst + i * a.ld[CERAR_BY_ROW], codes4(x[i], inv), nc);
+            if (i < nr) store_codes(dst + i * a.ld[CERAR_BY_ROW], codes4(x, inv, bad), nc);
         }
     }
     if constexpr (BY_ROW) {
@@ -116,8 +134,8 @@ __global__ void __launch_bounds__(32 * WARPS) fp8_quantize_kernel(const __grid_c
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            const uint4 v = *reinterpret_cast<const uint4*>(&colmax[w][4 * lane]);
-            cm[0] = max(cm[0], v.x); cm[1] = max(cm[1], v.y); cm[2] = max(cm[2], v.z); cm[3] = max(cm[3], v.w);
+            const uint4 q = *reinterpret_cast<const uint4*>(&colmax[w][4 * lane]);
+            cm[0] = max(cm[0], q.x); cm[1] = max(cm[1], q.y); cm[2] = max(cm[2], q.z); cm[3] = max(cm[3], q.w);
         }
     }
     if constexpr (BY_COL) {
@@ -126,11 +144,15 @@ __global__ void __launch_bounds__(32 * WARPS) fp8_quantize_kernel(const __grid_c
         for (int j = 0; j < 4; ++j) { const int e = fp8_scale_exponent(cm[j]); inv[j] = pow2f(-e); sc[j] = pow2f(e); }
         uint8_t* dc = a.codes[CERAR_BY_COLUMN] + r0 * a.ld[CERAR_BY_COLUMN] + c0;
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i)
-            if (i < nr) store_codes(dc + i * a.ld[CERAR_BY_COLUMN], codes4(x[i], inv), nc);
+        for (int i = 0; i < ROWS; ++i) {
+            float x[4];
+            v[i].get(x);
+            if (i < nr) store_codes(dc + i * a.ld[CERAR_BY_COLUMN], codes4(x, inv, bad), nc);
+        }
         if (warp == 0) {
             float* s = a.scales[CERAR_BY_COLUMN] + tr * a.lds[CERAR_BY_COLUMN] + c0;
-            for (int j = 0; j < nc; ++j) s[j] = sc[j];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (j < nc) s[j] = sc[j];
         }
     }
     if constexpr (BY_BLK) {
@@ -138,8 +160,11 @@ __global__ void __launch_bounds__(32 * WARPS) fp8_quantize_kernel(const __grid_c
         const float k = pow2f(-e), inv[4] = {k, k, k, k};
         uint8_t* db = a.codes[CERAR_BY_BLOCK] + r0 * a.ld[CERAR_BY_BLOCK] + c0;
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i)
-            if (i < nr) store_codes(db + i * a.ld[CERAR_BY_BLOCK], codes4(x[i], inv), nc);
+        for (int i = 0; i < ROWS; ++i) {
+            float x[4];
+            v[i].get(x);
+            if (i < nr) store_codes(db + i * a.ld[CERAR_BY_BLOCK], codes4(x, inv, bad), nc);
+        }
         if (threadIdx.x == 0) a.scales[CERAR_BY_BLOCK][tr * a.lds[CERAR_BY_BLOCK] + tc] = pow2f(e);
     }
 }

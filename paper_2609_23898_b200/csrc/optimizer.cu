@@ -7,6 +7,7 @@
 // In a chunk warp w owns the 256 elements 256 w .. 256 w + 255: lane l has elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3 of
 // them, so every access of a warp is contiguous, and the 256 elements that share a scale of the 8-bit states belong to one warp.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
 #include <type_traits>
@@ -162,12 +163,34 @@ __device__ __forceinline__ uint32_t block_key(int64_t block, uint64_t seed, uint
 }
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// Value of an e4m3 code: shifted to the binary32 exponent and mantissa it is the value times 2^-120, subnormals included.
-__device__ __forceinline__ float code_value(uint32_t code) {
-    const float mag = __uint_as_float((code & 0x7Fu) << 20) * 0x1p120f;
-    const float v = (code & 0x7Fu) == 0x7Fu ? __uint_as_float(0x7FC00000u) : mag;
-    return __uint_as_float(__float_as_uint(v) | ((code & 0x80u) << 24));
+// Values of four e4m3 codes times a scale (the conversion goes through binary16, which holds them all).
+__device__ __forceinline__ void code_values(uint32_t codes, float scale, float* x) {
+    uint32_t lo, hi;
+    asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n" : "=r"(lo), "=r"(hi) : "r"(codes));
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    x[0] = a.x * scale; x[1] = a.y * scale; x[2] = b.x * scale; x[3] = b.y * scale;
 }
+__device__ __forceinline__ float max_nan(float a, float b) {           // NaN if one of them is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t sign_bytes(float a, float b) {     // bytes 0 and 1: 0xFF where a, b are negative, else 0
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, 0xFBFB;" : "=r"(r) : "r"(__float_as_uint(a)), "r"(__float_as_uint(b)));
+    return r;
+}
+__device__ __forceinline__ uint32_t bytes4(const uint32_t* c) {        // four numbers below 256 in the bytes of a word
+    return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+}
+__device__ __forceinline__ float pick(const float* x, int j) {         // x[j] of eight, without an array in memory
+    float v = x[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v = j == i ? x[i] : v;
+    return v;
+}
+// Moments below this (2^14) have a scale exponent up to 6, so that 2^-e 2^-120 is a normal binary32 number.
+constexpr uint32_t LARGE_STATE = (127u + 14u) << 23;
 // Code of y, |y| <= 448, rounded away from zero with the probability of the part that is cut off: times 2^-120 the code is the
 // top of the binary32 number, and 16 random bits (plus half of their last place) are added to the 20 bits below it.
 __device__ __forceinline__ uint32_t random_code(float y, uint32_t bits16) {
@@ -216,25 +239,27 @@ __device__ __forceinline__ void adamw_warp(const AdamwArgs& a, const TensorRec& 
         vc[1] = load_codes(static_cast<const uint8_t*>(t.v) + i1, n1, v1);
         msc = t.m_scale[e0 / PER_WARP];
         vsc = t.v_scale[e0 / PER_WARP];
+        code_values(mc[0], msc, m);
+        code_values(mc[1], msc, m + 4);
+        code_values(vc[0], vsc, v);
+        code_values(vc[1], vsc, v + 4);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            m[j] = code_value((mc[j >> 2] >> (8 * (j & 3))) & 0xFFu) * msc;
-            const float r = code_value((vc[j >> 2] >> (8 * (j & 3))) & 0xFFu) * vsc;
-            v[j] = __fmul_rn(r, r);
-        }
+        for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], v[j]);
     }
     const float step = a.step_size * t.lr_scale, keep = 1.f - a.lr * t.lr_scale * t.weight_decay;
     float r[8];
-    uint32_t mmax = 0u, rmax = 0u;
+    float mtop = 0.f, rtop = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         // each product and sum rounded by itself (no contraction), as the formula is written
         const float gc = __fmul_rn(g[j], coef);
         m[j] = __fadd_rn(__fmul_rn(m[j], a.beta1), __fmul_rn(gc, a.one_minus_beta1));
         v[j] = __fadd_rn(__fmul_rn(v[j], a.beta2), __fmul_rn(__fmul_rn(gc, gc), a.one_minus_beta2));
-        r[j] = __fsqrt_rn(v[j]);
+        // (the root of an 8-bit state decides which code is kept: rounded to nearest; otherwise only the update sees it: within 2 u)
+        if constexpr (BITS == 8) r[j] = __fsqrt_rn(v[j]);
+        else asm("sqrt.approx.f32 %0, %1;" : "=f"(r[j]) : "f"(v[j]));
         p[j] = fmaf(-step, __fdividef(m[j], fmaf(r[j], a.root_scale, a.eps)), p[j] * keep);
-        if constexpr (BITS == 8) { mmax = max(mmax, finite_magnitude(m[j])); rmax = max(rmax, finite_magnitude(r[j])); }
+        if constexpr (BITS == 8) { mtop = max_nan(mtop, fabsf(m[j])); rtop = max_nan(rtop, r[j]); }
     }
     if constexpr (BITS == 32) {
         store4(static_cast<float*>(t.m) + i0, m, n0, v0);
@@ -242,18 +267,47 @@ __device__ __forceinline__ void adamw_warp(const AdamwArgs& a, const TensorRec& 
         store4(static_cast<float*>(t.v) + i0, v, n0, v0);
         store4(static_cast<float*>(t.v) + i1, v + 4, n1, v1);
     } else {
-        const int em = fp8_scale_exponent(__reduce_max_sync(0xffffffffu, mmax));
-        const int er = fp8_scale_exponent(__reduce_max_sync(0xffffffffu, rmax));
-        const float im = pow2f(-em), ir = pow2f(-er);
-        const uint32_t key = block_key(t.block0 + e0 / PER_WARP, a.seed, 0u);
+        uint32_t mmax = __reduce_max_sync(0xffffffffu, __float_as_uint(mtop)), rmax = __reduce_max_sync(0xffffffffu, __float_as_uint(rtop));
+        const uint32_t key = block_key(t.block0 + e0 / PER_WARP, a.seed, 0u) + (uint32_t)lane * (4u * 0x9E3779B9u);
+        int em, er;
         mc[0] = mc[1] = vc[0] = vc[1] = 0u;
+        if (mmax < LARGE_STATE && rmax < LARGE_STATE) {
+            // everything is finite, and 2^-e 2^-120 is a number: one product brings the code to the top of the binary32 number
+            em = fp8_scale_exponent(mmax);
+            er = fp8_scale_exponent(rmax);
+            const float im = pow2f(-em) * 0x1p-120f, ir = pow2f(-er) * 0x1p-120f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t h = scramble(key + (uint32_t)((j >> 2) * 128 + 4 * lane + (j & 3)) * 0x9E3779B9u);
-            mc[j >> 2] |= random_code(m[j] * im, h >> 16) << (8 * (j & 3));
-            uint32_t c = random_code(r[j] * ir, h & 0xFFFFu);
-            if (r[j] > 0.f) c = max(c, 1u);
-            vc[j >> 2] |= c << (8 * (j & 3));
+            for (int q = 0; q < 2; ++q) {
+                uint32_t cm[4], cr[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = 4 * q + i;
+                    const uint32_t h = scramble(key + (uint32_t)(q * 128 + i) * 0x9E3779B9u);
+                    cm[i] = (__float_as_uint(fabsf(m[j]) * im) + (((h >> 12) & 0xFFFF0u) | 8u)) >> 20;
+                    cr[i] = max((__float_as_uint(r[j] * ir) + (((h << 4) & 0xFFFF0u) | 8u)) >> 20, min(__float_as_uint(r[j]), 1u));
+                }
+                // four codes to a word; the signs come from the top bytes of m, spread over a byte each by the permutation
+                const uint32_t neg = __byte_perm(sign_bytes(m[4 * q], m[4 * q + 1]), sign_bytes(m[4 * q + 2], m[4 * q + 3]), 0x5410);
+                mc[q] = bytes4(cm) | (neg & 0x80808080u);
+                vc[q] = bytes4(cr);
+            }
+        } else {
+            mmax = rmax = 0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { mmax = max(mmax, finite_magnitude(m[j])); rmax = max(rmax, finite_magnitude(r[j])); }
+            em = fp8_scale_exponent(__reduce_max_sync(0xffffffffu, mmax));
+            er = fp8_scale_exponent(__reduce_max_sync(0xffffffffu, rmax));
+            const float im = pow2f(-em), ir = pow2f(-er);
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t h = scramble(key + (uint32_t)((j >> 2) * 128 + (j & 3)) * 0x9E3779B9u);
+                const float mj = pick(m, j), rj = pick(r, j);
+                const uint32_t cm = random_code(mj * im, h >> 16) << (8 * (j & 3));
+                uint32_t c = random_code(rj * ir, h & 0xFFFFu);
+                if (rj > 0.f) c = max(c, 1u);
+                c <<= 8 * (j & 3);
+                if (j < 4) { mc[0] |= cm; vc[0] |= c; } else { mc[1] |= cm; vc[1] |= c; }
+            }
         }
         store_codes(static_cast<uint8_t*>(t.m) + i0, mc[0], n0, v0);
         store_codes(static_cast<uint8_t*>(t.m) + i1, mc[1], n1, v1);

@@ -27,10 +27,16 @@ STATE_BLOCK = 256      # elements that share a scale of an 8-bit optimizer state
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 _check = cerar._check
+_E4M3, _F32 = torch.float8_e4m3fn, torch.float32
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the same handle without the Stream object around it
+_quantize, _matmul, _norm, _adamw = lib.cerar_fp8_quantize, lib.cerar_fp8_matmul, lib.cerar_grad_norm, lib.cerar_adamw_step
 
 
-def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+def _stream(device: int | None = None) -> int:
+    """The current stream of a device (of the current one)."""
+    if _raw_stream is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    return _raw_stream(torch.cuda.current_device() if device is None else device)
 
 
 def _type(t: torch.Tensor, what: str) -> int:
@@ -61,7 +67,7 @@ class Quantized:
     scales are read once, here, to see (which waits for the device).  Scales that are changed later have to keep to it:
     what they touch becomes NaN otherwise."""
 
-    __slots__ = ("codes", "scales", "scaling", "desc")
+    __slots__ = ("codes", "scales", "scaling", "desc", "at")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, scaling: int, pow2: bool | None = None):
         if codes.element_size() != 1:
@@ -85,15 +91,21 @@ class Quantized:
     def _set(self, codes, scales, scaling, rows, cols, ld, lds, pow2):
         self.codes, self.scales, self.scaling = codes, scales, scaling
         self.desc = Fp8Matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, lds, scaling, pow2)
+        self.at = C.addressof(self.desc)
 
     @classmethod
     def empty(cls, rows: int, cols: int, scaling: int, device) -> "Quantized":
-        ld = -(-cols // 16) * 16
-        nr, nc = -(-rows // BLOCK), -(-cols // BLOCK)
-        shape = (nc, rows) if scaling == BY_ROW else (nr, cols) if scaling == BY_COLUMN else (nr, nc)
-        codes = torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=device)
+        ld = (cols + 15) & -16
+        nr, nc = (rows + 127) >> 7, (cols + 127) >> 7
+        if scaling == BY_ROW:
+            nr, nc = nc, rows
+        elif scaling == BY_COLUMN:
+            nc = cols
+        elif scaling != BY_BLOCK:
+            raise ValueError("scaling must be BY_ROW, BY_COLUMN or BY_BLOCK")
+        codes = torch.empty(rows, ld, dtype=_E4M3, device=device)
         q = cls.__new__(cls)
-        q._set(codes if ld == cols else codes[:, :cols], torch.empty(shape, dtype=torch.float32, device=device), scaling, rows, cols, ld, shape[1], True)
+        q._set(codes if ld == cols else codes[:, :cols], torch.empty(nr, nc, dtype=_F32, device=device), scaling, rows, cols, ld, nc, True)
         return q
 
     @property
@@ -142,25 +154,38 @@ class Ops:
         t = _type(x, "x")
         _matrix(x, "x")
         rows, cols = x.shape
-        out = [Quantized.empty(rows, cols, s, x.device) for s in scalings]
-        arr = (Fp8Matrix * len(out))(*[q.desc for q in out])
-        _check(lib.cerar_fp8_quantize(self._h, x.data_ptr(), t, _ld(x), arr, len(out), _stream()))
+        device = x.device
+        out = [Quantized.empty(rows, cols, s, device) for s in scalings]
+        n = len(out)
+        if n == 1:
+            at = out[0].at
+        else:
+            arr = (Fp8Matrix * n)(*[q.desc for q in out])
+            at = C.addressof(arr)
+        st = _quantize(self._h, x.data_ptr(), t, _ld(x), at, n, _stream(device.index))
+        if st:
+            _check(st)
         return out
 
     def matmul(self, a: Quantized, b: Quantized, *, trans_a=False, trans_b=False, out: torch.Tensor | None = None,
                dtype: torch.dtype = torch.bfloat16, accumulate=False) -> torch.Tensor:
         """op(a) op(b), into `out` if given (added to it with accumulate)."""
+        da, db = a.desc, b.desc
+        m, n = (da.cols if trans_a else da.rows), (db.rows if trans_b else db.cols)
+        device = a.codes.device
         if out is None:
             if accumulate:
                 raise ValueError("accumulate wants an `out` to add to")
-            out = torch.empty((a.desc.cols if trans_a else a.desc.rows, b.desc.rows if trans_b else b.desc.cols), dtype=dtype,
-                              device=a.codes.device)
+            out = torch.empty(m, n, dtype=dtype, device=device)
+            ld = n
         else:
             _matrix(out, "out")
-            want = (a.desc.cols if trans_a else a.desc.rows, b.desc.rows if trans_b else b.desc.cols)
-            if tuple(out.shape) != want:
-                raise ValueError(f"out of shape {want} wanted, got {tuple(out.shape)}")
-        _check(lib.cerar_fp8_matmul(self._h, a.desc, trans_a, b.desc, trans_b, out.data_ptr(), _type(out, "out"), _ld(out), accumulate, _stream()))
+            if tuple(out.shape) != (m, n):
+                raise ValueError(f"out of shape {(m, n)} wanted, got {tuple(out.shape)}")
+            ld = _ld(out)
+        st = _matmul(self._h, a.at, trans_a, b.at, trans_b, out.data_ptr(), _type(out, "out"), ld, accumulate, _stream(device.index))
+        if st:
+            _check(st)
         return out
 
 
@@ -283,7 +308,9 @@ class TensorSet:
         out = C.c_void_p()
         _check(lib.cerar_tensors_create(ops._h, len(n), desc, self.state_bits, C.byref(out)))
         self._h = out
+        self._device = dev
         self._opt = cerar.AdamwOptions()
+        self._opt_at = C.addressof(self._opt)
 
     def destroy(self):
         if getattr(self, "_h", None):
@@ -307,8 +334,12 @@ class TensorSet:
     def grad_norm(self, max_norm: float = 0.0, out: torch.Tensor | None = None) -> torch.Tensor:
         """[norm, clip coefficient, 1 if finite] on the device; the third argument of a step that skips itself otherwise."""
         if out is None:
-            out = torch.empty(3, dtype=torch.float32, device="cuda")
-        _check(lib.cerar_grad_norm(self._h, max_norm, out.data_ptr(), _stream()))
+            out = torch.empty(3, dtype=_F32, device=self._device)
+        elif out.dtype != _F32 or out.numel() != 3 or not out.is_cuda or not out.is_contiguous():
+            raise ValueError("out: three contiguous floats on the device are wanted")
+        st = _norm(self._h, max_norm, out.data_ptr(), _stream(self._device.index))
+        if st:
+            _check(st)
         return out
 
     def adamw(self, *, lr: float, betas=(0.9, 0.95), eps: float = 1e-8, step: int, clip: torch.Tensor | None = None, seed: int = 0):
@@ -316,6 +347,8 @@ class TensorSet:
         parameters without masters), another one for every step."""
         o = self._opt
         o.lr, o.beta1, o.beta2, o.eps, o.step, o.seed = lr, betas[0], betas[1], eps, step, seed
-        if clip is not None and (clip.dtype != torch.float32 or clip.numel() != 3 or not clip.is_cuda or not clip.is_contiguous()):
+        if clip is not None and (clip.dtype != _F32 or clip.numel() != 3 or not clip.is_cuda or not clip.is_contiguous()):
             raise ValueError("clip: the three floats that grad_norm returned are wanted")
-        _check(lib.cerar_adamw_step(self._h, o, None if clip is None else clip.data_ptr(), _stream()))
+        st = _adamw(self._h, self._opt_at, None if clip is None else clip.data_ptr(), _stream(self._device.index))
+        if st:
+            _check(st)

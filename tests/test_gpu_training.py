@@ -104,7 +104,7 @@ def test_quantize_writes_nothing_else(ops):
         codes = torch.full((rows * ld + 64,), 0xA5, dtype=torch.uint8, device="cuda")
         scales = torch.full((nr, nc + 3), -7.0, device="cuda")
         d = cerar.Fp8Matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, nc + 3, scaling)
-        cerar._check(cerar.lib.cerar_fp8_quantize(ops._h, x.data_ptr(), 0, cols, C.byref(d), 1, torch.cuda.current_stream().cuda_stream))
+        cerar._check(cerar.lib.cerar_fp8_quantize(ops._h, x.data_ptr(), 0, cols, C.addressof(d), 1, torch.cuda.current_stream().cuda_stream))
         body = codes[:rows * ld].view(rows, ld)
         assert bool((body[:, cols:] == 0xA5).all()) and bool((codes[rows * ld:] == 0xA5).all())
         assert bool((scales[:, nc:] == -7.0).all()) and bool((scales[:, :nc] > 0).all())
@@ -597,7 +597,7 @@ def test_refusals(ops):
         R.Quantized(q0.codes, q0.scales[:, :10], 0)
 
     def raw(d, status, cols=64):
-        s = cerar.lib.cerar_fp8_quantize(ops._h, x.data_ptr(), 0, 64, C.byref(d), 1, 0)
+        s = cerar.lib.cerar_fp8_quantize(ops._h, x.data_ptr(), 0, 64, C.addressof(d), 1, 0)
         assert s == status and cerar.lib.cerar_last_error()
 
     c, s = q0.codes.data_ptr(), q0.scales.data_ptr()
