@@ -13,6 +13,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "kernels.cuh"
 #include "ops.cuh"
 #include "ptx.cuh"
@@ -26,17 +28,46 @@ constexpr uint32_t INF = 0x7F800000u;
 
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// Four values of one row as they are in memory, and as binary32.
+// Four values of one row as they are in memory; their largest magnitudes, column by column (Top) and together (row_top), as the
+// bit patterns of binary32 numbers, which order like the magnitudes, with infinity and NaN above all numbers.
 template <typename X> struct Four;
 template <> struct Four<float> {
     float4 v;
+    struct Top { float t[4] = {0.f, 0.f, 0.f, 0.f}; };
+    static __device__ __forceinline__ float larger(float a, float b) {    // NaN if one of them is
+        float r;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+        return r;
+    }
+    static __device__ __forceinline__ float finite(float x) { return (__float_as_uint(x) & 0x7FFFFFFFu) < INF ? x : 0.f; }
     __device__ __forceinline__ void clear() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void load(const float* p) { v = __ldcs(reinterpret_cast<const float4*>(p)); }
     __device__ __forceinline__ void set(int j, float x) { (&v.x)[j] = x; }
     __device__ __forceinline__ void get(float* x) const { x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+    __device__ __forceinline__ Four finite_only() const { Four f; f.v = make_float4(finite(v.x), finite(v.y), finite(v.z), finite(v.w)); return f; }
+    __device__ __forceinline__ void fold(Top& t) const {
+        t.t[0] = larger(t.t[0], fabsf(v.x)); t.t[1] = larger(t.t[1], fabsf(v.y));
+        t.t[2] = larger(t.t[2], fabsf(v.z)); t.t[3] = larger(t.t[3], fabsf(v.w));
+    }
+    __device__ __forceinline__ uint32_t row_top() const {
+        return __float_as_uint(larger(larger(fabsf(v.x), fabsf(v.y)), larger(fabsf(v.z), fabsf(v.w))));
+    }
+    static __device__ __forceinline__ void bits(const Top& t, uint32_t* b) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(t.t[j]);
+    }
 };
 template <> struct Four<__nv_bfloat16> {
     uint2 v;
+    struct Top { uint32_t x = 0u, y = 0u; };                              // two 16-bit patterns each
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static __device__ __forceinline__ uint32_t finite(uint32_t x) {
+        return ((x & 0x7F80u) == 0x7F80u ? 0u : x & 0xFFFFu) | ((x & 0x7F800000u) == 0x7F800000u ? 0u : x & 0xFFFF0000u);
+    }
     __device__ __forceinline__ void clear() { v = make_uint2(0u, 0u); }
     __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint2*>(p)); }
     __device__ __forceinline__ void set(int j, __nv_bfloat16 x) {
@@ -47,22 +78,30 @@ template <> struct Four<__nv_bfloat16> {
         x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
         x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
     }
+    __device__ __forceinline__ Four finite_only() const { Four f; f.v = make_uint2(finite(v.x), finite(v.y)); return f; }
+    __device__ __forceinline__ void fold(Top& t) const { t.x = larger(t.x, v.x & 0x7FFF7FFFu); t.y = larger(t.y, v.y & 0x7FFF7FFFu); }
+    __device__ __forceinline__ uint32_t row_top() const {
+        const uint32_t h = larger(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu);
+        return max(h << 16, h & 0xFFFF0000u);
+    }
+    static __device__ __forceinline__ void bits(const Top& t, uint32_t* b) {
+        b[0] = t.x << 16; b[1] = t.x & 0xFFFF0000u; b[2] = t.y << 16; b[3] = t.y & 0xFFFF0000u;
+    }
 };
 
-// Four scaled values to four codes.  bad: there may be values that are not finite, which become NaN: x * 0 is NaN exactly there
+// Four scaled values to four codes.  BAD: there may be values that are not finite, which become NaN: x * 0 is NaN exactly there
 // (the conversion by itself would turn an infinity into 448).
-__device__ __forceinline__ uint32_t codes4(const float* x, const float* inv, bool bad) {
+template <bool BAD>
+__device__ __forceinline__ uint32_t codes4(const float* x, const float* inv) {
     uint16_t lo, hi;
     float y[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = x[j] * inv[j];
-    if (bad) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] += x[j] * 0.f;
-    }
+    for (int j = 0; j < 4; ++j) y[j] = BAD ? fmaf(x[j], inv[j], x[j] * 0.f) : x[j] * inv[j];
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(y[1]), "f"(y[0]));
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(y[3]), "f"(y[2]));
-    return (uint32_t)lo | ((uint32_t)hi << 16);
+    uint32_t r;
+    asm("mov.b32 %0, {%1, %2};" : "=r"(r) : "h"(lo), "h"(hi));
+    return r;
 }
 __device__ __forceinline__ void store_codes(uint8_t* dst, uint32_t v, int n) {
     if (n >= 4) { *reinterpret_cast<uint32_t*>(dst) = v; return; }
@@ -99,35 +138,45 @@ __global__ void __launch_bounds__(32 * WARPS, sizeof(X) == 2 ? 3 : 2) fp8_quanti
                 if (i < nr && j < nc) v[i].set(j, src[i * a.ldx + j]);
     }
 
-    uint32_t cm[4] = {0u, 0u, 0u, 0u};
-    bool bad = false;
-    float row_scale = 1.f;                                             // of row `lane` of this warp (lanes 0 .. ROWS - 1)
-    uint8_t* dst = BY_ROW ? a.codes[CERAR_BY_ROW] + r0 * a.ld[CERAR_BY_ROW] + c0 : nullptr;
+    // largest magnitudes: of each of this lane's columns, and lane i's of row i (lanes 0 .. ROWS - 1)
+    typename Four<X>::Top top;
+    uint32_t cm[4], row_top = 0u;
+    auto look = [&](auto finite_only) {
+        top = typename Four<X>::Top();
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        float x[4];
-        v[i].get(x);
-        uint32_t m[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) m[j] = __float_as_uint(x[j]) & 0x7FFFFFFFu;
-        if (max(max(m[0], m[1]), max(m[2], m[3])) >= INF) {           // rare: only finite magnitudes count
-            bad = true;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) if (m[j] >= INF) m[j] = 0u;
+        for (int i = 0; i < ROWS; ++i) {
+            const Four<X> f = decltype(finite_only)::value ? v[i].finite_only() : v[i];
+            if constexpr (BY_COL || BY_BLK) f.fold(top);
+            if constexpr (BY_ROW) {
+                const uint32_t t = __reduce_max_sync(0xffffffffu, f.row_top());
+                if (lane == i) row_top = t;
+            }
         }
-        if constexpr (BY_COL || BY_BLK) {
+        Four<X>::bits(top, cm);
+    };
+    look(std::false_type());
+    const bool bad = __any_sync(0xffffffffu, BY_ROW ? row_top >= INF : max(max(cm[0], cm[1]), max(cm[2], cm[3])) >= INF);
+    if (bad) look(std::true_type());                                    // rare: once more, over the finite values only
+
+    auto put = [&](int form, auto inv_of_row) {
+        uint8_t* dst = a.codes[form] + r0 * a.ld[form] + c0;
+        auto all = [&](auto with_nan) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) cm[j] = max(cm[j], m[j]);
-        }
-        if constexpr (BY_ROW) {
-            const int e = fp8_scale_exponent(__reduce_max_sync(0xffffffffu, max(max(m[0], m[1]), max(m[2], m[3]))));
-            if (lane == i) row_scale = pow2f(e);
-            const float k = pow2f(-e), inv[4] = {k, k, k, k};
-            if (i < nr) store_codes(dst + i * a.ld[CERAR_BY_ROW], codes4(x, inv, bad), nc);
-        }
-    }
+            for (int i = 0; i < ROWS; ++i) {
+                float x[4], inv[4];
+                v[i].get(x);
+                inv_of_row(i, inv);
+                const uint32_t q = codes4<decltype(with_nan)::value>(x, inv);
+                if (i < nr) store_codes(dst + i * a.ld[form], q, nc);
+            }
+        };
+        if (bad) all(std::true_type()); else all(std::false_type());
+    };
     if constexpr (BY_ROW) {
-        if (lane < nr) a.scales[CERAR_BY_ROW][tc * a.lds[CERAR_BY_ROW] + r0 + lane] = row_scale;
+        const int e = fp8_scale_exponent(row_top);
+        const float inv = pow2f(-e);
+        if (lane < nr) a.scales[CERAR_BY_ROW][tc * a.lds[CERAR_BY_ROW] + r0 + lane] = pow2f(e);
+        put(CERAR_BY_ROW, [&](int i, float* k) { k[0] = k[1] = k[2] = k[3] = __shfl_sync(0xffffffffu, inv, i); });
     }
     if constexpr (BY_COL || BY_BLK) {
         *reinterpret_cast<uint4*>(&colmax[warp][4 * lane]) = make_uint4(cm[0], cm[1], cm[2], cm[3]);
@@ -139,32 +188,19 @@ __global__ void __launch_bounds__(32 * WARPS, sizeof(X) == 2 ? 3 : 2) fp8_quanti
         }
     }
     if constexpr (BY_COL) {
-        float inv[4], sc[4];
+        float inv[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { const int e = fp8_scale_exponent(cm[j]); inv[j] = pow2f(-e); sc[j] = pow2f(e); }
-        uint8_t* dc = a.codes[CERAR_BY_COLUMN] + r0 * a.ld[CERAR_BY_COLUMN] + c0;
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            float x[4];
-            v[i].get(x);
-            if (i < nr) store_codes(dc + i * a.ld[CERAR_BY_COLUMN], codes4(x, inv, bad), nc);
+        for (int j = 0; j < 4; ++j) {
+            const int e = fp8_scale_exponent(cm[j]);
+            inv[j] = pow2f(-e);
+            if (warp == 0 && j < nc) a.scales[CERAR_BY_COLUMN][tr * a.lds[CERAR_BY_COLUMN] + c0 + j] = pow2f(e);
         }
-        if (warp == 0) {
-            float* s = a.scales[CERAR_BY_COLUMN] + tr * a.lds[CERAR_BY_COLUMN] + c0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) if (j < nc) s[j] = sc[j];
-        }
+        put(CERAR_BY_COLUMN, [&](int, float* k) { k[0] = inv[0]; k[1] = inv[1]; k[2] = inv[2]; k[3] = inv[3]; });
     }
     if constexpr (BY_BLK) {
         const int e = fp8_scale_exponent(__reduce_max_sync(0xffffffffu, max(max(cm[0], cm[1]), max(cm[2], cm[3]))));
-        const float k = pow2f(-e), inv[4] = {k, k, k, k};
-        uint8_t* db = a.codes[CERAR_BY_BLOCK] + r0 * a.ld[CERAR_BY_BLOCK] + c0;
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            float x[4];
-            v[i].get(x);
-            if (i < nr) store_codes(db + i * a.ld[CERAR_BY_BLOCK], codes4(x, inv, bad), nc);
-        }
+        const float inv = pow2f(-e);
+        put(CERAR_BY_BLOCK, [&](int, float* k) { k[0] = k[1] = k[2] = k[3] = inv; });
         if (threadIdx.x == 0) a.scales[CERAR_BY_BLOCK][tr * a.lds[CERAR_BY_BLOCK] + tc] = pow2f(e);
     }
 }

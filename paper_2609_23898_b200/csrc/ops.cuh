@@ -54,9 +54,12 @@ struct TensorRec {
     int64_t block0;                      // first state block of this tensor, counted over the set
     float lr_scale, weight_decay;
     int param_type, grad_type;
+    int vec, gvec;                       // all pointers but the gradient's / the gradient's are aligned for four elements at a time
+    int unused[2];                       // (a multiple of 16 bytes)
 };
-// Work is cut into chunks of CHUNK consecutive elements of one tensor; a list names the tensor and the chunk's
-// number inside it, so that a block finds its work with two dependent loads however many tensors there are.
+__host__ __device__ inline bool grad_vec(const void* p, int type) { return (reinterpret_cast<uintptr_t>(p) & (type == CERAR_TYPE_F32 ? 15u : 7u)) == 0; }
+// Work is cut into chunks of up to `steps` times 2048 consecutive elements of one tensor; a list names the tensor and the chunk's
+// place inside it, so that a block finds its work with two dependent loads however many tensors there are.
 constexpr int CHUNK = 2048;
 struct ChunkRef {
     int tensor;
@@ -69,6 +72,7 @@ struct NormArgs {
     const TensorRec* tensors;
     const ChunkRef* chunks;
     int64_t nchunks;
+    int steps;
     double* partial;                     // one per block
     unsigned* ticket;                    // zero between calls
     float max_norm;
@@ -80,6 +84,7 @@ struct AdamwArgs {
     const TensorRec* tensors;
     const ChunkRef* chunks;
     int64_t nchunks;
+    int steps;
     const float* clip;
     float lr, beta1, beta2, eps;         // and what the host derives from them in binary64:
     float one_minus_beta1, one_minus_beta2, step_size /* lr / (1 - beta1^step) */, root_scale /* (1 - beta2^step)^-1/2 */;

@@ -23,6 +23,7 @@ struct cerar_tensors {
     int64_t count = 0;
     int state_bits = 0;
     int64_t nchunks = 0;
+    int steps = 1;                             // a chunk has up to steps * CHUNK elements
     cerar::TensorRec* d_tensors = nullptr;
     cerar::ChunkRef* d_chunks = nullptr;       // grouped by (parameter kind, gradient type)
     double* d_partial = nullptr;
@@ -206,11 +207,18 @@ cerar_status_t cerar_tensors_create(cerar_ops_t* o, int64_t count, const cerar_t
     try {
         std::vector<cerar::TensorRec> recs((size_t)count);
         std::vector<cerar::ChunkRef> chunks;
-        int64_t block = 0;
+        int64_t block = 0, total = 0;
+        for (int64_t i = 0; i < count; ++i) total += tensors[i].numel;
+        // Long chunks where there are many (16 per SM): memory serves longer runs better (32-bit states 6.1 -> 6.4 TB/s).  Sets with
+        // 8-bit states, whose step is bound by its instructions and short of registers, keep short ones (4.6 against 5.0 TB/s).
+        set->steps = state_bits != 8 && total >= (int64_t)o->num_sms * 16 * 4 * cerar::CHUNK ? 4 : 1;
         for (int64_t i = 0; i < count; ++i) {
             const cerar_tensor_t& t = tensors[i];
             recs[i] = cerar::TensorRec{t.param, t.master, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.numel, block, t.lr_scale, t.weight_decay,
-                                       t.param_type, t.grad_type};
+                                       t.param_type, t.grad_type, 0, cerar::grad_vec(t.grad, t.grad_type) ? 1 : 0, {0, 0}};
+            const uintptr_t sa = state_bits == 32 ? 16 : 4;
+            recs[i].vec = !misaligned(t.m, sa) && !misaligned(t.v, sa) && !misaligned(t.master, 16) &&
+                          !misaligned(t.param, t.param_type == CERAR_TYPE_F32 ? 16 : 8);
             block += (t.numel + CERAR_STATE_BLOCK - 1) / CERAR_STATE_BLOCK;
             set->numel.push_back(t.numel);
             set->grad_type.push_back(t.grad_type);
@@ -222,7 +230,7 @@ cerar_status_t cerar_tensors_create(cerar_ops_t* o, int64_t count, const cerar_t
                     const cerar_tensor_t& t = tensors[i];
                     const int k = !state_bits || t.param_type == CERAR_TYPE_F32 ? cerar::PARAM_F32 : t.master ? cerar::PARAM_MASTER : cerar::PARAM_BF16;
                     if (k != kind || t.grad_type != gt) continue;
-                    for (int64_t c = 0; c * cerar::CHUNK < t.numel; ++c) chunks.push_back(cerar::ChunkRef{(int)i, (int)c});
+                    for (int64_t c = 0; c * cerar::CHUNK < t.numel; c += set->steps) chunks.push_back(cerar::ChunkRef{(int)i, (int)c});
                 }
                 if (chunks.size() > first) set->groups.push_back({kind, gt, (int64_t)first, (int64_t)(chunks.size() - first)});
             }
@@ -280,7 +288,7 @@ cerar_status_t cerar_grad_norm(cerar_tensors_t* set, float max_norm, float* clip
     if (st != CERAR_OK) return st;
     if (!clip || misaligned(clip, 4)) return fail(CERAR_ERR_INVALID_ARG, "clip must be three floats of device memory");
     if (std::isnan(max_norm)) return fail(CERAR_ERR_INVALID_ARG, "max_norm is NaN");
-    cerar::NormArgs a = {set->d_tensors, set->d_chunks, set->nchunks, set->d_partial, set->d_ticket, max_norm, clip};
+    cerar::NormArgs a = {set->d_tensors, set->d_chunks, set->nchunks, set->steps, set->d_partial, set->d_ticket, max_norm, clip};
     const cudaError_t e = cerar::launch_grad_norm(a, set->norm_blocks, (cudaStream_t)stream, &set->ops->launches);
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "grad norm launch");
 }
@@ -295,7 +303,7 @@ cerar_status_t cerar_adamw_step(cerar_tensors_t* set, const cerar_adamw_options_
         !(opt->eps >= 0.0 && std::isfinite(opt->eps)) || opt->step < 1)
         return fail(CERAR_ERR_INVALID_ARG, "AdamW wants a finite lr, betas in [0, 1), a finite eps >= 0 and a step from 1 on");
     cerar::AdamwArgs a = {};
-    a.tensors = set->d_tensors; a.clip = clip;
+    a.tensors = set->d_tensors; a.steps = set->steps; a.clip = clip;
     a.lr = (float)opt->lr; a.beta1 = (float)opt->beta1; a.beta2 = (float)opt->beta2; a.eps = (float)opt->eps; a.seed = opt->seed;
     a.one_minus_beta1 = (float)(1.0 - opt->beta1);
     a.one_minus_beta2 = (float)(1.0 - opt->beta2);

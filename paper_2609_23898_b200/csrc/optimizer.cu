@@ -71,7 +71,6 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint32_t v, int n, bool 
 #pragma unroll
     for (int j = 0; j < 4; ++j) if (j < n) p[j] = (uint8_t)(v >> (8 * j));
 }
-__device__ __forceinline__ bool aligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 // ---------------------------------------------------------------- gradient norm
 
@@ -109,22 +108,24 @@ __global__ void __launch_bounds__(THREADS) grad_norm_kernel(const __grid_constan
     for (int64_t c = blockIdx.x; c < a.nchunks; c += gridDim.x) {
         const ChunkRef ref = a.chunks[c];
         const TensorRec& t = a.tensors[ref.tensor];
-        const int64_t e0 = (int64_t)ref.index * CHUNK + warp * PER_WARP + 4 * lane;
+        int64_t e0 = (int64_t)ref.index * CHUNK + warp * PER_WARP + 4 * lane;
+        for (int step = 0; step < a.steps && e0 < t.numel; ++step, e0 += CHUNK) {
         const int64_t left = t.numel - e0;
         const int n0 = left >= 4 ? 4 : (int)max((int64_t)0, left), n1 = left >= 132 ? 4 : (int)max((int64_t)0, left - 128);
         float x[8];
         if (t.grad_type == CERAR_TYPE_F32) {
             const float* g = static_cast<const float*>(t.grad) + e0;
-            const bool al = aligned(t.grad, 16);
+            const bool al = t.gvec;
             load4(x, g, n0, al && n0 == 4);
             load4(x + 4, g + 128, n1, al && n1 == 4);
         } else {
             const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(t.grad) + e0;
-            const bool al = aligned(t.grad, 8);
+            const bool al = t.gvec;
             load4(x, g, n0, al && n0 == 4);
             load4(x + 4, g + 128, n1, al && n1 == 4);
         }
         sum += sum8(x);
+        }
     }
     sum = block_sum(sum, sh);
     // the block that arrives last adds the partial sums of all blocks, in their order
@@ -341,8 +342,13 @@ __device__ __forceinline__ void adamw_warp(const AdamwArgs& a, const TensorRec& 
     }
 }
 
+// Blocks per SM: two where the step streams 28 bytes per element and more (longer runs of each, 6.4 against 6.2 TB/s for binary32
+// parameters and states), else four.
+template <int PK, int BITS>
+constexpr int blocks_per_sm() { return BITS == 32 && PK != PARAM_BF16 ? 2 : 4; }
+
 template <int PK, typename G, int BITS>
-__global__ void __launch_bounds__(THREADS, 4) adamw_kernel(const __grid_constant__ AdamwArgs a) {
+__global__ void __launch_bounds__(THREADS, (blocks_per_sm<PK, BITS>())) adamw_kernel(const __grid_constant__ AdamwArgs a) {
     ptx::grid_dependency_wait();
     float coef = 1.f;
     if (a.clip) {
@@ -353,24 +359,28 @@ __global__ void __launch_bounds__(THREADS, 4) adamw_kernel(const __grid_constant
     for (int64_t c = blockIdx.x; c < a.nchunks; c += gridDim.x) {
         const ChunkRef ref = a.chunks[c];
         const TensorRec t = a.tensors[ref.tensor];
-        const int64_t e0 = (int64_t)ref.index * CHUNK + warp * PER_WARP;
-        if (e0 >= t.numel) continue;
-        bool vec = BITS == 32 ? aligned(t.m, 16) && aligned(t.v, 16) : aligned(t.m, 4) && aligned(t.v, 4);
-        if (PK == PARAM_F32) vec = vec && aligned(t.param, 16);
-        else vec = vec && aligned(t.param, 8) && (PK != PARAM_MASTER || aligned(t.master, 16));
-        adamw_warp<PK, G, BITS>(a, t, e0, coef, vec, aligned(t.grad, 4 * sizeof(G)));
+        int64_t e0 = (int64_t)ref.index * CHUNK + warp * PER_WARP;
+        if constexpr (BITS == 32) {
+#pragma unroll 1
+            for (int step = 0; step < a.steps && e0 < t.numel; ++step, e0 += CHUNK) adamw_warp<PK, G, BITS>(a, t, e0, coef, t.vec, t.gvec);
+        } else {
+            if (e0 < t.numel) adamw_warp<PK, G, BITS>(a, t, e0, coef, t.vec, t.gvec);
+        }
     }
 }
 
 struct GradPointers { void* p[SET_GRADS_MAX]; };
 __global__ void set_grads_kernel(TensorRec* tensors, int64_t first, int count, const __grid_constant__ GradPointers g) {
     ptx::grid_dependency_wait();
-    if ((int)threadIdx.x < count) tensors[first + threadIdx.x].grad = g.p[threadIdx.x];
+    if ((int)threadIdx.x >= count) return;
+    TensorRec& t = tensors[first + threadIdx.x];
+    t.grad = g.p[threadIdx.x];
+    t.gvec = grad_vec(t.grad, t.grad_type);
 }
 
 template <int PK, typename G, int BITS>
 cudaError_t launch_kind(const AdamwArgs& a, int num_sms, cudaStream_t s) {
-    int64_t blocks = a.nchunks < (int64_t)num_sms * 4 ? a.nchunks : (int64_t)num_sms * 4;
+    const int64_t most = (int64_t)num_sms * blocks_per_sm<PK, BITS>(), blocks = a.nchunks < most ? a.nchunks : most;
     return launch_pdl(adamw_kernel<PK, G, BITS>, dim3((unsigned)blocks), dim3(THREADS), 0, s, a);
 }
 template <int PK>
