@@ -29,6 +29,7 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 _check = cerar._check
 _E4M3, _F32 = torch.float8_e4m3fn, torch.float32
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the same handle without the Stream object around it
+_MATRIX_BYTES = C.sizeof(Fp8Matrix)
 _quantize, _matmul, _norm, _adamw = lib.cerar_fp8_quantize, lib.cerar_fp8_matmul, lib.cerar_grad_norm, lib.cerar_adamw_step
 
 
@@ -67,7 +68,7 @@ class Quantized:
     scales are read once, here, to see (which waits for the device).  Scales that are changed later have to keep to it:
     what they touch becomes NaN otherwise."""
 
-    __slots__ = ("codes", "scales", "scaling", "desc", "at")
+    __slots__ = ("_codes", "_scales", "scaling", "desc", "at", "_buffer")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, scaling: int, pow2: bool | None = None):
         if codes.element_size() != 1:
@@ -89,28 +90,75 @@ class Quantized:
         self._set(codes, scales, scaling, rows, cols, ld, _ld(scales), pow2)
 
     def _set(self, codes, scales, scaling, rows, cols, ld, lds, pow2):
-        self.codes, self.scales, self.scaling = codes, scales, scaling
+        self._codes, self._scales, self.scaling, self._buffer = codes, scales, scaling, None
         self.desc = Fp8Matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, lds, scaling, pow2)
         self.at = C.addressof(self.desc)
 
+    @staticmethod
+    def _sizes(rows, cols, scaling):
+        """Bytes between rows of codes, and the shape of the scales."""
+        ld, nr, nc = (cols + 15) & -16, (rows + 127) >> 7, (cols + 127) >> 7
+        if scaling == BY_ROW:
+            return ld, nc, rows
+        if scaling == BY_COLUMN:
+            return ld, nr, cols
+        if scaling != BY_BLOCK:
+            raise ValueError("scaling must be BY_ROW, BY_COLUMN or BY_BLOCK")
+        return ld, nr, nc
+
     @classmethod
     def empty(cls, rows: int, cols: int, scaling: int, device) -> "Quantized":
-        ld = (cols + 15) & -16
-        nr, nc = (rows + 127) >> 7, (cols + 127) >> 7
-        if scaling == BY_ROW:
-            nr, nc = nc, rows
-        elif scaling == BY_COLUMN:
-            nc = cols
-        elif scaling != BY_BLOCK:
-            raise ValueError("scaling must be BY_ROW, BY_COLUMN or BY_BLOCK")
+        ld, nr, nc = cls._sizes(rows, cols, scaling)
         codes = torch.empty(rows, ld, dtype=_E4M3, device=device)
         q = cls.__new__(cls)
         q._set(codes if ld == cols else codes[:, :cols], torch.empty(nr, nc, dtype=_F32, device=device), scaling, rows, cols, ld, nc, True)
         return q
 
+    @classmethod
+    def _several(cls, rows, cols, scalings, device):
+        """As many matrices in one allocation; their tensors are made when they are asked for.  Also the descriptors in a row."""
+        n = len(scalings)
+        out, arr, size = [], (Fp8Matrix * n)(), 0
+        for i in range(n):
+            scaling = scalings[i]
+            ld, nr, nc = cls._sizes(rows, cols, scaling)
+            at = (rows * ld + 255) & -256                            # the scales start there
+            arr[i] = Fp8Matrix(size, size + at, rows, cols, ld, nc, scaling, True)
+            size += (at + 4 * nr * nc + 255) & -256
+        buffer = torch.empty(size, dtype=_E4M3, device=device)
+        base = buffer.data_ptr()
+        first = C.addressof(arr)
+        for i in range(n):
+            q = cls.__new__(cls)
+            d = arr[i]
+            d.codes, d.scales = (d.codes or 0) + base, (d.scales or 0) + base
+            q._codes = q._scales = None
+            q.scaling, q.desc, q.at, q._buffer = d.scaling, d, first + i * _MATRIX_BYTES, buffer
+            out.append(q)
+        return out, first
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            d, b = self.desc, self._buffer
+            self._codes = b.as_strided((d.rows, d.cols), (d.ld, 1), (d.codes or 0) - b.data_ptr())
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            d, b = self.desc, self._buffer
+            _, nr, nc = self._sizes(d.rows, d.cols, d.scaling)
+            self._scales = b.view(_F32).as_strided((nr, nc), (nc, 1), ((d.scales or 0) - b.data_ptr()) >> 2)
+        return self._scales
+
+    @property
+    def device(self) -> torch.device:
+        return (self._codes if self._buffer is None else self._buffer).device
+
     @property
     def shape(self):
-        return self.codes.shape
+        return torch.Size((self.desc.rows, self.desc.cols))
 
     def dequantize(self) -> torch.Tensor:
         """The values in float32 (for inspection; torch operations)."""
@@ -155,13 +203,12 @@ class Ops:
         _matrix(x, "x")
         rows, cols = x.shape
         device = x.device
-        out = [Quantized.empty(rows, cols, s, device) for s in scalings]
-        n = len(out)
+        n = len(scalings)
         if n == 1:
+            out = [Quantized.empty(rows, cols, scalings[0], device)]
             at = out[0].at
         else:
-            arr = (Fp8Matrix * n)(*[q.desc for q in out])
-            at = C.addressof(arr)
+            out, at = Quantized._several(rows, cols, scalings, device)
         st = _quantize(self._h, x.data_ptr(), t, _ld(x), at, n, _stream(device.index))
         if st:
             _check(st)
@@ -172,7 +219,7 @@ class Ops:
         """op(a) op(b), into `out` if given (added to it with accumulate)."""
         da, db = a.desc, b.desc
         m, n = (da.cols if trans_a else da.rows), (db.rows if trans_b else db.cols)
-        device = a.codes.device
+        device = a.device
         if out is None:
             if accumulate:
                 raise ValueError("accumulate wants an `out` to add to")
