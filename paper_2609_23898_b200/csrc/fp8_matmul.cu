@@ -125,6 +125,18 @@ __device__ __forceinline__ void ld32_done(uint32_t* r) {
           "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
           "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
+__device__ __forceinline__ void ld16_start(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void ld16_done(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+          "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
 // two sums at a time (one instruction): a += x * y
 __device__ __forceinline__ uint64_t pair(uint32_t x, uint32_t y) {
     uint64_t r;
@@ -266,12 +278,18 @@ __device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, in
                 }
             } else {
                 const int e = hc + lane;
-                for (int r = 0; r < nrows; ++r) {
-                    float q;
-                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(q) : "r"(staging + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
-                    if (e < n) {
-                        C* dst = c + (int64_t)(row0 + r) * p.ldc + col0 + e;
-                        *dst = (C)((float)*dst + q);
+                C* at = c + (int64_t)row0 * p.ldc + col0 + e;
+#pragma unroll 1
+                for (int r0 = 0; r0 < nrows; r0 += 8) {                    // (eight reads of C before their stores)
+                    float old[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) old[i] = e < n && r0 + i < nrows ? (float)at[(r0 + i) * p.ldc] : 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = r0 + i;
+                        float q;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(q) : "r"(staging + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
+                        if (e < n && r < nrows) at[r * p.ldc] = (C)(old[i] + q);
                     }
                 }
             }
@@ -449,15 +467,16 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             float a_next = __ldg(sa + kb0 * p.sa.sb), b_next = 1.f;
             float bv[CW / 32];
             if constexpr (!BVEC) b_next = __ldg(sb + kb0 * p.sb.sb);
+            auto column_scales = [&](int kb) {
+#pragma unroll
+                for (int j = 0; j < CW / 32; ++j) {
+                    const int n = col0 + j * 32 + lane;
+                    bv[j] = __ldg(p.sb.p + (n < p.N ? n : p.N - 1) + kb * p.sb.sb);
+                }
+            };
+            if constexpr (BVEC) column_scales(kb0);
             for (int kb = kb0; kb < kb1; ++kb, ++it) {
                 const uint32_t buf = it % NBUF, bph = (it / NBUF) & 1u;
-                if constexpr (BVEC) {
-#pragma unroll
-                    for (int j = 0; j < CW / 32; ++j) {
-                        const int n = col0 + j * 32 + lane;
-                        bv[j] = __ldg(p.sb.p + (int64_t)(n < p.N ? n : p.N - 1) + kb * p.sb.sb);
-                    }
-                }
                 const uint64_t s = pair(__float_as_uint(a_next * b_next), __float_as_uint(a_next * b_next));
                 if (kb + 1 < kb1) {
                     a_next = __ldg(sa + (kb + 1) * p.sa.sb);
@@ -468,36 +487,34 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
                     for (int j = 0; j < CW / 32; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(staging + 4u * (j * 32 + lane)), "f"(bv[j]) : "memory");
                     __syncwarp();
+                    if (kb + 1 < kb1) column_scales(kb + 1);
                 }
                 if (!warp_wait_soon(acc_full + 8u * buf, bph)) { failed = true; break; }
                 tc_fence_after();
-                // the next 32 columns are on their way while these are added
-                uint32_t v[2][32];
+                // the next 16 columns are on their way while these are added (32 at a time leave no registers for the loop's own
+                // variables beside 128 sums: 8192^3 745 us instead of 570)
+                uint32_t v[2][16];
                 const uint32_t from = tmem + lanes + buf * BN + half * CW;
-                ld32_start(from, v[0]);
+                ld16_start(from, v[0]);
 #pragma unroll
-                for (int c = 0; c < CW / 32; ++c) {
+                for (int c = 0; c < CW / 16; ++c) {
                     uint32_t* x = v[c & 1];
-                    ld32_done(x);
-                    if (c < CW / 32 - 1) {
-                        ld32_start(from + (c + 1) * 32, v[(c + 1) & 1]);
+                    uint64_t q[8];                       // the column scales of these 16, in pairs
+                    if constexpr (BVEC) {
+#pragma unroll
+                        for (int j = 0; j < 8; j += 2)
+                            asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(q[j]), "=l"(q[j + 1]) : "r"(staging + 4u * (c * 16 + 2 * j)));
+                    }
+                    ld16_done(x);
+                    if (c < CW / 16 - 1) {
+                        ld16_start(from + (c + 1) * 16, v[(c + 1) & 1]);
                     } else {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(acc_empty + 8u * buf);
                     }
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        if constexpr (BVEC) {
-                            uint64_t q0, q1;
-                            asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(q0), "=l"(q1) : "r"(staging + 4u * (c * 32 + j)));
-                            fma_pair(acc2[c * 16 + j / 2], mul_pair(s, pair(x[j], x[j + 1])), q0);
-                            fma_pair(acc2[c * 16 + j / 2 + 1], mul_pair(s, pair(x[j + 2], x[j + 3])), q1);
-                        } else {
-                            fma_pair(acc2[c * 16 + j / 2], s, pair(x[j], x[j + 1]));
-                            fma_pair(acc2[c * 16 + j / 2 + 1], s, pair(x[j + 2], x[j + 3]));
-                        }
-                    }
+                    for (int j = 0; j < 8; ++j) fma_pair(acc2[c * 8 + j], BVEC ? mul_pair(s, q[j]) : s, pair(x[2 * j], x[2 * j + 1]));
                 }
             }
             if (failed) break;
@@ -873,6 +890,26 @@ Kernel kernel_for(bool wide, bool pow2, bool bvec) {
     return wide ? fp8_matmul_kernel<256, false, C> : fp8_matmul_kernel<128, false, C>;
 }
 
+// Tile and split.  The times are a model (ns, B200) of what was measured: a block of k costs 420 in a tile of 256 x 256 (by a pair of
+// blocks) and 315 in one of 128 x 128 where the tensor core applies the scales, 640 in 128 x 256 and 400 in 128 x 128 where it does
+// not; a tile's end costs about 800; adding up partial tiles 800 and 2000 more for 128 full rows (16 tiles of 16 blocks of k, us
+// for split 1, 2, 3, 4, 6: 9.3, 10.0, 9.1, 8.0, 7.9; one row, 16 tiles of 64: 24.7, 15.3, 12.2, 10.2, 10.6).  Large clusters do not
+// fill the GPU's groups of SMs: 128 blocks in clusters of 8 take two turns (14 us instead of 8), 108 in clusters of 4 do not.
+struct Shape { bool wide; int split; };
+Shape choose_shape(int M, int N, int kblocks, bool pow2, int num_sms) {
+    const int64_t m = (M + BM - 1) / BM, n = (N + 127) / 128, narrow = m * n;
+    const int64_t wide = pow2 ? ((m + 1) / 2) * ((n + 1) / 2) : m * ((n + 1) / 2), wide_slots = pow2 ? num_sms / 2 : num_sms;
+    Shape best{true, 1};
+    int64_t cost = ((wide + wide_slots - 1) / wide_slots) * ((int64_t)kblocks * (pow2 ? 420 : 640) + 1600);
+    for (int q = 1; q <= MAX_SPLIT && q <= kblocks; ++q) {
+        if (q > 1 && narrow * q * 100 > (int64_t)num_sms * (q == 2 ? 100 : q <= 4 ? 82 : 65)) continue;
+        const int64_t waves = q > 1 ? 1 : (narrow + num_sms - 1) / num_sms;
+        const int64_t c = waves * ((int64_t)((kblocks + q - 1) / q) * (pow2 ? 315 : 400) + 800) + (q > 1 ? 800 + 2000 * (M < BM ? M : BM) / BM : 0);
+        if (c < cost) { cost = c; best = {false, q}; }
+    }
+    return best;
+}
+
 }  // namespace
 
 cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, uint64_t* launches) {
@@ -880,21 +917,14 @@ cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, 
     Params p = {};
     const bool bvec = a.B.scaling != CERAR_BY_BLOCK, pow2 = a.A.pow2 && a.B.pow2;
     p.M = (int)a.M; p.N = (int)a.N; p.kblocks = (int)((a.K + BK - 1) / BK);
-    // wide tiles where they fill the GPU, otherwise narrow ones, and a tile shared by several blocks while SMs are left over
-    const bool wide = (int64_t)((p.M + BM - 1) / BM) * ((p.N + 255) / 256) >= num_sms;
-    const bool paired = wide && pow2;                    // tiles of 256 rows, by two blocks
+    const Shape shape = choose_shape(p.M, p.N, p.kblocks, pow2, num_sms);
+    const bool wide = shape.wide, paired = wide && pow2;                   // paired: tiles of 256 rows, by two blocks
     const int BN = wide ? 256 : 128, rows = paired ? 2 * BM : BM, b_rows = paired ? BN / 2 : BN;
     p.tiles_m = (p.M + rows - 1) / rows;
     p.tiles_n = (p.N + BN - 1) / BN;
     if ((int64_t)p.tiles_m * p.tiles_n > 0x3FFFFFFF) return cudaErrorInvalidConfiguration;
     p.tiles = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n;
-    // as many blocks per tile as keep the grid within 0.82 of the SMs, 0.65 in clusters of more than 4, which do not fill the
-    // GPU's groups of SMs (measured, us for split 1, 2, .. 6, 8: 16 tiles of 64 blocks of k 25.6, 18.5, 15.1, 12.7, 11.7, 11.0, 18.7;
-    // 27 tiles of 16 13.0, 10.3, 9.4, 8.2, 13.7; 40 tiles of 32 19.1, 13.5, 11.5; 64 tiles of 16 9.7, 10.5)
-    p.split = 1;
-    if (!wide)
-        for (int q = 2; q <= MAX_SPLIT && q <= p.kblocks; ++q)
-            if ((int64_t)p.tiles * q * 100 <= (int64_t)num_sms * (q > 4 ? 65 : 82)) p.split = q;
+    p.split = shape.split;
     p.group_m = paired ? 8 : 16;
     p.stages = wide && !paired ? 4 : 6;
     p.a_mn = a.trans_a; p.b_mn = !a.trans_b;

@@ -42,6 +42,17 @@ template <> struct Four<float> {
     static __device__ __forceinline__ float finite(float x) { return (__float_as_uint(x) & 0x7FFFFFFFu) < INF ? x : 0.f; }
     __device__ __forceinline__ void clear() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void load(const float* p) { v = __ldcs(reinterpret_cast<const float4*>(p)); }
+    // from an address that is not on a 16-byte boundary: the two groups of 16 bytes that hold the four values
+    __device__ __forceinline__ void load_across(const float* p) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15;
+        const float4 w = __ldg(reinterpret_cast<const float4*>(a)), u = __ldg(reinterpret_cast<const float4*>(a) + 1);
+        switch ((reinterpret_cast<uintptr_t>(p) >> 2) & 3u) {
+            case 1: v = make_float4(w.y, w.z, w.w, u.x); break;
+            case 2: v = make_float4(w.z, w.w, u.x, u.y); break;
+            default: v = make_float4(w.w, u.x, u.y, u.z); break;
+        }
+    }
+    static constexpr uintptr_t GROUP = 15;
     __device__ __forceinline__ void set(int j, float x) { (&v.x)[j] = x; }
     __device__ __forceinline__ void get(float* x) const { x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
     __device__ __forceinline__ Four finite_only() const { Four f; f.v = make_float4(finite(v.x), finite(v.y), finite(v.z), finite(v.w)); return f; }
@@ -70,6 +81,16 @@ template <> struct Four<__nv_bfloat16> {
     }
     __device__ __forceinline__ void clear() { v = make_uint2(0u, 0u); }
     __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint2*>(p)); }
+    __device__ __forceinline__ void load_across(const __nv_bfloat16* p) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)7;
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(a)), u = __ldg(reinterpret_cast<const uint2*>(a) + 1);
+        switch ((reinterpret_cast<uintptr_t>(p) >> 1) & 3u) {
+            case 1: v = make_uint2(__funnelshift_r(w.x, w.y, 16), __funnelshift_r(w.y, u.x, 16)); break;
+            case 2: v = make_uint2(w.y, u.x); break;
+            default: v = make_uint2(__funnelshift_r(w.y, u.x, 16), __funnelshift_r(u.x, u.y, 16)); break;
+        }
+    }
+    static constexpr uintptr_t GROUP = 7;
     __device__ __forceinline__ void set(int j, __nv_bfloat16 x) {
         const uint32_t b = (uint32_t)__bfloat16_as_ushort(x) << (16 * (j & 1));
         if (j < 2) v.x |= b; else v.y |= b;
@@ -130,6 +151,16 @@ __global__ void __launch_bounds__(32 * WARPS, sizeof(X) == 2 ? 3 : 2) fp8_quanti
 #pragma unroll
         for (int i = 0; i < ROWS; ++i)
             if (i < nr) v[i].load(src + i * a.ldx);
+    } else if (nc == 4) {
+        // rows that start anywhere: where they start is the same for the whole warp, row by row
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const X* p = src + i * a.ldx;
+            if (i < nr) {
+                if ((reinterpret_cast<uintptr_t>(p) & Four<X>::GROUP) == 0) v[i].load(p);
+                else v[i].load_across(p);
+            }
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < ROWS; ++i)

@@ -99,33 +99,44 @@ __device__ __forceinline__ double sum8(const float* x) {
     return d;
 }
 
+// Sum over n consecutive gradients of what this thread reads of them.  The order does not matter here, so a run that starts
+// off a 16-byte boundary is read from the boundary below on, in whole groups of four elements that hold at least one of the run's,
+// and what does not belong to the run counts as zero.
+template <typename G>
+__device__ __forceinline__ double sum_squares(const G* g, int n) {
+    constexpr uintptr_t GROUP = 4 * sizeof(G);
+    const int head = (int)((reinterpret_cast<uintptr_t>(g) & (GROUP - 1)) / sizeof(G));
+    g -= head;
+    n += head;
+    double sum = 0.0;
+    for (int at = (int)(threadIdx.x >> 5) * PER_WARP + 4 * (int)(threadIdx.x & 31); at < n; at += CHUNK) {
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        load4(x, g + at, 4, true);
+        if (at + 128 < n) load4(x + 4, g + at + 128, 4, true);
+        if (at < head || at + 132 > n) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = at + (j & 3) + (j >> 2) * 128;
+                if (i < head || i >= n) x[j] = 0.f;
+            }
+        }
+        sum += sum8(x);
+    }
+    return sum;
+}
+
 __global__ void __launch_bounds__(THREADS) grad_norm_kernel(const __grid_constant__ NormArgs a) {
     __shared__ double sh[THREADS / 32];
     __shared__ bool last;
     ptx::grid_dependency_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     double sum = 0.0;
     for (int64_t c = blockIdx.x; c < a.nchunks; c += gridDim.x) {
         const ChunkRef ref = a.chunks[c];
         const TensorRec& t = a.tensors[ref.tensor];
-        int64_t e0 = (int64_t)ref.index * CHUNK + warp * PER_WARP + 4 * lane;
-        for (int step = 0; step < a.steps && e0 < t.numel; ++step, e0 += CHUNK) {
-        const int64_t left = t.numel - e0;
-        const int n0 = left >= 4 ? 4 : (int)max((int64_t)0, left), n1 = left >= 132 ? 4 : (int)max((int64_t)0, left - 128);
-        float x[8];
-        if (t.grad_type == CERAR_TYPE_F32) {
-            const float* g = static_cast<const float*>(t.grad) + e0;
-            const bool al = t.gvec;
-            load4(x, g, n0, al && n0 == 4);
-            load4(x + 4, g + 128, n1, al && n1 == 4);
-        } else {
-            const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(t.grad) + e0;
-            const bool al = t.gvec;
-            load4(x, g, n0, al && n0 == 4);
-            load4(x + 4, g + 128, n1, al && n1 == 4);
-        }
-        sum += sum8(x);
-        }
+        const int64_t begin = (int64_t)ref.index * CHUNK;
+        const int64_t n = t.numel - begin < (int64_t)a.steps * CHUNK ? t.numel - begin : (int64_t)a.steps * CHUNK;
+        if (t.grad_type == CERAR_TYPE_F32) sum += sum_squares(static_cast<const float*>(t.grad) + begin, (int)n);
+        else sum += sum_squares(static_cast<const __nv_bfloat16*>(t.grad) + begin, (int)n);
     }
     sum = block_sum(sum, sh);
     // the block that arrives last adds the partial sums of all blocks, in their order
