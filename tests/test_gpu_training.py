@@ -563,6 +563,72 @@ def test_adamw_8_bit_states_hold_a_small_constant_gradient(ops):
     assert abs(m / (1e-3 * (1 - 0.9 ** 60)) - 1) < 0.01
 
 
+# ---------------------------------------------------------------------------------------------------- long tensors
+
+def test_more_than_32_bits_of_elements(ops):
+    """A tensor of more than 2^31 elements: norm, 8-bit states, stochastic bfloat16 and conversion at its far end."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    n, tail = (1 << 31) + 1000, 700
+    g = torch.zeros(n, device="cuda", dtype=torch.bfloat16)
+    g[-tail:].normal_(std=1e-3)
+    p = torch.zeros_like(g)
+    p[-tail:].normal_(std=0.02)
+    s = R.TensorSet(ops, grads=[g], params=[p], state_bits=8)
+    gt, pt = f64(g[-tail:]), f64(p[-tail:])
+    n64 = np.sqrt((gt ** 2).sum())
+    assert abs(f64(s.grad_norm(1.0))[0] - n64) <= 12 * U * n64
+    s.adamw(lr=1e-3, step=1, seed=3)
+    p64, m64, v64, up = T.adamw(pt, gt, 0.0, 0.0, lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, decay=0.0, step=1)
+    first = (n - tail) // 256 * 256                                          # the block of the first of them, and what is before it there
+    pad = n - tail - first
+    h1 = T.random_bits(first // 256, tail + pad, 3, 1)[pad:] >> np.uint64(16)
+    h0 = T.random_bits(first // 256, tail + pad, 3, 0)[pad:]
+    spacing = lambda x: 2.0 ** (np.floor(np.log2(np.maximum(x, 1e-37))) - 7)  # noqa: E731
+    assert between(np.abs(f64(p[-tail:])), np.abs(p64), 3 * U * np.abs(pt) + 24 * U * np.abs(up) + U * np.abs(p64), spacing, h1.astype(np.float64) / 65536).all()
+    full = np.concatenate([np.zeros(pad), m64])
+    bits = np.concatenate([np.zeros(pad, np.uint64), h0])
+    codes = s.m.view(torch.uint8)[first:n].cpu().numpy()
+    check_state8(codes, f64(s.m_scale)[first // 256:], full, 4 * U * np.abs(full), bits >> np.uint64(16), False)
+    assert not bool(p[:1 << 20].any()) and not bool(s.m.view(torch.uint8)[(1 << 31) - (1 << 20):1 << 31].any())
+    del s, p
+    x = g[:(n // 4096) * 4096].view(-1, 4096)
+    x[-3:].normal_()
+    want = f64(x[-3:])
+    q, = ops.quantize(x, 0)
+    qc, qs = T.quantize(want, 1, 128)
+    assert np.array_equal(f64(q.codes[-3:]), qc) and np.array_equal(f64(q.scales[:, -3:]).T, qs)
+
+
+# ---------------------------------------------------------------------------------------------------- together
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_step_of_all_workers(bits):
+    """The example: products, ring, clip and optimizer together.  The decoded mean is the workers' mean gradient up to the design's
+    error, the gradient that enters the ring is the layers' own (64-bit products of the same 8-bit operands), the loss falls."""
+    import torch
+    from paper_2609_23898_b200 import example, training as R
+    job = example.Job(workers=4, tokens=160, width=200, hidden=328, state_bits=bits)
+    losses = [job.step().item() for _ in range(40)]
+    job.check()
+    exact = job.grads.double().mean(0)
+    # eps = 1e-2: the design's error is of that order (below 10 eps); binary32 adds about kappa 2^-24 = 1e-3 of it
+    for i in range(4):
+        assert ((job.means[i].double() - exact).norm() / exact.norm()).item() < 0.1
+    n64 = float(job.means[0][:sum(p.numel() for p in job.params)].double().norm())
+    assert abs(job.clip[0].item() - n64) <= 12 * U * n64 and job.clip[2].item() == 1
+    assert losses[-1] < 0.7 * losses[0]
+    x = torch.randn(160, 200, device="cuda", dtype=torch.bfloat16)
+    w, = job.ops.quantize(job.params[0], R.BY_BLOCK)
+    y, xc = R.linear(job.ops, x, w)
+    dy = torch.randn_like(y)
+    dw = torch.zeros(328, 200, device="cuda")
+    R.linear_backward(job.ops, dy, xc, w, dw)
+    dc, = job.ops.quantize(dy, R.BY_COLUMN)
+    a, b = f64(dc.dequantize()).T, f64(xc.dequantize())
+    assert (np.abs(f64(dw) - a @ b) <= product_bound(a, b, 2, a @ b, False)).all()
+
+
 # ---------------------------------------------------------------------------------------------------- refusals
 
 def test_refusals(ops):
