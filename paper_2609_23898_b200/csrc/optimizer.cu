@@ -175,12 +175,36 @@ __device__ __forceinline__ uint32_t block_key(int64_t block, uint64_t seed, uint
 }
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
+// Two binary32 numbers in a 64-bit register and the instructions that work on both.
+__device__ __forceinline__ uint64_t two(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void split2(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2x(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
 // Values of four e4m3 codes times a scale (the conversion goes through binary16, which holds them all).
 __device__ __forceinline__ void code_values(uint32_t codes, float scale, float* x) {
     uint32_t lo, hi;
     asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n" : "=r"(lo), "=r"(hi) : "r"(codes));
     const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-    x[0] = a.x * scale; x[1] = a.y * scale; x[2] = b.x * scale; x[3] = b.y * scale;
+    const uint64_t s2 = two(scale, scale);
+    split2(mul2(two(a.x, a.y), s2), x[0], x[1]);
+    split2(mul2(two(b.x, b.y), s2), x[2], x[3]);
 }
 __device__ __forceinline__ float max_nan(float a, float b) {           // NaN if one of them is
     float r;
@@ -256,22 +280,36 @@ __device__ __forceinline__ void adamw_warp(const AdamwArgs& a, const TensorRec& 
         code_values(vc[0], vsc, v);
         code_values(vc[1], vsc, v + 4);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], v[j]);
+        for (int j = 0; j < 8; j += 2) split2(mul2(two(v[j], v[j + 1]), two(v[j], v[j + 1])), v[j], v[j + 1]);
     }
     const float step = a.step_size * t.lr_scale, keep = 1.f - a.lr * t.lr_scale * t.weight_decay;
+    const uint64_t coef2 = two(coef, coef), b1 = two(a.beta1, a.beta1), c1 = two(a.one_minus_beta1, a.one_minus_beta1), b2 = two(a.beta2, a.beta2),
+                   c2 = two(a.one_minus_beta2, a.one_minus_beta2), keep2 = two(keep, keep), rs2 = two(a.root_scale, a.root_scale), eps2 = two(a.eps, a.eps);
     float r[8];
     float mtop = 0.f, rtop = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        // each product and sum rounded by itself (no contraction), as the formula is written
-        const float gc = __fmul_rn(g[j], coef);
-        m[j] = __fadd_rn(__fmul_rn(m[j], a.beta1), __fmul_rn(gc, a.one_minus_beta1));
-        v[j] = __fadd_rn(__fmul_rn(v[j], a.beta2), __fmul_rn(__fmul_rn(gc, gc), a.one_minus_beta2));
-        // (the root of an 8-bit state decides which code is kept: rounded to nearest; otherwise only the update sees it: within 2 u)
-        if constexpr (BITS == 8) r[j] = __fsqrt_rn(v[j]);
-        else asm("sqrt.approx.f32 %0, %1;" : "=f"(r[j]) : "f"(v[j]));
-        p[j] = fmaf(-step, __fdividef(m[j], fmaf(r[j], a.root_scale, a.eps)), p[j] * keep);
-        if constexpr (BITS == 8) { mtop = max_nan(mtop, fabsf(m[j])); rtop = max_nan(rtop, r[j]); }
+    for (int j = 0; j < 8; j += 2) {
+        // two elements per instruction; each product and sum rounded by itself (no contraction), as the formula is written
+        const uint64_t g2 = mul2(two(g[j], g[j + 1]), coef2);
+        const uint64_t m2 = add2(mul2(two(m[j], m[j + 1]), b1), mul2(g2, c1));
+        const uint64_t v2 = add2(mul2(two(v[j], v[j + 1]), b2), mul2(mul2(g2, g2), c2));
+        split2(m2, m[j], m[j + 1]);
+        split2(v2, v[j], v[j + 1]);
+#pragma unroll
+        for (int i = j; i < j + 2; ++i) {
+            // (the root of an 8-bit state decides which code is kept: rounded to nearest; otherwise only the update sees it: within 2 u)
+            if constexpr (BITS == 8) r[i] = __fsqrt_rn(v[i]);
+            else asm("sqrt.approx.f32 %0, %1;" : "=f"(r[i]) : "f"(v[i]));
+        }
+        float d0, d1, q0, q1;
+        split2(fma2x(two(r[j], r[j + 1]), rs2, eps2), d0, d1);
+        split2(mul2(two(p[j], p[j + 1]), keep2), q0, q1);
+        p[j] = fmaf(-step, __fdividef(m[j], d0), q0);
+        p[j + 1] = fmaf(-step, __fdividef(m[j + 1], d1), q1);
+        if constexpr (BITS == 8) {
+            mtop = max_nan(mtop, max_nan(fabsf(m[j]), fabsf(m[j + 1])));
+            rtop = max_nan(rtop, max_nan(r[j], r[j + 1]));
+        }
     }
     if constexpr (BITS == 32) {
         store4(static_cast<float*>(t.m) + i0, m, n0, v0);
