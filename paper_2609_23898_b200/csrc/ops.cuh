@@ -88,6 +88,7 @@ struct AdamwArgs {
     const float* clip;
     float lr, beta1, beta2, eps;         // and what the host derives from them in binary64:
     float one_minus_beta1, one_minus_beta2, step_size /* lr / (1 - beta1^step) */, root_scale /* (1 - beta2^step)^-1/2 */;
+    float minus_zero;                    // -0
     uint64_t seed;
 };
 cudaError_t launch_adamw(const AdamwArgs& a, int param_kind, int grad_type, int state_bits, int num_sms, cudaStream_t s,

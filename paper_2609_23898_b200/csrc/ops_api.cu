@@ -304,6 +304,7 @@ cerar_status_t cerar_adamw_step(cerar_tensors_t* set, const cerar_adamw_options_
         return fail(CERAR_ERR_INVALID_ARG, "AdamW wants a finite lr, betas in [0, 1), a finite eps >= 0 and a step from 1 on");
     cerar::AdamwArgs a = {};
     a.tensors = set->d_tensors; a.steps = set->steps; a.clip = clip;
+    a.minus_zero = -0.f;
     a.lr = (float)opt->lr; a.beta1 = (float)opt->beta1; a.beta2 = (float)opt->beta2; a.eps = (float)opt->eps; a.seed = opt->seed;
     a.one_minus_beta1 = (float)(1.0 - opt->beta1);
     a.one_minus_beta2 = (float)(1.0 - opt->beta2);

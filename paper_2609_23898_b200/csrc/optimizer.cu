@@ -285,14 +285,17 @@ __device__ __forceinline__ void adamw_warp(const AdamwArgs& a, const TensorRec& 
     const float step = a.step_size * t.lr_scale, keep = 1.f - a.lr * t.lr_scale * t.weight_decay;
     const uint64_t coef2 = two(coef, coef), b1 = two(a.beta1, a.beta1), c1 = two(a.one_minus_beta1, a.one_minus_beta1), b2 = two(a.beta2, a.beta2),
                    c2 = two(a.one_minus_beta2, a.one_minus_beta2), keep2 = two(keep, keep), rs2 = two(a.root_scale, a.root_scale), eps2 = two(a.eps, a.eps);
+    // a b + (-0) rounded once is the product a b; written as a product it is contracted with the sum behind it, and the states differ
+    // in the last place from the formula's, now and then in the code that is kept.  -0 comes from the host: known here, it is folded away
+    const uint64_t nil = two(a.minus_zero, a.minus_zero);
     float r[8];
     float mtop = 0.f, rtop = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
         // two elements per instruction; each product and sum rounded by itself (no contraction), as the formula is written
         const uint64_t g2 = mul2(two(g[j], g[j + 1]), coef2);
-        const uint64_t m2 = add2(mul2(two(m[j], m[j + 1]), b1), mul2(g2, c1));
-        const uint64_t v2 = add2(mul2(two(v[j], v[j + 1]), b2), mul2(mul2(g2, g2), c2));
+        const uint64_t m2 = add2(fma2x(two(m[j], m[j + 1]), b1, nil), fma2x(g2, c1, nil));
+        const uint64_t v2 = add2(fma2x(two(v[j], v[j + 1]), b2, nil), fma2x(mul2(g2, g2), c2, nil));
         split2(m2, m[j], m[j + 1]);
         split2(v2, v[j], v[j + 1]);
 #pragma unroll
