@@ -6,7 +6,7 @@
 // 128 values of a row, 128 values of a column, or 128 x 128 values; every wanted form is made from one
 // reading of x.  Nothing but bytes bounds this: 2 or 4 in, 1 out per form and element.
 //
-// One CTA per 128 x 128 tile, the tile in registers: warp w holds rows 16 w .. 16 w + 15, lane l the columns 4 l .. 4 l + 3 of
+// One CTA per 128 x 128 tile, the tile in registers: a warp holds 16 (or 8) consecutive rows, lane l the columns 4 l .. 4 l + 3 of
 // each, so a warp reads whole row segments (256 or 512 contiguous bytes) and stores 128.
 // A row's maximum is one warp reduction; a column's goes through shared memory once; all forms are stored row-major, as the
 // products read them, so nothing is transposed.
@@ -23,7 +23,11 @@ namespace cerar {
 namespace {
 
 constexpr int T = FP8_BLOCK;             // tile edge
-constexpr int WARPS = 8, ROWS = T / WARPS;
+// Warps of a CTA and CTAs per SM: what keeps a tile's values in registers and as many loads on their way as possible.  Measured
+// (16384 x 8192, by row / by column / both, TB/s): bfloat16 8 warps x 3 6.1 / 6.0 / 5.5, 8 x 4 6.4 / 6.3 / 4.4 (spills with two forms),
+// 8 x 2 6.1 / 4.9 / 4.9; binary32 16 x 2 6.7 / 5.8 / 5.9, 16 x 1 6.7 / 4.0 / 4.4.
+template <typename X> constexpr int kWarps = sizeof(X) == 2 ? 8 : 16;
+template <typename X, int FORMS> constexpr int kPerSm = sizeof(X) == 4 ? 2 : (FORMS & (FORMS - 1)) == 0 ? 4 : 3;
 constexpr uint32_t INF = 0x7F800000u;
 
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
@@ -132,7 +136,8 @@ __device__ __forceinline__ void store_codes(uint8_t* dst, uint32_t v, int n) {
 
 // FORMS: bit per cerar_scaling_t
 template <typename X, int FORMS>
-__global__ void __launch_bounds__(32 * WARPS, sizeof(X) == 2 ? 3 : 2) fp8_quantize_kernel(const __grid_constant__ QuantizeArgs a, uint32_t tiles_c) {
+__global__ void __launch_bounds__(32 * kWarps<X>, (kPerSm<X, FORMS>)) fp8_quantize_kernel(const __grid_constant__ QuantizeArgs a, uint32_t tiles_c) {
+    constexpr int WARPS = kWarps<X>, ROWS = T / WARPS;
     constexpr bool BY_ROW = FORMS & (1 << CERAR_BY_ROW), BY_COL = FORMS & (1 << CERAR_BY_COLUMN), BY_BLK = FORMS & (1 << CERAR_BY_BLOCK);
     __shared__ uint32_t colmax[BY_COL || BY_BLK ? WARPS : 1][T];
     ptx::grid_dependency_wait();
@@ -145,17 +150,23 @@ __global__ void __launch_bounds__(32 * WARPS, sizeof(X) == 2 ? 3 : 2) fp8_quanti
 
     Four<X> v[ROWS];
     const X* src = static_cast<const X*>(a.x) + r0 * a.ldx + c0;
+    // a tile inside the matrix needs no bounds, row by row (the same for the whole CTA)
+    const bool whole = (int64_t)(tr + 1) * T <= a.rows && (int64_t)(tc + 1) * T <= a.cols;
+    if (whole && a.vec) {
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) v[i].clear();
-    if (a.vec && nc == 4) {
+        for (int i = 0; i < ROWS; ++i, src += a.ldx) v[i].load(src);
+    } else if (a.vec && nc == 4) {
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i)
+        for (int i = 0; i < ROWS; ++i) {
+            v[i].clear();
             if (i < nr) v[i].load(src + i * a.ldx);
+        }
     } else if (nc == 4) {
         // rows that start anywhere: where they start is the same for the whole warp, row by row
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             const X* p = src + i * a.ldx;
+            v[i].clear();
             if (i < nr) {
                 if ((reinterpret_cast<uintptr_t>(p) & Four<X>::GROUP) == 0) v[i].load(p);
                 else v[i].load_across(p);
@@ -163,10 +174,12 @@ __global__ void __launch_bounds__(32 * WARPS, sizeof(X) == 2 ? 3 : 2) fp8_quanti
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i)
+        for (int i = 0; i < ROWS; ++i) {
+            v[i].clear();
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (i < nr && j < nc) v[i].set(j, src[i * a.ldx + j]);
+        }
     }
 
     // largest magnitudes: of each of this lane's columns, and lane i's of row i (lanes 0 .. ROWS - 1)
@@ -191,17 +204,25 @@ __global__ void __launch_bounds__(32 * WARPS, sizeof(X) == 2 ? 3 : 2) fp8_quanti
 
     auto put = [&](int form, auto inv_of_row) {
         uint8_t* dst = a.codes[form] + r0 * a.ld[form] + c0;
-        auto all = [&](auto with_nan) {
+        const int64_t ld = a.ld[form];
+        if (whole && !bad) {
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
+            for (int i = 0; i < ROWS; ++i, dst += ld) {
                 float x[4], inv[4];
                 v[i].get(x);
                 inv_of_row(i, inv);
-                const uint32_t q = codes4<decltype(with_nan)::value>(x, inv);
-                if (i < nr) store_codes(dst + i * a.ld[form], q, nc);
+                *reinterpret_cast<uint32_t*>(dst) = codes4<false>(x, inv);
             }
-        };
-        if (bad) all(std::true_type()); else all(std::false_type());
+        } else {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i, dst += ld) {
+                float x[4], inv[4];
+                v[i].get(x);
+                inv_of_row(i, inv);
+                const uint32_t q = codes4<true>(x, inv);
+                if (i < nr) store_codes(dst, q, nc);
+            }
+        }
     };
     if constexpr (BY_ROW) {
         const int e = fp8_scale_exponent(row_top);
@@ -241,7 +262,7 @@ cudaError_t launch_forms(const QuantizeArgs& a, int forms, dim3 grid, uint32_t t
 
 template <typename X, int FORMS>
 cudaError_t launch_one(const QuantizeArgs& a, dim3 grid, uint32_t tiles_c, cudaStream_t s) {
-    return launch_pdl(fp8_quantize_kernel<X, FORMS>, grid, dim3(32 * WARPS), 0, s, a, tiles_c);
+    return launch_pdl(fp8_quantize_kernel<X, FORMS>, grid, dim3(32 * kWarps<X>), 0, s, a, tiles_c);
 }
 template <typename X>
 cudaError_t launch_forms(const QuantizeArgs& a, int forms, dim3 grid, uint32_t tiles_c, cudaStream_t s) {

@@ -1,0 +1,73 @@
+"""Host side of the training-step operators: what the binding and the argument checks do without a device."""
+import ctypes as C
+import os
+import re
+
+import pytest
+
+from paper_2609_23898_b200 import cerar
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_every_declared_call_is_exported_and_bound():
+    text = open(os.path.join(ROOT, "include", "cerar.h")).read()
+    names = set(re.findall(r"\b(cerar_(?:ops|fp8_quantize|fp8_matmul|tensors|grad|adamw)\w*)\s*\(", text))
+    assert {"cerar_ops_create", "cerar_fp8_quantize", "cerar_fp8_matmul", "cerar_grad_norm", "cerar_adamw_step"} <= names
+    for n in names:
+        assert getattr(cerar.lib, n).argtypes is not None, n
+
+
+def test_structures_have_the_header_s_layout():
+    # pointers and 64-bit numbers first, the 32-bit ones behind them: no padding but at the end
+    assert C.sizeof(cerar.Fp8Matrix) == 2 * 8 + 4 * 8 + 2 * 4
+    assert C.sizeof(cerar.TensorDesc) == 8 * 8 + 4 * 4
+    assert C.sizeof(cerar.AdamwOptions) == 6 * 8
+    text = open(os.path.join(ROOT, "include", "cerar.h")).read()
+    for struct, end in ((cerar.Fp8Matrix, "cerar_fp8_matrix_t"), (cerar.TensorDesc, "cerar_tensor_t"), (cerar.AdamwOptions, "cerar_adamw_options_t")):
+        body = re.sub(r"/\*.*?\*/", "", text[:text.index("} " + end)].rsplit("typedef struct {", 1)[1], flags=re.S)
+        fields = [f.strip(" *") for line in body.split(";") if line.strip() for f in re.sub(r"^\s*(const\s+)?\w+", "", line.strip()).split(",")]
+        assert fields == [f for f, _ in struct._fields_], end
+
+
+def test_without_a_handle_every_call_is_refused():
+    lib = cerar.lib
+    d, o = cerar.Fp8Matrix(), cerar.AdamwOptions()
+    assert lib.cerar_ops_create(None) == 1
+    assert lib.cerar_ops_status(None, None) == 1
+    assert lib.cerar_ops_launch_count(None) == 0
+    assert lib.cerar_fp8_quantize(None, 16, 0, 1, C.addressof(d), 1, None) == 1
+    assert lib.cerar_fp8_matmul(None, C.addressof(d), 0, C.addressof(d), 1, 16, 0, 1, 0, None) == 1
+    out = C.c_void_p(7)
+    assert lib.cerar_tensors_create(None, 0, None, 32, C.byref(out)) == 1 and not out.value
+    assert lib.cerar_tensors_set_grads(None, None, None) == 1
+    assert lib.cerar_grad_norm(None, 1.0, 16, None) == 1
+    assert lib.cerar_adamw_step(None, C.addressof(o), None, None) == 1
+    lib.cerar_ops_destroy(None)
+    lib.cerar_tensors_destroy(None)
+    assert b"NULL" in lib.cerar_last_error()
+
+
+def test_without_a_device_there_is_no_handle():
+    import torch
+    from paper_2609_23898_b200 import training
+    if torch.cuda.is_available():
+        pytest.skip("there is a device")
+    with pytest.raises(cerar.CerarError) as e:
+        training.Ops()
+    assert e.value.status == 6
+
+
+def test_matrices_that_are_refused_before_any_call():
+    import torch
+    from paper_2609_23898_b200 import training as R
+    codes, scales = torch.zeros(4, 16, dtype=torch.uint8), torch.ones(1, 4)
+    with pytest.raises(ValueError):
+        R.Quantized(codes, scales, R.BY_ROW)                    # not on a device
+    with pytest.raises(TypeError):
+        R.Quantized(codes.float(), scales, R.BY_ROW)
+    with pytest.raises(ValueError):
+        R.Quantized._sizes(4, 16, 3)
+    assert R.Quantized._sizes(130, 300, R.BY_ROW) == (304, 3, 130)
+    assert R.Quantized._sizes(130, 300, R.BY_COLUMN) == (304, 2, 300)
+    assert R.Quantized._sizes(130, 300, R.BY_BLOCK) == (304, 2, 3)
