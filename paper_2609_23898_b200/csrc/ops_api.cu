@@ -208,10 +208,15 @@ cerar_status_t cerar_tensors_create(cerar_ops_t* o, int64_t count, const cerar_t
         std::vector<cerar::TensorRec> recs((size_t)count);
         std::vector<cerar::ChunkRef> chunks;
         int64_t block = 0, total = 0;
-        for (int64_t i = 0; i < count; ++i) total += tensors[i].numel;
+        bool plain_bf16 = false;
+        for (int64_t i = 0; i < count; ++i) {
+            total += tensors[i].numel;
+            plain_bf16 = plain_bf16 || (state_bits && tensors[i].param_type == CERAR_TYPE_BF16 && !tensors[i].master);
+        }
         // Long chunks where there are many (16 per SM): memory serves longer runs better (32-bit states 6.1 -> 6.4 TB/s).  Sets with
-        // 8-bit states, whose step is bound by its instructions and short of registers, keep short ones (4.6 against 5.0 TB/s).
-        set->steps = state_bits != 8 && total >= (int64_t)o->num_sms * 16 * 4 * cerar::CHUNK ? 4 : 1;
+        // 8-bit states, whose step is bound by its instructions and short of registers, keep short ones (4.6 against 5.0 TB/s), and so do
+        // sets with bfloat16 parameters without master copies (6.4 against 6.65).
+        set->steps = state_bits != 8 && !plain_bf16 && total >= (int64_t)o->num_sms * 16 * 4 * cerar::CHUNK ? 4 : 1;
         for (int64_t i = 0; i < count; ++i) {
             const cerar_tensor_t& t = tensors[i];
             recs[i] = cerar::TensorRec{t.param, t.master, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.numel, block, t.lr_scale, t.weight_decay,

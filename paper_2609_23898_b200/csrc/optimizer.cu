@@ -240,14 +240,15 @@ __device__ __forceinline__ uint32_t finite_magnitude(float x) {
     return b < 0x7F800000u ? b : 0u;
 }
 
-template <int PK, typename G, int BITS>
+// FULL: all 256 elements exist and everything but the gradient is aligned for four at a time; nothing is checked element by element.
+template <int PK, typename G, int BITS, bool FULL>
 __device__ __forceinline__ void adamw_warp(const AdamwArgs& a, const TensorRec& t, int64_t e0 /* first element of the warp's block */, float coef,
                                            bool vec, bool gvec) {
     const int lane = threadIdx.x & 31;
     const int64_t left = t.numel - e0 - 4 * lane;
-    const int n0 = left >= 4 ? 4 : (int)max((int64_t)0, left), n1 = left >= 132 ? 4 : (int)max((int64_t)0, left - 128);
+    const int n0 = FULL || left >= 4 ? 4 : (int)max((int64_t)0, left), n1 = FULL || left >= 132 ? 4 : (int)max((int64_t)0, left - 128);
     const int64_t i0 = e0 + 4 * lane, i1 = i0 + 128;
-    const bool v0 = vec && n0 == 4, v1 = vec && n1 == 4, g0 = gvec && n0 == 4, g1 = gvec && n1 == 4;
+    const bool v0 = FULL || (vec && n0 == 4), v1 = FULL || (vec && n1 == 4), g0 = gvec && n0 == 4, g1 = gvec && n1 == 4;
     float g[8], p[8], m[8], v[8];
     uint32_t mc[2], vc[2];
     float msc = 0.f, vsc = 0.f;
@@ -412,11 +413,10 @@ __global__ void __launch_bounds__(THREADS, (blocks_per_sm<PK, BITS>())) adamw_ke
         const ChunkRef ref = a.chunks[c];
         const TensorRec t = a.tensors[ref.tensor];
         int64_t e0 = (int64_t)ref.index * CHUNK + warp * PER_WARP;
-        if constexpr (BITS == 32) {
 #pragma unroll 1
-            for (int step = 0; step < a.steps && e0 < t.numel; ++step, e0 += CHUNK) adamw_warp<PK, G, BITS>(a, t, e0, coef, t.vec, t.gvec);
-        } else {
-            if (e0 < t.numel) adamw_warp<PK, G, BITS>(a, t, e0, coef, t.vec, t.gvec);
+        for (int step = 0; step < (BITS == 32 ? a.steps : 1) && e0 < t.numel; ++step, e0 += CHUNK) {
+            if ((BITS == 8 || PK != PARAM_BF16) && t.vec && e0 + PER_WARP <= t.numel) adamw_warp<PK, G, BITS, true>(a, t, e0, coef, true, t.gvec);
+            else adamw_warp<PK, G, BITS, false>(a, t, e0, coef, t.vec, t.gvec);
         }
     }
 }
