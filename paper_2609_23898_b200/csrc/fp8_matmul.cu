@@ -63,6 +63,8 @@ struct Params {
     int a_mn, b_mn;                                    // 1: the operand's own dimension (m or n) is the contiguous one
     int accumulate, c_vec;
     int stages, split;
+    uint32_t a_bytes;                                  // what a load of A brings (a matrix of few rows: those rows only; the others'
+                                                       // sums are made of whatever lies there, row by row, and not stored)
     int early;                                         // 1: the next kernel of the stream may set itself up meanwhile (on SMs that this one leaves free)
     int* status;
 };
@@ -302,6 +304,7 @@ template <int BN>
 __device__ __forceinline__ void produce(const Params& p, const CUtensorMap& map_a, const CUtensorMap& map_b, uint32_t smem, uint32_t full, uint32_t empty,
                                         uint32_t t0, uint32_t tstep, int kb0, int kb1, bool& failed) {
     constexpr uint32_t STAGE = A_BYTES + BN * BK;
+    const uint32_t loaded = p.a_bytes + BN * BK;
     uint32_t it = 0;
     for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
         int tm, tn;
@@ -311,7 +314,7 @@ __device__ __forceinline__ void produce(const Params& p, const CUtensorMap& map_
             const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u;
             if (!wait_soon(empty + 8u * s, ph ^ 1u)) { failed = true; break; }
             const uint32_t a = smem + s * STAGE, b = a + A_BYTES, bar = full + 8u * s;
-            mbar_arrive_expect_tx(bar, STAGE);
+            mbar_arrive_expect_tx(bar, loaded);
             if (p.a_mn) tma_load_2d(a, &map_a, m0, kb * BK, bar);
             else tma_load_2d(a, &map_a, kb * BK, m0, bar);
             if (p.b_mn) {
@@ -669,7 +672,7 @@ fp8_matmul_pow2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
                         const uint32_t s = it % p.stages, ph = (it / p.stages) & 1u;
                         if (!wait_soon(empty + 8u * s, ph ^ 1u)) { failed = true; break; }
                         const uint32_t a = smem + s * STAGE, b = a + A_BYTES;
-                        if (pair_rank == 0) mbar_arrive_expect_tx(full + 8u * s, CG * STAGE);       // what both blocks load
+                        if (pair_rank == 0) mbar_arrive_expect_tx(full + 8u * s, CG * (p.a_bytes + B_ROWS * BK));       // what both blocks load
                         const uint32_t bar = CG == 1 ? full + 8u * s : in_block(full + 8u * s, 0);
                         if (p.a_mn) tma_load_operand<CG>(a, &map_a, m0, kb * BK, bar);
                         else tma_load_operand<CG>(a, &map_a, kb * BK, m0, bar);
@@ -934,7 +937,9 @@ cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, 
     const int64_t size = a.type == CERAR_TYPE_F32 ? 4 : 2;
     p.c_vec = (reinterpret_cast<uintptr_t>(a.C) & 15u) == 0 && (a.ldc * size) % 16 == 0;
     CUtensorMap ma, mb;
-    if (!make_map_8bit(&ma, a.A, BM) || !make_map_8bit(&mb, a.B, p.b_mn ? BK : b_rows)) return cudaErrorInvalidValue;
+    const int a_rows = !p.a_mn && p.M < BM ? (p.M + 7) & ~7 : BM;
+    p.a_bytes = (uint32_t)a_rows * BK;
+    if (!make_map_8bit(&ma, a.A, p.a_mn ? BK : a_rows) || !make_map_8bit(&mb, a.B, p.b_mn ? BK : b_rows)) return cudaErrorInvalidValue;
     const int cluster = paired ? 2 : p.split, most = num_sms / cluster;
     const int grid = cluster * (p.split > 1 || (int)p.tiles < most ? (int)p.tiles : most);
     p.early = 2 * grid <= num_sms;
