@@ -7,7 +7,12 @@
 // taken out after every block, multiplied by its scales and added to the running sum in registers (binary32), while the
 // tensor core works on the next block in the other half of tensor memory.  At 128 x 256 x 128 the products take 512 clk; taking
 // them out is 256 columns per warp quadrant (256 clk) and 64 packed multiply-adds per warp (twice that with a scale per
-// column of B), done by two warps per quadrant.
+// column of B), done by two warps per quadrant.  Taking out is what bounds this form (tensor pipe 52 % active; 31 % with a scale
+// per column).  Measured on B200, bfloat16 results: 8192^3 530 us (2070 TFLOP/s), 890 us with a scale per column of B.
+//
+// Where all scales are powers of two the tensor core multiplies by them itself and nothing is taken out before 16 blocks of k are
+// summed up: fp8_matmul_pow2_kernel below, 8192^3 416 us (2640 TFLOP/s), 16384 x 8192 x 2048 234 us (2350).  In a long
+// loop the power limit decides (8192^3: 485 us at 1.27 GHz); the library's own 8-bit product takes 413 and 197 us at these sizes.
 //
 // Operands come in as tiles of 128 bytes of one dimension by 128 (or BN) of the other, in the 128-byte swizzle that the
 // tensor core reads, whichever dimension is contiguous in memory: a transposed operand is read in place (the "MN-major" form).
