@@ -363,9 +363,14 @@ __device__ __forceinline__ void add_partials(const Params& p, uint32_t smem, int
         const int n0 = tn * BN + 4 * j;
         C* dst = c + (int64_t)(tm * BM + r) * p.ldc + n0;
         const float x[4] = {v.x, v.y, v.z, v.w};
+        if (p.c_vec && !p.accumulate && n0 + 4 <= p.N) {
+            if constexpr (sizeof(C) == 4) *reinterpret_cast<float4*>(dst) = v;
+            else *reinterpret_cast<uint2*>(dst) = make_uint2(Out<C>::two(v.x, v.y), Out<C>::two(v.z, v.w));
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (n0 + e < p.N) dst[e] = (C)(p.accumulate ? (float)dst[e] + x[e] : x[e]);
+            for (int e = 0; e < 4; ++e)
+                if (n0 + e < p.N) dst[e] = (C)(p.accumulate ? (float)dst[e] + x[e] : x[e]);
+        }
     }
 }
 

@@ -30,6 +30,7 @@ _check = cerar._check
 _E4M3, _F32 = torch.float8_e4m3fn, torch.float32
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the same handle without the Stream object around it
 _MATRIX_BYTES = C.sizeof(Fp8Matrix)
+_LAYOUTS: dict = {}      # (rows, cols, scalings) -> where the parts of such matrices lie in one allocation
 _quantize, _matmul, _norm, _adamw = lib.cerar_fp8_quantize, lib.cerar_fp8_matmul, lib.cerar_grad_norm, lib.cerar_adamw_step
 
 
@@ -117,25 +118,38 @@ class Quantized:
     @classmethod
     def _several(cls, rows, cols, scalings, device):
         """As many matrices in one allocation; their tensors are made when they are asked for.  Also the descriptors in a row."""
-        n = len(scalings)
-        out, arr, size = [], (Fp8Matrix * n)(), 0
-        for i in range(n):
-            scaling = scalings[i]
-            ld, nr, nc = cls._sizes(rows, cols, scaling)
-            at = (rows * ld + 255) & -256                            # the scales start there
-            arr[i] = Fp8Matrix(size, size + at, rows, cols, ld, nc, scaling, True)
-            size += (at + 4 * nr * nc + 255) & -256
+        layout = _LAYOUTS.get((rows, cols, scalings))
+        if layout is None:
+            layout = cls._layout(rows, cols, scalings)
+        size, kind, template, offsets = layout
+        arr = kind.from_buffer_copy(template)
         buffer = torch.empty(size, dtype=_E4M3, device=device)
-        base = buffer.data_ptr()
-        first = C.addressof(arr)
-        for i in range(n):
+        base, at = buffer.data_ptr(), C.addressof(arr)
+        first, out = at, []
+        for d, (codes, scales) in zip(arr, offsets):
+            d.codes, d.scales = base + codes, base + scales
             q = cls.__new__(cls)
-            d = arr[i]
-            d.codes, d.scales = (d.codes or 0) + base, (d.scales or 0) + base
             q._codes = q._scales = None
-            q.scaling, q.desc, q.at, q._buffer = d.scaling, d, first + i * _MATRIX_BYTES, buffer
+            q.scaling, q.desc, q.at, q._buffer = d.scaling, d, at, buffer
+            at += _MATRIX_BYTES
             out.append(q)
         return out, first
+
+    @classmethod
+    def _layout(cls, rows, cols, scalings):
+        """Where codes and scales of these matrices lie in one allocation, and their descriptors but for the addresses."""
+        n = len(scalings)
+        arr, offsets, size = (Fp8Matrix * n)(), [], 0
+        for i, scaling in enumerate(scalings):
+            ld, nr, nc = cls._sizes(rows, cols, scaling)
+            at = size + ((rows * ld + 255) & -256)                   # the scales start there
+            arr[i] = Fp8Matrix(0, 0, rows, cols, ld, nc, scaling, True)
+            offsets.append((size, at))
+            size = (at + 4 * nr * nc + 255) & -256
+        if len(_LAYOUTS) >= 1024:
+            _LAYOUTS.clear()
+        _LAYOUTS[rows, cols, scalings] = layout = (size, Fp8Matrix * n, bytes(arr), offsets)
+        return layout
 
     @property
     def codes(self) -> torch.Tensor:
@@ -203,13 +217,12 @@ class Ops:
         _matrix(x, "x")
         rows, cols = x.shape
         device = x.device
-        n = len(scalings)
-        if n == 1:
+        if len(scalings) == 1 and not cols & 15:                    # two allocations cost the host less than two views of one
             out = [Quantized.empty(rows, cols, scalings[0], device)]
             at = out[0].at
         else:
             out, at = Quantized._several(rows, cols, scalings, device)
-        st = _quantize(self._h, x.data_ptr(), t, _ld(x), at, n, _stream(device.index))
+        st = _quantize(self._h, x.data_ptr(), t, _ld(x), at, len(out), _stream(device.index))
         if st:
             _check(st)
         return out
