@@ -480,7 +480,7 @@ typedef struct cerar_tensors cerar_tensors_t;    /* opaque, library-owned */
 typedef enum { CERAR_TYPE_F32 = 0, CERAR_TYPE_BF16 = 1 } cerar_type_t;
 
 cerar_status_t cerar_ops_create(cerar_ops_t** out);     /* CERAR_ERR_CUDA without a device */
-void           cerar_ops_destroy(cerar_ops_t* ops);
+void           cerar_ops_destroy(cerar_ops_t* ops);     /* after the sets that were made with it */
 /* Synchronises `stream`; CERAR_ERR_TIMEOUT if a kernel gave up on a bounded wait since the last check. */
 cerar_status_t cerar_ops_status(cerar_ops_t* ops, cerar_stream_t stream);
 uint64_t       cerar_ops_launch_count(const cerar_ops_t* ops);

@@ -192,6 +192,7 @@ class Ops:
         out = C.c_void_p()
         _check(lib.cerar_ops_create(C.byref(out)))
         self._h = out
+        self._index = torch.cuda.current_device()
 
     def destroy(self):
         if self._h:
@@ -203,6 +204,10 @@ class Ops:
             self.destroy()
         except Exception:
             pass
+
+    def _here(self, device):
+        if device.index != self._index:
+            raise ValueError(f"a tensor on {device}, but these operators were made on cuda:{self._index}")
 
     def status(self):
         """Waits for the current stream; raises if a kernel gave up on a bounded wait."""
@@ -217,6 +222,7 @@ class Ops:
         _matrix(x, "x")
         rows, cols = x.shape
         device = x.device
+        self._here(device)
         if len(scalings) == 1 and not cols & 15:                    # two allocations cost the host less than two views of one
             out = [Quantized.empty(rows, cols, scalings[0], device)]
             at = out[0].at
@@ -233,6 +239,9 @@ class Ops:
         da, db = a.desc, b.desc
         m, n = (da.cols if trans_a else da.rows), (db.rows if trans_b else db.cols)
         device = a.device
+        self._here(device)
+        if b.device != device:
+            raise ValueError("the operands are on different devices")
         if out is None:
             if accumulate:
                 raise ValueError("accumulate wants an `out` to add to")
@@ -240,6 +249,7 @@ class Ops:
             ld = n
         else:
             _matrix(out, "out")
+            self._here(out.device)
             if tuple(out.shape) != (m, n):
                 raise ValueError(f"out of shape {(m, n)} wanted, got {tuple(out.shape)}")
             ld = _ld(out)
@@ -320,6 +330,7 @@ class TensorSet:
         n = [t.numel() for t in grads]
         dev = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
         _flat(grads, "grads", device=dev)
+        ops._here(dev)
         self.ops, self.grads = ops, grads
         self.params = None if params is None else _flat(params, "params", n, dev)
         self.masters = None if masters is None else _flat(masters, "masters", n, dev)
@@ -395,8 +406,8 @@ class TensorSet:
         """[norm, clip coefficient, 1 if finite] on the device; the third argument of a step that skips itself otherwise."""
         if out is None:
             out = torch.empty(3, dtype=_F32, device=self._device)
-        elif out.dtype != _F32 or out.numel() != 3 or not out.is_cuda or not out.is_contiguous():
-            raise ValueError("out: three contiguous floats on the device are wanted")
+        elif out.dtype != _F32 or out.numel() != 3 or out.device != self._device or not out.is_contiguous():
+            raise ValueError("out: three contiguous floats on the set's device are wanted")
         st = _norm(self._h, max_norm, out.data_ptr(), _stream(self._device.index))
         if st:
             _check(st)
@@ -407,7 +418,7 @@ class TensorSet:
         parameters without masters), another one for every step."""
         o = self._opt
         o.lr, o.beta1, o.beta2, o.eps, o.step, o.seed = lr, betas[0], betas[1], eps, step, seed
-        if clip is not None and (clip.dtype != _F32 or clip.numel() != 3 or not clip.is_cuda or not clip.is_contiguous()):
+        if clip is not None and (clip.dtype != _F32 or clip.numel() != 3 or clip.device != self._device or not clip.is_contiguous()):
             raise ValueError("clip: the three floats that grad_norm returned are wanted")
         st = _adamw(self._h, self._opt_at, None if clip is None else clip.data_ptr(), _stream(self._device.index))
         if st:

@@ -94,6 +94,13 @@ def test_quantize_special_values(ops, dtype):
         assert np.array_equal(f64(q.codes), qc, equal_nan=True)
 
 
+def test_quantize_of_nothing(ops):
+    import torch
+    for shape in ((0, 5), (5, 0), (0, 0)):
+        for q in [*ops.quantize(torch.empty(*shape, device="cuda"), 0, 1, 2), *ops.quantize(torch.empty(*shape, device="cuda"), 1)]:
+            assert tuple(q.codes.shape) == shape and q.dequantize().shape == shape
+
+
 def test_quantize_writes_nothing_else(ops):
     """Codes between cols and ld, scales beyond the matrix and the bytes behind it keep what they hold."""
     import torch
@@ -687,6 +694,14 @@ def test_refusals(ops):
     refused(1, t.grad_norm, float("nan"))
     with pytest.raises(ValueError):
         t.adamw(lr=0.1, step=1, clip=torch.ones(2, device="cuda"))
+    with pytest.raises(ValueError):
+        t.adamw(lr=0.1, step=1, clip=torch.ones(3))
+    with pytest.raises(ValueError):
+        t.grad_norm(1.0, out=torch.ones(3))
+    with pytest.raises(ValueError):
+        ops.matmul(q0, q0, trans_b=True, out=torch.empty(64, 64))
+    with pytest.raises(ValueError):
+        R.TensorSet(ops, grads=[torch.ones(3)])
     refused(1, R.TensorSet, ops, grads=g, params=p, masters=[torch.randn(10, device="cuda")])   # master of a float32 parameter
     with pytest.raises(ValueError):
         R.TensorSet(ops, grads=g, params=[torch.randn(9, device="cuda")])
