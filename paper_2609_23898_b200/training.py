@@ -218,17 +218,21 @@ class Ops:
 
     def quantize(self, x: torch.Tensor, *scalings: int):
         """8-bit matrices of x, one for each of `scalings` (BY_ROW, BY_COLUMN, BY_BLOCK), from one reading of x."""
-        t = _type(x, "x")
-        _matrix(x, "x")
-        rows, cols = x.shape
+        t = _TYPES.get(x.dtype)
+        shape, strides = x.shape, x.stride()
+        if t is None or len(shape) != 2 or not x.is_cuda or strides[1] != 1 or strides[0] < shape[1]:
+            t = _type(x, "x")                                       # the whole check, where the short one is not enough
+            _matrix(x, "x")
+        rows, cols = shape
         device = x.device
-        self._here(device)
+        if device.index != self._index:
+            self._here(device)
         if len(scalings) == 1 and not cols & 15:                    # two allocations cost the host less than two views of one
             out = [Quantized.empty(rows, cols, scalings[0], device)]
             at = out[0].at
         else:
             out, at = Quantized._several(rows, cols, scalings, device)
-        st = _quantize(self._h, x.data_ptr(), t, _ld(x), at, len(out), _stream(device.index))
+        st = _quantize(self._h, x.data_ptr(), t, strides[0] if rows > 1 else max(strides[0], cols), at, len(out), _stream(device.index))
         if st:
             _check(st)
         return out
