@@ -66,7 +66,7 @@ struct Params {
     int tiles_m, tiles_n, group_m;
     uint32_t tiles;
     int a_mn, b_mn;                                    // 1: the operand's own dimension (m or n) is the contiguous one
-    int accumulate, c_vec;
+    int accumulate, c_vec, c_pair;                     // rows of C start on 16-byte, on 4-byte boundaries
     int stages, split;
     uint32_t a_bytes;                                  // what a load of A brings (a matrix of few rows: those rows only; the others'
                                                        // sums are made of whatever lies there, row by row, and not stored)
@@ -224,6 +224,16 @@ __device__ __forceinline__ void write_slab(const Params& p, uint32_t staging, in
                 uint4 q;
                 asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
                 if (r < nrows) *reinterpret_cast<uint4*>(c + (int64_t)(row0 + r) * p.ldc + col0 + j * PER16) = q;
+            }
+        } else if (sizeof(C) == 2 && p.c_pair) {
+            // rows that start on 4-byte boundaries: two elements at a time
+            const int e = 2 * lane;
+            for (int r = 0; r < nrows; ++r) {
+                uint32_t q;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(q) : "r"(staging + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
+                C* dst = c + (int64_t)(row0 + r) * p.ldc + col0 + e;
+                if (e + 1 < n) *reinterpret_cast<uint32_t*>(dst) = q;
+                else if (e < n) *reinterpret_cast<uint16_t*>(dst) = (uint16_t)q;
             }
         } else {
             for (int r = 0; r < nrows; ++r)
@@ -946,6 +956,7 @@ cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, 
     p.C = a.C; p.ldc = a.ldc; p.accumulate = a.accumulate; p.status = a.status;
     const int64_t size = a.type == CERAR_TYPE_F32 ? 4 : 2;
     p.c_vec = (reinterpret_cast<uintptr_t>(a.C) & 15u) == 0 && (a.ldc * size) % 16 == 0;
+    p.c_pair = (reinterpret_cast<uintptr_t>(a.C) & 3u) == 0 && (a.ldc * size) % 4 == 0;
     CUtensorMap ma, mb;
     const int a_rows = !p.a_mn && p.M < BM ? (p.M + 7) & ~7 : BM;
     p.a_bytes = (uint32_t)a_rows * BK;
