@@ -512,7 +512,8 @@ cerar_status_t cerar_fp8_quantize(cerar_ops_t* ops, const void* x, cerar_type_t 
 /* C (M x N of `type`, ldc elements between rows) = op(A) op(B), or C + op(A) op(B) with accumulate != 0;
  * op is the matrix itself or, with trans_* != 0, its transpose.  The scales run along the summed
  * dimension or in blocks: op(A) = A wants A by row or by block, op(A) = A^T by column or by block;
- * op(B) = B wants B by column or by block, op(B) = B^T by row or by block.  Any finite scales.
+ * op(B) = B wants B by column or by block, op(B) = B^T by row or by block.  Any finite scales whose
+ * products sA sB stay within binary32's range.
  *     C[m,n] (+)= sum_b sA(m,b) sB(b,n) sum_{k in block b} A[m,k] B[k,n]
  * The inner sums run on the tensor cores, the outer one in binary32; one rounding to `type` at the end.
  * Where both matrices say pow2 the tensor cores apply the scales too, which is faster; a scale that is
