@@ -69,7 +69,7 @@ class Quantized:
     scales are read once, here, to see (which waits for the device).  Scales that are changed later have to keep to it:
     what they touch becomes NaN otherwise."""
 
-    __slots__ = ("_codes", "_scales", "scaling", "desc", "at", "_buffer")
+    __slots__ = ("_codes", "_scales", "scaling", "desc", "at", "_buffer", "_parts")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, scaling: int, pow2: bool | None = None):
         if codes.element_size() != 1:
@@ -126,25 +126,26 @@ class Quantized:
         buffer = torch.empty(size, dtype=_E4M3, device=device)
         base, at = buffer.data_ptr(), C.addressof(arr)
         first, out = at, []
-        for d, (codes, scales) in zip(arr, offsets):
-            d.codes, d.scales = base + codes, base + scales
+        for d, scaling, parts in zip(arr, scalings, offsets):
+            d.codes, d.scales = base + parts[0], base + parts[1]
             q = cls.__new__(cls)
             q._codes = q._scales = None
-            q.scaling, q.desc, q.at, q._buffer = d.scaling, d, at, buffer
+            q.scaling, q.desc, q.at, q._buffer, q._parts = scaling, d, at, buffer, parts
             at += _MATRIX_BYTES
             out.append(q)
         return out, first
 
     @classmethod
     def _layout(cls, rows, cols, scalings):
-        """Where codes and scales of these matrices lie in one allocation, and their descriptors but for the addresses."""
+        """Where codes and scales of these matrices lie in one allocation (and their shapes and strides), and their descriptors but
+        for the addresses."""
         n = len(scalings)
         arr, offsets, size = (Fp8Matrix * n)(), [], 0
         for i, scaling in enumerate(scalings):
             ld, nr, nc = cls._sizes(rows, cols, scaling)
             at = size + ((rows * ld + 255) & -256)                   # the scales start there
             arr[i] = Fp8Matrix(0, 0, rows, cols, ld, nc, scaling, True)
-            offsets.append((size, at))
+            offsets.append((size, at, (rows, cols), (ld, 1), (nr, nc), (nc, 1)))
             size = (at + 4 * nr * nc + 255) & -256
         if len(_LAYOUTS) >= 1024:
             _LAYOUTS.clear()
@@ -154,16 +155,15 @@ class Quantized:
     @property
     def codes(self) -> torch.Tensor:
         if self._codes is None:
-            d, b = self.desc, self._buffer
-            self._codes = b.as_strided((d.rows, d.cols), (d.ld, 1), (d.codes or 0) - b.data_ptr())
+            p = self._parts
+            self._codes = self._buffer.as_strided(p[2], p[3], p[0])
         return self._codes
 
     @property
     def scales(self) -> torch.Tensor:
         if self._scales is None:
-            d, b = self.desc, self._buffer
-            _, nr, nc = self._sizes(d.rows, d.cols, d.scaling)
-            self._scales = b.view(_F32).as_strided((nr, nc), (nc, 1), ((d.scales or 0) - b.data_ptr()) >> 2)
+            p = self._parts
+            self._scales = self._buffer.view(_F32).as_strided(p[4], p[5], p[1] >> 2)
         return self._scales
 
     @property
