@@ -285,21 +285,29 @@ def linear_backward(ops: Ops, dy: torch.Tensor, xc: Quantized, w: Quantized, dw:
     return ops.matmul(dr, w, dtype=dy.dtype) if need_dx else None
 
 
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """t (..., columns) as a matrix whose rows the conversion can read: a copy where a row's elements are not contiguous or rows overlap
+    (transposed inputs, gradients that autograd expands from one element)."""
+    t = t.unsqueeze(0) if t.dim() == 1 else t.flatten(0, -2)
+    rows, cols = t.shape
+    if t.stride(1) != 1 and cols > 1 or t.stride(0) < cols and rows > 1:
+        t = t.contiguous()
+    return t
+
+
 class Linear8(torch.autograd.Function):
-    """linear and linear_backward for torch.autograd: y = Linear8.apply(x, w, ops, dw).  w: quantized weights (no gradient of
-    their own: it is added to `dw`, which may be None)."""
+    """linear and linear_backward for torch.autograd: y = Linear8.apply(x, w, ops, dw), x (..., inputs) with any strides.  w: quantized
+    weights (no gradient of their own: it is added to `dw`, which may be None)."""
 
     @staticmethod
     def forward(ctx, x, w, ops, dw):
-        x2 = x.reshape(-1, x.shape[-1])
-        y, xc = linear(ops, x2, w)
+        y, xc = linear(ops, _rows(x), w)
         ctx.ops, ctx.w, ctx.dw, ctx.xc = ops, w, dw, xc
         return y.view(*x.shape[:-1], y.shape[-1])
 
     @staticmethod
     def backward(ctx, dy):
-        d2 = dy.reshape(-1, dy.shape[-1])
-        dx = linear_backward(ctx.ops, d2, ctx.xc, ctx.w, ctx.dw, need_dx=ctx.needs_input_grad[0])
+        dx = linear_backward(ctx.ops, _rows(dy), ctx.xc, ctx.w, ctx.dw, need_dx=ctx.needs_input_grad[0])
         return None if dx is None else dx.view(*dy.shape[:-1], dx.shape[-1]), None, None, None
 
 

@@ -1,0 +1,80 @@
+"""training.Linear8 inside an autograd graph, on the GPU.
+
+Where numbers are compared, inputs are small integers, which the 8-bit format holds exactly with any of its scales, and all sums stay
+below 2^24: y, dx and dw are then equal to the layer's formulas y = x w^T, dx = dy w, dw = dy^T x in 64 bits, with no tolerance.
+"""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    import torch
+    from paper_2609_23898_b200 import training
+    assert torch.cuda.is_available()
+    o = training.Ops()
+    yield o
+    o.status()
+
+
+def whole(rng, *shape):
+    import torch
+    return torch.from_numpy(rng.integers(-8, 9, shape).astype(np.float32)).cuda()
+
+
+def layer(ops, rng, n, k):
+    from paper_2609_23898_b200 import training as R
+    import torch
+    w = whole(rng, n, k)
+    return w, ops.quantize(w, R.BY_BLOCK)[0], torch.zeros(n, k, device="cuda")
+
+
+# ---------------------------------------------------------------------------------------------------- strides
+
+def strided(t, how):
+    """The same values with other strides: rows not contiguous, a slice of a wider tensor, an element repeated."""
+    import torch
+    if how == "transposed":
+        return t.t().contiguous().t()
+    if how == "every second":
+        return torch.stack((t, t + 1), -1).flatten(-2)[:, ::2]
+    if how == "permuted":
+        return t.view(10, -1, t.size(1)).transpose(0, 1).contiguous().transpose(0, 1)
+    return t[:1, :1].expand_as(t) if how == "expanded" else t[:1].expand_as(t)
+
+
+@pytest.mark.parametrize("how", ["transposed", "every second", "permuted", "expanded", "one row"])
+def test_inputs_and_gradients_of_any_strides(ops, how):
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(4)
+    n, k = 70, 48
+    w, wq, dw = layer(ops, rng, n, k)
+    x = strided(whole(rng, 60, k), how).requires_grad_()
+    dy = strided(whole(rng, 60, n), how)
+    y = R.Linear8.apply(x, wq, ops, dw)
+    assert y.shape == (*x.shape[:-1], n)
+    assert torch.equal(y.detach().double(), x.detach().double() @ w.double().t())
+    y.backward(dy)
+    x2, d2 = x.detach().double().reshape(-1, k), dy.double().reshape(-1, n)
+    assert torch.equal(x.grad.double().reshape(-1, k), d2 @ w.double()) and torch.equal(dw.double(), d2.t() @ x2)
+
+
+def test_losses_whose_gradient_is_expanded_or_transposed(ops):
+    """y.sum() hands back one element with strides 0, a loss on y.t() a transposed gradient."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(5)
+    w, wq, dw = layer(ops, rng, 70, 48)
+    x = whole(rng, 60, 48).requires_grad_()
+    R.Linear8.apply(x, wq, ops, dw).sum().backward()
+    ones = torch.ones(60, 70, device="cuda", dtype=torch.float64)
+    assert torch.equal(x.grad.double(), ones @ w.double()) and torch.equal(dw.double(), ones.t() @ x.detach().double())
+    dw.zero_()
+    x.grad = None
+    v = whole(rng, 60)
+    (R.Linear8.apply(x, wq, ops, dw).t().contiguous() @ v).sum().backward()
+    dy = v.double()[:, None].expand(60, 70)
+    assert torch.equal(x.grad.double(), dy @ w.double()) and torch.equal(dw.double(), dy.t() @ x.detach().double())
