@@ -48,9 +48,11 @@ def _type(t: torch.Tensor, what: str) -> int:
 
 
 def _matrix(t: torch.Tensor, what: str) -> torch.Tensor:
-    """A two-dimensional device tensor whose rows are contiguous."""
+    """A two-dimensional device tensor whose rows are contiguous (an empty one may have any strides: there is nothing at them)."""
     if t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{what}: a two-dimensional CUDA tensor is wanted")
+    if not t.numel():
+        return t
     if t.stride(1) != 1 and t.size(1) > 1 or t.stride(0) < t.size(1) and t.size(0) > 1:
         raise ValueError(f"{what}: elements of a row must be contiguous and rows must not overlap")
     return t

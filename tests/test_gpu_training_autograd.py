@@ -78,3 +78,18 @@ def test_losses_whose_gradient_is_expanded_or_transposed(ops):
     (R.Linear8.apply(x, wq, ops, dw).t().contiguous() @ v).sum().backward()
     dy = v.double()[:, None].expand(60, 70)
     assert torch.equal(x.grad.double(), dy @ w.double()) and torch.equal(dw.double(), dy.t() @ x.detach().double())
+
+
+@pytest.mark.parametrize("shape,strides", [((0, 200), (0, 0)), ((0, 200), (1, 2)), ((200, 0), (0, 1)), ((200, 0), (0, 0))])
+def test_nothing_may_have_any_strides(ops, shape, strides):
+    import torch
+    from paper_2609_23898_b200 import training as R
+    x = torch.empty(8, device="cuda").as_strided(shape, strides)
+    for q in [*ops.quantize(x, 0, 1, 2), *ops.quantize(x, 0)]:
+        assert tuple(q.shape) == shape and q.dequantize().shape == shape
+    w, = ops.quantize(torch.ones(70, shape[1], device="cuda"), R.BY_BLOCK)
+    assert torch.equal(R.Linear8.apply(x, w, ops, None), torch.zeros(shape[0], 70, device="cuda"))
+    out = torch.empty(8, device="cuda").as_strided((0, 70), strides)
+    a, = ops.quantize(torch.empty(0, 200, device="cuda"), R.BY_ROW)
+    b, = ops.quantize(torch.ones(70, 200, device="cuda"), R.BY_ROW)
+    assert ops.matmul(a, b, trans_b=True, out=out) is out
