@@ -299,10 +299,21 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
 
 class Linear8(torch.autograd.Function):
     """linear and linear_backward for torch.autograd: y = Linear8.apply(x, w, ops, dw), x (..., inputs) with any strides.  w: quantized
-    weights (no gradient of their own: it is added to `dw`, which may be None)."""
+    weights (no gradient of their own: it is added to `dw`, which may be None).  y has a gradient wherever x or dw wants one, so `dw` is
+    served too where x is data or comes from frozen layers."""
+
+    @classmethod
+    def apply(cls, x, w, ops, dw):
+        # Neither w nor dw is a tensor that autograd follows.  Where x is not one either, an empty one takes that place: without it y
+        # would have no gradient and backward would not be called.  It lies on x's device, so that the stream dw is written on
+        # is among those that the end of the backward pass waits for.
+        anchor = None
+        if dw is not None and not x.requires_grad and torch.is_grad_enabled():
+            anchor = torch.empty(0, device=x.device, requires_grad=True)
+        return super().apply(x, w, ops, dw, anchor)
 
     @staticmethod
-    def forward(ctx, x, w, ops, dw):
+    def forward(ctx, x, w, ops, dw, anchor):
         y, xc = linear(ops, _rows(x), w)
         ctx.ops, ctx.w, ctx.dw, ctx.xc = ops, w, dw, xc
         return y.view(*x.shape[:-1], y.shape[-1])
@@ -310,7 +321,7 @@ class Linear8(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         dx = linear_backward(ctx.ops, _rows(dy), ctx.xc, ctx.w, ctx.dw, need_dx=ctx.needs_input_grad[0])
-        return None if dx is None else dx.view(*dy.shape[:-1], dx.shape[-1]), None, None, None
+        return None if dx is None else dx.view(*dy.shape[:-1], dx.shape[-1]), None, None, None, None
 
 
 # ------------------------------------------------------------------------------------------------ norm and optimizer

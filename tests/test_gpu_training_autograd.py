@@ -93,3 +93,81 @@ def test_nothing_may_have_any_strides(ops, shape, strides):
     a, = ops.quantize(torch.empty(0, 200, device="cuda"), R.BY_ROW)
     b, = ops.quantize(torch.ones(70, 200, device="cuda"), R.BY_ROW)
     assert ops.matmul(a, b, trans_b=True, out=out) is out
+
+
+# ---------------------------------------------------------------------------------------------------- inputs without a gradient
+
+@pytest.mark.parametrize("shape", [(150, 200), (10, 15, 200), (200,), (1, 200), (0, 200)])
+def test_weight_gradient_of_a_first_layer(ops, shape):
+    """x is data: nothing but what lies above the layer has a gradient of its own, and dw is dy^T x all the same."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(len(shape))
+    n, k = 70, 200
+    x, (w, wq, dw) = whole(rng, *shape), layer(ops, rng, n, k)
+    gain = torch.ones(n, device="cuda", requires_grad=True)
+    y = R.Linear8.apply(x, wq, ops, dw)
+    dy = whole(rng, *y.shape)
+    (y * gain * dy).sum().backward()
+    want = dy.double().reshape(-1, n).t() @ x.double().reshape(-1, k)
+    assert torch.equal(dw.double(), want)
+    assert x.grad is None and torch.equal(gain.grad.double(), (dy.double() * (x.double() @ w.double().t())).reshape(-1, n).sum(0))
+
+
+def test_two_layers_the_first_on_data(ops):
+    """Frozen layers below, a ReLU between: both weight gradients are those of the formula."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(2)
+    x = torch.from_numpy(rng.integers(-2, 3, (130, 40)).astype(np.float32)).cuda()
+    (w1, q1, d1), (w2, q2, d2) = layer(ops, rng, 24, 40), layer(ops, rng, 50, 24)
+    with torch.no_grad():
+        x = x * 1.0                                                        # what a frozen layer hands on
+    h = R.Linear8.apply(x, q1, ops, d1)
+    a = torch.where(h > 0, 4.0, -1.0) + 0 * h                              # values the format holds; its gradient with respect to h is 0
+    y = R.Linear8.apply(a + h.clamp(-8, 8), q2, ops, d2)
+    dy = torch.from_numpy(rng.integers(-1, 2, tuple(y.shape)).astype(np.float32)).cuda()
+    y.backward(dy)
+    hin = (a + h.clamp(-8, 8)).detach().double()
+    assert torch.equal(d2.double(), dy.double().t() @ hin)
+    dh = (dy.double() @ w2.double()) * ((h >= -8) & (h <= 8))
+    # dh is quantized by column for dw1: within 2^-4 of each element or of 2^-17 of its column's largest
+    err = (dh.abs() / 16 + dh.abs().amax(0) * 2.0 ** -17).t() @ x.double().abs()
+    assert bool(((d1.double() - dh.t() @ x.double()).abs() <= err * 1.01).all()) and bool(d1.any())
+
+
+def test_frozen_weights_and_frozen_input(ops):
+    """Without dw only x has a gradient; with neither, or without gradients enabled, the result has none."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(3)
+    x, (w, wq, dw) = whole(rng, 60, 48), layer(ops, rng, 33, 48)
+    assert not R.Linear8.apply(x, wq, ops, None).requires_grad
+    with torch.no_grad():
+        assert not R.Linear8.apply(x, wq, ops, dw).requires_grad
+    with torch.inference_mode():
+        assert torch.equal(R.Linear8.apply(x, wq, ops, dw).double(), x.double() @ w.double().t())
+    x.requires_grad_()
+    y = R.Linear8.apply(x, wq, ops, None)
+    dy = whole(rng, 60, 33)
+    y.backward(dy)
+    assert torch.equal(x.grad.double(), dy.double() @ w.double()) and not bool(dw.any())
+
+
+def test_forward_on_a_side_stream(ops):
+    """dw, written on the stream of the forward pass, may be read on the caller's stream as soon as backward returns."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(10)
+    w, wq, dw = layer(ops, rng, 512, 1024)
+    x, dy = whole(rng, 2048, 1024), whole(rng, 2048, 512)
+    want = dy.double().t() @ x.double()
+    side = torch.cuda.Stream()
+    for _ in range(5):
+        dw.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            y = R.Linear8.apply(x, wq, ops, dw)
+        torch.cuda.current_stream().wait_stream(side)
+        y.backward(dy)
+        assert torch.equal(dw.double(), want)
