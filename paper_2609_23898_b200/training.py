@@ -17,6 +17,7 @@ from __future__ import annotations
 import ctypes as C
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import cerar
 from .cerar import CerarError, Fp8Matrix, lib
@@ -96,6 +97,17 @@ class Quantized:
         self._codes, self._scales, self.scaling, self._buffer = codes, scales, scaling, None
         self.desc = Fp8Matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, lds, scaling, pow2)
         self.at = C.addressof(self.desc)
+
+    @classmethod
+    def _of(cls, codes, scales, scaling, pow2):
+        """Of tensors that were saved for a backward pass, with `codes` copied where they came back in another layout (from the host)."""
+        rows, cols = codes.shape
+        if rows > 1 and (codes.stride(0) & 15 or codes.stride(1) != 1) or codes.data_ptr() & 15:
+            wide = torch.empty(rows, (cols + 15) & -16, dtype=codes.dtype, device=codes.device)
+            codes = wide[:, :cols].copy_(codes)
+        q = cls.__new__(cls)
+        q._set(codes, scales, scaling, rows, cols, codes.stride(0) if rows > 1 else (cols + 15) & -16, _ld(scales), pow2)
+        return q
 
     @staticmethod
     def _sizes(rows, cols, scaling):
@@ -300,7 +312,8 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
 class Linear8(torch.autograd.Function):
     """linear and linear_backward for torch.autograd: y = Linear8.apply(x, w, ops, dw), x (..., inputs) with any strides.  w: quantized
     weights (no gradient of their own: it is added to `dw`, which may be None).  y has a gradient wherever x or dw wants one, so `dw` is
-    served too where x is data or comes from frozen layers."""
+    served too where x is data or comes from frozen layers.  Every pass backward through the layer adds to dw, torch.autograd.grad's
+    too; second derivatives are refused."""
 
     @classmethod
     def apply(cls, x, w, ops, dw):
@@ -315,12 +328,28 @@ class Linear8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, ops, dw, anchor):
         y, xc = linear(ops, _rows(x), w)
-        ctx.ops, ctx.w, ctx.dw, ctx.xc = ops, w, dw, xc
+        # Saved as autograd saves tensors: freed by the backward pass, within reach of saved-tensor hooks, and refused if changed in between.
+        # (Weights made in inference mode cannot be saved; they are held as they are.)
+        ctx.ops, ctx.dw, ctx.kinds, ctx.w = ops, dw, (xc.scaling, xc.desc.pow2, w.scaling, w.desc.pow2), None
+        keep = [None] * 4
+        if dw is not None:
+            keep[:2] = xc.codes, xc.scales
+        if ctx.needs_input_grad[0]:
+            if w.codes.is_inference() or w.scales.is_inference():
+                ctx.w = w
+            else:
+                keep[2:] = w.codes, w.scales
+        ctx.save_for_backward(*keep)
         return y.view(*x.shape[:-1], y.shape[-1])
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
-        dx = linear_backward(ctx.ops, _rows(dy), ctx.xc, ctx.w, ctx.dw, need_dx=ctx.needs_input_grad[0])
+        xs, xp, ws, wp = ctx.kinds
+        x_codes, x_scales, w_codes, w_scales = ctx.saved_tensors
+        xc = None if x_codes is None else Quantized._of(x_codes, x_scales, xs, xp)
+        w = ctx.w if w_codes is None else Quantized._of(w_codes, w_scales, ws, wp)
+        dx = linear_backward(ctx.ops, _rows(dy), xc, w, ctx.dw, need_dx=ctx.needs_input_grad[0])
         return None if dx is None else dx.view(*dy.shape[:-1], dx.shape[-1]), None, None, None, None
 
 

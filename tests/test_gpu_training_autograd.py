@@ -171,3 +171,80 @@ def test_forward_on_a_side_stream(ops):
         torch.cuda.current_stream().wait_stream(side)
         y.backward(dy)
         assert torch.equal(dw.double(), want)
+
+
+# ---------------------------------------------------------------------------------------------------- the graph
+
+def test_second_derivatives_are_refused(ops):
+    """backward has no graph of its own: differentiating through it raises instead of leaving a part out."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(6)
+    w, wq, dw = layer(ops, rng, 70, 48)
+    x = whole(rng, 60, 48).requires_grad_()
+    y = R.Linear8.apply(x, wq, ops, dw)
+    g, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (g.square().sum() + x.square().sum()).backward()
+
+
+def test_what_is_kept_is_released_and_used_once(ops):
+    """After a backward pass the kept activations are freed though y lives on, and a second pass is refused unless the graph was
+    retained; retained, it adds to dw again."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(7)
+    w, wq, dw = layer(ops, rng, 16, 2048)
+    x = whole(rng, 4096, 2048)
+    dy = whole(rng, 4096, 16)
+    y = R.Linear8.apply(x, wq, ops, dw)
+    held = torch.cuda.memory_allocated()
+    y.backward(dy)
+    assert held - torch.cuda.memory_allocated() >= 4096 * 2048            # the 8-bit copy
+    once = dw.clone()
+    with pytest.raises(RuntimeError):
+        y.backward(dy)
+    assert torch.equal(dw, once)
+    y = R.Linear8.apply(x, wq, ops, dw.zero_())
+    y.backward(dy, retain_graph=True)
+    y.backward(dy)
+    assert torch.equal(dw, 2 * once)
+
+
+@pytest.mark.parametrize("k", [64, 200])
+def test_saved_tensor_hooks_reach_what_is_kept(ops, k):
+    """Activations on the host between the passes (rows of 200 bytes come back packed: not a multiple of 16 apart)."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(8)
+    w, wq, dw = layer(ops, rng, 70, k)
+    x = whole(rng, 60, k).requires_grad_()
+    dy = whole(rng, 60, 70)
+    with torch.autograd.graph.save_on_cpu():
+        y = R.Linear8.apply(x, wq, ops, dw)
+    y.backward(dy)
+    assert torch.equal(x.grad.double(), dy.double() @ w.double()) and torch.equal(dw.double(), dy.double().t() @ x.detach().double())
+
+
+def test_weights_changed_between_the_passes_are_noticed(ops):
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(9)
+    w, wq, dw = layer(ops, rng, 70, 48)
+    x = whole(rng, 60, 48).requires_grad_()
+    y = R.Linear8.apply(x, wq, ops, dw)
+    wq.scales.mul_(2)
+    with pytest.raises(RuntimeError):
+        y.backward(torch.ones_like(y))
+
+
+def test_weights_made_in_inference_mode(ops):
+    import torch
+    from paper_2609_23898_b200 import training as R
+    rng = np.random.default_rng(11)
+    with torch.inference_mode():
+        w, wq, _ = layer(ops, rng, 70, 48)
+    x, dy, dw = whole(rng, 60, 48).requires_grad_(), whole(rng, 60, 70), torch.zeros(70, 48, device="cuda")
+    y = R.Linear8.apply(x, wq, ops, dw)
+    y.backward(dy)
+    assert torch.equal(x.grad.double(), dy.double() @ w.double()) and torch.equal(dw.double(), dy.double().t() @ x.detach().double())
