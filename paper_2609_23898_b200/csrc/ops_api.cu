@@ -75,6 +75,10 @@ cerar_status_t check_matrix(const cerar_fp8_matrix_t* m) {
     return CERAR_OK;
 }
 
+// What was copied or set on the legacy stream is on the device when this returns.  cudaMemcpy from pageable memory and cudaMemset may
+// return earlier, and the caller's streams need not wait for that one (torch's do not).
+cudaError_t set_up_done() { return cudaStreamSynchronize(cudaStreamLegacy); }
+
 }  // namespace
 
 extern "C" {
@@ -92,8 +96,9 @@ cerar_status_t cerar_ops_create(cerar_ops_t** out) {
     if (!o) return fail(CERAR_ERR_NOMEM, "out of host memory");
     if ((e = cudaGetDevice(&o->device)) == cudaSuccess &&
         (e = cudaDeviceGetAttribute(&o->num_sms, cudaDevAttrMultiProcessorCount, o->device)) == cudaSuccess &&
-        (e = cudaMalloc(&o->d_status, sizeof(int))) == cudaSuccess)
-        e = cudaMemset(o->d_status, 0, sizeof(int));
+        (e = cudaMalloc(&o->d_status, sizeof(int))) == cudaSuccess &&
+        (e = cudaMemset(o->d_status, 0, sizeof(int))) == cudaSuccess)
+        e = set_up_done();
     if (e != cudaSuccess) {
         const cerar_status_t st = cuda_fail(e, "ops set-up");
         cerar_ops_destroy(o);
@@ -247,8 +252,9 @@ cerar_status_t cerar_tensors_create(cerar_ops_t* o, int64_t count, const cerar_t
             (e = cudaMalloc(&set->d_partial, sizeof(double) * set->norm_blocks)) == cudaSuccess &&
             (e = cudaMalloc(&set->d_ticket, sizeof(unsigned))) == cudaSuccess &&
             (e = cudaMemset(set->d_ticket, 0, sizeof(unsigned))) == cudaSuccess &&
-            (e = cudaMemcpy(set->d_tensors, recs.data(), sizeof(cerar::TensorRec) * recs.size(), cudaMemcpyHostToDevice)) == cudaSuccess)
-            e = cudaMemcpy(set->d_chunks, chunks.data(), sizeof(cerar::ChunkRef) * chunks.size(), cudaMemcpyHostToDevice);
+            (e = cudaMemcpy(set->d_tensors, recs.data(), sizeof(cerar::TensorRec) * recs.size(), cudaMemcpyHostToDevice)) == cudaSuccess &&
+            (e = cudaMemcpy(set->d_chunks, chunks.data(), sizeof(cerar::ChunkRef) * chunks.size(), cudaMemcpyHostToDevice)) == cudaSuccess)
+            e = set_up_done();
     } catch (const std::bad_alloc&) {
         cerar_tensors_destroy(set);
         return fail(CERAR_ERR_NOMEM, "out of host memory");
