@@ -42,6 +42,7 @@ cerar_status_t fail(cerar_status_t s, const char* msg) {
     return s;
 }
 cerar_status_t cuda_fail(cudaError_t e, const char* what) {
+    cudaGetLastError();      // reported here: left where it is, the next check of somebody else's launch would find it
     try {
         cerar_internal_set_error((std::string(what) + ": " + cudaGetErrorString(e)).c_str());
     } catch (...) {
@@ -51,7 +52,9 @@ cerar_status_t cuda_fail(cudaError_t e, const char* what) {
 cerar_status_t check_ops(const cerar_ops* o) {
     if (!o) return fail(CERAR_ERR_INVALID_ARG, "ops handle is NULL");
     int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev != o->device)
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_fail(e, "current device");
+    if (dev != o->device)
         return fail(CERAR_ERR_CUDA, "the device the ops handle was created on must be current");
     return CERAR_OK;
 }

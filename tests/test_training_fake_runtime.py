@@ -83,3 +83,30 @@ def test_a_set_that_fails_is_no_set(fake, ops, call, status):
     st, s = make_set(fake, ops)
     assert st == status and not s.value and b"made to fail" in fake.fake_error()
     fake.fake_reset(b"")
+
+
+# The runtime keeps the last error until it is asked for, and torch asks after each of its own launches: an error that a call here
+# has reported must not be found there as well.
+
+@pytest.mark.parametrize("call", ["malloc", "memset", "memcpy"])
+def test_a_set_that_fails_leaves_no_error_behind(fake, ops, call):
+    fake.fake_reset(call.encode())
+    assert make_set(fake, ops)[0] != 0
+    assert fake.fake_last() == 0
+    fake.fake_reset(b"")
+
+
+def test_calls_that_fail_leave_no_error_behind(fake, ops):
+    st, s = make_set(fake, ops)
+    q = cerar.Fp8Matrix(4096, 4096, 16, 16, 16, 16, 0, 1)
+    fake.fake_reset(b"launch")
+    assert fake.cerar_grad_norm(s, 1.0, 4096, None) == 6 and fake.fake_last() == 0
+    assert fake.cerar_fp8_quantize(ops, 4096, 0, 16, C.addressof(q), 1, None) == 6 and fake.fake_last() == 0
+    assert fake.cerar_fp8_matmul(ops, C.addressof(q), 0, C.addressof(q), 1, 4096, 0, 16, 0, None) == 6 and fake.fake_last() == 0
+    fake.fake_reset(b"memcpy async")
+    assert fake.cerar_ops_status(ops, None) != 0 and fake.fake_last() == 0
+    h = C.c_void_p()
+    fake.fake_reset(b"malloc")
+    assert fake.cerar_ops_create(C.byref(h)) == 7 and not h.value and fake.fake_last() == 0
+    fake.fake_reset(b"")
+    fake.cerar_tensors_destroy(s)
