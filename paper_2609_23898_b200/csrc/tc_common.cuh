@@ -7,6 +7,7 @@
 
 #include "kernels.cuh"
 #include "ptx.cuh"
+#include "tensor_map.hpp"
 
 namespace cerar {
 namespace tc {
@@ -169,24 +170,6 @@ __device__ __forceinline__ void split_coefficients(const ContractArgs& a, int w,
 }
 
 // ---- host side: tensor maps over [N workers][rows][p positions] fp32 arrays
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-inline EncodeTiledFn get_encode_fn() {
-    static EncodeTiledFn fn = nullptr;
-    static bool tried = false;
-    if (!tried) {
-        tried = true;
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiledFn>(p);
-    }
-    return fn;
-}
-
 // box = box_cols positions x box_rows rows of one worker; positions beyond p and rows
 // beyond `rows` read as zero and are not written
 inline bool make_map(CUtensorMap* m, const float* base, int64_t p, int rows, int N, int64_t rstride, int64_t wstride,
