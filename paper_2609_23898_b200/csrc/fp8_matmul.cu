@@ -869,8 +869,8 @@ fp8_matmul_pow2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_c
 bool make_map_8bit(CUtensorMap* m, const cerar_fp8_matrix_t& x, int box_rows) {
     const cuuint64_t dim[2] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows}, stride[1] = {(cuuint64_t)x.ld};
     const cuuint32_t box[2] = {(cuuint32_t)BK, (cuuint32_t)box_rows}, step[2] = {1, 1};
-    return get_encode_fn()(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, x.codes, dim, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, x.codes, dim, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
 // rows_are_k: the summed dimension runs down the rows of the stored matrix

@@ -22,5 +22,16 @@ inline EncodeTiledFn get_encode_fn() {
     return fn;
 }
 
+// One map.  The encoder wants a current context, which a host thread does not have before its first call of the runtime that needs
+// one; only there, it is tried again with the thread's device made current.
+template <typename... Args>
+inline bool encode_tiled(Args... args) {
+    const EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    if (fn(args...) == CUDA_SUCCESS) return true;
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && fn(args...) == CUDA_SUCCESS;
+}
+
 }  // namespace tc
 }  // namespace cerar

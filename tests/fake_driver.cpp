@@ -42,5 +42,16 @@ int found_by(int n) {
     for (auto& x : t) x.join();
     return found;
 }
+// a map by a thread whose first call this is
+int first_map_of_a_thread() {
+    bool ok = false;
+    std::thread([&] {
+        CUtensorMap m;
+        ok = cerar::tc::encode_tiled(&m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2u, (void*)nullptr, (const cuuint64_t*)nullptr, (const cuuint64_t*)nullptr,
+                                     (const cuuint32_t*)nullptr, (const cuuint32_t*)nullptr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                     CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    }).join();
+    return ok;
+}
 int lookups() { return g_lookups; }
 }

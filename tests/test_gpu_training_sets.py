@@ -42,3 +42,67 @@ def test_a_set_used_at_once_on_a_side_stream(ops):
             o.status()
             n64 = 2 * np.sqrt(flat.numel())
             assert abs(out[0].item() - n64) <= 12 * U * n64
+
+
+FIRST_PRODUCTS = """
+import ctypes as C, threading, torch
+from paper_2609_23898_b200 import cerar, training as R
+torch.cuda.init()
+n = 16
+jobs = []
+for i in range(n):
+    o = R.Ops()
+    q, = o.quantize(torch.ones(16, 128, device="cuda"), R.BY_ROW)
+    jobs.append((o, q, torch.zeros(16, 16, device="cuda"), torch.cuda.Stream()))
+torch.cuda.synchronize()
+start, status = threading.Barrier(n), [None] * n
+def work(i):
+    o, q, out, s = jobs[i]
+    start.wait()
+    status[i] = cerar.lib.cerar_fp8_matmul(o._h, q.at, 0, q.at, 1, out.data_ptr(), 0, 16, 0, s.cuda_stream)
+threads = [threading.Thread(target=work, args=(i,)) for i in range(n)]
+[t.start() for t in threads]
+[t.join() for t in threads]
+torch.cuda.synchronize()
+assert status == [0] * n, status
+assert all(bool((j[2] == 128).all()) for j in jobs)
+"""
+
+
+FIRST_AGGREGATION = """
+import threading, torch
+from paper_2609_23898_b200 import cerar
+N, c, d = 4, 32, 32 * 4096
+plan = cerar.Plan.create(N, c, cerar.EPSILON, 1e-2)
+plan.set_kernel_mode(3)
+g = torch.randn(N, d, device="cuda")
+out, want, ws = torch.empty_like(g), torch.empty_like(g), torch.empty(plan.workspace_bytes(d) // 4, device="cuda")
+s = torch.cuda.current_stream().cuda_stream
+errors = []
+def work():
+    try:
+        plan.allreduce_sim(g, d, out, d, ws, d, 1.0 / N, s)
+    except Exception as e:
+        errors.append(e)
+t = threading.Thread(target=work)
+t.start()
+t.join()
+assert not errors, errors
+plan.allreduce_sim(g, d, want, d, ws, d, 1.0 / N, s)
+torch.cuda.synchronize()
+plan.device_status(s)
+assert torch.equal(out, want)
+"""
+
+
+def test_first_products_of_several_threads():
+    """Each thread with a handle of its own, as the header allows: the first call of a process sets up what all of them share."""
+    for _ in range(3):
+        r = subprocess.run([sys.executable, "-c", FIRST_PRODUCTS], cwd=ROOT, capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, r.stdout + r.stderr
+
+
+def test_first_aggregation_of_a_thread():
+    """The tensor-core contraction from a host thread that has not touched the device before."""
+    r = subprocess.run([sys.executable, "-c", FIRST_AGGREGATION], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
