@@ -81,6 +81,8 @@ cerar_status_t upload(cerar_plan* P) {
     if ((e = cudaMemcpy(P->d_R, hR.data(), hR.size() * sizeof(float), cudaMemcpyHostToDevice)) != cudaSuccess)
         return cuda_fail(e, "upload R");
     if ((e = cudaMemset(P->d_status, 0, sizeof(int))) != cudaSuccess) return cuda_fail(e, "memset status");
+    // both kinds of copy may return before the device has the data, and the caller's streams need not wait for the legacy one
+    if ((e = cudaStreamSynchronize(cudaStreamLegacy)) != cudaSuccess) return cuda_fail(e, "set-up");
     if ((e = cudaStreamCreateWithFlags(&P->s_h2d, cudaStreamNonBlocking)) != cudaSuccess) return cuda_fail(e, "stream");
     if ((e = cudaStreamCreateWithFlags(&P->s_d2h, cudaStreamNonBlocking)) != cudaSuccess) return cuda_fail(e, "stream");
     if ((e = cudaEventCreateWithFlags(&P->ev_start, cudaEventDisableTiming)) != cudaSuccess) return cuda_fail(e, "event");

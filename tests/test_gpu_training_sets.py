@@ -106,3 +106,22 @@ def test_first_aggregation_of_a_thread():
     """The tensor-core contraction from a host thread that has not touched the device before."""
     r = subprocess.run([sys.executable, "-c", FIRST_AGGREGATION], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stdout + r.stderr
+
+
+def test_a_plan_used_at_once_on_a_side_stream():
+    """The aggregation's own tables, as those of a set above."""
+    import torch
+    from paper_2609_23898_b200 import cerar
+    N, c, d = 4, 8, 8 * 4096
+    g = torch.randn(N, d, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    outs = []
+    with torch.cuda.stream(side):
+        for _ in range(5):
+            plan = cerar.Plan.create(N, c, cerar.EPSILON, 1e-2)
+            out, ws = torch.empty_like(g), torch.empty(plan.workspace_bytes(d) // 4, device="cuda")
+            plan.allreduce_sim(g, d, out, d, ws, d, 1.0 / N, side.cuda_stream)
+            plan.device_status(side.cuda_stream)
+            outs.append(out)
+    assert all(torch.equal(o, outs[0]) for o in outs)
