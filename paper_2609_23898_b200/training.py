@@ -15,6 +15,7 @@ stand in include/cerar.h.
 from __future__ import annotations
 
 import ctypes as C
+import weakref
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -207,9 +208,13 @@ class Ops:
         _check(lib.cerar_ops_create(C.byref(out)))
         self._h = out
         self._index = torch.cuda.current_device()
+        self._sets = weakref.WeakSet()
 
     def destroy(self):
+        """Also destroys the sets that were made with it: they hold its address."""
         if self._h:
+            for s in list(self._sets):
+                s.destroy()
             lib.cerar_ops_destroy(self._h)
             self._h = None
 
@@ -433,6 +438,7 @@ class TensorSet:
         out = C.c_void_p()
         _check(lib.cerar_tensors_create(ops._h, len(n), desc, self.state_bits, C.byref(out)))
         self._h = out
+        ops._sets.add(self)
         self._device = dev
         self._opt = cerar.AdamwOptions()
         self._opt_at = C.addressof(self._opt)

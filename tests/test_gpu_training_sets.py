@@ -125,3 +125,15 @@ def test_a_plan_used_at_once_on_a_side_stream():
             plan.device_status(side.cuda_stream)
             outs.append(out)
     assert all(torch.equal(o, outs[0]) for o in outs)
+
+
+def test_an_ops_that_goes_before_its_sets():
+    import torch
+    from paper_2609_23898_b200 import cerar, training as R
+    o = R.Ops()
+    s = R.TensorSet(o, grads=[torch.ones(10, device="cuda")], params=[torch.ones(10, device="cuda")])
+    o.destroy()
+    for call in (lambda: s.grad_norm(1.0), lambda: s.adamw(lr=0.1, step=1), lambda: s.set_grads([torch.zeros(10, device="cuda")]), o.status):
+        with pytest.raises(cerar.CerarError) as e:
+            call()
+        assert e.value.status == 1

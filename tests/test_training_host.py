@@ -71,3 +71,46 @@ def test_matrices_that_are_refused_before_any_call():
     assert R.Quantized._sizes(130, 300, R.BY_ROW) == (304, 3, 130)
     assert R.Quantized._sizes(130, 300, R.BY_COLUMN) == (304, 2, 300)
     assert R.Quantized._sizes(130, 300, R.BY_BLOCK) == (304, 2, 3)
+
+
+def test_an_ops_destroys_its_sets_first(monkeypatch):
+    """A set keeps the address of the handle it was made with: calls on it after Ops.destroy() would read freed memory."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+
+    class Lib:
+        def __init__(self):
+            self.alive, self.log = {}, []
+
+        def make(self, what, out):
+            C.cast(out, C.POINTER(C.c_void_p))[0] = len(self.log) + 16
+            self.log.append(what)
+            return 0
+
+        def cerar_ops_create(self, out):
+            return self.make("ops", out)
+
+        def cerar_tensors_create(self, ops, count, desc, bits, out):
+            return self.make("set", out)
+
+        def cerar_ops_destroy(self, h):
+            self.log.append("ops gone")
+
+        def cerar_tensors_destroy(self, h):
+            self.log.append("set gone")
+
+    lib = Lib()
+    monkeypatch.setattr(R, "lib", lib)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    ops = R.Ops()
+    a, b = R.TensorSet(ops, grads=[]), R.TensorSet(ops, grads=[])
+    b.destroy()
+    ops.destroy()
+    assert lib.log == ["ops", "set", "set", "set gone", "set gone", "ops gone"] and not a._h
+    ops.destroy()
+    del a, b
+    assert lib.log[-1] == "ops gone"
+    ops, log = R.Ops(), len(lib.log)
+    R.TensorSet(ops, grads=[])
+    ops.destroy()
+    assert lib.log[log:] == ["set", "set gone", "ops gone"]
