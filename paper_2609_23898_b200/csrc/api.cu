@@ -149,8 +149,14 @@ int cerar_build_is_checked(void) {
 #endif
 }
 
-// for the library's other translation units
-void cerar_internal_set_error(const char* msg) { g_err = msg ? msg : ""; }
+// for the library's other translation units; a text that there is no memory for is dropped
+void cerar_internal_set_error(const char* msg) {
+    try {
+        g_err = msg ? msg : "";
+    } catch (...) {
+        g_err.clear();
+    }
+}
 // device ordinal the plan's fp32 copies live on, or -1 for a plan without device copies
 int cerar_internal_plan_device(const cerar_plan_t* P) { return (P && P->on_device) ? P->device : -1; }
 

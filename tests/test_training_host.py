@@ -114,3 +114,27 @@ def test_an_ops_destroys_its_sets_first(monkeypatch):
     R.TensorSet(ops, grads=[])
     ops.destroy()
     assert lib.log[log:] == ["set", "set gone", "ops gone"]
+
+
+LONG_MESSAGE = """
+import ctypes as C, resource
+from paper_2609_23898_b200 import cerar
+lib = cerar.lib
+lib.cerar_internal_set_error.argtypes = [C.c_char_p]
+lib.cerar_internal_set_error.restype = None
+message = b"x" * (64 << 20)
+now = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (now + (8 << 20), resource.RLIM_INFINITY))
+lib.cerar_internal_set_error(message)
+assert lib.cerar_last_error() == b""
+lib.cerar_internal_set_error(b"short")
+assert lib.cerar_last_error() == b"short"
+"""
+
+
+def test_an_error_text_without_memory_for_it():
+    """No C++ exception leaves a C entry: a text that cannot be kept is dropped."""
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-c", LONG_MESSAGE], cwd=ROOT, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, (r.returncode, r.stderr)
