@@ -375,7 +375,7 @@ class TensorSet:
     """Parameters, gradients and optimizer states of a step (cerar_tensors_t).
 
     grads              tensors of float32 or bfloat16, e.g. views into the aggregated vector
-    params, masters    the parameters (float32 or bfloat16), and for bfloat16 ones optional float32 copies
+    params, masters    the parameters (float32 or bfloat16), and for bfloat16 ones optional float32 copies (None where one has none)
     state_bits         32 or 8; with no params the set serves grad_norm only
     m, v               states of all tensors in one flat tensor each (zeros are made where none are given), tensor i at
                        state_offsets[i]: float32 of both moments, or e4m3 codes of the first moment and of the second one's
@@ -392,9 +392,14 @@ class TensorSet:
         ops._here(dev)
         self.ops, self.grads = ops, grads
         self.params = None if params is None else _flat(params, "params", n, dev)
-        self.masters = None if masters is None else _flat(masters, "masters", n, dev)
-        if self.masters is not None and any(t.dtype != torch.float32 for t in self.masters):
-            raise TypeError("masters: float32 wanted")
+        self.masters = None if masters is None else list(masters)
+        if self.masters is not None:
+            if len(self.masters) != len(n):
+                raise ValueError("masters: one for each tensor, or None in its place")
+            there = [i for i, t in enumerate(self.masters) if t is not None]
+            _flat([self.masters[i] for i in there], "masters", [n[i] for i in there], dev)
+            if any(self.masters[i].dtype != torch.float32 for i in there):
+                raise TypeError("masters: float32 wanted")
         self.state_bits = state_bits if params is not None else 0
         self.state_offsets = [0]
         for k in n:
@@ -429,7 +434,7 @@ class TensorSet:
             if self.state_bits:
                 at, size = self.state_offsets[i], state_bits // 8
                 d.param, d.param_type = self.params[i].data_ptr(), _type(self.params[i], "params")
-                d.master = None if self.masters is None else self.masters[i].data_ptr()
+                d.master = None if self.masters is None or self.masters[i] is None else self.masters[i].data_ptr()
                 d.m, d.v = self.m.data_ptr() + at * size, self.v.data_ptr() + at * size
                 if state_bits == 8:
                     d.m_scale = self.m_scale.data_ptr() + at // STATE_BLOCK * 4

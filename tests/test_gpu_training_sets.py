@@ -137,3 +137,40 @@ def test_an_ops_that_goes_before_its_sets():
         with pytest.raises(cerar.CerarError) as e:
             call()
         assert e.value.status == 1
+
+
+def test_parameters_of_mixed_kinds_in_one_set(ops):
+    """bfloat16 with and without a master copy and float32 in one set: the bits of a set of each kind (the stochastic one comes
+    first: its random bits go by its place)."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    torch.manual_seed(3)
+    sizes = [700, 1300, 5, 2049]
+    grads = [torch.randn(n, device="cuda") * 1e-3 for n in sizes]
+    start = [torch.randn(n, device="cuda") * 0.02 for n in sizes]
+    types = [torch.bfloat16, torch.bfloat16, torch.float32, torch.bfloat16]
+    with_master = [False, True, False, True]
+
+    def run(which, masters_of):
+        p = [start[i].to(types[i]) for i in which]
+        c = masters_of([start[i].clone() if with_master[i] else None for i in which])
+        s = R.TensorSet(ops, grads=[grads[i] for i in which], params=p, masters=c, weight_decay=[0.1 * i for i in which])
+        for step in (1, 2):
+            s.adamw(lr=1e-2, step=step, seed=step)
+        m = [s.m[a:a + grads[i].numel()] for a, i in zip(s.state_offsets, which)]
+        return p, c or [None] * len(which), m
+
+    p, c, m = run(range(4), lambda x: x)
+    for which, masters_of in (([0], lambda x: None), ([1, 3], lambda x: x), ([2], lambda x: [None])):
+        ps, cs, ms = run(which, masters_of)
+        for j, i in enumerate(which):
+            assert torch.equal(p[i], ps[j]) and torch.equal(m[i], ms[j])
+            assert (c[i] is None) == (cs[j] is None) == (not with_master[i])
+            if with_master[i]:
+                assert torch.equal(c[i], cs[j]) and torch.equal(p[i], c[i].bfloat16())
+    with pytest.raises(ValueError):
+        R.TensorSet(ops, grads=grads, params=[s.bfloat16() for s in start], masters=[None, start[1][:5], None, None])
+    with pytest.raises(ValueError):
+        R.TensorSet(ops, grads=grads, params=[s.bfloat16() for s in start], masters=[None] * 3)
+    with pytest.raises(TypeError):
+        R.TensorSet(ops, grads=grads, params=[s.bfloat16() for s in start], masters=[None, start[1].bfloat16(), None, None])
