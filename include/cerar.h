@@ -524,6 +524,11 @@ cerar_status_t cerar_fp8_matmul(cerar_ops_t* ops, const cerar_fp8_matrix_t* A, i
                                 const cerar_fp8_matrix_t* B, int trans_b, void* C, cerar_type_t type,
                                 int64_t ldc, int accumulate, cerar_stream_t stream);
 
+/* How such a product runs on a GPU of num_sms SMs, without a device: the columns of its tiles, 128 or 256 (of
+ * 128 rows; with pow2, both matrices', and 256 columns: of 256 rows, by a pair of blocks), and in *split the blocks
+ * that share the sum of a tile.  -1 for sizes that no product has. */
+int            cerar_fp8_matmul_tile(int64_t M, int64_t N, int64_t K, int pow2, int num_sms, int* split);
+
 /* A set of parameter tensors with their gradients and optimizer states, described once (the table is
  * copied to the device) and then used by one launch, or a few, per call however many tensors there are.
  * All pointers are device memory aligned to their elements; 16-byte alignment (and 4 bytes for the 8-bit

@@ -135,6 +135,7 @@ lib.cerar_ops_launch_count.argtypes = [_vp]
 lib.cerar_ops_launch_count.restype = C.c_uint64
 lib.cerar_fp8_quantize.argtypes = [_vp, _vp, C.c_int, _i64, _vp, C.c_int, _vp]       # (structures: by address)
 lib.cerar_fp8_matmul.argtypes = [_vp, _vp, C.c_int, _vp, C.c_int, _vp, C.c_int, _i64, C.c_int, _vp]
+lib.cerar_fp8_matmul_tile.argtypes = [_i64, _i64, _i64, C.c_int, C.c_int, C.POINTER(C.c_int)]
 lib.cerar_tensors_create.argtypes = [_vp, _i64, C.POINTER(TensorDesc), C.c_int, C.POINTER(_vp)]
 lib.cerar_tensors_destroy.argtypes = [_vp]
 lib.cerar_tensors_destroy.restype = None

@@ -935,6 +935,12 @@ Shape choose_shape(int M, int N, int kblocks, bool pow2, int num_sms) {
 
 }  // namespace
 
+int fp8_matmul_tile(int64_t M, int64_t N, int64_t K, bool pow2, int num_sms, int* split) {
+    const Shape shape = choose_shape((int)M, (int)N, (int)((K + BK - 1) / BK), pow2, num_sms);
+    *split = shape.split;
+    return shape.wide ? 256 : 128;
+}
+
 cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, uint64_t* launches) {
     if (!get_encode_fn()) return cudaErrorNotSupported;
     Params p = {};

@@ -40,6 +40,7 @@ struct MatmulArgs {
     int* status;
 };
 cudaError_t launch_fp8_matmul(const MatmulArgs& a, int num_sms, cudaStream_t s, uint64_t* launches);
+int fp8_matmul_tile(int64_t M, int64_t N, int64_t K, bool pow2, int num_sms, int* split);
 
 // One tensor of a set as the kernels see it.
 struct TensorRec {

@@ -185,6 +185,11 @@ cerar_status_t cerar_fp8_matmul(cerar_ops_t* o, const cerar_fp8_matrix_t* A, int
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "fp8 matmul launch");
 }
 
+int cerar_fp8_matmul_tile(int64_t M, int64_t N, int64_t K, int pow2, int num_sms, int* split) {
+    if (M < 1 || N < 1 || K < 1 || M > 0x7FFFFF00 || N > 0x7FFFFF00 || K > 0x7FFFFF00 || num_sms < 1 || !split) return -1;
+    return cerar::fp8_matmul_tile(M, N, K, pow2 != 0, num_sms, split);
+}
+
 cerar_status_t cerar_tensors_create(cerar_ops_t* o, int64_t count, const cerar_tensor_t* tensors, int state_bits,
                                     cerar_tensors_t** out) {
     if (!out) return fail(CERAR_ERR_INVALID_ARG, "out is NULL");

@@ -71,6 +71,7 @@ void cerar_internal_set_error(const char* msg) { g_error = msg; }
 namespace cerar {
 cudaError_t launch_fp8_quantize(const QuantizeArgs&, cerar_type_t, cudaStream_t, uint64_t* n) { ++*n; return call("launch", cudaErrorLaunchFailure); }
 cudaError_t launch_fp8_matmul(const MatmulArgs&, int, cudaStream_t, uint64_t* n) { ++*n; return call("launch", cudaErrorLaunchFailure); }
+int fp8_matmul_tile(int64_t, int64_t, int64_t, bool, int, int* split) { *split = 1; return 128; }
 cudaError_t launch_grad_norm(const NormArgs&, int, cudaStream_t, uint64_t* n) { ++*n; return call("launch", cudaErrorLaunchFailure); }
 cudaError_t launch_adamw(const AdamwArgs&, int, int, int, int, cudaStream_t, uint64_t* n) { ++*n; return call("launch", cudaErrorLaunchFailure); }
 cudaError_t launch_set_grads(TensorRec*, int64_t, int, void* const*, cudaStream_t, uint64_t* n) { ++*n; return call("launch", cudaErrorLaunchFailure); }

@@ -174,3 +174,65 @@ def test_parameters_of_mixed_kinds_in_one_set(ops):
         R.TensorSet(ops, grads=grads, params=[s.bfloat16() for s in start], masters=[None] * 3)
     with pytest.raises(TypeError):
         R.TensorSet(ops, grads=grads, params=[s.bfloat16() for s in start], masters=[None, start[1].bfloat16(), None, None])
+
+
+LONG = [8192 * 1200 + 5, 7, 2049, 8193, 8191, 0, 3, 10_000_001, 16384]        # 19.9 million: chunks of four times 2048 elements
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("offset", [0, 1, 3])
+def test_norm_of_long_chunks(ops, dtype, offset):
+    import torch
+    from paper_2609_23898_b200 import training as R
+    torch.manual_seed(offset)
+    flat = torch.randn(sum(LONG) + 8, device="cuda").to(getattr(torch, dtype))
+    flat[:offset] = float("nan")
+    flat[offset + sum(LONG):] = float("nan")
+    g = list(flat[offset:offset + sum(LONG)].split(LONG))
+    s = R.TensorSet(ops, grads=g)
+    n64 = float(flat[offset:offset + sum(LONG)].double().square().sum().sqrt())
+    a = s.grad_norm(1.0)
+    assert abs(a[0].item() - n64) <= 12 * U * n64 and a[2].item() == 1 and torch.equal(a, s.grad_norm(1.0))
+    for at in (0, 8192 * 1200 + 4, sum(LONG[:7]) + 9_999_999, sum(LONG) - 1):   # every element counts
+        keep = flat[offset + at].clone()
+        flat[offset + at] = float("inf")
+        assert s.grad_norm(1.0)[2].item() == 0
+        flat[offset + at] = keep
+
+
+@pytest.mark.parametrize("grad", ["float32", "bfloat16"])
+@pytest.mark.parametrize("param,offset", [("float32", 0), ("float32", 1), ("master", 0), ("master", 2)])
+def test_adamw_of_long_chunks(ops, param, offset, grad):
+    import torch
+    from paper_2609_23898_b200 import training as R
+    torch.manual_seed(7 + offset)
+    total = sum(LONG)
+    cut = lambda t: list(t[offset:offset + total].split(LONG))  # noqa: E731
+    gflat = (torch.randn(total + 8, device="cuda") * 1e-3).to(getattr(torch, grad))
+    pflat = torch.randn(total + 8, device="cuda") * 0.02
+    cflat = pflat.bfloat16() if param == "master" else None
+    edges = [torch.cat((t[:offset], t[offset + total:])) for t in (pflat, cflat) if t is not None]
+    s = R.TensorSet(ops, grads=cut(gflat), params=cut(cflat if param == "master" else pflat), masters=cut(pflat) if param == "master" else None,
+                    weight_decay=[0.1 * (i % 2) for i in range(len(LONG))])
+    s.m.normal_(std=3e-4)
+    s.v.exponential_(1.0).mul_(2.5e-7)
+    m0, v0, p0 = s.m.double(), s.v.double(), pflat.double()
+    clip = torch.tensor([2.0, 0.5, 1.0], device="cuda")
+    s.adamw(lr=3e-3, step=3, clip=clip)
+    at = offset
+    for i, n in enumerate(LONG):
+        a = s.state_offsets[i]
+        g, m, v, p = 0.5 * gflat[at:at + n].double(), m0[a:a + n], v0[a:a + n], p0[at:at + n]
+        terms = (0.9 * m).abs() + (0.1 * g).abs()
+        m1, v1 = 0.9 * m + (1 - 0.9) * g, 0.95 * v + (1 - 0.95) * g * g
+        root = (v1 / (1 - 0.95 ** 3)).sqrt() + 1e-8
+        p1 = p - 3e-3 * float(np.float32(0.1 * (i % 2))) * p - 3e-3 / (1 - 0.9 ** 3) * m1 / root
+        bound = 3 * U * p.abs() + 24 * U * 3e-3 / (1 - 0.9 ** 3) * terms / root + U * p1.abs()
+        assert bool(((s.m[a:a + n].double() - m1).abs() <= 4 * U * terms).all())
+        assert bool(((s.v[a:a + n].double() - v1).abs() <= 5 * U * v1).all())
+        assert bool(((pflat[at:at + n].double() - p1).abs() <= bound).all())
+        at += n
+    now = [torch.cat((t[:offset], t[offset + total:])) for t in (pflat, cflat) if t is not None]
+    assert all(torch.equal(x, y) for x, y in zip(edges, now))
+    if param == "master":
+        assert torch.equal(cflat[offset:offset + total], pflat[offset:offset + total].bfloat16())

@@ -138,3 +138,34 @@ def test_an_error_text_without_memory_for_it():
     import sys
     r = subprocess.run([sys.executable, "-c", LONG_MESSAGE], cwd=ROOT, capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, (r.returncode, r.stderr)
+
+
+def tile(m, n, k, pow2, sms=148):
+    split = C.c_int(-7)
+    return cerar.lib.cerar_fp8_matmul_tile(m, n, k, pow2, sms, C.byref(split)), split.value
+
+
+def test_products_of_the_gpu_tests_reach_every_kernel():
+    """What the comparison with 64 bits at these sizes is worth hangs on the tiles the rule takes there."""
+    from tests.test_gpu_training_tiles import SIZES
+    for (m, n, k), want in SIZES.items():
+        for pow2 in (0, 1):
+            cols, turns = want[pow2]
+            assert tile(m, n, k, pow2) == (cols, 1)
+            rows = 256 if pow2 and cols == 256 else 128
+            slots = 74 if rows == 256 else 148
+            assert -(-(-(-m // rows) * -(-n // cols)) // slots) == turns, (m, n, k, pow2)
+    reached = {(pow2, want[pow2][0], want[pow2][1] > 1) for want in SIZES.values() for pow2 in (0, 1)}
+    assert reached >= {(p, c, True) for p in (0, 1) for c in (128, 256)} | {(p, 256, False) for p in (0, 1)}
+
+
+def test_tiles_of_small_and_large_products():
+    assert tile(1, 8192, 2048, 1)[0] == 128 and tile(8192, 8192, 8192, 1) == (256, 1) and tile(8192, 8192, 8192, 0) == (256, 1)
+    assert tile(16, 16, 20000, 1)[1] > 1                                   # few tiles, a long sum: shared by a cluster
+    for m, n, k in ((1, 1, 1), (129, 1, 128), (1000, 1000, 100000), (0x7FFFFF00, 0x7FFFFF00, 0x7FFFFF00)):
+        for pow2 in (0, 1):
+            cols, split = tile(m, n, k, pow2)
+            assert cols in (128, 256) and 1 <= split <= min(8, -(-k // 128)) and (cols == 128 or split == 1)
+    for bad in ((0, 1, 1, 0), (1, -1, 1, 0), (1, 1, 0, 0), (1 << 31, 1, 1, 0), (1, 1, 1, 0, 0)):
+        assert tile(*bad) == (-1, -7)
+    assert cerar.lib.cerar_fp8_matmul_tile(1, 1, 1, 0, 148, None) == -1
