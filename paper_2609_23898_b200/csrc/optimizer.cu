@@ -244,13 +244,6 @@ __device__ __forceinline__ uint32_t finite_magnitude(float x) {
 template <int PK, typename G, int BITS, bool FULL>
 __device__ __forceinline__ void adamw_warp(const AdamwArgs& a, const TensorRec& t, int64_t e0 /* first element of the warp's block */, float coef,
                                            bool vec, bool gvec) {
-    // Root and quotient of the update are rounded to nearest like everything else, which costs at most 1 % and mostly gains (with
-    // approximations and so, us: 1.41e9 binary32 parameters, 32-bit states 6190, 6000; 2.7e8 elements with masters 1286, 1253, with 8-bit
-    // states 951, 911; binary32 parameters with 8-bit states 823, 834).  A bfloat16 parameter without a copy is rounded at random behind
-    // them, a choice that 2^-21 of the update changes once in a million; there rounded ones cost 9 % (32-bit states 900, 983) and
-    // 4 % (8-bit states 957, 1000), so the root (2^-23) and the quotient (2 units in the last place) are approximations.  The root of an
-    // 8-bit state decides which code is kept and is rounded everywhere.
-    constexpr bool ROUNDED = PK != PARAM_BF16;
     const int lane = threadIdx.x & 31;
     const int64_t left = t.numel - e0 - 4 * lane;
     const int n0 = FULL || left >= 4 ? 4 : (int)max((int64_t)0, left), n1 = FULL || left >= 132 ? 4 : (int)max((int64_t)0, left - 128);
@@ -308,14 +301,15 @@ __device__ __forceinline__ void adamw_warp(const AdamwArgs& a, const TensorRec& 
         split2(v2, v[j], v[j + 1]);
 #pragma unroll
         for (int i = j; i < j + 2; ++i) {
-            if constexpr (ROUNDED || BITS == 8) r[i] = __fsqrt_rn(v[i]);
+            // (the root of an 8-bit state decides which code is kept: rounded to nearest; otherwise only the update sees it: within 2 u)
+            if constexpr (BITS == 8) r[i] = __fsqrt_rn(v[i]);
             else asm("sqrt.approx.f32 %0, %1;" : "=f"(r[i]) : "f"(v[i]));
         }
         float d0, d1, q0, q1;
         split2(fma2x(two(r[j], r[j + 1]), rs2, eps2), d0, d1);
         split2(mul2(two(p[j], p[j + 1]), keep2), q0, q1);
-        p[j] = fmaf(-step, ROUNDED ? __fdiv_rn(m[j], d0) : __fdividef(m[j], d0), q0);
-        p[j + 1] = fmaf(-step, ROUNDED ? __fdiv_rn(m[j + 1], d1) : __fdividef(m[j + 1], d1), q1);
+        p[j] = fmaf(-step, __fdividef(m[j], d0), q0);
+        p[j + 1] = fmaf(-step, __fdividef(m[j + 1], d1), q1);
         if constexpr (BITS == 8) {
             mtop = max_nan(mtop, max_nan(fabsf(m[j]), fabsf(m[j + 1])));
             rtop = max_nan(rtop, max_nan(r[j], r[j + 1]));
