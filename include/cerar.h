@@ -566,7 +566,9 @@ cerar_status_t cerar_grad_norm(cerar_tensors_t* set, float max_norm, float* clip
  *     g1 = clip[1] g;  m1 = beta1 m + (1 - beta1) g1;  v1 = beta2 v + (1 - beta2) g1^2
  *     p1 = p (1 - lr weight_decay) - lr / (1 - beta1^step) m1 / (sqrt(v1 / (1 - beta2^step)) + eps)
  * with lr times the tensor's lr_scale; 1 - beta and the step's corrections are derived in binary64 and rounded
- * once, all arithmetic on elements is binary32.  clip: what cerar_grad_norm wrote (device),
+ * once.  Arithmetic on elements is binary32, rounded to nearest but for two approximations that only the
+ * update sees: its quotient (2 units in the last place) and, with 32-bit states, its root (2^-23).  lr / ... m1 /
+ * (...) is within 2^-21 of itself from the new m1 and v1 (eps below 2^125).  clip: what cerar_grad_norm wrote (device),
  * or NULL for no clipping; where clip[2] is 0 the call changes nothing.  step counts from 1.
  * 8-bit states: m and sqrt(v) are kept as e4m3 codes with one power-of-two scale (as in cerar_fp8_quantize)
  * per 256 consecutive elements of a tensor, rounded up or down at random with the probabilities that make

@@ -301,7 +301,11 @@ __device__ __forceinline__ void adamw_warp(const AdamwArgs& a, const TensorRec& 
         split2(v2, v[j], v[j + 1]);
 #pragma unroll
         for (int i = j; i < j + 2; ++i) {
-            // (the root of an 8-bit state decides which code is kept: rounded to nearest; otherwise only the update sees it: within 2 u)
+            // The root of an 8-bit state decides which code is kept and is rounded to nearest.  Otherwise only the update sees it, and it
+            // is an approximation (2^-23), as the quotient below is (2 units in the last place): the update is within 2^-21 of the formula's,
+            // and usually far smaller than the parameter it is added to.  Rounded to nearest both are branches, eight of each per
+            // thread: 65,536 elements 3.95 -> 4.32 us, bfloat16 parameters without copies 900 -> 983 (2.7e8 elements, 32-bit states) and
+            // 957 -> 1000 (8-bit states), while 1.41e9 binary32 elements gain (6240 -> 5960).
             if constexpr (BITS == 8) r[i] = __fsqrt_rn(v[i]);
             else asm("sqrt.approx.f32 %0, %1;" : "=f"(r[i]) : "f"(v[i]));
         }

@@ -44,6 +44,10 @@ def test_a_set_used_at_once_on_a_side_stream(ops):
             assert abs(out[0].item() - n64) <= 12 * U * n64
 
 
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
 FIRST_PRODUCTS = """
 import ctypes as C, threading, torch
 from paper_2609_23898_b200 import cerar, training as R
@@ -236,3 +240,44 @@ def test_adamw_of_long_chunks(ops, param, offset, grad):
     assert all(torch.equal(x, y) for x, y in zip(edges, now))
     if param == "master":
         assert torch.equal(cflat[offset:offset + total], pflat[offset:offset + total].bfloat16())
+
+
+@pytest.mark.parametrize("grad", ["float32", "bfloat16"])
+@pytest.mark.parametrize("param,bits", [("float32", 32), ("master", 32), ("float32", 8), ("master", 8)])
+def test_adamw_rounds_as_the_header_says(ops, param, bits, grad):
+    """32-bit states have the bits of the formula in binary32, operation by operation (numpy's are rounded to nearest).  Parameters of zero
+    show the update by itself: within 2^-21 of its formula in 64 bits from those states (root 2^-23, its product with the correction 2^-24,
+    quotient 2^-22, last product 2^-24)."""
+    import torch
+    from paper_2609_23898_b200 import training as R
+    f = np.float32
+    n, lr, b1, b2, step = 100_000, 3e-3, 0.9, 0.95, 7
+    rng = np.random.default_rng(bits)
+    g = torch.from_numpy((rng.standard_normal(n) * 1e-3).astype(f)).cuda().to(getattr(torch, grad))
+    p = torch.zeros(n, device="cuda", dtype=torch.float32 if param == "float32" else torch.bfloat16)
+    c = torch.zeros(n, device="cuda") if param == "master" else None
+    s = R.TensorSet(ops, grads=[g], params=[p], masters=None if c is None else [c], state_bits=bits)
+    if bits == 32:
+        s.m.normal_(std=3e-4)
+        s.v.exponential_(1.0).mul_(2.5e-7)
+        m, v = s.m.cpu().numpy()[:n], s.v.cpu().numpy()[:n]
+    else:
+        s.adamw(lr=lr, betas=(b1, b2), eps=1e-8, step=1, seed=1)           # states that have something in them
+        p.zero_()
+        if c is not None:
+            c.zero_()
+        wide = lambda t, w: (t.float() * w.repeat_interleave(256)).cpu().numpy()[:n]  # noqa: E731
+        m, r = wide(s.m, s.m_scale), wide(s.v, s.v_scale)
+        v = r * r
+    s.adamw(lr=lr, betas=(b1, b2), eps=0.0, step=step, seed=2)
+    g = g.float().cpu().numpy()
+    m = f(b1) * m + f(1 - b1) * g
+    v = f(b2) * v + f(1 - b2) * (g * g)
+    if bits == 32:
+        assert np.array_equal(s.m.cpu().numpy()[:n], m) and np.array_equal(s.v.cpu().numpy()[:n], v)
+    m, v = m.astype(np.float64), v.astype(np.float64)
+    want = -float(f(lr / (1 - b1 ** step))) * m / (np.sqrt(v) * float(f(1 / np.sqrt(1 - b2 ** step))))
+    got = f64(p if c is None else c)
+    assert (np.abs(got - want) <= 2.0 ** -21 * np.abs(want)).all()
+    if c is not None:
+        assert torch.equal(p, c.bfloat16())
