@@ -56,6 +56,7 @@ def dequantize(q, s, rows, cols):
 
 
 def scramble(h):
+    """Shifts and multipliers: C. Wellons, "Prospecting for Hash Functions", 2018."""
     h = ((h ^ (h >> np.uint64(16))) * np.uint64(0x7FEB352D)) & M32
     h = ((h ^ (h >> np.uint64(15))) * np.uint64(0x846CA68B)) & M32
     return h ^ (h >> np.uint64(16))

@@ -12,7 +12,8 @@
 //
 // Where all scales are powers of two the tensor core multiplies by them itself and nothing is taken out before 16 blocks of k are
 // summed up: fp8_matmul_pow2_kernel below, 8192^3 416 us (2640 TFLOP/s), 16384 x 8192 x 2048 234 us (2350).  In a long
-// loop the power limit decides (8192^3: 485 us at 1.27 GHz); the library's own 8-bit product takes 413 and 197 us at these sizes.
+// loop the power limit decides (8192^3: 485 us at 1.27 GHz); the library's own 8-bit product takes 413 and 197 us at these sizes, so
+// with short sums (16 blocks of k: one segment per tile) there is something left in the hand-over from tile to tile.
 //
 // Operands come in as tiles of 128 bytes of one dimension by 128 (or BN) of the other, in the 128-byte swizzle that the
 // tensor core reads, whichever dimension is contiguous in memory: a transposed operand is read in place (the "MN-major" form).

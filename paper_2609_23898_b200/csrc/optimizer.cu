@@ -163,7 +163,9 @@ __global__ void __launch_bounds__(THREADS) grad_norm_kernel(const __grid_constan
 
 // ---------------------------------------------------------------- AdamW
 
-__device__ __forceinline__ uint32_t scramble(uint32_t h) {             // multiply and xor-shift rounds: every input bit reaches every output bit
+// Multiply and xor-shift rounds: every input bit reaches every output bit.  Shifts and multipliers are published: C. Wellons, "Prospecting
+// for Hash Functions", 2018 (a search for 32-bit hashes of this form with little bias).
+__device__ __forceinline__ uint32_t scramble(uint32_t h) {
     h = (h ^ (h >> 16)) * 0x7FEB352Du;
     h = (h ^ (h >> 15)) * 0x846CA68Bu;
     return h ^ (h >> 16);

@@ -480,7 +480,8 @@ class TensorSet:
 
     def adamw(self, *, lr: float, betas=(0.9, 0.95), eps: float = 1e-8, step: int, clip: torch.Tensor | None = None, seed: int = 0):
         """One AdamW step, in place.  clip: what grad_norm returned; seed: of the random rounding (8-bit states, bfloat16
-        parameters without masters), another one for every step."""
+        parameters without masters), another one for every step.  All of these are values of the call: a CUDA graph that captured it
+        repeats them."""
         o = self._opt
         o.lr, o.beta1, o.beta2, o.eps, o.step, o.seed = lr, betas[0], betas[1], eps, step, seed
         if clip is not None and (clip.dtype != _F32 or clip.numel() != 3 or clip.device != self._device or not clip.is_contiguous()):
