@@ -99,15 +99,32 @@ class Quantized:
         self.desc = Fp8Matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, lds, scaling, pow2)
         self.at = C.addressof(self.desc)
 
+    def _saved(self):
+        """(tensors to save for a backward pass, what _restored wants beside them, which holds no memory)."""
+        tensors = (self._codes, self._scales) if self._buffer is None else (self._buffer, None)
+        return tensors, (self.scaling, self.desc, None if self._buffer is None else self._parts)
+
     @classmethod
-    def _of(cls, codes, scales, scaling, pow2):
-        """Of tensors that were saved for a backward pass, with `codes` copied where they came back in another layout (from the host)."""
-        rows, cols = codes.shape
-        if rows > 1 and (codes.stride(0) & 15 or codes.stride(1) != 1) or codes.data_ptr() & 15:
-            wide = torch.empty(rows, (cols + 15) & -16, dtype=codes.dtype, device=codes.device)
-            codes = wide[:, :cols].copy_(codes)
+    def _restored(cls, first, second, rest):
+        """The matrix of tensors that _saved gave: the same memory, or copies of it (from the host, packed)."""
+        scaling, desc, parts = rest
         q = cls.__new__(cls)
-        q._set(codes, scales, scaling, rows, cols, codes.stride(0) if rows > 1 else (cols + 15) & -16, _ld(scales), pow2)
+        if second is None:
+            base = first.data_ptr()
+            if base + parts[0] != desc.codes:
+                desc = Fp8Matrix(base + parts[0], base + parts[1], desc.rows, desc.cols, desc.ld, desc.lds, scaling, desc.pow2)
+            q._codes = q._scales = None
+            q.scaling, q.desc, q.at, q._buffer, q._parts = scaling, desc, C.addressof(desc), first, parts
+            return q
+        rows, cols = first.shape
+        if first.data_ptr() == desc.codes and second.data_ptr() == desc.scales and (rows < 2 or first.stride(0) == desc.ld) and \
+                (second.size(0) < 2 or second.stride(0) == desc.lds):
+            q._codes, q._scales, q.scaling, q.desc, q.at, q._buffer = first, second, scaling, desc, C.addressof(desc), None
+            return q
+        if rows > 1 and (first.stride(0) & 15 or first.stride(1) != 1) or first.data_ptr() & 15:
+            wide = torch.empty(rows, (cols + 15) & -16, dtype=first.dtype, device=first.device)
+            first = wide[:, :cols].copy_(first)
+        q._set(first, second, scaling, rows, cols, first.stride(0) if rows > 1 else (cols + 15) & -16, _ld(second), desc.pow2)
         return q
 
     @staticmethod
@@ -307,11 +324,10 @@ def linear_backward(ops: Ops, dy: torch.Tensor, xc: Quantized, w: Quantized, dw:
 def _rows(t: torch.Tensor) -> torch.Tensor:
     """t (..., columns) as a matrix whose rows the conversion can read: a copy where a row's elements are not contiguous or rows overlap
     (transposed inputs, gradients that autograd expands from one element)."""
-    t = t.unsqueeze(0) if t.dim() == 1 else t.flatten(0, -2)
-    rows, cols = t.shape
-    if t.stride(1) != 1 and cols > 1 or t.stride(0) < cols and rows > 1:
-        t = t.contiguous()
-    return t
+    if t.dim() != 2:
+        t = t.unsqueeze(0) if t.dim() == 1 else t.flatten(0, -2)
+    (rows, cols), (row, col) = t.shape, t.stride()
+    return t.contiguous() if col != 1 and cols > 1 or row < cols and rows > 1 else t
 
 
 class Linear8(torch.autograd.Function):
@@ -335,25 +351,23 @@ class Linear8(torch.autograd.Function):
         y, xc = linear(ops, _rows(x), w)
         # Saved as autograd saves tensors: freed by the backward pass, within reach of saved-tensor hooks, and refused if changed in between.
         # (Weights made in inference mode cannot be saved; they are held as they are.)
-        ctx.ops, ctx.dw, ctx.kinds, ctx.w = ops, dw, (xc.scaling, xc.desc.pow2, w.scaling, w.desc.pow2), None
-        keep = [None] * 4
+        ctx.ops, ctx.dw, ctx.x_rest, ctx.w_rest, ctx.w = ops, dw, None, None, None
+        xs = ws = (None, None)
         if dw is not None:
-            keep[:2] = xc.codes, xc.scales
+            xs, ctx.x_rest = xc._saved()
         if ctx.needs_input_grad[0]:
-            if w.codes.is_inference() or w.scales.is_inference():
-                ctx.w = w
-            else:
-                keep[2:] = w.codes, w.scales
-        ctx.save_for_backward(*keep)
+            ws, ctx.w_rest = w._saved()
+            if any(t is not None and t.is_inference() for t in ws):
+                ws, ctx.w_rest, ctx.w = (None, None), None, w
+        ctx.save_for_backward(*xs, *ws)
         return y.view(*x.shape[:-1], y.shape[-1])
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        xs, xp, ws, wp = ctx.kinds
-        x_codes, x_scales, w_codes, w_scales = ctx.saved_tensors
-        xc = None if x_codes is None else Quantized._of(x_codes, x_scales, xs, xp)
-        w = ctx.w if w_codes is None else Quantized._of(w_codes, w_scales, ws, wp)
+        saved = ctx.saved_tensors
+        xc = None if ctx.x_rest is None else Quantized._restored(saved[0], saved[1], ctx.x_rest)
+        w = ctx.w if ctx.w_rest is None else Quantized._restored(saved[2], saved[3], ctx.w_rest)
         dx = linear_backward(ctx.ops, _rows(dy), xc, w, ctx.dw, need_dx=ctx.needs_input_grad[0])
         return None if dx is None else dx.view(*dy.shape[:-1], dx.shape[-1]), None, None, None, None
 

@@ -226,25 +226,27 @@ def test_saved_tensor_hooks_reach_what_is_kept(ops, k):
     assert torch.equal(x.grad.double(), dy.double() @ w.double()) and torch.equal(dw.double(), dy.double().t() @ x.detach().double())
 
 
-def test_weights_changed_between_the_passes_are_noticed(ops):
+@pytest.mark.parametrize("k", [48, 200])
+def test_weights_changed_between_the_passes_are_noticed(ops, k):
     import torch
     from paper_2609_23898_b200 import training as R
     rng = np.random.default_rng(9)
-    w, wq, dw = layer(ops, rng, 70, 48)
-    x = whole(rng, 60, 48).requires_grad_()
+    w, wq, dw = layer(ops, rng, 70, k)
+    x = whole(rng, 60, k).requires_grad_()
     y = R.Linear8.apply(x, wq, ops, dw)
     wq.scales.mul_(2)
     with pytest.raises(RuntimeError):
         y.backward(torch.ones_like(y))
 
 
-def test_weights_made_in_inference_mode(ops):
+@pytest.mark.parametrize("k", [48, 200])
+def test_weights_made_in_inference_mode(ops, k):
     import torch
     from paper_2609_23898_b200 import training as R
     rng = np.random.default_rng(11)
     with torch.inference_mode():
-        w, wq, _ = layer(ops, rng, 70, 48)
-    x, dy, dw = whole(rng, 60, 48).requires_grad_(), whole(rng, 60, 70), torch.zeros(70, 48, device="cuda")
+        w, wq, _ = layer(ops, rng, 70, k)
+    x, dy, dw = whole(rng, 60, k).requires_grad_(), whole(rng, 60, 70), torch.zeros(70, k, device="cuda")
     y = R.Linear8.apply(x, wq, ops, dw)
     y.backward(dy)
     assert torch.equal(x.grad.double(), dy.double() @ w.double()) and torch.equal(dw.double(), dy.double().t() @ x.detach().double())
