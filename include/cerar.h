@@ -61,7 +61,8 @@ typedef enum {
     CERAR_ERR_NOMEM = 7,
     CERAR_ERR_TIMEOUT = 8,
     CERAR_ERR_TOO_LARGE = 9,     /* request exceeds the built-in workspace (see below)    */
-    CERAR_ERR_BOUNDS = 10        /* checked build only: a kernel formed an address outside its buffer */
+    CERAR_ERR_BOUNDS = 10        /* checked build: a kernel formed an address outside its buffer;
+                                    cerar_ops_status: a token or position beyond its table was met    */
 } cerar_status_t;
 
 typedef enum {
@@ -481,7 +482,8 @@ typedef enum { CERAR_TYPE_F32 = 0, CERAR_TYPE_BF16 = 1 } cerar_type_t;
 
 cerar_status_t cerar_ops_create(cerar_ops_t** out);     /* CERAR_ERR_CUDA without a device */
 void           cerar_ops_destroy(cerar_ops_t* ops);     /* after the sets that were made with it */
-/* Synchronises `stream`; CERAR_ERR_TIMEOUT if a kernel gave up on a bounded wait since the last check. */
+/* Synchronises `stream`; CERAR_ERR_TIMEOUT if a kernel gave up on a bounded wait since the last check, CERAR_ERR_BOUNDS if
+ * one met a token or a position beyond the end of its table (cerar_embed, cerar_head_norm). */
 cerar_status_t cerar_ops_status(cerar_ops_t* ops, cerar_stream_t stream);
 uint64_t       cerar_ops_launch_count(const cerar_ops_t* ops);
 
@@ -590,6 +592,68 @@ typedef struct {
 } cerar_adamw_options_t;
 cerar_status_t cerar_adamw_step(cerar_tensors_t* set, const cerar_adamw_options_t* opt, const float* clip,
                                 cerar_stream_t stream);
+
+/* ---- Layers around the linear ones ----
+ *
+ * The rest of a model's weights: embedding rows, norm weights of heads, gated feed-forward blocks.  The same rules as above; the
+ * gradients of weights are written, or added (accumulate != 0), where the caller wants them, e.g. into the aggregated vector.  Calls
+ * that take a workspace want cerar_..._workspace bytes of device memory, 16-byte aligned; calls that may run at the same time,
+ * replayed graphs included, want one each. */
+
+/* Lookup: y[t] = scale table[ids[t]], product in binary32, one rounding to y_type.  table: vocab x width of `type`, ld elements between
+ * rows; y: tokens x width, ldy between rows.  ids: tokens integers of id_bytes (4 or 8) bytes.  An id below zero is padding: its row
+ * of y is zero.  One from vocab on is treated like padding and reported by cerar_ops_status. */
+cerar_status_t cerar_embed(cerar_ops_t* ops, const void* table, cerar_type_t type, int64_t vocab, int64_t width, int64_t ld,
+                           const void* ids, int id_bytes, int64_t tokens, float scale, void* y, cerar_type_t y_type, int64_t ldy,
+                           cerar_stream_t stream);
+
+/* Its gradient: dtable[v] = scale sum_{t: ids[t] = v} dy[t], or dtable[v] + that with accumulate != 0 (rows of no token are then not
+ * touched; otherwise they become zero).  Sums in binary32: pieces of a fixed length of the tokens in order, then the pieces in order;
+ * one rounding to d_type.  Deterministic.  dy of padding is not read. */
+size_t         cerar_embed_grad_workspace(int64_t tokens, int64_t vocab, int64_t width);
+cerar_status_t cerar_embed_grad(cerar_ops_t* ops, const void* dy, cerar_type_t type, int64_t lddy, const void* ids, int id_bytes,
+                                int64_t tokens, float scale, void* dtable, cerar_type_t d_type, int64_t vocab, int64_t width,
+                                int64_t ld, int accumulate, void* workspace, size_t workspace_bytes, cerar_stream_t stream);
+
+/* Norm of every head's values and rotation by position, for queries and keys in one call:
+ *     r = 1 / sqrt(mean_j x_j^2 + eps),  z_j = w_j r x_j,  y = z with its first `rotated` values turned in pairs:
+ *     (z_a, z_b) -> (z_a cos - z_b sin, z_b cos + z_a sin)
+ * pairs: j and j + rotated / 2, or 2 j and 2 j + 1 with `neighbours`; cos and sin of pair j from table[position][j].
+ * Arithmetic in binary32, one rounding at the end.  Rows (dim values, next to one another) of token t and head h start at
+ * x + t x_token + h x_head elements; strides may be anything, as long as rows that are written overlap neither one another nor what is read. */
+#define CERAR_HEAD_DIM_MAX 512
+typedef struct {
+    const void* x;
+    void*       y;               /* the result; in the gradient: dx                                       */
+    const void* w;               /* dim weights of w_type; NULL: all one                                  */
+    const void* dy;              /* gradient only                                                         */
+    void*       dw;              /* gradient only: dim values of dw_type; NULL: not wanted                */
+    int64_t     x_token, x_head, y_token, y_head, dy_token, dy_head;
+    int64_t     heads;
+} cerar_heads_t;
+typedef struct {
+    const float* table;          /* rows x rotated / 2 pairs (cos, sin), as cerar_rotation_table makes it  */
+    int64_t      rows;
+    const void*  positions;      /* period integers of position_bytes (4 or 8) bytes; NULL: 0 .. period - 1 */
+    int64_t      period;         /* token t has position number t % period: positions that repeat for every sequence */
+    int32_t      position_bytes;
+    int32_t      rotated;        /* values that are turned, even, up to dim; 0: a norm alone, no table      */
+    int32_t      neighbours;
+} cerar_rotation_t;
+/* A position below zero is padding: its rows of y (dx) are zero, it adds nothing to dw, and its x and dy may hold anything.  A
+ * position from `rows` on is treated like padding and reported by cerar_ops_status.
+ * dim: even, 2 to 512.  parts: 1 or 2, e.g. queries and keys. */
+cerar_status_t cerar_head_norm(cerar_ops_t* ops, cerar_type_t type, const cerar_heads_t* parts, int count, cerar_type_t w_type,
+                               int64_t tokens, int dim, float eps, const cerar_rotation_t* rotation, cerar_stream_t stream);
+/* Its gradient.  dz: dy turned back;  dw_j (+)= sum over rows of dz_j r x_j;  dn = w dz;  dx = r (dn - r x mean_j(dn_j r x_j)).
+ * Sums over rows in binary32 in a fixed order: deterministic. */
+size_t         cerar_head_norm_grad_workspace(int count, int dim);
+cerar_status_t cerar_head_norm_grad(cerar_ops_t* ops, cerar_type_t type, const cerar_heads_t* parts, int count, cerar_type_t w_type,
+                                    cerar_type_t dw_type, int accumulate, int64_t tokens, int dim, float eps,
+                                    const cerar_rotation_t* rotation, void* workspace, size_t workspace_bytes, cerar_stream_t stream);
+/* table[i][j] = (cos, sin) of (first + i) freqs[j], worked out in binary64 and rounded once.  freqs: `pairs` (up to 256) numbers on the host. */
+cerar_status_t cerar_rotation_table(cerar_ops_t* ops, const double* freqs, int pairs, int64_t first, int64_t rows, float* table,
+                                    cerar_stream_t stream);
 
 const char*    cerar_status_string(cerar_status_t s);
 const char*    cerar_last_error(void);   /* thread-local detail of the last failure */

@@ -52,6 +52,17 @@ class Fp8Matrix(C.Structure):
                 ("ld", C.c_int64), ("lds", C.c_int64), ("scaling", C.c_int32), ("pow2", C.c_int32)]
 
 
+class Heads(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("w", C.c_void_p), ("dy", C.c_void_p), ("dw", C.c_void_p),
+                ("x_token", C.c_int64), ("x_head", C.c_int64), ("y_token", C.c_int64), ("y_head", C.c_int64),
+                ("dy_token", C.c_int64), ("dy_head", C.c_int64), ("heads", C.c_int64)]
+
+
+class Rotation(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("rows", C.c_int64), ("positions", C.c_void_p), ("period", C.c_int64),
+                ("position_bytes", C.c_int32), ("rotated", C.c_int32), ("neighbours", C.c_int32)]
+
+
 class TensorDesc(C.Structure):
     _fields_ = [("numel", C.c_int64), ("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p),
                 ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
@@ -142,6 +153,16 @@ lib.cerar_tensors_destroy.restype = None
 lib.cerar_tensors_set_grads.argtypes = [_vp, C.POINTER(_vp), _vp]
 lib.cerar_grad_norm.argtypes = [_vp, C.c_float, _vp, _vp]
 lib.cerar_adamw_step.argtypes = [_vp, _vp, _vp, _vp]
+lib.cerar_embed.argtypes = [_vp, _vp, C.c_int, _i64, _i64, _i64, _vp, C.c_int, _i64, C.c_float, _vp, C.c_int, _i64, _vp]
+lib.cerar_embed_grad_workspace.argtypes = [_i64, _i64, _i64]
+lib.cerar_embed_grad_workspace.restype = C.c_size_t
+lib.cerar_embed_grad.argtypes = [_vp, _vp, C.c_int, _i64, _vp, C.c_int, _i64, C.c_float, _vp, C.c_int, _i64, _i64, _i64, C.c_int, _vp,
+                                 C.c_size_t, _vp]
+lib.cerar_rotation_table.argtypes = [_vp, C.POINTER(C.c_double), C.c_int, _i64, _i64, _vp, _vp]
+lib.cerar_head_norm.argtypes = [_vp, C.c_int, _vp, C.c_int, C.c_int, _i64, C.c_int, C.c_float, _vp, _vp]
+lib.cerar_head_norm_grad_workspace.argtypes = [C.c_int, C.c_int]
+lib.cerar_head_norm_grad_workspace.restype = C.c_size_t
+lib.cerar_head_norm_grad.argtypes = [_vp, C.c_int, _vp, C.c_int, C.c_int, C.c_int, C.c_int, _i64, C.c_int, C.c_float, _vp, _vp, C.c_size_t, _vp]
 lib.cerar_status_string.argtypes = [C.c_int]
 lib.cerar_status_string.restype = C.c_char_p
 lib.cerar_last_error.restype = C.c_char_p

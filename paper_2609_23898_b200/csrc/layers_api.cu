@@ -1,0 +1,176 @@
+// C ABI of the layers' operators (embedding, head norms): argument checks, launches.
+#include <cuda_runtime.h>
+
+#include <cmath>
+
+#include "../../include/cerar.h"
+#include "ops.cuh"
+#include "ops_handle.hpp"
+
+using cerar::check_ops;
+using cerar::cuda_fail;
+using cerar::fail;
+using cerar::misaligned;
+using cerar::type_bytes;
+using cerar::type_ok;
+
+namespace {
+
+constexpr int64_t TOKENS_MAX = 0x7FFFFF00, SIZE_MAX_ = 0x7FFFFF00, LD_MAX = (int64_t)1 << 40;
+
+cerar_status_t check_ids(const void* ids, int id_bytes, int64_t tokens, int64_t vocab, int64_t width) {
+    if (id_bytes != 4 && id_bytes != 8) return fail(CERAR_ERR_INVALID_ARG, "ids of 4 or 8 bytes are wanted");
+    if (tokens < 0 || tokens > TOKENS_MAX || vocab < 0 || vocab > SIZE_MAX_ || width < 0 || width > SIZE_MAX_)
+        return fail(CERAR_ERR_SHAPE, "embedding: negative sizes, or above 2^31 - 256");
+    if (tokens > 0 && (!ids || misaligned(ids, (uintptr_t)id_bytes))) return fail(CERAR_ERR_INVALID_ARG, "ids NULL or not aligned to their elements");
+    return CERAR_OK;
+}
+// rows x width of `type`, ld elements between rows
+cerar_status_t check_rows(const void* p, int type, int64_t rows, int64_t width, int64_t ld, const char* null_text) {
+    if (!type_ok(type)) return fail(CERAR_ERR_INVALID_ARG, "unknown element type");
+    if (rows == 0 || width == 0) return CERAR_OK;
+    if (!p || misaligned(p, type_bytes(type))) return fail(CERAR_ERR_INVALID_ARG, null_text);
+    if (rows > 1 && (ld < width || ld > LD_MAX)) return fail(CERAR_ERR_SHAPE, "rows overlap, or lie more than 2^40 elements apart");
+    return CERAR_OK;
+}
+
+cerar_status_t check_heads(const cerar_heads_t* parts, int count, cerar_type_t type, int64_t tokens, int dim, bool grad, cerar::HeadNormArgs& a) {
+    if (!type_ok(type)) return fail(CERAR_ERR_INVALID_ARG, "unknown element type");
+    if (!parts || count < 1 || count > 2) return fail(CERAR_ERR_INVALID_ARG, "1 or 2 groups of heads are wanted");
+    if (tokens < 0 || tokens > TOKENS_MAX) return fail(CERAR_ERR_SHAPE, "a negative number of tokens, or above 2^31 - 256");
+    if (dim < 2 || dim > CERAR_HEAD_DIM_MAX || dim % 2) return fail(CERAR_ERR_SHAPE, "the values of a head must be an even number from 2 to 512");
+    a.count = count; a.tokens = tokens; a.dim = dim; a.type = type;
+    for (int i = 0; i < count; ++i) {
+        const cerar_heads_t& h = parts[i];
+        if (h.heads < 0 || h.heads > 0xFFFF) return fail(CERAR_ERR_SHAPE, "a negative number of heads, or above 65535");
+        auto rows_ok = [&](const void* p, int64_t token, int64_t head) {
+            if (!p || misaligned(p, type_bytes(type))) return false;
+            return token > -LD_MAX && token < LD_MAX && head > -LD_MAX && head < LD_MAX;
+        };
+        // written rows: no two of them may lie over one another
+        auto apart = [&](int64_t token, int64_t head) {
+            const int64_t t = token < 0 ? -token : token, d = head < 0 ? -head : head;
+            if (h.heads < 2) return tokens < 2 || t >= dim;
+            if (tokens < 2) return d >= dim;
+            return (d >= dim && t >= d * (h.heads - 1) + dim) || (t >= dim && d >= t * (tokens - 1) + dim);
+        };
+        if (tokens > 0 && h.heads > 0) {
+            if (!rows_ok(h.x, h.x_token, h.x_head) || !rows_ok(h.y, h.y_token, h.y_head) || (grad && !rows_ok(h.dy, h.dy_token, h.dy_head)))
+                return fail(CERAR_ERR_INVALID_ARG, "heads: a pointer is NULL or not aligned to its elements, or strides are above 2^40");
+            if (!apart(h.y_token, h.y_head)) return fail(CERAR_ERR_SHAPE, "heads: rows that are written overlap");
+        }
+        cerar::HeadPart& p = a.part[i];
+        p = {h.x, h.dy, h.w, h.y, grad ? h.dw : nullptr, h.x_token, h.x_head, h.dy_token, h.dy_head, h.y_token, h.y_head, (int)h.heads};
+    }
+    return CERAR_OK;
+}
+cerar_status_t check_rotation(const cerar_rotation_t* r, int dim, cerar::HeadNormArgs& a) {
+    if (!r) return fail(CERAR_ERR_INVALID_ARG, "rotation is NULL");
+    if (r->rotated < 0 || r->rotated > dim || r->rotated % 2) return fail(CERAR_ERR_SHAPE, "the values that are turned must be an even number up to the head's");
+    if (r->period < 1) return fail(CERAR_ERR_SHAPE, "period must be at least 1");
+    if (r->rows < 0 || (r->rotated > 0 && (!r->table || misaligned(r->table, 8)))) return fail(CERAR_ERR_INVALID_ARG, "rotation table NULL, not aligned to 8 bytes, or of a negative length");
+    if (r->positions && ((r->position_bytes != 4 && r->position_bytes != 8) || misaligned(r->positions, (uintptr_t)r->position_bytes)))
+        return fail(CERAR_ERR_INVALID_ARG, "positions of 4 or 8 bytes, aligned, are wanted");
+    a.rotated = r->rotated; a.neighbours = r->neighbours != 0; a.period = r->period;
+    a.table = reinterpret_cast<const float2*>(r->table);
+    a.table_rows = r->rotated > 0 ? r->rows : (int64_t)1 << 62;          // (nothing is looked up: any position will do)
+    a.positions = r->positions; a.position_bytes = r->position_bytes;
+    return CERAR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cerar_status_t cerar_embed(cerar_ops_t* o, const void* table, cerar_type_t type, int64_t vocab, int64_t width, int64_t ld, const void* ids,
+                           int id_bytes, int64_t tokens, float scale, void* y, cerar_type_t y_type, int64_t ldy, cerar_stream_t stream) {
+    cerar_status_t st = check_ops(o);
+    if (st != CERAR_OK) return st;
+    if ((st = check_ids(ids, id_bytes, tokens, vocab, width)) != CERAR_OK ||
+        (st = check_rows(table, type, vocab, width, ld, "table NULL or not aligned to its elements")) != CERAR_OK ||
+        (st = check_rows(y, y_type, tokens, width, ldy, "y NULL or not aligned to its elements")) != CERAR_OK)
+        return st;
+    if (tokens == 0 || width == 0) return CERAR_OK;
+    const cerar::EmbedArgs a = {table, vocab, width, ld, ids, id_bytes, tokens, scale, y, ldy, type, y_type, o->d_status};
+    const cudaError_t e = cerar::launch_embed(a, o->num_sms, (cudaStream_t)stream, &o->launches);
+    return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "embed launch");
+}
+
+size_t cerar_embed_grad_workspace(int64_t tokens, int64_t vocab, int64_t width) {
+    if (tokens < 0 || tokens > TOKENS_MAX || vocab < 0 || vocab > SIZE_MAX_ || width < 0 || width > SIZE_MAX_) return 0;
+    return cerar::embed_grad_workspace(tokens, vocab, width);
+}
+
+cerar_status_t cerar_embed_grad(cerar_ops_t* o, const void* dy, cerar_type_t type, int64_t lddy, const void* ids, int id_bytes, int64_t tokens,
+                                float scale, void* dtable, cerar_type_t d_type, int64_t vocab, int64_t width, int64_t ld, int accumulate,
+                                void* workspace, size_t workspace_bytes, cerar_stream_t stream) {
+    cerar_status_t st = check_ops(o);
+    if (st != CERAR_OK) return st;
+    if ((st = check_ids(ids, id_bytes, tokens, vocab, width)) != CERAR_OK ||
+        (st = check_rows(dy, type, tokens, width, lddy, "dy NULL or not aligned to its elements")) != CERAR_OK ||
+        (st = check_rows(dtable, d_type, vocab, width, ld, "dtable NULL or not aligned to its elements")) != CERAR_OK)
+        return st;
+    if (vocab == 0 || width == 0 || (tokens == 0 && accumulate)) return CERAR_OK;
+    const size_t need = cerar::embed_grad_workspace(tokens, vocab, width);
+    if (need > 0 && (!workspace || misaligned(workspace, 16))) return fail(CERAR_ERR_INVALID_ARG, "workspace NULL or not aligned to 16 bytes");
+    if (workspace_bytes < need) return fail(CERAR_ERR_SHAPE, "the workspace is too small");
+    const cerar::EmbedGradArgs a = {dy, lddy, ids, id_bytes, tokens, scale, dtable, vocab, width, ld, type, d_type, accumulate != 0, workspace, o->d_status};
+    const cudaError_t e = cerar::launch_embed_grad(a, (cudaStream_t)stream, &o->launches);
+    return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "embed gradient launch");
+}
+
+cerar_status_t cerar_rotation_table(cerar_ops_t* o, const double* freqs, int pairs, int64_t first, int64_t rows, float* table, cerar_stream_t stream) {
+    cerar_status_t st = check_ops(o);
+    if (st != CERAR_OK) return st;
+    if (pairs < 0 || pairs > CERAR_HEAD_DIM_MAX / 2 || rows < 0 || rows > TOKENS_MAX) return fail(CERAR_ERR_SHAPE, "rotation table: up to 256 pairs and 2^31 - 256 positions");
+    if (pairs == 0 || rows == 0) return CERAR_OK;
+    if (!freqs) return fail(CERAR_ERR_INVALID_ARG, "freqs is NULL");
+    for (int i = 0; i < pairs; ++i)
+        if (!std::isfinite(freqs[i])) return fail(CERAR_ERR_INVALID_ARG, "a frequency is not finite");
+    if (!table || misaligned(table, 8)) return fail(CERAR_ERR_INVALID_ARG, "table NULL or not aligned to 8 bytes");
+    const cudaError_t e = cerar::launch_rotation_table(freqs, pairs, first, rows, table, o->num_sms, (cudaStream_t)stream, &o->launches);
+    return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "rotation table launch");
+}
+
+cerar_status_t cerar_head_norm(cerar_ops_t* o, cerar_type_t type, const cerar_heads_t* parts, int count, cerar_type_t w_type, int64_t tokens, int dim,
+                               float eps, const cerar_rotation_t* rotation, cerar_stream_t stream) {
+    cerar_status_t st = check_ops(o);
+    if (st != CERAR_OK) return st;
+    cerar::HeadNormArgs a = {};
+    if ((st = check_heads(parts, count, type, tokens, dim, false, a)) != CERAR_OK || (st = check_rotation(rotation, dim, a)) != CERAR_OK) return st;
+    if (!type_ok(w_type)) return fail(CERAR_ERR_INVALID_ARG, "unknown element type");
+    for (int i = 0; i < count; ++i)
+        if (misaligned(parts[i].w, type_bytes(w_type))) return fail(CERAR_ERR_INVALID_ARG, "w is not aligned to its elements");
+    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(CERAR_ERR_INVALID_ARG, "eps must be positive and finite");
+    if (tokens == 0) return CERAR_OK;
+    a.eps = eps; a.w_type = w_type; a.status = o->d_status;
+    const cudaError_t e = cerar::launch_head_norm(a, o->num_sms, (cudaStream_t)stream, &o->launches);
+    return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "head norm launch");
+}
+
+size_t cerar_head_norm_grad_workspace(int count, int dim) {
+    if (count < 1 || count > 2 || dim < 2 || dim > CERAR_HEAD_DIM_MAX) return 0;
+    return cerar::head_norm_grad_workspace(count, dim);
+}
+
+cerar_status_t cerar_head_norm_grad(cerar_ops_t* o, cerar_type_t type, const cerar_heads_t* parts, int count, cerar_type_t w_type, cerar_type_t dw_type,
+                                    int accumulate, int64_t tokens, int dim, float eps, const cerar_rotation_t* rotation, void* workspace,
+                                    size_t workspace_bytes, cerar_stream_t stream) {
+    cerar_status_t st = check_ops(o);
+    if (st != CERAR_OK) return st;
+    cerar::HeadNormArgs a = {};
+    if ((st = check_heads(parts, count, type, tokens, dim, true, a)) != CERAR_OK || (st = check_rotation(rotation, dim, a)) != CERAR_OK) return st;
+    if (!type_ok(w_type) || !type_ok(dw_type)) return fail(CERAR_ERR_INVALID_ARG, "unknown element type");
+    for (int i = 0; i < count; ++i)
+        if (misaligned(parts[i].w, type_bytes(w_type)) || misaligned(parts[i].dw, type_bytes(dw_type)))
+            return fail(CERAR_ERR_INVALID_ARG, "w or dw is not aligned to its elements");
+    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(CERAR_ERR_INVALID_ARG, "eps must be positive and finite");
+    const size_t need = cerar::head_norm_grad_workspace(count, dim);
+    if (!workspace || misaligned(workspace, 16)) return fail(CERAR_ERR_INVALID_ARG, "workspace NULL or not aligned to 16 bytes");
+    if (workspace_bytes < need) return fail(CERAR_ERR_SHAPE, "the workspace is too small");
+    a.eps = eps; a.w_type = w_type; a.dw_type = dw_type; a.accumulate = accumulate != 0; a.status = o->d_status;
+    const cudaError_t e = cerar::launch_head_norm_grad(a, workspace, o->num_sms, (cudaStream_t)stream, &o->launches);
+    return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "head norm gradient launch");
+}
+
+}  // extern "C"

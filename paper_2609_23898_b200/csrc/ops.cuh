@@ -1,4 +1,5 @@
-// Launch descriptors of the training-step operators (8-bit products and conversions, gradient norm, AdamW).
+// Launch descriptors of the training-step operators (8-bit products and conversions, gradient norm, AdamW; embedding, head norms,
+// bfloat16 products and the gated block made of them).
 #pragma once
 #include <cuda_runtime.h>
 
@@ -9,6 +10,9 @@
 namespace cerar {
 
 constexpr int FP8_BLOCK = 128;          // values that share a scale
+
+// What kernels leave in a handle's status word.
+enum { STATUS_TIMEOUT = 2, STATUS_BEYOND = 3 };
 
 // Power-of-two scale exponent of the 8-bit format from the bit pattern of a block's largest finite magnitude:
 // the smallest e with amax 2^-e <= 448, within [-100, 100]; 0 for a block of zeros.
@@ -97,5 +101,61 @@ cudaError_t launch_adamw(const AdamwArgs& a, int param_kind, int grad_type, int 
 cudaError_t launch_set_grads(TensorRec* tensors, int64_t first, int count, void* const* grads, cudaStream_t s,
                              uint64_t* launches);
 constexpr int SET_GRADS_MAX = 256;       // pointers per launch
+
+struct EmbedArgs {
+    const void* table;
+    int64_t vocab, width, ld;
+    const void* ids;
+    int id_bytes;
+    int64_t tokens;
+    float scale;
+    void* y;
+    int64_t ldy;
+    int type, y_type;
+    int* status;
+};
+cudaError_t launch_embed(const EmbedArgs& a, int num_sms, cudaStream_t s, uint64_t* launches);
+
+struct EmbedGradArgs {
+    const void* dy;
+    int64_t lddy;
+    const void* ids;
+    int id_bytes;
+    int64_t tokens;
+    float scale;
+    void* dtable;
+    int64_t vocab, width, ld;
+    int type, d_type, accumulate;
+    void* workspace;
+    int* status;
+};
+size_t embed_grad_workspace(int64_t tokens, int64_t vocab, int64_t width);
+cudaError_t launch_embed_grad(const EmbedGradArgs& a, cudaStream_t s, uint64_t* launches);
+
+struct HeadPart {                        // queries or keys
+    const void *x, *dy, *w;              // w: null where all are one
+    void* y;                             // or dx
+    void* dw;
+    int64_t x_token, x_head, dy_token, dy_head, y_token, y_head;
+    int heads;
+};
+struct HeadNormArgs {
+    HeadPart part[2];
+    int count;
+    int64_t tokens, period;              // token t has position number t % period
+    int dim, rotated, neighbours;
+    float eps;
+    const float2* table;                 // [table_rows][rotated / 2]: cosine, sine
+    int64_t table_rows;
+    const void* positions;               // null: the position is the number
+    int position_bytes;
+    int type, w_type, dw_type, accumulate;
+    int* status;
+};
+constexpr int HEAD_NORM_BLOCKS = 1024;   // of each part, at most, in the gradient
+size_t head_norm_grad_workspace(int count, int dim);
+cudaError_t launch_head_norm(const HeadNormArgs& a, int num_sms, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_head_norm_grad(const HeadNormArgs& a, void* workspace, int num_sms, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_rotation_table(const double* freqs, int pairs, int64_t first, int64_t rows, float* table, int num_sms, cudaStream_t s, uint64_t* launches);
 
 }  // namespace cerar

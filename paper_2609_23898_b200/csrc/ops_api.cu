@@ -8,15 +8,14 @@
 
 #include "../../include/cerar.h"
 #include "ops.cuh"
+#include "ops_handle.hpp"
 
-extern "C" void cerar_internal_set_error(const char* msg);    // api.cu: text behind cerar_last_error()
-
-struct cerar_ops {
-    int device = -1;
-    int num_sms = 0;
-    int* d_status = nullptr;
-    uint64_t launches = 0;
-};
+using cerar::check_ops;
+using cerar::cuda_fail;
+using cerar::fail;
+using cerar::misaligned;
+using cerar::type_bytes;
+using cerar::type_ok;
 
 struct cerar_tensors {
     cerar_ops* ops = nullptr;
@@ -36,31 +35,6 @@ struct cerar_tensors {
 };
 
 namespace {
-
-cerar_status_t fail(cerar_status_t s, const char* msg) {
-    cerar_internal_set_error(msg);
-    return s;
-}
-cerar_status_t cuda_fail(cudaError_t e, const char* what) {
-    cudaGetLastError();      // reported here: left where it is, the next check of somebody else's launch would find it
-    try {
-        cerar_internal_set_error((std::string(what) + ": " + cudaGetErrorString(e)).c_str());
-    } catch (...) {
-    }
-    return e == cudaErrorMemoryAllocation ? CERAR_ERR_NOMEM : CERAR_ERR_CUDA;
-}
-cerar_status_t check_ops(const cerar_ops* o) {
-    if (!o) return fail(CERAR_ERR_INVALID_ARG, "ops handle is NULL");
-    int dev = -1;
-    const cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return cuda_fail(e, "current device");
-    if (dev != o->device)
-        return fail(CERAR_ERR_CUDA, "the device the ops handle was created on must be current");
-    return CERAR_OK;
-}
-bool type_ok(int t) { return t == CERAR_TYPE_F32 || t == CERAR_TYPE_BF16; }
-int type_bytes(int t) { return t == CERAR_TYPE_F32 ? 4 : 2; }
-bool misaligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
 
 cerar_status_t check_matrix(const cerar_fp8_matrix_t* m) {
     if (!m) return fail(CERAR_ERR_INVALID_ARG, "8-bit matrix is NULL");
@@ -126,6 +100,7 @@ cerar_status_t cerar_ops_status(cerar_ops_t* o, cerar_stream_t stream) {
     if (e != cudaSuccess) return cuda_fail(e, "status read");
     if (flag == 0) return CERAR_OK;
     cudaMemsetAsync(o->d_status, 0, sizeof(int), (cudaStream_t)stream);
+    if (flag == cerar::STATUS_BEYOND) return fail(CERAR_ERR_BOUNDS, "a token or a position beyond the end of its table");
     return fail(CERAR_ERR_TIMEOUT, "a kernel gave up on a bounded wait");
 }
 

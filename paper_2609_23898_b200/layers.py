@@ -1,0 +1,269 @@
+"""Layers around the linear ones, on torch tensors: what else of a model has weights whose gradients are aggregated.
+
+  embed, embed_backward, Embed              embedding lookup with scaling, and its gradient by sorted tokens (cerar_embed, cerar_embed_grad)
+  rotation_table, head_norm, head_norm_backward, HeadNorm
+                                            norms of queries and keys for each head, with the rotation by position in the same pass
+                                            (cerar_rotation_table, cerar_head_norm, cerar_head_norm_grad)
+
+As with training.Linear8 the gradients of weights are added to buffers of the caller's (slices of the vector that is aggregated) and the
+weights have none of their own.  Everything runs on the current stream of the tensors' device, without synchronisation.
+The formulas and rules stand in include/cerar.h.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import cerar
+from .cerar import lib
+from .training import Ops, _check, _ld, _matrix, _rows, _stream, _type
+
+HALVES, NEIGHBOURS = "halves", "neighbours"
+_IDS = {torch.int32: 4, torch.int64: 8}
+
+
+def _whole(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in _IDS:
+        raise TypeError(f"{what}: int32 or int64 wanted, got {t.dtype}")
+    return _IDS[t.dtype]
+
+
+def _same_device(ops: Ops, **tensors):
+    for what, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{what}: a CUDA tensor is wanted")
+        ops._here(t.device)
+
+
+def _no_gradient(**tensors):
+    for what, t in tensors.items():
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{what} has no gradient of its own (it is added to d{what}): it must not require one")
+
+
+def _anchor(device, wanted: bool):
+    """Where no input is a tensor that autograd follows, an empty one takes that place (see training.Linear8)."""
+    return torch.empty(0, device=device, requires_grad=True) if wanted and torch.is_grad_enabled() else None
+
+
+# ------------------------------------------------------------------------------------------------ embedding
+
+
+def embed(ops: Ops, table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, dtype: torch.dtype | None = None) -> torch.Tensor:
+    """scale * table[ids], of `dtype` (the table's): shape of ids, then the table's width.  An id below zero is padding and gives zeros;
+    one beyond the table does so too, and Ops.status raises."""
+    _same_device(ops, table=table, ids=ids)
+    _matrix(table, "table")
+    kind, size = _type(table, "table"), _whole(ids, "ids")
+    if not ids.is_contiguous():
+        ids = ids.contiguous()
+    vocab, width = table.shape
+    y = torch.empty(*ids.shape, width, dtype=dtype or table.dtype, device=table.device)
+    st = lib.cerar_embed(ops._h, table.data_ptr(), kind, vocab, width, _ld(table), ids.data_ptr(), size, ids.numel(), scale, y.data_ptr(),
+                         _type(y, "dtype"), width, _stream(table.device.index))
+    if st:
+        _check(st)
+    return y
+
+
+def embed_backward(ops: Ops, dy: torch.Tensor, ids: torch.Tensor, dtable: torch.Tensor, *, scale: float = 1.0, accumulate=True):
+    """dtable[v] += scale * the sum of dy over the tokens v (without accumulate: = that, and zeros for tokens that ids has none of).
+    Deterministic."""
+    _same_device(ops, dy=dy, ids=ids, dtable=dtable)
+    _matrix(dtable, "dtable")
+    vocab, width = dtable.shape
+    if dy.dim() < 1 or tuple(dy.shape) != (*ids.shape, width):
+        raise ValueError(f"dy of shape {(*ids.shape, width)} wanted, got {tuple(dy.shape)}")
+    kind, size = _type(dy, "dy"), _whole(ids, "ids")
+    dy = _rows(dy)
+    if not ids.is_contiguous():
+        ids = ids.contiguous()
+    n = ids.numel()
+    need = lib.cerar_embed_grad_workspace(n, vocab, width)
+    ws = torch.empty(need, dtype=torch.uint8, device=dtable.device)
+    st = lib.cerar_embed_grad(ops._h, dy.data_ptr(), kind, _ld(dy) if dy.numel() else width, ids.data_ptr(), size, n, scale, dtable.data_ptr(),
+                              _type(dtable, "dtable"), vocab, width, _ld(dtable) if dtable.numel() else width, accumulate, ws.data_ptr(), need,
+                              _stream(dtable.device.index))
+    if st:
+        _check(st)
+
+
+class Embed(torch.autograd.Function):
+    """embed and embed_backward for torch.autograd: y = Embed.apply(table, ids, ops, dtable, scale).  Every pass backward adds to `dtable`
+    (None: no gradient); second derivatives are refused."""
+
+    @classmethod
+    def apply(cls, table, ids, ops, dtable, scale=1.0):
+        _no_gradient(table=table)
+        return super().apply(table, ids, ops, dtable, scale, _anchor(table.device, dtable is not None))
+
+    @staticmethod
+    def forward(ctx, table, ids, ops, dtable, scale, anchor):
+        ctx.ops, ctx.dtable, ctx.scale = ops, dtable, scale
+        ctx.save_for_backward(ids)
+        return embed(ops, table, ids, scale=scale)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        ids, = ctx.saved_tensors
+        embed_backward(ctx.ops, dy, ids, ctx.dtable, scale=ctx.scale)
+        return None, None, None, None, None, None
+
+
+# ------------------------------------------------------------------------------------------------ head norms
+
+
+def rotation_table(ops: Ops, rows: int, dim: int, *, base: float = 10000.0, freqs=None, first: int = 0) -> torch.Tensor:
+    """Cosine and sine of the angles of positions first .. first + rows - 1, float32 (rows, dim / 2, 2); pair j turns by freqs[j]
+    (base ** (-2 j / dim)) per position.  The angles are worked out in 64 bits."""
+    freqs = [base ** (-2.0 * j / dim) for j in range(dim // 2)] if freqs is None else [float(f) for f in freqs]
+    if dim < 0 or dim % 2 or len(freqs) != dim // 2:
+        raise ValueError("rotation_table: an even dim and dim / 2 frequencies are wanted")
+    table = torch.empty(rows, dim // 2, 2, dtype=torch.float32, device=torch.device("cuda", ops._index))
+    _check(lib.cerar_rotation_table(ops._h, (C.c_double * len(freqs))(*freqs), len(freqs), first, rows, table.data_ptr(), _stream(ops._index)))
+    return table
+
+
+def _heads(t: torch.Tensor, what: str) -> torch.Tensor:
+    """t (..., heads, dim) as (tokens, heads, dim) with a head's values next to one another: a copy only where there is no such view."""
+    if t.dim() < 3:
+        raise ValueError(f"{what}: (tokens, heads, values) or more dimensions are wanted")
+    t = t if t.dim() == 3 else t.flatten(0, -3)
+    return t if t.stride(2) == 1 or t.size(2) < 2 else t.contiguous()
+
+
+def _rotation(table, positions, lead, pairs, dim):
+    if pairs not in (HALVES, NEIGHBOURS):
+        raise ValueError("pairs must be 'halves' or 'neighbours'")
+    period = lead[-1]
+    if positions is not None:
+        size = _whole(positions, "positions")
+        if tuple(positions.shape) != lead and tuple(positions.shape) != lead[-1:]:
+            raise ValueError(f"positions of shape {lead} or {lead[-1:]} wanted, got {tuple(positions.shape)}")
+        if not positions.is_contiguous():
+            positions = positions.contiguous()
+        period = positions.numel()
+    rotated = 0
+    if table is not None:
+        if table.dtype != torch.float32 or table.dim() != 3 or table.size(2) != 2 or not table.is_contiguous():
+            raise ValueError("table: contiguous float32 of shape (positions, pairs, 2) wanted, as rotation_table makes it")
+        rotated = 2 * table.size(1)
+    r = cerar.Rotation(None if table is None else table.data_ptr(), 0 if table is None else table.size(0),
+                       None if positions is None else positions.data_ptr(), max(period, 1), 8 if positions is None else size, rotated, pairs == NEIGHBOURS)
+    return r, positions               # (positions: kept until the call has been made)
+
+
+def _parts(q, k, wq, wk, out, dq=None, dk=None, dwq=None, dwk=None):
+    """The descriptors of a call, its results, and the weights' types."""
+    if out is None:
+        out = (None, None)
+    parts = (cerar.Heads * (1 if k is None else 2))()
+    keep, ys, w_type, dw_type = [], [], None, None
+    for i, (x, w, y, dy, dw) in enumerate(((q, wq, out[0], dq, dwq), (k, wk, out[1], dk, dwk))[:len(parts)]):
+        what = "qk"[i]
+        x3 = _heads(x, what)
+        n, h, d = x3.shape
+        if i and (x.shape[:-2] != q.shape[:-2] or d != q.shape[-1] or x.dtype != q.dtype):
+            raise ValueError("q and k: the same tokens, values per head and type are wanted")
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        elif y.shape != x.shape or y.dtype != x.dtype:
+            raise ValueError("out: tensors of the shapes and type of q and k are wanted")
+        y3 = y if y.dim() == 3 else y.view(n, h, d) if y.is_contiguous() else y.flatten(0, -3)
+        if y3.data_ptr() != y.data_ptr() or (y3.stride(2) != 1 and d > 1):
+            raise ValueError("out: leading dimensions that can be flattened and contiguous heads are wanted")
+        p = parts[i]
+        p.x, p.x_token, p.x_head, p.y, p.y_token, p.y_head, p.heads = x3.data_ptr(), x3.stride(0), x3.stride(1), y3.data_ptr(), y3.stride(0), y3.stride(1), h
+        if w is not None:
+            if w.dim() != 1 or w.numel() != d or not w.is_contiguous():
+                raise ValueError(f"w{what}: {d} contiguous weights wanted")
+            t = _type(w, "w" + what)
+            if w_type is not None and t != w_type:
+                raise TypeError("wq and wk: one type is wanted")
+            p.w, w_type = w.data_ptr(), t
+        if dy is not None:
+            if dy.shape != x.shape or dy.dtype != x.dtype:
+                raise ValueError(f"d{what}: the shape and type of {what} wanted")
+            dy3 = _heads(dy, "d" + what)
+            p.dy, p.dy_token, p.dy_head = dy3.data_ptr(), dy3.stride(0), dy3.stride(1)
+            keep.append(dy3)
+        if dw is not None:
+            if dw.dim() != 1 or dw.numel() != d or not dw.is_contiguous():
+                raise ValueError(f"dw{what}: {d} contiguous values wanted")
+            t = _type(dw, "dw" + what)
+            if dw_type is not None and t != dw_type:
+                raise TypeError("dwq and dwk: one type is wanted")
+            p.dw, dw_type = dw.data_ptr(), t
+        keep += [x3, y3]
+        ys.append(y)
+    return parts, (ys + [None])[:2], w_type or 0, dw_type or 0, keep
+
+
+def head_norm(ops: Ops, q: torch.Tensor, k: torch.Tensor | None, wq, wk, table: torch.Tensor | None, positions: torch.Tensor | None = None, *,
+              eps: float = 1e-6, pairs: str = HALVES, out=None):
+    """Every head of q and k (..., heads, values; k may be None) divided by its root mean square, times wq, wk (None: one), its first values turned
+    by the token's position: those that `table` (rotation_table; None: no rotation) has pairs for.  positions: of every token, or of
+    the last dimension of the tokens, for all sequences alike (None: 0, 1, ...); below zero: padding, whose result is zero; beyond the
+    table: the same, and Ops.status raises.  q and k may be slices of one projection's result.  Returns both (in `out`, if given)."""
+    _same_device(ops, q=q, k=k, wq=wq, wk=wk, table=table, positions=positions)
+    kind = _type(q, "q")
+    parts, ys, w_type, _, keep = _parts(q, k, wq, wk, out)
+    lead = tuple(q.shape[:-2])
+    rot, positions = _rotation(table, positions, lead, pairs, q.shape[-1])
+    st = lib.cerar_head_norm(ops._h, kind, C.addressof(parts), len(parts), w_type, keep[0].size(0), q.shape[-1], eps, C.addressof(rot),
+                             _stream(q.device.index))
+    if st:
+        _check(st)
+    return ys[0], ys[1]
+
+
+def head_norm_backward(ops: Ops, dq: torch.Tensor, dk: torch.Tensor | None, q: torch.Tensor, k: torch.Tensor | None, wq, wk, table, positions=None, *,
+                       dwq=None, dwk=None, accumulate=True, eps: float = 1e-6, pairs: str = HALVES, out=None):
+    """Gradients of q and k (in `out`, if given) from those of head_norm's results; dwq, dwk (float32 or bfloat16, None: not wanted) += those
+    of the weights.  Deterministic."""
+    _same_device(ops, dq=dq, dk=dk, q=q, k=k, wq=wq, wk=wk, table=table, positions=positions, dwq=dwq, dwk=dwk)
+    kind = _type(q, "q")
+    if (dk is None) != (k is None) or (k is None and dwk is not None):
+        raise ValueError("dk and dwk belong to k")
+    parts, ys, w_type, dw_type, keep = _parts(q, k, wq, wk, out, dq, dk, dwq, dwk)
+    lead = tuple(q.shape[:-2])
+    rot, positions = _rotation(table, positions, lead, pairs, q.shape[-1])
+    need = lib.cerar_head_norm_grad_workspace(len(parts), q.shape[-1])
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    st = lib.cerar_head_norm_grad(ops._h, kind, C.addressof(parts), len(parts), w_type, dw_type, accumulate, keep[1].size(0), q.shape[-1], eps,
+                                  C.addressof(rot), ws.data_ptr(), need, _stream(q.device.index))
+    if st:
+        _check(st)
+    return ys[0], ys[1]
+
+
+class HeadNorm(torch.autograd.Function):
+    """head_norm and head_norm_backward for torch.autograd: q, k = HeadNorm.apply(q, k, wq, wk, ops, table, positions, dwq, dwk, eps, pairs).
+    Every pass backward adds to dwq and dwk (None: not wanted); second derivatives are refused."""
+
+    @classmethod
+    def apply(cls, q, k, wq, wk, ops, table, positions=None, dwq=None, dwk=None, eps=1e-6, pairs=HALVES):
+        _no_gradient(wq=wq, wk=wk)
+        followed = q.requires_grad or (k is not None and k.requires_grad)
+        anchor = _anchor(q.device, (dwq is not None or dwk is not None) and not followed)
+        return super().apply(q, k, wq, wk, ops, table, positions, dwq, dwk, eps, pairs, anchor)
+
+    @staticmethod
+    def forward(ctx, q, k, wq, wk, ops, table, positions, dwq, dwk, eps, pairs, anchor):
+        ctx.ops, ctx.dw, ctx.rest = ops, (dwq, dwk), (eps, pairs)
+        ctx.save_for_backward(q, k, wq, wk, table, positions)
+        return head_norm(ops, q, k, wq, wk, table, positions, eps=eps, pairs=pairs)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk):
+        q, k, wq, wk, table, positions = ctx.saved_tensors
+        eps, pairs = ctx.rest
+        dxq, dxk = head_norm_backward(ctx.ops, dq, dk, q, k, wq, wk, table, positions, dwq=ctx.dw[0], dwk=ctx.dw[1], eps=eps, pairs=pairs)
+        need = ctx.needs_input_grad
+        return (dxq if need[0] else None, dxk if need[1] else None) + (None,) * 10
