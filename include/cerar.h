@@ -655,6 +655,39 @@ cerar_status_t cerar_head_norm_grad(cerar_ops_t* ops, cerar_type_t type, const c
 cerar_status_t cerar_rotation_table(cerar_ops_t* ops, const double* freqs, int pairs, int64_t first, int64_t rows, float* table,
                                     cerar_stream_t stream);
 
+/* C (M x N of `type`, ldc elements between rows) = op(A) op(B), or C + op(A) op(B) with accumulate != 0, of bfloat16 matrices; op is the
+ * matrix itself or, with trans_* != 0, its transpose: A is stored as M x K (K x M), B as K x N (N x K).  A and B start on 16-byte boundaries
+ * and their ld (elements between rows) is a multiple of 8: what tensor-map copies need; nothing between columns and ld is used.
+ * Sums run on the tensor cores in accumulators of 24 bits that drop what does not fit, up to 4096 values of k; longer ones are put together
+ * in binary32: |C - exact| <= 2^-23 (264 + K / 4096) sum |A| |B| before the rounding to `type`.  Deterministic. */
+cerar_status_t cerar_matmul_bf16(cerar_ops_t* ops, const void* A, int64_t lda, int trans_a, const void* B, int64_t ldb, int trans_b,
+                                 int64_t M, int64_t N, int64_t K, void* C, cerar_type_t type, int64_t ldc, int accumulate,
+                                 cerar_stream_t stream);
+/* How it runs on a GPU of num_sms SMs, without a device: the columns of its tiles, 128 or 256 (of 128 rows; with 256: of 256 rows, by a pair
+ * of blocks), and in *split the blocks that share the sum of a tile.  -1 for sizes that no product has. */
+int            cerar_matmul_bf16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* split);
+
+/* The two products of a gated feed-forward block that carry its elementwise part.  The block, for x (tokens x width) and bfloat16 weights
+ * w_in (2 hidden x width: the gate's rows, then the other projection's) and w_out (outputs x hidden):
+ *     [g u] = x w_in^T,   h = act(g) u,   y = h w_out^T
+ *     dh = dy w_out,  dg = dh u act'(g),  du = dh act(g),  dx = [dg du] w_in,  dw_in += [dg du]^T x,  dw_out += dy^T h
+ * cerar_gated_in makes h (tokens x hidden) from the binary32 sums and, where gu is not NULL, leaves [g u] (tokens x 2 hidden) rounded to
+ * bfloat16 for the backward pass.  cerar_gated_grad makes [dg du] (tokens x 2 hidden) from dy (tokens x width), w_out (width x hidden) and
+ * gu: dh stays in binary32.  g, u, dg, du and h are bfloat16 in memory, as the operands of the products that follow have to be; each is
+ * rounded once.  x, dy, w: as the operands of cerar_matmul_bf16; the others need alignment to their elements (16-byte rows and
+ * hidden a multiple of 8 are faster). */
+typedef enum {
+    CERAR_ACT_SILU = 0,          /* g / (1 + e^-g)                                                        */
+    CERAR_ACT_GELU = 1,          /* g Phi(g), Phi the normal distribution                                 */
+    CERAR_ACT_GELU_TANH = 2,     /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2                      */
+    CERAR_ACT_RELU = 3           /* max(g, 0); its derivative at 0 is 0                                    */
+} cerar_activation_t;
+cerar_status_t cerar_gated_in(cerar_ops_t* ops, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t tokens, int64_t width,
+                              int64_t hidden, cerar_activation_t act, void* h, int64_t ldh, void* gu, int64_t ldgu, cerar_stream_t stream);
+cerar_status_t cerar_gated_grad(cerar_ops_t* ops, const void* dy, int64_t lddy, const void* w, int64_t ldw, int64_t tokens, int64_t width,
+                                int64_t hidden, cerar_activation_t act, const void* gu, int64_t ldgu, void* dgu, int64_t lddgu,
+                                cerar_stream_t stream);
+
 const char*    cerar_status_string(cerar_status_t s);
 const char*    cerar_last_error(void);   /* thread-local detail of the last failure */
 

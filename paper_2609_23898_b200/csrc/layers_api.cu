@@ -1,4 +1,4 @@
-// C ABI of the layers' operators (embedding, head norms): argument checks, launches.
+// C ABI of the layers' operators (embedding, head norms, bfloat16 products, gated block): argument checks, launches.
 #include <cuda_runtime.h>
 
 #include <cmath>
@@ -76,6 +76,18 @@ cerar_status_t check_rotation(const cerar_rotation_t* r, int dim, cerar::HeadNor
     a.table_rows = r->rotated > 0 ? r->rows : (int64_t)1 << 62;          // (nothing is looked up: any position will do)
     a.positions = r->positions; a.position_bytes = r->position_bytes;
     return CERAR_OK;
+}
+
+// A bfloat16 operand of a product: rows x cols, read by tensor-map copies
+cerar_status_t check_operand(const void* p, int64_t rows, int64_t cols, int64_t ld) {
+    if (rows < 0 || cols < 0 || rows > SIZE_MAX_ || cols > SIZE_MAX_) return fail(CERAR_ERR_SHAPE, "matrix: sizes from 0 to 2^31 - 256 are wanted");
+    if (rows == 0 || cols == 0) return CERAR_OK;
+    if (!p || misaligned(p, 16)) return fail(CERAR_ERR_INVALID_ARG, "matrix: NULL, or not on a 16-byte boundary");
+    if (ld < cols || ld % 8 || ld >= (int64_t)1 << 39) return fail(CERAR_ERR_SHAPE, "matrix: ld must be a multiple of 8, at least the number of columns and below 2^39");
+    return CERAR_OK;
+}
+cerar_status_t check_act(int act) {
+    return act >= CERAR_ACT_SILU && act <= CERAR_ACT_RELU ? CERAR_OK : fail(CERAR_ERR_INVALID_ARG, "unknown activation");
 }
 
 }  // namespace
@@ -171,6 +183,72 @@ cerar_status_t cerar_head_norm_grad(cerar_ops_t* o, cerar_type_t type, const cer
     a.eps = eps; a.w_type = w_type; a.dw_type = dw_type; a.accumulate = accumulate != 0; a.status = o->d_status;
     const cudaError_t e = cerar::launch_head_norm_grad(a, workspace, o->num_sms, (cudaStream_t)stream, &o->launches);
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "head norm gradient launch");
+}
+
+cerar_status_t cerar_matmul_bf16(cerar_ops_t* o, const void* A, int64_t lda, int trans_a, const void* B, int64_t ldb, int trans_b, int64_t M, int64_t N,
+                                 int64_t K, void* C, cerar_type_t type, int64_t ldc, int accumulate, cerar_stream_t stream) {
+    cerar_status_t st = check_ops(o);
+    if (st != CERAR_OK) return st;
+    if ((st = check_operand(A, trans_a ? K : M, trans_a ? M : K, lda)) != CERAR_OK || (st = check_operand(B, trans_b ? N : K, trans_b ? K : N, ldb)) != CERAR_OK ||
+        (st = check_rows(C, type, M, N, ldc, "C NULL or not aligned to its elements")) != CERAR_OK)
+        return st;
+    if (M == 0 || N == 0) return CERAR_OK;
+    cudaError_t e = cudaSuccess;
+    if (K == 0) {                         // an empty sum
+        if (!accumulate)
+            e = cudaMemset2DAsync(C, (size_t)(M > 1 ? ldc : N) * type_bytes(type), 0, (size_t)N * type_bytes(type), (size_t)M, (cudaStream_t)stream);
+    } else {
+        const cerar::Matmul16Args a = {A, B, lda, ldb, trans_a != 0, trans_b != 0, M, N, K, C, ldc, type, accumulate != 0, o->d_status};
+        e = cerar::launch_matmul16(a, o->num_sms, (cudaStream_t)stream, &o->launches);
+    }
+    return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "bfloat16 matmul launch");
+}
+
+int cerar_matmul_bf16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* split) {
+    if (M < 1 || N < 1 || K < 1 || M > SIZE_MAX_ || N > SIZE_MAX_ || K > SIZE_MAX_ || num_sms < 1 || !split) return -1;
+    return cerar::matmul16_tile(M, N, K, num_sms, split);
+}
+
+cerar_status_t cerar_gated_in(cerar_ops_t* o, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t tokens, int64_t width, int64_t hidden,
+                              cerar_activation_t act, void* h, int64_t ldh, void* gu, int64_t ldgu, cerar_stream_t stream) {
+    cerar_status_t st = check_ops(o);
+    if (st != CERAR_OK) return st;
+    if (hidden < 0 || hidden > SIZE_MAX_ / 2) return fail(CERAR_ERR_SHAPE, "gated: hidden must be from 0 to 2^30 - 128");
+    if ((st = check_act(act)) != CERAR_OK || (st = check_operand(x, tokens, width, ldx)) != CERAR_OK || (st = check_operand(w, 2 * hidden, width, ldw)) != CERAR_OK ||
+        (st = check_rows(h, CERAR_TYPE_BF16, tokens, hidden, ldh, "h NULL or not aligned to its elements")) != CERAR_OK ||
+        (gu && (st = check_rows(gu, CERAR_TYPE_BF16, tokens, 2 * hidden, ldgu, "gu not aligned to its elements")) != CERAR_OK))
+        return st;
+    if (tokens == 0 || hidden == 0) return CERAR_OK;
+    cudaError_t e = cudaSuccess;
+    if (width == 0) {                     // empty sums: g = u = 0, and act(0) 0 = 0
+        e = cudaMemset2DAsync(h, (size_t)(tokens > 1 ? ldh : hidden) * 2, 0, (size_t)hidden * 2, (size_t)tokens, (cudaStream_t)stream);
+        if (e == cudaSuccess && gu)
+            e = cudaMemset2DAsync(gu, (size_t)(tokens > 1 ? ldgu : 2 * hidden) * 2, 0, (size_t)hidden * 4, (size_t)tokens, (cudaStream_t)stream);
+    } else {
+        const cerar::GatedInArgs a = {x, w, ldx, ldw, tokens, width, hidden, act, h, gu, ldh, ldgu, o->d_status};
+        e = cerar::launch_gated_in(a, o->num_sms, (cudaStream_t)stream, &o->launches);
+    }
+    return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "gated block launch");
+}
+
+cerar_status_t cerar_gated_grad(cerar_ops_t* o, const void* dy, int64_t lddy, const void* w, int64_t ldw, int64_t tokens, int64_t width, int64_t hidden,
+                                cerar_activation_t act, const void* gu, int64_t ldgu, void* dgu, int64_t lddgu, cerar_stream_t stream) {
+    cerar_status_t st = check_ops(o);
+    if (st != CERAR_OK) return st;
+    if (hidden < 0 || hidden > SIZE_MAX_ / 2) return fail(CERAR_ERR_SHAPE, "gated: hidden must be from 0 to 2^30 - 128");
+    if ((st = check_act(act)) != CERAR_OK || (st = check_operand(dy, tokens, width, lddy)) != CERAR_OK || (st = check_operand(w, width, hidden, ldw)) != CERAR_OK ||
+        (st = check_rows(gu, CERAR_TYPE_BF16, tokens, 2 * hidden, ldgu, "gu NULL or not aligned to its elements")) != CERAR_OK ||
+        (st = check_rows(dgu, CERAR_TYPE_BF16, tokens, 2 * hidden, lddgu, "dgu NULL or not aligned to its elements")) != CERAR_OK)
+        return st;
+    if (tokens == 0 || hidden == 0) return CERAR_OK;
+    cudaError_t e = cudaSuccess;
+    if (width == 0) {                     // dh = 0
+        e = cudaMemset2DAsync(dgu, (size_t)(tokens > 1 ? lddgu : 2 * hidden) * 2, 0, (size_t)hidden * 4, (size_t)tokens, (cudaStream_t)stream);
+    } else {
+        const cerar::GatedGradArgs a = {dy, w, gu, lddy, ldw, ldgu, tokens, width, hidden, act, dgu, lddgu, o->d_status};
+        e = cerar::launch_gated_grad(a, o->num_sms, (cudaStream_t)stream, &o->launches);
+    }
+    return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "gated block gradient launch");
 }
 
 }  // extern "C"

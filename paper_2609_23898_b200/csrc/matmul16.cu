@@ -1,0 +1,634 @@
+// Products of bfloat16 matrices on the tensor cores, and the two of a gated feed-forward block that carry its elementwise part
+// (cerar_matmul_bf16, cerar_gated_in, cerar_gated_grad; sm_100a: TMA + tcgen05 + TMEM).
+//
+//   plain   C (+)= op(A) op(B)
+//   gate    [g u] = x W^T in one accumulator, h = act(g) u: a tile holds the same columns of both projections side by side
+//   grad    dh = dy W_out in the accumulator, dg = dh u act'(g) and du = dh act(g) from the kept g and u
+//
+// A tile of C is 256 x 256 by a pair of blocks (cta_group::2, each with its 128 rows of A and half of B), or 128 x 128 by one.  At 256 x 256
+// a k of 64 costs the tensor cores 256 clk and each block 32 KB of shared memory written and read; two accumulators fill tensor memory, so
+// that a tile is written while the next one's products run.  Operands are read in place whichever of their dimensions is contiguous.
+//
+//   warp 0     producer: TMA loads of the stages (64 values of k: rows of 128 bytes in the 128-byte swizzle)
+//   warp 1     issues the products; owns the tensor memory
+//   warps 4-11 take the sums out (32 lanes of tensor memory, half of the tile's columns each), finish them in binary32 and write
+// (Warps 2, 3 complete the warpgroup that hands most of its registers to the others.)
+//
+// The accumulator drops what does not fit its 24 bits instead of rounding, an error that grows with the number of additions, so sums of more than
+// SEGMENT blocks of k are put together in registers.
+// Few tiles, long sums: a cluster of S blocks shares a tile, each sums 1/S of the blocks of k, and the partial tiles are added through
+// distributed shared memory, in a fixed order.
+// Every wait is bounded; one that runs out sets the status word and the block leaves through the common exit.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+
+#include "kernels.cuh"
+#include "mma_tile.cuh"
+#include "ops.cuh"
+
+namespace cerar {
+namespace {
+
+using namespace mma;
+typedef __nv_bfloat16 bf16;
+
+constexpr int BK = 64;                                  // values of k in a stage: rows of 128 bytes
+constexpr int UK = 16;                                  // of one product
+constexpr int WARP_EPI0 = 4, THREADS = 32 * (WARP_EPI0 + EPI_WARPS), MAX_SPLIT = 8;
+// registers per thread: 128 x 56 + 256 x 224 = 384 x 168, what the block is launched with
+constexpr int REGS_FEW = 56, REGS_MANY = 224;
+constexpr uint32_t A_BYTES = BM * BK * 2, PART = 64 * BK * 2;      // an operand lies in parts of 64 of its own rows or columns
+constexpr int SEGMENT = 64;
+
+enum { PLAIN = 0, GATE = 1, GRAD = 2 };
+
+struct Params {
+    void* C;                                           // PLAIN: C; GATE: h; GRAD: [dg du]
+    int64_t ldc;
+    bf16* keep;                                        // GATE: where [g u] go, or null
+    const bf16* gu;                                    // GRAD: [g u]
+    int64_t ldgu;
+    int M, N, kblocks;                                 // N: columns of C (GATE, GRAD: of h)
+    int tiles_m, tiles_n, group_m;
+    uint32_t tiles;
+    int a_mn, b_mn;                                    // 1: the operand's own dimension (m or n) is the contiguous one
+    int accumulate, c_vec, c_pair;                     // rows of C start on 16-byte, on 4-byte boundaries
+    int gu_vec, four;                                  // GATE: rows of g and of u on 16-byte boundaries; GRAD: g, u, dg and du on 8-byte ones
+    int act;
+    int stages, split;
+    uint32_t a_bytes;                                  // what a load of A brings (few rows: those only; the others' sums are made of
+                                                       // whatever lies there, row by row, and not stored)
+    int early;                                         // 1: the next kernel of the stream may set itself up meanwhile
+    int* status;
+};
+
+template <int CG>
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (CG == 1)
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                     " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                     " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// ---------------------------------------------------------------- activations (binary32; the exponential and the quotient are the
+// hardware's, some 2^-21 of themselves off, far below the step of a bfloat16 result)
+
+template <int ACT> struct Act;
+template <> struct Act<CERAR_ACT_SILU> {
+    static __device__ __forceinline__ float value(float g) { return __fdividef(g, 1.f + __expf(-g)); }
+    static __device__ __forceinline__ void both(float g, float& a, float& d) {
+        const float s = __fdividef(1.f, 1.f + __expf(-g));
+        a = g * s;
+        d = fmaf(a, 1.f - s, s);
+    }
+};
+template <> struct Act<CERAR_ACT_GELU> {               // g Phi(g); Phi from the error function, its complement where that is small
+    static __device__ __forceinline__ float phi(float g) { return g < -1.f ? 0.5f * erfcf(-0.70710678f * g) : fmaf(0.5f, erff(0.70710678f * g), 0.5f); }
+    static __device__ __forceinline__ float value(float g) { return g * phi(g); }
+    static __device__ __forceinline__ void both(float g, float& a, float& d) {
+        const float c = phi(g);
+        a = g * c;
+        d = fmaf(g * 0.39894228f, __expf(-0.5f * g * g), c);
+    }
+};
+template <> struct Act<CERAR_ACT_GELU_TANH> {          // g / (1 + e^-2v) with v = sqrt(2 / pi) (g + 0.044715 g^3): (1 + tanh v) / 2 is that quotient
+    static __device__ __forceinline__ float part(float g) { return __fdividef(1.f, 1.f + __expf(-1.5957691f * g * fmaf(0.044715f, g * g, 1.f))); }
+    static __device__ __forceinline__ float value(float g) { return g * part(g); }
+    static __device__ __forceinline__ void both(float g, float& a, float& d) {
+        const float s = part(g);
+        a = g * s;
+        d = fmaf(a * (1.f - s), 1.5957691f * fmaf(0.134145f, g * g, 1.f), s);
+    }
+};
+template <> struct Act<CERAR_ACT_RELU> {
+    static __device__ __forceinline__ float value(float g) { return g > 0.f ? g : g != g ? g : 0.f; }
+    static __device__ __forceinline__ void both(float g, float& a, float& d) {
+        a = value(g);
+        d = g > 0.f ? 1.f : 0.f;
+    }
+};
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    if (act == CERAR_ACT_SILU) f(Act<CERAR_ACT_SILU>());
+    else if (act == CERAR_ACT_GELU) f(Act<CERAR_ACT_GELU>());
+    else if (act == CERAR_ACT_GELU_TANH) f(Act<CERAR_ACT_GELU_TANH>());
+    else f(Act<CERAR_ACT_RELU>());
+}
+
+// ---------------------------------------------------------------- writing
+
+// Rows row0 .. row0 + 31 (those below M) and columns col0 .. col0 + W - 1 (those below N) of a bfloat16 matrix; the warp holds row (lane)'s values.
+template <int W>
+__device__ __forceinline__ void write_rows(uint32_t staging, bf16* c, int64_t ld, int M, int N, int row0, int col0, const float* v, bool vec) {
+    const int lane = threadIdx.x & 31;
+    const int nrows = M - row0 < 32 ? M - row0 : 32, n = N - col0 < W ? N - col0 : W;
+    if (nrows <= 0 || n <= 0) return;
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < W / 8; ++j) {
+        const uint4 q = Out<bf16>::pack(v + j * 8);
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
+    }
+    __syncwarp();
+    if (vec) {
+        constexpr int PER_ROW = W / 8, ROWS = 32 / PER_ROW;
+        const int j = lane % PER_ROW;
+#pragma unroll
+        for (int it = 0; it < 32 / ROWS; ++it) {
+            const int r = it * ROWS + lane / PER_ROW;
+            uint4 q;
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
+            if (r >= nrows) continue;
+            bf16* dst = c + (int64_t)(row0 + r) * ld + col0 + j * 8;
+            if (8 * j + 8 <= n) {
+                *reinterpret_cast<uint4*>(dst) = q;
+            } else {
+                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (8 * j + e < n) reinterpret_cast<unsigned short*>(dst)[e] = (unsigned short)(e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xFFFFu);
+            }
+        }
+    } else {
+        for (int r = 0; r < nrows; ++r)
+            for (int e = lane; e < n; e += 32) {
+                uint16_t q;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(q) : "r"(staging + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2) : "memory");
+                *reinterpret_cast<uint16_t*>(c + (int64_t)(row0 + r) * ld + col0 + e) = q;
+            }
+    }
+}
+
+// Four columns of a row in the gate's epilogues, `n` of them there.
+__device__ __forceinline__ uint2 load4(const bf16* p, int n, bool vec) {
+    if (vec && n >= 4) return __ldg(reinterpret_cast<const uint2*>(p));
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = e < n ? __ldg(reinterpret_cast<const unsigned short*>(p) + e) : 0u;
+    return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+}
+__device__ __forceinline__ float element(uint2 q, int e) {
+    const uint32_t w = e < 2 ? q.x : q.y;
+    return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
+}
+__device__ __forceinline__ void store4(bf16* p, int n, bool vec, const float* v) {
+    if (vec && n >= 4) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(Out<bf16>::two(v[0], v[1]), Out<bf16>::two(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n) p[e] = __float2bfloat16_rn(v[e]);
+    }
+}
+// dg and du of four columns from dh and the kept g and u
+__device__ __forceinline__ void write_grad4(const Params& p, int row, int col, const float* dh, uint2 g, uint2 u) {
+    const int n = p.N - col;
+    if (n <= 0) return;
+    float dg[4], du[4];
+    with_act(p.act, [&](auto act) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float a, d;
+            act.both(element(g, e), a, d);
+            dg[e] = dh[e] * element(u, e) * d;
+            du[e] = dh[e] * a;
+        }
+    });
+    bf16* c = static_cast<bf16*>(p.C) + (int64_t)row * p.ldc + col;
+    store4(c, n, p.four, dg);
+    store4(c + p.N, n, p.four, du);
+}
+
+// The whole tile's sums of this warp: rows row0 .. row0 + 31, CW columns, in registers.
+template <int KIND, int BN, typename C>
+__device__ __forceinline__ void write_tile(const Params& p, uint32_t staging, int row0, int tn, int half, float* acc) {
+    constexpr int CW = BN / 2;
+    const int lane = threadIdx.x & 31;
+    if constexpr (KIND == PLAIN) {
+        constexpr int SLAB = 8 * Out<C>::PER16;
+#pragma unroll
+        for (int c = 0; c < CW / SLAB; ++c) write_slab<C>(p, staging, row0, tn * BN + half * CW + c * SLAB, acc + c * SLAB);
+    } else if constexpr (KIND == GATE) {
+        constexpr int FW = BN / 4;                      // columns of h: acc holds their g, then their u
+        const int col0 = tn * (BN / 2) + half * FW;
+        if (p.keep) {
+            write_rows<FW>(staging, p.keep, p.ldgu, p.M, p.N, row0, col0, acc, p.gu_vec);
+            write_rows<FW>(staging, p.keep + p.N, p.ldgu, p.M, p.N, row0, col0, acc + FW, p.gu_vec);
+        }
+        with_act(p.act, [&](auto act) {
+#pragma unroll
+            for (int j = 0; j < FW; ++j) acc[j] = act.value(acc[j]) * acc[FW + j];
+        });
+        write_rows<FW>(staging, static_cast<bf16*>(p.C), p.ldc, p.M, p.N, row0, col0, acc, p.c_vec);
+    } else {
+        // dh through the staging rows, 32 columns at a time, so that a row's g, u, dg and du are touched in pieces of 64 bytes
+        const int nrows = p.M - row0 < 32 ? p.M - row0 : 32;
+        if (nrows <= 0) return;
+#pragma unroll
+        for (int h = 0; h < CW / 32; ++h) {
+            const int col = tn * BN + half * CW + h * 32 + (lane & 7) * 4;
+            uint2 g[8], u[8];
+#pragma unroll
+            for (int it = 0; it < 8; ++it) {
+                const int r = it * 4 + (lane >> 3);
+                const int n = r < nrows ? p.N - col : 0;
+                const bf16* at = p.gu + (int64_t)(row0 + r) * p.ldgu + col;
+                g[it] = load4(at, n, p.four);
+                u[it] = load4(at + p.N, n, p.four);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((j ^ (lane & 7)) << 4)), "f"(acc[h * 32 + 4 * j]), "f"(acc[h * 32 + 4 * j + 1]),
+                             "f"(acc[h * 32 + 4 * j + 2]), "f"(acc[h * 32 + 4 * j + 3]) : "memory");
+            __syncwarp();
+#pragma unroll
+            for (int it = 0; it < 8; ++it) {
+                const int r = it * 4 + (lane >> 3), j = lane & 7;
+                float dh[4];
+                asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(dh[0]), "=f"(dh[1]), "=f"(dh[2]), "=f"(dh[3]) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
+                if (r < nrows) write_grad4(p, row0 + r, col, dh, g[it], u[it]);
+            }
+        }
+    }
+}
+
+// A tile whose sum is split over a cluster: every block leaves the rows of its partial tile that exist in its stages (free by then), row
+// r at r * BN floats, 16-byte pieces exchanged by the row so that lanes do not meet in a bank ...
+template <int BN>
+__device__ __forceinline__ void store_partial(uint32_t smem, int rows, int row, int col, int n, const float* v) {
+    if (row >= rows) return;
+    const uint32_t base = smem + (uint32_t)row * (BN * 4u);
+#pragma unroll
+    for (int j = 0; j < n / 4; ++j)
+        asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + ((uint32_t)((col / 4 + j) ^ (row & 7)) << 4)), "f"(v[4 * j]), "f"(v[4 * j + 1]),
+                     "f"(v[4 * j + 2]), "f"(v[4 * j + 3]) : "memory");
+}
+__device__ __forceinline__ float4 add_piece(const Params& p, uint32_t at) {
+    float4 w[MAX_SPLIT];
+#pragma unroll
+    for (int q = 0; q < MAX_SPLIT; ++q)
+        if (q < p.split) w[q] = ld_cluster4(at, q);
+    float4 v = w[0];
+#pragma unroll
+    for (int q = 1; q < MAX_SPLIT; ++q)
+        if (q < p.split) { v.x += w[q].x; v.y += w[q].y; v.z += w[q].z; v.w += w[q].w; }
+    return v;
+}
+// ... and adds every split-th run of 32 pieces (a warp's) of all partial tiles, in the order of their blocks of k.
+template <int KIND, int BN, typename C>
+__device__ __forceinline__ void add_partials(const Params& p, uint32_t smem, int tm, int tn, int rows, int rank, int thread) {
+    constexpr int PER_ROW = KIND == GATE ? BN / 8 : BN / 4;
+    const int pieces = rows * PER_ROW;
+    for (int run = (thread >> 5) * p.split + rank; run * 32 < pieces; run += EPI_WARPS * p.split) {
+        const int i = run * 32 + (thread & 31);
+        if (i >= pieces) continue;
+        const int r = i / PER_ROW, j = i % PER_ROW, row = tm * BM + r;
+        const uint32_t base = smem + (uint32_t)r * (BN * 4u);
+        const float4 v4 = add_piece(p, base + ((uint32_t)(j ^ (r & 7)) << 4));
+        const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+        const int col = tn * (PER_ROW * 4) + 4 * j, n = p.N - col;
+        if constexpr (KIND == PLAIN) {
+            C* dst = static_cast<C*>(p.C) + (int64_t)row * p.ldc + col;
+            if (p.c_vec && !p.accumulate && n >= 4) {
+                if constexpr (sizeof(C) == 4) *reinterpret_cast<float4*>(dst) = v4;
+                else *reinterpret_cast<uint2*>(dst) = make_uint2(Out<C>::two(v[0], v[1]), Out<C>::two(v[2], v[3]));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < n) dst[e] = (C)(p.accumulate ? (float)dst[e] + v[e] : v[e]);
+            }
+        } else if constexpr (KIND == GATE) {
+            // a warp's 32 columns of g are followed by the same ones of u
+            const float4 u4 = add_piece(p, base + ((uint32_t)((j + PER_ROW) ^ (r & 7)) << 4));
+            const float u[4] = {u4.x, u4.y, u4.z, u4.w};
+            if (p.keep) {
+                bf16* at = p.keep + (int64_t)row * p.ldgu + col;
+                store4(at, n, p.gu_vec, v);
+                store4(at + p.N, n, p.gu_vec, u);
+            }
+            float h[4];
+            with_act(p.act, [&](auto act) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = act.value(v[e]) * u[e];
+            });
+            store4(static_cast<bf16*>(p.C) + (int64_t)row * p.ldc + col, n, p.c_vec, h);
+        } else {
+            const bf16* at = p.gu + (int64_t)row * p.ldgu + col;
+            const uint2 g = load4(at, n, p.four), u = load4(at + p.N, n, p.four);
+            write_grad4(p, row, col, v, g, u);
+        }
+    }
+}
+
+template <int CG, int BN, int KIND, typename C>
+__global__ void __launch_bounds__(THREADS, 1)
+matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Params p) {
+    constexpr int CW = BN / 2;                           // columns of the accumulator per writing warp
+    constexpr int B_ROWS = BN / CG;                      // of the tile of B, in this block
+    constexpr uint32_t STAGE = A_BYTES + B_ROWS * BK * 2;
+    extern __shared__ unsigned char smem_dyn[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    const uint32_t staging0 = smem + (uint32_t)p.stages * STAGE;
+    const uint32_t bars = staging0 + EPI_WARPS * STAGING;
+    const uint32_t full = bars, empty = full + 8u * p.stages, acc_full = empty + 8u * p.stages, acc_empty = acc_full + 16u, slot = acc_empty + 16u;
+
+    if (threadIdx.x == 0) {
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+        for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8u * s, 1); mbar_init(empty + 8u * s, 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(acc_full + 8u * b, 1); mbar_init(acc_empty + 8u * b, CG * EPI_WARPS); }
+        mbar_init_fence();
+    }
+    if (warp == 1) {
+        if constexpr (CG == 1) {
+            tc_alloc(slot, 512u);
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(512u) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();               // the other block's barriers are there before anything is sent to them
+    tc_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    if (p.early) grid_dependents_may_launch();
+    grid_dependency_wait();
+
+    // a cluster is a pair of blocks that share a tile of 256 rows (CG = 2), or `split` blocks that share the sum of a tile
+    const int crank = CG == 2 || p.split > 1 ? (int)cluster_rank() : 0;
+    const int pair_rank = CG == 2 ? crank : 0, rank = CG == 2 ? 0 : crank;
+    const uint32_t csize = CG == 2 ? 2 : p.split;
+    const uint32_t t0 = blockIdx.x / csize, tstep = gridDim.x / csize;
+    const int kb0 = (int)((int64_t)p.kblocks * rank / p.split), kb1 = (int)((int64_t)p.kblocks * (rank + 1) / p.split);
+    bool failed = false;
+
+    if (warp < WARP_EPI0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
+        if (warp == 0) {
+            if (lane == 0) {
+                uint32_t s = 0, ph = 1;
+                for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
+                    int tm, tn;
+                    tile_of(p, t, tm, tn);
+                    const int m0 = (tm * CG + pair_rank) * BM;
+                    // first row or column of every part of 64 of B: GATE takes its first half from g's weights, its second from u's
+                    int n0 = tn * BN + pair_rank * B_ROWS, n1 = n0 + 64;
+                    if constexpr (KIND == GATE) {
+                        n0 = tn * (BN / 2) + pair_rank * p.N;
+                        n1 = CG == 2 ? n0 + 64 : n0 + p.N;
+                    }
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        if (!wait_soon(empty + 8u * s, ph)) { failed = true; break; }
+                        const uint32_t a = smem + s * STAGE, b = a + A_BYTES;
+                        if (pair_rank == 0) mbar_arrive_expect_tx(full + 8u * s, CG * (p.a_bytes + B_ROWS * BK * 2));       // what both blocks load
+                        const uint32_t bar = CG == 1 ? full + 8u * s : in_block(full + 8u * s, 0);
+                        if (p.a_mn) {
+                            tma_load_operand<CG>(a, &map_a, m0, kb * BK, bar);
+                            tma_load_operand<CG>(a + PART, &map_a, m0 + 64, kb * BK, bar);
+                        } else {
+                            tma_load_operand<CG>(a, &map_a, kb * BK, m0, bar);
+                        }
+                        if (p.b_mn) {
+                            tma_load_operand<CG>(b, &map_b, n0, kb * BK, bar);
+                            tma_load_operand<CG>(b + PART, &map_b, n1, kb * BK, bar);
+                        } else {
+                            tma_load_operand<CG>(b, &map_b, kb * BK, n0, bar);
+                            tma_load_operand<CG>(b + PART, &map_b, kb * BK, n1, bar);
+                        }
+                        if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+                    }
+                }
+            }
+        } else if (warp == 1) {
+            if (pair_rank == 0) {
+                // The whole warp goes through the loop and one lane issues: what the products are made from then stays in uniform registers.
+                const uint32_t one = elect_one();
+                // D binary32, A and B bfloat16, M = 128 CG, N = BN
+                const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) |
+                                       ((uint32_t)(CG * BM >> 4) << 24);
+                // 16 values of k further: 32 bytes in a row of k, or 16 rows of 128 bytes
+                const uint64_t a_step = p.a_mn ? (UK * 128u) >> 4 : (UK * 2u) >> 4, b_step = p.b_mn ? (UK * 128u) >> 4 : (UK * 2u) >> 4;
+                const uint64_t desc0 = swizzled_desc(smem, PART);
+                uint32_t s = 0, ph = 0, seg = 0;
+                for (uint32_t t = t0; t < p.tiles && !failed; t += tstep)
+                    for (int k0 = kb0; k0 < kb1 && !failed; k0 += SEGMENT, ++seg) {
+                        const uint32_t buf = seg & 1u, d = tmem + buf * 256u;
+                        if (!warp_wait_soon(acc_empty + 8u * buf, ((seg >> 1) & 1u) ^ 1u)) { failed = true; break; }
+                        const int k1 = k0 + SEGMENT < kb1 ? k0 + SEGMENT : kb1;
+                        for (int kb = k0; kb < k1; ++kb) {
+                            if (!warp_wait_soon(full + 8u * s, ph)) { failed = true; break; }
+                            tc_fence_after();
+                            const uint64_t da = desc0 + (uint64_t)(s * (STAGE >> 4)), db = da + (A_BYTES >> 4);
+                            if (one) {
+#pragma unroll
+                                for (int k = 0; k < BK / UK; ++k) mma_bf16<CG>(d, da + k * a_step, db + k * b_step, idesc, kb != k0 || k != 0);
+                                commit<CG>(empty + 8u * s);
+                                if (kb + 1 == k1) commit<CG>(acc_full + 8u * buf);
+                            }
+                            __syncwarp();
+                            if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
+                        }
+                    }
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY));
+        const int quad = warp & 3, half = (warp - WARP_EPI0) >> 2;
+        const uint32_t staging = staging0 + (uint32_t)(warp - WARP_EPI0) * STAGING;
+        const uint32_t freed = CG == 1 ? acc_empty : in_block(acc_empty, 0);
+        uint32_t seg = 0;
+        for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
+            int tm, tn;
+            tile_of(p, t, tm, tn);
+            float acc[CW];
+            for (int k0 = kb0; k0 < kb1; k0 += SEGMENT, ++seg) {
+                const uint32_t buf = seg & 1u;
+                if (!warp_wait_soon(acc_full + 8u * buf, (seg >> 1) & 1u)) { failed = true; break; }
+                tc_fence_after();
+                const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + buf * 256u;
+#pragma unroll
+                for (int c = 0; c < CW / 32; ++c) {
+                    // GATE: this warp's columns of g, then the same ones of u
+                    const uint32_t col = KIND != GATE ? half * CW + c * 32 : c * 32 < CW / 2 ? half * (CW / 2) + c * 32 : CW + half * (CW / 2) + c * 32 - CW / 2;
+                    uint32_t v[32];
+                    ld32_start(from + col, v);
+                    ld32_done(v);
+                    if (c == CW / 32 - 1) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive<CG>(freed + 8u * buf);
+                    }
+                    if (k0 == kb0) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) acc[c * 32 + j] = __uint_as_float(v[j]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) acc[c * 32 + j] += __uint_as_float(v[j]);
+                    }
+                }
+            }
+            if (failed) break;
+            if (CG == 2 || p.split == 1) {
+                write_tile<KIND, BN, C>(p, staging, (tm * CG + pair_rank) * BM + quad * 32, tn, half, acc);
+                __syncwarp();
+            } else if constexpr (KIND == GATE) {
+                store_partial<BN>(smem, p.M - tm * BM, quad * 32 + lane, half * (CW / 2), CW / 2, acc);
+                store_partial<BN>(smem, p.M - tm * BM, quad * 32 + lane, CW + half * (CW / 2), CW / 2, acc + CW / 2);
+            } else {
+                store_partial<BN>(smem, p.M - tm * BM, quad * 32 + lane, half * CW, CW, acc);
+            }
+        }
+    }
+    __syncwarp();
+    if (CG == 1 && p.split > 1) {
+        cluster_sync();
+        if (warp >= WARP_EPI0) {
+            int tm, tn;                                  // (one tile per cluster)
+            tile_of(p, t0, tm, tn);
+            add_partials<KIND, BN, C>(p, smem, tm, tn, p.M - tm * BM < BM ? p.M - tm * BM : BM, rank, threadIdx.x - 32 * WARP_EPI0);
+        }
+        __syncwarp();
+        cluster_sync();                                  // no block leaves while another reads its part
+    }
+    if constexpr (CG == 2) {
+        tc_fence_before();
+        cluster_sync();                                  // nothing is sent to a block that has left
+        tc_fence_after();
+    }
+    leave<CG>(p, failed, warp, lane, tmem);
+}
+
+bool make_map_16bit(CUtensorMap* m, const void* x, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+    const cuuint64_t dim[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {(cuuint32_t)BK, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(x), dim, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+typedef void (*Kernel)(CUtensorMap, CUtensorMap, Params);
+constexpr int MAX_SMEM = 232448, KERNELS = 8;
+constexpr int STAGES = 6;
+
+cudaError_t launch_one(Kernel kern, int which, int cluster, const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, int grid, cudaStream_t s) {
+    const size_t smem = 1024 + (size_t)p.stages * (2 * A_BYTES) + EPI_WARPS * STAGING + 512;
+    // Once per kernel and device (a call costs the host more than the rest of this function): every launch is allowed the most.
+    static std::atomic<uint64_t> allowed[KERNELS];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (!(allowed[which].load(std::memory_order_relaxed) & bit)) {
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
+        if (e != cudaSuccess) return e;
+        allowed[which].fetch_or(bit, std::memory_order_relaxed);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = g_tune_pdl_off ? 0 : 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {(unsigned)cluster, 1, 1};
+    cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, ma, mb, p);
+}
+
+// Tile and split, from a model of the time (ns): a block of k in a tile of 256 x 256 by a pair of blocks and in one of 128 x 128, a tile's end,
+// the adding up of partial tiles.
+struct Shape { bool wide; int split; };
+Shape choose_shape(int M, int N, int kblocks, int num_sms) {
+    const int64_t m = (M + BM - 1) / BM, n = (N + 127) / 128, narrow = m * n;
+    const int64_t wide = ((m + 1) / 2) * ((n + 1) / 2), wide_slots = num_sms / 2;
+    Shape best{true, 1};
+    int64_t cost = ((wide + wide_slots - 1) / wide_slots) * ((int64_t)kblocks * 165 + 1600);
+    for (int q = 1; q <= MAX_SPLIT && q <= kblocks; ++q) {
+        // (clusters do not fill the GPU's groups of SMs: 128 blocks in clusters of 8 take two turns)
+        if (q > 1 && narrow * q * 100 > (int64_t)num_sms * (q == 2 ? 100 : q <= 4 ? 82 : 65)) continue;
+        const int64_t waves = q > 1 ? 1 : (narrow + num_sms - 1) / num_sms;
+        const int64_t c = waves * ((int64_t)((kblocks + q - 1) / q) * 150 + 800) + (q > 1 ? 800 + 2000 * (M < BM ? M : BM) / BM : 0);
+        if (c < cost) { cost = c; best = {false, q}; }
+    }
+    return best;
+}
+
+bool on(const void* p, int64_t ld, int64_t bytes, int64_t size) { return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * size % bytes == 0; }
+
+// p: the output's part is filled in.  N: columns of the accumulators all tiles together (GATE: twice those of h).
+cudaError_t launch(Params p, int kind, int type, const void* A, int64_t lda, bool trans_a, const void* B, int64_t ldb, bool trans_b, int64_t M, int64_t N, int64_t K,
+                   int* status, int num_sms, cudaStream_t s, uint64_t* launches) {
+    if (!get_encode_fn()) return cudaErrorNotSupported;
+    p.M = (int)M; p.kblocks = (int)((K + BK - 1) / BK); p.status = status;
+    const Shape shape = choose_shape((int)M, (int)N, p.kblocks, num_sms);
+    const bool wide = shape.wide;
+    const int BN = wide ? 256 : 128, rows = wide ? 2 * BM : BM, columns = kind == GATE ? BN / 2 : BN;
+    p.N = (int)(kind == GATE ? N / 2 : N);
+    p.tiles_m = (p.M + rows - 1) / rows;
+    p.tiles_n = (p.N + columns - 1) / columns;
+    if ((int64_t)p.tiles_m * p.tiles_n > 0x3FFFFFFF) return cudaErrorInvalidConfiguration;
+    p.tiles = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n;
+    p.split = shape.split;
+    p.group_m = wide ? 8 : 16;
+    p.stages = STAGES;
+    p.a_mn = trans_a; p.b_mn = !trans_b;
+    const int a_rows = !p.a_mn && p.M < BM ? (p.M + 7) & ~7 : BM;
+    p.a_bytes = (uint32_t)a_rows * BK * 2;
+    CUtensorMap ma, mb;
+    if (!make_map_16bit(&ma, A, trans_a ? K : M, trans_a ? M : K, lda, p.a_mn ? BK : a_rows) ||
+        !make_map_16bit(&mb, B, trans_b ? N : K, trans_b ? K : N, ldb, 64))
+        return cudaErrorInvalidValue;
+    const int cluster = wide ? 2 : p.split, most = num_sms / cluster;
+    const int grid = cluster * (p.split > 1 || (int)p.tiles < most ? (int)p.tiles : most);
+    p.early = 2 * grid <= num_sms;
+    Kernel kern;
+    int which;
+    if (kind == GATE) { kern = wide ? matmul16_kernel<2, 256, GATE, bf16> : matmul16_kernel<1, 128, GATE, bf16>; which = 4 + wide; }
+    else if (kind == GRAD) { kern = wide ? matmul16_kernel<2, 256, GRAD, bf16> : matmul16_kernel<1, 128, GRAD, bf16>; which = 6 + wide; }
+    else if (type == CERAR_TYPE_F32) { kern = wide ? matmul16_kernel<2, 256, PLAIN, float> : matmul16_kernel<1, 128, PLAIN, float>; which = wide; }
+    else { kern = wide ? matmul16_kernel<2, 256, PLAIN, bf16> : matmul16_kernel<1, 128, PLAIN, bf16>; which = 2 + wide; }
+    const cudaError_t e = launch_one(kern, which, cluster, ma, mb, p, grid, s);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
+}  // namespace
+
+int matmul16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* split) {
+    const Shape shape = choose_shape((int)M, (int)N, (int)((K + BK - 1) / BK), num_sms);
+    *split = shape.split;
+    return shape.wide ? 256 : 128;
+}
+
+cudaError_t launch_matmul16(const Matmul16Args& a, int num_sms, cudaStream_t s, uint64_t* launches) {
+    Params p = {};
+    const int64_t size = a.type == CERAR_TYPE_F32 ? 4 : 2;
+    p.C = a.C; p.ldc = a.ldc; p.accumulate = a.accumulate;
+    p.c_vec = on(a.C, a.ldc, 16, size);
+    p.c_pair = on(a.C, a.ldc, 4, size);
+    return launch(p, PLAIN, a.type, a.A, a.lda, a.trans_a, a.B, a.ldb, a.trans_b, a.M, a.N, a.K, a.status, num_sms, s, launches);
+}
+
+cudaError_t launch_gated_in(const GatedInArgs& a, int num_sms, cudaStream_t s, uint64_t* launches) {
+    Params p = {};
+    p.C = a.h; p.ldc = a.ldh; p.keep = static_cast<bf16*>(a.gu); p.ldgu = a.ldgu; p.act = a.act;
+    p.c_vec = on(a.h, a.ldh, 16, 2);
+    p.gu_vec = a.gu && on(a.gu, a.ldgu, 16, 2) && a.hidden % 8 == 0;
+    return launch(p, GATE, CERAR_TYPE_BF16, a.x, a.ldx, false, a.w, a.ldw, true, a.tokens, 2 * a.hidden, a.width, a.status, num_sms, s, launches);
+}
+
+cudaError_t launch_gated_grad(const GatedGradArgs& a, int num_sms, cudaStream_t s, uint64_t* launches) {
+    Params p = {};
+    p.C = a.dgu; p.ldc = a.lddgu; p.gu = static_cast<const bf16*>(a.gu); p.ldgu = a.ldgu; p.act = a.act;
+    p.four = on(a.dgu, a.lddgu, 8, 2) && on(a.gu, a.ldgu, 8, 2) && a.hidden % 4 == 0;
+    return launch(p, GRAD, CERAR_TYPE_BF16, a.dy, a.lddy, false, a.w, a.ldw, false, a.tokens, a.hidden, a.width, a.status, num_sms, s, launches);
+}
+
+}  // namespace cerar

@@ -158,4 +158,39 @@ cudaError_t launch_head_norm(const HeadNormArgs& a, int num_sms, cudaStream_t s,
 cudaError_t launch_head_norm_grad(const HeadNormArgs& a, void* workspace, int num_sms, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_rotation_table(const double* freqs, int pairs, int64_t first, int64_t rows, float* table, int num_sms, cudaStream_t s, uint64_t* launches);
 
+
+// C = op(A) op(B) of bfloat16 matrices; rows on 16-byte boundaries, M, N, K above zero
+struct Matmul16Args {
+    const void *A, *B;
+    int64_t lda, ldb;
+    bool trans_a, trans_b;
+    int64_t M, N, K;
+    void* C;
+    int64_t ldc;
+    int type, accumulate;
+    int* status;
+};
+cudaError_t launch_matmul16(const Matmul16Args& a, int num_sms, cudaStream_t s, uint64_t* launches);
+int matmul16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* split);
+struct GatedInArgs {
+    const void *x, *w;
+    int64_t ldx, ldw;
+    int64_t tokens, width, hidden;
+    int act;
+    void *h, *gu;                        // gu: null where nothing is kept
+    int64_t ldh, ldgu;
+    int* status;
+};
+cudaError_t launch_gated_in(const GatedInArgs& a, int num_sms, cudaStream_t s, uint64_t* launches);
+struct GatedGradArgs {
+    const void *dy, *w, *gu;
+    int64_t lddy, ldw, ldgu;
+    int64_t tokens, width, hidden;
+    int act;
+    void* dgu;
+    int64_t lddgu;
+    int* status;
+};
+cudaError_t launch_gated_grad(const GatedGradArgs& a, int num_sms, cudaStream_t s, uint64_t* launches);
+
 }  // namespace cerar

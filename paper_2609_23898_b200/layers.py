@@ -4,6 +4,8 @@
   rotation_table, head_norm, head_norm_backward, HeadNorm
                                             norms of queries and keys for each head, with the rotation by position in the same pass
                                             (cerar_rotation_table, cerar_head_norm, cerar_head_norm_grad)
+  matmul, gated, gated_backward, Gated      bfloat16 products, and a gated feed-forward block made of them (cerar_matmul_bf16, cerar_gated_in,
+                                            cerar_gated_grad)
 
 As with training.Linear8 the gradients of weights are added to buffers of the caller's (slices of the vector that is aggregated) and the
 weights have none of their own.  Everything runs on the current stream of the tensors' device, without synchronisation.
@@ -267,3 +269,166 @@ class HeadNorm(torch.autograd.Function):
         dxq, dxk = head_norm_backward(ctx.ops, dq, dk, q, k, wq, wk, table, positions, dwq=ctx.dw[0], dwk=ctx.dw[1], eps=eps, pairs=pairs)
         need = ctx.needs_input_grad
         return (dxq if need[0] else None, dxk if need[1] else None) + (None,) * 10
+
+
+# ------------------------------------------------------------------------------------------------ bfloat16 products, gated block
+
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
+_BF16 = torch.bfloat16
+
+
+def _operand(t: torch.Tensor, what: str) -> torch.Tensor:
+    """A bfloat16 matrix as tensor-map copies read it, rows on 16-byte boundaries: a copy where it is not."""
+    if t.dtype != _BF16:
+        raise TypeError(f"{what}: bfloat16 wanted, got {t.dtype}")
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what}: a two-dimensional CUDA tensor is wanted")
+    rows, cols = t.shape
+    row, col = t.stride()
+    if not t.numel() or (col == 1 or cols == 1) and (rows == 1 or row >= cols and not row & 7) and not t.data_ptr() & 15:
+        return t
+    wide = torch.empty(rows, (cols + 7) & -8, dtype=_BF16, device=t.device)
+    return wide[:, :cols].copy_(t)
+
+
+def _ld8(t: torch.Tensor) -> int:
+    """Elements between rows (one row: any multiple of 8 that holds it)."""
+    return t.stride(0) if t.size(0) > 1 else (t.size(1) + 7) & -8
+
+
+def _padded(rows: int, cols: int, device) -> torch.Tensor:
+    """An empty bfloat16 matrix with rows on 16-byte boundaries."""
+    ld = (cols + 7) & -8
+    t = torch.empty(rows, ld, dtype=_BF16, device=device)
+    return t if ld == cols else t[:, :cols]
+
+
+def _matmul(ops, a, trans_a, b, trans_b, m, n, k, out, accumulate):
+    """(operands as _operand gives them)"""
+    st = lib.cerar_matmul_bf16(ops._h, a.data_ptr(), _ld8(a), trans_a, b.data_ptr(), _ld8(b), trans_b, m, n, k, out.data_ptr(), _type(out, "out"),
+                               _ld(out) if out.numel() else n, accumulate, _stream(out.device.index))
+    if st:
+        _check(st)
+    return out
+
+
+def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b=False, out: torch.Tensor | None = None,
+           dtype: torch.dtype = torch.bfloat16, accumulate=False) -> torch.Tensor:
+    """op(a) op(b) of bfloat16 matrices, into `out` (float32 or bfloat16) if given, added to it with accumulate."""
+    _same_device(ops, a=a, b=b, out=out)
+    a, b = _operand(a, "a"), _operand(b, "b")
+    m, k = (a.size(1), a.size(0)) if trans_a else a.shape
+    k2, n = (b.size(1), b.size(0)) if trans_b else b.shape
+    if k != k2:
+        raise ValueError("the summed dimensions of a and b differ")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate wants an `out` to add to")
+        out = torch.empty(m, n, dtype=dtype, device=a.device)
+    else:
+        _matrix(out, "out")
+        if tuple(out.shape) != (m, n):
+            raise ValueError(f"out of shape {(m, n)} wanted, got {tuple(out.shape)}")
+    return _matmul(ops, a, trans_a, b, trans_b, m, n, k, out, accumulate)
+
+
+def _gated_sizes(x, w_in, w_out, activation):
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(_ACTIVATIONS)}")
+    if w_in.dim() != 2 or w_out.dim() != 2 or w_in.size(0) != 2 * w_out.size(1):
+        raise ValueError("w_in (2 hidden x inputs: the gate's rows, then the others) and w_out (outputs x hidden) are wanted")
+    if x.dim() < 1 or x.size(-1) != w_in.size(1):
+        raise ValueError(f"x: {w_in.size(1)} values in the last dimension wanted")
+
+
+def _gated(ops, x, w_in, w_out, activation, keep):
+    """x as a matrix; returns y, g and u (kept), h."""
+    t, d = x.shape
+    o, f = w_out.shape
+    wi = _operand(w_in, "w_in")
+    h = _padded(t, f, x.device)
+    gu = _padded(t, 2 * f, x.device) if keep else None
+    st = lib.cerar_gated_in(ops._h, x.data_ptr(), _ld8(x), wi.data_ptr(), _ld8(wi), t, d, f, _ACTIVATIONS[activation], h.data_ptr(), _ld8(h),
+                            None if gu is None else gu.data_ptr(), 0 if gu is None else _ld8(gu), _stream(x.device.index))
+    if st:
+        _check(st)
+    y = _matmul(ops, h, False, _operand(w_out, "w_out"), True, t, o, f, torch.empty(t, o, dtype=_BF16, device=x.device), False)
+    return y, gu, h
+
+
+def gated(ops: Ops, x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *, activation: str = "silu", keep=False):
+    """(act(x w_g^T) * (x w_u^T)) w_out^T for x (..., inputs), w_in = w_g over w_u (2 hidden x inputs) and w_out (outputs x hidden), all bfloat16.
+    activation: silu, gelu, gelu_tanh or relu.  With keep also what gated_backward wants of it: (x, g and u, h, the activation)."""
+    _same_device(ops, x=x, w_in=w_in, w_out=w_out)
+    _gated_sizes(x, w_in, w_out, activation)
+    xm = _operand(_rows(x), "x")
+    y, gu, h = _gated(ops, xm, w_in, w_out, activation, keep)
+    y = y.view(*x.shape[:-1], y.size(-1))
+    return (y, (xm, gu, h, activation)) if keep else y
+
+
+def _gated_backward(ops, dy, kept, w_in, w_out, dw_in, dw_out, accumulate, need_dx):
+    x, gu, h, activation = kept
+    (t, d), (o, f) = x.shape, w_out.shape
+    dx = None
+    if dw_out is not None:
+        _matmul(ops, dy, True, h, False, o, f, t, dw_out, accumulate)
+    if dw_in is not None or need_dx:
+        wo = _operand(w_out, "w_out")
+        dgu = _padded(t, 2 * f, x.device)
+        st = lib.cerar_gated_grad(ops._h, dy.data_ptr(), _ld8(dy), wo.data_ptr(), _ld8(wo), t, o, f, _ACTIVATIONS[activation], gu.data_ptr(), _ld8(gu),
+                                  dgu.data_ptr(), _ld8(dgu), _stream(x.device.index))
+        if st:
+            _check(st)
+        if need_dx:
+            dx = _matmul(ops, dgu, False, _operand(w_in, "w_in"), False, t, d, 2 * f, torch.empty(t, d, dtype=_BF16, device=x.device), False)
+        if dw_in is not None:
+            _matmul(ops, dgu, True, x, False, 2 * f, d, t, dw_in, accumulate)
+    return dx
+
+
+def gated_backward(ops: Ops, dy: torch.Tensor, kept, w_in: torch.Tensor, w_out: torch.Tensor, dw_in: torch.Tensor | None, dw_out: torch.Tensor | None, *,
+                   accumulate=True, need_dx=True):
+    """dx from dy and what gated kept; dw_in and dw_out (float32 or bfloat16, e.g. slices of the gradient vector; None: not wanted) += the
+    gradients of the weights."""
+    x, gu, h, activation = kept
+    _same_device(ops, dy=dy, x=x, w_in=w_in, w_out=w_out, dw_in=dw_in, dw_out=dw_out)
+    _gated_sizes(x, w_in, w_out, activation)
+    for what, dw, w in (("dw_in", dw_in, w_in), ("dw_out", dw_out, w_out)):
+        if dw is not None:
+            _matrix(dw, what)
+            if dw.shape != w.shape:
+                raise ValueError(f"{what} of shape {tuple(w.shape)} wanted, got {tuple(dw.shape)}")
+    dym = _operand(_rows(dy), "dy")
+    if tuple(dym.shape) != (x.size(0), w_out.size(0)):
+        raise ValueError(f"dy: {x.size(0)} rows of {w_out.size(0)} values wanted")
+    dx = _gated_backward(ops, dym, kept, w_in, w_out, dw_in, dw_out, accumulate, need_dx)
+    return None if dx is None else dx.view(*dy.shape[:-1], dx.size(-1))
+
+
+class Gated(torch.autograd.Function):
+    """gated and gated_backward for torch.autograd: y = Gated.apply(x, w_in, w_out, ops, dw_in, dw_out, activation).  Every pass backward adds to
+    dw_in and dw_out (None: not wanted); second derivatives are refused."""
+
+    @classmethod
+    def apply(cls, x, w_in, w_out, ops, dw_in, dw_out, activation="silu"):
+        _no_gradient(w_in=w_in, w_out=w_out)
+        wanted = dw_in is not None or dw_out is not None
+        return super().apply(x, w_in, w_out, ops, dw_in, dw_out, activation, _anchor(x.device, wanted and not x.requires_grad))
+
+    @staticmethod
+    def forward(ctx, x, w_in, w_out, ops, dw_in, dw_out, activation, anchor):
+        keep = ctx.needs_input_grad[0] or anchor is not None
+        if not keep:
+            return gated(ops, x, w_in, w_out, activation=activation)
+        y, kept = gated(ops, x, w_in, w_out, activation=activation, keep=True)
+        ctx.ops, ctx.dw, ctx.activation = ops, (dw_in, dw_out), activation
+        ctx.save_for_backward(*kept[:3], w_in, w_out)
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        *kept, w_in, w_out = ctx.saved_tensors
+        dx = gated_backward(ctx.ops, dy, (*kept, ctx.activation), w_in, w_out, *ctx.dw, need_dx=ctx.needs_input_grad[0])
+        return (dx,) + (None,) * 7
