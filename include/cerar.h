@@ -671,21 +671,24 @@ int            cerar_matmul_bf16_tile(int64_t M, int64_t N, int64_t K, int num_s
  * w_in (2 hidden x width: the gate's rows, then the other projection's) and w_out (outputs x hidden):
  *     [g u] = x w_in^T,   h = act(g) u,   y = h w_out^T
  *     dh = dy w_out,  dg = dh u act'(g),  du = dh act(g),  dx = [dg du] w_in,  dw_in += [dg du]^T x,  dw_out += dy^T h
- * cerar_gated_in makes h (tokens x hidden) from the binary32 sums and, where gu is not NULL, leaves [g u] (tokens x 2 hidden) rounded to
- * bfloat16 for the backward pass.  cerar_gated_grad makes [dg du] (tokens x 2 hidden) from dy (tokens x width), w_out (width x hidden) and
- * gu: dh stays in binary32.  g, u, dg, du and h are bfloat16 in memory, as the operands of the products that follow have to be; each is
- * rounded once.  x, dy, w: as the operands of cerar_matmul_bf16; the others need alignment to their elements (16-byte rows and
- * hidden a multiple of 8 are faster). */
+ * cerar_gated_in makes h (tokens x hidden) from the binary32 sums and, where `kept` is not NULL, leaves there g and u for the backward pass,
+ * in 24 bits each (2^-16 of themselves off): cerar_gated_kept_bytes bytes on a 16-byte boundary, in a layout of its own.  cerar_gated_grad makes
+ * [dg du] (tokens x 2 hidden) and, where h is not NULL, h again, from dy (tokens x width), w_out (width x hidden; width > 0) and kept; dh stays in
+ * binary32.  dg, du and h are bfloat16 in memory, as the operands of the products that follow have to be; each is rounded once.
+ * The sums are within 2^-23 (8 + K / 16) of the sum of their terms' magnitudes, K the width.
+ * x, dy, w: as the operands of cerar_matmul_bf16; the others need alignment to their elements (16-byte rows and hidden a multiple of 8 are
+ * faster). */
 typedef enum {
     CERAR_ACT_SILU = 0,          /* g / (1 + e^-g)                                                        */
     CERAR_ACT_GELU = 1,          /* g Phi(g), Phi the normal distribution                                 */
     CERAR_ACT_GELU_TANH = 2,     /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2                      */
     CERAR_ACT_RELU = 3           /* max(g, 0); its derivative at 0 is 0                                    */
 } cerar_activation_t;
+size_t         cerar_gated_kept_bytes(int64_t tokens, int64_t hidden);
 cerar_status_t cerar_gated_in(cerar_ops_t* ops, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t tokens, int64_t width,
-                              int64_t hidden, cerar_activation_t act, void* h, int64_t ldh, void* gu, int64_t ldgu, cerar_stream_t stream);
+                              int64_t hidden, cerar_activation_t act, void* h, int64_t ldh, void* kept, cerar_stream_t stream);
 cerar_status_t cerar_gated_grad(cerar_ops_t* ops, const void* dy, int64_t lddy, const void* w, int64_t ldw, int64_t tokens, int64_t width,
-                                int64_t hidden, cerar_activation_t act, const void* gu, int64_t ldgu, void* dgu, int64_t lddgu,
+                                int64_t hidden, cerar_activation_t act, const void* kept, void* dgu, int64_t lddgu, void* h, int64_t ldh,
                                 cerar_stream_t stream);
 
 const char*    cerar_status_string(cerar_status_t s);

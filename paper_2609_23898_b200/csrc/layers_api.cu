@@ -209,45 +209,46 @@ int cerar_matmul_bf16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* sp
     return cerar::matmul16_tile(M, N, K, num_sms, split);
 }
 
+size_t cerar_gated_kept_bytes(int64_t tokens, int64_t hidden) {
+    if (tokens < 0 || tokens > TOKENS_MAX || hidden < 0 || hidden > SIZE_MAX_ / 2) return 0;
+    return cerar::gated_kept_bytes(tokens, hidden);
+}
+
 cerar_status_t cerar_gated_in(cerar_ops_t* o, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t tokens, int64_t width, int64_t hidden,
-                              cerar_activation_t act, void* h, int64_t ldh, void* gu, int64_t ldgu, cerar_stream_t stream) {
+                              cerar_activation_t act, void* h, int64_t ldh, void* kept, cerar_stream_t stream) {
     cerar_status_t st = check_ops(o);
     if (st != CERAR_OK) return st;
     if (hidden < 0 || hidden > SIZE_MAX_ / 2) return fail(CERAR_ERR_SHAPE, "gated: hidden must be from 0 to 2^30 - 128");
     if ((st = check_act(act)) != CERAR_OK || (st = check_operand(x, tokens, width, ldx)) != CERAR_OK || (st = check_operand(w, 2 * hidden, width, ldw)) != CERAR_OK ||
-        (st = check_rows(h, CERAR_TYPE_BF16, tokens, hidden, ldh, "h NULL or not aligned to its elements")) != CERAR_OK ||
-        (gu && (st = check_rows(gu, CERAR_TYPE_BF16, tokens, 2 * hidden, ldgu, "gu not aligned to its elements")) != CERAR_OK))
+        (st = check_rows(h, CERAR_TYPE_BF16, tokens, hidden, ldh, "h NULL or not aligned to its elements")) != CERAR_OK)
         return st;
+    if (misaligned(kept, 16)) return fail(CERAR_ERR_INVALID_ARG, "kept is not on a 16-byte boundary");
     if (tokens == 0 || hidden == 0) return CERAR_OK;
     cudaError_t e = cudaSuccess;
     if (width == 0) {                     // empty sums: g = u = 0, and act(0) 0 = 0
         e = cudaMemset2DAsync(h, (size_t)(tokens > 1 ? ldh : hidden) * 2, 0, (size_t)hidden * 2, (size_t)tokens, (cudaStream_t)stream);
-        if (e == cudaSuccess && gu)
-            e = cudaMemset2DAsync(gu, (size_t)(tokens > 1 ? ldgu : 2 * hidden) * 2, 0, (size_t)hidden * 4, (size_t)tokens, (cudaStream_t)stream);
+        if (e == cudaSuccess && kept) e = cudaMemsetAsync(kept, 0, cerar::gated_kept_bytes(tokens, hidden), (cudaStream_t)stream);
     } else {
-        const cerar::GatedInArgs a = {x, w, ldx, ldw, tokens, width, hidden, act, h, gu, ldh, ldgu, o->d_status};
+        const cerar::GatedInArgs a = {x, w, ldx, ldw, tokens, width, hidden, act, h, kept, ldh, o->d_status};
         e = cerar::launch_gated_in(a, o->num_sms, (cudaStream_t)stream, &o->launches);
     }
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "gated block launch");
 }
 
 cerar_status_t cerar_gated_grad(cerar_ops_t* o, const void* dy, int64_t lddy, const void* w, int64_t ldw, int64_t tokens, int64_t width, int64_t hidden,
-                                cerar_activation_t act, const void* gu, int64_t ldgu, void* dgu, int64_t lddgu, cerar_stream_t stream) {
+                                cerar_activation_t act, const void* kept, void* dgu, int64_t lddgu, void* h, int64_t ldh, cerar_stream_t stream) {
     cerar_status_t st = check_ops(o);
     if (st != CERAR_OK) return st;
     if (hidden < 0 || hidden > SIZE_MAX_ / 2) return fail(CERAR_ERR_SHAPE, "gated: hidden must be from 0 to 2^30 - 128");
     if ((st = check_act(act)) != CERAR_OK || (st = check_operand(dy, tokens, width, lddy)) != CERAR_OK || (st = check_operand(w, width, hidden, ldw)) != CERAR_OK ||
-        (st = check_rows(gu, CERAR_TYPE_BF16, tokens, 2 * hidden, ldgu, "gu NULL or not aligned to its elements")) != CERAR_OK ||
-        (st = check_rows(dgu, CERAR_TYPE_BF16, tokens, 2 * hidden, lddgu, "dgu NULL or not aligned to its elements")) != CERAR_OK)
+        (st = check_rows(dgu, CERAR_TYPE_BF16, tokens, 2 * hidden, lddgu, "dgu NULL or not aligned to its elements")) != CERAR_OK ||
+        (h && (st = check_rows(h, CERAR_TYPE_BF16, tokens, hidden, ldh, "h not aligned to its elements")) != CERAR_OK))
         return st;
     if (tokens == 0 || hidden == 0) return CERAR_OK;
-    cudaError_t e = cudaSuccess;
-    if (width == 0) {                     // dh = 0
-        e = cudaMemset2DAsync(dgu, (size_t)(tokens > 1 ? lddgu : 2 * hidden) * 2, 0, (size_t)hidden * 4, (size_t)tokens, (cudaStream_t)stream);
-    } else {
-        const cerar::GatedGradArgs a = {dy, w, gu, lddy, ldw, ldgu, tokens, width, hidden, act, dgu, lddgu, o->d_status};
-        e = cerar::launch_gated_grad(a, o->num_sms, (cudaStream_t)stream, &o->launches);
-    }
+    if (!kept || misaligned(kept, 16)) return fail(CERAR_ERR_INVALID_ARG, "kept NULL, or not on a 16-byte boundary");
+    if (width == 0) return fail(CERAR_ERR_SHAPE, "gated gradient: a block without outputs has none");
+    const cerar::GatedGradArgs a = {dy, w, kept, lddy, ldw, tokens, width, hidden, act, dgu, h, lddgu, ldh, o->d_status};
+    const cudaError_t e = cerar::launch_gated_grad(a, o->num_sms, (cudaStream_t)stream, &o->launches);
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "gated block gradient launch");
 }
 

@@ -14,8 +14,9 @@
 //   warps 4-11 take the sums out (32 lanes of tensor memory, half of the tile's columns each), finish them in binary32 and write
 // (Warps 2, 3 complete the warpgroup that hands most of its registers to the others.)
 //
-// The accumulator drops what does not fit its 24 bits instead of rounding, an error that grows with the number of additions, so sums of more than
-// SEGMENT blocks of k are put together in registers.
+// The accumulator drops what does not fit its 24 bits instead of rounding, an error that grows with the number of additions, so plain sums of more
+// than SEGMENT blocks of k are put together in registers.  (The gate's results have 16 bits, 24 at most: their sums stay in one piece, so that
+// GRAD can take dh out of tensor memory as it goes.)
 // Few tiles, long sums: a cluster of S blocks shares a tile, each sums 1/S of the blocks of k, and the partial tiles are added through
 // distributed shared memory, in a fixed order.
 // Every wait is bounded; one that runs out sets the status word and the block leaves through the common exit.
@@ -41,22 +42,27 @@ constexpr int WARP_EPI0 = 4, THREADS = 32 * (WARP_EPI0 + EPI_WARPS), MAX_SPLIT =
 // registers per thread: 128 x 56 + 256 x 224 = 384 x 168, what the block is launched with
 constexpr int REGS_FEW = 56, REGS_MANY = 224;
 constexpr uint32_t A_BYTES = BM * BK * 2, PART = 64 * BK * 2;      // an operand lies in parts of 64 of its own rows or columns
-constexpr int SEGMENT = 64;
+constexpr int SEGMENT = 64;                             // 4096 values of k: 256 additions
 
 enum { PLAIN = 0, GATE = 1, GRAD = 2 };
 
+struct Kept {
+    uint16_t* high;
+    uint8_t* low;
+    int64_t plane, cols;                               // plane = tokens * cols
+};
 struct Params {
     void* C;                                           // PLAIN: C; GATE: h; GRAD: [dg du]
     int64_t ldc;
-    bf16* keep;                                        // GATE: where [g u] go, or null
-    const bf16* gu;                                    // GRAD: [g u]
-    int64_t ldgu;
+    Kept kept;                                         // GATE: where g and u go (high null: nowhere); GRAD: where they are
+    bf16* h;                                           // GRAD: h, or null
+    int64_t ldh;
     int M, N, kblocks;                                 // N: columns of C (GATE, GRAD: of h)
     int tiles_m, tiles_n, group_m;
     uint32_t tiles;
     int a_mn, b_mn;                                    // 1: the operand's own dimension (m or n) is the contiguous one
     int accumulate, c_vec, c_pair;                     // rows of C start on 16-byte, on 4-byte boundaries
-    int gu_vec, four;                                  // GATE: rows of g and of u on 16-byte boundaries; GRAD: g, u, dg and du on 8-byte ones
+    int four;                                          // GRAD: rows of dg, du and h on 8-byte boundaries
     int act;
     int stages, split;
     uint32_t a_bytes;                                  // what a load of A brings (few rows: those only; the others' sums are made of
@@ -75,41 +81,122 @@ __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uin
                      " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// ---------------------------------------------------------------- activations (binary32; the exponential and the quotient are the
-// hardware's, some 2^-21 of themselves off, far below the step of a bfloat16 result)
+// ---------------------------------------------------------------- activations
+//
+// In binary32, two values at a time (one instruction for both, where there is one).  The exponential and the reciprocal are the hardware's, some
+// 2^-22 of themselves off, far below the step of a bfloat16 result.
+
+__device__ __forceinline__ uint64_t two_of(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void parts(uint64_t r, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r)); }
+__device__ __forceinline__ uint64_t all(float x) { return two_of(x, x); }
+__device__ __forceinline__ uint64_t mul2(uint64_t x, uint64_t y) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t mad2(uint64_t x, uint64_t y, uint64_t z) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+    return r;
+}
+__device__ __forceinline__ uint64_t exp2_2(uint64_t x) {
+    float a, b;
+    parts(x, a, b);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return two_of(a, b);
+}
+__device__ __forceinline__ uint64_t rcp_2(uint64_t x) {
+    float a, b;
+    parts(x, a, b);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return two_of(a, b);
+}
+constexpr float LOG2E = 1.44269504f;
 
 template <int ACT> struct Act;
 template <> struct Act<CERAR_ACT_SILU> {
-    static __device__ __forceinline__ float value(float g) { return __fdividef(g, 1.f + __expf(-g)); }
-    static __device__ __forceinline__ void both(float g, float& a, float& d) {
-        const float s = __fdividef(1.f, 1.f + __expf(-g));
-        a = g * s;
-        d = fmaf(a, 1.f - s, s);
+    static __device__ __forceinline__ uint64_t part(uint64_t g) { return rcp_2(add2(exp2_2(mul2(g, all(-LOG2E))), all(1.f))); }
+    static __device__ __forceinline__ uint64_t value(uint64_t g) { return mul2(g, part(g)); }
+    static __device__ __forceinline__ void both(uint64_t g, uint64_t& a, uint64_t& d) {
+        const uint64_t s = part(g);
+        a = mul2(g, s);
+        d = mad2(a, mad2(s, all(-1.f), all(1.f)), s);
     }
 };
-template <> struct Act<CERAR_ACT_GELU> {               // g Phi(g); Phi from the error function, its complement where that is small
-    static __device__ __forceinline__ float phi(float g) { return g < -1.f ? 0.5f * erfcf(-0.70710678f * g) : fmaf(0.5f, erff(0.70710678f * g), 0.5f); }
-    static __device__ __forceinline__ float value(float g) { return g * phi(g); }
-    static __device__ __forceinline__ void both(float g, float& a, float& d) {
-        const float c = phi(g);
-        a = g * c;
-        d = fmaf(g * 0.39894228f, __expf(-0.5f * g * g), c);
+// g Phi(g).  Phi(-|g|) = erfc(z) / 2 with z = |g| / sqrt 2, and erfc(z) = t e^(-z^2 + P(t)), t = 1 / (1 + z / 2), P of degree 9: the
+// Chebyshev fit published in Numerical Recipes (erfcc, relative error below 1.2e-7 for all z), its coefficients here times log2 e.
+template <> struct Act<CERAR_ACT_GELU> {
+    static __device__ __forceinline__ void fit(uint64_t g, uint64_t& t, uint64_t& square, uint64_t& p) {
+        const uint64_t z = mul2(g & 0x7FFFFFFF7FFFFFFFull, all(0.70710678f));
+        t = rcp_2(mad2(z, all(0.5f), all(1.f)));
+        square = mul2(mul2(z, all(-LOG2E)), z);
+        p = mad2(t, all(0.17087277f * LOG2E), all(-0.82215223f * LOG2E));
+        p = mad2(t, p, all(1.48851587f * LOG2E));
+        p = mad2(t, p, all(-1.13520398f * LOG2E));
+        p = mad2(t, p, all(0.27886807f * LOG2E));
+        p = mad2(t, p, all(-0.18628806f * LOG2E));
+        p = mad2(t, p, all(0.09678418f * LOG2E));
+        p = mad2(t, p, all(0.37409196f * LOG2E));
+        p = mad2(t, p, all(1.00002368f * LOG2E));
+        p = mad2(t, p, all(-1.26551223f * LOG2E - 1.f));                 // (- 1: half of erfc)
+    }
+    // Phi(g) from Phi(-|g|)
+    static __device__ __forceinline__ uint64_t side(uint64_t g, uint64_t low) {
+        const uint64_t high = mad2(low, all(-1.f), all(1.f));
+        float g0, g1, l0, l1, h0, h1;
+        parts(g, g0, g1); parts(low, l0, l1); parts(high, h0, h1);
+        return two_of(g0 < 0.f ? l0 : h0, g1 < 0.f ? l1 : h1);
+    }
+    static __device__ __forceinline__ uint64_t value(uint64_t g) {
+        uint64_t t, square, p;
+        fit(g, t, square, p);
+        return mul2(g, side(g, mul2(t, exp2_2(add2(square, p)))));
+    }
+    static __device__ __forceinline__ void both(uint64_t g, uint64_t& a, uint64_t& d) {
+        uint64_t t, square, p;
+        fit(g, t, square, p);
+        const uint64_t e = exp2_2(square);                               // e^(-g^2 / 2)
+        const uint64_t phi = side(g, mul2(mul2(t, e), exp2_2(p)));
+        a = mul2(g, phi);
+        d = mad2(mul2(g, all(0.39894228f)), e, phi);
     }
 };
 template <> struct Act<CERAR_ACT_GELU_TANH> {          // g / (1 + e^-2v) with v = sqrt(2 / pi) (g + 0.044715 g^3): (1 + tanh v) / 2 is that quotient
-    static __device__ __forceinline__ float part(float g) { return __fdividef(1.f, 1.f + __expf(-1.5957691f * g * fmaf(0.044715f, g * g, 1.f))); }
-    static __device__ __forceinline__ float value(float g) { return g * part(g); }
-    static __device__ __forceinline__ void both(float g, float& a, float& d) {
-        const float s = part(g);
-        a = g * s;
-        d = fmaf(a * (1.f - s), 1.5957691f * fmaf(0.134145f, g * g, 1.f), s);
+    static __device__ __forceinline__ uint64_t part(uint64_t g, uint64_t gg) {
+        return rcp_2(add2(exp2_2(mul2(mul2(g, all(-1.5957691f * LOG2E)), mad2(gg, all(0.044715f), all(1.f)))), all(1.f)));
+    }
+    static __device__ __forceinline__ uint64_t value(uint64_t g) { return mul2(g, part(g, mul2(g, g))); }
+    static __device__ __forceinline__ void both(uint64_t g, uint64_t& a, uint64_t& d) {
+        const uint64_t gg = mul2(g, g), s = part(g, gg);
+        a = mul2(g, s);
+        // (far out 1 - s or s is 0 and the cubic may be anything: the product is then kept at 0 by ordering it last)
+        const uint64_t rest = mul2(a, mad2(s, all(-1.f), all(1.f)));
+        d = mad2(rest, mad2(gg, all(1.5957691f * 0.134145f), all(1.5957691f)), s);
     }
 };
 template <> struct Act<CERAR_ACT_RELU> {
-    static __device__ __forceinline__ float value(float g) { return g > 0.f ? g : g != g ? g : 0.f; }
-    static __device__ __forceinline__ void both(float g, float& a, float& d) {
-        a = value(g);
-        d = g > 0.f ? 1.f : 0.f;
+    static __device__ __forceinline__ float one(float g) { return g > 0.f ? g : g != g ? g : 0.f; }
+    static __device__ __forceinline__ uint64_t value(uint64_t g) {
+        float x, y;
+        parts(g, x, y);
+        return two_of(one(x), one(y));
+    }
+    static __device__ __forceinline__ void both(uint64_t g, uint64_t& a, uint64_t& d) {
+        float x, y;
+        parts(g, x, y);
+        a = two_of(one(x), one(y));
+        d = two_of(x > 0.f ? 1.f : 0.f, y > 0.f ? 1.f : 0.f);
     }
 };
 template <typename F>
@@ -118,6 +205,42 @@ __device__ __forceinline__ void with_act(int act, F f) {
     else if (act == CERAR_ACT_GELU) f(Act<CERAR_ACT_GELU>());
     else if (act == CERAR_ACT_GELU_TANH) f(Act<CERAR_ACT_GELU_TANH>());
     else f(Act<CERAR_ACT_RELU>());
+}
+
+// ---------------------------------------------------------------- what is kept for the backward pass
+//
+// g and u in 24 bits: sign, exponent and 15 bits of the fraction, rounded to nearest (2^-16 of themselves off), the upper 16 bits of all values in one
+// plane, the lower 8 in another.  Kept in bfloat16 their rounding would be the largest part of the error of dx and dw_in (3.0e-3 instead of
+// 2.4e-3 of the norm); h is made again from them, so that no more is kept than g, u and h in bfloat16 would be.
+// Planes: [g, u][tokens][cols], cols the hidden size rounded up to 16.
+
+__device__ __forceinline__ uint32_t to24(float x) {    // (a carry into the exponent is right; NaN keeps its upper bits)
+    const uint32_t b = __float_as_uint(x);
+    return x != x ? b | 0x00400000u : b + 0x80u;
+}
+__device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x7632); }
+__device__ __forceinline__ uint32_t lows(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0051), __byte_perm(c, d, 0x0051), 0x5410);
+}
+struct Four {                                          // four neighbouring values of one plane pair
+    uint2 high;
+    uint32_t low;
+};
+__device__ __forceinline__ Four load_kept(const Kept& k, int which, int64_t row, int col) {
+    const int64_t at = which * k.plane + row * k.cols + col;
+    return {__ldg(reinterpret_cast<const uint2*>(k.high + at)), __ldg(reinterpret_cast<const uint32_t*>(k.low + at))};
+}
+__device__ __forceinline__ void store_kept(const Kept& k, int which, int64_t row, int col, const float* v) {
+    const int64_t at = which * k.plane + row * k.cols + col;
+    const uint32_t a = to24(v[0]), b = to24(v[1]), c = to24(v[2]), d = to24(v[3]);
+    *reinterpret_cast<uint2*>(k.high + at) = make_uint2(highs(a, b), highs(c, d));
+    *reinterpret_cast<uint32_t*>(k.low + at) = lows(a, b, c, d);
+}
+// values 2 i and 2 i + 1 of four
+__device__ __forceinline__ uint64_t pair_of(const Four& f, int i) {
+    const uint32_t h = i ? f.high.y : f.high.x;
+    const uint32_t x = __byte_perm(h, f.low, i ? 0x1066 : 0x1044) & 0xFFFFFF00u, y = __byte_perm(h, f.low, i ? 0x3277 : 0x3255) & 0xFFFFFF00u;
+    return two_of(__uint_as_float(x), __uint_as_float(y));
 }
 
 // ---------------------------------------------------------------- writing
@@ -164,19 +287,31 @@ __device__ __forceinline__ void write_rows(uint32_t staging, bf16* c, int64_t ld
     }
 }
 
-// Four columns of a row in the gate's epilogues, `n` of them there.
-__device__ __forceinline__ uint2 load4(const bf16* p, int n, bool vec) {
-    if (vec && n >= 4) return __ldg(reinterpret_cast<const uint2*>(p));
-    uint32_t w[4];
+// 32 rows of `words` 32-bit words each (a multiple of 4, at most 32; the warp holds row (lane)'s) to rows `pitch` bytes apart of which nrows and
+// `bytes` bytes exist, all on 16-byte boundaries and a multiple of 16 bytes.
+template <int WORDS>
+__device__ __forceinline__ void write_words(uint32_t staging, unsigned char* dst, int64_t pitch, int nrows, int bytes, const uint32_t* v) {
+    constexpr int PER_ROW = WORDS / 4, ROWS = 32 / PER_ROW;
+    const int lane = threadIdx.x & 31, j = lane % PER_ROW;
+    __syncwarp();
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = e < n ? __ldg(reinterpret_cast<const unsigned short*>(p) + e) : 0u;
-    return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+    for (int i = 0; i < PER_ROW; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
+    __syncwarp();
+#pragma unroll
+    for (int it = 0; it < 32 / ROWS; ++it) {
+        const int r = it * ROWS + lane / PER_ROW;
+        uint4 q;
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
+        if (r < nrows && 16 * j < bytes) *reinterpret_cast<uint4*>(dst + r * pitch + 16 * j) = q;
+    }
 }
-__device__ __forceinline__ float element(uint2 q, int e) {
-    const uint32_t w = e < 2 ? q.x : q.y;
-    return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
-}
-__device__ __forceinline__ void store4(bf16* p, int n, bool vec, const float* v) {
+
+// Four columns of a row to bfloat16, `n` of them there
+__device__ __forceinline__ void store4(bf16* p, int n, bool vec, uint64_t lo, uint64_t hi) {
+    float v[4];
+    parts(lo, v[0], v[1]);
+    parts(hi, v[2], v[3]);
     if (vec && n >= 4) {
         *reinterpret_cast<uint2*>(p) = make_uint2(Out<bf16>::two(v[0], v[1]), Out<bf16>::two(v[2], v[3]));
     } else {
@@ -185,23 +320,37 @@ __device__ __forceinline__ void store4(bf16* p, int n, bool vec, const float* v)
             if (e < n) p[e] = __float2bfloat16_rn(v[e]);
     }
 }
-// dg and du of four columns from dh and the kept g and u
-__device__ __forceinline__ void write_grad4(const Params& p, int row, int col, const float* dh, uint2 g, uint2 u) {
+// dg, du and h of four columns from dh and the kept g and u
+template <typename A>
+__device__ __forceinline__ void write_grad4(const Params& p, A act, int row, int col, const uint64_t* dh, const Four& g, const Four& u) {
     const int n = p.N - col;
-    if (n <= 0) return;
-    float dg[4], du[4];
-    with_act(p.act, [&](auto act) {
+    uint64_t dg[2], du[2], h[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float a, d;
-            act.both(element(g, e), a, d);
-            dg[e] = dh[e] * element(u, e) * d;
-            du[e] = dh[e] * a;
-        }
-    });
+    for (int i = 0; i < 2; ++i) {
+        uint64_t a, d;
+        const uint64_t up = pair_of(u, i);
+        act.both(pair_of(g, i), a, d);
+        dg[i] = mul2(mul2(dh[i], up), d);
+        du[i] = mul2(dh[i], a);
+        h[i] = mul2(a, up);
+    }
     bf16* c = static_cast<bf16*>(p.C) + (int64_t)row * p.ldc + col;
-    store4(c, n, p.four, dg);
-    store4(c + p.N, n, p.four, du);
+    store4(c, n, p.four, dg[0], dg[1]);
+    store4(c + p.N, n, p.four, du[0], du[1]);
+    if (p.h) store4(p.h + (int64_t)row * p.ldh + col, n, p.four, h[0], h[1]);
+}
+
+// g and u of four columns (this lane's) of every fourth row
+__device__ __forceinline__ void load_grad(const Params& p, int row0, int nrows, int col, Four* next) {
+    const int r0 = (threadIdx.x & 31) >> 3;
+#pragma unroll
+    for (int it = 0; it < 8; ++it) {
+        next[2 * it] = next[2 * it + 1] = {make_uint2(0u, 0u), 0u};
+        if (it * 4 + r0 < nrows && col < p.N) {
+            next[2 * it] = load_kept(p.kept, 0, row0 + it * 4 + r0, col);
+            next[2 * it + 1] = load_kept(p.kept, 1, row0 + it * 4 + r0, col);
+        }
+    }
 }
 
 // The whole tile's sums of this warp: rows row0 .. row0 + 31, CW columns, in registers.
@@ -215,47 +364,68 @@ __device__ __forceinline__ void write_tile(const Params& p, uint32_t staging, in
         for (int c = 0; c < CW / SLAB; ++c) write_slab<C>(p, staging, row0, tn * BN + half * CW + c * SLAB, acc + c * SLAB);
     } else if constexpr (KIND == GATE) {
         constexpr int FW = BN / 4;                      // columns of h: acc holds their g, then their u
-        const int col0 = tn * (BN / 2) + half * FW;
-        if (p.keep) {
-            write_rows<FW>(staging, p.keep, p.ldgu, p.M, p.N, row0, col0, acc, p.gu_vec);
-            write_rows<FW>(staging, p.keep + p.N, p.ldgu, p.M, p.N, row0, col0, acc + FW, p.gu_vec);
+        const int col0 = tn * (BN / 2) + half * FW, nrows = p.M - row0 < 32 ? p.M - row0 : 32;
+        if (nrows <= 0 || col0 >= p.N) return;
+        if (p.kept.high) {
+            uint32_t low[FW / 2];
+            const int cols = (int)(p.kept.cols - col0 < FW ? p.kept.cols - col0 : FW);
+            const int64_t at = (int64_t)row0 * p.kept.cols + col0;
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                uint32_t high[FW / 2];
+#pragma unroll
+                for (int j = 0; j < FW; j += 4) {
+                    const float* v = acc + which * FW + j;
+                    const uint32_t a = to24(v[0]), b = to24(v[1]), c = to24(v[2]), d = to24(v[3]);
+                    high[j / 2] = highs(a, b);
+                    high[j / 2 + 1] = highs(c, d);
+                    low[which * (FW / 4) + j / 4] = lows(a, b, c, d);
+                }
+                write_words<FW / 2>(staging, reinterpret_cast<unsigned char*>(p.kept.high + which * p.kept.plane + at), 2 * p.kept.cols, nrows, 2 * cols, high);
+            }
+            write_words<FW / 4>(staging, p.kept.low + at, p.kept.cols, nrows, cols, low);
+            write_words<FW / 4>(staging, p.kept.low + p.kept.plane + at, p.kept.cols, nrows, cols, low + FW / 4);
         }
         with_act(p.act, [&](auto act) {
 #pragma unroll
-            for (int j = 0; j < FW; ++j) acc[j] = act.value(acc[j]) * acc[FW + j];
+            for (int j = 0; j < FW; j += 2) parts(mul2(act.value(two_of(acc[j], acc[j + 1])), two_of(acc[FW + j], acc[FW + j + 1])), acc[j], acc[j + 1]);
         });
         write_rows<FW>(staging, static_cast<bf16*>(p.C), p.ldc, p.M, p.N, row0, col0, acc, p.c_vec);
-    } else {
-        // dh through the staging rows, 32 columns at a time, so that a row's g, u, dg and du are touched in pieces of 64 bytes
-        const int nrows = p.M - row0 < 32 ? p.M - row0 : 32;
-        if (nrows <= 0) return;
-#pragma unroll
+    }
+}
+
+// GRAD: dh comes from tensor memory (`from`: this warp's lanes and columns) 32 columns at a time and goes through the staging rows, so that the
+// rows of g, u, dg, du and h are touched in pieces of 64 bytes; g and u of the next 32 columns are on their way meanwhile (next: of the first).
+template <int BN, typename Release>
+__device__ __forceinline__ void write_grad(const Params& p, uint32_t staging, uint32_t from, int row0, int col0, Four* next, Release release) {
+    constexpr int CW = BN / 2;
+    const int lane = threadIdx.x & 31, nrows = p.M - row0 < 32 ? p.M - row0 : 32, r0 = lane >> 3, j = lane & 7;
+    with_act(p.act, [&](auto act) {
+#pragma unroll 1
         for (int h = 0; h < CW / 32; ++h) {
-            const int col = tn * BN + half * CW + h * 32 + (lane & 7) * 4;
-            uint2 g[8], u[8];
-#pragma unroll
-            for (int it = 0; it < 8; ++it) {
-                const int r = it * 4 + (lane >> 3);
-                const int n = r < nrows ? p.N - col : 0;
-                const bf16* at = p.gu + (int64_t)(row0 + r) * p.ldgu + col;
-                g[it] = load4(at, n, p.four);
-                u[it] = load4(at + p.N, n, p.four);
-            }
+            const int col = col0 + h * 32 + j * 4;
+            uint32_t v[32];
+            ld32_start(from + h * 32, v);
+            ld32_done(v);
+            if (h + 1 == CW / 32) release();
             __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((j ^ (lane & 7)) << 4)), "f"(acc[h * 32 + 4 * j]), "f"(acc[h * 32 + 4 * j + 1]),
-                             "f"(acc[h * 32 + 4 * j + 2]), "f"(acc[h * 32 + 4 * j + 3]) : "memory");
+            for (int i = 0; i < 8; ++i)
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
+            Four now[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) now[i] = next[i];
+            if (h + 1 < CW / 32) load_grad(p, row0, nrows, col + 32, next);
             __syncwarp();
 #pragma unroll
             for (int it = 0; it < 8; ++it) {
-                const int r = it * 4 + (lane >> 3), j = lane & 7;
-                float dh[4];
-                asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(dh[0]), "=f"(dh[1]), "=f"(dh[2]), "=f"(dh[3]) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
-                if (r < nrows) write_grad4(p, row0 + r, col, dh, g[it], u[it]);
+                const int r = it * 4 + r0;
+                uint64_t dh[2];
+                asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(dh[0]), "=l"(dh[1]) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
+                if (r < nrows && col < p.N) write_grad4(p, act, row0 + r, col, dh, now[2 * it], now[2 * it + 1]);
             }
         }
-    }
+    });
 }
 
 // A tile whose sum is split over a cluster: every block leaves the rows of its partial tile that exist in its stages (free by then), row
@@ -304,24 +474,24 @@ __device__ __forceinline__ void add_partials(const Params& p, uint32_t smem, int
                     if (e < n) dst[e] = (C)(p.accumulate ? (float)dst[e] + v[e] : v[e]);
             }
         } else if constexpr (KIND == GATE) {
-            // a warp's 32 columns of g are followed by the same ones of u
+            // a row's columns of g are followed by the same ones of u
             const float4 u4 = add_piece(p, base + ((uint32_t)((j + PER_ROW) ^ (r & 7)) << 4));
             const float u[4] = {u4.x, u4.y, u4.z, u4.w};
-            if (p.keep) {
-                bf16* at = p.keep + (int64_t)row * p.ldgu + col;
-                store4(at, n, p.gu_vec, v);
-                store4(at + p.N, n, p.gu_vec, u);
+            if (p.kept.high && col < p.kept.cols) {
+                store_kept(p.kept, 0, row, col, v);
+                store_kept(p.kept, 1, row, col, u);
             }
-            float h[4];
-            with_act(p.act, [&](auto act) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = act.value(v[e]) * u[e];
-            });
-            store4(static_cast<bf16*>(p.C) + (int64_t)row * p.ldc + col, n, p.c_vec, h);
+            if (n > 0)
+                with_act(p.act, [&](auto act) {
+                    store4(static_cast<bf16*>(p.C) + (int64_t)row * p.ldc + col, n, p.c_vec, mul2(act.value(two_of(v[0], v[1])), two_of(u[0], u[1])),
+                           mul2(act.value(two_of(v[2], v[3])), two_of(u[2], u[3])));
+                });
         } else {
-            const bf16* at = p.gu + (int64_t)row * p.ldgu + col;
-            const uint2 g = load4(at, n, p.four), u = load4(at + p.N, n, p.four);
-            write_grad4(p, row, col, v, g, u);
+            if (n > 0) {
+                const uint64_t dh[2] = {two_of(v[0], v[1]), two_of(v[2], v[3])};
+                const Four g = load_kept(p.kept, 0, row, col), u = load_kept(p.kept, 1, row, col);
+                with_act(p.act, [&](auto act) { write_grad4(p, act, row, col, dh, g, u); });
+            }
         }
     }
 }
@@ -369,6 +539,7 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const uint32_t csize = CG == 2 ? 2 : p.split;
     const uint32_t t0 = blockIdx.x / csize, tstep = gridDim.x / csize;
     const int kb0 = (int)((int64_t)p.kblocks * rank / p.split), kb1 = (int)((int64_t)p.kblocks * (rank + 1) / p.split);
+    const int segment = KIND == PLAIN ? SEGMENT : kb1;   // (kb0 + kb1 is behind the end)
     bool failed = false;
 
     if (warp < WARP_EPI0) {
@@ -420,10 +591,10 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const uint64_t desc0 = swizzled_desc(smem, PART);
                 uint32_t s = 0, ph = 0, seg = 0;
                 for (uint32_t t = t0; t < p.tiles && !failed; t += tstep)
-                    for (int k0 = kb0; k0 < kb1 && !failed; k0 += SEGMENT, ++seg) {
+                    for (int k0 = kb0; k0 < kb1 && !failed; k0 += segment, ++seg) {
                         const uint32_t buf = seg & 1u, d = tmem + buf * 256u;
                         if (!warp_wait_soon(acc_empty + 8u * buf, ((seg >> 1) & 1u) ^ 1u)) { failed = true; break; }
-                        const int k1 = k0 + SEGMENT < kb1 ? k0 + SEGMENT : kb1;
+                        const int k1 = k0 + segment < kb1 ? k0 + segment : kb1;
                         for (int kb = k0; kb < k1; ++kb) {
                             if (!warp_wait_soon(full + 8u * s, ph)) { failed = true; break; }
                             tc_fence_after();
@@ -449,8 +620,26 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
             int tm, tn;
             tile_of(p, t, tm, tn);
+            const int row0 = (tm * CG + pair_rank) * BM + quad * 32;
+            if constexpr (KIND == GRAD) {
+                if (CG == 2 || p.split == 1) {           // (one segment: see SEGMENT)
+                    const uint32_t buf = seg & 1u;
+                    const int col0 = tn * BN + half * CW;
+                    Four next[16];
+                    load_grad(p, row0, p.M - row0, col0 + (lane & 7) * 4, next);
+                    if (!warp_wait_soon(acc_full + 8u * buf, (seg >> 1) & 1u)) { failed = true; break; }
+                    tc_fence_after();
+                    write_grad<BN>(p, staging, tmem + ((uint32_t)(quad * 32) << 16) + buf * 256u + half * CW, row0, col0, next, [&] {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive<CG>(freed + 8u * buf);
+                    });
+                    ++seg;
+                    continue;
+                }
+            }
             float acc[CW];
-            for (int k0 = kb0; k0 < kb1; k0 += SEGMENT, ++seg) {
+            for (int k0 = kb0; k0 < kb1; k0 += segment, ++seg) {
                 const uint32_t buf = seg & 1u;
                 if (!warp_wait_soon(acc_full + 8u * buf, (seg >> 1) & 1u)) { failed = true; break; }
                 tc_fence_after();
@@ -477,8 +666,8 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 }
             }
             if (failed) break;
-            if (CG == 2 || p.split == 1) {
-                write_tile<KIND, BN, C>(p, staging, (tm * CG + pair_rank) * BM + quad * 32, tn, half, acc);
+            if (KIND != GRAD && (CG == 2 || p.split == 1)) {
+                write_tile<KIND, BN, C>(p, staging, row0, tn, half, acc);
                 __syncwarp();
             } else if constexpr (KIND == GATE) {
                 store_partial<BN>(smem, p.M - tm * BM, quad * 32 + lane, half * (CW / 2), CW / 2, acc);
@@ -616,18 +805,27 @@ cudaError_t launch_matmul16(const Matmul16Args& a, int num_sms, cudaStream_t s, 
     return launch(p, PLAIN, a.type, a.A, a.lda, a.trans_a, a.B, a.ldb, a.trans_b, a.M, a.N, a.K, a.status, num_sms, s, launches);
 }
 
+namespace {
+Kept kept_of(const void* p, int64_t tokens, int64_t hidden) {
+    const int64_t cols = (hidden + 15) / 16 * 16, plane = tokens * cols;
+    uint16_t* high = static_cast<uint16_t*>(const_cast<void*>(p));
+    return {high, reinterpret_cast<uint8_t*>(high + 2 * plane), plane, cols};
+}
+}  // namespace
+size_t gated_kept_bytes(int64_t tokens, int64_t hidden) { return (size_t)tokens * (size_t)((hidden + 15) / 16 * 16) * 6; }
+
 cudaError_t launch_gated_in(const GatedInArgs& a, int num_sms, cudaStream_t s, uint64_t* launches) {
     Params p = {};
-    p.C = a.h; p.ldc = a.ldh; p.keep = static_cast<bf16*>(a.gu); p.ldgu = a.ldgu; p.act = a.act;
+    p.C = a.h; p.ldc = a.ldh; p.act = a.act;
+    if (a.kept) p.kept = kept_of(a.kept, a.tokens, a.hidden);
     p.c_vec = on(a.h, a.ldh, 16, 2);
-    p.gu_vec = a.gu && on(a.gu, a.ldgu, 16, 2) && a.hidden % 8 == 0;
     return launch(p, GATE, CERAR_TYPE_BF16, a.x, a.ldx, false, a.w, a.ldw, true, a.tokens, 2 * a.hidden, a.width, a.status, num_sms, s, launches);
 }
 
 cudaError_t launch_gated_grad(const GatedGradArgs& a, int num_sms, cudaStream_t s, uint64_t* launches) {
     Params p = {};
-    p.C = a.dgu; p.ldc = a.lddgu; p.gu = static_cast<const bf16*>(a.gu); p.ldgu = a.ldgu; p.act = a.act;
-    p.four = on(a.dgu, a.lddgu, 8, 2) && on(a.gu, a.ldgu, 8, 2) && a.hidden % 4 == 0;
+    p.C = a.dgu; p.ldc = a.lddgu; p.kept = kept_of(a.kept, a.tokens, a.hidden); p.h = static_cast<bf16*>(a.h); p.ldh = a.ldh; p.act = a.act;
+    p.four = on(a.dgu, a.lddgu, 8, 2) && (!a.h || on(a.h, a.ldh, 8, 2)) && a.hidden % 4 == 0;
     return launch(p, GRAD, CERAR_TYPE_BF16, a.dy, a.lddy, false, a.w, a.ldw, false, a.tokens, a.hidden, a.width, a.status, num_sms, s, launches);
 }
 

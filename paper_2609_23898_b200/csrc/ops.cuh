@@ -177,20 +177,21 @@ struct GatedInArgs {
     int64_t ldx, ldw;
     int64_t tokens, width, hidden;
     int act;
-    void *h, *gu;                        // gu: null where nothing is kept
-    int64_t ldh, ldgu;
+    void *h, *kept;                      // kept: null where nothing is
+    int64_t ldh;
     int* status;
 };
 cudaError_t launch_gated_in(const GatedInArgs& a, int num_sms, cudaStream_t s, uint64_t* launches);
 struct GatedGradArgs {
-    const void *dy, *w, *gu;
-    int64_t lddy, ldw, ldgu;
+    const void *dy, *w, *kept;
+    int64_t lddy, ldw;
     int64_t tokens, width, hidden;
     int act;
-    void* dgu;
-    int64_t lddgu;
+    void *dgu, *h;                       // h: null where it is not wanted
+    int64_t lddgu, ldh;
     int* status;
 };
+size_t gated_kept_bytes(int64_t tokens, int64_t hidden);
 cudaError_t launch_gated_grad(const GatedGradArgs& a, int num_sms, cudaStream_t s, uint64_t* launches);
 
 }  // namespace cerar

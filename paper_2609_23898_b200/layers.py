@@ -342,48 +342,51 @@ def _gated_sizes(x, w_in, w_out, activation):
 
 
 def _gated(ops, x, w_in, w_out, activation, keep):
-    """x as a matrix; returns y, g and u (kept), h."""
+    """x as a matrix; returns y and the kept g and u."""
     t, d = x.shape
     o, f = w_out.shape
     wi = _operand(w_in, "w_in")
     h = _padded(t, f, x.device)
-    gu = _padded(t, 2 * f, x.device) if keep else None
+    gu = torch.empty(lib.cerar_gated_kept_bytes(t, f), dtype=torch.uint8, device=x.device) if keep else None
     st = lib.cerar_gated_in(ops._h, x.data_ptr(), _ld8(x), wi.data_ptr(), _ld8(wi), t, d, f, _ACTIVATIONS[activation], h.data_ptr(), _ld8(h),
-                            None if gu is None else gu.data_ptr(), 0 if gu is None else _ld8(gu), _stream(x.device.index))
+                            None if gu is None else gu.data_ptr(), _stream(x.device.index))
     if st:
         _check(st)
     y = _matmul(ops, h, False, _operand(w_out, "w_out"), True, t, o, f, torch.empty(t, o, dtype=_BF16, device=x.device), False)
-    return y, gu, h
+    return y, gu
 
 
 def gated(ops: Ops, x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *, activation: str = "silu", keep=False):
     """(act(x w_g^T) * (x w_u^T)) w_out^T for x (..., inputs), w_in = w_g over w_u (2 hidden x inputs) and w_out (outputs x hidden), all bfloat16.
-    activation: silu, gelu, gelu_tanh or relu.  With keep also what gated_backward wants of it: (x, g and u, h, the activation)."""
+    activation: silu, gelu, gelu_tanh or relu.  With keep also what gated_backward wants of it: (x, g and u in 24 bits, the activation)."""
     _same_device(ops, x=x, w_in=w_in, w_out=w_out)
     _gated_sizes(x, w_in, w_out, activation)
     xm = _operand(_rows(x), "x")
-    y, gu, h = _gated(ops, xm, w_in, w_out, activation, keep)
+    y, gu = _gated(ops, xm, w_in, w_out, activation, keep)
     y = y.view(*x.shape[:-1], y.size(-1))
-    return (y, (xm, gu, h, activation)) if keep else y
+    return (y, (xm, gu, activation)) if keep else y
 
 
 def _gated_backward(ops, dy, kept, w_in, w_out, dw_in, dw_out, accumulate, need_dx):
-    x, gu, h, activation = kept
+    x, gu, activation = kept
     (t, d), (o, f) = x.shape, w_out.shape
+    if not (o and f):                                                # nothing reaches x or w_in, and w_out has no elements
+        if dw_in is not None and not accumulate:
+            dw_in.zero_()
+        return torch.zeros(t, d, dtype=_BF16, device=x.device) if need_dx else None
     dx = None
-    if dw_out is not None:
+    wo, dgu = _operand(w_out, "w_out"), _padded(t, 2 * f, x.device)
+    h = None if dw_out is None else _padded(t, f, x.device)
+    st = lib.cerar_gated_grad(ops._h, dy.data_ptr(), _ld8(dy), wo.data_ptr(), _ld8(wo), t, o, f, _ACTIVATIONS[activation], gu.data_ptr(), dgu.data_ptr(),
+                              _ld8(dgu), None if h is None else h.data_ptr(), 0 if h is None else _ld8(h), _stream(x.device.index))
+    if st:
+        _check(st)
+    if need_dx:
+        dx = _matmul(ops, dgu, False, _operand(w_in, "w_in"), False, t, d, 2 * f, torch.empty(t, d, dtype=_BF16, device=x.device), False)
+    if dw_in is not None:
+        _matmul(ops, dgu, True, x, False, 2 * f, d, t, dw_in, accumulate)
+    if h is not None:
         _matmul(ops, dy, True, h, False, o, f, t, dw_out, accumulate)
-    if dw_in is not None or need_dx:
-        wo = _operand(w_out, "w_out")
-        dgu = _padded(t, 2 * f, x.device)
-        st = lib.cerar_gated_grad(ops._h, dy.data_ptr(), _ld8(dy), wo.data_ptr(), _ld8(wo), t, o, f, _ACTIVATIONS[activation], gu.data_ptr(), _ld8(gu),
-                                  dgu.data_ptr(), _ld8(dgu), _stream(x.device.index))
-        if st:
-            _check(st)
-        if need_dx:
-            dx = _matmul(ops, dgu, False, _operand(w_in, "w_in"), False, t, d, 2 * f, torch.empty(t, d, dtype=_BF16, device=x.device), False)
-        if dw_in is not None:
-            _matmul(ops, dgu, True, x, False, 2 * f, d, t, dw_in, accumulate)
     return dx
 
 
@@ -391,7 +394,7 @@ def gated_backward(ops: Ops, dy: torch.Tensor, kept, w_in: torch.Tensor, w_out: 
                    accumulate=True, need_dx=True):
     """dx from dy and what gated kept; dw_in and dw_out (float32 or bfloat16, e.g. slices of the gradient vector; None: not wanted) += the
     gradients of the weights."""
-    x, gu, h, activation = kept
+    x, gu, activation = kept
     _same_device(ops, dy=dy, x=x, w_in=w_in, w_out=w_out, dw_in=dw_in, dw_out=dw_out)
     _gated_sizes(x, w_in, w_out, activation)
     for what, dw, w in (("dw_in", dw_in, w_in), ("dw_out", dw_out, w_out)):
@@ -423,7 +426,7 @@ class Gated(torch.autograd.Function):
             return gated(ops, x, w_in, w_out, activation=activation)
         y, kept = gated(ops, x, w_in, w_out, activation=activation, keep=True)
         ctx.ops, ctx.dw, ctx.activation = ops, (dw_in, dw_out), activation
-        ctx.save_for_backward(*kept[:3], w_in, w_out)
+        ctx.save_for_backward(*kept[:2], w_in, w_out)
         return y
 
     @staticmethod

@@ -4,7 +4,7 @@ Products: operands are small integers, which bfloat16 holds exactly, and all sum
 where the result is bfloat16.  No tolerance.
 
 Block: against the formulas in 64 bits, by intervals.  A sum of K products from the tensor cores is within e S of itself, S the sum of the magnitudes,
-e = 2^-23 (264 + K / 4096).  A value kept in bfloat16 is off by 2^-8 of itself more.  The activation and its derivative move by at most 1.13 and 1 (their
+e = 2^-23 (264 + K / 4096), in the gate's own products 2^-23 (8 + K / 16).  A value rounded to bfloat16 is off by 2^-8 of itself more, one kept in 24 bits by 2^-16.  The activation and its derivative move by at most 1.13 and 1 (their
 own largest slopes) times what their argument moves, and the hardware's exponential and quotient are 2^-20 (1 + |g|) off.  An interval around every
 factor gives one around every product, and sums of those give the ones behind the next product.
 """
@@ -166,11 +166,11 @@ class Near:
     def __mul__(self, o):
         return Near(self.v * o.v, (self.v.abs() + self.off) * (o.v.abs() + o.off) - self.v.abs() * o.v.abs())
 
-    def kept(self):
-        return Near(self.v, self.off * (1 + 2.0 ** -8) + self.v.abs() * 2.0 ** -8)
+    def kept(self, u=2.0 ** -8):
+        return Near(self.v, self.off * (1 + u) + self.v.abs() * u)
 
     def product(self, w, k):
-        e = 2.0 ** -23 * (264 + k / 4096)
+        e = 2.0 ** -23 * max(264 + k / 4096, 8 + k / 16)
         return Near(self.v @ w, self.off @ w.abs() * (1 + e) + e * (self.v.abs() @ w.abs()))
 
     def plus_one(self):
@@ -201,13 +201,14 @@ def block(x, w_in, w_out, dy, act):
 
     h = (around(g, 1.13, 0) * u).kept()
     y = h.product(w_out.t(), f)
-    gk, uk = g.kept(), u.kept()
+    gk, uk = g.kept(2.0 ** -16), u.kept(2.0 ** -16)
     dh = exactly(dy).product(w_out, w_out.size(0))
     dg, du = (dh * uk * around(gk, 1.0, 1)).kept(), (dh * around(gk, 1.13, 0)).kept()
     import torch
     dgu = Near(torch.cat((dg.v, du.v), 1), torch.cat((dg.off, du.off), 1))
     dx = dgu.product(w_in, 2 * f)
     dw_in = Near(dgu.v.t().contiguous(), dgu.off.t().contiguous()).product(x, t)
+    h = (around(gk, 1.13, 0) * uk).kept()
     dw_out = Near(h.v.t().contiguous(), h.off.t().contiguous()).product(dy, t)
     return y, dx, dw_in, Near(dw_out.v.t(), dw_out.off.t())
 
