@@ -47,14 +47,13 @@ constexpr int SEGMENT = 64;                             // 4096 values of k: 256
 enum { PLAIN = 0, GATE = 1, GRAD = 2 };
 
 struct Kept {
-    uint16_t* high;
-    uint8_t* low;
-    int64_t plane, cols;                               // plane = tokens * cols
+    unsigned char* at;
+    int64_t blocks;                                    // of 32 columns, in a row of blocks
 };
 struct Params {
     void* C;                                           // PLAIN: C; GATE: h; GRAD: [dg du]
     int64_t ldc;
-    Kept kept;                                         // GATE: where g and u go (high null: nowhere); GRAD: where they are
+    Kept kept;                                         // GATE: where g and u go (null: nowhere); GRAD: where they are
     bf16* h;                                           // GRAD: h, or null
     int64_t ldh;
     int M, N, kblocks;                                 // N: columns of C (GATE, GRAD: of h)
@@ -209,11 +208,16 @@ __device__ __forceinline__ void with_act(int act, F f) {
 
 // ---------------------------------------------------------------- what is kept for the backward pass
 //
-// g and u in 24 bits: sign, exponent and 15 bits of the fraction, rounded to nearest (2^-16 of themselves off), the upper 16 bits of all values in one
-// plane, the lower 8 in another.  Kept in bfloat16 their rounding would be the largest part of the error of dx and dw_in (3.0e-3 instead of
-// 2.4e-3 of the norm); h is made again from them, so that no more is kept than g, u and h in bfloat16 would be.
-// Planes: [g, u][tokens][cols], cols the hidden size rounded up to 16.
+// g and u in 24 bits: sign, exponent and 15 bits of the fraction, rounded to nearest (2^-16 of themselves off).  Kept in bfloat16 their rounding would
+// be the largest part of the error of dx and dw_in (3.0e-3 instead of 2.3e-3 of the norm); h is made again from them, so that no more is kept
+// than g, u and h in bfloat16 would be.
+// They lie in blocks of 32 rows x 32 columns, 6 KB each: the upper 16 bits of g in pieces of 16 bytes (8 columns), piece j of row r at
+// (32 j + r) 16; the same of u; the lower 8 bits of g in pieces of 16 columns; the same of u.  A warp that holds a row per lane so reads and writes
+// 512 bytes at a time with no exchange between lanes, and a block is one run of memory (in rows of their own the reads came in pieces of 64 bytes
+// that were a row of the matrix apart: 16384 x 8192 x 2048 562 us).
 
+constexpr int64_t KEPT_BLOCK = 6144;
+__device__ __forceinline__ unsigned char* kept_block(const Kept& k, int row, int col) { return k.at + ((int64_t)(row >> 5) * k.blocks + (col >> 5)) * KEPT_BLOCK; }
 __device__ __forceinline__ uint32_t to24(float x) {    // (a carry into the exponent is right; NaN keeps its upper bits)
     const uint32_t b = __float_as_uint(x);
     return x != x ? b | 0x00400000u : b + 0x80u;
@@ -222,25 +226,64 @@ __device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) { return __byt
 __device__ __forceinline__ uint32_t lows(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0051), __byte_perm(c, d, 0x0051), 0x5410);
 }
-struct Four {                                          // four neighbouring values of one plane pair
+// values 2 i and 2 i + 1 of four, from their upper and lower bits
+__device__ __forceinline__ uint64_t pair_of(uint32_t h, uint32_t low, int i) {
+    const uint32_t x = __byte_perm(h, low, i ? 0x1066 : 0x1044) & 0xFFFFFF00u, y = __byte_perm(h, low, i ? 0x3277 : 0x3255) & 0xFFFFFF00u;
+    return two_of(__uint_as_float(x), __uint_as_float(y));
+}
+// four neighbouring values of one row
+struct Four {
     uint2 high;
     uint32_t low;
 };
-__device__ __forceinline__ Four load_kept(const Kept& k, int which, int64_t row, int col) {
-    const int64_t at = which * k.plane + row * k.cols + col;
-    return {__ldg(reinterpret_cast<const uint2*>(k.high + at)), __ldg(reinterpret_cast<const uint32_t*>(k.low + at))};
+__device__ __forceinline__ Four load_kept(const Kept& k, int which, int row, int col) {
+    const unsigned char* b = kept_block(k, row, col);
+    const int r = row & 31, c = col & 31;
+    return {__ldg(reinterpret_cast<const uint2*>(b + which * 2048 + ((c >> 3) * 32 + r) * 16 + (c & 7) * 2)),
+            __ldg(reinterpret_cast<const uint32_t*>(b + 4096 + which * 1024 + ((c >> 4) * 32 + r) * 16 + (c & 15)))};
 }
-__device__ __forceinline__ void store_kept(const Kept& k, int which, int64_t row, int col, const float* v) {
-    const int64_t at = which * k.plane + row * k.cols + col;
-    const uint32_t a = to24(v[0]), b = to24(v[1]), c = to24(v[2]), d = to24(v[3]);
-    *reinterpret_cast<uint2*>(k.high + at) = make_uint2(highs(a, b), highs(c, d));
-    *reinterpret_cast<uint32_t*>(k.low + at) = lows(a, b, c, d);
+__device__ __forceinline__ void store_kept(const Kept& k, int which, int row, int col, const float* v) {
+    unsigned char* b = kept_block(k, row, col);
+    const int r = row & 31, c = col & 31;
+    const uint32_t x = to24(v[0]), y = to24(v[1]), z = to24(v[2]), w = to24(v[3]);
+    *reinterpret_cast<uint2*>(b + which * 2048 + ((c >> 3) * 32 + r) * 16 + (c & 7) * 2) = make_uint2(highs(x, y), highs(z, w));
+    *reinterpret_cast<uint32_t*>(b + 4096 + which * 1024 + ((c >> 4) * 32 + r) * 16 + (c & 15)) = lows(x, y, z, w);
 }
-// values 2 i and 2 i + 1 of four
-__device__ __forceinline__ uint64_t pair_of(const Four& f, int i) {
-    const uint32_t h = i ? f.high.y : f.high.x;
-    const uint32_t x = __byte_perm(h, f.low, i ? 0x1066 : 0x1044) & 0xFFFFFF00u, y = __byte_perm(h, f.low, i ? 0x3277 : 0x3255) & 0xFFFFFF00u;
-    return two_of(__uint_as_float(x), __uint_as_float(y));
+// 32 values of a lane's row to a block, and the loads of both g's and u's
+__device__ __forceinline__ void store_kept32(unsigned char* block, int which, const float* v) {
+    const int lane = threadIdx.x & 31;
+    uint32_t low[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t b[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = to24(v[8 * j + e]);
+        *reinterpret_cast<uint4*>(block + which * 2048 + (j * 32 + lane) * 16) = make_uint4(highs(b[0], b[1]), highs(b[2], b[3]), highs(b[4], b[5]), highs(b[6], b[7]));
+        low[2 * j] = lows(b[0], b[1], b[2], b[3]);
+        low[2 * j + 1] = lows(b[4], b[5], b[6], b[7]);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        *reinterpret_cast<uint4*>(block + 4096 + which * 1024 + (j * 32 + lane) * 16) = make_uint4(low[4 * j], low[4 * j + 1], low[4 * j + 2], low[4 * j + 3]);
+}
+struct Kept32 {
+    uint4 high[2][4], low[2][2];
+};
+__device__ __forceinline__ void load_kept32(const unsigned char* block, Kept32& k) {     // (volatile: issued here, not where they are used)
+    const unsigned char* at = block + (threadIdx.x & 31) * 16;
+    auto load = [](const unsigned char* p, uint4& q) { asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(p)); };
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load(at + which * 2048 + j * 512, k.high[which][j]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) load(at + 4096 + which * 1024 + j * 512, k.low[which][j]);
+    }
+}
+__device__ __forceinline__ uint32_t word(const uint4& q, int i) { return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w; }
+// values 2 i and 2 i + 1 (i < 16) of g (which = 0) or u
+__device__ __forceinline__ uint64_t pair_of(const Kept32& k, int which, int i) {
+    return pair_of(word(k.high[which][i >> 2], i & 3), word(k.low[which][i >> 3], (i >> 1) & 3), i & 1);
 }
 
 // ---------------------------------------------------------------- writing
@@ -287,26 +330,6 @@ __device__ __forceinline__ void write_rows(uint32_t staging, bf16* c, int64_t ld
     }
 }
 
-// 32 rows of `words` 32-bit words each (a multiple of 4, at most 32; the warp holds row (lane)'s) to rows `pitch` bytes apart of which nrows and
-// `bytes` bytes exist, all on 16-byte boundaries and a multiple of 16 bytes.
-template <int WORDS>
-__device__ __forceinline__ void write_words(uint32_t staging, unsigned char* dst, int64_t pitch, int nrows, int bytes, const uint32_t* v) {
-    constexpr int PER_ROW = WORDS / 4, ROWS = 32 / PER_ROW;
-    const int lane = threadIdx.x & 31, j = lane % PER_ROW;
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < PER_ROW; ++i)
-        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
-    __syncwarp();
-#pragma unroll
-    for (int it = 0; it < 32 / ROWS; ++it) {
-        const int r = it * ROWS + lane / PER_ROW;
-        uint4 q;
-        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
-        if (r < nrows && 16 * j < bytes) *reinterpret_cast<uint4*>(dst + r * pitch + 16 * j) = q;
-    }
-}
-
 // Four columns of a row to bfloat16, `n` of them there
 __device__ __forceinline__ void store4(bf16* p, int n, bool vec, uint64_t lo, uint64_t hi) {
     float v[4];
@@ -328,8 +351,8 @@ __device__ __forceinline__ void write_grad4(const Params& p, A act, int row, int
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         uint64_t a, d;
-        const uint64_t up = pair_of(u, i);
-        act.both(pair_of(g, i), a, d);
+        const uint64_t up = pair_of(i ? u.high.y : u.high.x, u.low, i);
+        act.both(pair_of(i ? g.high.y : g.high.x, g.low, i), a, d);
         dg[i] = mul2(mul2(dh[i], up), d);
         du[i] = mul2(dh[i], a);
         h[i] = mul2(a, up);
@@ -338,19 +361,6 @@ __device__ __forceinline__ void write_grad4(const Params& p, A act, int row, int
     store4(c, n, p.four, dg[0], dg[1]);
     store4(c + p.N, n, p.four, du[0], du[1]);
     if (p.h) store4(p.h + (int64_t)row * p.ldh + col, n, p.four, h[0], h[1]);
-}
-
-// g and u of four columns (this lane's) of every fourth row
-__device__ __forceinline__ void load_grad(const Params& p, int row0, int nrows, int col, Four* next) {
-    const int r0 = (threadIdx.x & 31) >> 3;
-#pragma unroll
-    for (int it = 0; it < 8; ++it) {
-        next[2 * it] = next[2 * it + 1] = {make_uint2(0u, 0u), 0u};
-        if (it * 4 + r0 < nrows && col < p.N) {
-            next[2 * it] = load_kept(p.kept, 0, row0 + it * 4 + r0, col);
-            next[2 * it + 1] = load_kept(p.kept, 1, row0 + it * 4 + r0, col);
-        }
-    }
 }
 
 // The whole tile's sums of this warp: rows row0 .. row0 + 31, CW columns, in registers.
@@ -366,25 +376,14 @@ __device__ __forceinline__ void write_tile(const Params& p, uint32_t staging, in
         constexpr int FW = BN / 4;                      // columns of h: acc holds their g, then their u
         const int col0 = tn * (BN / 2) + half * FW, nrows = p.M - row0 < 32 ? p.M - row0 : 32;
         if (nrows <= 0 || col0 >= p.N) return;
-        if (p.kept.high) {
-            uint32_t low[FW / 2];
-            const int cols = (int)(p.kept.cols - col0 < FW ? p.kept.cols - col0 : FW);
-            const int64_t at = (int64_t)row0 * p.kept.cols + col0;
+        if (p.kept.at && lane < nrows) {
+            unsigned char* block = kept_block(p.kept, row0, col0);
 #pragma unroll
-            for (int which = 0; which < 2; ++which) {
-                uint32_t high[FW / 2];
-#pragma unroll
-                for (int j = 0; j < FW; j += 4) {
-                    const float* v = acc + which * FW + j;
-                    const uint32_t a = to24(v[0]), b = to24(v[1]), c = to24(v[2]), d = to24(v[3]);
-                    high[j / 2] = highs(a, b);
-                    high[j / 2 + 1] = highs(c, d);
-                    low[which * (FW / 4) + j / 4] = lows(a, b, c, d);
-                }
-                write_words<FW / 2>(staging, reinterpret_cast<unsigned char*>(p.kept.high + which * p.kept.plane + at), 2 * p.kept.cols, nrows, 2 * cols, high);
+            for (int c = 0; c < FW; c += 32) {
+                if (col0 + c >= p.N) break;
+                store_kept32(block + c / 32 * KEPT_BLOCK, 0, acc + c);
+                store_kept32(block + c / 32 * KEPT_BLOCK, 1, acc + FW + c);
             }
-            write_words<FW / 4>(staging, p.kept.low + at, p.kept.cols, nrows, cols, low);
-            write_words<FW / 4>(staging, p.kept.low + p.kept.plane + at, p.kept.cols, nrows, cols, low + FW / 4);
         }
         with_act(p.act, [&](auto act) {
 #pragma unroll
@@ -394,38 +393,37 @@ __device__ __forceinline__ void write_tile(const Params& p, uint32_t staging, in
     }
 }
 
-// GRAD: dh comes from tensor memory (`from`: this warp's lanes and columns) 32 columns at a time and goes through the staging rows, so that the
-// rows of g, u, dg, du and h are touched in pieces of 64 bytes; g and u of the next 32 columns are on their way meanwhile (next: of the first).
-template <int BN, typename Release>
-__device__ __forceinline__ void write_grad(const Params& p, uint32_t staging, uint32_t from, int row0, int col0, Four* next, Release release) {
+// GRAD: dh comes from tensor memory (`from`: this warp's lanes and columns) 32 columns at a time, a row per lane, as g and u do; those of the next 32
+// columns are on their way meanwhile (next: of the first).
+template <int BN, typename A, typename Release>
+__device__ __forceinline__ void write_grad(const Params& p, A act, uint32_t staging, uint32_t from, int row0, int col0, Kept32& next, Release release) {
     constexpr int CW = BN / 2;
-    const int lane = threadIdx.x & 31, nrows = p.M - row0 < 32 ? p.M - row0 : 32, r0 = lane >> 3, j = lane & 7;
-    with_act(p.act, [&](auto act) {
+    const bool there = row0 + (int)(threadIdx.x & 31) < p.M;
 #pragma unroll 1
-        for (int h = 0; h < CW / 32; ++h) {
-            const int col = col0 + h * 32 + j * 4;
-            uint32_t v[32];
-            ld32_start(from + h * 32, v);
-            ld32_done(v);
-            if (h + 1 == CW / 32) release();
-            __syncwarp();
+    for (int h = 0; h < CW / 32; ++h) {
+        const int col = col0 + h * 32;
+        uint32_t v[32];
+        ld32_start(from + h * 32, v);
+        const Kept32 now = next;
+        if (h + 1 < CW / 32 && there && col + 32 < p.N) load_kept32(kept_block(p.kept, row0, col + 32), next);
+        ld32_done(v);
+        if (h + 1 == CW / 32) release();
+        if (row0 >= p.M || col >= p.N) continue;
+        float dg[32], du[32], hv[32];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
-            Four now[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) now[i] = next[i];
-            if (h + 1 < CW / 32) load_grad(p, row0, nrows, col + 32, next);
-            __syncwarp();
-#pragma unroll
-            for (int it = 0; it < 8; ++it) {
-                const int r = it * 4 + r0;
-                uint64_t dh[2];
-                asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(dh[0]), "=l"(dh[1]) : "r"(staging + r * 128 + ((j ^ (r & 7)) << 4)) : "memory");
-                if (r < nrows && col < p.N) write_grad4(p, act, row0 + r, col, dh, now[2 * it], now[2 * it + 1]);
-            }
+        for (int i = 0; i < 16; ++i) {
+            const uint64_t dh = two_of(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), up = pair_of(now, 1, i);
+            uint64_t a, d;
+            act.both(pair_of(now, 0, i), a, d);
+            parts(mul2(mul2(dh, up), d), dg[2 * i], dg[2 * i + 1]);
+            parts(mul2(dh, a), du[2 * i], du[2 * i + 1]);
+            parts(mul2(a, up), hv[2 * i], hv[2 * i + 1]);
         }
-    });
+        bf16* c = static_cast<bf16*>(p.C);
+        write_rows<32>(staging, c, p.ldc, p.M, p.N, row0, col, dg, p.c_vec);
+        write_rows<32>(staging, c + p.N, p.ldc, p.M, p.N, row0, col, du, p.c_vec);
+        if (p.h) write_rows<32>(staging, p.h, p.ldh, p.M, p.N, row0, col, hv, p.c_vec);
+    }
 }
 
 // A tile whose sum is split over a cluster: every block leaves the rows of its partial tile that exist in its stages (free by then), row
@@ -477,7 +475,7 @@ __device__ __forceinline__ void add_partials(const Params& p, uint32_t smem, int
             // a row's columns of g are followed by the same ones of u
             const float4 u4 = add_piece(p, base + ((uint32_t)((j + PER_ROW) ^ (r & 7)) << 4));
             const float u[4] = {u4.x, u4.y, u4.z, u4.w};
-            if (p.kept.high && col < p.kept.cols) {
+            if (p.kept.at && n > 0) {
                 store_kept(p.kept, 0, row, col, v);
                 store_kept(p.kept, 1, row, col, u);
             }
@@ -625,14 +623,18 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 if (CG == 2 || p.split == 1) {           // (one segment: see SEGMENT)
                     const uint32_t buf = seg & 1u;
                     const int col0 = tn * BN + half * CW;
-                    Four next[16];
-                    load_grad(p, row0, p.M - row0, col0 + (lane & 7) * 4, next);
+                    Kept32 next = {};
+                    if (row0 + lane < p.M && col0 < p.N) load_kept32(kept_block(p.kept, row0, col0), next);
                     if (!warp_wait_soon(acc_full + 8u * buf, (seg >> 1) & 1u)) { failed = true; break; }
                     tc_fence_after();
-                    write_grad<BN>(p, staging, tmem + ((uint32_t)(quad * 32) << 16) + buf * 256u + half * CW, row0, col0, next, [&] {
+                    const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + buf * 256u + half * CW;
+                    auto release = [&] {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) arrive<CG>(freed + 8u * buf);
+                    };
+                    with_act(p.act, [&](auto act) {
+                        write_grad<BN>(p, act, staging, from, row0, col0, next, release);
                     });
                     ++seg;
                     continue;
@@ -806,26 +808,23 @@ cudaError_t launch_matmul16(const Matmul16Args& a, int num_sms, cudaStream_t s, 
 }
 
 namespace {
-Kept kept_of(const void* p, int64_t tokens, int64_t hidden) {
-    const int64_t cols = (hidden + 15) / 16 * 16, plane = tokens * cols;
-    uint16_t* high = static_cast<uint16_t*>(const_cast<void*>(p));
-    return {high, reinterpret_cast<uint8_t*>(high + 2 * plane), plane, cols};
-}
+Kept kept_of(const void* p, int64_t hidden) { return {static_cast<unsigned char*>(const_cast<void*>(p)), (hidden + 31) / 32}; }
 }  // namespace
-size_t gated_kept_bytes(int64_t tokens, int64_t hidden) { return (size_t)tokens * (size_t)((hidden + 15) / 16 * 16) * 6; }
+size_t gated_kept_bytes(int64_t tokens, int64_t hidden) { return (size_t)((tokens + 31) / 32) * (size_t)((hidden + 31) / 32) * KEPT_BLOCK; }
 
 cudaError_t launch_gated_in(const GatedInArgs& a, int num_sms, cudaStream_t s, uint64_t* launches) {
     Params p = {};
     p.C = a.h; p.ldc = a.ldh; p.act = a.act;
-    if (a.kept) p.kept = kept_of(a.kept, a.tokens, a.hidden);
+    if (a.kept) p.kept = kept_of(a.kept, a.hidden);
     p.c_vec = on(a.h, a.ldh, 16, 2);
     return launch(p, GATE, CERAR_TYPE_BF16, a.x, a.ldx, false, a.w, a.ldw, true, a.tokens, 2 * a.hidden, a.width, a.status, num_sms, s, launches);
 }
 
 cudaError_t launch_gated_grad(const GatedGradArgs& a, int num_sms, cudaStream_t s, uint64_t* launches) {
     Params p = {};
-    p.C = a.dgu; p.ldc = a.lddgu; p.kept = kept_of(a.kept, a.tokens, a.hidden); p.h = static_cast<bf16*>(a.h); p.ldh = a.ldh; p.act = a.act;
+    p.C = a.dgu; p.ldc = a.lddgu; p.kept = kept_of(a.kept, a.hidden); p.h = static_cast<bf16*>(a.h); p.ldh = a.ldh; p.act = a.act;
     p.four = on(a.dgu, a.lddgu, 8, 2) && (!a.h || on(a.h, a.ldh, 8, 2)) && a.hidden % 4 == 0;
+    p.c_vec = on(a.dgu, a.lddgu, 16, 2) && (!a.h || on(a.h, a.ldh, 16, 2)) && a.hidden % 8 == 0;
     return launch(p, GRAD, CERAR_TYPE_BF16, a.dy, a.lddy, false, a.w, a.ldw, false, a.tokens, a.hidden, a.width, a.status, num_sms, s, launches);
 }
 
