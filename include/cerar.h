@@ -663,8 +663,8 @@ cerar_status_t cerar_rotation_table(cerar_ops_t* ops, const double* freqs, int p
 cerar_status_t cerar_matmul_bf16(cerar_ops_t* ops, const void* A, int64_t lda, int trans_a, const void* B, int64_t ldb, int trans_b,
                                  int64_t M, int64_t N, int64_t K, void* C, cerar_type_t type, int64_t ldc, int accumulate,
                                  cerar_stream_t stream);
-/* How it runs on a GPU of num_sms SMs, without a device: the columns of its tiles, 128 or 256 (of 128 rows; with 256: of 256 rows, by a pair
- * of blocks), and in *split the blocks that share the sum of a tile.  -1 for sizes that no product has. */
+/* How it runs on a GPU of num_sms SMs, without a device: 0 in tiles of 256 x 256 and 1 in tiles of 256 x 128, by pairs of blocks, 2 in tiles of
+ * 128 x 128, and in *split the blocks that share the sum of a tile.  -1 for sizes that no product has. */
 int            cerar_matmul_bf16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* split);
 
 /* The two products of a gated feed-forward block that carry its elementwise part.  The block, for x (tokens x width) and bfloat16 weights

@@ -5,7 +5,7 @@
 //   gate    [g u] = x W^T in one accumulator, h = act(g) u: a tile holds the same columns of both projections side by side
 //   grad    dh = dy W_out in the accumulator, dg = dh u act'(g) and du = dh act(g) from the kept g and u
 //
-// A tile of C is 256 x 256 by a pair of blocks (cta_group::2, each with its 128 rows of A and half of B), or 128 x 128 by one.  At 256 x 256
+// A tile of C is 256 x 256 or 256 x 128 by a pair of blocks (cta_group::2, each with its 128 rows of A and half of B), or 128 x 128 by one.  At 256 x 256
 // a k of 64 costs the tensor cores 256 clk and each block 32 KB of shared memory written and read; two accumulators fill tensor memory, so
 // that a tile is written while the next one's products run.  Operands are read in place whichever of their dimensions is contiguous.
 //
@@ -17,7 +17,7 @@
 // The accumulator drops what does not fit its 24 bits instead of rounding, an error that grows with the number of additions, so plain sums of more
 // than SEGMENT blocks of k are put together in registers.  (The gate's results have 16 bits, 24 at most: their sums stay in one piece, so that
 // GRAD can take dh out of tensor memory as it goes.)
-// Few tiles, long sums: a cluster of S blocks shares a tile, each sums 1/S of the blocks of k, and the partial tiles are added through
+// Few tiles, long sums: a cluster of S blocks or pairs shares a tile, each sums 1/S of the blocks of k, and the partial tiles are added through
 // distributed shared memory, in a fixed order.
 // Every wait is bounded; one that runs out sets the status word and the block leaves through the common exit.
 #include <cuda.h>
@@ -38,7 +38,7 @@ typedef __nv_bfloat16 bf16;
 
 constexpr int BK = 64;                                  // values of k in a stage: rows of 128 bytes
 constexpr int UK = 16;                                  // of one product
-constexpr int WARP_EPI0 = 4, THREADS = 32 * (WARP_EPI0 + EPI_WARPS), MAX_SPLIT = 8;
+constexpr int WARP_EPI0 = 4, THREADS = 32 * (WARP_EPI0 + EPI_WARPS), MAX_SPLIT = 8;      // blocks of a (portable) cluster
 // registers per thread: 128 x 56 + 256 x 224 = 384 x 168, what the block is launched with
 constexpr int REGS_FEW = 56, REGS_MANY = 224;
 constexpr uint32_t A_BYTES = BM * BK * 2, PART = 64 * BK * 2;      // an operand lies in parts of 64 of its own rows or columns
@@ -78,6 +78,13 @@ __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uin
     else
         asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
                      " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// a barrier of this block, or the one at the same place in both blocks of the pair (bits of `blocks`)
+template <int CG>
+__device__ __forceinline__ void commit_to(uint32_t bar, uint32_t blocks) {
+    if constexpr (CG == 1) tc_commit(bar);
+    else asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)blocks) : "memory");
 }
 
 // ---------------------------------------------------------------- activations
@@ -437,28 +444,29 @@ __device__ __forceinline__ void store_partial(uint32_t smem, int rows, int row, 
         asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + ((uint32_t)((col / 4 + j) ^ (row & 7)) << 4)), "f"(v[4 * j]), "f"(v[4 * j + 1]),
                      "f"(v[4 * j + 2]), "f"(v[4 * j + 3]) : "memory");
 }
-__device__ __forceinline__ float4 add_piece(const Params& p, uint32_t at) {
-    float4 w[MAX_SPLIT];
+template <int CG>
+__device__ __forceinline__ float4 add_piece(const Params& p, uint32_t at, int pair_rank) {
+    float4 w[MAX_SPLIT / CG];
 #pragma unroll
-    for (int q = 0; q < MAX_SPLIT; ++q)
-        if (q < p.split) w[q] = ld_cluster4(at, q);
+    for (int q = 0; q < MAX_SPLIT / CG; ++q)
+        if (q < p.split) w[q] = ld_cluster4(at, q * CG + pair_rank);
     float4 v = w[0];
 #pragma unroll
-    for (int q = 1; q < MAX_SPLIT; ++q)
+    for (int q = 1; q < MAX_SPLIT / CG; ++q)
         if (q < p.split) { v.x += w[q].x; v.y += w[q].y; v.z += w[q].z; v.w += w[q].w; }
     return v;
 }
 // ... and adds every split-th run of 32 pieces (a warp's) of all partial tiles, in the order of their blocks of k.
-template <int KIND, int BN, typename C>
-__device__ __forceinline__ void add_partials(const Params& p, uint32_t smem, int tm, int tn, int rows, int rank, int thread) {
+template <int CG, int KIND, int BN, typename C>
+__device__ __noinline__ void add_partials(const Params& p, uint32_t smem, int row0, int tn, int rows, int rank, int pair_rank, int thread) {
     constexpr int PER_ROW = KIND == GATE ? BN / 8 : BN / 4;
     const int pieces = rows * PER_ROW;
     for (int run = (thread >> 5) * p.split + rank; run * 32 < pieces; run += EPI_WARPS * p.split) {
         const int i = run * 32 + (thread & 31);
         if (i >= pieces) continue;
-        const int r = i / PER_ROW, j = i % PER_ROW, row = tm * BM + r;
+        const int r = i / PER_ROW, j = i % PER_ROW, row = row0 + r;
         const uint32_t base = smem + (uint32_t)r * (BN * 4u);
-        const float4 v4 = add_piece(p, base + ((uint32_t)(j ^ (r & 7)) << 4));
+        const float4 v4 = add_piece<CG>(p, base + ((uint32_t)(j ^ (r & 7)) << 4), pair_rank);
         const float v[4] = {v4.x, v4.y, v4.z, v4.w};
         const int col = tn * (PER_ROW * 4) + 4 * j, n = p.N - col;
         if constexpr (KIND == PLAIN) {
@@ -473,7 +481,7 @@ __device__ __forceinline__ void add_partials(const Params& p, uint32_t smem, int
             }
         } else if constexpr (KIND == GATE) {
             // a row's columns of g are followed by the same ones of u
-            const float4 u4 = add_piece(p, base + ((uint32_t)((j + PER_ROW) ^ (r & 7)) << 4));
+            const float4 u4 = add_piece<CG>(p, base + ((uint32_t)((j + PER_ROW) ^ (r & 7)) << 4), pair_rank);
             const float u[4] = {u4.x, u4.y, u4.z, u4.w};
             if (p.kept.at && n > 0) {
                 store_kept(p.kept, 0, row, col, v);
@@ -531,10 +539,10 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     if (p.early) grid_dependents_may_launch();
     grid_dependency_wait();
 
-    // a cluster is a pair of blocks that share a tile of 256 rows (CG = 2), or `split` blocks that share the sum of a tile
+    // a cluster is `split` blocks, or pairs of blocks (CG = 2: tiles of 256 rows), that share the sum of a tile
     const int crank = CG == 2 || p.split > 1 ? (int)cluster_rank() : 0;
-    const int pair_rank = CG == 2 ? crank : 0, rank = CG == 2 ? 0 : crank;
-    const uint32_t csize = CG == 2 ? 2 : p.split;
+    const int pair_rank = crank % CG, rank = crank / CG, leader = crank - pair_rank;
+    const uint32_t csize = CG * p.split;
     const uint32_t t0 = blockIdx.x / csize, tstep = gridDim.x / csize;
     const int kb0 = (int)((int64_t)p.kblocks * rank / p.split), kb1 = (int)((int64_t)p.kblocks * (rank + 1) / p.split);
     const int segment = KIND == PLAIN ? SEGMENT : kb1;   // (kb0 + kb1 is behind the end)
@@ -559,7 +567,7 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         if (!wait_soon(empty + 8u * s, ph)) { failed = true; break; }
                         const uint32_t a = smem + s * STAGE, b = a + A_BYTES;
                         if (pair_rank == 0) mbar_arrive_expect_tx(full + 8u * s, CG * (p.a_bytes + B_ROWS * BK * 2));       // what both blocks load
-                        const uint32_t bar = CG == 1 ? full + 8u * s : in_block(full + 8u * s, 0);
+                        const uint32_t bar = CG == 1 ? full + 8u * s : in_block(full + 8u * s, leader);
                         if (p.a_mn) {
                             tma_load_operand<CG>(a, &map_a, m0, kb * BK, bar);
                             tma_load_operand<CG>(a + PART, &map_a, m0 + 64, kb * BK, bar);
@@ -568,10 +576,10 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         }
                         if (p.b_mn) {
                             tma_load_operand<CG>(b, &map_b, n0, kb * BK, bar);
-                            tma_load_operand<CG>(b + PART, &map_b, n1, kb * BK, bar);
+                            if (B_ROWS > 64) tma_load_operand<CG>(b + PART, &map_b, n1, kb * BK, bar);
                         } else {
                             tma_load_operand<CG>(b, &map_b, kb * BK, n0, bar);
-                            tma_load_operand<CG>(b + PART, &map_b, kb * BK, n1, bar);
+                            if (B_ROWS > 64) tma_load_operand<CG>(b + PART, &map_b, kb * BK, n1, bar);
                         }
                         if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
                     }
@@ -600,8 +608,8 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                             if (one) {
 #pragma unroll
                                 for (int k = 0; k < BK / UK; ++k) mma_bf16<CG>(d, da + k * a_step, db + k * b_step, idesc, kb != k0 || k != 0);
-                                commit<CG>(empty + 8u * s);
-                                if (kb + 1 == k1) commit<CG>(acc_full + 8u * buf);
+                                commit_to<CG>(empty + 8u * s, 3u << leader);
+                                if (kb + 1 == k1) commit_to<CG>(acc_full + 8u * buf, 3u << leader);
                             }
                             __syncwarp();
                             if (++s == (uint32_t)p.stages) { s = 0; ph ^= 1u; }
@@ -613,32 +621,38 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY));
         const int quad = warp & 3, half = (warp - WARP_EPI0) >> 2;
         const uint32_t staging = staging0 + (uint32_t)(warp - WARP_EPI0) * STAGING;
-        const uint32_t freed = CG == 1 ? acc_empty : in_block(acc_empty, 0);
+        const uint32_t freed = CG == 1 ? acc_empty : in_block(acc_empty, leader);
         uint32_t seg = 0;
         for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
             int tm, tn;
             tile_of(p, t, tm, tn);
             const int row0 = (tm * CG + pair_rank) * BM + quad * 32;
-            if constexpr (KIND == GRAD) {
-                if (CG == 2 || p.split == 1) {           // (one segment: see SEGMENT)
-                    const uint32_t buf = seg & 1u;
-                    const int col0 = tn * BN + half * CW;
-                    Kept32 next = {};
-                    if (row0 + lane < p.M && col0 < p.N) load_kept32(kept_block(p.kept, row0, col0), next);
-                    if (!warp_wait_soon(acc_full + 8u * buf, (seg >> 1) & 1u)) { failed = true; break; }
-                    tc_fence_after();
-                    const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + buf * 256u + half * CW;
-                    auto release = [&] {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) arrive<CG>(freed + 8u * buf);
-                    };
-                    with_act(p.act, [&](auto act) {
-                        write_grad<BN>(p, act, staging, from, row0, col0, next, release);
-                    });
-                    ++seg;
-                    continue;
+            if constexpr (KIND == GRAD) {                // (one segment: see SEGMENT)
+                const uint32_t buf = seg & 1u, from = tmem + ((uint32_t)(quad * 32) << 16) + buf * 256u + half * CW;
+                const int col0 = tn * BN + half * CW;
+                Kept32 next = {};
+                if (p.split == 1 && row0 + lane < p.M && col0 < p.N) load_kept32(kept_block(p.kept, row0, col0), next);
+                if (!warp_wait_soon(acc_full + 8u * buf, (seg >> 1) & 1u)) { failed = true; break; }
+                tc_fence_after();
+                auto release = [&] {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive<CG>(freed + 8u * buf);
+                };
+                if (p.split == 1) {
+                    with_act(p.act, [&](auto act) { write_grad<BN>(p, act, staging, from, row0, col0, next, release); });
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < CW / 32; ++c) {
+                        uint32_t v[32];
+                        ld32_start(from + c * 32, v);
+                        ld32_done(v);
+                        store_partial<BN>(smem, p.M - (tm * CG + pair_rank) * BM, quad * 32 + lane, half * CW + c * 32, 32, reinterpret_cast<const float*>(v));
+                    }
+                    release();
                 }
+                ++seg;
+                continue;
             }
             float acc[CW];
             for (int k0 = kb0; k0 < kb1; k0 += segment, ++seg) {
@@ -668,31 +682,31 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 }
             }
             if (failed) break;
-            if (KIND != GRAD && (CG == 2 || p.split == 1)) {
+            if (KIND != GRAD && p.split == 1) {
                 write_tile<KIND, BN, C>(p, staging, row0, tn, half, acc);
                 __syncwarp();
             } else if constexpr (KIND == GATE) {
-                store_partial<BN>(smem, p.M - tm * BM, quad * 32 + lane, half * (CW / 2), CW / 2, acc);
-                store_partial<BN>(smem, p.M - tm * BM, quad * 32 + lane, CW + half * (CW / 2), CW / 2, acc + CW / 2);
+                store_partial<BN>(smem, p.M - (tm * CG + pair_rank) * BM, quad * 32 + lane, half * (CW / 2), CW / 2, acc);
+                store_partial<BN>(smem, p.M - (tm * CG + pair_rank) * BM, quad * 32 + lane, CW + half * (CW / 2), CW / 2, acc + CW / 2);
             } else {
-                store_partial<BN>(smem, p.M - tm * BM, quad * 32 + lane, half * CW, CW, acc);
+                store_partial<BN>(smem, p.M - (tm * CG + pair_rank) * BM, quad * 32 + lane, half * CW, CW, acc);
             }
         }
     }
     __syncwarp();
-    if (CG == 1 && p.split > 1) {
+    if (p.split > 1) {
         cluster_sync();
         if (warp >= WARP_EPI0) {
             int tm, tn;                                  // (one tile per cluster)
             tile_of(p, t0, tm, tn);
-            add_partials<KIND, BN, C>(p, smem, tm, tn, p.M - tm * BM < BM ? p.M - tm * BM : BM, rank, threadIdx.x - 32 * WARP_EPI0);
+            const int row0 = (tm * CG + pair_rank) * BM;
+            add_partials<CG, KIND, BN, C>(p, smem, row0, tn, p.M - row0 < BM ? p.M - row0 : BM, rank, pair_rank, threadIdx.x - 32 * WARP_EPI0);
         }
         __syncwarp();
-        cluster_sync();                                  // no block leaves while another reads its part
     }
-    if constexpr (CG == 2) {
+    if (CG == 2 || p.split > 1) {
         tc_fence_before();
-        cluster_sync();                                  // nothing is sent to a block that has left
+        cluster_sync();                                  // no block leaves while another reads its part or sends to it
         tc_fence_after();
     }
     leave<CG>(p, failed, warp, lane, tmem);
@@ -706,11 +720,9 @@ bool make_map_16bit(CUtensorMap* m, const void* x, int64_t rows, int64_t cols, i
 }
 
 typedef void (*Kernel)(CUtensorMap, CUtensorMap, Params);
-constexpr int MAX_SMEM = 232448, KERNELS = 8;
-constexpr int STAGES = 6;
+constexpr int MAX_SMEM = 232448, KERNELS = 12;
 
-cudaError_t launch_one(Kernel kern, int which, int cluster, const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, int grid, cudaStream_t s) {
-    const size_t smem = 1024 + (size_t)p.stages * (2 * A_BYTES) + EPI_WARPS * STAGING + 512;
+cudaError_t launch_one(Kernel kern, int which, int cluster, size_t smem, const CUtensorMap& ma, const CUtensorMap& mb, const Params& p, int grid, cudaStream_t s) {
     // Once per kernel and device (a call costs the host more than the rest of this function): every launch is allowed the most.
     static std::atomic<uint64_t> allowed[KERNELS];
     int dev = 0;
@@ -733,22 +745,37 @@ cudaError_t launch_one(Kernel kern, int which, int cluster, const CUtensorMap& m
     return cudaLaunchKernelEx(&cfg, kern, ma, mb, p);
 }
 
-// Tile and split, from a model of the time (ns): a block of k in a tile of 256 x 256 by a pair of blocks and in one of 128 x 128, a tile's end,
-// the adding up of partial tiles.
-struct Shape { bool wide; int split; };
-Shape choose_shape(int M, int N, int kblocks, int num_sms) {
-    const int64_t m = (M + BM - 1) / BM, n = (N + 127) / 128, narrow = m * n;
-    const int64_t wide = ((m + 1) / 2) * ((n + 1) / 2), wide_slots = num_sms / 2;
-    Shape best{true, 1};
-    int64_t cost = ((wide + wide_slots - 1) / wide_slots) * ((int64_t)kblocks * 165 + 1600);
-    for (int q = 1; q <= MAX_SPLIT && q <= kblocks; ++q) {
-        // (clusters do not fill the GPU's groups of SMs: 128 blocks in clusters of 8 take two turns)
-        if (q > 1 && narrow * q * 100 > (int64_t)num_sms * (q == 2 ? 100 : q <= 4 ? 82 : 65)) continue;
-        const int64_t waves = q > 1 ? 1 : (narrow + num_sms - 1) / num_sms;
-        const int64_t c = waves * ((int64_t)((kblocks + q - 1) / q) * 150 + 800) + (q > 1 ? 800 + 2000 * (M < BM ? M : BM) / BM : 0);
-        if (c < cost) { cost = c; best = {false, q}; }
+// Tile and split, from a model of what was measured (ns, B200): a block of k costs 274 in a tile of 256 x 256 and 190 in one of 256 x 128, by pairs,
+// and 238 in one of 128 x 128; a turn of tiles 1600, 950 and 950 more; pairs start 1150 and 800 later than single blocks; adding partial
+// tiles up 300, 500 and 900 and for full tiles 3200, 1600 and 2000 more.  (M x N x K in us, forms in this order, alone and with the best split:
+// 128 x 4096 x 2048: 15.2, 11.2, 12.0; 12.3 (3), 10.7 (2), 8.9 (4).  4096 x 4096 x 1024: 26.6, 30.0, 34.7.  256 x 256 x 8192: 41.4, 28.8,
+// 34.5; 17.7 (4), 12.8 (4), 11.0 (8).)
+// Clusters do not fill the GPU's groups of SMs: of 148 SMs those of 2, 3 .. 8 blocks were found to use 148, 135, 132, 130, 132, 105 and 120 at a
+// time (one more cluster takes a second turn: 10.6 -> 18.9 us); the rule stays a little below that.
+enum { PAIR_256 = 0, PAIR_128 = 1, SINGLE_128 = 2 };
+struct Shape { int form, split; };
+Shape choose_shape(int64_t M, int64_t N, int64_t kblocks, int num_sms) {
+    static constexpr int BLOCK[3] = {274, 190, 238}, TURN[3] = {1600, 950, 950}, START[3] = {1150, 800, 0}, ADD[3] = {300, 500, 900}, ADD_FULL[3] = {3200, 1600, 2000};
+    static constexpr int USABLE[MAX_SPLIT + 1] = {0, 100, 100, 85, 87, 81, 81, 66, 76};        // percent of the SMs, by the blocks of a cluster
+    Shape best{PAIR_256, 1};
+    int64_t cost = INT64_MAX;
+    for (int form = 0; form < 3; ++form) {
+        const int blocks = form == SINGLE_128 ? 1 : 2, rows = blocks * BM, columns = form == PAIR_256 ? 256 : 128;
+        const int64_t tiles = ((M + rows - 1) / rows) * ((N + columns - 1) / columns);
+        for (int q = 1; q * blocks <= MAX_SPLIT && q <= kblocks; ++q) {
+            const int64_t slots = num_sms / (q * blocks);
+            if (q > 1 && tiles * q * blocks * 100 > (int64_t)num_sms * USABLE[q * blocks]) break;
+            const int64_t turns = q > 1 || slots < 1 ? 1 : (tiles + slots - 1) / slots;
+            const int64_t c = START[form] + turns * ((kblocks + q - 1) / q * BLOCK[form] + TURN[form]) + (q > 1 ? ADD[form] + ADD_FULL[form] * (M < rows ? M : rows) / rows : 0);
+            if (c < cost) { cost = c; best = {form, q}; }
+        }
     }
     return best;
+}
+
+template <int KIND, typename C>
+Kernel kernel_of(int form) {
+    return form == PAIR_256 ? matmul16_kernel<2, 256, KIND, C> : form == PAIR_128 ? matmul16_kernel<2, 128, KIND, C> : matmul16_kernel<1, 128, KIND, C>;
 }
 
 bool on(const void* p, int64_t ld, int64_t bytes, int64_t size) { return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * size % bytes == 0; }
@@ -758,17 +785,19 @@ cudaError_t launch(Params p, int kind, int type, const void* A, int64_t lda, boo
                    int* status, int num_sms, cudaStream_t s, uint64_t* launches) {
     if (!get_encode_fn()) return cudaErrorNotSupported;
     p.M = (int)M; p.kblocks = (int)((K + BK - 1) / BK); p.status = status;
-    const Shape shape = choose_shape((int)M, (int)N, p.kblocks, num_sms);
-    const bool wide = shape.wide;
-    const int BN = wide ? 256 : 128, rows = wide ? 2 * BM : BM, columns = kind == GATE ? BN / 2 : BN;
+    const Shape shape = choose_shape(M, N, p.kblocks, num_sms);
+    const bool paired = shape.form != SINGLE_128;
+    const int BN = shape.form == PAIR_256 ? 256 : 128, rows = paired ? 2 * BM : BM, columns = kind == GATE ? BN / 2 : BN;
     p.N = (int)(kind == GATE ? N / 2 : N);
     p.tiles_m = (p.M + rows - 1) / rows;
     p.tiles_n = (p.N + columns - 1) / columns;
     if ((int64_t)p.tiles_m * p.tiles_n > 0x3FFFFFFF) return cudaErrorInvalidConfiguration;
     p.tiles = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n;
     p.split = shape.split;
-    p.group_m = wide ? 8 : 16;
-    p.stages = STAGES;
+    p.group_m = paired ? 8 : 16;
+    const uint32_t stage = A_BYTES + (uint32_t)(paired ? BN / 2 : BN) * BK * 2;
+    const size_t fixed = 1024 + EPI_WARPS * STAGING + 512;
+    p.stages = (int)((MAX_SMEM - fixed) / stage);
     p.a_mn = trans_a; p.b_mn = !trans_b;
     const int a_rows = !p.a_mn && p.M < BM ? (p.M + 7) & ~7 : BM;
     p.a_bytes = (uint32_t)a_rows * BK * 2;
@@ -776,16 +805,13 @@ cudaError_t launch(Params p, int kind, int type, const void* A, int64_t lda, boo
     if (!make_map_16bit(&ma, A, trans_a ? K : M, trans_a ? M : K, lda, p.a_mn ? BK : a_rows) ||
         !make_map_16bit(&mb, B, trans_b ? N : K, trans_b ? K : N, ldb, 64))
         return cudaErrorInvalidValue;
-    const int cluster = wide ? 2 : p.split, most = num_sms / cluster;
+    const int cluster = (paired ? 2 : 1) * p.split, most = num_sms / cluster;
     const int grid = cluster * (p.split > 1 || (int)p.tiles < most ? (int)p.tiles : most);
     p.early = 2 * grid <= num_sms;
-    Kernel kern;
-    int which;
-    if (kind == GATE) { kern = wide ? matmul16_kernel<2, 256, GATE, bf16> : matmul16_kernel<1, 128, GATE, bf16>; which = 4 + wide; }
-    else if (kind == GRAD) { kern = wide ? matmul16_kernel<2, 256, GRAD, bf16> : matmul16_kernel<1, 128, GRAD, bf16>; which = 6 + wide; }
-    else if (type == CERAR_TYPE_F32) { kern = wide ? matmul16_kernel<2, 256, PLAIN, float> : matmul16_kernel<1, 128, PLAIN, float>; which = wide; }
-    else { kern = wide ? matmul16_kernel<2, 256, PLAIN, bf16> : matmul16_kernel<1, 128, PLAIN, bf16>; which = 2 + wide; }
-    const cudaError_t e = launch_one(kern, which, cluster, ma, mb, p, grid, s);
+    const Kernel kern = kind == GATE ? kernel_of<GATE, bf16>(shape.form) : kind == GRAD ? kernel_of<GRAD, bf16>(shape.form)
+                        : type == CERAR_TYPE_F32 ? kernel_of<PLAIN, float>(shape.form) : kernel_of<PLAIN, bf16>(shape.form);
+    const int which = 3 * (kind == PLAIN ? (type == CERAR_TYPE_F32 ? 0 : 1) : kind + 1) + shape.form;
+    const cudaError_t e = launch_one(kern, which, cluster, fixed + (size_t)p.stages * stage, ma, mb, p, grid, s);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
@@ -793,9 +819,9 @@ cudaError_t launch(Params p, int kind, int type, const void* A, int64_t lda, boo
 }  // namespace
 
 int matmul16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* split) {
-    const Shape shape = choose_shape((int)M, (int)N, (int)((K + BK - 1) / BK), num_sms);
+    const Shape shape = choose_shape(M, N, (K + BK - 1) / BK, num_sms);
     *split = shape.split;
-    return shape.wide ? 256 : 128;
+    return shape.form;
 }
 
 cudaError_t launch_matmul16(const Matmul16Args& a, int num_sms, cudaStream_t s, uint64_t* launches) {
