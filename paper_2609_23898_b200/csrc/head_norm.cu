@@ -8,8 +8,10 @@
 // Memory bound: forward reads and writes every value once, backward reads x and dy and writes dx; r is computed again from x, which
 // has to be read anyway.  A row belongs to a group of 1 .. 32 threads; a thread holds two chunks of it that contain both parts
 // of its pairs (the two halves' same places, or neighbours), so that nothing but the sums crosses threads.  The group goes through
-// several heads of one token with the weights and the rotation in registers; the loads of all of them are on their way together.
+// several heads of one token with the weights and the rotation, worked into one another, in registers; the loads of a few heads are on their
+// way together.  With p = dz x the gradient needs sum x^2 and sum w p only, one exchange for both: dw += r p, dx = r w dz - x r^3 mean(w p).
 // dw is summed in registers over all rows of a thread, then over the block in a fixed order; a second launch adds the blocks up.
+// (A grid of heads by tokens: two 64-bit divisions per row cost as many instructions as the row's arithmetic.)
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -64,7 +66,9 @@ template <int CH> struct Chunk<__nv_bfloat16, CH> {
 struct Work {                                  // how a launch is cut up
     int log_lanes;                             // threads per row
     int chunks;                                // chunks of half a row
-    int blocks[2];                             // of each part: queries, keys
+    int run;                                   // heads of a token that a group goes through
+    int runs[2];                               // of each part
+    int w_vec;                                 // weights are aligned to whole chunks
     float* partial;                            // gradient of w: [part][block][dim]
 };
 
@@ -81,8 +85,8 @@ __device__ __forceinline__ Place place(const HeadNormArgs& p, int c, int ch) {
     return {p.rotated + first - h, p.rotated + first - h + (p.dim - p.rotated) / 2, false, 0};
 }
 // Position of token t: below zero where it is padding; beyond the table it is reported and taken for padding.
-__device__ __forceinline__ int64_t position_of(const HeadNormArgs& p, int64_t t) {
-    const int64_t i = t % p.period;
+__device__ __forceinline__ int64_t position_of(const HeadNormArgs& p, uint32_t t) {
+    const uint32_t i = p.period > t ? t : t % (uint32_t)p.period;
     int64_t at = i;
     if (p.positions) at = p.position_bytes == 8 ? __ldg(static_cast<const long long*>(p.positions) + i) : (int64_t)__ldg(static_cast<const int*>(p.positions) + i);
     if (at >= p.table_rows) {
@@ -92,84 +96,123 @@ __device__ __forceinline__ int64_t position_of(const HeadNormArgs& p, int64_t t)
     return at;
 }
 // pair i of the 2 CH values of a chunk (halves: same places of its two parts; neighbours: next to one another)
-template <int CH> __device__ __forceinline__ int first_of(bool neighbours, int i) { return neighbours ? 2 * i : i; }
-template <int CH> __device__ __forceinline__ int second_of(bool neighbours, int i) { return neighbours ? 2 * i + 1 : CH + i; }
+template <int CH> __device__ __forceinline__ constexpr int first_of(bool neighbours, int i) { return neighbours ? 2 * i : i; }
+template <int CH> __device__ __forceinline__ constexpr int second_of(bool neighbours, int i) { return neighbours ? 2 * i + 1 : CH + i; }
 
-__device__ __forceinline__ float group_sum(float v, int log_lanes) {
-    for (int o = (1 << log_lanes) >> 1; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+// The 2 CH weights of a thread's chunk
+template <typename W, int CH>
+__device__ __forceinline__ void load_weights(const W* w, const Place& at, bool vec, float* v) {
+    if (vec) {
+        Chunk<W, CH> a, b;
+        a.load(w + at.a);
+        b.load(w + at.b);
+#pragma unroll
+        for (int e = 0; e < CH; ++e) { v[e] = a.get(e); v[CH + e] = b.get(e); }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 2 * CH; ++e) v[e] = (float)w[e < CH ? at.a + e : at.b + e - CH];
+    }
+}
+template <int CH>
+__device__ __forceinline__ void weights(const HeadNormArgs& p, const void* w, const Place& at, bool vec, float* v) {
+    if (w == nullptr) {
+#pragma unroll
+        for (int e = 0; e < 2 * CH; ++e) v[e] = 1.f;
+    } else if (p.w_type == CERAR_TYPE_F32) {
+        if constexpr (CH <= 4) load_weights<float, CH>(static_cast<const float*>(w), at, vec, v);
+        else {                                  // (chunks of 8 binary32 values: two of 4)
+            load_weights<float, 4>(static_cast<const float*>(w), {at.a, at.a + 4, false, 0}, vec, v);
+            load_weights<float, 4>(static_cast<const float*>(w), {at.b, at.b + 4, false, 0}, vec, v + 8);
+        }
+    } else {
+        load_weights<__nv_bfloat16, CH>(static_cast<const __nv_bfloat16*>(w), at, vec, v);
+    }
 }
 
 // NCH: chunks per thread.  HEADS: heads whose loads are on their way together.  NEIGHBOURS: which values are a pair.
+// blockIdx.y: a run of heads of a part; blockIdx.x: tokens.
 template <typename T, int CH, int NCH, int HEADS, bool NEIGHBOURS>
 __global__ void __launch_bounds__(THREADS) head_norm_kernel(const HeadNormArgs p, const Work wk) {
     grid_dependency_wait();
-    const int part = (int)blockIdx.x < wk.blocks[0] ? 0 : 1;
-    const HeadPart h = p.part[part];
-    const int lanes = 1 << wk.log_lanes, lane = threadIdx.x & (lanes - 1), per_block = THREADS >> wk.log_lanes;
-    const int64_t groups = (h.heads + HEADS - 1) / HEADS, units = p.tokens * groups, stride = (int64_t)wk.blocks[part] * per_block;
+    const int part = (int)blockIdx.y < wk.runs[0] ? 0 : 1;
+    const HeadPart& h = p.part[part];
+    const int lanes = 1 << wk.log_lanes, lane = threadIdx.x & (lanes - 1);
+    const int64_t t = (int64_t)blockIdx.x * (THREADS >> wk.log_lanes) + (threadIdx.x >> wk.log_lanes);
+    const bool there = t < p.tokens;            // (threads without a token stay: they share their warp's sums)
+    const int first = ((int)blockIdx.y - (part ? wk.runs[0] : 0)) * wk.run, last = there ? (first + wk.run < h.heads ? first + wk.run : h.heads) : first;
     Place at[NCH];
-    float w[NCH][2 * CH];
     bool mine[NCH];
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
         const int c = lane + j * lanes;
         mine[j] = c < wk.chunks;
         at[j] = place(p, mine[j] ? c : 0, CH);
-#pragma unroll
-        for (int e = 0; e < 2 * CH; ++e) {
-            const int i = (e < CH ? at[j].a + e : at[j].b + e - CH);
-            w[j][e] = h.w == nullptr ? 1.f : p.w_type == CERAR_TYPE_F32 ? __ldg(static_cast<const float*>(h.w) + i) : __bfloat162float(static_cast<const __nv_bfloat16*>(h.w)[i]);
-        }
     }
-    const float inv_dim = 1.f / (float)p.dim;
-    const int64_t rounds = (units + stride - 1) / stride;        // (the same for all threads of a warp: they share sums)
-    int64_t u = (int64_t)(blockIdx.x - (part ? wk.blocks[0] : 0)) * per_block + (threadIdx.x >> wk.log_lanes);
-    for (int64_t round = 0; round < rounds; ++round, u += stride) {
-        const bool there = u < units;
-        const int64_t t = there ? u / groups : 0;
-        const int head0 = there ? (int)(u - t * groups) * HEADS : 0, heads = !there ? 0 : h.heads - head0 < HEADS ? h.heads - head0 : HEADS;
-        const T* x = static_cast<const T*>(h.x) + t * h.x_token + head0 * h.x_head;
-        Chunk<T, CH> xa[HEADS][NCH], xb[HEADS][NCH];
+    const T* x = static_cast<const T*>(h.x) + t * h.x_token + first * h.x_head;
+    T* y = static_cast<T*>(h.y) + t * h.y_token + first * h.y_head;
+    Chunk<T, CH> xa[HEADS][NCH], xb[HEADS][NCH];
+    auto load = [&](int head) {
 #pragma unroll
         for (int i = 0; i < HEADS; ++i)
 #pragma unroll
             for (int j = 0; j < NCH; ++j)
-                if (i < heads && mine[j]) {
+                if (head + i < last && mine[j]) {
                     xa[i][j].load(x + i * h.x_head + at[j].a);
                     xb[i][j].load(x + i * h.x_head + at[j].b);
                 }
-        const int64_t pos = there ? position_of(p, t) : -1;
-        float2 turn[NCH][CH];
+    };
+    load(first);
+    // y_a = r (x_a ac - x_b bs), y_b = r (x_b bc + x_a as)
+    const int64_t pos = there ? position_of(p, (uint32_t)t) : -1;
+    float ac[NCH][CH], as[NCH][CH], bc[NCH][CH], bs[NCH][CH];
 #pragma unroll
-        for (int j = 0; j < NCH; ++j)
+    for (int j = 0; j < NCH; ++j) {
+        float w[2 * CH];
+        weights<CH>(p, h.w, at[j], wk.w_vec, w);
 #pragma unroll
-            for (int i = 0; i < CH; ++i)
-                turn[j][i] = pos >= 0 && mine[j] && at[j].turned ? __ldg(p.table + pos * (p.rotated / 2) + at[j].pair + i) : make_float2(1.f, 0.f);
-        T* y = static_cast<T*>(h.y) + t * h.y_token + head0 * h.y_head;
+        for (int i = 0; i < CH; ++i) {
+            const float2 turn = pos < 0 ? make_float2(0.f, 0.f) : mine[j] && at[j].turned ? __ldg(p.table + pos * (p.rotated / 2) + at[j].pair + i) : make_float2(1.f, 0.f);
+            const float a = w[first_of<CH>(NEIGHBOURS, i)], b = w[second_of<CH>(NEIGHBOURS, i)];
+            ac[j][i] = a * turn.x; as[j][i] = a * turn.y; bc[j][i] = b * turn.x; bs[j][i] = b * turn.y;
+        }
+    }
+    const float inv_dim = 1.f / (float)p.dim;
+    // (every warp goes through all heads of the run: its groups share sums)
+    for (int head = first; head < first + wk.run; head += HEADS) {
+        if (head != first) load(head);
+        float sum[HEADS];
 #pragma unroll
         for (int i = 0; i < HEADS; ++i) {
-            float v[NCH][2 * CH], sum = 0.f;
+            sum[i] = 0.f;
+            if (head + i < last && pos >= 0) {
 #pragma unroll
-            for (int j = 0; j < NCH; ++j)
+                for (int j = 0; j < NCH; ++j)
+                    if (mine[j])
 #pragma unroll
-                for (int e = 0; e < CH; ++e) {
-                    v[j][e] = i < heads && mine[j] ? xa[i][j].get(e) : 0.f;
-                    v[j][CH + e] = i < heads && mine[j] ? xb[i][j].get(e) : 0.f;
-                    sum = fmaf(v[j][e], v[j][e], sum);
-                    sum = fmaf(v[j][CH + e], v[j][CH + e], sum);
-                }
-            const float r = rsqrtf(fmaf(group_sum(sum, wk.log_lanes), inv_dim, p.eps));
-            if (i >= heads) continue;
+                        for (int e = 0; e < CH; ++e) {
+                            sum[i] = fmaf(xa[i][j].get(e), xa[i][j].get(e), sum[i]);
+                            sum[i] = fmaf(xb[i][j].get(e), xb[i][j].get(e), sum[i]);
+                        }
+            }
+        }
+        for (int o = lanes >> 1; o; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < HEADS; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            if (head + i >= last) break;
+            const float r = rsqrtf(fmaf(sum[i], inv_dim, p.eps));
 #pragma unroll
             for (int j = 0; j < NCH; ++j) {
                 float z[2 * CH];
 #pragma unroll
                 for (int e = 0; e < CH; ++e) {
-                    const int f = first_of<CH>(NEIGHBOURS, e), g = second_of<CH>(NEIGHBOURS, e);
-                    const float a = v[j][f] * r * w[j][f], b = v[j][g] * r * w[j][g], c = turn[j][e].x, s = turn[j][e].y;
-                    z[f] = pos < 0 ? 0.f : a * c - b * s;
-                    z[g] = pos < 0 ? 0.f : b * c + a * s;
+                    constexpr bool N = NEIGHBOURS;
+                    const int f = first_of<CH>(N, e), g = second_of<CH>(N, e);
+                    const float a = pos < 0 ? 0.f : f < CH ? xa[i][j].get(f < CH ? f : 0) : xb[i][j].get(f < CH ? 0 : f - CH);
+                    const float b = pos < 0 ? 0.f : g < CH ? xa[i][j].get(g < CH ? g : 0) : xb[i][j].get(g < CH ? 0 : g - CH);
+                    z[f] = r * fmaf(a, ac[j][e], -(b * bs[j][e]));
+                    z[g] = r * fmaf(b, bc[j][e], a * as[j][e]);
                 }
                 if (mine[j]) {
                     Chunk<T, CH>::store(y + i * h.y_head + at[j].a, z);
@@ -177,6 +220,8 @@ __global__ void __launch_bounds__(THREADS) head_norm_kernel(const HeadNormArgs p
                 }
             }
         }
+        x += HEADS * h.x_head;
+        y += HEADS * h.y_head;
     }
 }
 
@@ -184,10 +229,10 @@ template <typename T, int CH, int NCH, int HEADS, bool NEIGHBOURS>
 __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormArgs p, const Work wk) {
     extern __shared__ float sums[];                              // [groups of the block][dim]: their shares of dw
     grid_dependency_wait();
-    const int part = (int)blockIdx.x < wk.blocks[0] ? 0 : 1;
-    const HeadPart h = p.part[part];
+    const int part = (int)blockIdx.y < wk.runs[0] ? 0 : 1;
+    const HeadPart& h = p.part[part];
     const int lanes = 1 << wk.log_lanes, lane = threadIdx.x & (lanes - 1), per_block = THREADS >> wk.log_lanes;
-    const int64_t groups = (h.heads + HEADS - 1) / HEADS, units = p.tokens * groups, stride = (int64_t)wk.blocks[part] * per_block;
+    const int run = (int)blockIdx.y - (part ? wk.runs[0] : 0), first = run * wk.run;
     Place at[NCH];
     float w[NCH][2 * CH], dw[NCH][2 * CH];
     bool mine[NCH];
@@ -196,91 +241,90 @@ __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormA
         const int c = lane + j * lanes;
         mine[j] = c < wk.chunks;
         at[j] = place(p, mine[j] ? c : 0, CH);
+        weights<CH>(p, h.w, at[j], wk.w_vec, w[j]);
 #pragma unroll
-        for (int e = 0; e < 2 * CH; ++e) {
-            const int i = (e < CH ? at[j].a + e : at[j].b + e - CH);
-            w[j][e] = h.w == nullptr ? 1.f : p.w_type == CERAR_TYPE_F32 ? __ldg(static_cast<const float*>(h.w) + i) : __bfloat162float(static_cast<const __nv_bfloat16*>(h.w)[i]);
-            dw[j][e] = 0.f;
-        }
+        for (int e = 0; e < 2 * CH; ++e) dw[j][e] = 0.f;
     }
     const float inv_dim = 1.f / (float)p.dim;
-    const int64_t rounds = (units + stride - 1) / stride;
-    const int block = (int)blockIdx.x - (part ? wk.blocks[0] : 0);
-    int64_t u = (int64_t)block * per_block + (threadIdx.x >> wk.log_lanes);
-    for (int64_t round = 0; round < rounds; ++round, u += stride) {
-        const bool there = u < units;
-        const int64_t t = there ? u / groups : 0;
-        const int head0 = there ? (int)(u - t * groups) * HEADS : 0, heads = !there ? 0 : h.heads - head0 < HEADS ? h.heads - head0 : HEADS;
-        const T* x = static_cast<const T*>(h.x) + t * h.x_token + head0 * h.x_head;
-        const T* dy = static_cast<const T*>(h.dy) + t * h.dy_token + head0 * h.dy_head;
+    for (int64_t t0 = (int64_t)blockIdx.x * per_block; t0 < p.tokens; t0 += (int64_t)gridDim.x * per_block) {
+        const int64_t t = t0 + (threadIdx.x >> wk.log_lanes);
+        const bool there = t < p.tokens;
+        const int last = there ? (first + wk.run < h.heads ? first + wk.run : h.heads) : first;
+        const T* x = static_cast<const T*>(h.x) + t * h.x_token + first * h.x_head;
+        const T* dy = static_cast<const T*>(h.dy) + t * h.dy_token + first * h.dy_head;
+        T* dx = static_cast<T*>(h.y) + t * h.y_token + first * h.y_head;
         Chunk<T, CH> xa[HEADS][NCH], xb[HEADS][NCH], ya[HEADS][NCH], yb[HEADS][NCH];
+        auto load = [&](int head) {
 #pragma unroll
-        for (int i = 0; i < HEADS; ++i)
+            for (int i = 0; i < HEADS; ++i)
 #pragma unroll
-            for (int j = 0; j < NCH; ++j)
-                if (i < heads && mine[j]) {
-                    xa[i][j].load(x + i * h.x_head + at[j].a);
-                    xb[i][j].load(x + i * h.x_head + at[j].b);
-                    ya[i][j].load(dy + i * h.dy_head + at[j].a);
-                    yb[i][j].load(dy + i * h.dy_head + at[j].b);
-                }
-        const int64_t pos = there ? position_of(p, t) : -1;
+                for (int j = 0; j < NCH; ++j)
+                    if (head + i < last && mine[j]) {
+                        xa[i][j].load(x + i * h.x_head + at[j].a);
+                        xb[i][j].load(x + i * h.x_head + at[j].b);
+                        ya[i][j].load(dy + i * h.dy_head + at[j].a);
+                        yb[i][j].load(dy + i * h.dy_head + at[j].b);
+                    }
+        };
+        load(first);
+        const int64_t pos = there ? position_of(p, (uint32_t)t) : -1;
         float2 turn[NCH][CH];
 #pragma unroll
         for (int j = 0; j < NCH; ++j)
 #pragma unroll
             for (int i = 0; i < CH; ++i)
                 turn[j][i] = pos >= 0 && mine[j] && at[j].turned ? __ldg(p.table + pos * (p.rotated / 2) + at[j].pair + i) : make_float2(1.f, 0.f);
-        T* dx = static_cast<T*>(h.y) + t * h.y_token + head0 * h.y_head;
+        for (int head = first; head < first + wk.run; head += HEADS) {
+            if (head != first) load(head);
 #pragma unroll
-        for (int i = 0; i < HEADS; ++i) {
-            // (padding takes no part: its values are not looked at, NaN among them)
-            const bool live = i < heads && pos >= 0;
-            float n[NCH][2 * CH], sum = 0.f;
+            for (int i = 0; i < HEADS; ++i) {
+                // (padding takes no part: its values are not looked at, NaN among them)
+                const bool live = head + i < last && pos >= 0;
+                float v[NCH][2 * CH], dz[NCH][2 * CH], square = 0.f, dot = 0.f;
 #pragma unroll
-            for (int j = 0; j < NCH; ++j)
+                for (int j = 0; j < NCH; ++j)
 #pragma unroll
-                for (int e = 0; e < CH; ++e) {
-                    n[j][e] = live && mine[j] ? xa[i][j].get(e) : 0.f;
-                    n[j][CH + e] = live && mine[j] ? xb[i][j].get(e) : 0.f;
-                    sum = fmaf(n[j][e], n[j][e], sum);
-                    sum = fmaf(n[j][CH + e], n[j][CH + e], sum);
-                }
-            const float r = rsqrtf(fmaf(group_sum(sum, wk.log_lanes), inv_dim, p.eps));
-            float dn[NCH][2 * CH], dot = 0.f;
-#pragma unroll
-            for (int j = 0; j < NCH; ++j)
-#pragma unroll
-                for (int e = 0; e < CH; ++e) {
-                    const int f = first_of<CH>(NEIGHBOURS, e), g = second_of<CH>(NEIGHBOURS, e);
-                    float a = 0.f, b = 0.f;
-                    if (live && mine[j]) {
-                        a = f < CH ? ya[i][j].get(f < CH ? f : 0) : yb[i][j].get(f < CH ? 0 : f - CH);
-                        b = g < CH ? ya[i][j].get(g < CH ? g : 0) : yb[i][j].get(g < CH ? 0 : g - CH);
+                    for (int e = 0; e < CH; ++e) {
+                        const int f = first_of<CH>(NEIGHBOURS, e), g = second_of<CH>(NEIGHBOURS, e);
+                        const bool in = live && mine[j];
+                        const float a = in ? f < CH ? ya[i][j].get(f < CH ? f : 0) : yb[i][j].get(f < CH ? 0 : f - CH) : 0.f;
+                        const float b = in ? g < CH ? ya[i][j].get(g < CH ? g : 0) : yb[i][j].get(g < CH ? 0 : g - CH) : 0.f;
+                        v[j][f] = in ? f < CH ? xa[i][j].get(f < CH ? f : 0) : xb[i][j].get(f < CH ? 0 : f - CH) : 0.f;
+                        v[j][g] = in ? g < CH ? xa[i][j].get(g < CH ? g : 0) : xb[i][j].get(g < CH ? 0 : g - CH) : 0.f;
+                        dz[j][f] = fmaf(a, turn[j][e].x, b * turn[j][e].y);
+                        dz[j][g] = fmaf(b, turn[j][e].x, -(a * turn[j][e].y));
                     }
-                    const float c = turn[j][e].x, s = turn[j][e].y;
-                    const float za = a * c + b * s, zb = b * c - a * s;
-                    n[j][f] *= r;
-                    n[j][g] *= r;
-                    dw[j][f] = fmaf(za, n[j][f], dw[j][f]);
-                    dw[j][g] = fmaf(zb, n[j][g], dw[j][g]);
-                    dn[j][f] = za * w[j][f];
-                    dn[j][g] = zb * w[j][g];
-                    dot = fmaf(dn[j][f], n[j][f], dot);
-                    dot = fmaf(dn[j][g], n[j][g], dot);
+#pragma unroll
+                for (int j = 0; j < NCH; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2 * CH; ++e) {
+                        square = fmaf(v[j][e], v[j][e], square);
+                        dot = fmaf(w[j][e] * dz[j][e], v[j][e], dot);
+                    }
+                for (int o = lanes >> 1; o; o >>= 1) {
+                    square += __shfl_xor_sync(0xffffffffu, square, o);
+                    dot += __shfl_xor_sync(0xffffffffu, dot, o);
                 }
-            const float mean = group_sum(dot, wk.log_lanes) * inv_dim;
-            if (i >= heads) continue;
+                if (!live && head + i >= last) continue;
+                const float r = rsqrtf(fmaf(square, inv_dim, p.eps)), back = -(dot * inv_dim) * r * r * r;
 #pragma unroll
-            for (int j = 0; j < NCH; ++j) {
-                float v[2 * CH];
+                for (int j = 0; j < NCH; ++j) {
+                    float u[2 * CH];
 #pragma unroll
-                for (int e = 0; e < 2 * CH; ++e) v[e] = live ? r * fmaf(-n[j][e], mean, dn[j][e]) : 0.f;
-                if (mine[j]) {
-                    Chunk<T, CH>::store(dx + i * h.y_head + at[j].a, v);
-                    Chunk<T, CH>::store(dx + i * h.y_head + at[j].b, v + CH);
+                    for (int e = 0; e < 2 * CH; ++e) {
+                        const float rz = r * dz[j][e];
+                        dw[j][e] = fmaf(rz, v[j][e], dw[j][e]);
+                        u[e] = fmaf(v[j][e], back, rz * w[j][e]);
+                    }
+                    if (mine[j]) {
+                        Chunk<T, CH>::store(dx + i * h.y_head + at[j].a, u);
+                        Chunk<T, CH>::store(dx + i * h.y_head + at[j].b, u + CH);
+                    }
                 }
             }
+            x += HEADS * h.x_head;
+            dy += HEADS * h.dy_head;
+            dx += HEADS * h.y_head;
         }
     }
     if (h.dw == nullptr) return;                                 // (the same for the whole block)
@@ -291,7 +335,7 @@ __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormA
 #pragma unroll
             for (int e = 0; e < 2 * CH; ++e) row[e < CH ? at[j].a + e : at[j].b + e - CH] = dw[j][e];
     __syncthreads();
-    float* out = wk.partial + ((int64_t)part * HEAD_NORM_BLOCKS + block) * p.dim;
+    float* out = wk.partial + ((int64_t)part * HEAD_NORM_BLOCKS + (int64_t)run * gridDim.x + blockIdx.x) * p.dim;
     for (int c = threadIdx.x; c < p.dim; c += THREADS) {
         float v = 0.f;
         for (int g = 0; g < per_block; ++g) v += sums[g * p.dim + c];
@@ -301,13 +345,13 @@ __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormA
 
 // dw (+)= the blocks' shares, in their order: a block per 32 columns of a part, a warp per run of blocks.
 constexpr int FOLD_WARPS = 32;
-__global__ void __launch_bounds__(32 * FOLD_WARPS) head_norm_fold_kernel(const HeadNormArgs p, const Work wk) {
+__global__ void __launch_bounds__(32 * FOLD_WARPS) head_norm_fold_kernel(const HeadNormArgs p, const Work wk, int columns) {
     __shared__ float sums[FOLD_WARPS][32];
     grid_dependency_wait();
     const int part = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane;
     void* dw = p.part[part].dw;
     if (dw == nullptr) return;
-    const int n = wk.blocks[part], b0 = (int)((int64_t)n * warp / FOLD_WARPS), b1 = (int)((int64_t)n * (warp + 1) / FOLD_WARPS);
+    const int n = columns * wk.runs[part], b0 = (int)((int64_t)n * warp / FOLD_WARPS), b1 = (int)((int64_t)n * (warp + 1) / FOLD_WARPS);
     float v = 0.f;
     if (c < p.dim) {
         const float* from = wk.partial + (int64_t)part * HEAD_NORM_BLOCKS * p.dim + c;
@@ -351,25 +395,37 @@ cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int nu
     wk.chunks = (p.dim / 2 + CH - 1) / CH;
     while (((int64_t)NCH << wk.log_lanes) < wk.chunks) ++wk.log_lanes;
     const int per_block = THREADS >> wk.log_lanes;
-    const int64_t most = grad ? (int64_t)num_sms * 4 : (int64_t)num_sms * 32;
-    int64_t units[2] = {0, 0};
-    for (int i = 0; i < p.count; ++i) units[i] = p.tokens * ((p.part[i].heads + HEADS - 1) / HEADS);
-    for (int i = 0; i < p.count; ++i) {
-        int64_t b = (units[i] + per_block - 1) / per_block, share = most * units[i] / (units[0] + units[1] > 0 ? units[0] + units[1] : 1);
-        if (share > HEAD_NORM_BLOCKS && grad) share = HEAD_NORM_BLOCKS;
-        wk.blocks[i] = (int)(b < share ? b : share < 1 ? (b > 0 ? 1 : 0) : share);
-    }
+    const int64_t columns = (p.tokens + per_block - 1) / per_block;
+    wk.w_vec = 1;
+    for (int i = 0; i < p.count; ++i) wk.w_vec = wk.w_vec && reinterpret_cast<uintptr_t>(p.part[i].w) % (p.w_type == CERAR_TYPE_F32 ? (CH < 4 ? CH * 4 : 16) : CH * 2) == 0;
+    // Eight heads a run share a token's weights and rotation; as few as are loaded together where there are not enough runs for two blocks per SM.
+    // (Runs are also counted by blockIdx.y, and in the gradient by the blocks whose shares of dw are kept.)
+    auto count = [&](int run) {
+        wk.run = run;
+        for (int i = 0; i < 2; ++i) wk.runs[i] = i < p.count ? (p.part[i].heads + run - 1) / run : 0;
+        return wk.runs[0] + wk.runs[1];
+    };
+    constexpr int ROWS_MAX = 65535;
+    int rows = count(HEADS);
+    if (columns * rows >= 2 * num_sms || rows > 256) rows = count(8);
+    while (rows > (grad ? 256 : ROWS_MAX)) rows = count(2 * wk.run);
     wk.partial = partial;
-    const int grid = wk.blocks[0] + wk.blocks[1];
+    int64_t grid = columns;
+    if (grad) {
+        const int64_t most = (int64_t)num_sms * 6 / (rows > 0 ? rows : 1), kept = HEAD_NORM_BLOCKS / (wk.runs[0] > wk.runs[1] ? wk.runs[0] : wk.runs[1] > 0 ? wk.runs[1] : 1);
+        if (grid > most) grid = most < 1 ? 1 : most;
+        if (grid > kept) grid = kept;
+    }
     cudaError_t e = cudaSuccess;
-    if (grid > 0) {
-        e = grad ? launch_pdl(head_norm_grad_kernel<T, CH, NCH, HEADS, NEIGHBOURS>, dim3((unsigned)grid), dim3(THREADS), (size_t)per_block * p.dim * 4, s, p, wk)
-                 : launch_pdl(head_norm_kernel<T, CH, NCH, HEADS, NEIGHBOURS>, dim3((unsigned)grid), dim3(THREADS), 0, s, p, wk);
+    if (grid > 0 && rows > 0) {
+        const dim3 blocks((unsigned)grid, (unsigned)rows);
+        e = grad ? launch_pdl(head_norm_grad_kernel<T, CH, NCH, HEADS, NEIGHBOURS>, blocks, dim3(THREADS), (size_t)per_block * p.dim * 4, s, p, wk)
+                 : launch_pdl(head_norm_kernel<T, CH, NCH, HEADS, NEIGHBOURS>, blocks, dim3(THREADS), 0, s, p, wk);
         if (e != cudaSuccess) return e;
         ++*launches;
     }
     if (grad && (p.part[0].dw || (p.count > 1 && p.part[1].dw))) {
-        e = launch_pdl(head_norm_fold_kernel, dim3((unsigned)((p.dim + 31) / 32), (unsigned)p.count), dim3(32 * FOLD_WARPS), 0, s, p, wk);
+        e = launch_pdl(head_norm_fold_kernel, dim3((unsigned)((p.dim + 31) / 32), (unsigned)p.count), dim3(32 * FOLD_WARPS), 0, s, p, wk, (int)grid);
         if (e == cudaSuccess) ++*launches;
     }
     return e;
@@ -381,7 +437,7 @@ cudaError_t launch_pairs(const HeadNormArgs& p, bool grad, float* partial, int n
                         : launch_form<T, CH, NCH, HEADS, false>(p, grad, partial, num_sms, s, launches);
 }
 
-// Chunks of 16 bytes go with one per thread (half a row is at most 256 values); shorter ones with more, so that a row still fits a warp.
+// Chunks of 16 bytes go with one or two per thread (half a row is at most 256 values); shorter ones with more, so that a row still fits a warp.
 cudaError_t launch(const HeadNormArgs& p, bool grad, float* partial, int num_sms, cudaStream_t s, uint64_t* launches) {
     if (p.type == CERAR_TYPE_F32) {
         switch (chunk_of(p, 4, grad)) {
@@ -391,7 +447,7 @@ cudaError_t launch(const HeadNormArgs& p, bool grad, float* partial, int num_sms
         }
     }
     switch (chunk_of(p, 2, grad)) {
-        case 8: return launch_pairs<__nv_bfloat16, 8, 1, 2>(p, grad, partial, num_sms, s, launches);
+        case 8: return grad ? launch_pairs<__nv_bfloat16, 8, 1, 2>(p, grad, partial, num_sms, s, launches) : launch_pairs<__nv_bfloat16, 8, 1, 4>(p, grad, partial, num_sms, s, launches);
         case 4: return launch_pairs<__nv_bfloat16, 4, 2, 2>(p, grad, partial, num_sms, s, launches);
         case 2: return launch_pairs<__nv_bfloat16, 2, 4, 1>(p, grad, partial, num_sms, s, launches);
         default: return launch_pairs<__nv_bfloat16, 1, 8, 1>(p, grad, partial, num_sms, s, launches);
