@@ -12,7 +12,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libcerar.so")
 CHECKED_LIB_PATH = os.path.join(PKG_DIR, "libcerar_checked.so")   # the same sources with -DCERAR_BOUNDS_CHECK
 SOURCES = ["api.cu", "kernels.cu", "contract_tc.cu", "fused.cu", "ring.cu", "ring_fused.cu", "ring_fp8.cu", "static_ws.cu",
            "fp8_quantize.cu", "fp8_matmul.cu", "optimizer.cu", "ops_api.cu", "embed.cu", "head_norm.cu", "matmul16.cu", "layers_api.cu", "plan.cpp"]
-HEADERS = ["kernels.cuh", "ops.cuh", "ops_handle.hpp", "mma_tile.cuh", "ptx.cuh", "tc_common.cuh", "tensor_map.hpp", "plan.hpp", "linalg.hpp", os.path.join("..", "..", "include", "cerar.h")]
+HEADERS = ["kernels.cuh", "ops.cuh", "ops_handle.hpp", "mma_tile.cuh", "packed.cuh", "ptx.cuh", "tc_common.cuh", "tensor_map.hpp", "plan.hpp", "linalg.hpp", os.path.join("..", "..", "include", "cerar.h")]
 
 
 def _nvcc() -> str:

@@ -17,16 +17,18 @@
 
 #include "kernels.cuh"
 #include "ops.cuh"
+#include "packed.cuh"
 #include "ptx.cuh"
 
 namespace cerar {
 namespace {
 
+using namespace packed;
 using namespace ptx;
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 128;
 
-// CH elements as binary32, and back with one rounding; aligned to the chunk
+// CH elements of a row as they lie in memory (aligned to the chunk), as binary32, and back with one rounding
 template <typename T, int CH> struct Chunk;
 template <int CH> struct Chunk<float, CH> {
     uint32_t q[CH];
@@ -35,7 +37,12 @@ template <int CH> struct Chunk<float, CH> {
         else if constexpr (CH == 2) *reinterpret_cast<uint2*>(q) = __ldg(reinterpret_cast<const uint2*>(p));
         else q[0] = __float_as_uint(__ldg(p));
     }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) q[i] = 0u;
+    }
     __device__ __forceinline__ float get(int i) const { return __uint_as_float(q[i]); }
+    __device__ __forceinline__ uint64_t two(int i) const { return two_of(__uint_as_float(q[2 * i]), __uint_as_float(q[2 * i + 1])); }
     static __device__ __forceinline__ void store(float* p, const float* v) {
         if constexpr (CH == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
         else if constexpr (CH == 2) *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
@@ -43,22 +50,28 @@ template <int CH> struct Chunk<float, CH> {
     }
 };
 template <int CH> struct Chunk<__nv_bfloat16, CH> {
-    uint32_t q[CH > 1 ? CH / 2 : 1];
+    static constexpr int WORDS = CH > 1 ? CH / 2 : 1;
+    uint32_t q[WORDS];
     __device__ __forceinline__ void load(const __nv_bfloat16* p) {
         if constexpr (CH == 8) *reinterpret_cast<uint4*>(q) = __ldg(reinterpret_cast<const uint4*>(p));
         else if constexpr (CH == 4) *reinterpret_cast<uint2*>(q) = __ldg(reinterpret_cast<const uint2*>(p));
         else if constexpr (CH == 2) q[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
         else q[0] = __ldg(reinterpret_cast<const unsigned short*>(p));
     }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) q[i] = 0u;
+    }
     __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? q[i / 2] & 0xFFFF0000u : q[i / 2] << 16); }
-    static __device__ __forceinline__ uint32_t two(float a, float b) {
+    __device__ __forceinline__ uint64_t two(int i) const { return of_bf16(q[i]); }
+    static __device__ __forceinline__ uint32_t word(float a, float b) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);
     }
     static __device__ __forceinline__ void store(__nv_bfloat16* p, const float* v) {
-        if constexpr (CH == 8) *reinterpret_cast<uint4*>(p) = make_uint4(two(v[0], v[1]), two(v[2], v[3]), two(v[4], v[5]), two(v[6], v[7]));
-        else if constexpr (CH == 4) *reinterpret_cast<uint2*>(p) = make_uint2(two(v[0], v[1]), two(v[2], v[3]));
-        else if constexpr (CH == 2) *reinterpret_cast<uint32_t*>(p) = two(v[0], v[1]);
+        if constexpr (CH == 8) *reinterpret_cast<uint4*>(p) = make_uint4(word(v[0], v[1]), word(v[2], v[3]), word(v[4], v[5]), word(v[6], v[7]));
+        else if constexpr (CH == 4) *reinterpret_cast<uint2*>(p) = make_uint2(word(v[0], v[1]), word(v[2], v[3]));
+        else if constexpr (CH == 2) *reinterpret_cast<uint32_t*>(p) = word(v[0], v[1]);
         else p[0] = __float2bfloat16_rn(v[0]);
     }
 };
@@ -67,7 +80,7 @@ struct Work {                                  // how a launch is cut up
     int log_lanes;                             // threads per row
     int chunks;                                // chunks of half a row
     int run;                                   // heads of a token that a group goes through
-    int runs[2];                               // of each part
+    int runs[2], rows;                         // of each part, of both
     int w_vec;                                 // weights are aligned to whole chunks
     float* partial;                            // gradient of w: [part][block][dim]
 };
@@ -95,9 +108,56 @@ __device__ __forceinline__ int64_t position_of(const HeadNormArgs& p, uint32_t t
     }
     return at;
 }
-// pair i of the 2 CH values of a chunk (halves: same places of its two parts; neighbours: next to one another)
-template <int CH> __device__ __forceinline__ constexpr int first_of(bool neighbours, int i) { return neighbours ? 2 * i : i; }
-template <int CH> __device__ __forceinline__ constexpr int second_of(bool neighbours, int i) { return neighbours ? 2 * i + 1 : CH + i; }
+// A thread's part of a row: NCH times two chunks, in CH packed pairs of neighbours each.  The value that each one is turned with lies in the
+// other chunk's same place, or next to it (neighbours; chunks of one value).
+template <typename T, int CH, int NCH> struct Raw {
+    Chunk<T, CH> a[NCH], b[NCH];
+    __device__ __forceinline__ void load(const T* row, const Place* at, const bool* mine) {
+#pragma unroll
+        for (int j = 0; j < NCH; ++j)
+            if (mine[j]) {
+                a[j].load(row + at[j].a);
+                b[j].load(row + at[j].b);
+            }
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) { a[j].clear(); b[j].clear(); }
+    }
+    __device__ __forceinline__ void take(uint64_t (*v)[CH]) const {
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            if constexpr (CH == 1) {
+                v[j][0] = two_of(a[j].get(0), b[j].get(0));
+            } else {
+#pragma unroll
+                for (int m = 0; m < CH / 2; ++m) { v[j][m] = a[j].two(m); v[j][CH / 2 + m] = b[j].two(m); }
+            }
+        }
+    }
+};
+template <int CH, bool NEIGHBOURS>
+__device__ __forceinline__ uint64_t partner(const uint64_t* v, int m) { return NEIGHBOURS || CH == 1 ? swapped(v[m]) : v[(m + CH / 2) % CH]; }
+template <typename T, int CH>
+__device__ __forceinline__ void store_pairs(T* row, const Place& at, const uint64_t* v) {
+    float f[2 * CH];
+#pragma unroll
+    for (int m = 0; m < CH; ++m) parts(v[m], f[2 * m], f[2 * m + 1]);
+    Chunk<T, CH>::store(row + at.a, f);
+    Chunk<T, CH>::store(row + at.b, f + CH);
+}
+// Cosine and sine for every one of a thread's values: y = v c + partner s, the sine negative for the first of a pair.  sign = -1: turned back.
+template <int CH, bool NEIGHBOURS>
+__device__ __forceinline__ void rotation_of(const HeadNormArgs& p, int64_t pos, const Place& at, bool mine, float sign, float* c, float* s) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const float2 turn = pos >= 0 && mine && at.turned ? __ldg(p.table + pos * (p.rotated / 2) + at.pair + i) : make_float2(1.f, 0.f);
+        const int f = NEIGHBOURS ? 2 * i : i, g = NEIGHBOURS ? 2 * i + 1 : CH + i;
+        c[f] = c[g] = turn.x;
+        s[f] = -sign * turn.y;
+        s[g] = sign * turn.y;
+    }
+}
 
 // The 2 CH weights of a thread's chunk
 template <typename W, int CH>
@@ -129,213 +189,208 @@ __device__ __forceinline__ void weights(const HeadNormArgs& p, const void* w, co
     }
 }
 
-// NCH: chunks per thread.  HEADS: heads whose loads are on their way together.  NEIGHBOURS: which values are a pair.
-// blockIdx.y: a run of heads of a part; blockIdx.x: tokens.
-template <typename T, int CH, int NCH, int HEADS, bool NEIGHBOURS>
+// NCH: chunks per thread.  DEPTH: heads whose loads are on their way.  NEIGHBOURS: which values are a pair.
+// A block: a run of heads (the faster index, so that whole tokens are read at a time) of some tokens.  Threads without a token (a chunk) stay, with zeros: they share their warp's sums.
+template <typename T, int CH, int NCH, int DEPTH, bool NEIGHBOURS>
 __global__ void __launch_bounds__(THREADS) head_norm_kernel(const HeadNormArgs p, const Work wk) {
     grid_dependency_wait();
-    const int part = (int)blockIdx.y < wk.runs[0] ? 0 : 1;
+    const uint32_t column = blockIdx.x / wk.rows;
+    const int row = (int)(blockIdx.x - column * wk.rows), part = row < wk.runs[0] ? 0 : 1;
     const HeadPart& h = p.part[part];
     const int lanes = 1 << wk.log_lanes, lane = threadIdx.x & (lanes - 1);
-    const int64_t t = (int64_t)blockIdx.x * (THREADS >> wk.log_lanes) + (threadIdx.x >> wk.log_lanes);
-    const bool there = t < p.tokens;            // (threads without a token stay: they share their warp's sums)
-    const int first = ((int)blockIdx.y - (part ? wk.runs[0] : 0)) * wk.run, last = there ? (first + wk.run < h.heads ? first + wk.run : h.heads) : first;
+    const int64_t t = (int64_t)column * (THREADS >> wk.log_lanes) + (threadIdx.x >> wk.log_lanes);
+    const bool there = t < p.tokens;
+    const int first = (row - (part ? wk.runs[0] : 0)) * wk.run, last = first + wk.run < h.heads ? first + wk.run : h.heads;
     Place at[NCH];
     bool mine[NCH];
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
         const int c = lane + j * lanes;
-        mine[j] = c < wk.chunks;
+        mine[j] = there && c < wk.chunks;
         at[j] = place(p, mine[j] ? c : 0, CH);
     }
     const T* x = static_cast<const T*>(h.x) + t * h.x_token + first * h.x_head;
     T* y = static_cast<T*>(h.y) + t * h.y_token + first * h.y_head;
-    Chunk<T, CH> xa[HEADS][NCH], xb[HEADS][NCH];
-    auto load = [&](int head) {
+    Raw<T, CH, NCH> raw[DEPTH];
 #pragma unroll
-        for (int i = 0; i < HEADS; ++i)
-#pragma unroll
-            for (int j = 0; j < NCH; ++j)
-                if (head + i < last && mine[j]) {
-                    xa[i][j].load(x + i * h.x_head + at[j].a);
-                    xb[i][j].load(x + i * h.x_head + at[j].b);
-                }
-    };
-    load(first);
-    // y_a = r (x_a ac - x_b bs), y_b = r (x_b bc + x_a as)
+    for (int i = 0; i < DEPTH; ++i) {
+        raw[i].clear();
+        if (first + i < last) raw[i].load(x, at, mine);
+        x += h.x_head;
+    }
+    // y = r (v vc + partner vs): weights and rotation in one
     const int64_t pos = there ? position_of(p, (uint32_t)t) : -1;
-    float ac[NCH][CH], as[NCH][CH], bc[NCH][CH], bs[NCH][CH];
+    uint64_t vc[NCH][CH], vs[NCH][CH];
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
-        float w[2 * CH];
+        float w[2 * CH], c[2 * CH], s[2 * CH];
         weights<CH>(p, h.w, at[j], wk.w_vec, w);
+        rotation_of<CH, NEIGHBOURS>(p, pos, at[j], mine[j], 1.f, c, s);
+        uint64_t pw[CH];
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const float2 turn = pos < 0 ? make_float2(0.f, 0.f) : mine[j] && at[j].turned ? __ldg(p.table + pos * (p.rotated / 2) + at[j].pair + i) : make_float2(1.f, 0.f);
-            const float a = w[first_of<CH>(NEIGHBOURS, i)], b = w[second_of<CH>(NEIGHBOURS, i)];
-            ac[j][i] = a * turn.x; as[j][i] = a * turn.y; bc[j][i] = b * turn.x; bs[j][i] = b * turn.y;
+        for (int m = 0; m < CH; ++m) pw[m] = two_of(w[2 * m], w[2 * m + 1]);
+#pragma unroll
+        for (int m = 0; m < CH; ++m) {
+            vc[j][m] = mul2(pw[m], two_of(c[2 * m], c[2 * m + 1]));
+            vs[j][m] = mul2(partner<CH, NEIGHBOURS>(pw, m), two_of(s[2 * m], s[2 * m + 1]));
         }
     }
     const float inv_dim = 1.f / (float)p.dim;
-    // (every warp goes through all heads of the run: its groups share sums)
-    for (int head = first; head < first + wk.run; head += HEADS) {
-        if (head != first) load(head);
-        float sum[HEADS];
+    for (int head0 = first; head0 < last; head0 += DEPTH)
 #pragma unroll
-        for (int i = 0; i < HEADS; ++i) {
-            sum[i] = 0.f;
-            if (head + i < last && pos >= 0) {
+        for (int i = 0; i < DEPTH; ++i) {
+            if (head0 + i >= last) break;
+            uint64_t v[NCH][CH], sum2 = 0ull;
+            if (pos < 0) raw[i].clear();        // (padding may hold anything)
+            raw[i].take(v);
+            if (head0 + i + DEPTH < last) raw[i].load(x, at, mine);
+            x += h.x_head;
 #pragma unroll
-                for (int j = 0; j < NCH; ++j)
-                    if (mine[j])
+            for (int j = 0; j < NCH; ++j)
 #pragma unroll
-                        for (int e = 0; e < CH; ++e) {
-                            sum[i] = fmaf(xa[i][j].get(e), xa[i][j].get(e), sum[i]);
-                            sum[i] = fmaf(xb[i][j].get(e), xb[i][j].get(e), sum[i]);
-                        }
-            }
-        }
-        for (int o = lanes >> 1; o; o >>= 1)
-#pragma unroll
-            for (int i = 0; i < HEADS; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
-#pragma unroll
-        for (int i = 0; i < HEADS; ++i) {
-            if (head + i >= last) break;
-            const float r = rsqrtf(fmaf(sum[i], inv_dim, p.eps));
+                for (int m = 0; m < CH; ++m) sum2 = mad2(v[j][m], v[j][m], sum2);
+            float sum, other;
+            parts(sum2, sum, other);
+            sum += other;
+            for (int o = lanes >> 1; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            const uint64_t r = all(rsqrtf(fmaf(sum, inv_dim, p.eps)));
 #pragma unroll
             for (int j = 0; j < NCH; ++j) {
-                float z[2 * CH];
+                uint64_t z[CH];
 #pragma unroll
-                for (int e = 0; e < CH; ++e) {
-                    constexpr bool N = NEIGHBOURS;
-                    const int f = first_of<CH>(N, e), g = second_of<CH>(N, e);
-                    const float a = pos < 0 ? 0.f : f < CH ? xa[i][j].get(f < CH ? f : 0) : xb[i][j].get(f < CH ? 0 : f - CH);
-                    const float b = pos < 0 ? 0.f : g < CH ? xa[i][j].get(g < CH ? g : 0) : xb[i][j].get(g < CH ? 0 : g - CH);
-                    z[f] = r * fmaf(a, ac[j][e], -(b * bs[j][e]));
-                    z[g] = r * fmaf(b, bc[j][e], a * as[j][e]);
-                }
-                if (mine[j]) {
-                    Chunk<T, CH>::store(y + i * h.y_head + at[j].a, z);
-                    Chunk<T, CH>::store(y + i * h.y_head + at[j].b, z + CH);
-                }
+                for (int m = 0; m < CH; ++m) z[m] = mul2(r, mad2(v[j][m], vc[j][m], mul2(partner<CH, NEIGHBOURS>(v[j], m), vs[j][m])));
+                if (mine[j]) store_pairs<T, CH>(y, at[j], z);
             }
+            y += h.y_head;
         }
-        x += HEADS * h.x_head;
-        y += HEADS * h.y_head;
-    }
 }
 
-template <typename T, int CH, int NCH, int HEADS, bool NEIGHBOURS>
+template <typename T, int CH, int NCH, int DEPTH, bool NEIGHBOURS>
 __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormArgs p, const Work wk) {
     extern __shared__ float sums[];                              // [groups of the block][dim]: their shares of dw
     grid_dependency_wait();
-    const int part = (int)blockIdx.y < wk.runs[0] ? 0 : 1;
+    const uint32_t column = blockIdx.x / wk.rows, columns = gridDim.x / wk.rows;
+    const int row = (int)(blockIdx.x - column * wk.rows), part = row < wk.runs[0] ? 0 : 1;
     const HeadPart& h = p.part[part];
     const int lanes = 1 << wk.log_lanes, lane = threadIdx.x & (lanes - 1), per_block = THREADS >> wk.log_lanes;
-    const int run = (int)blockIdx.y - (part ? wk.runs[0] : 0), first = run * wk.run;
+    const int run = row - (part ? wk.runs[0] : 0), first = run * wk.run, last = first + wk.run < h.heads ? first + wk.run : h.heads;
     Place at[NCH];
-    float w[NCH][2 * CH], dw[NCH][2 * CH];
-    bool mine[NCH];
+    uint64_t w[NCH][CH], dw[NCH][CH];
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
         const int c = lane + j * lanes;
-        mine[j] = c < wk.chunks;
-        at[j] = place(p, mine[j] ? c : 0, CH);
-        weights<CH>(p, h.w, at[j], wk.w_vec, w[j]);
+        at[j] = place(p, c < wk.chunks ? c : 0, CH);
+        float f[2 * CH];
+        weights<CH>(p, h.w, at[j], wk.w_vec, f);
 #pragma unroll
-        for (int e = 0; e < 2 * CH; ++e) dw[j][e] = 0.f;
+        for (int m = 0; m < CH; ++m) {
+            w[j][m] = two_of(f[2 * m], f[2 * m + 1]);
+            dw[j][m] = 0ull;
+        }
     }
     const float inv_dim = 1.f / (float)p.dim;
-    for (int64_t t0 = (int64_t)blockIdx.x * per_block; t0 < p.tokens; t0 += (int64_t)gridDim.x * per_block) {
+    for (int64_t t0 = (int64_t)column * per_block; t0 < p.tokens; t0 += (int64_t)columns * per_block) {
         const int64_t t = t0 + (threadIdx.x >> wk.log_lanes);
-        const bool there = t < p.tokens;
-        const int last = there ? (first + wk.run < h.heads ? first + wk.run : h.heads) : first;
+        bool mine[NCH];
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) mine[j] = t < p.tokens && lane + j * lanes < wk.chunks;
         const T* x = static_cast<const T*>(h.x) + t * h.x_token + first * h.x_head;
         const T* dy = static_cast<const T*>(h.dy) + t * h.dy_token + first * h.dy_head;
         T* dx = static_cast<T*>(h.y) + t * h.y_token + first * h.y_head;
-        Chunk<T, CH> xa[HEADS][NCH], xb[HEADS][NCH], ya[HEADS][NCH], yb[HEADS][NCH];
-        auto load = [&](int head) {
+        Raw<T, CH, NCH> rx[DEPTH], ry[DEPTH];
 #pragma unroll
-            for (int i = 0; i < HEADS; ++i)
+        for (int i = 0; i < DEPTH; ++i) {
+            rx[i].clear();
+            ry[i].clear();
+            if (first + i < last) {
+                rx[i].load(x, at, mine);
+                ry[i].load(dy, at, mine);
+            }
+            x += h.x_head;
+            dy += h.dy_head;
+        }
+        const int64_t pos = t < p.tokens ? position_of(p, (uint32_t)t) : -1;
+        uint64_t vc[NCH][CH], vs[NCH][CH];
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            float c[2 * CH], s[2 * CH];
+            rotation_of<CH, NEIGHBOURS>(p, pos, at[j], mine[j], -1.f, c, s);
+#pragma unroll
+            for (int m = 0; m < CH; ++m) {
+                vc[j][m] = two_of(c[2 * m], c[2 * m + 1]);
+                vs[j][m] = two_of(s[2 * m], s[2 * m + 1]);
+            }
+        }
+        for (int head0 = first; head0 < last; head0 += DEPTH)
+#pragma unroll
+            for (int i = 0; i < DEPTH; ++i) {
+                if (head0 + i >= last) break;
+                if (pos < 0) {                  // (padding may hold anything)
+                    rx[i].clear();
+                    ry[i].clear();
+                }
+                uint64_t v[NCH][CH], dz[NCH][CH], square2 = 0ull, dot2 = 0ull;
+                rx[i].take(v);
+                {
+                    uint64_t g[NCH][CH];
+                    ry[i].take(g);
+                    if (head0 + i + DEPTH < last) {
+                        rx[i].load(x, at, mine);
+                        ry[i].load(dy, at, mine);
+                    }
+                    x += h.x_head;
+                    dy += h.dy_head;
+#pragma unroll
+                    for (int j = 0; j < NCH; ++j)
+#pragma unroll
+                        for (int m = 0; m < CH; ++m) dz[j][m] = mad2(g[j][m], vc[j][m], mul2(partner<CH, NEIGHBOURS>(g[j], m), vs[j][m]));
+                }
 #pragma unroll
                 for (int j = 0; j < NCH; ++j)
-                    if (head + i < last && mine[j]) {
-                        xa[i][j].load(x + i * h.x_head + at[j].a);
-                        xb[i][j].load(x + i * h.x_head + at[j].b);
-                        ya[i][j].load(dy + i * h.dy_head + at[j].a);
-                        yb[i][j].load(dy + i * h.dy_head + at[j].b);
+#pragma unroll
+                    for (int m = 0; m < CH; ++m) {
+                        square2 = mad2(v[j][m], v[j][m], square2);
+                        dot2 = mad2(mul2(w[j][m], dz[j][m]), v[j][m], dot2);
                     }
-        };
-        load(first);
-        const int64_t pos = there ? position_of(p, (uint32_t)t) : -1;
-        float2 turn[NCH][CH];
-#pragma unroll
-        for (int j = 0; j < NCH; ++j)
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-                turn[j][i] = pos >= 0 && mine[j] && at[j].turned ? __ldg(p.table + pos * (p.rotated / 2) + at[j].pair + i) : make_float2(1.f, 0.f);
-        for (int head = first; head < first + wk.run; head += HEADS) {
-            if (head != first) load(head);
-#pragma unroll
-            for (int i = 0; i < HEADS; ++i) {
-                // (padding takes no part: its values are not looked at, NaN among them)
-                const bool live = head + i < last && pos >= 0;
-                float v[NCH][2 * CH], dz[NCH][2 * CH], square = 0.f, dot = 0.f;
-#pragma unroll
-                for (int j = 0; j < NCH; ++j)
-#pragma unroll
-                    for (int e = 0; e < CH; ++e) {
-                        const int f = first_of<CH>(NEIGHBOURS, e), g = second_of<CH>(NEIGHBOURS, e);
-                        const bool in = live && mine[j];
-                        const float a = in ? f < CH ? ya[i][j].get(f < CH ? f : 0) : yb[i][j].get(f < CH ? 0 : f - CH) : 0.f;
-                        const float b = in ? g < CH ? ya[i][j].get(g < CH ? g : 0) : yb[i][j].get(g < CH ? 0 : g - CH) : 0.f;
-                        v[j][f] = in ? f < CH ? xa[i][j].get(f < CH ? f : 0) : xb[i][j].get(f < CH ? 0 : f - CH) : 0.f;
-                        v[j][g] = in ? g < CH ? xa[i][j].get(g < CH ? g : 0) : xb[i][j].get(g < CH ? 0 : g - CH) : 0.f;
-                        dz[j][f] = fmaf(a, turn[j][e].x, b * turn[j][e].y);
-                        dz[j][g] = fmaf(b, turn[j][e].x, -(a * turn[j][e].y));
-                    }
-#pragma unroll
-                for (int j = 0; j < NCH; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2 * CH; ++e) {
-                        square = fmaf(v[j][e], v[j][e], square);
-                        dot = fmaf(w[j][e] * dz[j][e], v[j][e], dot);
-                    }
+                float square, dot, other;
+                parts(square2, square, other);
+                square += other;
+                parts(dot2, dot, other);
+                dot += other;
                 for (int o = lanes >> 1; o; o >>= 1) {
                     square += __shfl_xor_sync(0xffffffffu, square, o);
                     dot += __shfl_xor_sync(0xffffffffu, dot, o);
                 }
-                if (!live && head + i >= last) continue;
-                const float r = rsqrtf(fmaf(square, inv_dim, p.eps)), back = -(dot * inv_dim) * r * r * r;
+                const float r = rsqrtf(fmaf(square, inv_dim, p.eps));
+                const uint64_t r2 = all(r), back = all(-(dot * inv_dim) * r * r * r);
 #pragma unroll
                 for (int j = 0; j < NCH; ++j) {
-                    float u[2 * CH];
+                    uint64_t u[CH];
 #pragma unroll
-                    for (int e = 0; e < 2 * CH; ++e) {
-                        const float rz = r * dz[j][e];
-                        dw[j][e] = fmaf(rz, v[j][e], dw[j][e]);
-                        u[e] = fmaf(v[j][e], back, rz * w[j][e]);
+                    for (int m = 0; m < CH; ++m) {
+                        const uint64_t rz = mul2(r2, dz[j][m]);
+                        dw[j][m] = mad2(rz, v[j][m], dw[j][m]);
+                        u[m] = mad2(v[j][m], back, mul2(rz, w[j][m]));
                     }
-                    if (mine[j]) {
-                        Chunk<T, CH>::store(dx + i * h.y_head + at[j].a, u);
-                        Chunk<T, CH>::store(dx + i * h.y_head + at[j].b, u + CH);
-                    }
+                    if (mine[j]) store_pairs<T, CH>(dx, at[j], u);
                 }
+                dx += h.y_head;
             }
-            x += HEADS * h.x_head;
-            dy += HEADS * h.dy_head;
-            dx += HEADS * h.y_head;
-        }
     }
     if (h.dw == nullptr) return;                                 // (the same for the whole block)
-    float* row = sums + (threadIdx.x >> wk.log_lanes) * p.dim;
+    float* share = sums + (threadIdx.x >> wk.log_lanes) * p.dim;
 #pragma unroll
     for (int j = 0; j < NCH; ++j)
-        if (mine[j])
+        if (lane + j * lanes < wk.chunks)
 #pragma unroll
-            for (int e = 0; e < 2 * CH; ++e) row[e < CH ? at[j].a + e : at[j].b + e - CH] = dw[j][e];
+            for (int m = 0; m < CH; ++m) {
+                float f[2];
+                parts(dw[j][m], f[0], f[1]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) share[2 * m + i < CH ? at[j].a + 2 * m + i : at[j].b + 2 * m + i - CH] = f[i];
+            }
     __syncthreads();
-    float* out = wk.partial + ((int64_t)part * HEAD_NORM_BLOCKS + (int64_t)run * gridDim.x + blockIdx.x) * p.dim;
+    float* out = wk.partial + ((int64_t)part * HEAD_NORM_BLOCKS + (int64_t)run * columns + column) * p.dim;
     for (int c = threadIdx.x; c < p.dim; c += THREADS) {
         float v = 0.f;
         for (int g = 0; g < per_block; ++g) v += sums[g * p.dim + c];
@@ -389,7 +444,7 @@ int chunk_of(const HeadNormArgs& p, int64_t size, bool grad) {
     return 1;
 }
 
-template <typename T, int CH, int NCH, int HEADS, bool NEIGHBOURS>
+template <typename T, int CH, int NCH, int DEPTH, bool NEIGHBOURS>
 cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int num_sms, cudaStream_t s, uint64_t* launches) {
     Work wk = {};
     wk.chunks = (p.dim / 2 + CH - 1) / CH;
@@ -398,17 +453,17 @@ cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int nu
     const int64_t columns = (p.tokens + per_block - 1) / per_block;
     wk.w_vec = 1;
     for (int i = 0; i < p.count; ++i) wk.w_vec = wk.w_vec && reinterpret_cast<uintptr_t>(p.part[i].w) % (p.w_type == CERAR_TYPE_F32 ? (CH < 4 ? CH * 4 : 16) : CH * 2) == 0;
-    // Eight heads a run share a token's weights and rotation; as few as are loaded together where there are not enough runs for two blocks per SM.
-    // (Runs are also counted by blockIdx.y, and in the gradient by the blocks whose shares of dw are kept.)
+    // Eight heads a run share a token's weights and rotation (sixteen where six are loaded at a time); two where there are not enough runs for
+    // four blocks per SM.
+    // (In the gradient runs are also counted by the blocks whose shares of dw are kept.)
     auto count = [&](int run) {
         wk.run = run;
         for (int i = 0; i < 2; ++i) wk.runs[i] = i < p.count ? (p.part[i].heads + run - 1) / run : 0;
         return wk.runs[0] + wk.runs[1];
     };
-    constexpr int ROWS_MAX = 65535;
-    int rows = count(HEADS);
-    if (columns * rows >= 2 * num_sms || rows > 256) rows = count(8);
-    while (rows > (grad ? 256 : ROWS_MAX)) rows = count(2 * wk.run);
+    int rows = count(2);
+    if (columns * rows >= 4 * num_sms || rows > 256) rows = count(DEPTH > 4 ? 16 : 8);
+    while (rows > (grad ? 256 : 65536)) rows = count(2 * wk.run);
     wk.partial = partial;
     int64_t grid = columns;
     if (grad) {
@@ -418,9 +473,11 @@ cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int nu
     }
     cudaError_t e = cudaSuccess;
     if (grid > 0 && rows > 0) {
-        const dim3 blocks((unsigned)grid, (unsigned)rows);
-        e = grad ? launch_pdl(head_norm_grad_kernel<T, CH, NCH, HEADS, NEIGHBOURS>, blocks, dim3(THREADS), (size_t)per_block * p.dim * 4, s, p, wk)
-                 : launch_pdl(head_norm_kernel<T, CH, NCH, HEADS, NEIGHBOURS>, blocks, dim3(THREADS), 0, s, p, wk);
+        if (grid * rows > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+        wk.rows = rows;
+        const dim3 blocks((unsigned)(grid * rows));
+        if (!grad) e = launch_pdl(head_norm_kernel<T, CH, NCH, DEPTH, NEIGHBOURS>, blocks, dim3(THREADS), 0, s, p, wk);
+        else if constexpr (DEPTH <= 2) e = launch_pdl(head_norm_grad_kernel<T, CH, NCH, DEPTH, NEIGHBOURS>, blocks, dim3(THREADS), (size_t)per_block * p.dim * 4, s, p, wk);
         if (e != cudaSuccess) return e;
         ++*launches;
     }
@@ -431,13 +488,15 @@ cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int nu
     return e;
 }
 
-template <typename T, int CH, int NCH, int HEADS>
+template <typename T, int CH, int NCH, int DEPTH>
 cudaError_t launch_pairs(const HeadNormArgs& p, bool grad, float* partial, int num_sms, cudaStream_t s, uint64_t* launches) {
-    return p.neighbours ? launch_form<T, CH, NCH, HEADS, true>(p, grad, partial, num_sms, s, launches)
-                        : launch_form<T, CH, NCH, HEADS, false>(p, grad, partial, num_sms, s, launches);
+    return p.neighbours ? launch_form<T, CH, NCH, DEPTH, true>(p, grad, partial, num_sms, s, launches)
+                        : launch_form<T, CH, NCH, DEPTH, false>(p, grad, partial, num_sms, s, launches);
 }
 
 // Chunks of 16 bytes go with one or two per thread (half a row is at most 256 values); shorter ones with more, so that a row still fits a warp.
+// Heads on their way: as many as registers hold (16384 x 40 x 128 in us, forward bfloat16 with 1, 2, 4, 6, 8: 67, 71, 61, 56, 62; binary32 with
+// 1, 2: 120, 107; gradient bfloat16 with 1, 2: 104, 102, binary32 200, 167).
 cudaError_t launch(const HeadNormArgs& p, bool grad, float* partial, int num_sms, cudaStream_t s, uint64_t* launches) {
     if (p.type == CERAR_TYPE_F32) {
         switch (chunk_of(p, 4, grad)) {
@@ -447,8 +506,8 @@ cudaError_t launch(const HeadNormArgs& p, bool grad, float* partial, int num_sms
         }
     }
     switch (chunk_of(p, 2, grad)) {
-        case 8: return grad ? launch_pairs<__nv_bfloat16, 8, 1, 2>(p, grad, partial, num_sms, s, launches) : launch_pairs<__nv_bfloat16, 8, 1, 4>(p, grad, partial, num_sms, s, launches);
-        case 4: return launch_pairs<__nv_bfloat16, 4, 2, 2>(p, grad, partial, num_sms, s, launches);
+        case 8: return grad ? launch_pairs<__nv_bfloat16, 8, 1, 2>(p, grad, partial, num_sms, s, launches) : launch_pairs<__nv_bfloat16, 8, 1, 6>(p, grad, partial, num_sms, s, launches);
+        case 4: return launch_pairs<__nv_bfloat16, 4, 2, 1>(p, grad, partial, num_sms, s, launches);
         case 2: return launch_pairs<__nv_bfloat16, 2, 4, 1>(p, grad, partial, num_sms, s, launches);
         default: return launch_pairs<__nv_bfloat16, 1, 8, 1>(p, grad, partial, num_sms, s, launches);
     }

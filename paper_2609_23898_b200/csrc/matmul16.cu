@@ -29,11 +29,13 @@
 #include "kernels.cuh"
 #include "mma_tile.cuh"
 #include "ops.cuh"
+#include "packed.cuh"
 
 namespace cerar {
 namespace {
 
 using namespace mma;
+using namespace packed;
 typedef __nv_bfloat16 bf16;
 
 constexpr int BK = 64;                                  // values of k in a stage: rows of 128 bytes
@@ -92,28 +94,6 @@ __device__ __forceinline__ void commit_to(uint32_t bar, uint32_t blocks) {
 // In binary32, two values at a time (one instruction for both, where there is one).  The exponential and the reciprocal are the hardware's, some
 // 2^-22 of themselves off, far below the step of a bfloat16 result.
 
-__device__ __forceinline__ uint64_t two_of(float x, float y) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ void parts(uint64_t r, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r)); }
-__device__ __forceinline__ uint64_t all(float x) { return two_of(x, x); }
-__device__ __forceinline__ uint64_t mul2(uint64_t x, uint64_t y) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-    return r;
-}
-__device__ __forceinline__ uint64_t mad2(uint64_t x, uint64_t y, uint64_t z) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
-    return r;
-}
 __device__ __forceinline__ uint64_t exp2_2(uint64_t x) {
     float a, b;
     parts(x, a, b);
