@@ -609,7 +609,7 @@ cerar_status_t cerar_embed(cerar_ops_t* ops, const void* table, cerar_type_t typ
 
 /* Its gradient: dtable[v] = scale sum_{t: ids[t] = v} dy[t], or dtable[v] + that with accumulate != 0 (rows of no token are then not
  * touched; otherwise they become zero).  Sums in binary32: pieces of a fixed length of the tokens in order, then the pieces in order;
- * one rounding to d_type.  Deterministic.  dy of padding is not read. */
+ * one rounding to d_type.  Deterministic.  dy of padding may hold anything. */
 size_t         cerar_embed_grad_workspace(int64_t tokens, int64_t vocab, int64_t width);
 cerar_status_t cerar_embed_grad(cerar_ops_t* ops, const void* dy, cerar_type_t type, int64_t lddy, const void* ids, int id_bytes,
                                 int64_t tokens, float scale, void* dtable, cerar_type_t d_type, int64_t vocab, int64_t width,

@@ -136,9 +136,10 @@ cudaError_t launch_lookup_typed(const EmbedArgs& a, int num_sms, cudaStream_t s)
 
 constexpr int RANK_THREADS = 256, RANK_SHARE = 8, RANK_MAX = 4096;
 
-__global__ void __launch_bounds__(RANK_THREADS) rank_kernel(const void* ids, int id_bytes, int tokens, int64_t vocab, uint32_t* keys, uint32_t* order, int* status) {
+__global__ void __launch_bounds__(RANK_THREADS) rank_kernel(const void* ids, int id_bytes, int tokens, int64_t vocab, uint32_t* keys, uint32_t* order, uint32_t* crossing, int* status) {
     __shared__ __align__(16) uint32_t all[RANK_MAX];
     grid_dependency_wait();
+    if (blockIdx.x == 0 && threadIdx.x < 2) crossing[threadIdx.x] = 0u;
     const int groups = (tokens + 3) >> 2;
     for (int t = threadIdx.x; t < 4 * groups; t += RANK_THREADS) all[t] = t < tokens ? key_of(ids, id_bytes, t, vocab, status) : 0xFFFFFFFFu;
     __syncthreads();
@@ -166,7 +167,8 @@ __global__ void __launch_bounds__(RANK_THREADS) rank_kernel(const void* ids, int
 // tile's tokens to their places.  A warp owns a run of its tile; equal digits among its 32 tokens are ranked by their lanes, so
 // every pass keeps the order.
 constexpr int DIGIT_MAX = 9, DIGITS = 1 << DIGIT_MAX, SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32;
-constexpr int SORT_TILE = 2048, SORT_TILES_MAX = 256;
+constexpr int SORT_TILE = 2048, SORT_TILES_MAX = 256, KEYS = SORT_TILE / SORT_THREADS;
+constexpr uint32_t NONE = 0xFFFFFFFFu;
 
 struct SortPass {
     const void* ids;                           // first pass: the keys are made from these
@@ -174,6 +176,7 @@ struct SortPass {
     int64_t vocab;
     const uint32_t *keys_in, *order_in;
     uint32_t *keys, *order, *counts;           // counts: [tiles][DIGITS]
+    uint32_t *named, *crossing;                // a bit for every row that some token names (cleared by the first count, set by the first placing)
     int64_t tokens;
     int tile, tiles, shift, digits;            // digits: a power of two
     int* status;
@@ -187,7 +190,13 @@ __global__ void __launch_bounds__(SORT_THREADS) count_kernel(const SortPass p) {
     count[threadIdx.x] = 0;
     grid_dependency_wait();
     __syncthreads();
+    if (p.ids) {
+        if (blockIdx.x == 0 && threadIdx.x < 2) p.crossing[threadIdx.x] = 0u;
+        if (p.named)
+            for (int64_t w = (int64_t)blockIdx.x * SORT_THREADS + threadIdx.x; w <= p.vocab / 32; w += (int64_t)gridDim.x * SORT_THREADS) p.named[w] = 0u;
+    }
     const int64_t t0 = (int64_t)blockIdx.x * p.tile, t1 = t0 + p.tile < p.tokens ? t0 + p.tile : p.tokens;
+#pragma unroll 4
     for (int64_t t = t0 + threadIdx.x; t < t1; t += SORT_THREADS) atomicAdd(&count[(sort_key(p, t) >> p.shift) & (p.digits - 1)], 1u);
     __syncthreads();
     p.counts[(int64_t)blockIdx.x * DIGITS + threadIdx.x] = count[threadIdx.x];
@@ -202,15 +211,30 @@ __global__ void __launch_bounds__(SORT_THREADS) place_kernel(const SortPass p) {
     __syncthreads();
     const int64_t t0 = (int64_t)blockIdx.x * p.tile + (int64_t)warp * (p.tile / SORT_WARPS), t1 = t0 + p.tile / SORT_WARPS;
     const uint32_t dmask = p.digits - 1;
-    for (int64_t t = t0 + lane; t - lane < t1 && t - lane < p.tokens; t += 32) {
-        const bool there = t < p.tokens;
-        const uint32_t d = there ? (sort_key(p, t) >> p.shift) & dmask : 0xFFFFFFFFu;
-        const uint32_t same = __match_any_sync(0xffffffffu, d);
-        if (there && lane == __ffs(same) - 1) at[warp][d] += __popc(same);
-        __syncwarp();
+    // A run of a tile of the usual size is four keys per lane, which stay in registers (and their loads on their way together).
+    uint32_t held[KEYS];
+    auto load = [&](int64_t from) {
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const int64_t t = from + i * 32 + lane;
+            held[i] = t < t1 && t < p.tokens ? sort_key(p, t) : NONE;
+        }
+    };
+    for (int64_t from = t0; from < t1 && from < p.tokens; from += 32 * KEYS) {
+        load(from);
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const bool there = held[i] != NONE;
+            const uint32_t d = there ? (held[i] >> p.shift) & dmask : NONE;
+            const uint32_t same = __match_any_sync(0xffffffffu, d);
+            if (there && lane == __ffs(same) - 1) at[warp][d] += __popc(same);
+            if (there && p.ids && p.named) atomicOr(p.named + (held[i] >> 5), 1u << (held[i] & 31));
+            __syncwarp();
+        }
     }
     // This digit's (thread's) first place: the smaller digits' tokens, the same digit's of the tiles in front.
     uint32_t total = 0, front = 0;
+#pragma unroll 8
     for (int i = 0; i < p.tiles; ++i) {
         const uint32_t c = p.counts[(int64_t)i * DIGITS + threadIdx.x];
         total += c;
@@ -232,26 +256,30 @@ __global__ void __launch_bounds__(SORT_THREADS) place_kernel(const SortPass p) {
         place += c;
     }
     __syncthreads();
-    for (int64_t t = t0 + lane; t - lane < t1 && t - lane < p.tokens; t += 32) {
-        const bool there = t < p.tokens;
-        const uint32_t key = there ? sort_key(p, t) : 0u, d = there ? (key >> p.shift) & dmask : 0xFFFFFFFFu;
-        const uint32_t same = __match_any_sync(0xffffffffu, d);
-        uint32_t to = 0;
-        if (there) to = at[warp][d] + __popc(same & ((1u << lane) - 1u));
-        __syncwarp();
-        if (there) {
-            if (lane == __ffs(same) - 1) at[warp][d] += __popc(same);
-            p.keys[to] = key;
-            p.order[to] = p.ids ? (uint32_t)t : p.order_in[t];
+    for (int64_t from = t0; from < t1 && from < p.tokens; from += 32 * KEYS) {
+        if (t1 - t0 > 32 * KEYS) load(from);
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const int64_t t = from + i * 32 + lane;
+            const bool there = held[i] != NONE;
+            const uint32_t d = there ? (held[i] >> p.shift) & dmask : NONE;
+            const uint32_t same = __match_any_sync(0xffffffffu, d);
+            uint32_t to = 0;
+            if (there) to = at[warp][d] + __popc(same & ((1u << lane) - 1u));
+            __syncwarp();
+            if (there) {
+                if (lane == __ffs(same) - 1) at[warp][d] += __popc(same);
+                p.keys[to] = held[i];
+                p.order[to] = p.ids ? (uint32_t)t : p.order_in[t];
+            }
+            __syncwarp();
         }
-        __syncwarp();
     }
 }
 
 // ------------------------------------------------------------------------------------------------ sums
 
 constexpr int SUM_THREADS = 128, PIECE_MAX = 64, ZERO_ROWS = 32;
-constexpr uint32_t NONE = 0xFFFFFFFFu;
 
 // Tokens of a piece.  Short batches need the blocks, long ones the few partial rows.
 __host__ int piece_of(int64_t tokens) { return tokens <= 2048 ? 4 : tokens <= 8192 ? 8 : tokens <= 32768 ? 16 : tokens <= 131072 ? 32 : PIECE_MAX; }
@@ -260,6 +288,8 @@ struct SumArgs {
     const void* dy;
     int64_t lddy;
     const uint32_t *keys, *order;              // sorted
+    const uint32_t* named;                     // a bit for every row that some token names; null: it is looked for in the sorted keys
+    uint32_t* crossing;                        // numbers of, and then, the pieces whose last token goes on into the next piece only; into more
     float* partial;                            // [pieces][2][ldp]: of the token that came over the piece's start, of the one that goes over its end
     int64_t ldp;
     int64_t tokens, vocab, width, ld;
@@ -294,22 +324,55 @@ __device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, int64_
     }
 }
 
-// Blocks 0 .. pieces * slabs - 1 add up pieces; the others (nothing is kept of what dtable held) set the rows of no token to zero, 32 rows each.
+// A chunk of a row as it lies in memory.  The loads are volatile: they are to be issued together, not each where it is used (which is what
+// becomes of them behind the branches of the sums: 65536 x 2048 in 269 us).
+template <int BYTES> struct Bits;
+template <> struct Bits<16> {
+    uint4 q;
+    __device__ __forceinline__ void load(const void* p) { asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(p)); }
+    __device__ __forceinline__ void values(const float*, float* v) const {
+        v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
+    }
+    __device__ __forceinline__ void values(const __nv_bfloat16*, float* v) const {
+        Chunk<__nv_bfloat16, 2>::two(q.x, v); Chunk<__nv_bfloat16, 2>::two(q.y, v + 2); Chunk<__nv_bfloat16, 2>::two(q.z, v + 4); Chunk<__nv_bfloat16, 2>::two(q.w, v + 6);
+    }
+};
+template <> struct Bits<4> {
+    uint32_t q;
+    __device__ __forceinline__ void load(const void* p) { asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(q) : "l"(p)); }
+    __device__ __forceinline__ void values(const float*, float* v) const { v[0] = __uint_as_float(q); }
+    __device__ __forceinline__ void values(const __nv_bfloat16*, float* v) const { Chunk<__nv_bfloat16, 2>::two(q, v); }
+};
+template <> struct Bits<2> {
+    uint16_t q;
+    __device__ __forceinline__ void load(const void* p) { asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(q) : "l"(p)); }
+    __device__ __forceinline__ void values(const __nv_bfloat16*, float* v) const { v[0] = __uint_as_float((uint32_t)q << 16); }
+};
+
+// pieces * slabs blocks add up pieces; the others (nothing is kept of what dtable held) set the rows of no token to zero, 32 rows each.  They take
+// turns, so that reads of the ones and writes of the others go on at the same time.
 template <typename T, int CH>
 __global__ void __launch_bounds__(SUM_THREADS) sum_kernel(const SumArgs a) {
     __shared__ uint32_t key[PIECE_MAX + 2], row[PIECE_MAX];
     grid_dependency_wait();
-    const int64_t sums = a.pieces * a.slabs;
-    if ((int64_t)blockIdx.x >= sums) {
-        const int64_t r0 = ((int64_t)blockIdx.x - sums) * ZERO_ROWS;
+    const uint64_t sums = (uint64_t)a.pieces * a.slabs;
+    const uint64_t before = sums * blockIdx.x / gridDim.x;                // blocks in front of this one that add up
+    if (sums * (blockIdx.x + 1ull) / gridDim.x == before) {
+        const int64_t r0 = (int64_t)(blockIdx.x - before) * ZERO_ROWS;
         if (threadIdx.x < ZERO_ROWS) {
             const int64_t r = r0 + threadIdx.x;
-            int64_t lo = 0, hi = a.tokens;       // the first sorted key that is not below r
-            while (lo < hi) {
-                const int64_t mid = (lo + hi) >> 1;
-                if (a.keys[mid] < (uint32_t)r) lo = mid + 1; else hi = mid;
+            bool skip = r >= a.vocab;
+            if (!skip && a.named) {
+                skip = a.named[r >> 5] >> (r & 31) & 1u;
+            } else if (!skip) {
+                int64_t lo = 0, hi = a.tokens;   // the first sorted key that is not below r
+                while (lo < hi) {
+                    const int64_t mid = (lo + hi) >> 1;
+                    if (a.keys[mid] < (uint32_t)r) lo = mid + 1; else hi = mid;
+                }
+                skip = lo < a.tokens && a.keys[lo] == (uint32_t)r;
             }
-            key[threadIdx.x] = r >= a.vocab || (lo < a.tokens && a.keys[lo] == (uint32_t)r) ? 1u : 0u;
+            key[threadIdx.x] = skip ? 1u : 0u;
         }
         __syncthreads();
         const int64_t size = a.d_type == CERAR_TYPE_F32 ? 4 : 2;
@@ -326,7 +389,8 @@ __global__ void __launch_bounds__(SUM_THREADS) sum_kernel(const SumArgs a) {
         }
         return;
     }
-    const int64_t piece = blockIdx.x / a.slabs, e0 = piece * a.piece;
+    const int64_t piece = (int64_t)before / a.slabs, e0 = piece * a.piece;
+    const int slab = (int)((int64_t)before - piece * a.slabs);
     const int n = (int)(a.tokens - e0 < a.piece ? a.tokens - e0 : a.piece);
     for (int i = threadIdx.x; i < n + 2; i += SUM_THREADS) {
         const int64_t e = e0 + i - 1;
@@ -334,7 +398,7 @@ __global__ void __launch_bounds__(SUM_THREADS) sum_kernel(const SumArgs a) {
         if (i < n) row[i] = a.order[e0 + i];
     }
     __syncthreads();
-    const int64_t col = ((int64_t)(blockIdx.x - piece * a.slabs) * SUM_THREADS + threadIdx.x) * CH;
+    const int64_t col = ((int64_t)slab * SUM_THREADS + threadIdx.x) * CH;
     if (col >= a.width) return;
     const T* dy = static_cast<const T*>(a.dy) + col;
     constexpr int AHEAD = 8;                     // rows whose loads are on their way together
@@ -343,21 +407,27 @@ __global__ void __launch_bounds__(SUM_THREADS) sum_kernel(const SumArgs a) {
     for (int e = 0; e < CH; ++e) acc[e] = 0.f;
     bool came = key[0] == key[1];                // the sum of this token began in an earlier piece
     for (int i0 = 0; i0 < n; i0 += AHEAD) {
-        float v[AHEAD][CH];
+        Bits<CH * sizeof(T)> raw[AHEAD];         // (behind the end: the last row again; of padding: not used)
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (i0 + i < n && key[i0 + i + 1] < (uint32_t)a.vocab) Chunk<T, CH>::load(dy + (int64_t)row[i0 + i] * a.lddy, v[i]);
+        for (int i = 0; i < AHEAD; ++i) raw[i].load(dy + (int64_t)row[i0 + i < n ? i0 + i : n - 1] * a.lddy);
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             if (i0 + i >= n) break;
             const uint32_t k = key[i0 + i + 1], next = key[i0 + i + 2];
             if (k >= (uint32_t)a.vocab) return;  // (the rest takes no part)
+            float v[CH];
+            raw[i].values(static_cast<const T*>(nullptr), v);
 #pragma unroll
-            for (int e = 0; e < CH; ++e) acc[e] += v[i][e];
+            for (int e = 0; e < CH; ++e) acc[e] += v[e];
             if (next == k && i0 + i + 1 < n) continue;
             if (next != k && !came) {
                 write_row<CH>(a, k, col, acc, true);
             } else {
+                if (!came && col == 0) {         // its sum begins here and goes on: the next kernel puts it together
+                    const int64_t after = e0 + 2 * a.piece;
+                    const int far = after < a.tokens && a.keys[after] == k;
+                    a.crossing[2 + far * a.pieces + atomicAdd(a.crossing + far, 1u)] = (uint32_t)piece;
+                }
                 float* p = a.partial + (piece * 2 + (came ? 0 : 1)) * a.ldp + col;
 #pragma unroll
                 for (int e = 0; e < CH; ++e) p[e] = acc[e];
@@ -369,57 +439,67 @@ __global__ void __launch_bounds__(SUM_THREADS) sum_kernel(const SumArgs a) {
     }
 }
 
-// The token that goes over the end of piece p, if its sum began there: partial rows p (second), p + 1 ... (first), in this order.  Eight warps
-// take a run of them each, their sums are added in the order of the runs; a warp works on 128 columns.
+// Tokens that go over the end of a piece p in which their sum began: partial rows p (second), p + 1 ... (first), in this order.  Those of two rows:
+// a warp adds 128 columns.  Those of more: eight warps take a run of the rows of 128 columns each, and their sums are added in the order of
+// the runs.  (The order of the lists is that of atomics; what is added, and in which order, does not depend on it.)
 constexpr int JOIN_WARPS = 8;
+__device__ __forceinline__ void write_four(const SumArgs& a, uint32_t k, int64_t col, const float4& v, bool aligned) {
+    const float acc[4] = {v.x, v.y, v.z, v.w};
+    if (col + 4 <= a.width) {
+        write_row<4>(a, k, col, acc, aligned);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < a.width) write_row<1>(a, k, col + e, acc + e, true);
+    }
+}
+__device__ __forceinline__ void add(float4& v, const float4& x) { v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w; }
 __global__ void __launch_bounds__(32 * JOIN_WARPS) join_kernel(const SumArgs a, int slabs, int aligned) {
     __shared__ float4 sums[JOIN_WARPS][32];
     grid_dependency_wait();
-    const int64_t p = blockIdx.x / slabs, e0 = p * a.piece, e1 = e0 + a.piece;
-    const uint32_t k = a.keys[e1 - 1];           // (a piece with one behind it is whole)
-    if (k >= (uint32_t)a.vocab || a.keys[e1] != k) return;
-    if (a.keys[e0] == k && e0 > 0 && a.keys[e0 - 1] == k) return;
-    int64_t lo = e1, hi = a.tokens;              // the first sorted key above k
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (a.keys[mid] <= k) lo = mid + 1; else hi = mid;
-    }
-    const int64_t rows = (lo - 1) / a.piece - p + 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t col = ((int64_t)(blockIdx.x - p * slabs) * 32 + lane) * 4;
-    const int64_t r0 = rows * warp / JOIN_WARPS, r1 = rows * (warp + 1) / JOIN_WARPS;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (col < a.ldp) {
-#pragma unroll 4
-        for (int64_t r = r0; r < r1; ++r) {
-            const float4 x = *reinterpret_cast<const float4*>(a.partial + ((p + r) * 2 + (r == 0 ? 1 : 0)) * a.ldp + col);
-            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    auto partial = [&](int64_t p, int which, int64_t col) { return *reinterpret_cast<const float4*>(a.partial + (p * 2 + which) * a.ldp + col); };
+    const int64_t near = (int64_t)a.crossing[0] * slabs, far = (int64_t)a.crossing[1] * slabs;
+    for (int64_t u = blockIdx.x; u < far; u += gridDim.x) {
+        const int64_t p = a.crossing[2 + a.pieces + u / slabs], col = (u % slabs * 32 + lane) * 4;
+        const uint32_t k = a.keys[p * a.piece + a.piece - 1];
+        int64_t lo = (p + 1) * a.piece, hi = a.tokens;          // the first sorted key above k
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) >> 1;
+            if (a.keys[mid] <= k) lo = mid + 1; else hi = mid;
         }
-    }
-    sums[warp][lane] = v;
-    __syncthreads();
-    if (warp != 0 || col >= a.width) return;
+        const int64_t rows = (lo - 1) / a.piece - p + 1, r0 = rows * warp / JOIN_WARPS, r1 = rows * (warp + 1) / JOIN_WARPS;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (col < a.ldp) {
+#pragma unroll 4
+            for (int64_t r = r0; r < r1; ++r) add(v, partial(p + r, r == 0 ? 1 : 0, col));
+        }
+        sums[warp][lane] = v;
+        __syncthreads();
+        if (warp == 0 && col < a.width) {
 #pragma unroll
-    for (int w = 1; w < JOIN_WARPS; ++w) {
-        const float4 x = sums[w][lane];
-        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+            for (int w = 1; w < JOIN_WARPS; ++w) add(v, sums[w][lane]);
+            write_four(a, k, col, v, aligned != 0);
+        }
+        __syncthreads();
     }
-    const float acc[4] = {v.x, v.y, v.z, v.w};
-    if (col + 4 <= a.width) {
-        write_row<4>(a, k, col, acc, aligned != 0);
-    } else {
-        for (int e = 0; col + e < a.width; ++e) write_row<1>(a, k, col + e, acc + e, true);
+    for (int64_t u = (int64_t)blockIdx.x * JOIN_WARPS + warp; u < near; u += (int64_t)gridDim.x * JOIN_WARPS) {
+        const int64_t p = a.crossing[2 + u / slabs], col = (u % slabs * 32 + lane) * 4;
+        if (col >= a.width) continue;
+        float4 v = partial(p, 1, col);
+        add(v, partial(p + 1, 0, col));
+        write_four(a, a.keys[p * a.piece + a.piece - 1], col, v, aligned != 0);
     }
 }
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 struct Layout {
-    int64_t keys, order, keys2, order2, counts, partial, bytes;
+    int64_t keys, order, keys2, order2, counts, named, crossing, partial, bytes;
     int64_t ldp, pieces;
     int piece, tile, tiles;
 };
-Layout layout_of(int64_t tokens, int64_t width) {
+Layout layout_of(int64_t tokens, int64_t vocab, int64_t width) {
     Layout l = {};
     l.piece = piece_of(tokens);
     l.pieces = (tokens + l.piece - 1) / l.piece;
@@ -434,7 +514,9 @@ Layout layout_of(int64_t tokens, int64_t width) {
         l.keys2 = at; at += list;
         l.order2 = at; at += list;
         l.counts = at; at += (int64_t)l.tiles * DIGITS * 4;
+        l.named = at; at += round_up(vocab / 8 + 8, 256);
     }
+    l.crossing = at; at += round_up(4 * (2 + 2 * l.pieces), 256);
     l.partial = at;
     at += l.pieces * 2 * l.ldp * 4;
     l.bytes = at;
@@ -459,17 +541,19 @@ cudaError_t launch_embed(const EmbedArgs& a, int num_sms, cudaStream_t s, uint64
     return e;
 }
 
-size_t embed_grad_workspace(int64_t tokens, int64_t, int64_t width) { return (size_t)layout_of(tokens, width).bytes; }
+size_t embed_grad_workspace(int64_t tokens, int64_t vocab, int64_t width) { return (size_t)layout_of(tokens, vocab, width).bytes; }
 
-cudaError_t launch_embed_grad(const EmbedGradArgs& a, cudaStream_t st, uint64_t* launches) {
-    const Layout l = layout_of(a.tokens, a.width);
+cudaError_t launch_embed_grad(const EmbedGradArgs& a, int num_sms, cudaStream_t st, uint64_t* launches) {
+    const Layout l = layout_of(a.tokens, a.vocab, a.width);
     unsigned char* ws = static_cast<unsigned char*>(a.workspace);
     uint32_t* keys = reinterpret_cast<uint32_t*>(ws + l.keys);
     uint32_t* order = reinterpret_cast<uint32_t*>(ws + l.order);
+    uint32_t* crossing = reinterpret_cast<uint32_t*>(ws + l.crossing);
+    uint32_t* named = !a.accumulate && a.tokens > RANK_MAX ? reinterpret_cast<uint32_t*>(ws + l.named) : nullptr;
     cudaError_t e = cudaSuccess;
     if (a.tokens > 0 && a.tokens <= RANK_MAX) {
         constexpr int PER = RANK_THREADS / RANK_SHARE;
-        e = launch_pdl(rank_kernel, dim3((unsigned)((a.tokens + PER - 1) / PER)), dim3(RANK_THREADS), 0, st, a.ids, a.id_bytes, (int)a.tokens, a.vocab, keys, order, a.status);
+        e = launch_pdl(rank_kernel, dim3((unsigned)((a.tokens + PER - 1) / PER)), dim3(RANK_THREADS), 0, st, a.ids, a.id_bytes, (int)a.tokens, a.vocab, keys, order, crossing, a.status);
         if (e != cudaSuccess) return e;
         ++*launches;
     } else if (a.tokens > 0) {
@@ -479,6 +563,7 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, cudaStream_t st, uint64_t*
         uint32_t *k2 = reinterpret_cast<uint32_t*>(ws + l.keys2), *o2 = reinterpret_cast<uint32_t*>(ws + l.order2);
         SortPass p = {};
         p.id_bytes = a.id_bytes; p.vocab = a.vocab; p.tokens = a.tokens; p.tile = l.tile; p.tiles = l.tiles; p.digits = 1 << digit; p.status = a.status;
+        p.named = named; p.crossing = crossing;
         p.counts = reinterpret_cast<uint32_t*>(ws + l.counts);
         for (int i = 0; i < passes; ++i) {
             // the last pass ends in keys and order
@@ -496,7 +581,7 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, cudaStream_t st, uint64_t*
     SumArgs s = {};
     s.dy = a.dy; s.lddy = a.lddy; s.keys = keys; s.order = order; s.partial = reinterpret_cast<float*>(ws + l.partial); s.ldp = l.ldp;
     s.tokens = a.tokens; s.vocab = a.vocab; s.width = a.width; s.ld = a.ld; s.dtable = a.dtable; s.scale = a.scale; s.d_type = a.d_type;
-    s.accumulate = a.accumulate; s.piece = l.piece; s.pieces = l.pieces;
+    s.named = named; s.crossing = crossing; s.accumulate = a.accumulate; s.piece = l.piece; s.pieces = l.pieces;
     const int64_t dsize = a.d_type == CERAR_TYPE_F32 ? 4 : 2;
     const uintptr_t dt = reinterpret_cast<uintptr_t>(a.dtable), dy = reinterpret_cast<uintptr_t>(a.dy);
     s.zero_vec = dt % 16 == 0 && a.ld * dsize % 16 == 0 && a.width * dsize % 16 == 0;
@@ -510,10 +595,8 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, cudaStream_t st, uint64_t*
     ++*launches;
     if (l.pieces > 1) {
         const int slabs = (int)((l.ldp + 127) / 128);
-        const int64_t blocks = (l.pieces - 1) * slabs;
-        if (blocks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
-        const int64_t four = 4 * dsize;
-        e = launch_pdl(join_kernel, dim3((unsigned)blocks), dim3(32 * JOIN_WARPS), 0, st, s, slabs, (int)(dt % four == 0 && a.ld * dsize % four == 0));
+        const int64_t units = (l.pieces - 1) * slabs, most = (int64_t)num_sms * 6, four = 4 * dsize;
+        e = launch_pdl(join_kernel, dim3((unsigned)(units < most ? units : most)), dim3(32 * JOIN_WARPS), 0, st, s, slabs, (int)(dt % four == 0 && a.ld * dsize % four == 0));
         if (e != cudaSuccess) return e;
         ++*launches;
     }

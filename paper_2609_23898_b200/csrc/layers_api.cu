@@ -127,7 +127,7 @@ cerar_status_t cerar_embed_grad(cerar_ops_t* o, const void* dy, cerar_type_t typ
     if (need > 0 && (!workspace || misaligned(workspace, 16))) return fail(CERAR_ERR_INVALID_ARG, "workspace NULL or not aligned to 16 bytes");
     if (workspace_bytes < need) return fail(CERAR_ERR_SHAPE, "the workspace is too small");
     const cerar::EmbedGradArgs a = {dy, lddy, ids, id_bytes, tokens, scale, dtable, vocab, width, ld, type, d_type, accumulate != 0, workspace, o->d_status};
-    const cudaError_t e = cerar::launch_embed_grad(a, (cudaStream_t)stream, &o->launches);
+    const cudaError_t e = cerar::launch_embed_grad(a, o->num_sms, (cudaStream_t)stream, &o->launches);
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "embed gradient launch");
 }
 

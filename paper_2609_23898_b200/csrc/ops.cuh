@@ -130,7 +130,7 @@ struct EmbedGradArgs {
     int* status;
 };
 size_t embed_grad_workspace(int64_t tokens, int64_t vocab, int64_t width);
-cudaError_t launch_embed_grad(const EmbedGradArgs& a, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_embed_grad(const EmbedGradArgs& a, int num_sms, cudaStream_t s, uint64_t* launches);
 
 struct HeadPart {                        // queries or keys
     const void *x, *dy, *w;              // w: null where all are one
