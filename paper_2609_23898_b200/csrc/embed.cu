@@ -134,7 +134,7 @@ cudaError_t launch_lookup_typed(const EmbedArgs& a, int num_sms, cudaStream_t s)
 // Short lists: a token's place is the number of keys in front of it, counted; eight threads share a token's count.  T^2 comparisons are
 // one launch where a radix sort would be four.
 
-constexpr int RANK_THREADS = 256, RANK_SHARE = 8, RANK_MAX = 4096;
+constexpr int RANK_THREADS = 256, RANK_SHARE = 8, RANK_MAX = 8192;
 
 __global__ void __launch_bounds__(RANK_THREADS) rank_kernel(const void* ids, int id_bytes, int tokens, int64_t vocab, uint32_t* keys, uint32_t* order, uint32_t* crossing, int* status) {
     __shared__ __align__(16) uint32_t all[RANK_MAX];
@@ -163,10 +163,10 @@ __global__ void __launch_bounds__(RANK_THREADS) rank_kernel(const void* ids, int
     }
 }
 
-// Long lists: least significant digit first, digits of up to 9 bits, two launches per digit: the digits' counts in every tile, then every
-// tile's tokens to their places.  A warp owns a run of its tile; equal digits among its 32 tokens are ranked by their lanes, so
-// every pass keeps the order.
-constexpr int DIGIT_MAX = 9, DIGITS = 1 << DIGIT_MAX, SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32;
+// Long lists: least significant digit first, digits of up to 9 bits.  One launch counts the first digit in every tile; one for each digit brings
+// every tile's tokens to their places and counts the next digit where they go.  A warp owns a run of its tile; equal digits among its 32
+// tokens are ranked by their lanes, so every pass keeps the order.
+constexpr int DIGIT_MAX = 9, PASSES_MAX = 4 /* 32 bits */, DIGITS = 1 << DIGIT_MAX, SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32;
 constexpr int SORT_TILE = 2048, SORT_TILES_MAX = 256, KEYS = SORT_TILE / SORT_THREADS;
 constexpr uint32_t NONE = 0xFFFFFFFFu;
 
@@ -175,10 +175,12 @@ struct SortPass {
     int id_bytes;
     int64_t vocab;
     const uint32_t *keys_in, *order_in;
-    uint32_t *keys, *order, *counts;           // counts: [tiles][DIGITS]
+    uint32_t *keys, *order, *counts;           // counts: [tiles][DIGITS], of this digit
+    uint32_t* next_counts;                     // of the next one (null: there is none): cleared by the first kernel, counted while placing
+    int passes;
     uint32_t *named, *crossing;                // a bit for every row that some token names (cleared by the first count, set by the first placing)
     int64_t tokens;
-    int tile, tiles, shift, digits;            // digits: a power of two
+    int tile, tiles, shift, next_shift, digits; // digits: a power of two
     int* status;
 };
 __device__ __forceinline__ uint32_t sort_key(const SortPass& p, int64_t t) {
@@ -190,8 +192,9 @@ __global__ void __launch_bounds__(SORT_THREADS) count_kernel(const SortPass p) {
     count[threadIdx.x] = 0;
     grid_dependency_wait();
     __syncthreads();
-    if (p.ids) {
+    {
         if (blockIdx.x == 0 && threadIdx.x < 2) p.crossing[threadIdx.x] = 0u;
+        for (int i = 1; i < p.passes; ++i) p.counts[((int64_t)i * p.tiles + blockIdx.x) * DIGITS + threadIdx.x] = 0u;
         if (p.named)
             for (int64_t w = (int64_t)blockIdx.x * SORT_THREADS + threadIdx.x; w <= p.vocab / 32; w += (int64_t)gridDim.x * SORT_THREADS) p.named[w] = 0u;
     }
@@ -212,16 +215,27 @@ __global__ void __launch_bounds__(SORT_THREADS) place_kernel(const SortPass p) {
     const int64_t t0 = (int64_t)blockIdx.x * p.tile + (int64_t)warp * (p.tile / SORT_WARPS), t1 = t0 + p.tile / SORT_WARPS;
     const uint32_t dmask = p.digits - 1;
     // A run of a tile of the usual size is four keys per lane, which stay in registers (and their loads on their way together).
-    uint32_t held[KEYS];
+    uint32_t held[KEYS], number[KEYS];
     auto load = [&](int64_t from) {
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
             const int64_t t = from + i * 32 + lane;
-            held[i] = t < t1 && t < p.tokens ? sort_key(p, t) : NONE;
+            const bool there = t < t1 && t < p.tokens;
+            held[i] = there ? sort_key(p, t) : NONE;
+            number[i] = !p.ids && there ? p.order_in[t] : (uint32_t)t;
         }
     };
+    if (t1 - t0 <= 32 * KEYS) load(t0);
+    // This digit's (thread's) tokens, and those of the tiles in front.
+    uint32_t total = 0, front = 0;
+#pragma unroll 16
+    for (int i = 0; i < p.tiles; ++i) {
+        const uint32_t c = p.counts[(int64_t)i * DIGITS + threadIdx.x];
+        total += c;
+        if (i < (int)blockIdx.x) front += c;
+    }
     for (int64_t from = t0; from < t1 && from < p.tokens; from += 32 * KEYS) {
-        load(from);
+        if (t1 - t0 > 32 * KEYS) load(from);
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
             const bool there = held[i] != NONE;
@@ -232,14 +246,7 @@ __global__ void __launch_bounds__(SORT_THREADS) place_kernel(const SortPass p) {
             __syncwarp();
         }
     }
-    // This digit's (thread's) first place: the smaller digits' tokens, the same digit's of the tiles in front.
-    uint32_t total = 0, front = 0;
-#pragma unroll 8
-    for (int i = 0; i < p.tiles; ++i) {
-        const uint32_t c = p.counts[(int64_t)i * DIGITS + threadIdx.x];
-        total += c;
-        if (i < (int)blockIdx.x) front += c;
-    }
+    // The first place: the smaller digits' tokens, the same digit's of the tiles in front.
     uint32_t incl = total;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -260,7 +267,6 @@ __global__ void __launch_bounds__(SORT_THREADS) place_kernel(const SortPass p) {
         if (t1 - t0 > 32 * KEYS) load(from);
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
-            const int64_t t = from + i * 32 + lane;
             const bool there = held[i] != NONE;
             const uint32_t d = there ? (held[i] >> p.shift) & dmask : NONE;
             const uint32_t same = __match_any_sync(0xffffffffu, d);
@@ -270,7 +276,8 @@ __global__ void __launch_bounds__(SORT_THREADS) place_kernel(const SortPass p) {
             if (there) {
                 if (lane == __ffs(same) - 1) at[warp][d] += __popc(same);
                 p.keys[to] = held[i];
-                p.order[to] = p.ids ? (uint32_t)t : p.order_in[t];
+                p.order[to] = number[i];
+                if (p.next_counts) atomicAdd(p.next_counts + (int64_t)(to / (uint32_t)p.tile) * DIGITS + ((held[i] >> p.next_shift) & dmask), 1u);
             }
             __syncwarp();
         }
@@ -279,6 +286,7 @@ __global__ void __launch_bounds__(SORT_THREADS) place_kernel(const SortPass p) {
 
 // ------------------------------------------------------------------------------------------------ sums
 
+constexpr int SHORT_ROWS = 16;
 constexpr int SUM_THREADS = 128, PIECE_MAX = 64, ZERO_ROWS = 32;
 
 // Tokens of a piece.  Short batches need the blocks, long ones the few partial rows.
@@ -289,7 +297,7 @@ struct SumArgs {
     int64_t lddy;
     const uint32_t *keys, *order;              // sorted
     const uint32_t* named;                     // a bit for every row that some token names; null: it is looked for in the sorted keys
-    uint32_t* crossing;                        // numbers of, and then, the pieces whose last token goes on into the next piece only; into more
+    uint32_t* crossing;                        // numbers of, and then, the pieces whose last token has up to SHORT_ROWS partial rows; more
     float* partial;                            // [pieces][2][ldp]: of the token that came over the piece's start, of the one that goes over its end
     int64_t ldp;
     int64_t tokens, vocab, width, ld;
@@ -424,7 +432,7 @@ __global__ void __launch_bounds__(SUM_THREADS) sum_kernel(const SumArgs a) {
                 write_row<CH>(a, k, col, acc, true);
             } else {
                 if (!came && col == 0) {         // its sum begins here and goes on: the next kernel puts it together
-                    const int64_t after = e0 + 2 * a.piece;
+                    const int64_t after = e0 + (int64_t)SHORT_ROWS * a.piece;
                     const int far = after < a.tokens && a.keys[after] == k;
                     a.crossing[2 + far * a.pieces + atomicAdd(a.crossing + far, 1u)] = (uint32_t)piece;
                 }
@@ -439,10 +447,10 @@ __global__ void __launch_bounds__(SUM_THREADS) sum_kernel(const SumArgs a) {
     }
 }
 
-// Tokens that go over the end of a piece p in which their sum began: partial rows p (second), p + 1 ... (first), in this order.  Those of two rows:
-// a warp adds 128 columns.  Those of more: eight warps take a run of the rows of 128 columns each, and their sums are added in the order of
-// the runs.  (The order of the lists is that of atomics; what is added, and in which order, does not depend on it.)
-constexpr int JOIN_WARPS = 8;
+// Tokens that go over the end of a piece p in which their sum began: partial rows p (second), p + 1 ... (first), in this order.  Up to sixteen rows:
+// a warp adds 128 columns.  More: sixteen warps take a run of the rows of 128 columns each, and their sums are added in the order of the
+// runs.  (The order of the lists is that of atomics; what is added, and in which order, does not depend on it.)
+constexpr int JOIN_WARPS = 16;
 __device__ __forceinline__ void write_four(const SumArgs& a, uint32_t k, int64_t col, const float4& v, bool aligned) {
     const float acc[4] = {v.x, v.y, v.z, v.w};
     if (col + 4 <= a.width) {
@@ -459,19 +467,18 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) join_kernel(const SumArgs a, 
     grid_dependency_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     auto partial = [&](int64_t p, int which, int64_t col) { return *reinterpret_cast<const float4*>(a.partial + (p * 2 + which) * a.ldp + col); };
-    const int64_t near = (int64_t)a.crossing[0] * slabs, far = (int64_t)a.crossing[1] * slabs;
-    for (int64_t u = blockIdx.x; u < far; u += gridDim.x) {
+    // whether the sum that began in piece p has a row in piece q > p: true up to its last one
+    auto goes_on = [&](uint32_t k, int64_t q) { return q * a.piece < a.tokens && a.keys[q * a.piece] == k; };
+    const int64_t few = (int64_t)a.crossing[0] * slabs, many = (int64_t)a.crossing[1] * slabs;
+    for (int64_t u = blockIdx.x; u < many; u += gridDim.x) {
         const int64_t p = a.crossing[2 + a.pieces + u / slabs], col = (u % slabs * 32 + lane) * 4;
         const uint32_t k = a.keys[p * a.piece + a.piece - 1];
-        int64_t lo = (p + 1) * a.piece, hi = a.tokens;          // the first sorted key above k
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (a.keys[mid] <= k) lo = mid + 1; else hi = mid;
-        }
-        const int64_t rows = (lo - 1) / a.piece - p + 1, r0 = rows * warp / JOIN_WARPS, r1 = rows * (warp + 1) / JOIN_WARPS;
+        int64_t rows = 1;
+        for (int n = 32 * JOIN_WARPS; n == 32 * JOIN_WARPS; rows += n) n = __syncthreads_count(goes_on(k, p + rows + threadIdx.x));
+        const int64_t r0 = rows * warp / JOIN_WARPS, r1 = rows * (warp + 1) / JOIN_WARPS;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (col < a.ldp) {
-#pragma unroll 4
+#pragma unroll 8
             for (int64_t r = r0; r < r1; ++r) add(v, partial(p + r, r == 0 ? 1 : 0, col));
         }
         sums[warp][lane] = v;
@@ -483,12 +490,15 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) join_kernel(const SumArgs a, 
         }
         __syncthreads();
     }
-    for (int64_t u = (int64_t)blockIdx.x * JOIN_WARPS + warp; u < near; u += (int64_t)gridDim.x * JOIN_WARPS) {
+    for (int64_t u = (int64_t)blockIdx.x * JOIN_WARPS + warp; u < few; u += (int64_t)gridDim.x * JOIN_WARPS) {
         const int64_t p = a.crossing[2 + u / slabs], col = (u % slabs * 32 + lane) * 4;
+        const uint32_t k = a.keys[p * a.piece + a.piece - 1];
+        const int rows = 1 + __popc(__ballot_sync(0xffffffffu, lane < SHORT_ROWS && goes_on(k, p + 1 + lane)));
         if (col >= a.width) continue;
         float4 v = partial(p, 1, col);
-        add(v, partial(p + 1, 0, col));
-        write_four(a, a.keys[p * a.piece + a.piece - 1], col, v, aligned != 0);
+#pragma unroll 4
+        for (int r = 1; r < rows; ++r) add(v, partial(p + r, 0, col));
+        write_four(a, k, col, v, aligned != 0);
     }
 }
 
@@ -513,7 +523,7 @@ Layout layout_of(int64_t tokens, int64_t vocab, int64_t width) {
         l.tiles = (int)((tokens + l.tile - 1) / l.tile);
         l.keys2 = at; at += list;
         l.order2 = at; at += list;
-        l.counts = at; at += (int64_t)l.tiles * DIGITS * 4;
+        l.counts = at; at += (int64_t)l.tiles * DIGITS * 4 * PASSES_MAX;
         l.named = at; at += round_up(vocab / 8 + 8, 256);
     }
     l.crossing = at; at += round_up(4 * (2 + 2 * l.pieces), 256);
@@ -565,17 +575,20 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, int num_sms, cudaStream_t 
         p.id_bytes = a.id_bytes; p.vocab = a.vocab; p.tokens = a.tokens; p.tile = l.tile; p.tiles = l.tiles; p.digits = 1 << digit; p.status = a.status;
         p.named = named; p.crossing = crossing;
         p.counts = reinterpret_cast<uint32_t*>(ws + l.counts);
+        p.passes = passes; p.ids = a.ids;
+        if ((e = launch_pdl(count_kernel, dim3((unsigned)l.tiles), dim3(SORT_THREADS), 0, st, p)) != cudaSuccess) return e;
+        ++*launches;
         for (int i = 0; i < passes; ++i) {
             // the last pass ends in keys and order
             const bool to_first = (passes - 1 - i) % 2 == 0;
             p.ids = i == 0 ? a.ids : nullptr;
             p.keys_in = to_first ? k2 : keys; p.order_in = to_first ? o2 : order;
             p.keys = to_first ? keys : k2; p.order = to_first ? order : o2;
-            p.shift = i * digit;
-            if ((e = launch_pdl(count_kernel, dim3((unsigned)l.tiles), dim3(SORT_THREADS), 0, st, p)) != cudaSuccess) return e;
-            ++*launches;
+            p.shift = i * digit; p.next_shift = p.shift + digit;
+            p.next_counts = i + 1 < passes ? p.counts + (int64_t)l.tiles * DIGITS : nullptr;
             if ((e = launch_pdl(place_kernel, dim3((unsigned)l.tiles), dim3(SORT_THREADS), 0, st, p)) != cudaSuccess) return e;
             ++*launches;
+            p.counts += (int64_t)l.tiles * DIGITS;
         }
     }
     SumArgs s = {};
@@ -595,7 +608,7 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, int num_sms, cudaStream_t 
     ++*launches;
     if (l.pieces > 1) {
         const int slabs = (int)((l.ldp + 127) / 128);
-        const int64_t units = (l.pieces - 1) * slabs, most = (int64_t)num_sms * 6, four = 4 * dsize;
+        const int64_t units = (l.pieces - 1) * slabs, most = (int64_t)num_sms * 4, four = 4 * dsize;
         e = launch_pdl(join_kernel, dim3((unsigned)(units < most ? units : most)), dim3(32 * JOIN_WARPS), 0, st, s, slabs, (int)(dt % four == 0 && a.ld * dsize % four == 0));
         if (e != cudaSuccess) return e;
         ++*launches;
