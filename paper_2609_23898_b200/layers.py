@@ -14,31 +14,46 @@ The formulas and rules stand in include/cerar.h.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 from torch.autograd.function import once_differentiable
 
 from . import cerar
 from .cerar import lib
-from .training import Ops, _check, _ld, _matrix, _rows, _stream, _type
+from .training import _TYPES, Ops, _check, _matrix, _raw_stream, _rows, _stream, _type
 
 HALVES, NEIGHBOURS = "halves", "neighbours"
+_raw = _stream if _raw_stream is None else _raw_stream
 _IDS = {torch.int32: 4, torch.int64: 8}
 
 
 def _whole(t: torch.Tensor, what: str) -> int:
-    if t.dtype not in _IDS:
+    size = _IDS.get(t.dtype)
+    if size is None:
         raise TypeError(f"{what}: int32 or int64 wanted, got {t.dtype}")
-    return _IDS[t.dtype]
+    return size
 
 
-def _same_device(ops: Ops, **tensors):
-    for what, t in tensors.items():
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError(f"{what}: a CUDA tensor is wanted")
-        ops._here(t.device)
+def _kind(t: torch.Tensor, what: str) -> int:
+    kind = _TYPES.get(t.dtype)
+    return _type(t, what) if kind is None else kind
+
+
+def _here(ops: Ops, tensors, names: str):
+    """All of them (but None) on the operators' device; `names` are looked at only to say which one is not."""
+    index = ops._index
+    for i, t in enumerate(tensors):
+        if t is not None and t.get_device() != index:
+            if not t.is_cuda:
+                raise ValueError(f"{names.split()[i]}: a CUDA tensor is wanted")
+            ops._here(t.device)
+
+
+def _stride(t: torch.Tensor) -> int:
+    """Elements between rows of a matrix that _matrix or _operand has let pass (one row, or none: its length)."""
+    rows, cols = t.shape
+    return t.stride(0) if rows > 1 and cols else cols
 
 
 def _no_gradient(**tensors):
@@ -58,15 +73,15 @@ def _anchor(device, wanted: bool):
 def embed(ops: Ops, table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, dtype: torch.dtype | None = None) -> torch.Tensor:
     """scale * table[ids], of `dtype` (the table's): shape of ids, then the table's width.  An id below zero is padding and gives zeros;
     one beyond the table does so too, and Ops.status raises."""
-    _same_device(ops, table=table, ids=ids)
+    _here(ops, (table, ids), "table ids")
     _matrix(table, "table")
-    kind, size = _type(table, "table"), _whole(ids, "ids")
+    kind, size = _kind(table, "table"), _whole(ids, "ids")
     if not ids.is_contiguous():
         ids = ids.contiguous()
     vocab, width = table.shape
-    y = torch.empty(*ids.shape, width, dtype=dtype or table.dtype, device=table.device)
-    st = lib.cerar_embed(ops._h, table.data_ptr(), kind, vocab, width, _ld(table), ids.data_ptr(), size, ids.numel(), scale, y.data_ptr(),
-                         _type(y, "dtype"), width, _stream(table.device.index))
+    y = torch.empty((*ids.shape, width), dtype=dtype or table.dtype, device=table.device)
+    st = lib.cerar_embed(ops._h, table.data_ptr(), kind, vocab, width, _stride(table), ids.data_ptr(), size, ids.numel(), scale, y.data_ptr(),
+                         _kind(y, "dtype"), width, _raw(ops._index))
     if st:
         _check(st)
     return y
@@ -75,21 +90,20 @@ def embed(ops: Ops, table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.
 def embed_backward(ops: Ops, dy: torch.Tensor, ids: torch.Tensor, dtable: torch.Tensor, *, scale: float = 1.0, accumulate=True):
     """dtable[v] += scale * the sum of dy over the tokens v (without accumulate: = that, and zeros for tokens that ids has none of).
     Deterministic."""
-    _same_device(ops, dy=dy, ids=ids, dtable=dtable)
+    _here(ops, (dy, ids, dtable), "dy ids dtable")
     _matrix(dtable, "dtable")
     vocab, width = dtable.shape
-    if dy.dim() < 1 or tuple(dy.shape) != (*ids.shape, width):
+    if dy.shape != (*ids.shape, width):
         raise ValueError(f"dy of shape {(*ids.shape, width)} wanted, got {tuple(dy.shape)}")
-    kind, size = _type(dy, "dy"), _whole(ids, "ids")
+    kind, size = _kind(dy, "dy"), _whole(ids, "ids")
     dy = _rows(dy)
     if not ids.is_contiguous():
         ids = ids.contiguous()
     n = ids.numel()
     need = lib.cerar_embed_grad_workspace(n, vocab, width)
     ws = torch.empty(need, dtype=torch.uint8, device=dtable.device)
-    st = lib.cerar_embed_grad(ops._h, dy.data_ptr(), kind, _ld(dy) if dy.numel() else width, ids.data_ptr(), size, n, scale, dtable.data_ptr(),
-                              _type(dtable, "dtable"), vocab, width, _ld(dtable) if dtable.numel() else width, accumulate, ws.data_ptr(), need,
-                              _stream(dtable.device.index))
+    st = lib.cerar_embed_grad(ops._h, dy.data_ptr(), kind, _stride(dy), ids.data_ptr(), size, n, scale, dtable.data_ptr(),
+                              _kind(dtable, "dtable"), vocab, width, _stride(dtable), accumulate, ws.data_ptr(), need, _raw(ops._index))
     if st:
         _check(st)
 
@@ -127,83 +141,84 @@ def rotation_table(ops: Ops, rows: int, dim: int, *, base: float = 10000.0, freq
     if dim < 0 or dim % 2 or len(freqs) != dim // 2:
         raise ValueError("rotation_table: an even dim and dim / 2 frequencies are wanted")
     table = torch.empty(rows, dim // 2, 2, dtype=torch.float32, device=torch.device("cuda", ops._index))
-    _check(lib.cerar_rotation_table(ops._h, (C.c_double * len(freqs))(*freqs), len(freqs), first, rows, table.data_ptr(), _stream(ops._index)))
+    _check(lib.cerar_rotation_table(ops._h, (C.c_double * len(freqs))(*freqs), len(freqs), first, rows, table.data_ptr(), _raw(ops._index)))
     return table
 
 
 def _heads(t: torch.Tensor, what: str) -> torch.Tensor:
     """t (..., heads, dim) as (tokens, heads, dim) with a head's values next to one another: a copy only where there is no such view."""
-    if t.dim() < 3:
-        raise ValueError(f"{what}: (tokens, heads, values) or more dimensions are wanted")
-    t = t if t.dim() == 3 else t.flatten(0, -3)
+    if t.dim() != 3:
+        if t.dim() < 3:
+            raise ValueError(f"{what}: (tokens, heads, values) or more dimensions are wanted")
+        t = t.flatten(0, -3)
     return t if t.stride(2) == 1 or t.size(2) < 2 else t.contiguous()
 
 
-def _rotation(table, positions, lead, pairs, dim):
-    if pairs not in (HALVES, NEIGHBOURS):
+_PARTS, _ROTATION = struct.Struct("24q"), struct.Struct("4q3i4x")         # two cerar_heads_t, one cerar_rotation_t
+assert _PARTS.size == 2 * C.sizeof(cerar.Heads) and _ROTATION.size == C.sizeof(cerar.Rotation)
+
+
+def _rotation(table, positions, lead, pairs) -> bytes:
+    """(positions: contiguous)"""
+    if pairs != HALVES and pairs != NEIGHBOURS:
         raise ValueError("pairs must be 'halves' or 'neighbours'")
-    period = lead[-1]
+    period, at, size, first, rows, rotated = lead[-1], 0, 8, 0, 0, 0
     if positions is not None:
         size = _whole(positions, "positions")
-        if tuple(positions.shape) != lead and tuple(positions.shape) != lead[-1:]:
-            raise ValueError(f"positions of shape {lead} or {lead[-1:]} wanted, got {tuple(positions.shape)}")
-        if not positions.is_contiguous():
-            positions = positions.contiguous()
-        period = positions.numel()
-    rotated = 0
+        if positions.shape != lead and positions.shape != lead[-1:]:
+            raise ValueError(f"positions of shape {tuple(lead)} or {tuple(lead[-1:])} wanted, got {tuple(positions.shape)}")
+        at, period = positions.data_ptr(), positions.numel()
     if table is not None:
         if table.dtype != torch.float32 or table.dim() != 3 or table.size(2) != 2 or not table.is_contiguous():
             raise ValueError("table: contiguous float32 of shape (positions, pairs, 2) wanted, as rotation_table makes it")
-        rotated = 2 * table.size(1)
-    r = cerar.Rotation(None if table is None else table.data_ptr(), 0 if table is None else table.size(0),
-                       None if positions is None else positions.data_ptr(), max(period, 1), 8 if positions is None else size, rotated, pairs == NEIGHBOURS)
-    return r, positions               # (positions: kept until the call has been made)
+        first, rows, rotated = table.data_ptr(), table.size(0), 2 * table.size(1)
+    return _ROTATION.pack(first, rows, at, period or 1, size, rotated, pairs == NEIGHBOURS)
 
 
-def _parts(q, k, wq, wk, out, dq=None, dk=None, dwq=None, dwk=None):
-    """The descriptors of a call, its results, and the weights' types."""
-    if out is None:
-        out = (None, None)
-    parts = (cerar.Heads * (1 if k is None else 2))()
-    keep, ys, w_type, dw_type = [], [], None, None
-    for i, (x, w, y, dy, dw) in enumerate(((q, wq, out[0], dq, dwq), (k, wk, out[1], dk, dwk))[:len(parts)]):
-        what = "qk"[i]
-        x3 = _heads(x, what)
-        n, h, d = x3.shape
-        if i and (x.shape[:-2] != q.shape[:-2] or d != q.shape[-1] or x.dtype != q.dtype):
-            raise ValueError("q and k: the same tokens, values per head and type are wanted")
-        if y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        elif y.shape != x.shape or y.dtype != x.dtype:
+def _part(what, x, w, y, dy, dw, like, types):
+    """One group of heads: its fields of the descriptor, the result, its numbers, and what has to live until the call has been made.
+    types: those of the weights and of their gradients so far."""
+    shape, dtype = x.shape, x.dtype
+    if like is not None and (shape[:-2] != like.shape[:-2] or shape[-1] != like.shape[-1] or dtype != like.dtype):
+        raise ValueError("q and k: the same tokens, values per head and type are wanted")
+    x3 = _heads(x, what)
+    n, h, d = x3.shape
+    sx = x3.stride()
+    if y is None:
+        y = torch.empty(shape, dtype=dtype, device=x.device)
+        y3, ty, hy = y, h * d, d
+    else:
+        if y.shape != shape or y.dtype != dtype:
             raise ValueError("out: tensors of the shapes and type of q and k are wanted")
-        y3 = y if y.dim() == 3 else y.view(n, h, d) if y.is_contiguous() else y.flatten(0, -3)
-        if y3.data_ptr() != y.data_ptr() or (y3.stride(2) != 1 and d > 1):
+        y3 = y if y.dim() == 3 else y.flatten(0, -3)
+        ty, hy, cy = y3.stride()
+        if y3.data_ptr() != y.data_ptr() or (cy != 1 and d > 1):
             raise ValueError("out: leading dimensions that can be flattened and contiguous heads are wanted")
-        p = parts[i]
-        p.x, p.x_token, p.x_head, p.y, p.y_token, p.y_head, p.heads = x3.data_ptr(), x3.stride(0), x3.stride(1), y3.data_ptr(), y3.stride(0), y3.stride(1), h
-        if w is not None:
-            if w.dim() != 1 or w.numel() != d or not w.is_contiguous():
-                raise ValueError(f"w{what}: {d} contiguous weights wanted")
-            t = _type(w, "w" + what)
-            if w_type is not None and t != w_type:
-                raise TypeError("wq and wk: one type is wanted")
-            p.w, w_type = w.data_ptr(), t
-        if dy is not None:
-            if dy.shape != x.shape or dy.dtype != x.dtype:
-                raise ValueError(f"d{what}: the shape and type of {what} wanted")
-            dy3 = _heads(dy, "d" + what)
-            p.dy, p.dy_token, p.dy_head = dy3.data_ptr(), dy3.stride(0), dy3.stride(1)
-            keep.append(dy3)
-        if dw is not None:
-            if dw.dim() != 1 or dw.numel() != d or not dw.is_contiguous():
-                raise ValueError(f"dw{what}: {d} contiguous values wanted")
-            t = _type(dw, "dw" + what)
-            if dw_type is not None and t != dw_type:
-                raise TypeError("dwq and dwk: one type is wanted")
-            p.dw, dw_type = dw.data_ptr(), t
-        keep += [x3, y3]
-        ys.append(y)
-    return parts, (ys + [None])[:2], w_type or 0, dw_type or 0, keep
+    pw = pdw = pdy = tdy = hdy = 0
+    dy3 = None
+    if w is not None:
+        if w.shape != (d,) or not w.is_contiguous():
+            raise ValueError(f"w{what}: {d} contiguous weights wanted")
+        kind = _kind(w, "w" + what)
+        if types[0] is not None and types[0] != kind:
+            raise TypeError("wq and wk: one type is wanted")
+        pw, types[0] = w.data_ptr(), kind
+    if dy is not None:
+        if dy.shape != shape or dy.dtype != dtype:
+            raise ValueError(f"d{what}: the shape and type of {what} wanted")
+        dy3 = _heads(dy, "d" + what)
+        pdy, (tdy, hdy, _) = dy3.data_ptr(), dy3.stride()
+    if dw is not None:
+        if dw.shape != (d,) or not dw.is_contiguous():
+            raise ValueError(f"dw{what}: {d} contiguous values wanted")
+        kind = _kind(dw, "dw" + what)
+        if types[1] is not None and types[1] != kind:
+            raise TypeError("dwq and dwk: one type is wanted")
+        pdw, types[1] = dw.data_ptr(), kind
+    return (x3.data_ptr(), y3.data_ptr(), pw, pdy, pdw, sx[0], sx[1], ty, hy, tdy, hdy, h), y, n, d, (x3, dy3)
+
+
+_NO_PART = (0,) * 12
 
 
 def head_norm(ops: Ops, q: torch.Tensor, k: torch.Tensor | None, wq, wk, table: torch.Tensor | None, positions: torch.Tensor | None = None, *,
@@ -212,36 +227,42 @@ def head_norm(ops: Ops, q: torch.Tensor, k: torch.Tensor | None, wq, wk, table: 
     by the token's position: those that `table` (rotation_table; None: no rotation) has pairs for.  positions: of every token, or of
     the last dimension of the tokens, for all sequences alike (None: 0, 1, ...); below zero: padding, whose result is zero; beyond the
     table: the same, and Ops.status raises.  q and k may be slices of one projection's result.  Returns both (in `out`, if given)."""
-    _same_device(ops, q=q, k=k, wq=wq, wk=wk, table=table, positions=positions)
-    kind = _type(q, "q")
-    parts, ys, w_type, _, keep = _parts(q, k, wq, wk, out)
-    lead = tuple(q.shape[:-2])
-    rot, positions = _rotation(table, positions, lead, pairs, q.shape[-1])
-    st = lib.cerar_head_norm(ops._h, kind, C.addressof(parts), len(parts), w_type, keep[0].size(0), q.shape[-1], eps, C.addressof(rot),
-                             _stream(q.device.index))
+    _here(ops, (q, k, wq, wk, table, positions), "q k wq wk table positions")
+    kind, types = _kind(q, "q"), [None, None]
+    yq, yk = (None, None) if out is None else out
+    first, yq, n, d, kept = _part("q", q, wq, yq, None, None, None, types)
+    second, yk, _, _, kept2 = (_NO_PART, None, 0, 0, None) if k is None else _part("k", k, wk, yk, None, None, q, types)
+    if positions is not None and not positions.is_contiguous():
+        positions = positions.contiguous()
+    rotation = _rotation(table, positions, q.shape[:-2], pairs)
+    st = lib.cerar_head_norm(ops._h, kind, _PARTS.pack(*first, *second), 1 if k is None else 2, types[0] or 0, n, d, eps, rotation, _raw(ops._index))
     if st:
         _check(st)
-    return ys[0], ys[1]
+    return yq, yk
 
 
 def head_norm_backward(ops: Ops, dq: torch.Tensor, dk: torch.Tensor | None, q: torch.Tensor, k: torch.Tensor | None, wq, wk, table, positions=None, *,
                        dwq=None, dwk=None, accumulate=True, eps: float = 1e-6, pairs: str = HALVES, out=None):
     """Gradients of q and k (in `out`, if given) from those of head_norm's results; dwq, dwk (float32 or bfloat16, None: not wanted) += those
     of the weights.  Deterministic."""
-    _same_device(ops, dq=dq, dk=dk, q=q, k=k, wq=wq, wk=wk, table=table, positions=positions, dwq=dwq, dwk=dwk)
-    kind = _type(q, "q")
+    _here(ops, (dq, dk, q, k, wq, wk, table, positions, dwq, dwk), "dq dk q k wq wk table positions dwq dwk")
+    kind, types = _kind(q, "q"), [None, None]
     if (dk is None) != (k is None) or (k is None and dwk is not None):
         raise ValueError("dk and dwk belong to k")
-    parts, ys, w_type, dw_type, keep = _parts(q, k, wq, wk, out, dq, dk, dwq, dwk)
-    lead = tuple(q.shape[:-2])
-    rot, positions = _rotation(table, positions, lead, pairs, q.shape[-1])
-    need = lib.cerar_head_norm_grad_workspace(len(parts), q.shape[-1])
+    yq, yk = (None, None) if out is None else out
+    first, yq, n, d, kept = _part("q", q, wq, yq, dq, dwq, None, types)
+    second, yk, _, _, kept2 = (_NO_PART, None, 0, 0, None) if k is None else _part("k", k, wk, yk, dk, dwk, q, types)
+    if positions is not None and not positions.is_contiguous():
+        positions = positions.contiguous()
+    rotation = _rotation(table, positions, q.shape[:-2], pairs)
+    count = 1 if k is None else 2
+    need = lib.cerar_head_norm_grad_workspace(count, d)
     ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-    st = lib.cerar_head_norm_grad(ops._h, kind, C.addressof(parts), len(parts), w_type, dw_type, accumulate, keep[1].size(0), q.shape[-1], eps,
-                                  C.addressof(rot), ws.data_ptr(), need, _stream(q.device.index))
+    st = lib.cerar_head_norm_grad(ops._h, kind, _PARTS.pack(*first, *second), count, types[0] or 0, types[1] or 0, accumulate, n, d, eps, rotation,
+                                  ws.data_ptr(), need, _raw(ops._index))
     if st:
         _check(st)
-    return ys[0], ys[1]
+    return yq, yk
 
 
 class HeadNorm(torch.autograd.Function):
@@ -281,32 +302,32 @@ def _operand(t: torch.Tensor, what: str) -> torch.Tensor:
     """A bfloat16 matrix as tensor-map copies read it, rows on 16-byte boundaries: a copy where it is not."""
     if t.dtype != _BF16:
         raise TypeError(f"{what}: bfloat16 wanted, got {t.dtype}")
-    if t.dim() != 2 or not t.is_cuda:
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError(f"{what}: a two-dimensional CUDA tensor is wanted")
-    rows, cols = t.shape
+    rows, cols = shape
     row, col = t.stride()
-    if not t.numel() or (col == 1 or cols == 1) and (rows == 1 or row >= cols and not row & 7) and not t.data_ptr() & 15:
+    if (col == 1 or cols == 1) and (rows == 1 or row >= cols and not row & 7) and not t.data_ptr() & 15 or not rows or not cols:
         return t
     wide = torch.empty(rows, (cols + 7) & -8, dtype=_BF16, device=t.device)
     return wide[:, :cols].copy_(t)
 
 
-def _ld8(t: torch.Tensor) -> int:
-    """Elements between rows (one row: any multiple of 8 that holds it)."""
-    return t.stride(0) if t.size(0) > 1 else (t.size(1) + 7) & -8
-
-
 def _padded(rows: int, cols: int, device) -> torch.Tensor:
-    """An empty bfloat16 matrix with rows on 16-byte boundaries."""
-    ld = (cols + 7) & -8
-    t = torch.empty(rows, ld, dtype=_BF16, device=device)
-    return t if ld == cols else t[:, :cols]
+    """An empty bfloat16 matrix with rows on 16-byte boundaries (columns up to a multiple of 8 that belong to no one)."""
+    return torch.empty(rows, (cols + 7) & -8, dtype=_BF16, device=device)
 
 
-def _matmul(ops, a, trans_a, b, trans_b, m, n, k, out, accumulate):
-    """(operands as _operand gives them)"""
-    st = lib.cerar_matmul_bf16(ops._h, a.data_ptr(), _ld8(a), trans_a, b.data_ptr(), _ld8(b), trans_b, m, n, k, out.data_ptr(), _type(out, "out"),
-                               _ld(out) if out.numel() else n, accumulate, _stream(out.device.index))
+def _ld8(t: torch.Tensor) -> int:
+    """Elements between rows of what _operand gave (one row: any multiple of 8 that holds it)."""
+    rows, cols = t.shape
+    return t.stride(0) if rows > 1 else (cols + 7) & -8
+
+
+def _matmul(ops, a, lda, trans_a, b, ldb, trans_b, m, n, k, out, accumulate):
+    """(a and b: addresses of operands as _operand gives them)"""
+    st = lib.cerar_matmul_bf16(ops._h, a, lda, trans_a, b, ldb, trans_b, m, n, k, out.data_ptr(), _kind(out, "out"), _stride(out), accumulate,
+                               _raw(ops._index))
     if st:
         _check(st)
     return out
@@ -315,7 +336,7 @@ def _matmul(ops, a, trans_a, b, trans_b, m, n, k, out, accumulate):
 def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b=False, out: torch.Tensor | None = None,
            dtype: torch.dtype = torch.bfloat16, accumulate=False) -> torch.Tensor:
     """op(a) op(b) of bfloat16 matrices, into `out` (float32 or bfloat16) if given, added to it with accumulate."""
-    _same_device(ops, a=a, b=b, out=out)
+    _here(ops, (a, b, out), "a b out")
     a, b = _operand(a, "a"), _operand(b, "b")
     m, k = (a.size(1), a.size(0)) if trans_a else a.shape
     k2, n = (b.size(1), b.size(0)) if trans_b else b.shape
@@ -329,7 +350,7 @@ def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b
         _matrix(out, "out")
         if tuple(out.shape) != (m, n):
             raise ValueError(f"out of shape {(m, n)} wanted, got {tuple(out.shape)}")
-    return _matmul(ops, a, trans_a, b, trans_b, m, n, k, out, accumulate)
+    return _matmul(ops, a.data_ptr(), _ld8(a), trans_a, b.data_ptr(), _ld8(b), trans_b, m, n, k, out, accumulate)
 
 
 def _gated_sizes(x, w_in, w_out, activation):
@@ -345,21 +366,26 @@ def _gated(ops, x, w_in, w_out, activation, keep):
     """x as a matrix; returns y and the kept g and u."""
     t, d = x.shape
     o, f = w_out.shape
-    wi = _operand(w_in, "w_in")
-    h = _padded(t, f, x.device)
-    gu = torch.empty(lib.cerar_gated_kept_bytes(t, f), dtype=torch.uint8, device=x.device) if keep else None
-    st = lib.cerar_gated_in(ops._h, x.data_ptr(), _ld8(x), wi.data_ptr(), _ld8(wi), t, d, f, _ACTIVATIONS[activation], h.data_ptr(), _ld8(h),
-                            None if gu is None else gu.data_ptr(), _stream(x.device.index))
+    device, at = x.device, _raw(ops._index)
+    wi, wo = _operand(w_in, "w_in"), _operand(w_out, "w_out")
+    h = _padded(t, f, device)
+    hp, ldh = h.data_ptr(), (f + 7) & -8
+    gu = torch.empty(lib.cerar_gated_kept_bytes(t, f), dtype=torch.uint8, device=device) if keep else None
+    st = lib.cerar_gated_in(ops._h, x.data_ptr(), _ld8(x), wi.data_ptr(), _ld8(wi), t, d, f, _ACTIVATIONS[activation], hp, ldh,
+                            None if gu is None else gu.data_ptr(), at)
     if st:
         _check(st)
-    y = _matmul(ops, h, False, _operand(w_out, "w_out"), True, t, o, f, torch.empty(t, o, dtype=_BF16, device=x.device), False)
+    y = torch.empty(t, o, dtype=_BF16, device=device)
+    st = lib.cerar_matmul_bf16(ops._h, hp, ldh, False, wo.data_ptr(), _ld8(wo), True, t, o, f, y.data_ptr(), 1, o, False, at)
+    if st:
+        _check(st)
     return y, gu
 
 
 def gated(ops: Ops, x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *, activation: str = "silu", keep=False):
     """(act(x w_g^T) * (x w_u^T)) w_out^T for x (..., inputs), w_in = w_g over w_u (2 hidden x inputs) and w_out (outputs x hidden), all bfloat16.
     activation: silu, gelu, gelu_tanh or relu.  With keep also what gated_backward wants of it: (x, g and u in 24 bits, the activation)."""
-    _same_device(ops, x=x, w_in=w_in, w_out=w_out)
+    _here(ops, (x, w_in, w_out), "x w_in w_out")
     _gated_sizes(x, w_in, w_out, activation)
     xm = _operand(_rows(x), "x")
     y, gu = _gated(ops, xm, w_in, w_out, activation, keep)
@@ -374,19 +400,21 @@ def _gated_backward(ops, dy, kept, w_in, w_out, dw_in, dw_out, accumulate, need_
         if dw_in is not None and not accumulate:
             dw_in.zero_()
         return torch.zeros(t, d, dtype=_BF16, device=x.device) if need_dx else None
-    dx = None
-    wo, dgu = _operand(w_out, "w_out"), _padded(t, 2 * f, x.device)
-    h = None if dw_out is None else _padded(t, f, x.device)
-    st = lib.cerar_gated_grad(ops._h, dy.data_ptr(), _ld8(dy), wo.data_ptr(), _ld8(wo), t, o, f, _ACTIVATIONS[activation], gu.data_ptr(), dgu.data_ptr(),
-                              _ld8(dgu), None if h is None else h.data_ptr(), 0 if h is None else _ld8(h), _stream(x.device.index))
+    dx, device = None, x.device
+    wo, dgu = _operand(w_out, "w_out"), _padded(t, 2 * f, device)
+    h = None if dw_out is None else _padded(t, f, device)
+    dyp, lddy, gp, ldg, hp, ldh = dy.data_ptr(), _ld8(dy), dgu.data_ptr(), (2 * f + 7) & -8, None if h is None else h.data_ptr(), (f + 7) & -8
+    st = lib.cerar_gated_grad(ops._h, dyp, lddy, wo.data_ptr(), _ld8(wo), t, o, f, _ACTIVATIONS[activation], gu.data_ptr(), gp, ldg, hp, ldh,
+                              _raw(ops._index))
     if st:
         _check(st)
     if need_dx:
-        dx = _matmul(ops, dgu, False, _operand(w_in, "w_in"), False, t, d, 2 * f, torch.empty(t, d, dtype=_BF16, device=x.device), False)
+        wi = _operand(w_in, "w_in")
+        dx = _matmul(ops, gp, ldg, False, wi.data_ptr(), _ld8(wi), False, t, d, 2 * f, torch.empty(t, d, dtype=_BF16, device=device), False)
     if dw_in is not None:
-        _matmul(ops, dgu, True, x, False, 2 * f, d, t, dw_in, accumulate)
-    if h is not None:
-        _matmul(ops, dy, True, h, False, o, f, t, dw_out, accumulate)
+        _matmul(ops, gp, ldg, True, x.data_ptr(), _ld8(x), False, 2 * f, d, t, dw_in, accumulate)
+    if hp is not None:
+        _matmul(ops, dyp, lddy, True, hp, ldh, False, o, f, t, dw_out, accumulate)
     return dx
 
 
@@ -395,7 +423,7 @@ def gated_backward(ops: Ops, dy: torch.Tensor, kept, w_in: torch.Tensor, w_out: 
     """dx from dy and what gated kept; dw_in and dw_out (float32 or bfloat16, e.g. slices of the gradient vector; None: not wanted) += the
     gradients of the weights."""
     x, gu, activation = kept
-    _same_device(ops, dy=dy, x=x, w_in=w_in, w_out=w_out, dw_in=dw_in, dw_out=dw_out)
+    _here(ops, (dy, x, w_in, w_out, dw_in, dw_out), "dy x w_in w_out dw_in dw_out")
     _gated_sizes(x, w_in, w_out, activation)
     for what, dw, w in (("dw_in", dw_in, w_in), ("dw_out", dw_out, w_out)):
         if dw is not None:
@@ -403,7 +431,7 @@ def gated_backward(ops: Ops, dy: torch.Tensor, kept, w_in: torch.Tensor, w_out: 
             if dw.shape != w.shape:
                 raise ValueError(f"{what} of shape {tuple(w.shape)} wanted, got {tuple(dw.shape)}")
     dym = _operand(_rows(dy), "dy")
-    if tuple(dym.shape) != (x.size(0), w_out.size(0)):
+    if dym.shape != (x.size(0), w_out.size(0)):
         raise ValueError(f"dy: {x.size(0)} rows of {w_out.size(0)} values wanted")
     dx = _gated_backward(ops, dym, kept, w_in, w_out, dw_in, dw_out, accumulate, need_dx)
     return None if dx is None else dx.view(*dy.shape[:-1], dx.size(-1))
