@@ -667,6 +667,15 @@ cerar_status_t cerar_matmul_bf16(cerar_ops_t* ops, const void* A, int64_t lda, i
  * 128 x 128, and in *split the blocks that share the sum of a tile.  -1 for sizes that no product has. */
 int            cerar_matmul_bf16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* split);
 
+/* Copies bfloat16 matrices (rows x cols, ld elements between rows, any alignment) to rows on 16-byte boundaries, as the products want their
+ * operands: dst 16-byte aligned, ldd a multiple of 8; columns from cols up to the next multiple of 8 become zero.  1 to 4 in one launch. */
+typedef struct {
+    const void* src;
+    void*       dst;
+    int64_t     rows, cols, ld, ldd;
+} cerar_rows_t;
+cerar_status_t cerar_align_bf16(cerar_ops_t* ops, const cerar_rows_t* items, int count, cerar_stream_t stream);
+
 /* The two products of a gated feed-forward block that carry its elementwise part.  The block, for x (tokens x width) and bfloat16 weights
  * w_in (2 hidden x width: the gate's rows, then the other projection's) and w_out (outputs x hidden):
  *     [g u] = x w_in^T,   h = act(g) u,   y = h w_out^T

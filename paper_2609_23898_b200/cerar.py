@@ -165,6 +165,7 @@ lib.cerar_head_norm_grad_workspace.restype = C.c_size_t
 lib.cerar_head_norm_grad.argtypes = [_vp, C.c_int, _vp, C.c_int, C.c_int, C.c_int, C.c_int, _i64, C.c_int, C.c_float, _vp, _vp, C.c_size_t, _vp]
 lib.cerar_matmul_bf16.argtypes = [_vp, _vp, _i64, C.c_int, _vp, _i64, C.c_int, _i64, _i64, _i64, _vp, C.c_int, _i64, C.c_int, _vp]
 lib.cerar_matmul_bf16_tile.argtypes = [_i64, _i64, _i64, C.c_int, C.POINTER(C.c_int)]
+lib.cerar_align_bf16.argtypes = [_vp, _vp, C.c_int, _vp]
 lib.cerar_gated_kept_bytes.argtypes = [_i64, _i64]
 lib.cerar_gated_kept_bytes.restype = C.c_size_t
 lib.cerar_gated_in.argtypes = [_vp, _vp, _i64, _vp, _i64, _i64, _i64, _i64, C.c_int, _vp, _i64, _vp, _vp]

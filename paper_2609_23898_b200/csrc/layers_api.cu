@@ -209,6 +209,25 @@ int cerar_matmul_bf16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* sp
     return cerar::matmul16_tile(M, N, K, num_sms, split);
 }
 
+cerar_status_t cerar_align_bf16(cerar_ops_t* o, const cerar_rows_t* items, int count, cerar_stream_t stream) {
+    cerar_status_t st = check_ops(o);
+    if (st != CERAR_OK) return st;
+    if (!items || count < 1 || count > cerar::ALIGN_MAX) return fail(CERAR_ERR_INVALID_ARG, "1 to 4 matrices are wanted");
+    cerar::AlignArgs a[cerar::ALIGN_MAX];
+    for (int i = 0; i < count; ++i) {
+        const cerar_rows_t& m = items[i];
+        if (m.rows < 0 || m.cols < 0 || m.rows > SIZE_MAX_ || m.cols > SIZE_MAX_) return fail(CERAR_ERR_SHAPE, "matrix: sizes from 0 to 2^31 - 256 are wanted");
+        if ((st = check_rows(m.src, CERAR_TYPE_BF16, m.rows, m.cols, m.ld, "src NULL or not aligned to its elements")) != CERAR_OK) return st;
+        if (m.rows > 0 && m.cols > 0) {
+            if (!m.dst || misaligned(m.dst, 16)) return fail(CERAR_ERR_INVALID_ARG, "dst NULL, or not on a 16-byte boundary");
+            if (m.ldd % 8 || m.ldd < m.cols || m.ldd > LD_MAX) return fail(CERAR_ERR_SHAPE, "ldd must be a multiple of 8 and at least the number of columns");
+        }
+        a[i] = {m.src, m.dst, m.cols > 0 ? m.rows : 0, m.cols, m.ld, m.ldd};
+    }
+    const cudaError_t e = cerar::launch_align(a, count, (cudaStream_t)stream, &o->launches);
+    return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "row copy launch");
+}
+
 size_t cerar_gated_kept_bytes(int64_t tokens, int64_t hidden) {
     if (tokens < 0 || tokens > TOKENS_MAX || hidden < 0 || hidden > SIZE_MAX_ / 2) return 0;
     return cerar::gated_kept_bytes(tokens, hidden);

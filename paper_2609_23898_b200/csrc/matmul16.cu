@@ -308,12 +308,33 @@ __device__ __forceinline__ void write_rows(uint32_t staging, bf16* c, int64_t ld
             }
         }
     } else {
-        for (int r = 0; r < nrows; ++r)
-            for (int e = lane; e < n; e += 32) {
-                uint16_t q;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(q) : "r"(staging + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2) : "memory");
-                *reinterpret_cast<uint16_t*>(c + (int64_t)(row0 + r) * ld + col0 + e) = q;
+        // Rows on other boundaries: 16 bytes at a time from the first boundary inside the row on, its ends element by element.
+        constexpr int PER_ROW = W / 8, ROWS = 32 / PER_ROW;
+        const int j = lane % PER_ROW;
+        auto element = [&](int r, int e) {
+            uint16_t q;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(q) : "r"(staging + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2) : "memory");
+            return q;
+        };
+#pragma unroll 1
+        for (int it = 0; it < 32 / ROWS; ++it) {
+            const int r = it * ROWS + lane / PER_ROW;
+            if (r >= nrows) continue;
+            uint16_t* dst = reinterpret_cast<uint16_t*>(c + (int64_t)(row0 + r) * ld + col0);
+            const int gap = (int)(8u - (uint32_t)(reinterpret_cast<uintptr_t>(dst) >> 1)) & 7, first = gap < n ? gap : n;
+            const int whole = (n - first) >> 3, rest = (n - first) & 7, e0 = first + 8 * j;
+            if (j < whole) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = (uint32_t)element(r, e0 + 2 * i) | (uint32_t)element(r, e0 + 2 * i + 1) << 16;
+                *reinterpret_cast<uint4*>(dst + e0) = make_uint4(w[0], w[1], w[2], w[3]);
             }
+#pragma unroll
+            for (int i = j; i < 8; i += PER_ROW) {
+                if (i < first) dst[i] = element(r, i);
+                if (i < rest) dst[first + 8 * whole + i] = element(r, first + 8 * whole + i);
+            }
+        }
     }
 }
 
@@ -357,6 +378,11 @@ __device__ __forceinline__ void write_tile(const Params& p, uint32_t staging, in
     const int lane = threadIdx.x & 31;
     if constexpr (KIND == PLAIN) {
         constexpr int SLAB = 8 * Out<C>::PER16;
+        if (sizeof(C) == 2 && !p.accumulate && !p.c_vec) {
+#pragma unroll
+            for (int c = 0; c < CW / 64; ++c) write_rows<64>(staging, reinterpret_cast<bf16*>(p.C), p.ldc, p.M, p.N, row0, tn * BN + half * CW + c * 64, acc + c * 64, false);
+            return;
+        }
 #pragma unroll
         for (int c = 0; c < CW / SLAB; ++c) write_slab<C>(p, staging, row0, tn * BN + half * CW + c * SLAB, acc + c * SLAB);
     } else if constexpr (KIND == GATE) {
@@ -832,6 +858,68 @@ cudaError_t launch_gated_grad(const GatedGradArgs& a, int num_sms, cudaStream_t 
     p.four = on(a.dgu, a.lddgu, 8, 2) && (!a.h || on(a.h, a.ldh, 8, 2)) && a.hidden % 4 == 0;
     p.c_vec = on(a.dgu, a.lddgu, 16, 2) && (!a.h || on(a.h, a.ldh, 16, 2)) && a.hidden % 8 == 0;
     return launch(p, GRAD, CERAR_TYPE_BF16, a.dy, a.lddy, false, a.w, a.ldw, false, a.tokens, a.hidden, a.width, a.status, num_sms, s, launches);
+}
+
+// ---------------------------------------------------------------- copies to rows on 16-byte boundaries
+//
+// What tensor-map copies cannot read in place.  A thread writes 16 bytes and reads them as single elements (pairs, where rows start on 4-byte
+// boundaries), of which the first-level cache serves all but the first.  Several matrices go in one launch.
+
+namespace {
+constexpr int ALIGN_THREADS = 256, ALIGN_CHUNKS = 4;
+struct AlignItems {
+    AlignArgs m[ALIGN_MAX];
+    uint32_t first[ALIGN_MAX + 1];                     // blocks in front of each
+};
+__global__ void __launch_bounds__(ALIGN_THREADS) align_kernel(const AlignItems items) {
+    grid_dependency_wait();
+    int i = 0;
+    while (blockIdx.x >= items.first[i + 1]) ++i;
+    const AlignArgs& m = items.m[i];
+    const uint32_t chunks = (uint32_t)(m.cols + 7) / 8;
+    const int64_t total = m.rows * chunks;
+    const bool pairs = (reinterpret_cast<uintptr_t>(m.src) & 3) == 0 && (m.ld & 1) == 0;
+    int64_t at = (int64_t)(blockIdx.x - items.first[i]) * (ALIGN_THREADS * ALIGN_CHUNKS) + threadIdx.x;
+    uint32_t w[ALIGN_CHUNKS][4];
+    uint16_t* dst[ALIGN_CHUNKS];
+#pragma unroll
+    for (int c = 0; c < ALIGN_CHUNKS; ++c, at += ALIGN_THREADS) {
+        dst[c] = nullptr;
+        if (at >= total) continue;
+        const int64_t row = total < 0x7FFFFFFF ? (int64_t)((uint32_t)at / chunks) : at / chunks;
+        const int64_t col = (at - row * chunks) * 8;
+        const uint16_t* src = static_cast<const uint16_t*>(m.src) + row * m.ld + col;
+        dst[c] = static_cast<uint16_t*>(m.dst) + row * m.ldd + col;
+        const int n = (int)(m.cols - col < 8 ? m.cols - col : 8);
+        if (pairs && n == 8) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[c][e] = __ldg(reinterpret_cast<const uint32_t*>(src) + e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[c][e] = (2 * e < n ? (uint32_t)__ldg(src + 2 * e) : 0u) | (2 * e + 1 < n ? (uint32_t)__ldg(src + 2 * e + 1) << 16 : 0u);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < ALIGN_CHUNKS; ++c)
+        if (dst[c]) *reinterpret_cast<uint4*>(dst[c]) = make_uint4(w[c][0], w[c][1], w[c][2], w[c][3]);
+}
+}  // namespace
+
+cudaError_t launch_align(const AlignArgs* items, int count, cudaStream_t s, uint64_t* launches) {
+    AlignItems a = {};
+    int64_t blocks = 0;
+    for (int i = 0; i < count; ++i) {
+        a.m[i] = items[i];
+        blocks += (items[i].rows * ((items[i].cols + 7) / 8) + ALIGN_THREADS * ALIGN_CHUNKS - 1) / (ALIGN_THREADS * ALIGN_CHUNKS);
+        if (blocks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+        a.first[i + 1] = (uint32_t)blocks;
+    }
+    for (int i = count; i < ALIGN_MAX; ++i) a.first[i + 1] = (uint32_t)blocks;
+    if (blocks == 0) return cudaSuccess;
+    const cudaError_t e = launch_pdl(align_kernel, dim3((unsigned)blocks), dim3(ALIGN_THREADS), 0, s, a);
+    if (e == cudaSuccess) ++*launches;
+    return e;
 }
 
 }  // namespace cerar

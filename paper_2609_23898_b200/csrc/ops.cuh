@@ -172,6 +172,13 @@ struct Matmul16Args {
 };
 cudaError_t launch_matmul16(const Matmul16Args& a, int num_sms, cudaStream_t s, uint64_t* launches);
 int matmul16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* split);
+struct AlignArgs {                       // a bfloat16 matrix whose rows are copied to rows on 16-byte boundaries
+    const void* src;
+    void* dst;
+    int64_t rows, cols, ld, ldd;
+};
+constexpr int ALIGN_MAX = 4;
+cudaError_t launch_align(const AlignArgs* items, int count, cudaStream_t s, uint64_t* launches);
 struct GatedInArgs {
     const void *x, *w;
     int64_t ldx, ldw;

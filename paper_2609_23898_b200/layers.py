@@ -51,7 +51,7 @@ def _here(ops: Ops, tensors, names: str):
 
 
 def _stride(t: torch.Tensor) -> int:
-    """Elements between rows of a matrix that _matrix or _operand has let pass (one row, or none: its length)."""
+    """Elements between rows of a matrix that _matrix has let pass (one row, or none: its length)."""
     rows, cols = t.shape
     return t.stride(0) if rows > 1 and cols else cols
 
@@ -298,19 +298,38 @@ _ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 _BF16 = torch.bfloat16
 
 
-def _operand(t: torch.Tensor, what: str) -> torch.Tensor:
-    """A bfloat16 matrix as tensor-map copies read it, rows on 16-byte boundaries: a copy where it is not."""
-    if t.dtype != _BF16:
-        raise TypeError(f"{what}: bfloat16 wanted, got {t.dtype}")
-    shape = t.shape
-    if len(shape) != 2:
-        raise ValueError(f"{what}: a two-dimensional CUDA tensor is wanted")
-    rows, cols = shape
-    row, col = t.stride()
-    if (col == 1 or cols == 1) and (rows == 1 or row >= cols and not row & 7) and not t.data_ptr() & 15 or not rows or not cols:
-        return t
-    wide = torch.empty(rows, (cols + 7) & -8, dtype=_BF16, device=t.device)
-    return wide[:, :cols].copy_(t)
+_ROWS = struct.Struct("6q")          # cerar_rows_t
+
+
+def _operands(ops: Ops, *given):
+    """bfloat16 matrices (tensor, its name) as tensor-map copies read them, rows on 16-byte boundaries: copies (one launch for all of them) of those
+    that are not.  Each as [tensor, address, elements between rows]."""
+    out, copies = [], b""
+    for t, what in given:
+        if t.dtype != _BF16:
+            raise TypeError(f"{what}: bfloat16 wanted, got {t.dtype}")
+        shape = t.shape
+        if len(shape) != 2:
+            raise ValueError(f"{what}: a two-dimensional CUDA tensor is wanted")
+        rows, cols = shape
+        row, col = t.stride()
+        at = t.data_ptr()
+        if (col == 1 or cols == 1) and (rows == 1 or row >= cols and not row & 7) and not at & 15 or not rows or not cols:
+            out.append((t, at, row if rows > 1 and cols else (cols + 7) & -8))
+            continue
+        wide = _padded(rows, cols, t.device)
+        to = wide.data_ptr()
+        if (col == 1 or cols == 1) and (rows == 1 or row >= cols):
+            copies += _ROWS.pack(at, to, rows, cols, row if rows > 1 else cols, (cols + 7) & -8)
+            wide = wide if wide.size(1) == cols else wide[:, :cols]
+        else:
+            wide = wide[:, :cols].copy_(t)
+        out.append((wide, to, (cols + 7) & -8))
+    if copies:
+        st = lib.cerar_align_bf16(ops._h, copies, len(copies) // _ROWS.size, _raw(ops._index))
+        if st:
+            _check(st)
+    return out
 
 
 def _padded(rows: int, cols: int, device) -> torch.Tensor:
@@ -318,14 +337,8 @@ def _padded(rows: int, cols: int, device) -> torch.Tensor:
     return torch.empty(rows, (cols + 7) & -8, dtype=_BF16, device=device)
 
 
-def _ld8(t: torch.Tensor) -> int:
-    """Elements between rows of what _operand gave (one row: any multiple of 8 that holds it)."""
-    rows, cols = t.shape
-    return t.stride(0) if rows > 1 else (cols + 7) & -8
-
-
 def _matmul(ops, a, lda, trans_a, b, ldb, trans_b, m, n, k, out, accumulate):
-    """(a and b: addresses of operands as _operand gives them)"""
+    """(a and b: addresses of operands as _operands gives them)"""
     st = lib.cerar_matmul_bf16(ops._h, a, lda, trans_a, b, ldb, trans_b, m, n, k, out.data_ptr(), _kind(out, "out"), _stride(out), accumulate,
                                _raw(ops._index))
     if st:
@@ -337,7 +350,8 @@ def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b
            dtype: torch.dtype = torch.bfloat16, accumulate=False) -> torch.Tensor:
     """op(a) op(b) of bfloat16 matrices, into `out` (float32 or bfloat16) if given, added to it with accumulate."""
     _here(ops, (a, b, out), "a b out")
-    a, b = _operand(a, "a"), _operand(b, "b")
+    if a.dim() != 2 or b.dim() != 2:
+        raise ValueError("a and b: two-dimensional tensors are wanted")
     m, k = (a.size(1), a.size(0)) if trans_a else a.shape
     k2, n = (b.size(1), b.size(0)) if trans_b else b.shape
     if k != k2:
@@ -350,7 +364,8 @@ def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b
         _matrix(out, "out")
         if tuple(out.shape) != (m, n):
             raise ValueError(f"out of shape {(m, n)} wanted, got {tuple(out.shape)}")
-    return _matmul(ops, a.data_ptr(), _ld8(a), trans_a, b.data_ptr(), _ld8(b), trans_b, m, n, k, out, accumulate)
+    (a, pa, lda), (b, pb, ldb) = _operands(ops, (a, "a"), (b, "b"))
+    return _matmul(ops, pa, lda, trans_a, pb, ldb, trans_b, m, n, k, out, accumulate)
 
 
 def _gated_sizes(x, w_in, w_out, activation):
@@ -363,23 +378,22 @@ def _gated_sizes(x, w_in, w_out, activation):
 
 
 def _gated(ops, x, w_in, w_out, activation, keep):
-    """x as a matrix; returns y and the kept g and u."""
+    """x as a matrix; returns y, x as the products read it, and the kept g and u."""
     t, d = x.shape
     o, f = w_out.shape
     device, at = x.device, _raw(ops._index)
-    wi, wo = _operand(w_in, "w_in"), _operand(w_out, "w_out")
+    (x, xp, ldx), (wi, wip, ldi), (wo, wop, ldo) = _operands(ops, (x, "x"), (w_in, "w_in"), (w_out, "w_out"))
     h = _padded(t, f, device)
     hp, ldh = h.data_ptr(), (f + 7) & -8
     gu = torch.empty(lib.cerar_gated_kept_bytes(t, f), dtype=torch.uint8, device=device) if keep else None
-    st = lib.cerar_gated_in(ops._h, x.data_ptr(), _ld8(x), wi.data_ptr(), _ld8(wi), t, d, f, _ACTIVATIONS[activation], hp, ldh,
-                            None if gu is None else gu.data_ptr(), at)
+    st = lib.cerar_gated_in(ops._h, xp, ldx, wip, ldi, t, d, f, _ACTIVATIONS[activation], hp, ldh, None if gu is None else gu.data_ptr(), at)
     if st:
         _check(st)
     y = torch.empty(t, o, dtype=_BF16, device=device)
-    st = lib.cerar_matmul_bf16(ops._h, hp, ldh, False, wo.data_ptr(), _ld8(wo), True, t, o, f, y.data_ptr(), 1, o, False, at)
+    st = lib.cerar_matmul_bf16(ops._h, hp, ldh, False, wop, ldo, True, t, o, f, y.data_ptr(), 1, o, False, at)
     if st:
         _check(st)
-    return y, gu
+    return y, x, gu
 
 
 def gated(ops: Ops, x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *, activation: str = "silu", keep=False):
@@ -387,8 +401,7 @@ def gated(ops: Ops, x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *,
     activation: silu, gelu, gelu_tanh or relu.  With keep also what gated_backward wants of it: (x, g and u in 24 bits, the activation)."""
     _here(ops, (x, w_in, w_out), "x w_in w_out")
     _gated_sizes(x, w_in, w_out, activation)
-    xm = _operand(_rows(x), "x")
-    y, gu = _gated(ops, xm, w_in, w_out, activation, keep)
+    y, xm, gu = _gated(ops, _rows(x), w_in, w_out, activation, keep)
     y = y.view(*x.shape[:-1], y.size(-1))
     return (y, (xm, gu, activation)) if keep else y
 
@@ -401,18 +414,18 @@ def _gated_backward(ops, dy, kept, w_in, w_out, dw_in, dw_out, accumulate, need_
             dw_in.zero_()
         return torch.zeros(t, d, dtype=_BF16, device=x.device) if need_dx else None
     dx, device = None, x.device
-    wo, dgu = _operand(w_out, "w_out"), _padded(t, 2 * f, device)
+    given = [(dy, "dy"), (w_out, "w_out"), (x, "x")] + ([(w_in, "w_in")] if need_dx else [])
+    (dy, dyp, lddy), (wo, wop, ldo), (x, xp, ldx), *wi = _operands(ops, *given)
+    dgu = _padded(t, 2 * f, device)
     h = None if dw_out is None else _padded(t, f, device)
-    dyp, lddy, gp, ldg, hp, ldh = dy.data_ptr(), _ld8(dy), dgu.data_ptr(), (2 * f + 7) & -8, None if h is None else h.data_ptr(), (f + 7) & -8
-    st = lib.cerar_gated_grad(ops._h, dyp, lddy, wo.data_ptr(), _ld8(wo), t, o, f, _ACTIVATIONS[activation], gu.data_ptr(), gp, ldg, hp, ldh,
-                              _raw(ops._index))
+    gp, ldg, hp, ldh = dgu.data_ptr(), (2 * f + 7) & -8, None if h is None else h.data_ptr(), (f + 7) & -8
+    st = lib.cerar_gated_grad(ops._h, dyp, lddy, wop, ldo, t, o, f, _ACTIVATIONS[activation], gu.data_ptr(), gp, ldg, hp, ldh, _raw(ops._index))
     if st:
         _check(st)
     if need_dx:
-        wi = _operand(w_in, "w_in")
-        dx = _matmul(ops, gp, ldg, False, wi.data_ptr(), _ld8(wi), False, t, d, 2 * f, torch.empty(t, d, dtype=_BF16, device=device), False)
+        dx = _matmul(ops, gp, ldg, False, wi[0][1], wi[0][2], False, t, d, 2 * f, torch.empty(t, d, dtype=_BF16, device=device), False)
     if dw_in is not None:
-        _matmul(ops, gp, ldg, True, x.data_ptr(), _ld8(x), False, 2 * f, d, t, dw_in, accumulate)
+        _matmul(ops, gp, ldg, True, xp, ldx, False, 2 * f, d, t, dw_in, accumulate)
     if hp is not None:
         _matmul(ops, dyp, lddy, True, hp, ldh, False, o, f, t, dw_out, accumulate)
     return dx
@@ -430,7 +443,7 @@ def gated_backward(ops: Ops, dy: torch.Tensor, kept, w_in: torch.Tensor, w_out: 
             _matrix(dw, what)
             if dw.shape != w.shape:
                 raise ValueError(f"{what} of shape {tuple(w.shape)} wanted, got {tuple(dw.shape)}")
-    dym = _operand(_rows(dy), "dy")
+    dym = _rows(dy)
     if dym.shape != (x.size(0), w_out.size(0)):
         raise ValueError(f"dy: {x.size(0)} rows of {w_out.size(0)} values wanted")
     dx = _gated_backward(ops, dym, kept, w_in, w_out, dw_in, dw_out, accumulate, need_dx)
