@@ -768,10 +768,11 @@ Shape choose_shape(int64_t M, int64_t N, int64_t kblocks, int num_sms) {
     for (int form = 0; form < 3; ++form) {
         const int blocks = form == SINGLE_128 ? 1 : 2, rows = blocks * BM, columns = form == PAIR_256 ? 256 : 128;
         const int64_t tiles = ((M + rows - 1) / rows) * ((N + columns - 1) / columns);
+        if (blocks > num_sms) continue;
         for (int q = 1; q * blocks <= MAX_SPLIT && q <= kblocks; ++q) {
             const int64_t slots = num_sms / (q * blocks);
             if (q > 1 && tiles * q * blocks * 100 > (int64_t)num_sms * USABLE[q * blocks]) break;
-            const int64_t turns = q > 1 || slots < 1 ? 1 : (tiles + slots - 1) / slots;
+            const int64_t turns = q > 1 ? 1 : (tiles + slots - 1) / slots;
             const int64_t c = START[form] + turns * ((kblocks + q - 1) / q * BLOCK[form] + TURN[form]) + (q > 1 ? ADD[form] + ADD_FULL[form] * (M < rows ? M : rows) / rows : 0);
             if (c < cost) { cost = c; best = {form, q}; }
         }
