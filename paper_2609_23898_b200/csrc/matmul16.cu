@@ -725,6 +725,139 @@ bool make_map_16bit(CUtensorMap* m, const void* x, int64_t rows, int64_t cols, i
                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
+// ---------------------------------------------------------------- few rows
+//
+// Up to sixteen rows of A against weights whose rows are the sums' terms (B transposed): the weights are read once and that is all there is to it.
+// A block takes 16 rows of B (GATE: of both halves), its warps every W-th run of 32 terms of them, straight from memory into the operands of
+// mma.sync (16 weights' rows x 8 tokens): a lane's 16 bytes are 8 neighbouring terms of one row, and since both operands name the terms in the
+// same order, any order will do.  The warps' sums are added in their order.  The next kernel may set itself up meanwhile.
+// (Scalar multiply-adds were bound by unpacking from two rows on: 4 x 16384 x 2048 in 29 us, one row 14.6.)
+constexpr int FEW_ROWS = 16, FEW_AHEAD = 4;
+constexpr int64_t FEW_TERMS = 65536;                   // a warp's sum is then at most 256 additions, as in a tile
+// Weights up to this size: they come in pieces of 64 bytes, which costs nothing while latency is what counts (2048 x 512: 5.0 -> 3.1 us, 2048 x 2048:
+// 7.1 -> 4.9), but does where bandwidth does (4096 x 2048: 8.2 -> 8.9, 4096 x 8192: 16.7 -> 27.5).
+constexpr int64_t FEW_BYTES = 12 << 20;
+struct FewParams {
+    const bf16 *A, *B;
+    int64_t lda, ldb;
+    int M, K;
+    int64_t N;
+};
+// 8 terms of a row from k on; zeros from K on (rows are 16-byte aligned: the 16 bytes hold a term of the row)
+template <bool ONCE>
+__device__ __forceinline__ uint4 load_terms(const bf16* row, int k, int K) {
+    uint4 q = make_uint4(0u, 0u, 0u, 0u);
+    if (k >= K) return q;
+    if constexpr (ONCE) asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(row + k));
+    else q = __ldg(reinterpret_cast<const uint4*>(row + k));
+    if (k + 8 > K) {
+        const int n = K - k;
+        auto cut = [&](uint32_t w, int i) { return n >= 2 * i + 2 ? w : n == 2 * i + 1 ? w & 0xFFFFu : 0u; };
+        q = make_uint4(cut(q.x, 0), cut(q.y, 1), cut(q.z, 2), cut(q.w, 3));
+    }
+    return q;
+}
+__device__ __forceinline__ void mma_16x8(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// W warps; NT groups of 8 rows of A
+template <int NT, int W, int KIND, typename C>
+__global__ void __launch_bounds__(32 * W) few_rows_kernel(const FewParams f, const Params p) {
+    constexpr int H = KIND == GATE ? 2 : 1;
+    __shared__ float sums[W][H][NT][32][4];
+    grid_dependents_may_launch();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const bf16 *b[H][2], *a[NT];
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int64_t n = n0 + g + 8 * r;           // (rows behind the last: the last one's, not stored)
+            b[h][r] = f.B + (h * f.N + (n < f.N ? n : f.N - 1)) * f.ldb;
+        }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) a[t] = f.A + (8 * t + g < f.M ? 8 * t + g : f.M - 1) * f.lda;
+    grid_dependency_wait();
+    float acc[H][NT][4] = {};
+    for (int k0 = warp * (32 * FEW_AHEAD) + c * 8; k0 - c * 8 < f.K; k0 += 32 * W * FEW_AHEAD) {
+        uint4 w[FEW_AHEAD][H][2], x[FEW_AHEAD][NT];
+#pragma unroll
+        for (int i = 0; i < FEW_AHEAD; ++i)
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) w[i][h][r] = load_terms<true>(b[h][r], k0 + i * 32, f.K);
+#pragma unroll
+        for (int i = 0; i < FEW_AHEAD; ++i)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) x[i][t] = load_terms<false>(a[t], k0 + i * 32, f.K);
+#pragma unroll
+        for (int i = 0; i < FEW_AHEAD; ++i)
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    mma_16x8(acc[h][t], w[i][h][0].x, w[i][h][1].x, w[i][h][0].y, w[i][h][1].y, x[i][t].x, x[i][t].y);
+                    mma_16x8(acc[h][t], w[i][h][0].z, w[i][h][1].z, w[i][h][0].w, w[i][h][1].w, x[i][t].z, x[i][t].w);
+                }
+    }
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            *reinterpret_cast<float4*>(sums[warp][h][t][lane]) = make_float4(acc[h][t][0], acc[h][t][1], acc[h][t][2], acc[h][t][3]);
+    __syncthreads();
+    // value i of lane l: column n0 + l / 4 + 8 (i / 2) of the result, row 2 (l % 4) + i % 2 (of the group of 8)
+    for (int i = threadIdx.x; i < NT * 128; i += 32 * W) {
+        const int t = i >> 7, j = i & 127, l = ((j >> 3) & 7) * 4 + ((j >> 1) & 3), e = (j >> 6) * 2 + (j & 1);
+        const int64_t n = n0 + (l >> 2) + 8 * (e >> 1);
+        const int m = 8 * t + 2 * (l & 3) + (e & 1);
+        if (m >= f.M || n >= f.N) continue;
+        float v[H];
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            v[h] = sums[0][h][t][l][e];
+#pragma unroll
+            for (int q = 1; q < W; ++q) v[h] += sums[q][h][t][l][e];
+        }
+        if constexpr (KIND == GATE) {
+            if (p.kept.at) {
+                unsigned char* k = kept_block(p.kept, m, (int)n);
+                const int col = (int)n & 31;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t bits = to24(v[h]);
+                    *reinterpret_cast<uint16_t*>(k + h * 2048 + ((col >> 3) * 32 + m) * 16 + (col & 7) * 2) = (uint16_t)(bits >> 16);
+                    k[4096 + h * 1024 + ((col >> 4) * 32 + m) * 16 + (col & 15)] = (unsigned char)(bits >> 8);
+                }
+            }
+            with_act(p.act, [&](auto act) {
+                float h, other;
+                parts(mul2(act.value(two_of(v[0], v[0])), two_of(v[1], v[1])), h, other);
+                static_cast<bf16*>(p.C)[m * p.ldc + n] = __float2bfloat16_rn(h);
+            });
+        } else {
+            C* q = static_cast<C*>(p.C) + m * p.ldc + n;
+            *q = (C)(p.accumulate ? (float)*q + v[0] : v[0]);
+        }
+    }
+}
+// Warps per block: enough for sixteen per SM, and for sums that stay within 256 additions.
+template <int NT, int KIND, typename C>
+cudaError_t launch_few(const FewParams& f, const Params& p, int num_sms, cudaStream_t s) {
+    const int64_t blocks = (f.N + 15) / 16;
+    const dim3 grid((unsigned)blocks);
+    if (blocks * 4 >= 16 * num_sms && f.K <= FEW_TERMS / 4) return launch_pdl(few_rows_kernel<NT, 4, KIND, C>, grid, dim3(128), 0, s, f, p);
+    if (blocks * 8 >= 16 * num_sms && f.K <= FEW_TERMS / 2) return launch_pdl(few_rows_kernel<NT, 8, KIND, C>, grid, dim3(256), 0, s, f, p);
+    return launch_pdl(few_rows_kernel<NT, 16, KIND, C>, grid, dim3(512), 0, s, f, p);
+}
+template <int KIND, typename C>
+cudaError_t launch_few_rows(const FewParams& f, const Params& p, int num_sms, cudaStream_t s) {
+    return f.M <= 8 ? launch_few<1, KIND, C>(f, p, num_sms, s) : launch_few<2, KIND, C>(f, p, num_sms, s);
+}
+
 typedef void (*Kernel)(CUtensorMap, CUtensorMap, Params);
 constexpr int MAX_SMEM = 232448, KERNELS = 12;
 
@@ -790,6 +923,13 @@ bool on(const void* p, int64_t ld, int64_t bytes, int64_t size) { return reinter
 // p: the output's part is filled in.  N: columns of the accumulators all tiles together (GATE: twice those of h).
 cudaError_t launch(Params p, int kind, int type, const void* A, int64_t lda, bool trans_a, const void* B, int64_t ldb, bool trans_b, int64_t M, int64_t N, int64_t K,
                    int* status, int num_sms, cudaStream_t s, uint64_t* launches) {
+    if (kind != GRAD && !trans_a && trans_b && M <= FEW_ROWS && K <= FEW_TERMS && N * K * 2 <= FEW_BYTES) {
+        const FewParams f = {static_cast<const bf16*>(A), static_cast<const bf16*>(B), lda, ldb, (int)M, (int)K, kind == GATE ? N / 2 : N};
+        const cudaError_t e = kind == GATE ? launch_few_rows<GATE, bf16>(f, p, num_sms, s) : type == CERAR_TYPE_F32 ? launch_few_rows<PLAIN, float>(f, p, num_sms, s)
+                                                                                             : launch_few_rows<PLAIN, bf16>(f, p, num_sms, s);
+        if (e == cudaSuccess) ++*launches;
+        return e;
+    }
     if (!get_encode_fn()) return cudaErrorNotSupported;
     p.M = (int)M; p.kblocks = (int)((K + BK - 1) / BK); p.status = status;
     const Shape shape = choose_shape(M, N, p.kblocks, num_sms);
@@ -814,7 +954,7 @@ cudaError_t launch(Params p, int kind, int type, const void* A, int64_t lda, boo
         return cudaErrorInvalidValue;
     const int cluster = (paired ? 2 : 1) * p.split, most = num_sms / cluster;
     const int grid = cluster * (p.split > 1 || (int)p.tiles < most ? (int)p.tiles : most);
-    p.early = 2 * grid <= num_sms;
+    p.early = p.split > 1 || (int64_t)p.tiles * cluster <= num_sms;      // (one turn: the next kernel's blocks come where this one's have left)
     const Kernel kern = kind == GATE ? kernel_of<GATE, bf16>(shape.form) : kind == GRAD ? kernel_of<GRAD, bf16>(shape.form)
                         : type == CERAR_TYPE_F32 ? kernel_of<PLAIN, float>(shape.form) : kernel_of<PLAIN, bf16>(shape.form);
     const int which = 3 * (kind == PLAIN ? (type == CERAR_TYPE_F32 ? 0 : 1) : kind + 1) + shape.form;
