@@ -67,6 +67,17 @@ def _anchor(device, wanted: bool):
     return torch.empty(0, device=device, requires_grad=True) if wanted and torch.is_grad_enabled() else None
 
 
+def _save(ctx, *tensors):
+    """Saved as autograd saves tensors: freed by the backward pass, within reach of saved-tensor hooks, and refused if changed in between.
+    (Those made in inference mode cannot be saved; they are held as they are.)"""
+    ctx.held = tuple(t if t is not None and t.is_inference() else None for t in tensors)
+    ctx.save_for_backward(*(t if h is None else None for t, h in zip(tensors, ctx.held)))
+
+
+def _saved(ctx) -> list:
+    return [t if h is None else h for t, h in zip(ctx.saved_tensors, ctx.held)]
+
+
 # ------------------------------------------------------------------------------------------------ embedding
 
 
@@ -120,13 +131,13 @@ class Embed(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, ids, ops, dtable, scale, anchor):
         ctx.ops, ctx.dtable, ctx.scale = ops, dtable, scale
-        ctx.save_for_backward(ids)
+        _save(ctx, ids)
         return embed(ops, table, ids, scale=scale)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        ids, = ctx.saved_tensors
+        ids, = _saved(ctx)
         embed_backward(ctx.ops, dy, ids, ctx.dtable, scale=ctx.scale)
         return None, None, None, None, None, None
 
@@ -279,13 +290,13 @@ class HeadNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, wq, wk, ops, table, positions, dwq, dwk, eps, pairs, anchor):
         ctx.ops, ctx.dw, ctx.rest = ops, (dwq, dwk), (eps, pairs)
-        ctx.save_for_backward(q, k, wq, wk, table, positions)
+        _save(ctx, q, k, wq, wk, table, positions)
         return head_norm(ops, q, k, wq, wk, table, positions, eps=eps, pairs=pairs)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dq, dk):
-        q, k, wq, wk, table, positions = ctx.saved_tensors
+        q, k, wq, wk, table, positions = _saved(ctx)
         eps, pairs = ctx.rest
         dxq, dxk = head_norm_backward(ctx.ops, dq, dk, q, k, wq, wk, table, positions, dwq=ctx.dw[0], dwk=ctx.dw[1], eps=eps, pairs=pairs)
         need = ctx.needs_input_grad
@@ -467,12 +478,12 @@ class Gated(torch.autograd.Function):
             return gated(ops, x, w_in, w_out, activation=activation)
         y, kept = gated(ops, x, w_in, w_out, activation=activation, keep=True)
         ctx.ops, ctx.dw, ctx.activation = ops, (dw_in, dw_out), activation
-        ctx.save_for_backward(*kept[:2], w_in, w_out)
+        _save(ctx, *kept[:2], w_in, w_out)
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        *kept, w_in, w_out = ctx.saved_tensors
+        *kept, w_in, w_out = _saved(ctx)
         dx = gated_backward(ctx.ops, dy, (*kept, ctx.activation), w_in, w_out, *ctx.dw, need_dx=ctx.needs_input_grad[0])
         return (dx,) + (None,) * 7

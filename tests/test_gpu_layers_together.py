@@ -152,3 +152,67 @@ def test_captured_backward_pass_beside_an_eager_graph():
     alive.backward()
     assert all(torch.equal(a, b) for a, b in zip(first, grads))
     ops.status()
+
+
+def test_weights_made_in_inference_mode_and_saved_tensor_hooks():
+    """Such weights cannot be saved by autograd: they are held; what is saved passes through hooks (here: to the host and back) and comes back the same."""
+    import torch
+    from paper_2609_23898_b200 import layers, training
+    ops = training.Ops()
+    with torch.inference_mode():
+        frozen = [torch.randn(96, 32, device="cuda").bfloat16() * 0.2, torch.randn(32, 48, device="cuda").bfloat16() * 0.2,
+                  torch.randn(50, 32, device="cuda").bfloat16(), torch.ones(8, device="cuda").bfloat16()]
+    ids = torch.randint(50, (20,), device="cuda")
+    rot = layers.rotation_table(ops, 20, 8)
+    results = []
+    for weights, hooks in ((frozen, False), ([t.clone() for t in frozen], False), ([t.clone() for t in frozen], True)):
+        grads = [torch.zeros(50, 32, device="cuda"), torch.zeros(8, device="cuda"), torch.zeros(96, 32, device="cuda"), torch.zeros(32, 48, device="cuda")]
+
+        def run():
+            x = layers.Embed.apply(weights[2], ids, ops, grads[0], 1.0)
+            x, _ = layers.HeadNorm.apply(x.view(20, 4, 8), None, weights[3], None, ops, rot, None, grads[1])
+            return layers.Gated.apply(x.flatten(1), weights[0], weights[1], ops, grads[2], grads[3])
+
+        if hooks:
+            with torch.autograd.graph.saved_tensors_hooks(lambda t: t.cpu(), lambda t: t.cuda()):
+                y = run()
+        else:
+            y = run()
+        y.backward(torch.ones_like(y))
+        results.append(grads)
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+    ops.status()
+
+
+def test_two_host_threads_and_launch_counts():
+    """Handles of their own on two host threads at a time; every launch is counted."""
+    import threading
+    import torch
+    from paper_2609_23898_b200 import layers, training
+    table, ids = torch.randn(300, 40, device="cuda"), torch.randint(300, (700,), device="cuda")
+    x, w_in, w_out = torch.randn(64, 40, device="cuda").bfloat16(), torch.randn(96, 40, device="cuda").bfloat16(), torch.randn(40, 48, device="cuda").bfloat16()
+    torch.cuda.synchronize()
+    out, errors = [None, None], []
+
+    def work(i):
+        try:
+            ops = training.Ops()
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    d = torch.zeros(300, 40, device="cuda")
+                    layers.embed_backward(ops, layers.embed(ops, table, ids), ids, d)
+                    y = layers.gated(ops, x, w_in, w_out)
+                ops.status()
+                out[i] = (d, y, ops.launch_count())
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1]) and out[0][2] == out[1][2] == 20 * (1 + 3 + 2)
