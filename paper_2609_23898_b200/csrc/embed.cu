@@ -11,6 +11,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "kernels.cuh"
 #include "ops.cuh"
 #include "ptx.cuh"
@@ -21,11 +23,14 @@ namespace {
 using namespace ptx;
 
 // A token's key: its id; `vocab` for those that take no part (negative: padding; beyond the table: also reported).
-__device__ __forceinline__ uint32_t key_of(const void* ids, int id_bytes, int64_t t, int64_t vocab, int* status) {
-    const int64_t id = id_bytes == 8 ? __ldg(static_cast<const long long*>(ids) + t) : (int64_t)__ldg(static_cast<const int*>(ids) + t);
+__device__ __forceinline__ int64_t id_of(const void* ids, int id_bytes, int64_t t) {
+    return id_bytes == 8 ? __ldg(static_cast<const long long*>(ids) + t) : (int64_t)__ldg(static_cast<const int*>(ids) + t);
+}
+__device__ __forceinline__ uint32_t key_of(int64_t id, int64_t vocab, int* status) {
     if (id >= vocab) atomicCAS(status, 0, STATUS_BEYOND);
     return id < 0 || id >= vocab ? (uint32_t)vocab : (uint32_t)id;
 }
+__device__ __forceinline__ uint32_t key_of(const void* ids, int id_bytes, int64_t t, int64_t vocab, int* status) { return key_of(id_of(ids, id_bytes, t), vocab, status); }
 
 // CH consecutive elements as binary32
 template <typename T, int CH> struct Chunk;
@@ -107,6 +112,74 @@ __global__ void __launch_bounds__(LOOKUP_THREADS) embed_kernel(const EmbedArgs a
     }
 }
 
+// Rows on other boundaries (an odd width in bfloat16): 16 bytes are written at a time from the first boundary inside a row of y on, and read as the
+// one or two aligned pieces that they lie in (each holds an element of the row), shifted to their place.  65536 x 1999 of bfloat16 184 us element by
+// element.
+constexpr int SHIFTED_CHUNKS = 2;
+__device__ __forceinline__ uint4 load_shifted(const unsigned char* p) {
+    const uint32_t s = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u);
+    const uint4* q = reinterpret_cast<const uint4*>(p - s);
+    const uint4 a = __ldg(q), b = s ? __ldg(q + 1) : a;
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (s & 4u)
+#pragma unroll
+        for (int i = 0; i < 7; ++i) w[i] = w[i + 1];
+    if (s & 8u)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    if (s & 2u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__global__ void __launch_bounds__(LOOKUP_THREADS) embed_shifted_kernel(const EmbedArgs a, int log_lanes, int turns) {
+    constexpr int CH = 16 / sizeof(T);
+    grid_dependency_wait();
+    const int lanes = 1 << log_lanes, lane = threadIdx.x & (lanes - 1);
+    const int64_t groups = (int64_t)gridDim.x * (LOOKUP_THREADS >> log_lanes), units = a.tokens * turns;
+    for (int64_t u = (int64_t)blockIdx.x * (LOOKUP_THREADS >> log_lanes) + (threadIdx.x >> log_lanes); u < units; u += groups) {
+        const int64_t t = turns == 1 ? u : u / turns;
+        const int turn = (int)(u - t * turns);
+        const uint32_t key = key_of(a.ids, a.id_bytes, t, a.vocab, a.status);
+        const bool there = key < (uint32_t)a.vocab;
+        const T* src = static_cast<const T*>(a.table) + (int64_t)key * a.ld;
+        T* dst = static_cast<T*>(a.y) + t * a.ldy;
+        const int gap = (int)((16u - (uint32_t)(reinterpret_cast<uintptr_t>(dst) & 15u)) & 15u) / (int)sizeof(T);
+        const int first = gap < a.width ? gap : (int)a.width, whole = ((int)a.width - first) / CH, end = first + whole * CH;
+        auto element = [&](int e) {
+            float v;
+            if (there) Chunk<T, 1>::load(src + e, &v);
+            v = there ? v * a.scale : 0.f;
+            store<1>(dst + e, &v);
+        };
+        if (turn == 0) {                         // the ends
+            for (int e = lane; e < first; e += lanes) element(e);
+            for (int e = end + lane; e < a.width; e += lanes) element(e);
+        }
+        uint4 q[SHIFTED_CHUNKS];
+#pragma unroll
+        for (int i = 0; i < SHIFTED_CHUNKS; ++i) {
+            const int c = (turn * SHIFTED_CHUNKS + i) * lanes + lane;
+            if (there && c < whole) q[i] = load_shifted(reinterpret_cast<const unsigned char*>(src + first + c * CH));
+        }
+#pragma unroll
+        for (int i = 0; i < SHIFTED_CHUNKS; ++i) {
+            const int c = (turn * SHIFTED_CHUNKS + i) * lanes + lane;
+            if (c >= whole) continue;
+            float v[CH];
+            if constexpr (sizeof(T) == 2) {
+                Chunk<T, 2>::two(q[i].x, v); Chunk<T, 2>::two(q[i].y, v + 2); Chunk<T, 2>::two(q[i].z, v + 4); Chunk<T, 2>::two(q[i].w, v + 6);
+            } else {
+                v[0] = __uint_as_float(q[i].x); v[1] = __uint_as_float(q[i].y); v[2] = __uint_as_float(q[i].z); v[3] = __uint_as_float(q[i].w);
+            }
+#pragma unroll
+            for (int e = 0; e < CH; ++e) v[e] = there ? v[e] * a.scale : 0.f;
+            store<CH>(dst + first + c * CH, v);
+        }
+    }
+}
+
 template <typename T, typename Y, int CH>
 cudaError_t launch_lookup(const EmbedArgs& a, int num_sms, cudaStream_t s) {
     const int64_t chunks = (a.width + CH - 1) / CH;
@@ -125,6 +198,16 @@ cudaError_t launch_lookup_typed(const EmbedArgs& a, int num_sms, cudaStream_t s)
                reinterpret_cast<uintptr_t>(a.y) % out == 0 && a.ldy * sizeof(Y) % out == 0;
     };
     if (fits(WIDE)) return launch_lookup<T, Y, WIDE>(a, num_sms, s);
+    if constexpr (std::is_same<T, Y>::value) {
+        if (a.width >= 4 * WIDE) {               // (shorter rows are mostly ends)
+            const int64_t chunks = a.width / WIDE;
+            int log_lanes = 0;
+            while (log_lanes < 5 && ((int64_t)SHIFTED_CHUNKS << log_lanes) < chunks) ++log_lanes;
+            const int64_t turns = (chunks + (SHIFTED_CHUNKS << log_lanes) - 1) / (SHIFTED_CHUNKS << log_lanes), per_block = LOOKUP_THREADS >> log_lanes;
+            const int64_t blocks = (a.tokens * turns + per_block - 1) / per_block, most = (int64_t)num_sms * 64;
+            return launch_pdl(embed_shifted_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(LOOKUP_THREADS), 0, s, a, log_lanes, (int)turns);
+        }
+    }
     if constexpr (sizeof(T) == 2) if (fits(2)) return launch_lookup<T, Y, 2>(a, num_sms, s);
     return launch_lookup<T, Y, 1>(a, num_sms, s);
 }
@@ -141,13 +224,23 @@ __global__ void __launch_bounds__(RANK_THREADS) rank_kernel(const void* ids, int
     grid_dependency_wait();
     if (blockIdx.x == 0 && threadIdx.x < 2) crossing[threadIdx.x] = 0u;
     const int groups = (tokens + 3) >> 2;
-    for (int t = threadIdx.x; t < 4 * groups; t += RANK_THREADS) all[t] = t < tokens ? key_of(ids, id_bytes, t, vocab, status) : 0xFFFFFFFFu;
+    for (int t0 = threadIdx.x; t0 < 4 * groups; t0 += 8 * RANK_THREADS) {
+        int64_t id[8];                         // (their loads together)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) id[i] = t0 + i * RANK_THREADS < tokens ? id_of(ids, id_bytes, t0 + i * RANK_THREADS) : -1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = t0 + i * RANK_THREADS;
+            if (t < 4 * groups) all[t] = t < tokens ? key_of(id[i], vocab, status) : 0xFFFFFFFFu;
+        }
+    }
     __syncthreads();
     const int t = blockIdx.x * (RANK_THREADS / RANK_SHARE) + threadIdx.x / RANK_SHARE, share = threadIdx.x % RANK_SHARE;
     const bool mine = t < tokens;
     const uint32_t key = mine ? all[t] : 0u;
     int before = 0;
     const int own = t >> 2;                    // equal keys come before this one in the groups in front of its own ...
+#pragma unroll 4
     for (int g = share; g < groups; g += RANK_SHARE) {
         const uint4 q = reinterpret_cast<const uint4*>(all)[g];
         const uint32_t limit = key + (g < own ? 1u : 0u);
@@ -306,7 +399,6 @@ struct SumArgs {
     int d_type, accumulate;
     int piece, slabs;
     int64_t pieces;
-    int zero_vec;
 };
 
 template <int CH>
@@ -386,14 +478,14 @@ __global__ void __launch_bounds__(SUM_THREADS) sum_kernel(const SumArgs a) {
         const int64_t size = a.d_type == CERAR_TYPE_F32 ? 4 : 2;
         for (int i = 0; i < ZERO_ROWS; ++i) {
             if (key[i]) continue;
+            // 16 bytes at a time from the first boundary inside the row on
             unsigned char* p = static_cast<unsigned char*>(a.dtable) + (r0 + i) * a.ld * size;
-            if (a.zero_vec) {
-                for (int64_t b = threadIdx.x * 16; b < a.width * size; b += SUM_THREADS * 16) *reinterpret_cast<uint4*>(p + b) = make_uint4(0, 0, 0, 0);
-            } else if (size == 4) {
-                for (int64_t c = threadIdx.x; c < a.width; c += SUM_THREADS) reinterpret_cast<float*>(p)[c] = 0.f;
-            } else {
-                for (int64_t c = threadIdx.x; c < a.width; c += SUM_THREADS) reinterpret_cast<unsigned short*>(p)[c] = 0;
-            }
+            const int64_t bytes = a.width * size, gap = (int64_t)(-reinterpret_cast<uintptr_t>(p) & 15u), first = gap < bytes ? gap : bytes;
+            const int64_t end = first + ((bytes - first) & ~15ll);
+            for (int64_t b = first + threadIdx.x * 16; b < end; b += SUM_THREADS * 16) *reinterpret_cast<uint4*>(p + b) = make_uint4(0, 0, 0, 0);
+            const int64_t head = 2 * threadIdx.x, tail = end + 2 * threadIdx.x;
+            if (head < first) *reinterpret_cast<unsigned short*>(p + head) = 0;
+            if (tail < bytes) *reinterpret_cast<unsigned short*>(p + tail) = 0;
         }
         return;
     }
@@ -597,7 +689,6 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, int num_sms, cudaStream_t 
     s.named = named; s.crossing = crossing; s.accumulate = a.accumulate; s.piece = l.piece; s.pieces = l.pieces;
     const int64_t dsize = a.d_type == CERAR_TYPE_F32 ? 4 : 2;
     const uintptr_t dt = reinterpret_cast<uintptr_t>(a.dtable), dy = reinterpret_cast<uintptr_t>(a.dy);
-    s.zero_vec = dt % 16 == 0 && a.ld * dsize % 16 == 0 && a.width * dsize % 16 == 0;
     auto fits = [&](int ch) {
         const int64_t in = ch * (a.type == CERAR_TYPE_F32 ? 4 : 2), out = ch * dsize < 16 ? ch * dsize : 16;
         return a.width % ch == 0 && dy % in == 0 && a.lddy * (in / ch) % in == 0 && dt % out == 0 && a.ld * dsize % out == 0;

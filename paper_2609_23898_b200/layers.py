@@ -90,7 +90,7 @@ def embed(ops: Ops, table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.
     if not ids.is_contiguous():
         ids = ids.contiguous()
     vocab, width = table.shape
-    y = torch.empty((*ids.shape, width), dtype=dtype or table.dtype, device=table.device)
+    y = torch.empty(*ids.shape, width, dtype=dtype or table.dtype, device=table.device)      # (numbers: a torch.Size takes twice as long)
     st = lib.cerar_embed(ops._h, table.data_ptr(), kind, vocab, width, _stride(table), ids.data_ptr(), size, ids.numel(), scale, y.data_ptr(),
                          _kind(y, "dtype"), width, _raw(ops._index))
     if st:
@@ -190,13 +190,13 @@ def _part(what, x, w, y, dy, dw, like, types):
     """One group of heads: its fields of the descriptor, the result, its numbers, and what has to live until the call has been made.
     types: those of the weights and of their gradients so far."""
     shape, dtype = x.shape, x.dtype
-    if like is not None and (shape[:-2] != like.shape[:-2] or shape[-1] != like.shape[-1] or dtype != like.dtype):
-        raise ValueError("q and k: the same tokens, values per head and type are wanted")
     x3 = _heads(x, what)
     n, h, d = x3.shape
+    if like is not None and (n != like[0] or d != like[1] or dtype != like[2] or (len(like[3]) != 1 if x3 is x else shape[:-2] != like[3])):
+        raise ValueError("q and k: the same tokens, values per head and type are wanted")
     sx = x3.stride()
     if y is None:
-        y = torch.empty(shape, dtype=dtype, device=x.device)
+        y = torch.empty(*shape, dtype=dtype, device=x.device)
         y3, ty, hy = y, h * d, d
     else:
         if y.shape != shape or y.dtype != dtype:
@@ -242,7 +242,7 @@ def head_norm(ops: Ops, q: torch.Tensor, k: torch.Tensor | None, wq, wk, table: 
     kind, types = _kind(q, "q"), [None, None]
     yq, yk = (None, None) if out is None else out
     first, yq, n, d, kept = _part("q", q, wq, yq, None, None, None, types)
-    second, yk, _, _, kept2 = (_NO_PART, None, 0, 0, None) if k is None else _part("k", k, wk, yk, None, None, q, types)
+    second, yk, _, _, kept2 = (_NO_PART, None, 0, 0, None) if k is None else _part("k", k, wk, yk, None, None, (n, d, q.dtype, q.shape[:-2]), types)
     if positions is not None and not positions.is_contiguous():
         positions = positions.contiguous()
     rotation = _rotation(table, positions, q.shape[:-2], pairs)
@@ -262,7 +262,7 @@ def head_norm_backward(ops: Ops, dq: torch.Tensor, dk: torch.Tensor | None, q: t
         raise ValueError("dk and dwk belong to k")
     yq, yk = (None, None) if out is None else out
     first, yq, n, d, kept = _part("q", q, wq, yq, dq, dwq, None, types)
-    second, yk, _, _, kept2 = (_NO_PART, None, 0, 0, None) if k is None else _part("k", k, wk, yk, dk, dwk, q, types)
+    second, yk, _, _, kept2 = (_NO_PART, None, 0, 0, None) if k is None else _part("k", k, wk, yk, dk, dwk, (n, d, q.dtype, q.shape[:-2]), types)
     if positions is not None and not positions.is_contiguous():
         positions = positions.contiguous()
     rotation = _rotation(table, positions, q.shape[:-2], pairs)
