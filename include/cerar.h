@@ -676,29 +676,48 @@ typedef struct {
 } cerar_rows_t;
 cerar_status_t cerar_align_bf16(cerar_ops_t* ops, const cerar_rows_t* items, int count, cerar_stream_t stream);
 
-/* The two products of a gated feed-forward block that carry its elementwise part.  The block, for x (tokens x width) and bfloat16 weights
- * w_in (2 hidden x width: the gate's rows, then the other projection's) and w_out (outputs x hidden):
+/* A gated feed-forward block, for x (tokens x width) and bfloat16 weights w_in (2 hidden x width: the gate's rows, then the other
+ * projection's) and w_out (outputs x hidden):
  *     [g u] = x w_in^T,   h = act(g) u,   y = h w_out^T
  *     dh = dy w_out,  dg = dh u act'(g),  du = dh act(g),  dx = [dg du] w_in,  dw_in += [dg du]^T x,  dw_out += dy^T h
- * cerar_gated_in makes h (tokens x hidden) from the binary32 sums and, where `kept` is not NULL, leaves there g and u for the backward pass,
- * in 24 bits each (2^-16 of themselves off): cerar_gated_kept_bytes bytes on a 16-byte boundary, in a layout of its own.  cerar_gated_grad makes
- * [dg du] (tokens x 2 hidden) and, where h is not NULL, h again, from dy (tokens x width), w_out (width x hidden; width > 0) and kept; dh stays in
- * binary32.  dg, du and h are bfloat16 in memory, as the operands of the products that follow have to be; each is rounded once.
- * The sums are within 2^-23 (8 + K / 16) of the sum of their terms' magnitudes, K the width.
- * x, dy, w: as the operands of cerar_matmul_bf16; the others need alignment to their elements (16-byte rows and hidden a multiple of 8 are
- * faster). */
+ * Activation and gate are made from the binary32 sums in the first product, their gradient in the product for dh, which stays in binary32.
+ * h, dg and du are bfloat16 in memory, as the operands of the products that follow have to be; each is rounded once.  Where `kept` is
+ * not NULL, cerar_gated_forward leaves there g and u for the backward pass, in 24 bits each (2^-16 of themselves off):
+ * cerar_gated_kept_bytes bytes on a 16-byte boundary, in a layout of its own; h is made from them again.
+ * The sums of g, u and dh are within 2^-23 (8 + K / 16) of the sum of their terms' magnitudes, the others' as cerar_matmul_bf16's. */
 typedef enum {
     CERAR_ACT_SILU = 0,          /* g / (1 + e^-g)                                                        */
     CERAR_ACT_GELU = 1,          /* g Phi(g), Phi the normal distribution                                 */
     CERAR_ACT_GELU_TANH = 2,     /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2                      */
     CERAR_ACT_RELU = 3           /* max(g, 0); its derivative at 0 is 0                                    */
 } cerar_activation_t;
+typedef struct {
+    int64_t     tokens, width, hidden, outputs;
+    int64_t     activation;      /* cerar_activation_t */
+    int64_t     accumulate;      /* backward: dw_in and dw_out are added to                                        */
+    const void* x;               /* tokens x width, bfloat16, ldx elements between rows; backward: for dw_in only   */
+    int64_t     ldx;
+    const void* w_in;            /* 2 hidden x width; backward: for dx only                                        */
+    int64_t     ldw_in;
+    const void* w_out;           /* outputs x hidden                                                               */
+    int64_t     ldw_out;
+    void*       kept;            /* forward: written (NULL: nothing is kept); backward: read                       */
+    void*       y;               /* forward: tokens x outputs, bfloat16                                            */
+    int64_t     ldy;
+    const void* dy;              /* backward: tokens x outputs, bfloat16                                           */
+    int64_t     lddy;
+    void*       dx;              /* backward: tokens x width, bfloat16; NULL: not wanted                           */
+    int64_t     lddx;
+    void*       dw_in;           /* backward: 2 hidden x width of dw_in_type; NULL: not wanted                     */
+    int64_t     lddw_in, dw_in_type;
+    void*       dw_out;          /* backward: outputs x hidden of dw_out_type; NULL: not wanted                    */
+    int64_t     lddw_out, dw_out_type;
+} cerar_gated_t;
+/* Everything is aligned to its elements; operands whose rows are not on 16-byte boundaries are copied to the workspace in every call. */
 size_t         cerar_gated_kept_bytes(int64_t tokens, int64_t hidden);
-cerar_status_t cerar_gated_in(cerar_ops_t* ops, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t tokens, int64_t width,
-                              int64_t hidden, cerar_activation_t act, void* h, int64_t ldh, void* kept, cerar_stream_t stream);
-cerar_status_t cerar_gated_grad(cerar_ops_t* ops, const void* dy, int64_t lddy, const void* w, int64_t ldw, int64_t tokens, int64_t width,
-                                int64_t hidden, cerar_activation_t act, const void* kept, void* dgu, int64_t lddgu, void* h, int64_t ldh,
-                                cerar_stream_t stream);
+size_t         cerar_gated_workspace(const cerar_gated_t* block, int backward);
+cerar_status_t cerar_gated_forward(cerar_ops_t* ops, const cerar_gated_t* block, void* workspace, size_t workspace_bytes, cerar_stream_t stream);
+cerar_status_t cerar_gated_backward(cerar_ops_t* ops, const cerar_gated_t* block, void* workspace, size_t workspace_bytes, cerar_stream_t stream);
 
 const char*    cerar_status_string(cerar_status_t s);
 const char*    cerar_last_error(void);   /* thread-local detail of the last failure */

@@ -63,6 +63,14 @@ class Rotation(C.Structure):
                 ("position_bytes", C.c_int32), ("rotated", C.c_int32), ("neighbours", C.c_int32)]
 
 
+class GatedBlock(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("tokens", "width", "hidden", "outputs", "activation", "accumulate")] + \
+               [("x", C.c_void_p), ("ldx", C.c_int64), ("w_in", C.c_void_p), ("ldw_in", C.c_int64), ("w_out", C.c_void_p), ("ldw_out", C.c_int64),
+                ("kept", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_int64), ("dy", C.c_void_p), ("lddy", C.c_int64), ("dx", C.c_void_p),
+                ("lddx", C.c_int64), ("dw_in", C.c_void_p), ("lddw_in", C.c_int64), ("dw_in_type", C.c_int64), ("dw_out", C.c_void_p),
+                ("lddw_out", C.c_int64), ("dw_out_type", C.c_int64)]
+
+
 class TensorDesc(C.Structure):
     _fields_ = [("numel", C.c_int64), ("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p),
                 ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
@@ -168,8 +176,10 @@ lib.cerar_matmul_bf16_tile.argtypes = [_i64, _i64, _i64, C.c_int, C.POINTER(C.c_
 lib.cerar_align_bf16.argtypes = [_vp, _vp, C.c_int, _vp]
 lib.cerar_gated_kept_bytes.argtypes = [_i64, _i64]
 lib.cerar_gated_kept_bytes.restype = C.c_size_t
-lib.cerar_gated_in.argtypes = [_vp, _vp, _i64, _vp, _i64, _i64, _i64, _i64, C.c_int, _vp, _i64, _vp, _vp]
-lib.cerar_gated_grad.argtypes = [_vp, _vp, _i64, _vp, _i64, _i64, _i64, _i64, C.c_int, _vp, _vp, _i64, _vp, _i64, _vp]
+lib.cerar_gated_workspace.argtypes = [_vp, C.c_int]
+lib.cerar_gated_workspace.restype = C.c_size_t
+lib.cerar_gated_forward.argtypes = [_vp, _vp, _vp, C.c_size_t, _vp]
+lib.cerar_gated_backward.argtypes = [_vp, _vp, _vp, C.c_size_t, _vp]
 lib.cerar_status_string.argtypes = [C.c_int]
 lib.cerar_status_string.restype = C.c_char_p
 lib.cerar_last_error.restype = C.c_char_p

@@ -86,8 +86,84 @@ cerar_status_t check_operand(const void* p, int64_t rows, int64_t cols, int64_t 
     if (ld < cols || ld % 8 || ld >= (int64_t)1 << 39) return fail(CERAR_ERR_SHAPE, "matrix: ld must be a multiple of 8, at least the number of columns and below 2^39");
     return CERAR_OK;
 }
-cerar_status_t check_act(int act) {
-    return act >= CERAR_ACT_SILU && act <= CERAR_ACT_RELU ? CERAR_OK : fail(CERAR_ERR_INVALID_ARG, "unknown activation");
+
+// ---- the gated block: its operands as the products read them, and what it makes on the way, in one workspace
+
+struct Mat {                                                 // rows of bfloat16, 16-byte aligned
+    void* p;
+    int64_t ld;
+};
+struct Block {
+    Mat x, w_in, w_out, dy, h, dgu;
+    cerar::AlignArgs copies[cerar::ALIGN_MAX];
+    int count;
+    int64_t bytes;
+};
+cerar_status_t check_gated(const cerar_gated_t& g, bool backward) {
+    if (g.tokens < 0 || g.tokens > TOKENS_MAX || g.width < 0 || g.width > SIZE_MAX_ || g.outputs < 0 || g.outputs > SIZE_MAX_ || g.hidden < 0 || g.hidden > SIZE_MAX_ / 2)
+        return fail(CERAR_ERR_SHAPE, "gated block: negative sizes, above 2^31 - 256, or hidden above 2^30 - 128");
+    if (g.activation < CERAR_ACT_SILU || g.activation > CERAR_ACT_RELU) return fail(CERAR_ERR_INVALID_ARG, "unknown activation");
+    cerar_status_t st;
+    const bool x = !backward || g.dw_in, w_in = !backward || g.dx;
+    if ((x && (st = check_rows(g.x, CERAR_TYPE_BF16, g.tokens, g.width, g.ldx, "x NULL or not aligned to its elements")) != CERAR_OK) ||
+        (w_in && (st = check_rows(g.w_in, CERAR_TYPE_BF16, 2 * g.hidden, g.width, g.ldw_in, "w_in NULL or not aligned to its elements")) != CERAR_OK) ||
+        (st = check_rows(g.w_out, CERAR_TYPE_BF16, g.outputs, g.hidden, g.ldw_out, "w_out NULL or not aligned to its elements")) != CERAR_OK)
+        return st;
+    if (misaligned(g.kept, 16) || (backward && !g.kept && g.tokens > 0 && g.hidden > 0 && g.outputs > 0))
+        return fail(CERAR_ERR_INVALID_ARG, "kept NULL where it is needed, or not on a 16-byte boundary");
+    if (!backward) return check_rows(g.y, CERAR_TYPE_BF16, g.tokens, g.outputs, g.ldy, "y NULL or not aligned to its elements");
+    if ((st = check_rows(g.dy, CERAR_TYPE_BF16, g.tokens, g.outputs, g.lddy, "dy NULL or not aligned to its elements")) != CERAR_OK ||
+        (g.dx && (st = check_rows(g.dx, CERAR_TYPE_BF16, g.tokens, g.width, g.lddx, "dx not aligned to its elements")) != CERAR_OK) ||
+        (g.dw_in && (st = check_rows(g.dw_in, (int)g.dw_in_type, 2 * g.hidden, g.width, g.lddw_in, "dw_in not aligned to its elements")) != CERAR_OK) ||
+        (g.dw_out && (st = check_rows(g.dw_out, (int)g.dw_out_type, g.outputs, g.hidden, g.lddw_out, "dw_out not aligned to its elements")) != CERAR_OK))
+        return st;
+    return CERAR_OK;
+}
+// false: the workspace would have more than 2^62 bytes
+bool lay_out(const cerar_gated_t& g, bool backward, void* workspace, Block& b) {
+    b = {};
+    unsigned char* at = static_cast<unsigned char*>(workspace);
+    bool fits = true;
+    auto take = [&](int64_t rows, int64_t cols, Mat& m) {
+        m.ld = (cols + 7) & ~(int64_t)7;
+        const __int128 size = (__int128)rows * m.ld * 2 + 255;
+        if (b.bytes + size > (__int128)1 << 62) { fits = false; return; }
+        m.p = at + b.bytes;
+        b.bytes += (int64_t)size & ~(int64_t)255;
+    };
+    auto operand = [&](const void* p, int64_t rows, int64_t cols, int64_t ld, Mat& m) {
+        if (rows == 0 || cols == 0) { m = {nullptr, 8}; return; }
+        if (rows < 2) ld = (cols + 7) & ~(int64_t)7;
+        if (!misaligned(p, 16) && ld % 8 == 0) { m = {const_cast<void*>(p), ld}; return; }
+        take(rows, cols, m);
+        b.copies[b.count++] = {p, m.p, rows, cols, ld, m.ld};
+    };
+    const bool empty = g.tokens == 0 || g.hidden == 0 || g.outputs == 0;
+    if (backward && empty) return true;
+    if (!backward || g.dw_in) operand(g.x, g.tokens, g.width, g.ldx, b.x);
+    if (!backward || g.dx) operand(g.w_in, 2 * g.hidden, g.width, g.ldw_in, b.w_in);
+    operand(g.w_out, g.outputs, g.hidden, g.ldw_out, b.w_out);
+    if (backward) {
+        operand(g.dy, g.tokens, g.outputs, g.lddy, b.dy);
+        take(g.tokens, 2 * g.hidden, b.dgu);
+        if (g.dw_out) take(g.tokens, g.hidden, b.h);
+    } else {
+        take(g.tokens, g.hidden, b.h);
+    }
+    return fits;
+}
+cerar_status_t check_workspace(const cerar_gated_t& g, bool backward, void* workspace, size_t bytes, Block& b) {
+    if (!lay_out(g, backward, workspace, b)) return fail(CERAR_ERR_TOO_LARGE, "gated block: a workspace above 2^62 bytes");
+    if (b.bytes > 0 && (!workspace || misaligned(workspace, 16))) return fail(CERAR_ERR_INVALID_ARG, "workspace NULL or not aligned to 16 bytes");
+    if ((int64_t)bytes < b.bytes) return fail(CERAR_ERR_SHAPE, "the workspace is too small");
+    return CERAR_OK;
+}
+// C (+)= op(a) op(b); an empty sum is zero
+cudaError_t product(cerar_ops* o, const Mat& a, bool trans_a, const Mat& b, bool trans_b, int64_t M, int64_t N, int64_t K, void* C, int type, int64_t ldc, bool accumulate, cudaStream_t s) {
+    if (M == 0 || N == 0) return cudaSuccess;
+    if (K == 0)
+        return accumulate ? cudaSuccess : cudaMemset2DAsync(C, (size_t)(M > 1 ? ldc : N) * type_bytes(type), 0, (size_t)N * type_bytes(type), (size_t)M, s);
+    return cerar::launch_matmul16({a.p, b.p, a.ld, b.ld, trans_a, trans_b, M, N, K, C, ldc, type, accumulate ? 1 : 0, o->d_status}, o->num_sms, s, &o->launches);
 }
 
 }  // namespace
@@ -193,14 +269,7 @@ cerar_status_t cerar_matmul_bf16(cerar_ops_t* o, const void* A, int64_t lda, int
         (st = check_rows(C, type, M, N, ldc, "C NULL or not aligned to its elements")) != CERAR_OK)
         return st;
     if (M == 0 || N == 0) return CERAR_OK;
-    cudaError_t e = cudaSuccess;
-    if (K == 0) {                         // an empty sum
-        if (!accumulate)
-            e = cudaMemset2DAsync(C, (size_t)(M > 1 ? ldc : N) * type_bytes(type), 0, (size_t)N * type_bytes(type), (size_t)M, (cudaStream_t)stream);
-    } else {
-        const cerar::Matmul16Args a = {A, B, lda, ldb, trans_a != 0, trans_b != 0, M, N, K, C, ldc, type, accumulate != 0, o->d_status};
-        e = cerar::launch_matmul16(a, o->num_sms, (cudaStream_t)stream, &o->launches);
-    }
+    const cudaError_t e = product(o, {const_cast<void*>(A), lda}, trans_a != 0, {const_cast<void*>(B), ldb}, trans_b != 0, M, N, K, C, type, ldc, accumulate != 0, (cudaStream_t)stream);
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "bfloat16 matmul launch");
 }
 
@@ -233,41 +302,47 @@ size_t cerar_gated_kept_bytes(int64_t tokens, int64_t hidden) {
     return cerar::gated_kept_bytes(tokens, hidden);
 }
 
-cerar_status_t cerar_gated_in(cerar_ops_t* o, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t tokens, int64_t width, int64_t hidden,
-                              cerar_activation_t act, void* h, int64_t ldh, void* kept, cerar_stream_t stream) {
+size_t cerar_gated_workspace(const cerar_gated_t* g, int backward) {
+    Block b;
+    return g && check_gated(*g, backward != 0) == CERAR_OK && lay_out(*g, backward != 0, nullptr, b) ? (size_t)b.bytes : 0;
+}
+
+cerar_status_t cerar_gated_forward(cerar_ops_t* o, const cerar_gated_t* g, void* workspace, size_t workspace_bytes, cerar_stream_t stream) {
     cerar_status_t st = check_ops(o);
     if (st != CERAR_OK) return st;
-    if (hidden < 0 || hidden > SIZE_MAX_ / 2) return fail(CERAR_ERR_SHAPE, "gated: hidden must be from 0 to 2^30 - 128");
-    if ((st = check_act(act)) != CERAR_OK || (st = check_operand(x, tokens, width, ldx)) != CERAR_OK || (st = check_operand(w, 2 * hidden, width, ldw)) != CERAR_OK ||
-        (st = check_rows(h, CERAR_TYPE_BF16, tokens, hidden, ldh, "h NULL or not aligned to its elements")) != CERAR_OK)
-        return st;
-    if (misaligned(kept, 16)) return fail(CERAR_ERR_INVALID_ARG, "kept is not on a 16-byte boundary");
-    if (tokens == 0 || hidden == 0) return CERAR_OK;
-    cudaError_t e = cudaSuccess;
-    if (width == 0) {                     // empty sums: g = u = 0, and act(0) 0 = 0
-        e = cudaMemset2DAsync(h, (size_t)(tokens > 1 ? ldh : hidden) * 2, 0, (size_t)hidden * 2, (size_t)tokens, (cudaStream_t)stream);
-        if (e == cudaSuccess && kept) e = cudaMemsetAsync(kept, 0, cerar::gated_kept_bytes(tokens, hidden), (cudaStream_t)stream);
-    } else {
-        const cerar::GatedInArgs a = {x, w, ldx, ldw, tokens, width, hidden, act, h, kept, ldh, o->d_status};
-        e = cerar::launch_gated_in(a, o->num_sms, (cudaStream_t)stream, &o->launches);
+    if (!g) return fail(CERAR_ERR_INVALID_ARG, "the block's description is NULL");
+    if ((st = check_gated(*g, false)) != CERAR_OK) return st;
+    if (g->tokens == 0 || g->outputs == 0) return CERAR_OK;
+    Block b;
+    if ((st = check_workspace(*g, false, workspace, workspace_bytes, b)) != CERAR_OK) return st;
+    const cudaStream_t s = (cudaStream_t)stream;
+    cudaError_t e = cerar::launch_align(b.copies, b.count, s, &o->launches);
+    if (e == cudaSuccess && g->hidden > 0 && g->width == 0) {            // empty sums: g = u = 0, and act(0) 0 = 0
+        e = cudaMemsetAsync(b.h.p, 0, (size_t)g->tokens * b.h.ld * 2, s);
+        if (e == cudaSuccess && g->kept) e = cudaMemsetAsync(g->kept, 0, cerar::gated_kept_bytes(g->tokens, g->hidden), s);
+    } else if (e == cudaSuccess && g->hidden > 0) {
+        e = cerar::launch_gated_in({b.x.p, b.w_in.p, b.x.ld, b.w_in.ld, g->tokens, g->width, g->hidden, (int)g->activation, b.h.p, g->kept, b.h.ld, o->d_status}, o->num_sms, s, &o->launches);
     }
+    if (e == cudaSuccess) e = product(o, b.h, false, b.w_out, true, g->tokens, g->outputs, g->hidden, g->y, CERAR_TYPE_BF16, g->ldy, false, s);
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "gated block launch");
 }
 
-cerar_status_t cerar_gated_grad(cerar_ops_t* o, const void* dy, int64_t lddy, const void* w, int64_t ldw, int64_t tokens, int64_t width, int64_t hidden,
-                                cerar_activation_t act, const void* kept, void* dgu, int64_t lddgu, void* h, int64_t ldh, cerar_stream_t stream) {
+cerar_status_t cerar_gated_backward(cerar_ops_t* o, const cerar_gated_t* g, void* workspace, size_t workspace_bytes, cerar_stream_t stream) {
     cerar_status_t st = check_ops(o);
     if (st != CERAR_OK) return st;
-    if (hidden < 0 || hidden > SIZE_MAX_ / 2) return fail(CERAR_ERR_SHAPE, "gated: hidden must be from 0 to 2^30 - 128");
-    if ((st = check_act(act)) != CERAR_OK || (st = check_operand(dy, tokens, width, lddy)) != CERAR_OK || (st = check_operand(w, width, hidden, ldw)) != CERAR_OK ||
-        (st = check_rows(dgu, CERAR_TYPE_BF16, tokens, 2 * hidden, lddgu, "dgu NULL or not aligned to its elements")) != CERAR_OK ||
-        (h && (st = check_rows(h, CERAR_TYPE_BF16, tokens, hidden, ldh, "h not aligned to its elements")) != CERAR_OK))
-        return st;
-    if (tokens == 0 || hidden == 0) return CERAR_OK;
-    if (!kept || misaligned(kept, 16)) return fail(CERAR_ERR_INVALID_ARG, "kept NULL, or not on a 16-byte boundary");
-    if (width == 0) return fail(CERAR_ERR_SHAPE, "gated gradient: a block without outputs has none");
-    const cerar::GatedGradArgs a = {dy, w, kept, lddy, ldw, tokens, width, hidden, act, dgu, h, lddgu, ldh, o->d_status};
-    const cudaError_t e = cerar::launch_gated_grad(a, o->num_sms, (cudaStream_t)stream, &o->launches);
+    if (!g) return fail(CERAR_ERR_INVALID_ARG, "the block's description is NULL");
+    if ((st = check_gated(*g, true)) != CERAR_OK) return st;
+    Block b;
+    if ((st = check_workspace(*g, true, workspace, workspace_bytes, b)) != CERAR_OK) return st;
+    const cudaStream_t s = (cudaStream_t)stream;
+    const int64_t t = g->tokens, d = g->width, f = g->hidden, n = g->outputs;
+    cudaError_t e = cerar::launch_align(b.copies, b.count, s, &o->launches);
+    const bool reached = t > 0 && f > 0 && n > 0;                        // otherwise every sum below is empty
+    if (e == cudaSuccess && reached)
+        e = cerar::launch_gated_grad({b.dy.p, b.w_out.p, g->kept, b.dy.ld, b.w_out.ld, t, n, f, (int)g->activation, b.dgu.p, b.h.p, b.dgu.ld, b.h.ld, o->d_status}, o->num_sms, s, &o->launches);
+    if (e == cudaSuccess && g->dx) e = product(o, b.dgu, false, b.w_in, false, t, d, reached ? 2 * f : 0, g->dx, CERAR_TYPE_BF16, g->lddx, false, s);
+    if (e == cudaSuccess && g->dw_in) e = product(o, b.dgu, true, b.x, false, 2 * f, d, reached ? t : 0, g->dw_in, (int)g->dw_in_type, g->lddw_in, g->accumulate != 0, s);
+    if (e == cudaSuccess && g->dw_out) e = product(o, b.dy, true, b.h, false, n, f, reached ? t : 0, g->dw_out, (int)g->dw_out_type, g->lddw_out, g->accumulate != 0, s);
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "gated block gradient launch");
 }
 

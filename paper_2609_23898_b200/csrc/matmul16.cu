@@ -1,5 +1,5 @@
 // Products of bfloat16 matrices on the tensor cores, and the two of a gated feed-forward block that carry its elementwise part
-// (cerar_matmul_bf16, cerar_gated_in, cerar_gated_grad; sm_100a: TMA + tcgen05 + TMEM).
+// (cerar_matmul_bf16, cerar_gated_forward, cerar_gated_backward; sm_100a: TMA + tcgen05 + TMEM).
 //
 //   plain   C (+)= op(A) op(B)
 //   gate    [g u] = x W^T in one accumulator, h = act(g) u: a tile holds the same columns of both projections side by side

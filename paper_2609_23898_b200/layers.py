@@ -4,8 +4,8 @@
   rotation_table, head_norm, head_norm_backward, HeadNorm
                                             norms of queries and keys for each head, with the rotation by position in the same pass
                                             (cerar_rotation_table, cerar_head_norm, cerar_head_norm_grad)
-  matmul, gated, gated_backward, Gated      bfloat16 products, and a gated feed-forward block made of them (cerar_matmul_bf16, cerar_gated_in,
-                                            cerar_gated_grad)
+  matmul, gated, gated_backward, Gated      bfloat16 products, and a gated feed-forward block made of them (cerar_matmul_bf16, cerar_gated_forward,
+                                            cerar_gated_backward)
 
 As with training.Linear8 the gradients of weights are added to buffers of the caller's (slices of the vector that is aggregated) and the
 weights have none of their own.  Everything runs on the current stream of the tensors' device, without synchronisation.
@@ -310,32 +310,33 @@ _BF16 = torch.bfloat16
 
 
 _ROWS = struct.Struct("6q")          # cerar_rows_t
+_BLOCK = struct.Struct("25q")        # cerar_gated_t
+assert _BLOCK.size == C.sizeof(cerar.GatedBlock)
+
+
+def _bf16(t: torch.Tensor, what: str) -> torch.Tensor:
+    """A bfloat16 matrix whose rows are contiguous: a copy where they are not."""
+    if t.dtype != _BF16:
+        raise TypeError(f"{what}: bfloat16 wanted, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{what}: a two-dimensional tensor is wanted")
+    return _rows(t)
 
 
 def _operands(ops: Ops, *given):
-    """bfloat16 matrices (tensor, its name) as tensor-map copies read them, rows on 16-byte boundaries: copies (one launch for all of them) of those
-    that are not.  Each as [tensor, address, elements between rows]."""
+    """bfloat16 matrices (as _bf16 gives them) with rows on 16-byte boundaries, as tensor-map copies read them: copies, one launch for all of them, of
+    those that are not.  Each as (tensor, address, elements between rows)."""
     out, copies = [], b""
-    for t, what in given:
-        if t.dtype != _BF16:
-            raise TypeError(f"{what}: bfloat16 wanted, got {t.dtype}")
-        shape = t.shape
-        if len(shape) != 2:
-            raise ValueError(f"{what}: a two-dimensional CUDA tensor is wanted")
-        rows, cols = shape
-        row, col = t.stride()
-        at = t.data_ptr()
-        if (col == 1 or cols == 1) and (rows == 1 or row >= cols and not row & 7) and not at & 15 or not rows or not cols:
-            out.append((t, at, row if rows > 1 and cols else (cols + 7) & -8))
+    for t in given:
+        rows, cols = t.shape
+        row, at, ld = t.stride(0), t.data_ptr(), (cols + 7) & -8
+        if not (rows and cols) or not at & 15 and (rows == 1 or not row & 7):
+            out.append((t, at, row if rows > 1 and cols else ld))
             continue
-        wide = _padded(rows, cols, t.device)
+        wide = torch.empty(rows, ld, dtype=_BF16, device=t.device)
         to = wide.data_ptr()
-        if (col == 1 or cols == 1) and (rows == 1 or row >= cols):
-            copies += _ROWS.pack(at, to, rows, cols, row if rows > 1 else cols, (cols + 7) & -8)
-            wide = wide if wide.size(1) == cols else wide[:, :cols]
-        else:
-            wide = wide[:, :cols].copy_(t)
-        out.append((wide, to, (cols + 7) & -8))
+        copies += _ROWS.pack(at, to, rows, cols, row if rows > 1 else cols, ld)
+        out.append((wide, to, ld))
     if copies:
         st = lib.cerar_align_bf16(ops._h, copies, len(copies) // _ROWS.size, _raw(ops._index))
         if st:
@@ -343,26 +344,11 @@ def _operands(ops: Ops, *given):
     return out
 
 
-def _padded(rows: int, cols: int, device) -> torch.Tensor:
-    """An empty bfloat16 matrix with rows on 16-byte boundaries (columns up to a multiple of 8 that belong to no one)."""
-    return torch.empty(rows, (cols + 7) & -8, dtype=_BF16, device=device)
-
-
-def _matmul(ops, a, lda, trans_a, b, ldb, trans_b, m, n, k, out, accumulate):
-    """(a and b: addresses of operands as _operands gives them)"""
-    st = lib.cerar_matmul_bf16(ops._h, a, lda, trans_a, b, ldb, trans_b, m, n, k, out.data_ptr(), _kind(out, "out"), _stride(out), accumulate,
-                               _raw(ops._index))
-    if st:
-        _check(st)
-    return out
-
-
 def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b=False, out: torch.Tensor | None = None,
            dtype: torch.dtype = torch.bfloat16, accumulate=False) -> torch.Tensor:
     """op(a) op(b) of bfloat16 matrices, into `out` (float32 or bfloat16) if given, added to it with accumulate."""
     _here(ops, (a, b, out), "a b out")
-    if a.dim() != 2 or b.dim() != 2:
-        raise ValueError("a and b: two-dimensional tensors are wanted")
+    a, b = _bf16(a, "a"), _bf16(b, "b")
     m, k = (a.size(1), a.size(0)) if trans_a else a.shape
     k2, n = (b.size(1), b.size(0)) if trans_b else b.shape
     if k != k2:
@@ -375,8 +361,12 @@ def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b
         _matrix(out, "out")
         if tuple(out.shape) != (m, n):
             raise ValueError(f"out of shape {(m, n)} wanted, got {tuple(out.shape)}")
-    (a, pa, lda), (b, pb, ldb) = _operands(ops, (a, "a"), (b, "b"))
-    return _matmul(ops, pa, lda, trans_a, pb, ldb, trans_b, m, n, k, out, accumulate)
+    (a, pa, lda), (b, pb, ldb) = _operands(ops, a, b)
+    st = lib.cerar_matmul_bf16(ops._h, pa, lda, trans_a, pb, ldb, trans_b, m, n, k, out.data_ptr(), _kind(out, "out"), _stride(out), accumulate,
+                               _raw(ops._index))
+    if st:
+        _check(st)
+    return out
 
 
 def _gated_sizes(x, w_in, w_out, activation):
@@ -388,58 +378,25 @@ def _gated_sizes(x, w_in, w_out, activation):
         raise ValueError(f"x: {w_in.size(1)} values in the last dimension wanted")
 
 
-def _gated(ops, x, w_in, w_out, activation, keep):
-    """x as a matrix; returns y, x as the products read it, and the kept g and u."""
-    t, d = x.shape
-    o, f = w_out.shape
-    device, at = x.device, _raw(ops._index)
-    (x, xp, ldx), (wi, wip, ldi), (wo, wop, ldo) = _operands(ops, (x, "x"), (w_in, "w_in"), (w_out, "w_out"))
-    h = _padded(t, f, device)
-    hp, ldh = h.data_ptr(), (f + 7) & -8
-    gu = torch.empty(lib.cerar_gated_kept_bytes(t, f), dtype=torch.uint8, device=device) if keep else None
-    st = lib.cerar_gated_in(ops._h, xp, ldx, wip, ldi, t, d, f, _ACTIVATIONS[activation], hp, ldh, None if gu is None else gu.data_ptr(), at)
-    if st:
-        _check(st)
-    y = torch.empty(t, o, dtype=_BF16, device=device)
-    st = lib.cerar_matmul_bf16(ops._h, hp, ldh, False, wop, ldo, True, t, o, f, y.data_ptr(), 1, o, False, at)
-    if st:
-        _check(st)
-    return y, x, gu
-
-
 def gated(ops: Ops, x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *, activation: str = "silu", keep=False):
     """(act(x w_g^T) * (x w_u^T)) w_out^T for x (..., inputs), w_in = w_g over w_u (2 hidden x inputs) and w_out (outputs x hidden), all bfloat16.
     activation: silu, gelu, gelu_tanh or relu.  With keep also what gated_backward wants of it: (x, g and u in 24 bits, the activation)."""
     _here(ops, (x, w_in, w_out), "x w_in w_out")
     _gated_sizes(x, w_in, w_out, activation)
-    y, xm, gu = _gated(ops, _rows(x), w_in, w_out, activation, keep)
-    y = y.view(*x.shape[:-1], y.size(-1))
-    return (y, (xm, gu, activation)) if keep else y
-
-
-def _gated_backward(ops, dy, kept, w_in, w_out, dw_in, dw_out, accumulate, need_dx):
-    x, gu, activation = kept
-    (t, d), (o, f) = x.shape, w_out.shape
-    if not (o and f):                                                # nothing reaches x or w_in, and w_out has no elements
-        if dw_in is not None and not accumulate:
-            dw_in.zero_()
-        return torch.zeros(t, d, dtype=_BF16, device=x.device) if need_dx else None
-    dx, device = None, x.device
-    given = [(dy, "dy"), (w_out, "w_out"), (x, "x")] + ([(w_in, "w_in")] if need_dx else [])
-    (dy, dyp, lddy), (wo, wop, ldo), (x, xp, ldx), *wi = _operands(ops, *given)
-    dgu = _padded(t, 2 * f, device)
-    h = None if dw_out is None else _padded(t, f, device)
-    gp, ldg, hp, ldh = dgu.data_ptr(), (2 * f + 7) & -8, None if h is None else h.data_ptr(), (f + 7) & -8
-    st = lib.cerar_gated_grad(ops._h, dyp, lddy, wop, ldo, t, o, f, _ACTIVATIONS[activation], gu.data_ptr(), gp, ldg, hp, ldh, _raw(ops._index))
+    xm, wi, wo = _bf16(_rows(x), "x"), _bf16(w_in, "w_in"), _bf16(w_out, "w_out")
+    (t, d), (o, f), device = xm.shape, wo.shape, x.device
+    gu = torch.empty(lib.cerar_gated_kept_bytes(t, f), dtype=torch.uint8, device=device) if keep else None
+    y = torch.empty(t, o, dtype=_BF16, device=device)
+    block = _BLOCK.pack(t, d, f, o, _ACTIVATIONS[activation], 0, xm.data_ptr(), _stride(xm), wi.data_ptr(), _stride(wi), wo.data_ptr(), _stride(wo),
+                        gu.data_ptr() if keep else 0, y.data_ptr(), o, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    need = lib.cerar_gated_workspace(block, 0)
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    st = lib.cerar_gated_forward(ops._h, block, ws.data_ptr(), need, _raw(ops._index))
     if st:
         _check(st)
-    if need_dx:
-        dx = _matmul(ops, gp, ldg, False, wi[0][1], wi[0][2], False, t, d, 2 * f, torch.empty(t, d, dtype=_BF16, device=device), False)
-    if dw_in is not None:
-        _matmul(ops, gp, ldg, True, xp, ldx, False, 2 * f, d, t, dw_in, accumulate)
-    if hp is not None:
-        _matmul(ops, dyp, lddy, True, hp, ldh, False, o, f, t, dw_out, accumulate)
-    return dx
+    if x.dim() != 2:
+        y = y.view(*x.shape[:-1], o)
+    return (y, (xm, gu, activation)) if keep else y
 
 
 def gated_backward(ops: Ops, dy: torch.Tensor, kept, w_in: torch.Tensor, w_out: torch.Tensor, dw_in: torch.Tensor | None, dw_out: torch.Tensor | None, *,
@@ -449,16 +406,28 @@ def gated_backward(ops: Ops, dy: torch.Tensor, kept, w_in: torch.Tensor, w_out: 
     x, gu, activation = kept
     _here(ops, (dy, x, w_in, w_out, dw_in, dw_out), "dy x w_in w_out dw_in dw_out")
     _gated_sizes(x, w_in, w_out, activation)
+    dym, wi, wo = _bf16(_rows(dy), "dy"), _bf16(w_in, "w_in"), _bf16(w_out, "w_out")
+    (t, d), (o, f), device = x.shape, wo.shape, x.device
+    if dym.shape != (t, o):
+        raise ValueError(f"dy: {t} rows of {o} values wanted")
+    grads = []
     for what, dw, w in (("dw_in", dw_in, w_in), ("dw_out", dw_out, w_out)):
-        if dw is not None:
-            _matrix(dw, what)
-            if dw.shape != w.shape:
-                raise ValueError(f"{what} of shape {tuple(w.shape)} wanted, got {tuple(dw.shape)}")
-    dym = _rows(dy)
-    if dym.shape != (x.size(0), w_out.size(0)):
-        raise ValueError(f"dy: {x.size(0)} rows of {w_out.size(0)} values wanted")
-    dx = _gated_backward(ops, dym, kept, w_in, w_out, dw_in, dw_out, accumulate, need_dx)
-    return None if dx is None else dx.view(*dy.shape[:-1], dx.size(-1))
+        if dw is None:
+            grads += (0, 0, 0)
+            continue
+        _matrix(dw, what)
+        if dw.shape != w.shape:
+            raise ValueError(f"{what} of shape {tuple(w.shape)} wanted, got {tuple(dw.shape)}")
+        grads += (dw.data_ptr(), _stride(dw), _kind(dw, what))
+    dx = torch.empty(t, d, dtype=_BF16, device=device) if need_dx else None
+    block = _BLOCK.pack(t, d, f, o, _ACTIVATIONS[activation], bool(accumulate), x.data_ptr(), _stride(x), wi.data_ptr(), _stride(wi), wo.data_ptr(), _stride(wo),
+                        gu.data_ptr(), 0, 0, dym.data_ptr(), _stride(dym), dx.data_ptr() if need_dx else 0, d, *grads)
+    need = lib.cerar_gated_workspace(block, 1)
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    st = lib.cerar_gated_backward(ops._h, block, ws.data_ptr(), need, _raw(ops._index))
+    if st:
+        _check(st)
+    return dx if not need_dx or dy.dim() == 2 else dx.view(*dy.shape[:-1], d)
 
 
 class Gated(torch.autograd.Function):

@@ -29,8 +29,9 @@ def fake(tmp_path_factory):
     lib.fake_log.restype = lib.fake_error.restype = lib.fake_launches.restype = C.c_char_p
     lib.fake_reset.argtypes = [C.c_char_p]
     for name in ("cerar_ops_create", "cerar_ops_destroy", "cerar_ops_status", "cerar_embed", "cerar_embed_grad", "cerar_rotation_table", "cerar_head_norm",
-                 "cerar_head_norm_grad", "cerar_matmul_bf16", "cerar_align_bf16", "cerar_gated_in", "cerar_gated_grad"):
+                 "cerar_head_norm_grad", "cerar_matmul_bf16", "cerar_align_bf16", "cerar_gated_forward", "cerar_gated_backward", "cerar_gated_workspace"):
         getattr(lib, name).argtypes = getattr(cerar.lib, name).argtypes
+    lib.cerar_gated_workspace.restype = C.c_size_t
     lib.fake_reset(b"")
     return lib
 
@@ -176,38 +177,85 @@ def test_row_copies(fake, ops):
     assert fake.cerar_align_bf16(ops, None, 1, None) == ARG
 
 
+def block(**changes):
+    d = dict(tokens=10, width=40, hidden=24, outputs=32, activation=0, accumulate=0, x=P, ldx=40, w_in=P, ldw_in=40, w_out=P, ldw_out=24, kept=P, y=P, ldy=32,
+             dy=P, lddy=32, dx=P, lddx=40, dw_in=P, lddw_in=40, dw_in_type=F32, dw_out=P, lddw_out=24, dw_out_type=BF16)
+    d.update(changes)
+    return cerar.GatedBlock(**d)
+
+
 def test_gated(fake, ops):
-    #       ops x ldx w ldw tokens width hidden act h ldh kept stream
-    good = (ops, P, 40, P, 40, 10, 40, 24, 0, P, 24, P, None)
-    check(fake, fake.cerar_gated_in, good, [(1, None, ARG), (1, P + 2, ARG), (2, 36, SHAPE), (3, None, ARG), (4, 32, SHAPE), (5, -1, SHAPE), (6, -1, SHAPE), (7, -1, SHAPE), (7, 2 ** 30, SHAPE),
-                                            (8, 4, ARG), (8, -1, ARG), (9, None, ARG), (9, P + 1, ARG), (10, 23, SHAPE), (11, P + 8, ARG), (11, None, OK)], "gated_in")
-    #       ops dy lddy w ldw tokens width hidden act kept dgu lddgu h ldh stream
-    good = (ops, P, 40, P, 24, 10, 40, 24, 0, P, P, 48, P, 24, None)
-    check(fake, fake.cerar_gated_grad, good, [(1, None, ARG), (2, 36, SHAPE), (3, P + 4, ARG), (4, 20, SHAPE), (5, -1, SHAPE), (6, 0, SHAPE), (7, -1, SHAPE), (8, 9, ARG), (9, None, ARG),
-                                              (9, P + 8, ARG), (10, None, ARG), (11, 47, SHAPE), (12, P + 1, ARG), (12, None, OK), (13, 23, SHAPE)], "gated_grad")
-    host = (C.c_uint16 * 32)(*([7] * 32))
-    kept = (C.c_uint8 * 256)(*([7] * 256))
-    buf = (C.c_uint8 * 16).from_buffer(kept)
-    at = (C.addressof(buf) + 15) & -16
-    assert fake.cerar_gated_in(ops, P, 8, P, 8, 2, 0, 3, 0, C.addressof(host), 8, None, None) == OK and launched(fake) == []
-    assert [host[8 * r + c] for r in range(2) for c in range(3)] == [0] * 6 and host[3] == 7 and host[12] == 7
-    assert fake.cerar_gated_in(ops, P, 8, P, 8, 2, 0, 3, 0, C.addressof(host), 8, at, None) == OK and launched(fake) == []
-    assert sum(kept) == 7 * (256 - 36)
-    for tokens, hidden in ((0, 24), (10, 0)):
-        assert fake.cerar_gated_in(ops, P, 40, P, 40, tokens, 40, hidden, 0, None, 24, None, None) == OK and launched(fake) == []
+    def call(backward=False, ws=P, size=None, **kw):
+        b = block(**kw)
+        need = fake.cerar_gated_workspace(C.addressof(b), backward)
+        st = (fake.cerar_gated_backward if backward else fake.cerar_gated_forward)(ops, C.addressof(b), ws, need if size is None else size, None)
+        return st, launched(fake), need
+
+    def padded(rows, cols):
+        return (rows * ((cols + 7) // 8 * 8) * 2 + 255) // 256 * 256
+
+    forward, backward = ["align", "gated_in", "matmul"], ["align", "gated_grad", "matmul", "matmul", "matmul"]
+    assert call() == (OK, forward, padded(10, 24)) and call(True) == (OK, backward, padded(10, 48) + padded(10, 24))
+    # operands off 16-byte boundaries are copied, each into rows of its own
+    assert call(x=P + 2)[2] == padded(10, 24) + padded(10, 40) and call(ldw_in=41)[2] == padded(10, 24) + padded(48, 40)
+    assert call(x=P + 2, w_in=P + 2, w_out=P + 4)[2] == padded(10, 24) + padded(10, 40) + padded(48, 40) + padded(32, 24)
+    assert call(True, x=P + 2, w_in=P + 2, w_out=P + 4, dy=P + 6)[2] == padded(10, 48) + padded(10, 24) + padded(10, 40) + padded(48, 40) + padded(32, 24) + padded(10, 32)
+    assert call(tokens=1, ldx=39)[2] == padded(1, 24)                             # one row may carry any stride
+    # what is not wanted is not made, and its operands are not looked at
+    assert call(True, dw_out=None) == (OK, backward[:-1], padded(10, 48))
+    assert call(True, dx=None, w_in=None)[:2] == (OK, backward[:-1]) and call(True, dw_in=None, x=None)[:2] == (OK, backward[:-1])
+    assert call(True, dx=None, dw_in=None, dw_out=None)[:2] == (OK, backward[:2]) and call(kept=None)[:2] == (OK, forward)
+    for status, kw in ((SHAPE, dict(tokens=-1)), (SHAPE, dict(tokens=2 ** 31)), (SHAPE, dict(width=-1)), (SHAPE, dict(hidden=-1)), (SHAPE, dict(hidden=2 ** 30)),
+                       (SHAPE, dict(outputs=-1)), (ARG, dict(activation=4)), (ARG, dict(activation=-1)), (ARG, dict(x=None)), (ARG, dict(x=P + 1)), (SHAPE, dict(ldx=39)),
+                       (ARG, dict(w_in=None)), (SHAPE, dict(ldw_in=39)), (ARG, dict(w_out=P + 1)), (SHAPE, dict(ldw_out=23)), (SHAPE, dict(ldw_out=2 ** 41)),
+                       (ARG, dict(kept=P + 8))):
+        assert call(**kw) == (status, [], 0) and call(True, **kw) == (status, [], 0), kw
+    for status, kw in ((ARG, dict(y=None)), (ARG, dict(y=P + 1)), (SHAPE, dict(ldy=31))):
+        assert call(**kw) == (status, [], 0), kw
+    for status, kw in ((ARG, dict(kept=None)), (ARG, dict(dy=None)), (SHAPE, dict(lddy=31)), (ARG, dict(dx=P + 1)), (SHAPE, dict(lddx=39)), (ARG, dict(dw_in=P + 2)),
+                       (SHAPE, dict(lddw_in=39)), (ARG, dict(dw_in_type=2)), (ARG, dict(dw_out=P + 1)), (SHAPE, dict(lddw_out=23)), (ARG, dict(dw_out_type=-1))):
+        assert call(True, **kw) == (status, [], 0), kw
+    for back in (False, True):
+        good = call(back)[2]
+        assert call(back, ws=None)[:2] == (ARG, []) and call(back, ws=P + 8)[:2] == (ARG, []) and call(back, size=good - 1)[:2] == (SHAPE, [])
+    assert fake.cerar_gated_workspace(None, 0) == 0 and fake.cerar_gated_forward(ops, None, P, 10 ** 6, None) == ARG and fake.cerar_gated_backward(ops, None, P, 10 ** 6, None) == ARG
+    # nothing to do; empty sums are zero, or nothing is added
+    assert call(tokens=0)[:2] == (OK, []) and call(outputs=0)[:2] == (OK, [])
+    for back, changes in ((False, dict(hidden=0)), (True, dict(tokens=0)), (True, dict(outputs=0)), (True, dict(hidden=0))):
+        host = (C.c_uint16 * 4096)(*([7] * 4096))
+        at = C.addressof(host)
+        sizes = dict(tokens=3, width=4, hidden=2, outputs=5, ldx=8, ldw_in=8, ldw_out=8, ldy=8, lddy=8, lddx=8, lddw_in=8, lddw_out=8, dw_in_type=BF16, dw_out_type=BF16)
+        sizes.update(changes)
+        where = dict(y=at, dx=at + 1000, dw_in=at + 2000, dw_out=at + 3000)
+        assert call(back, accumulate=1, **sizes, **where)[0] == OK
+        if back:
+            assert [host[1000 + 8 * r] for r in range(2 * sizes["hidden"])] == [7] * (2 * sizes["hidden"])
+            assert call(back, **sizes, **where)[0] == OK
+            n, f = sizes["outputs"], sizes["hidden"]
+            assert [host[1000 + 8 * r + c] for r in range(2 * f) for c in range(4)] == [0] * (8 * f) and [host[1500 + 8 * r + c] for r in range(n) for c in range(f)] == [0] * (n * f)
+            assert [host[500 + 8 * r + c] for r in range(sizes["tokens"]) for c in range(4)] == [0] * (4 * sizes["tokens"])
+            assert host[1004] == 7 and host[504] == 7
+        else:
+            assert [host[8 * r + c] for r in range(3) for c in range(5)] == [0] * 15 and host[5] == 7
+        launched(fake)
+    # no inputs: g = u = 0, h = 0, y = 0; what is kept says so
+    space, kept = (C.c_uint8 * 2048)(*([7] * 2048)), (C.c_uint8 * 8192)(*([7] * 8192))
+    ws, k = (C.addressof(space) + 15) & -16, (C.addressof(kept) + 15) & -16
+    assert call(ws=ws, width=0, kept=k, hidden=3, ldw_out=8)[:2] == (OK, ["align", "matmul"])
+    assert sum(kept) == 7 * (8192 - 180) and sum(space) == 7 * (2048 - 160)
 
 
 def test_calls_that_fail_report_it_and_leave_no_error_behind(fake, ops):
     f = (C.c_double * 1)(1.0)
-    part, rot = (cerar.Heads * 1)(heads()), rotation()
+    part, rot, gated = (cerar.Heads * 1)(heads()), rotation(), block()
     calls = [lambda: fake.cerar_embed(ops, P, F32, 10, 16, 16, P, 8, 5, 1.0, P, BF16, 16, None),
              lambda: fake.cerar_embed_grad(ops, P, BF16, 16, P, 4, 5, 1.0, P, F32, 10, 16, 16, 0, P, 1024, None),
              lambda: fake.cerar_rotation_table(ops, f, 1, 0, 10, P, None),
              lambda: fake.cerar_head_norm(ops, BF16, C.addressof(part), 1, BF16, 7, 64, 1e-6, C.addressof(rot), None),
              lambda: fake.cerar_head_norm_grad(ops, BF16, C.addressof(part), 1, BF16, F32, 0, 7, 64, 1e-6, C.addressof(rot), P, 256, None),
              lambda: fake.cerar_matmul_bf16(ops, P, 72, 0, P, 72, 1, 30, 50, 70, P, F32, 50, 0, None),
-             lambda: fake.cerar_gated_in(ops, P, 40, P, 40, 10, 40, 24, 0, P, 24, P, None),
-             lambda: fake.cerar_gated_grad(ops, P, 40, P, 24, 10, 40, 24, 0, P, P, 48, P, 24, None)]
+             lambda: fake.cerar_gated_forward(ops, C.addressof(gated), P, 10 ** 6, None),
+             lambda: fake.cerar_gated_backward(ops, C.addressof(gated), P, 10 ** 6, None)]
     for call in calls:
         fake.fake_launches_reset(1)
         assert call() == CUDA and b"launch: " in fake.fake_error() and fake.fake_last() == 0
@@ -218,7 +266,7 @@ def test_the_header_declares_what_the_binding_uses():
     text = open(os.path.join(build.PKG_DIR, "..", "include", "cerar.h")).read()
     names = set(re.findall(r"\b(cerar_(?:embed|head_norm|rotation|matmul_bf16|align|gated)\w*)\s*\(", text))
     assert {"cerar_embed", "cerar_embed_grad", "cerar_embed_grad_workspace", "cerar_head_norm", "cerar_head_norm_grad", "cerar_rotation_table", "cerar_matmul_bf16",
-            "cerar_matmul_bf16_tile", "cerar_align_bf16", "cerar_gated_in", "cerar_gated_grad", "cerar_gated_kept_bytes"} <= names
+            "cerar_matmul_bf16_tile", "cerar_align_bf16", "cerar_gated_forward", "cerar_gated_backward", "cerar_gated_workspace", "cerar_gated_kept_bytes"} <= names
     for name in names:
         assert getattr(cerar.lib, name).argtypes is not None, name
 
@@ -228,7 +276,7 @@ def test_structures_are_the_headers():
     gcc = shutil.which("gcc")
     assert gcc, "gcc is needed"
     source = '#include <stdio.h>\n#include <stddef.h>\n#include "cerar.h"\nint main(void) {\n'
-    for t, cls in (("cerar_heads_t", cerar.Heads), ("cerar_rotation_t", cerar.Rotation)):
+    for t, cls in (("cerar_heads_t", cerar.Heads), ("cerar_rotation_t", cerar.Rotation), ("cerar_gated_t", cerar.GatedBlock)):
         source += f'printf("%zu ", sizeof({t}));\n' + "".join(f'printf("%zu ", offsetof({t}, {f[0]}));\n' for f in cls._fields_)
     import tempfile
     with tempfile.TemporaryDirectory() as d:
@@ -236,7 +284,7 @@ def test_structures_are_the_headers():
             f.write(source + "return 0; }\n")
         subprocess.run([gcc, "-I", os.path.join(build.PKG_DIR, "..", "include"), os.path.join(d, "a.c"), "-o", os.path.join(d, "a")], check=True)
         got = [int(v) for v in subprocess.run([os.path.join(d, "a")], capture_output=True, text=True, check=True).stdout.split()]
-    want = [v for cls in (cerar.Heads, cerar.Rotation) for v in [C.sizeof(cls)] + [getattr(cls, f[0]).offset for f in cls._fields_]]
+    want = [v for cls in (cerar.Heads, cerar.Rotation, cerar.GatedBlock) for v in [C.sizeof(cls)] + [getattr(cls, f[0]).offset for f in cls._fields_]]
     assert got == want
 
 
@@ -244,7 +292,7 @@ def test_without_a_device_calls_are_refused():
     lib = cerar.lib
     assert lib.cerar_embed(None, P, F32, 10, 16, 16, P, 8, 5, 1.0, P, BF16, 16, None) == ARG
     assert lib.cerar_matmul_bf16(None, P, 72, 0, P, 72, 1, 30, 50, 70, P, F32, 50, 0, None) == ARG
-    assert lib.cerar_gated_in(None, P, 40, P, 40, 10, 40, 24, 0, P, 24, P, None) == ARG
+    assert lib.cerar_gated_forward(None, None, P, 10 ** 6, None) == ARG
 
 
 def test_workspaces():
