@@ -159,11 +159,12 @@ cerar_status_t check_workspace(const cerar_gated_t& g, bool backward, void* work
     return CERAR_OK;
 }
 // C (+)= op(a) op(b); an empty sum is zero
-cudaError_t product(cerar_ops* o, const Mat& a, bool trans_a, const Mat& b, bool trans_b, int64_t M, int64_t N, int64_t K, void* C, int type, int64_t ldc, bool accumulate, cudaStream_t s) {
+cudaError_t product(cerar_ops* o, const Mat& a, bool trans_a, const Mat& b, bool trans_b, int64_t M, int64_t N, int64_t K, void* C, int type, int64_t ldc, bool accumulate, cudaStream_t s,
+                    bool after = false, bool followed = false) {
     if (M == 0 || N == 0) return cudaSuccess;
     if (K == 0)
         return accumulate ? cudaSuccess : cudaMemset2DAsync(C, (size_t)(M > 1 ? ldc : N) * type_bytes(type), 0, (size_t)N * type_bytes(type), (size_t)M, s);
-    return cerar::launch_matmul16({a.p, b.p, a.ld, b.ld, trans_a, trans_b, M, N, K, C, ldc, type, accumulate ? 1 : 0, o->d_status}, o->num_sms, s, &o->launches);
+    return cerar::launch_matmul16({a.p, b.p, a.ld, b.ld, trans_a, trans_b, M, N, K, C, ldc, type, accumulate ? 1 : 0, o->d_status, after ? 1 : 0, followed ? 1 : 0}, o->num_sms, s, &o->launches);
 }
 
 }  // namespace
@@ -340,9 +341,18 @@ cerar_status_t cerar_gated_backward(cerar_ops_t* o, const cerar_gated_t* g, void
     const bool reached = t > 0 && f > 0 && n > 0;                        // otherwise every sum below is empty
     if (e == cudaSuccess && reached)
         e = cerar::launch_gated_grad({b.dy.p, b.w_out.p, g->kept, b.dy.ld, b.w_out.ld, t, n, f, (int)g->activation, b.dgu.p, b.h.p, b.dgu.ld, b.h.ld, o->d_status}, o->num_sms, s, &o->launches);
-    if (e == cudaSuccess && g->dx) e = product(o, b.dgu, false, b.w_in, false, t, d, reached ? 2 * f : 0, g->dx, CERAR_TYPE_BF16, g->lddx, false, s);
-    if (e == cudaSuccess && g->dw_in) e = product(o, b.dgu, true, b.x, false, 2 * f, d, reached ? t : 0, g->dw_in, (int)g->dw_in_type, g->lddw_in, g->accumulate != 0, s);
-    if (e == cudaSuccess && g->dw_out) e = product(o, b.dy, true, b.h, false, n, f, reached ? t : 0, g->dw_out, (int)g->dw_out_type, g->lddw_out, g->accumulate != 0, s);
+    // The three products need what the one above made and not one another's results: the first waits for it, the others begin where blocks of the
+    // one in front have left.
+    bool after = false;
+    if (e == cudaSuccess && g->dw_out) {
+        e = product(o, b.dy, true, b.h, false, n, f, reached ? t : 0, g->dw_out, (int)g->dw_out_type, g->lddw_out, g->accumulate != 0, s, after, g->dx || g->dw_in);
+        after = reached;
+    }
+    if (e == cudaSuccess && g->dx) {
+        e = product(o, b.dgu, false, b.w_in, false, t, d, reached ? 2 * f : 0, g->dx, CERAR_TYPE_BF16, g->lddx, false, s, after, g->dw_in != nullptr);
+        after = after || (reached && d > 0);
+    }
+    if (e == cudaSuccess && g->dw_in) e = product(o, b.dgu, true, b.x, false, 2 * f, d, reached ? t : 0, g->dw_in, (int)g->dw_in_type, g->lddw_in, g->accumulate != 0, s, after);
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "gated block gradient launch");
 }
 

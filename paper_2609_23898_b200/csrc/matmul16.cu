@@ -69,6 +69,7 @@ struct Params {
     uint32_t a_bytes;                                  // what a load of A brings (few rows: those only; the others' sums are made of
                                                        // whatever lies there, row by row, and not stored)
     int early;                                         // 1: the next kernel of the stream may set itself up meanwhile
+    int after, followed;                               // 1: the kernel in front has nothing to do with this one; nor has the one behind
     int* status;
 };
 
@@ -542,8 +543,9 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
-    if (p.early) grid_dependents_may_launch();
-    grid_dependency_wait();
+    if (p.early && !p.followed) grid_dependents_may_launch();
+    if (!p.after) grid_dependency_wait();
+    if (p.followed) grid_dependents_may_launch();        // (behind the wait: what ran before this kernel is then complete for that one too)
 
     // a cluster is `split` blocks, or pairs of blocks (CG = 2: tiles of 256 rows), that share the sum of a tile
     const int crank = CG == 2 || p.split > 1 ? (int)cluster_rank() : 0;
@@ -558,6 +560,7 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
         if (warp == 0) {
             if (lane == 0) {
+                if (p.after) asm volatile("fence.proxy.async;" ::: "memory");
                 uint32_t s = 0, ph = 1;
                 for (uint32_t t = t0; t < p.tiles && !failed; t += tstep) {
                     int tm, tn;
@@ -715,6 +718,7 @@ matmul16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         cluster_sync();                                  // no block leaves while another reads its part or sends to it
         tc_fence_after();
     }
+    if (p.after) grid_dependency_wait();                 // this kernel's end is the end of those in front too
     leave<CG>(p, failed, warp, lane, tmem);
 }
 
@@ -766,7 +770,7 @@ template <int NT, int W, int KIND, typename C>
 __global__ void __launch_bounds__(32 * W) few_rows_kernel(const FewParams f, const Params p) {
     constexpr int H = KIND == GATE ? 2 : 1;
     __shared__ float sums[W][H][NT][32][4];
-    grid_dependents_may_launch();
+    if (!p.followed) grid_dependents_may_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
     const bf16 *b[H][2], *a[NT];
@@ -780,6 +784,7 @@ __global__ void __launch_bounds__(32 * W) few_rows_kernel(const FewParams f, con
 #pragma unroll
     for (int t = 0; t < NT; ++t) a[t] = f.A + (8 * t + g < f.M ? 8 * t + g : f.M - 1) * f.lda;
     grid_dependency_wait();
+    if (p.followed) grid_dependents_may_launch();
     float acc[H][NT][4] = {};
     for (int k0 = warp * (32 * FEW_AHEAD) + c * 8; k0 - c * 8 < f.K; k0 += 32 * W * FEW_AHEAD) {
         uint4 w[FEW_AHEAD][H][2], x[FEW_AHEAD][NT];
@@ -974,7 +979,7 @@ int matmul16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* split) {
 cudaError_t launch_matmul16(const Matmul16Args& a, int num_sms, cudaStream_t s, uint64_t* launches) {
     Params p = {};
     const int64_t size = a.type == CERAR_TYPE_F32 ? 4 : 2;
-    p.C = a.C; p.ldc = a.ldc; p.accumulate = a.accumulate;
+    p.C = a.C; p.ldc = a.ldc; p.accumulate = a.accumulate; p.after = a.after; p.followed = a.followed;
     p.c_vec = on(a.C, a.ldc, 16, size);
     p.c_pair = on(a.C, a.ldc, 4, size);
     return launch(p, PLAIN, a.type, a.A, a.lda, a.trans_a, a.B, a.ldb, a.trans_b, a.M, a.N, a.K, a.status, num_sms, s, launches);

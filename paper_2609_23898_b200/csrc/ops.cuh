@@ -169,6 +169,9 @@ struct Matmul16Args {
     int64_t ldc;
     int type, accumulate;
     int* status;
+    // after: the kernel in front is a product with `followed` that this one has nothing to do with, and what this one needs was complete before that
+    // one began; it may run beside that one's last blocks and waits for it at its own end
+    int after, followed;
 };
 cudaError_t launch_matmul16(const Matmul16Args& a, int num_sms, cudaStream_t s, uint64_t* launches);
 int matmul16_tile(int64_t M, int64_t N, int64_t K, int num_sms, int* split);
