@@ -620,7 +620,8 @@ cerar_status_t cerar_embed_grad(cerar_ops_t* ops, const void* dy, cerar_type_t t
  *     (z_a, z_b) -> (z_a cos - z_b sin, z_b cos + z_a sin)
  * pairs: j and j + rotated / 2, or 2 j and 2 j + 1 with `neighbours`; cos and sin of pair j from table[position][j].
  * Arithmetic in binary32, one rounding at the end.  Rows (dim values, next to one another) of token t and head h start at
- * x + t x_token + h x_head elements; strides may be anything, as long as rows that are written overlap neither one another nor what is read. */
+ * x + t x_token + h x_head elements; strides may be anything, as long as rows that are written overlap neither one another nor what is read,
+ * but for rows in place: y may be x (dx may be x or dy) with its strides. */
 #define CERAR_HEAD_DIM_MAX 512
 typedef struct {
     const void* x;
@@ -646,7 +647,8 @@ typedef struct {
 cerar_status_t cerar_head_norm(cerar_ops_t* ops, cerar_type_t type, const cerar_heads_t* parts, int count, cerar_type_t w_type,
                                int64_t tokens, int dim, float eps, const cerar_rotation_t* rotation, cerar_stream_t stream);
 /* Its gradient.  dz: dy turned back;  dw_j (+)= sum over rows of dz_j r x_j;  dn = w dz;  dx = r (dn - r x mean_j(dn_j r x_j)).
- * Sums over rows in binary32 in a fixed order: deterministic. */
+ * Sums over rows in binary32 in a fixed order: deterministic.  dw of both groups may be one and the same (norms that share their weights):
+ * it gets both sums. */
 size_t         cerar_head_norm_grad_workspace(int count, int dim);
 cerar_status_t cerar_head_norm_grad(cerar_ops_t* ops, cerar_type_t type, const cerar_heads_t* parts, int count, cerar_type_t w_type,
                                     cerar_type_t dw_type, int accumulate, int64_t tokens, int dim, float eps,
@@ -656,7 +658,7 @@ cerar_status_t cerar_rotation_table(cerar_ops_t* ops, const double* freqs, int p
                                     cerar_stream_t stream);
 
 /* C (M x N of `type`, ldc elements between rows) = op(A) op(B), or C + op(A) op(B) with accumulate != 0, of bfloat16 matrices; op is the
- * matrix itself or, with trans_* != 0, its transpose: A is stored as M x K (K x M), B as K x N (N x K).  A and B start on 16-byte boundaries
+ * matrix itself or, with trans_* != 0, its transpose: A is stored as M x K (K x M), B as K x N (N x K).  C overlaps neither.  A and B start on 16-byte boundaries
  * and their ld (elements between rows) is a multiple of 8: what tensor-map copies need; nothing between columns and ld is used.
  * Sums run on the tensor cores in accumulators of 24 bits that drop what does not fit, up to 4096 values of k; longer ones are put together
  * in binary32: |C - exact| <= 2^-23 (264 + K / 4096) sum |A| |B| before the rounding to `type`.  Deterministic. */

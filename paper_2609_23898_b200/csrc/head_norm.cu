@@ -28,14 +28,15 @@ using namespace ptx;
 
 constexpr int THREADS = 128;
 
-// CH elements of a row as they lie in memory (aligned to the chunk), as binary32, and back with one rounding
+// CH elements of a row as they lie in memory (aligned to the chunk), as binary32, and back with one rounding.  Plain loads, not read-only ones: a row may be
+// written where it was read (a thread writes the very places that it has read before).
 template <typename T, int CH> struct Chunk;
 template <int CH> struct Chunk<float, CH> {
     uint32_t q[CH];
     __device__ __forceinline__ void load(const float* p) {
-        if constexpr (CH == 4) *reinterpret_cast<uint4*>(q) = __ldg(reinterpret_cast<const uint4*>(p));
-        else if constexpr (CH == 2) *reinterpret_cast<uint2*>(q) = __ldg(reinterpret_cast<const uint2*>(p));
-        else q[0] = __float_as_uint(__ldg(p));
+        if constexpr (CH == 4) *reinterpret_cast<uint4*>(q) = *reinterpret_cast<const uint4*>(p);
+        else if constexpr (CH == 2) *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(p);
+        else q[0] = __float_as_uint(*p);
     }
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -53,10 +54,10 @@ template <int CH> struct Chunk<__nv_bfloat16, CH> {
     static constexpr int WORDS = CH > 1 ? CH / 2 : 1;
     uint32_t q[WORDS];
     __device__ __forceinline__ void load(const __nv_bfloat16* p) {
-        if constexpr (CH == 8) *reinterpret_cast<uint4*>(q) = __ldg(reinterpret_cast<const uint4*>(p));
-        else if constexpr (CH == 4) *reinterpret_cast<uint2*>(q) = __ldg(reinterpret_cast<const uint2*>(p));
-        else if constexpr (CH == 2) q[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
-        else q[0] = __ldg(reinterpret_cast<const unsigned short*>(p));
+        if constexpr (CH == 8) *reinterpret_cast<uint4*>(q) = *reinterpret_cast<const uint4*>(p);
+        else if constexpr (CH == 4) *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(p);
+        else if constexpr (CH == 2) q[0] = *reinterpret_cast<const uint32_t*>(p);
+        else q[0] = *reinterpret_cast<const unsigned short*>(p);
     }
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -398,7 +399,7 @@ __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormA
     }
 }
 
-// dw (+)= the blocks' shares, in their order: a block per 32 columns of a part, a warp per run of blocks.
+// dw (+)= the blocks' shares, in their order: a block per 32 columns of a part, or of both where they have one dw; a warp per run of blocks.
 constexpr int FOLD_WARPS = 32;
 __global__ void __launch_bounds__(32 * FOLD_WARPS) head_norm_fold_kernel(const HeadNormArgs p, const Work wk, int columns) {
     __shared__ float sums[FOLD_WARPS][32];
@@ -406,10 +407,10 @@ __global__ void __launch_bounds__(32 * FOLD_WARPS) head_norm_fold_kernel(const H
     const int part = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane;
     void* dw = p.part[part].dw;
     if (dw == nullptr) return;
-    const int n = columns * wk.runs[part], b0 = (int)((int64_t)n * warp / FOLD_WARPS), b1 = (int)((int64_t)n * (warp + 1) / FOLD_WARPS);
     float v = 0.f;
-    if (c < p.dim) {
-        const float* from = wk.partial + (int64_t)part * HEAD_NORM_BLOCKS * p.dim + c;
+    for (int q = part; q < (gridDim.y == 1 ? p.count : part + 1) && c < p.dim; ++q) {
+        const int n = columns * wk.runs[q], b0 = (int)((int64_t)n * warp / FOLD_WARPS), b1 = (int)((int64_t)n * (warp + 1) / FOLD_WARPS);
+        const float* from = wk.partial + (int64_t)q * HEAD_NORM_BLOCKS * p.dim + c;
 #pragma unroll 8
         for (int b = b0; b < b1; ++b) v += from[(int64_t)b * p.dim];
     }
@@ -482,7 +483,8 @@ cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int nu
         ++*launches;
     }
     if (grad && (p.part[0].dw || (p.count > 1 && p.part[1].dw))) {
-        e = launch_pdl(head_norm_fold_kernel, dim3((unsigned)((p.dim + 31) / 32), (unsigned)p.count), dim3(32 * FOLD_WARPS), 0, s, p, wk, (int)grid);
+        const bool one = p.count > 1 && p.part[0].dw == p.part[1].dw;
+        e = launch_pdl(head_norm_fold_kernel, dim3((unsigned)((p.dim + 31) / 32), one ? 1u : (unsigned)p.count), dim3(32 * FOLD_WARPS), 0, s, p, wk, (int)grid);
         if (e == cudaSuccess) ++*launches;
     }
     return e;

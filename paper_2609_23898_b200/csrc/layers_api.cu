@@ -253,6 +253,10 @@ cerar_status_t cerar_head_norm_grad(cerar_ops_t* o, cerar_type_t type, const cer
     for (int i = 0; i < count; ++i)
         if (misaligned(parts[i].w, type_bytes(w_type)) || misaligned(parts[i].dw, type_bytes(dw_type)))
             return fail(CERAR_ERR_INVALID_ARG, "w or dw is not aligned to its elements");
+    if (count > 1 && parts[0].dw && parts[1].dw && parts[0].dw != parts[1].dw) {
+        const uintptr_t q = reinterpret_cast<uintptr_t>(parts[0].dw), k = reinterpret_cast<uintptr_t>(parts[1].dw);
+        if ((q < k ? k - q : q - k) < (uintptr_t)dim * type_bytes(dw_type)) return fail(CERAR_ERR_SHAPE, "dw of the two groups overlap without being the same");
+    }
     if (!(eps > 0.f) || !std::isfinite(eps)) return fail(CERAR_ERR_INVALID_ARG, "eps must be positive and finite");
     const size_t need = cerar::head_norm_grad_workspace(count, dim);
     if (!workspace || misaligned(workspace, 16)) return fail(CERAR_ERR_INVALID_ARG, "workspace NULL or not aligned to 16 bytes");

@@ -237,7 +237,8 @@ def head_norm(ops: Ops, q: torch.Tensor, k: torch.Tensor | None, wq, wk, table: 
     """Every head of q and k (..., heads, values; k may be None) divided by its root mean square, times wq, wk (None: one), its first values turned
     by the token's position: those that `table` (rotation_table; None: no rotation) has pairs for.  positions: of every token, or of
     the last dimension of the tokens, for all sequences alike (None: 0, 1, ...); below zero: padding, whose result is zero; beyond the
-    table: the same, and Ops.status raises.  q and k may be slices of one projection's result.  Returns both (in `out`, if given)."""
+    table: the same, and Ops.status raises.  q and k may be slices of one projection's result.  Returns both (in `out`, if given: q and k
+    themselves for results in place)."""
     _here(ops, (q, k, wq, wk, table, positions), "q k wq wk table positions")
     kind, types = _kind(q, "q"), [None, None]
     yq, yk = (None, None) if out is None else out
@@ -254,8 +255,8 @@ def head_norm(ops: Ops, q: torch.Tensor, k: torch.Tensor | None, wq, wk, table: 
 
 def head_norm_backward(ops: Ops, dq: torch.Tensor, dk: torch.Tensor | None, q: torch.Tensor, k: torch.Tensor | None, wq, wk, table, positions=None, *,
                        dwq=None, dwk=None, accumulate=True, eps: float = 1e-6, pairs: str = HALVES, out=None):
-    """Gradients of q and k (in `out`, if given) from those of head_norm's results; dwq, dwk (float32 or bfloat16, None: not wanted) += those
-    of the weights.  Deterministic."""
+    """Gradients of q and k (in `out`, if given, e.g. dq and dk themselves) from those of head_norm's results; dwq, dwk (float32 or bfloat16,
+    None: not wanted; the same one where q and k share their weights) += those of the weights.  Deterministic."""
     _here(ops, (dq, dk, q, k, wq, wk, table, positions, dwq, dwk), "dq dk q k wq wk table positions dwq dwk")
     kind, types = _kind(q, "q"), [None, None]
     if (dk is None) != (k is None) or (k is None and dwk is not None):
@@ -346,7 +347,7 @@ def _operands(ops: Ops, *given):
 
 def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b=False, out: torch.Tensor | None = None,
            dtype: torch.dtype = torch.bfloat16, accumulate=False) -> torch.Tensor:
-    """op(a) op(b) of bfloat16 matrices, into `out` (float32 or bfloat16) if given, added to it with accumulate."""
+    """op(a) op(b) of bfloat16 matrices, into `out` (float32 or bfloat16, over neither of them) if given, added to it with accumulate."""
     _here(ops, (a, b, out), "a b out")
     a, b = _bf16(a, "a"), _bf16(b, "b")
     m, k = (a.size(1), a.size(0)) if trans_a else a.shape
@@ -362,7 +363,10 @@ def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b
         if tuple(out.shape) != (m, n):
             raise ValueError(f"out of shape {(m, n)} wanted, got {tuple(out.shape)}")
     (a, pa, lda), (b, pb, ldb) = _operands(ops, a, b)
-    st = lib.cerar_matmul_bf16(ops._h, pa, lda, trans_a, pb, ldb, trans_b, m, n, k, out.data_ptr(), _kind(out, "out"), _stride(out), accumulate,
+    pc = out.data_ptr()
+    if pc and (pc == pa or pc == pb):
+        raise ValueError("out lies over a or b")
+    st = lib.cerar_matmul_bf16(ops._h, pa, lda, trans_a, pb, ldb, trans_b, m, n, k, pc, _kind(out, "out"), _stride(out), accumulate,
                                _raw(ops._index))
     if st:
         _check(st)
@@ -404,10 +408,12 @@ def gated_backward(ops: Ops, dy: torch.Tensor, kept, w_in: torch.Tensor, w_out: 
     """dx from dy and what gated kept; dw_in and dw_out (float32 or bfloat16, e.g. slices of the gradient vector; None: not wanted) += the
     gradients of the weights."""
     x, gu, activation = kept
-    _here(ops, (dy, x, w_in, w_out, dw_in, dw_out), "dy x w_in w_out dw_in dw_out")
+    _here(ops, (dy, x, gu, w_in, w_out, dw_in, dw_out), "dy x kept w_in w_out dw_in dw_out")
     _gated_sizes(x, w_in, w_out, activation)
     dym, wi, wo = _bf16(_rows(dy), "dy"), _bf16(w_in, "w_in"), _bf16(w_out, "w_out")
     (t, d), (o, f), device = x.shape, wo.shape, x.device
+    if gu.numel() != lib.cerar_gated_kept_bytes(t, f):
+        raise ValueError("kept does not belong to weights of these sizes")
     if dym.shape != (t, o):
         raise ValueError(f"dy: {t} rows of {o} values wanted")
     grads = []

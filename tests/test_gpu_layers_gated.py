@@ -366,13 +366,20 @@ def test_refusals(ops):
         layers.gated(ops, x, w_in, w_out, activation="tanh")
     for error, a in ((ValueError, (dy[:9], kept, w_in, w_out, None, None)), (ValueError, (dy, kept, w_in, w_out, dw[:40], None)),
                      (ValueError, (dy, kept, w_in, w_out, dw.t(), None)), (TypeError, (dy, kept, w_in, w_out, dw.double(), None)),
-                     (TypeError, (dy.float(), kept, w_in, w_out, dw, None))):
+                     (TypeError, (dy.float(), kept, w_in, w_out, dw, None)),
+                     (ValueError, (dy, (kept[0], kept[1][:6143], kept[2]), w_in, w_out, None, None)),          # shorter than these sizes' is
+                     (ValueError, (dy, (kept[0], kept[1].cpu(), kept[2]), w_in, w_out, None, None)),
+                     (ValueError, (dy, kept, torch.zeros(128, 16, device="cuda").bfloat16(), torch.zeros(16, 64, device="cuda").bfloat16(), None, None))):
         with pytest.raises(error):
             layers.gated_backward(ops, *a)
     for error, a, kw in ((TypeError, (x.float(), w_in.t()), {}), (ValueError, (x, w_in), {}), (ValueError, (x, w_in.t()), dict(accumulate=True)),
                          (ValueError, (x, w_in.t()), dict(out=dw)), (ValueError, (x[0], w_in.t()), {}), (TypeError, (x, w_in.t()), dict(dtype=torch.float16))):
         with pytest.raises(error):
             layers.matmul(ops, *a, **kw)
+    square = torch.zeros(16, 16, device="cuda").bfloat16()
+    for a in ((square, w_in[:16].clone()), (w_in[:16].clone(), square), (square, square)):
+        with pytest.raises(ValueError):
+            layers.matmul(ops, *a, out=square)
 
 
 def test_captured_and_replayed(ops):

@@ -271,6 +271,56 @@ def test_results_in_place_of_slices(ops):
     assert torch.equal(c[0], d[0]) and torch.equal(joint[:, 4:6], d[1])
 
 
+@pytest.mark.parametrize("ty,dim,heads,pairs,layout", [("bf16", 128, 21, "halves", "joint"), ("bf16", 64, 3, "neighbours", "by head"), ("f32", 128, 9, "halves", "by head"),
+                                                       ("bf16", 70, 5, "halves", "odd"), ("f32", 30, 2, "neighbours", "odd"), ("bf16", 512, 7, "halves", "joint")])
+@pytest.mark.parametrize("tokens", [1, 333])
+def test_in_place(ops, ty, dim, heads, pairs, layout, tokens):
+    """Results where q and k, gradients where either q and k or their results' gradients were: the same bits as next to them."""
+    import torch
+    from paper_2609_23898_b200 import layers
+    q, k, w, dy, _ = inputs(tokens, heads, 2, dim, dim, ty, "f32", layout)
+    table, pos = layers.rotation_table(ops, 400, dim), torch.arange(tokens, device="cuda").flip(0)
+    pos[::5] = -1
+    want = layers.head_norm(ops, q, k, *w, table, pos, pairs=pairs)
+    grads = layers.head_norm_backward(ops, *dy, q, k, *w, table, pos, pairs=pairs)
+    over = [d.clone() for d in dy]
+    layers.head_norm_backward(ops, *over, q, k, *w, table, pos, pairs=pairs, out=over)
+    assert torch.equal(over[0], grads[0]) and torch.equal(over[1], grads[1])
+    # (a second pair with the same strides as q and k)
+    q2, k2, _, _, _ = inputs(tokens, heads, 2, dim, dim, ty, "f32", layout)
+    layers.head_norm(ops, q2, k2, *w, table, pos, pairs=pairs, out=(q2, k2))
+    assert torch.equal(q2, want[0]) and torch.equal(k2, want[1])
+    layers.head_norm_backward(ops, *dy, q, k, *w, table, pos, pairs=pairs, out=(q, k))
+    assert torch.equal(q, grads[0]) and torch.equal(k, grads[1])
+
+
+@pytest.mark.parametrize("accumulate", [True, False])
+@pytest.mark.parametrize("dty", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,hq,hk", [(1, 1, 1), (77, 6, 2), (2000, 16, 16), (50, 3, 0)])
+def test_weights_that_queries_and_keys_share(ops, tokens, hq, hk, dty, accumulate):
+    """One weight vector and one dw for both: it gets the two sums.  Terms are 0, 1 and -1 but for r, two steps of binary32 off one at most; fewer than
+    256 of them, so sums are within 256 (2^-22 + 2^-24 256) < 2^-7 of whole numbers below 256, which bfloat16 holds."""
+    import torch
+    from paper_2609_23898_b200 import cerar, layers
+    dim = 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(tokens)
+    q, k = (torch.where(torch.rand(tokens, h, dim, device="cuda", generator=g) < 0.5, -1.0, 1.0) for h in (hq, hk))
+    dq, dk = (torch.where(torch.rand(tokens, h, dim, device="cuda", generator=g) < 1 / (8 * tokens), 1.0, 0.0) for h in (hq, hk))
+    w = torch.ones(dim, device="cuda")
+    apart = [torch.full((dim,), 3.0, device="cuda") for _ in range(2)]
+    # eps so small beside 1 that r is 1
+    layers.head_norm_backward(ops, dq, dk, q, k, w, w, None, dwq=apart[0], dwk=apart[1], eps=1e-12, accumulate=accumulate)
+    start = 3.0 if accumulate else 0.0
+    dw = torch.full((dim,), 3.0, device="cuda", dtype=types()[dty])
+    layers.head_norm_backward(ops, dq, dk, q, k, w, w, None, dwq=dw, dwk=dw, eps=1e-12, accumulate=accumulate)
+    sums = [(d * x).double().sum((0, 1)) for d, x in ((dq, q), (dk, k))]
+    assert float((apart[0] - start - sums[0]).abs().max()) <= 2 ** -7 and float((dw.double() - start - sums[0] - sums[1]).abs().max()) <= 2 ** -7
+    both = torch.zeros(dim + 8, device="cuda", dtype=types()[dty])
+    with pytest.raises(cerar.CerarError):
+        layers.head_norm_backward(ops, dq, dk, q, k, w, w, None, dwq=both[:dim], dwk=both[8:], eps=1e-12)
+
+
 def test_autograd(ops):
     import torch
     from paper_2609_23898_b200 import layers

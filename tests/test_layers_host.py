@@ -134,6 +134,9 @@ def test_head_norm(fake, ops):
     assert call(tokens=0) == (OK, [])
     for status, kw in ((ARG, dict(h=heads(dy=None))), (ARG, dict(dw_type=5)), (ARG, dict(h=heads(dw=P + 2))), (ARG, dict(ws=None)), (ARG, dict(ws=P + 8)), (SHAPE, dict(size=511))):
         assert call(grad=True, **kw) == (status, []), kw
+    for gap, w_type, status in ((16, F32, SHAPE), (127, BF16, ARG), (126, BF16, SHAPE), (128, BF16, OK), (128, F32, SHAPE), (256, F32, OK)):        # dw of both groups
+        for a, b in ((P, P + gap), (P + gap, P)):
+            assert call(grad=True, h=heads(dw=a), second=heads(dw=b), dw_type=w_type)[0] == status, (gap, w_type)
     assert fake.cerar_head_norm(ops, BF16, None, 1, BF16, 1, 64, 1e-6, C.addressof(rotation()), None) == ARG
     assert fake.cerar_head_norm(ops, BF16, C.addressof((cerar.Heads * 1)(heads())), 1, BF16, 1, 64, 1e-6, None, None) == ARG
 
