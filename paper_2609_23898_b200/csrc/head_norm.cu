@@ -15,6 +15,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "kernels.cuh"
 #include "ops.cuh"
 #include "packed.cuh"
@@ -399,6 +401,188 @@ __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormA
     }
 }
 
+// The same for bfloat16 in whole 16-byte chunks, one to a thread's half.  Rows, and a token's part of the table, are on their way in shared memory, in
+// slots of the thread's own (nothing has to be waited for but its own copies): AHEAD heads of the block's sequence of tokens and heads, over the
+// ends of tokens, and no register holds them.  16384 x 40 x 128 in 87 us, 5.9 TB/s (two heads of one token ahead in registers, and the table's latency
+// at each token: 102; one or three heads here 99 and 86, 4096 x 20 x 256 with one to three 35, 32, 33; four blocks per SM in one turn, eight in
+// two: 90).  Copies go through L1, or the halves of a 32-byte piece come from L2 twice (neighbours: 144).  binary32 has twice the bytes per
+// instruction and is slower this way (168 -> 196).
+constexpr int AHEAD = 2, SLOTS = AHEAD + 1, AHEAD_BLOCKS = 4;
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void shared16(uint32_t from, uint32_t* q) {
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "r"(from) : "memory");
+}
+constexpr int PIECE = 16 * THREADS;                              // 16 bytes of every thread
+constexpr int TURN = 4;                                          // pieces of a chunk's eight pairs (cos, sin)
+constexpr int RING_BYTES = (SLOTS * 4 + 2 * TURN) * PIECE;
+
+template <bool NEIGHBOURS>
+__global__ void __launch_bounds__(THREADS, AHEAD_BLOCKS) head_norm_grad_ahead_kernel(const HeadNormArgs p, const Work wk) {
+    using T = __nv_bfloat16;
+    constexpr int CH = 8;
+    extern __shared__ __align__(16) float sums[];                // the ring; in the end [groups of the block][dim]: their shares of dw
+    grid_dependency_wait();
+    const uint32_t column = blockIdx.x / wk.rows, columns = gridDim.x / wk.rows;
+    const int row = (int)(blockIdx.x - column * wk.rows), part = row < wk.runs[0] ? 0 : 1;
+    const HeadPart& h = p.part[part];
+    const int lanes = 1 << wk.log_lanes, lane = threadIdx.x & (lanes - 1), per_block = THREADS >> wk.log_lanes;
+    const int run = row - (part ? wk.runs[0] : 0), first = run * wk.run, len = (first + wk.run < h.heads ? first + wk.run : h.heads) - first;
+    const bool mine = lane < wk.chunks;
+    const Place at = place(p, mine ? lane : 0, CH);
+    uint64_t w[CH], dw[CH];
+    {
+        float f[2 * CH];
+        weights<CH>(p, h.w, at, wk.w_vec, f);
+#pragma unroll
+        for (int m = 0; m < CH; ++m) {
+            w[m] = two_of(f[2 * m], f[2 * m + 1]);
+            dw[m] = 0ull;
+        }
+    }
+    const float inv_dim = 1.f / (float)p.dim;
+    const int64_t t0 = (int64_t)column * per_block, step = (int64_t)columns * per_block;
+    const int64_t items = t0 < p.tokens ? (p.tokens - t0 + step - 1) / step * len : 0;       // the same for the whole block
+    const int dist = len < AHEAD ? len : AHEAD;                  // (no further than into the next token)
+    const uint32_t own = smem_u32(sums) + 16 * threadIdx.x, turns = own + SLOTS * 4 * PIECE;
+
+    // what is brought next: token it, its head ih; positions of that token and the one behind it
+    int64_t it = t0 + (threadIdx.x >> wk.log_lanes), left = items;
+    int64_t pos_in = -1, pos_next = it < p.tokens ? position_of(p, (uint32_t)it) : -1;
+    int ih = 0, slot_in = 0, turn_in = 0;
+    const T *x = nullptr, *dy = nullptr;
+    auto bring = [&]() {
+        if (left > 0) {
+            --left;
+            if (ih == 0) {
+                pos_in = pos_next;
+                if (pos_in >= 0 && mine && at.turned) {
+                    const float2* from = p.table + pos_in * (p.rotated / 2) + at.pair;
+#pragma unroll
+                    for (int i = 0; i < TURN; ++i) copy16(turns + (turn_in * TURN + i) * PIECE, from + 2 * i);
+                }
+                turn_in ^= 1;
+                x = static_cast<const T*>(h.x) + it * h.x_token + first * h.x_head;
+                dy = static_cast<const T*>(h.dy) + it * h.dy_token + first * h.dy_head;
+                it += step;
+                pos_next = it < p.tokens ? position_of(p, (uint32_t)it) : -1;
+            }
+            if (pos_in >= 0 && mine) {
+                const uint32_t to = own + slot_in * 4 * PIECE;
+                copy16(to, x + at.a);
+                copy16(to + PIECE, x + at.b);
+                copy16(to + 2 * PIECE, dy + at.a);
+                copy16(to + 3 * PIECE, dy + at.b);
+            }
+            x += h.x_head;
+            dy += h.dy_head;
+            slot_in = slot_in + 1 == SLOTS ? 0 : slot_in + 1;
+            if (++ih == len) ih = 0;
+        }
+        copies_done();
+    };
+    for (int i = 0; i < dist; ++i) bring();
+
+    int64_t pos = -1, t = t0 + (threadIdx.x >> wk.log_lanes);
+    int head = 0, slot = 0, turn = 0;
+    T* dx = nullptr;
+    uint64_t vc[CH], vs[CH];
+    for (int64_t k = 0; k < items; ++k) {
+        if (dist == AHEAD) copies_wait<AHEAD - 1>();
+        else copies_wait<0>();
+        if (head == 0) {
+            pos = pos_in;                                        // (what is on its way is of this token as yet)
+            dx = static_cast<T*>(h.y) + t * h.y_token + first * h.y_head;
+            t += step;
+            float q[2 * CH];                                     // cosine and sine of each pair
+#pragma unroll
+            for (int i = 0; i < CH; ++i) { q[2 * i] = 1.f; q[2 * i + 1] = 0.f; }
+            if (pos >= 0 && mine && at.turned)
+#pragma unroll
+                for (int i = 0; i < TURN; ++i) shared16(turns + (turn * TURN + i) * PIECE, reinterpret_cast<uint32_t*>(q) + 4 * i);
+            turn ^= 1;
+            float c[2 * CH], s[2 * CH];
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int f = NEIGHBOURS ? 2 * i : i, g = NEIGHBOURS ? 2 * i + 1 : CH + i;
+                c[f] = c[g] = q[2 * i];
+                s[f] = q[2 * i + 1];
+                s[g] = -q[2 * i + 1];
+            }
+#pragma unroll
+            for (int m = 0; m < CH; ++m) {
+                vc[m] = two_of(c[2 * m], c[2 * m + 1]);
+                vs[m] = two_of(s[2 * m], s[2 * m + 1]);
+            }
+        }
+        Raw<T, CH, 1> rx, ry;
+        rx.clear();                                              // (padding may hold anything)
+        ry.clear();
+        if (pos >= 0 && mine) {
+            const uint32_t from = own + slot * 4 * PIECE;
+            shared16(from, rx.a[0].q);
+            shared16(from + PIECE, rx.b[0].q);
+            shared16(from + 2 * PIECE, ry.a[0].q);
+            shared16(from + 3 * PIECE, ry.b[0].q);
+        }
+        slot = slot + 1 == SLOTS ? 0 : slot + 1;
+        bring();                                                 // into the slot of the head before this one
+        uint64_t v[1][CH], dz[CH], square2 = 0ull, dot2 = 0ull;
+        rx.take(v);
+        {
+            uint64_t g[1][CH];
+            ry.take(g);
+#pragma unroll
+            for (int m = 0; m < CH; ++m) dz[m] = mad2(g[0][m], vc[m], mul2(partner<CH, NEIGHBOURS>(g[0], m), vs[m]));
+        }
+#pragma unroll
+        for (int m = 0; m < CH; ++m) {
+            square2 = mad2(v[0][m], v[0][m], square2);
+            dot2 = mad2(mul2(w[m], dz[m]), v[0][m], dot2);
+        }
+        float square, dot, other;
+        parts(square2, square, other);
+        square += other;
+        parts(dot2, dot, other);
+        dot += other;
+        for (int o = lanes >> 1; o; o >>= 1) {
+            square += __shfl_xor_sync(0xffffffffu, square, o);
+            dot += __shfl_xor_sync(0xffffffffu, dot, o);
+        }
+        const float r = rsqrtf(fmaf(square, inv_dim, p.eps));
+        const uint64_t r2 = all(r), back = all(-(dot * inv_dim) * r * r * r);
+        uint64_t u[CH];
+#pragma unroll
+        for (int m = 0; m < CH; ++m) {
+            const uint64_t rz = mul2(r2, dz[m]);
+            dw[m] = mad2(rz, v[0][m], dw[m]);
+            u[m] = mad2(v[0][m], back, mul2(rz, w[m]));
+        }
+        if (mine && t - step < p.tokens) store_pairs<T, CH>(dx, at, u);
+        dx += h.y_head;
+        if (++head == len) head = 0;
+    }
+    if (h.dw == nullptr) return;                                 // (the same for the whole block)
+    __syncthreads();                                             // (nothing is on its way to the ring: all of it has been waited for)
+    float* share = sums + (threadIdx.x >> wk.log_lanes) * p.dim;
+    if (mine)
+#pragma unroll
+        for (int m = 0; m < CH; ++m) {
+            float f[2];
+            parts(dw[m], f[0], f[1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) share[2 * m + i < CH ? at.a + 2 * m + i : at.b + 2 * m + i - CH] = f[i];
+        }
+    __syncthreads();
+    float* out = wk.partial + ((int64_t)part * HEAD_NORM_BLOCKS + (int64_t)run * columns + column) * p.dim;
+    for (int c = threadIdx.x; c < p.dim; c += THREADS) {
+        float v = 0.f;
+        for (int g = 0; g < per_block; ++g) v += sums[g * p.dim + c];
+        out[c] = v;
+    }
+}
+
 // dw (+)= the blocks' shares, in their order: a block per 32 columns of a part, or of both where they have one dw; a warp per run of blocks.
 constexpr int FOLD_WARPS = 32;
 __global__ void __launch_bounds__(32 * FOLD_WARPS) head_norm_fold_kernel(const HeadNormArgs p, const Work wk, int columns) {
@@ -432,6 +616,7 @@ int chunk_of(const HeadNormArgs& p, int64_t size, bool grad) {
     for (int ch = (int)(16 / size); ch > 1; ch /= 2) {
         const int64_t bytes = ch * size;
         bool ok = (p.rotated / 2) % ch == 0 && (p.dim / 2) % ch == 0;
+        if (grad && ch == 8 && p.rotated > 0) ok = ok && reinterpret_cast<uintptr_t>(p.table) % 16 == 0;      // (read in such pieces)
         for (int i = 0; i < p.count && ok; ++i) {
             const HeadPart& h = p.part[i];
             auto fits = [&](const void* q, int64_t token, int64_t head) {
@@ -449,6 +634,7 @@ template <typename T, int CH, int NCH, int DEPTH, bool NEIGHBOURS>
 cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int num_sms, cudaStream_t s, uint64_t* launches) {
     Work wk = {};
     wk.chunks = (p.dim / 2 + CH - 1) / CH;
+    constexpr bool ahead = std::is_same<T, __nv_bfloat16>::value && CH == 8;      // (the gradient)
     while (((int64_t)NCH << wk.log_lanes) < wk.chunks) ++wk.log_lanes;
     const int per_block = THREADS >> wk.log_lanes;
     const int64_t columns = (p.tokens + per_block - 1) / per_block;
@@ -463,12 +649,12 @@ cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int nu
         return wk.runs[0] + wk.runs[1];
     };
     int rows = count(2);
-    if (columns * rows >= 4 * num_sms || rows > 256) rows = count(DEPTH > 4 ? 16 : 8);
+    if (columns * rows >= 4 * num_sms || rows > 256) rows = count(DEPTH > 4 && !grad ? 16 : 8);
     while (rows > (grad ? 256 : 65536)) rows = count(2 * wk.run);
     wk.partial = partial;
     int64_t grid = columns;
     if (grad) {
-        const int64_t most = (int64_t)num_sms * 6 / (rows > 0 ? rows : 1), kept = HEAD_NORM_BLOCKS / (wk.runs[0] > wk.runs[1] ? wk.runs[0] : wk.runs[1] > 0 ? wk.runs[1] : 1);
+        const int64_t most = (int64_t)num_sms * (ahead ? AHEAD_BLOCKS : 6) / (rows > 0 ? rows : 1), kept = HEAD_NORM_BLOCKS / (wk.runs[0] > wk.runs[1] ? wk.runs[0] : wk.runs[1] > 0 ? wk.runs[1] : 1);
         if (grid > most) grid = most < 1 ? 1 : most;
         if (grid > kept) grid = kept;
     }
@@ -478,7 +664,8 @@ cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int nu
         wk.rows = rows;
         const dim3 blocks((unsigned)(grid * rows));
         if (!grad) e = launch_pdl(head_norm_kernel<T, CH, NCH, DEPTH, NEIGHBOURS>, blocks, dim3(THREADS), 0, s, p, wk);
-        else if constexpr (DEPTH <= 2) e = launch_pdl(head_norm_grad_kernel<T, CH, NCH, DEPTH, NEIGHBOURS>, blocks, dim3(THREADS), (size_t)per_block * p.dim * 4, s, p, wk);
+        else if constexpr (ahead) e = launch_pdl(head_norm_grad_ahead_kernel<NEIGHBOURS>, blocks, dim3(THREADS), (size_t)RING_BYTES, s, p, wk);
+        else e = launch_pdl(head_norm_grad_kernel<T, CH, NCH, DEPTH, NEIGHBOURS>, blocks, dim3(THREADS), (size_t)per_block * p.dim * 4, s, p, wk);
         if (e != cudaSuccess) return e;
         ++*launches;
     }
@@ -498,7 +685,7 @@ cudaError_t launch_pairs(const HeadNormArgs& p, bool grad, float* partial, int n
 
 // Chunks of 16 bytes go with one or two per thread (half a row is at most 256 values); shorter ones with more, so that a row still fits a warp.
 // Heads on their way: as many as registers hold (16384 x 40 x 128 in us, forward bfloat16 with 1, 2, 4, 6, 8: 67, 71, 61, 56, 62; binary32 with
-// 1, 2: 120, 107; gradient bfloat16 with 1, 2: 104, 102, binary32 200, 167).
+// 1, 2: 120, 107; gradient binary32 200, 167; bfloat16's with 8 values per chunk has its own way).
 cudaError_t launch(const HeadNormArgs& p, bool grad, float* partial, int num_sms, cudaStream_t s, uint64_t* launches) {
     if (p.type == CERAR_TYPE_F32) {
         switch (chunk_of(p, 4, grad)) {
@@ -508,7 +695,7 @@ cudaError_t launch(const HeadNormArgs& p, bool grad, float* partial, int num_sms
         }
     }
     switch (chunk_of(p, 2, grad)) {
-        case 8: return grad ? launch_pairs<__nv_bfloat16, 8, 1, 2>(p, grad, partial, num_sms, s, launches) : launch_pairs<__nv_bfloat16, 8, 1, 6>(p, grad, partial, num_sms, s, launches);
+        case 8: return launch_pairs<__nv_bfloat16, 8, 1, 6>(p, grad, partial, num_sms, s, launches);
         case 4: return launch_pairs<__nv_bfloat16, 4, 2, 1>(p, grad, partial, num_sms, s, launches);
         case 2: return launch_pairs<__nv_bfloat16, 2, 4, 1>(p, grad, partial, num_sms, s, launches);
         default: return launch_pairs<__nv_bfloat16, 1, 8, 1>(p, grad, partial, num_sms, s, launches);

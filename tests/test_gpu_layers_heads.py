@@ -96,6 +96,7 @@ CASES = [  # tokens, query heads, key heads, dim, rotated, pairs, type, weights'
     (40, 2, 2, 96, 32, "neighbours", "bf16", "f32"), (19, 3, 1, 256, 256, "halves", "bf16", None), (9, 2, 1, 512, 512, "neighbours", "f32", "bf16"),
     (21, 2, 3, 512, 128, "halves", "bf16", "bf16"), (50, 3, 2, 34, 34, "halves", "bf16", "bf16"), (31, 1, 2, 6, 2, "neighbours", "f32", "f32"),
     (64, 2, 1, 26, 26, "halves", "bf16", "f32"), (11, 9, 4, 128, 0, "halves", "bf16", "bf16"), (700, 8, 2, 16, 16, "halves", "bf16", "bf16"),
+    (6000, 9, 1, 64, 64, "halves", "bf16", "bf16"), (3000, 1, 3, 128, 96, "neighbours", "bf16", "f32"), (1200, 10, 2, 512, 512, "halves", "bf16", None),
     (3, 2, 2, 510, 254, "halves", "f32", "f32"), (2500, 12, 4, 128, 128, "halves", "f32", "f32"), (2500, 32, 8, 128, 64, "halves", "bf16", "bf16"),
 ]
 
@@ -269,6 +270,28 @@ def test_results_in_place_of_slices(ops):
     c = layers.head_norm(ops, q, k, None, None, table, out=(joint[:, :4], joint[:, 4:6]))
     d = layers.head_norm(ops, q, k, None, None, table)
     assert torch.equal(c[0], d[0]) and torch.equal(joint[:, 4:6], d[1])
+
+
+@pytest.mark.parametrize("pairs", ["halves", "neighbours"])
+def test_table_on_any_boundary(ops, pairs):
+    """A table that begins 8 bytes behind a boundary gives what one on it gives."""
+    import torch
+    from paper_2609_23898_b200 import layers
+    q, k, w, dy, _ = inputs(300, 6, 2, 128, 128, "bf16", "bf16", "joint")
+    table = layers.rotation_table(ops, 300, 128)
+    off = torch.empty(table.numel() + 2, device="cuda")[2:].view_as(table).copy_(table)
+    assert off.data_ptr() % 16 == 8
+    for t in (table, off):
+        dw = [torch.zeros(128, device="cuda") for _ in range(2)]
+        got = [*layers.head_norm(ops, q, k, *w, t, pairs=pairs), *layers.head_norm_backward(ops, *dy, q, k, *w, t, dwq=dw[0], dwk=dw[1], pairs=pairs), *dw]
+        if t is table:
+            want = got
+    pos = torch.arange(300, device="cuda")
+    for x, wi, d, a, dwb in zip((q, k), w, dy, got[2:4], got[4:]):
+        exact_dx, size, exact_dw, dws = exact_grad(d, x, wi, table, pos, pairs, 1e-6)
+        near(a, exact_dx, size, 2 * 128 + 24)
+        near(dwb, exact_dw, dws, 300 * x.size(1) + 64 + 12)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 @pytest.mark.parametrize("ty,dim,heads,pairs,layout", [("bf16", 128, 21, "halves", "joint"), ("bf16", 64, 3, "neighbours", "by head"), ("f32", 128, 9, "halves", "by head"),
