@@ -770,7 +770,7 @@ template <int NT, int W, int KIND, typename C>
 __global__ void __launch_bounds__(32 * W) few_rows_kernel(const FewParams f, const Params p) {
     constexpr int H = KIND == GATE ? 2 : 1;
     __shared__ float sums[W][H][NT][32][4];
-    if (!p.followed) grid_dependents_may_launch();
+    grid_dependents_may_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
     const bf16 *b[H][2], *a[NT];
@@ -784,7 +784,6 @@ __global__ void __launch_bounds__(32 * W) few_rows_kernel(const FewParams f, con
 #pragma unroll
     for (int t = 0; t < NT; ++t) a[t] = f.A + (8 * t + g < f.M ? 8 * t + g : f.M - 1) * f.lda;
     grid_dependency_wait();
-    if (p.followed) grid_dependents_may_launch();
     float acc[H][NT][4] = {};
     for (int k0 = warp * (32 * FEW_AHEAD) + c * 8; k0 - c * 8 < f.K; k0 += 32 * W * FEW_AHEAD) {
         uint4 w[FEW_AHEAD][H][2], x[FEW_AHEAD][NT];
@@ -928,7 +927,8 @@ bool on(const void* p, int64_t ld, int64_t bytes, int64_t size) { return reinter
 // p: the output's part is filled in.  N: columns of the accumulators all tiles together (GATE: twice those of h).
 cudaError_t launch(Params p, int kind, int type, const void* A, int64_t lda, bool trans_a, const void* B, int64_t ldb, bool trans_b, int64_t M, int64_t N, int64_t K,
                    int* status, int num_sms, cudaStream_t s, uint64_t* launches) {
-    if (kind != GRAD && !trans_a && trans_b && M <= FEW_ROWS && K <= FEW_TERMS && N * K * 2 <= FEW_BYTES) {
+    // (the blocks of few rows let the next kernel in before they wait: not where one follows that relies on their wait)
+    if (kind != GRAD && !p.followed && !trans_a && trans_b && M <= FEW_ROWS && K <= FEW_TERMS && N * K * 2 <= FEW_BYTES) {
         const FewParams f = {static_cast<const bf16*>(A), static_cast<const bf16*>(B), lda, ldb, (int)M, (int)K, kind == GATE ? N / 2 : N};
         const cudaError_t e = kind == GATE ? launch_few_rows<GATE, bf16>(f, p, num_sms, s) : type == CERAR_TYPE_F32 ? launch_few_rows<PLAIN, float>(f, p, num_sms, s)
                                                                                              : launch_few_rows<PLAIN, bf16>(f, p, num_sms, s);

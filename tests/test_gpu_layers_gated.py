@@ -382,6 +382,39 @@ def test_refusals(ops):
             layers.matmul(ops, *a, out=square)
 
 
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("t,d,f", [(64, 256, 512), (333, 520, 1377), (2, 64, 96), (512, 1024, 1024), (700, 96, 2000), (40, 2048, 64)])
+def test_passes_one_behind_the_other(ops, t, d, f, captured):
+    """Many passes without a pause, whose workspaces lie where those before them had theirs, give what each gives alone: kernels that begin early
+    neither read what is not there yet nor write what is still read."""
+    import torch
+    from paper_2609_23898_b200 import layers
+    cases = [weights(t, d, f, d, seed=s) for s in range(12)]
+
+    def run(case):
+        x, w_in, w_out, dy = case
+        y, kept = layers.gated(ops, x, w_in, w_out, keep=True)
+        dw = torch.ones_like(w_in, dtype=torch.float32), torch.ones_like(w_out, dtype=torch.float32)
+        return y, layers.gated_backward(ops, dy, kept, w_in, w_out, *dw), *dw
+
+    want = []
+    for case in cases:
+        want.append(run(case))
+        torch.cuda.synchronize()
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = [run(case) for case in cases]
+        for _ in range(3):
+            graph.replay()
+    else:
+        got = [run(case) for case in cases]
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+    ops.status()
+
+
 def test_captured_and_replayed(ops):
     import torch
     from paper_2609_23898_b200 import layers
