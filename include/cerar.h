@@ -686,7 +686,9 @@ cerar_status_t cerar_align_bf16(cerar_ops_t* ops, const cerar_rows_t* items, int
  * h, dg and du are bfloat16 in memory, as the operands of the products that follow have to be; each is rounded once.  Where `kept` is
  * not NULL, cerar_gated_forward leaves there g and u for the backward pass, in 24 bits each (2^-16 of themselves off):
  * cerar_gated_kept_bytes bytes on a 16-byte boundary, in a layout of its own; h is made from them again.
- * The sums of g, u and dh are within 2^-23 (8 + K / 16) of the sum of their terms' magnitudes, the others' as cerar_matmul_bf16's. */
+ * The sums of g, u and dh are within 2^-23 (8 + K / 16) of the sum of their terms' magnitudes, the others' as cerar_matmul_bf16's.
+ * y may lie over x, and dx over dy (the products that may run beside one another then follow one another); otherwise what is written overlaps neither
+ * anything else that is written nor an operand. */
 typedef enum {
     CERAR_ACT_SILU = 0,          /* g / (1 + e^-g)                                                        */
     CERAR_ACT_GELU = 1,          /* g Phi(g), Phi the normal distribution                                 */

@@ -167,6 +167,31 @@ cudaError_t product(cerar_ops* o, const Mat& a, bool trans_a, const Mat& b, bool
     return cerar::launch_matmul16({a.p, b.p, a.ld, b.ld, trans_a, trans_b, M, N, K, C, ldc, type, accumulate ? 1 : 0, o->d_status, after ? 1 : 0, followed ? 1 : 0}, o->num_sms, s, &o->launches);
 }
 
+// Memory from the first to behind the last element of a matrix (above zero rows and columns)
+struct Span {
+    uintptr_t from, to;
+};
+Span span_of(const void* p, int64_t rows, int64_t cols, int64_t ld, int size) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    return {at, at + (uintptr_t)(((rows - 1) * ld + cols) * size)};
+}
+Span span_of(const Mat& m, int64_t rows, int64_t cols) { return span_of(m.p, rows, cols, m.ld, 2); }
+// Products that run beside one another: since the last one that waited, what each writes and what it reads.
+struct Beside {
+    struct { Span out, a, b; } running[3];
+    int count = 0;
+    // Whether the next product may begin beside them.  Where it may not it waits for the one in front, which ends after those in front of it.
+    bool add(const Span& out, const Span& a, const Span& b) {
+        auto meet = [](const Span& x, const Span& y) { return x.from < y.to && y.from < x.to; };
+        bool free = count > 0;
+        for (int i = 0; i < count; ++i)
+            if (meet(out, running[i].out) || meet(out, running[i].a) || meet(out, running[i].b) || meet(a, running[i].out) || meet(b, running[i].out)) free = false;
+        if (!free) count = 0;
+        running[count++] = {out, a, b};
+        return free;
+    }
+};
+
 }  // namespace
 
 extern "C" {
@@ -346,17 +371,20 @@ cerar_status_t cerar_gated_backward(cerar_ops_t* o, const cerar_gated_t* g, void
     if (e == cudaSuccess && reached)
         e = cerar::launch_gated_grad({b.dy.p, b.w_out.p, g->kept, b.dy.ld, b.w_out.ld, t, n, f, (int)g->activation, b.dgu.p, b.h.p, b.dgu.ld, b.h.ld, o->d_status}, o->num_sms, s, &o->launches);
     // The three products need what the one above made and not one another's results: the first waits for it, the others begin where blocks of the
-    // one in front have left.
-    bool after = false;
+    // one in front have left, unless a result lies over what those in front read or write (dx over dy).
+    Beside beside;
     if (e == cudaSuccess && g->dw_out) {
-        e = product(o, b.dy, true, b.h, false, n, f, reached ? t : 0, g->dw_out, (int)g->dw_out_type, g->lddw_out, g->accumulate != 0, s, after, g->dx || g->dw_in);
-        after = reached;
+        const bool early = reached && beside.add(span_of(g->dw_out, n, f, g->lddw_out, type_bytes((int)g->dw_out_type)), span_of(b.dy, t, n), span_of(b.h, t, f));
+        e = product(o, b.dy, true, b.h, false, n, f, reached ? t : 0, g->dw_out, (int)g->dw_out_type, g->lddw_out, g->accumulate != 0, s, early, g->dx || g->dw_in);
     }
     if (e == cudaSuccess && g->dx) {
-        e = product(o, b.dgu, false, b.w_in, false, t, d, reached ? 2 * f : 0, g->dx, CERAR_TYPE_BF16, g->lddx, false, s, after, g->dw_in != nullptr);
-        after = after || (reached && d > 0);
+        const bool early = reached && d > 0 && beside.add(span_of(g->dx, t, d, g->lddx, 2), span_of(b.dgu, t, 2 * f), span_of(b.w_in, 2 * f, d));
+        e = product(o, b.dgu, false, b.w_in, false, t, d, reached ? 2 * f : 0, g->dx, CERAR_TYPE_BF16, g->lddx, false, s, early, g->dw_in != nullptr);
     }
-    if (e == cudaSuccess && g->dw_in) e = product(o, b.dgu, true, b.x, false, 2 * f, d, reached ? t : 0, g->dw_in, (int)g->dw_in_type, g->lddw_in, g->accumulate != 0, s, after);
+    if (e == cudaSuccess && g->dw_in) {
+        const bool early = reached && d > 0 && beside.add(span_of(g->dw_in, 2 * f, d, g->lddw_in, type_bytes((int)g->dw_in_type)), span_of(b.dgu, t, 2 * f), span_of(b.x, t, d));
+        e = product(o, b.dgu, true, b.x, false, 2 * f, d, reached ? t : 0, g->dw_in, (int)g->dw_in_type, g->lddw_in, g->accumulate != 0, s, early);
+    }
     return e == cudaSuccess ? CERAR_OK : cuda_fail(e, "gated block gradient launch");
 }
 
