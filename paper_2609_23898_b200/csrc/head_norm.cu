@@ -139,8 +139,11 @@ template <typename T, int CH, int NCH> struct Raw {
         }
     }
 };
+// What values m are turned with: zero where they are not turned, or zero times an infinite neighbour would be NaN.
 template <int CH, bool NEIGHBOURS>
-__device__ __forceinline__ uint64_t partner(const uint64_t* v, int m) { return NEIGHBOURS || CH == 1 ? swapped(v[m]) : v[(m + CH / 2) % CH]; }
+__device__ __forceinline__ uint64_t partner(const uint64_t* v, int m, bool turned) {
+    return !turned ? 0ull : NEIGHBOURS || CH == 1 ? swapped(v[m]) : v[(m + CH / 2) % CH];
+}
 template <typename T, int CH>
 __device__ __forceinline__ void store_pairs(T* row, const Place& at, const uint64_t* v) {
     float f[2 * CH];
@@ -192,9 +195,10 @@ __device__ __forceinline__ void weights(const HeadNormArgs& p, const void* w, co
     }
 }
 
-// NCH: chunks per thread.  DEPTH: heads whose loads are on their way.  NEIGHBOURS: which values are a pair.
+// NCH: chunks per thread.  DEPTH: heads whose loads are on their way.  NEIGHBOURS: which values are a pair.  WHOLE: all of them are turned (as a value of the launch it costs
+// 16384 x 40 x 128 in bfloat16 56.6 -> 57.7 us).
 // A block: a run of heads (the faster index, so that whole tokens are read at a time) of some tokens.  Threads without a token (a chunk) stay, with zeros: they share their warp's sums.
-template <typename T, int CH, int NCH, int DEPTH, bool NEIGHBOURS>
+template <typename T, int CH, int NCH, int DEPTH, bool NEIGHBOURS, bool WHOLE>
 __global__ void __launch_bounds__(THREADS) head_norm_kernel(const HeadNormArgs p, const Work wk) {
     grid_dependency_wait();
     const uint32_t column = blockIdx.x / wk.rows;
@@ -235,7 +239,7 @@ __global__ void __launch_bounds__(THREADS) head_norm_kernel(const HeadNormArgs p
 #pragma unroll
         for (int m = 0; m < CH; ++m) {
             vc[j][m] = mul2(pw[m], two_of(c[2 * m], c[2 * m + 1]));
-            vs[j][m] = mul2(partner<CH, NEIGHBOURS>(pw, m), two_of(s[2 * m], s[2 * m + 1]));
+            vs[j][m] = mul2(partner<CH, NEIGHBOURS>(pw, m, WHOLE || at[j].turned), two_of(s[2 * m], s[2 * m + 1]));
         }
     }
     const float inv_dim = 1.f / (float)p.dim;
@@ -261,14 +265,14 @@ __global__ void __launch_bounds__(THREADS) head_norm_kernel(const HeadNormArgs p
             for (int j = 0; j < NCH; ++j) {
                 uint64_t z[CH];
 #pragma unroll
-                for (int m = 0; m < CH; ++m) z[m] = mul2(r, mad2(v[j][m], vc[j][m], mul2(partner<CH, NEIGHBOURS>(v[j], m), vs[j][m])));
+                for (int m = 0; m < CH; ++m) z[m] = mul2(r, mad2(v[j][m], vc[j][m], mul2(partner<CH, NEIGHBOURS>(v[j], m, WHOLE || at[j].turned), vs[j][m])));
                 if (mine[j]) store_pairs<T, CH>(y, at[j], z);
             }
             y += h.y_head;
         }
 }
 
-template <typename T, int CH, int NCH, int DEPTH, bool NEIGHBOURS>
+template <typename T, int CH, int NCH, int DEPTH, bool NEIGHBOURS, bool WHOLE>
 __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormArgs p, const Work wk) {
     extern __shared__ float sums[];                              // [groups of the block][dim]: their shares of dw
     grid_dependency_wait();
@@ -346,7 +350,7 @@ __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormA
 #pragma unroll
                     for (int j = 0; j < NCH; ++j)
 #pragma unroll
-                        for (int m = 0; m < CH; ++m) dz[j][m] = mad2(g[j][m], vc[j][m], mul2(partner<CH, NEIGHBOURS>(g[j], m), vs[j][m]));
+                        for (int m = 0; m < CH; ++m) dz[j][m] = mad2(g[j][m], vc[j][m], mul2(partner<CH, NEIGHBOURS>(g[j], m, WHOLE || at[j].turned), vs[j][m]));
                 }
 #pragma unroll
                 for (int j = 0; j < NCH; ++j)
@@ -418,7 +422,7 @@ constexpr int PIECE = 16 * THREADS;                              // 16 bytes of 
 constexpr int TURN = 4;                                          // pieces of a chunk's eight pairs (cos, sin)
 constexpr int RING_BYTES = (SLOTS * 4 + 2 * TURN) * PIECE;
 
-template <bool NEIGHBOURS>
+template <bool NEIGHBOURS, bool WHOLE>
 __global__ void __launch_bounds__(THREADS, AHEAD_BLOCKS) head_norm_grad_ahead_kernel(const HeadNormArgs p, const Work wk) {
     using T = __nv_bfloat16;
     constexpr int CH = 8;
@@ -534,7 +538,7 @@ __global__ void __launch_bounds__(THREADS, AHEAD_BLOCKS) head_norm_grad_ahead_ke
             uint64_t g[1][CH];
             ry.take(g);
 #pragma unroll
-            for (int m = 0; m < CH; ++m) dz[m] = mad2(g[0][m], vc[m], mul2(partner<CH, NEIGHBOURS>(g[0], m), vs[m]));
+            for (int m = 0; m < CH; ++m) dz[m] = mad2(g[0][m], vc[m], mul2(partner<CH, NEIGHBOURS>(g[0], m, WHOLE || at.turned), vs[m]));
         }
 #pragma unroll
         for (int m = 0; m < CH; ++m) {
@@ -630,7 +634,7 @@ int chunk_of(const HeadNormArgs& p, int64_t size, bool grad) {
     return 1;
 }
 
-template <typename T, int CH, int NCH, int DEPTH, bool NEIGHBOURS>
+template <typename T, int CH, int NCH, int DEPTH, bool NEIGHBOURS, bool WHOLE>
 cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int num_sms, cudaStream_t s, uint64_t* launches) {
     Work wk = {};
     wk.chunks = (p.dim / 2 + CH - 1) / CH;
@@ -663,9 +667,9 @@ cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int nu
         if (grid * rows > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
         wk.rows = rows;
         const dim3 blocks((unsigned)(grid * rows));
-        if (!grad) e = launch_pdl(head_norm_kernel<T, CH, NCH, DEPTH, NEIGHBOURS>, blocks, dim3(THREADS), 0, s, p, wk);
-        else if constexpr (ahead) e = launch_pdl(head_norm_grad_ahead_kernel<NEIGHBOURS>, blocks, dim3(THREADS), (size_t)RING_BYTES, s, p, wk);
-        else e = launch_pdl(head_norm_grad_kernel<T, CH, NCH, DEPTH, NEIGHBOURS>, blocks, dim3(THREADS), (size_t)per_block * p.dim * 4, s, p, wk);
+        if (!grad) e = launch_pdl(head_norm_kernel<T, CH, NCH, DEPTH, NEIGHBOURS, WHOLE>, blocks, dim3(THREADS), 0, s, p, wk);
+        else if constexpr (ahead) e = launch_pdl(head_norm_grad_ahead_kernel<NEIGHBOURS, WHOLE>, blocks, dim3(THREADS), (size_t)RING_BYTES, s, p, wk);
+        else e = launch_pdl(head_norm_grad_kernel<T, CH, NCH, DEPTH, NEIGHBOURS, WHOLE>, blocks, dim3(THREADS), (size_t)per_block * p.dim * 4, s, p, wk);
         if (e != cudaSuccess) return e;
         ++*launches;
     }
@@ -679,8 +683,9 @@ cudaError_t launch_form(const HeadNormArgs& p, bool grad, float* partial, int nu
 
 template <typename T, int CH, int NCH, int DEPTH>
 cudaError_t launch_pairs(const HeadNormArgs& p, bool grad, float* partial, int num_sms, cudaStream_t s, uint64_t* launches) {
-    return p.neighbours ? launch_form<T, CH, NCH, DEPTH, true>(p, grad, partial, num_sms, s, launches)
-                        : launch_form<T, CH, NCH, DEPTH, false>(p, grad, partial, num_sms, s, launches);
+    auto form = p.rotated == p.dim ? p.neighbours ? launch_form<T, CH, NCH, DEPTH, true, true> : launch_form<T, CH, NCH, DEPTH, false, true>
+                                   : p.neighbours ? launch_form<T, CH, NCH, DEPTH, true, false> : launch_form<T, CH, NCH, DEPTH, false, false>;
+    return form(p, grad, partial, num_sms, s, launches);
 }
 
 // Chunks of 16 bytes go with one or two per thread (half a row is at most 256 values); shorter ones with more, so that a row still fits a warp.
