@@ -240,6 +240,7 @@ __global__ void __launch_bounds__(THREADS) head_norm_kernel(const HeadNormArgs p
         for (int m = 0; m < CH; ++m) {
             vc[j][m] = mul2(pw[m], two_of(c[2 * m], c[2 * m + 1]));
             vs[j][m] = mul2(partner<CH, NEIGHBOURS>(pw, m, WHOLE || at[j].turned), two_of(s[2 * m], s[2 * m + 1]));
+            if (pos < 0) vc[j][m] = vs[j][m] = 0ull;                 // (padding: zero whatever the weights are)
         }
     }
     const float inv_dim = 1.f / (float)p.dim;
@@ -379,6 +380,9 @@ __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormA
                         dw[j][m] = mad2(rz, v[j][m], dw[j][m]);
                         u[m] = mad2(v[j][m], back, mul2(rz, w[j][m]));
                     }
+                    if (pos < 0)                // (zero whatever the weights are)
+#pragma unroll
+                        for (int m = 0; m < CH; ++m) u[m] = 0ull;
                     if (mine[j]) store_pairs<T, CH>(dx, at[j], u);
                 }
                 dx += h.y_head;
@@ -563,6 +567,9 @@ __global__ void __launch_bounds__(THREADS, AHEAD_BLOCKS) head_norm_grad_ahead_ke
             dw[m] = mad2(rz, v[0][m], dw[m]);
             u[m] = mad2(v[0][m], back, mul2(rz, w[m]));
         }
+        if (pos < 0)                                             // (zero whatever the weights are)
+#pragma unroll
+            for (int m = 0; m < CH; ++m) u[m] = 0ull;
         if (mine && t - step < p.tokens) store_pairs<T, CH>(dx, at, u);
         dx += h.y_head;
         if (++head == len) head = 0;

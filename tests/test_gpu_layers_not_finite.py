@@ -101,3 +101,24 @@ def roll(t, rot, pairs):
     a = t[..., :rot]
     p = a.roll(rot // 2, -1) if pairs == "halves" else a.unflatten(-1, (rot // 2, 2)).flip(-1).flatten(-2)
     return torch.cat((p, t[..., rot:]), -1)
+
+
+@pytest.mark.parametrize("pairs", ["halves", "neighbours"])
+@pytest.mark.parametrize("ty,d,rot", FORMS)
+def test_padding_is_zero_whatever_the_weights_are(ops, ty, d, rot, pairs):
+    import torch
+    from paper_2609_23898_b200 import layers
+    dtype = torch.float32 if ty == "f32" else torch.bfloat16
+    x, dy = (torch.randn(60, 3, d, device="cuda").to(dtype) for _ in range(2))
+    table = layers.rotation_table(ops, 60, rot) if rot else None
+    pos = torch.arange(60, device="cuda")
+    pos[::3] = -1
+    for value in (float("inf"), float("-inf"), float("nan")):
+        for where in (slice(None), slice(1, 2), slice(d - 1, d)):
+            w = torch.ones(d, device="cuda")
+            w[where] = value
+            y, _ = layers.head_norm(ops, x, None, w, None, table, pos, pairs=pairs)
+            dw = torch.zeros(d, device="cuda")
+            dx, _ = layers.head_norm_backward(ops, dy, None, x, None, w, None, table, pos, dwq=dw, pairs=pairs)
+            assert not bool(y[::3].any()) and not bool(dx[::3].any()) and bool(torch.isfinite(dw).all())
+            assert not bool(torch.isfinite(y[1::3]).all()) and not bool(torch.isfinite(dx[1::3]).any())
