@@ -160,14 +160,18 @@ template <> struct Act<CERAR_ACT_GELU> {
     }
 };
 template <> struct Act<CERAR_ACT_GELU_TANH> {          // g / (1 + e^-2v) with v = sqrt(2 / pi) (g + 0.044715 g^3): (1 + tanh v) / 2 is that quotient
+    static constexpr float FAR_OUT = 1e6f;             // of g^2: |v| is above 10^7 there
     static __device__ __forceinline__ uint64_t part(uint64_t g, uint64_t gg) {
         return rcp_2(add2(exp2_2(mul2(mul2(g, all(-1.5957691f * LOG2E)), mad2(gg, all(0.044715f), all(1.f)))), all(1.f)));
     }
     static __device__ __forceinline__ uint64_t value(uint64_t g) { return mul2(g, part(g, mul2(g, g))); }
     static __device__ __forceinline__ void both(uint64_t g, uint64_t& a, uint64_t& d) {
-        const uint64_t gg = mul2(g, g), s = part(g, gg);
+        // Far out s is 0 or 1 and the derivative too: g s (1 - s), which is zero there, has a finite factor as long as the square is finite
+        // (g may be up to the end of the range).
+        float x, y;
+        parts(mul2(g, g), x, y);
+        const uint64_t gg = two_of(fminf(x, FAR_OUT), fminf(y, FAR_OUT)), s = part(g, gg);
         a = mul2(g, s);
-        // (far out 1 - s or s is 0 and the cubic may be anything: the product is then kept at 0 by ordering it last)
         const uint64_t rest = mul2(a, mad2(s, all(-1.f), all(1.f)));
         d = mad2(rest, mad2(gg, all(1.5957691f * 0.134145f), all(1.5957691f)), s);
     }

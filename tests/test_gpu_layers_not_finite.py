@@ -122,3 +122,24 @@ def test_padding_is_zero_whatever_the_weights_are(ops, ty, d, rot, pairs):
             dx, _ = layers.head_norm_backward(ops, dy, None, x, None, w, None, table, pos, dwq=dw, pairs=pairs)
             assert not bool(y[::3].any()) and not bool(dx[::3].any()) and bool(torch.isfinite(dw).all())
             assert not bool(torch.isfinite(y[1::3]).all()) and not bool(torch.isfinite(dx[1::3]).any())
+
+
+@pytest.mark.parametrize("outputs", [1, 8192])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+def test_activations_far_out(ops, act, outputs):
+    """Beyond 10^4 every activation is g or 0 and its derivative 1 or 0, up to the ends of the range: one token, one input, one hidden value with u = 1, dh = 1."""
+    import torch
+    from paper_2609_23898_b200 import layers
+    one = torch.ones(1, 1, device="cuda").bfloat16()
+    w_out = torch.ones(outputs, 1, device="cuda").bfloat16()
+    dy = torch.zeros(1, outputs, device="cuda").bfloat16()
+    dy[0, outputs // 2] = 1
+    for size in (1e4, 1e10, 1e19, 3e19, 1e20, 3e38):
+        for sign in (1, -1):
+            w_in = torch.tensor([[sign * size], [1.0]], device="cuda").bfloat16()
+            y, kept = layers.gated(ops, one, w_in, w_out, activation=act, keep=True)
+            dw_in, dw_out = torch.zeros(2, 1, device="cuda"), torch.zeros(outputs, 1, device="cuda")
+            layers.gated_backward(ops, dy, kept, w_in, w_out, dw_in, dw_out)
+            g = float(w_in[0, 0]) if sign > 0 else 0.0
+            assert bool((y == g).all()) and float(dw_in[0, 0]) == (1.0 if sign > 0 else 0.0) and float(dw_in[1, 0]) == g, (size, sign, dw_in)
+            assert float(dw_out[outputs // 2, 0]) == g
