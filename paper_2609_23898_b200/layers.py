@@ -345,6 +345,23 @@ def _operands(ops: Ops, *given):
     return out
 
 
+def _meet(p, rows, width, pitch, q, rows2, cols2, ld2) -> bool:
+    """Whether two matrices share a byte: address, rows, bytes of a row, bytes between rows; the second one, of bfloat16, with its columns and elements between rows."""
+    width2, pitch2 = 2 * cols2, 2 * ld2
+    if q + (rows2 - 1) * pitch2 + width2 <= p or p + (rows - 1) * pitch + width <= q or not (rows and width and rows2 and width2):
+        return False
+    if rows == 1:
+        pitch = pitch2
+    elif rows2 == 1:
+        pitch2 = pitch
+    if pitch == pitch2:      # two rows lie apart as the first one does from some row of a longer matrix
+        starts, q, rows2 = (p,), q - (rows - 1) * pitch, rows + rows2 - 1
+    else:
+        starts = range(p, p + rows * pitch, pitch)
+    # for each row: the numbers of the other matrix's rows that end behind its start, and that start in front of its end
+    return any(max(0, (at - width2 - q) // pitch2 + 1) <= min(rows2 - 1, (at + width - 1 - q) // pitch2) for at in starts)
+
+
 def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b=False, out: torch.Tensor | None = None,
            dtype: torch.dtype = torch.bfloat16, accumulate=False) -> torch.Tensor:
     """op(a) op(b) of bfloat16 matrices, into `out` (float32 or bfloat16, over neither of them) if given, added to it with accumulate."""
@@ -354,7 +371,8 @@ def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b
     k2, n = (b.size(1), b.size(0)) if trans_b else b.shape
     if k != k2:
         raise ValueError("the summed dimensions of a and b differ")
-    if out is None:
+    fresh = out is None
+    if fresh:
         if accumulate:
             raise ValueError("accumulate wants an `out` to add to")
         out = torch.empty(m, n, dtype=dtype, device=a.device)
@@ -363,11 +381,13 @@ def matmul(ops: Ops, a: torch.Tensor, b: torch.Tensor, *, trans_a=False, trans_b
         if tuple(out.shape) != (m, n):
             raise ValueError(f"out of shape {(m, n)} wanted, got {tuple(out.shape)}")
     (a, pa, lda), (b, pb, ldb) = _operands(ops, a, b)
-    pc = out.data_ptr()
-    if pc and (pc == pa or pc == pb):
-        raise ValueError("out lies over a or b")
-    st = lib.cerar_matmul_bf16(ops._h, pa, lda, trans_a, pb, ldb, trans_b, m, n, k, pc, _kind(out, "out"), _stride(out), accumulate,
-                               _raw(ops._index))
+    pc, ldc = out.data_ptr(), _stride(out)
+    if not fresh:
+        size = out.element_size()
+        end = pc + m * ldc * size                    # (where the ranges lie apart there is no more to do)
+        if (pa < end and _meet(pc, m, n * size, ldc * size, pa, *a.shape, lda)) or (pb < end and _meet(pc, m, n * size, ldc * size, pb, *b.shape, ldb)):
+            raise ValueError("out lies over a or b")
+    st = lib.cerar_matmul_bf16(ops._h, pa, lda, trans_a, pb, ldb, trans_b, m, n, k, pc, _kind(out, "out"), ldc, accumulate, _raw(ops._index))
     if st:
         _check(st)
     return out
