@@ -464,11 +464,12 @@ class Gated(torch.autograd.Function):
     def apply(cls, x, w_in, w_out, ops, dw_in, dw_out, activation="silu"):
         _no_gradient(w_in=w_in, w_out=w_out)
         wanted = dw_in is not None or dw_out is not None
-        return super().apply(x, w_in, w_out, ops, dw_in, dw_out, activation, _anchor(x.device, wanted and not x.requires_grad))
+        # (forward does not see the caller's mode: under no_grad needs_input_grad still says what x requires)
+        keep = torch.is_grad_enabled() and (wanted or x.requires_grad)
+        return super().apply(x, w_in, w_out, ops, dw_in, dw_out, activation, _anchor(x.device, wanted and not x.requires_grad), keep)
 
     @staticmethod
-    def forward(ctx, x, w_in, w_out, ops, dw_in, dw_out, activation, anchor):
-        keep = ctx.needs_input_grad[0] or anchor is not None
+    def forward(ctx, x, w_in, w_out, ops, dw_in, dw_out, activation, anchor, keep):
         if not keep:
             return gated(ops, x, w_in, w_out, activation=activation)
         y, kept = gated(ops, x, w_in, w_out, activation=activation, keep=True)
@@ -481,4 +482,4 @@ class Gated(torch.autograd.Function):
     def backward(ctx, dy):
         *kept, w_in, w_out = _saved(ctx)
         dx = gated_backward(ctx.ops, dy, (*kept, ctx.activation), w_in, w_out, *ctx.dw, need_dx=ctx.needs_input_grad[0])
-        return (dx,) + (None,) * 7
+        return (dx,) + (None,) * 8
