@@ -56,3 +56,51 @@ def test_dx_over_dy(ops, t, d, f, o):
     for _, _, _, over, got, dx, dw in runs:
         assert torch.equal(over, dx) and torch.equal(got[0], dw[0]) and torch.equal(got[1], dw[1])
     ops.status()
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("wanted", [(1, 1, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1)])
+@pytest.mark.parametrize("t,d,f,o", SIZES)
+def test_every_choice_of_results_without_a_pause(ops, t, d, f, o, wanted, captured):
+    """Passes one behind the other in the same memory, with some of dw_out, dx and dw_in wanted: the bits of a pass alone with all of them."""
+    import torch
+    from paper_2609_23898_b200 import layers
+    cases = [weights(t, d, f, o, s) for s in range(6)]
+
+    def run(case, wanted):
+        x, w_in, w_out, dy = case
+        _, kept = layers.gated(ops, x, w_in, w_out, keep=True)
+        dw_in, dw_out = (torch.ones_like(w, dtype=torch.float32) if want else None for w, want in ((w_in, wanted[2]), (w_out, wanted[0])))
+        return dw_out, layers.gated_backward(ops, dy, kept, w_in, w_out, dw_in, dw_out, need_dx=bool(wanted[1])), dw_in
+
+    want = []
+    for case in cases:
+        want.append(run(case, (1, 1, 1)))
+        torch.cuda.synchronize()
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = [run(case, wanted) for case in cases]
+        for _ in range(2):
+            graph.replay()
+    else:
+        got = [run(case, wanted) for case in cases]
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        for p, q, w in zip(a, b, wanted):
+            assert (p is None) == (not w) and (p is None or torch.equal(p, q))
+    ops.status()
+
+
+def test_one_and_several_turns_are_tested():
+    """Of every product's tiles, on 148 SMs."""
+    from paper_2609_23898_b200 import cerar
+
+    def turns(m, n, k):
+        split = C.c_int()
+        form = cerar.lib.cerar_matmul_bf16_tile(m, n, k, 148, C.byref(split))
+        rows, cols, blocks = ((256, 256, 2), (256, 128, 2), (128, 128, 1))[form]
+        return -(-m // rows) * -(-n // cols) * split.value * blocks > 148
+
+    for product in (lambda t, d, f, o: (o, f, t), lambda t, d, f, o: (t, d, 2 * f), lambda t, d, f, o: (2 * f, d, t)):
+        assert {turns(*product(*s)) for s in SIZES} == {True, False}

@@ -1,6 +1,7 @@
-"""Which of the gated block's gradient products begin beside the one in front (`after`) and let the one behind begin (`followed`), without a device: where results lie
-over what another product reads or writes."""
+"""Which of the gated block's gradient products begin beside the one in front (`after`) and let the one behind begin (`followed`), without a device: for every
+choice of results, for empty sums, and where results lie over what another product reads or writes."""
 import ctypes as C
+import itertools
 import os
 import shutil
 import subprocess
@@ -57,6 +58,23 @@ def products(fake):
 def sound(flags):
     """The first one waits for the gate's gradient; one that begins early stands behind one that lets it."""
     return all(not after if i == 0 else not after or flags[i - 1][1] for i, (after, _) in enumerate(flags))
+
+
+CHOICES = [c for n in range(4) for c in itertools.combinations(("dw_out", "dx", "dw_in"), n)]
+
+
+@pytest.mark.parametrize("wanted", CHOICES, ids=str)
+def test_every_choice_of_results(products, wanted):
+    absent = {name: None for name in ("dw_out", "dx", "dw_in") if name not in wanted}
+    n = len(wanted)
+    full = [(int(i > 0), int(i + 1 < n)) for i in range(n)]
+    assert products(**absent) == full
+    assert products(**absent, x=FAR + 2, w_in=2 * FAR + 2, dy=5 * FAR + 2, lddy=33) == full              # operands that are copied
+    flags = products(**absent, width=0)                                                                  # no inputs: dw_out alone
+    assert len(flags) == int("dw_out" in wanted) and sound(flags)
+    if "dx" not in wanted:                                                                               # empty sums, nothing added: no products
+        for sizes in (dict(tokens=0), dict(hidden=0), dict(outputs=0)):
+            assert products(**absent, **sizes, accumulate=1) == []
 
 
 DY = 10 * 32 * 2             # bytes of dy
