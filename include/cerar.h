@@ -598,7 +598,7 @@ cerar_status_t cerar_adamw_step(cerar_tensors_t* set, const cerar_adamw_options_
  * The rest of a model's weights: embedding rows, norm weights of heads, gated feed-forward blocks.  The same rules as above; the
  * gradients of weights are written, or added (accumulate != 0), where the caller wants them, e.g. into the aggregated vector.  Calls
  * that take a workspace want cerar_..._workspace bytes of device memory, 16-byte aligned; calls that may run at the same time,
- * replayed graphs included, want one each. */
+ * replayed graphs included, want one each.  Results overlap neither one another nor what a call reads, but where it says that they may. */
 
 /* Lookup: y[t] = scale table[ids[t]], product in binary32, one rounding to y_type.  table: vocab x width of `type`, ld elements between
  * rows; y: tokens x width, ldy between rows.  ids: tokens integers of id_bytes (4 or 8) bytes.  An id below zero is padding: its row

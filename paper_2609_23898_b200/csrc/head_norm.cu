@@ -411,9 +411,9 @@ __global__ void __launch_bounds__(THREADS) head_norm_grad_kernel(const HeadNormA
 
 // The same for bfloat16 in whole 16-byte chunks, one to a thread's half.  Rows, and a token's part of the table, are on their way in shared memory, in
 // slots of the thread's own (nothing has to be waited for but its own copies): AHEAD heads of the block's sequence of tokens and heads, over the
-// ends of tokens, and no register holds them.  16384 x 40 x 128 in a loop 87 us, 5.9 TB/s; 94 with a cold L2 (two heads of one token ahead in registers, and the table's latency
-// at each token: 102; one or three heads here 99 and 86, 4096 x 20 x 256 with one to three 35, 32, 33; four blocks per SM in one turn, eight in
-// two: 90).  Copies go through L1, or the halves of a 32-byte piece come from L2 twice (neighbours: 144).  binary32 has twice the bytes per
+// ends of tokens, and no register holds them.  16384 x 40 x 128 in a loop 87 us, 5.9 TB/s, and 95 with L2 flushed before each pass (two heads of one token ahead
+// in registers, and the table's latency at each token: 104 and 112; in a loop one or three heads here 99 and 86, 4096 x 20 x 256 with one to
+// three 35, 32, 33; four blocks per SM in one turn, eight in two: 90).  Copies go through L1, or the halves of a 32-byte piece come from L2 twice (neighbours: 144).  binary32 has twice the bytes per
 // instruction and is slower this way (168 -> 196).
 constexpr int AHEAD = 2, SLOTS = AHEAD + 1, AHEAD_BLOCKS = 4;
 __device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
