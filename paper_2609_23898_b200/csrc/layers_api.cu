@@ -173,7 +173,7 @@ struct Span {
 };
 Span span_of(const void* p, int64_t rows, int64_t cols, int64_t ld, int size) {
     const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-    return {at, at + (uintptr_t)(((rows - 1) * ld + cols) * size)};
+    return {at, at + ((uintptr_t)(rows - 1) * (uintptr_t)ld + (uintptr_t)cols) * (uintptr_t)size};      // (ld up to 2^40: no signed overflow)
 }
 Span span_of(const Mat& m, int64_t rows, int64_t cols) { return span_of(m.p, rows, cols, m.ld, 2); }
 // Products that run beside one another: since the last one that waited, what each writes and what it reads.
